@@ -304,6 +304,120 @@ int chela_linattn_step(const void *q, const void *k, const void *v, float *S, vo
 int chela_linattn_step_gated(const void *q, const void *k, const void *v, const void *g, float *S, void *y, float eps,
                              int B, int H, int dk, int dv, void *stream);
 
+/* ---- operators on rows: a token's channels next to each other, as a projection leaves them ------------------------
+ * Three operators of a selective state space block, the other linear-time token mixer: its short causal convolution, its
+ * scan, and the norms around a block.  Common to the first two:
+ *   rows     : [T, D] tensors of T tokens, bf16 (plain name) or fp32 (_f32); arithmetic and sums are fp32 for either, outputs are
+ *              rounded once.  A tensor that comes with a row stride (ld..., elements from a token to the next, at least the
+ *              row's width) may be a slice of a wider one and needs only its elements' alignment; all others are contiguous
+ *              and 16-byte aligned.
+ *   sequences: the T rows belong to n_seq sequences, one after the other.  cu NULL: of T / n_seq rows each.  Otherwise cu is
+ *              n_seq + 1 ascending int32 offsets on the device, sequence s has rows cu[s] .. cu[s+1] - 1, none is an empty
+ *              sequence; rows in front of cu[0] and from cu[n_seq] on belong to nobody: they are not computed, and what the
+ *              outputs hold there stays.  (Offsets outside [0, T] or not ascending give unspecified values in the outputs, nothing else.)
+ *   states   : what a sequence takes from the tokens in front of it (S_in, NULL: none) and hands to those behind it (S_out, NULL:
+ *              not wanted).  slots NULL: sequence s has the s-th of n_slots = n_seq states.  Otherwise slots is n_seq int32
+ *              on the device, sequence s has state slots[s] of a pool of n_slots; a sequence whose slot is not in [0, n_slots)
+ *              begins with nothing and leaves nothing, and in the single-token calls its output row is left as it is.  Two
+ *              sequences of one call must not share a slot (their states would be unspecified).  S_out may be S_in (exactly
+ *              the same pointer); states of slots that no sequence has are not touched.  An empty sequence hands its state on.
+ * Limits: T < 2^31 - 4096; n_seq, R < 2^24; D <= 2^20; T D, n_seq D and R D below 2^37.  With T = 0 nothing is done but
+ * that states pass through and gradients of parameters are zeroed.  Everything else (streams, scratch, threads, errors) as for the
+ * calls above; scratch: the _workspace_bytes queries (0 for invalid arguments).
+ *
+ * Short causal convolution, one kernel of m taps per channel (1 <= m <= 8), lag 0 first:
+ *     u_t = bias + sum_{j<m} w[j] x_{t-j},   y_t = silu != 0 ? u_t / (1 + exp(-u_t)) : u_t.
+ *   w [D, m] fp32; bias [D] fp32 or NULL; states [n_slots, m-1, D] in the I/O type: the last m - 1 inputs, the latest last (with
+ *   m = 1 there are none and the pointers are not looked at).
+ *   bwd : dX [T, D], dw [D, m] and dbias [D] fp32 (dbias NULL without a bias), dS_in [n_seq, m-1, D] (NULL: not wanted) for the
+ *         upstream gradients dY [T, D] and dS_out [n_seq, m-1, D] (NULL: zero).  Nothing is saved by the forward call.  Sums over
+ *         rows are taken in a fixed order.
+ *   step: one row for each of R requests, x [R, D]: y as above, and S [n_slots, m-1, D] moved on by the row, in place. */
+int chela_short_conv_fwd(const void *X, long long ldx, const float *w, int m, const float *bias, int silu, const int *cu,
+                         int n_seq, int T, int D, const void *S_in, void *S_out, const int *slots, int n_slots, void *Y,
+                         void *stream);
+int chela_short_conv_fwd_f32(const void *X, long long ldx, const float *w, int m, const float *bias, int silu, const int *cu,
+                             int n_seq, int T, int D, const void *S_in, void *S_out, const int *slots, int n_slots, void *Y,
+                             void *stream);
+int chela_short_conv_bwd(const void *X, long long ldx, const float *w, int m, const float *bias, int silu, const int *cu,
+                         int n_seq, int T, int D, const void *S_in, const void *dY, long long lddy, const void *dS_out,
+                         void *dX, float *dw, float *dbias, void *dS_in, void *stream);
+int chela_short_conv_bwd_f32(const void *X, long long ldx, const float *w, int m, const float *bias, int silu, const int *cu,
+                             int n_seq, int T, int D, const void *S_in, const void *dY, long long lddy, const void *dS_out,
+                             void *dX, float *dw, float *dbias, void *dS_in, void *stream);
+int chela_short_conv_step(const void *x, long long ldx, const float *w, int m, const float *bias, int silu, void *S,
+                          const int *slots, int n_slots, int R, int D, void *y, void *stream);
+int chela_short_conv_step_f32(const void *x, long long ldx, const float *w, int m, const float *bias, int silu, void *S,
+                              const int *slots, int n_slots, int R, int D, void *y, void *stream);
+size_t chela_short_conv_bwd_workspace_bytes(int T, int D, int m, int dtype);
+
+/* Selective scan: a state of N values per channel (N in {8, 16, 32}), whose decay, input and output maps depend on the token.
+ * With dl_t = softplus != 0 ? log(1 + exp(delta_t + bias)) : delta_t + bias, per channel c of group g = c / (D / G):
+ *     h_t[n] = exp(dl_t A[n]) h_{t-1}[n] + dl_t u_t B_t[g,n],   y_t = sum_n C_t[g,n] h_t[n] + Dskip u_t,
+ *     out_t = Z ? y_t z_t / (1 + exp(-z_t)) : y_t.
+ *   U, delta, Z (or NULL) [T, D]; Bm, Cm [T, G, N], G divides D; A [N, D], Dskip [D] (or NULL), delta_bias [D] (or NULL) fp32;
+ *   states [n_slots, N, D] fp32.  The decay is formed as 2^(dl A log2 e); nothing is assumed of A's sign.
+ *   fwd  : Y [T, D].  saved: NULL, or a caller-owned buffer of chela_selscan_saved_bytes() bytes (16-byte aligned, opaque) that carries
+ *          the states in front of every 16th row to the backward call.
+ *   bwd  : gradients dU, ddelta, dZ (NULL without Z) [T, D], dB, dC [T, G, N] in the I/O type, dA [N, D], dDskip, ddelta_bias [D] (each
+ *          NULL without its input) fp32, dS_in [n_seq, N, D] fp32 (NULL: not wanted), for the upstream dY [T, D] and dS_out
+ *          [n_seq, N, D] fp32 (NULL: zero).  saved: as the forward call with the same inputs left it, or NULL: the states are worked
+ *          out again.  Sums over rows and channels are taken in a fixed order.
+ *   step : one row for each of R requests; S [n_slots, N, D] is updated in place. */
+int chela_selscan_fwd(const void *U, long long ldu, const void *delta, long long ldd, const float *A, const void *Bm, long long ldb,
+                      const void *Cm, long long ldc, const float *Dskip, const void *Z, long long ldz, const float *delta_bias,
+                      int softplus, const int *cu, int n_seq, int T, int D, int N, int G, const float *S_in, float *S_out,
+                      const int *slots, int n_slots, void *Y, void *saved, void *stream);
+int chela_selscan_fwd_f32(const void *U, long long ldu, const void *delta, long long ldd, const float *A, const void *Bm,
+                          long long ldb, const void *Cm, long long ldc, const float *Dskip, const void *Z, long long ldz,
+                          const float *delta_bias, int softplus, const int *cu, int n_seq, int T, int D, int N, int G,
+                          const float *S_in, float *S_out, const int *slots, int n_slots, void *Y, void *saved, void *stream);
+int chela_selscan_bwd(const void *U, long long ldu, const void *delta, long long ldd, const float *A, const void *Bm, long long ldb,
+                      const void *Cm, long long ldc, const float *Dskip, const void *Z, long long ldz, const float *delta_bias,
+                      int softplus, const int *cu, int n_seq, int T, int D, int N, int G, const float *S_in, const void *dY,
+                      long long lddy, const float *dS_out, const void *saved, void *dU, void *ddelta, float *dA, void *dB, void *dC,
+                      float *dDskip, void *dZ, float *ddelta_bias, float *dS_in, void *stream);
+int chela_selscan_bwd_f32(const void *U, long long ldu, const void *delta, long long ldd, const float *A, const void *Bm,
+                          long long ldb, const void *Cm, long long ldc, const float *Dskip, const void *Z, long long ldz,
+                          const float *delta_bias, int softplus, const int *cu, int n_seq, int T, int D, int N, int G,
+                          const float *S_in, const void *dY, long long lddy, const float *dS_out, const void *saved, void *dU,
+                          void *ddelta, float *dA, void *dB, void *dC, float *dDskip, void *dZ, float *ddelta_bias, float *dS_in,
+                          void *stream);
+int chela_selscan_step(const void *u, long long ldu, const void *delta, long long ldd, const float *A, const void *Bm, long long ldb,
+                       const void *Cm, long long ldc, const float *Dskip, const void *z, long long ldz, const float *delta_bias,
+                       int softplus, float *S, const int *slots, int n_slots, int R, int D, int N, int G, void *y, void *stream);
+int chela_selscan_step_f32(const void *u, long long ldu, const void *delta, long long ldd, const float *A, const void *Bm,
+                           long long ldb, const void *Cm, long long ldc, const float *Dskip, const void *z, long long ldz,
+                           const float *delta_bias, int softplus, float *S, const int *slots, int n_slots, int R, int D, int N,
+                           int G, void *y, void *stream);
+size_t chela_selscan_saved_bytes(int T, int D, int N);
+/* is_bwd: of the backward call; has_saved: given `saved`. */
+size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int has_saved);
+
+/* Norms before and after a block, with its gate and the residual, in one pass over `rows` contiguous rows of D features
+ * (1 <= D <= 8192):
+ *     X_out = X + scale * Norm(Y) * w_post * gate      (w_post NULL: scale * Y * gate; gate NULL: 1)
+ *     Nrm   = Norm(X_out) * w_pre                       (w_pre NULL: not wanted, Nrm is not looked at)
+ * with Norm(x) = x / sqrt(mean_j x_j^2 + eps) as defined above, over the row; eps >= 0 and scale are finite constants.  Y is the
+ * block's output, X the residual stream, Nrm the next block's input.  Y NULL (in front of the first block; gate, w_post and X_out are
+ * then not looked at): Nrm = Norm(X) * w_pre.  The second norm takes X_out before it is rounded.
+ *   Y, gate, Nrm: bf16 (plain name) or fp32 (_f32); X, X_out: the same, or fp32 beside bf16 (x_f32 != 0).  w_post, w_pre [D] fp32.
+ *   X_out may be X (exactly the same pointer).
+ *   bwd: from Y, gate and X, the stream as the forward call left it (its X_out; with Y NULL its X), for the upstream gradients dX_out (type
+ *   of X; NULL: zero) and dN (only with w_pre): dY, dgate, dX (type of X; may be dX_out, exactly the same pointer), dw_post and dw_pre [D] fp32,
+ *   each only where there is its input.  Sums over rows are taken in a fixed order.  rows = 0: dw_post and dw_pre are zeroed. */
+int chela_block_norm_fwd(const void *Y, const void *gate, const void *X, const float *w_post, const float *w_pre, void *X_out,
+                         void *Nrm, float scale, float eps, long long rows, int D, int x_f32, void *stream);
+int chela_block_norm_fwd_f32(const void *Y, const void *gate, const void *X, const float *w_post, const float *w_pre, void *X_out,
+                             void *Nrm, float scale, float eps, long long rows, int D, int x_f32, void *stream);
+int chela_block_norm_bwd(const void *Y, const void *gate, const void *X, const float *w_post, const float *w_pre,
+                         const void *dX_out, const void *dN, void *dY, void *dgate, void *dX, float *dw_post, float *dw_pre,
+                         float scale, float eps, long long rows, int D, int x_f32, void *stream);
+int chela_block_norm_bwd_f32(const void *Y, const void *gate, const void *X, const float *w_post, const float *w_pre,
+                             const void *dX_out, const void *dN, void *dY, void *dgate, void *dX, float *dw_post, float *dw_pre,
+                             float scale, float eps, long long rows, int D, int x_f32, void *stream);
+size_t chela_block_norm_bwd_workspace_bytes(long long rows, int D);
+
 /* Bytes of device scratch one call with these arguments needs, with or without
  * carried states (0 if the arguments are invalid; the training pair has its own query,
  * chela_linattn_train_workspace_bytes).  The size is B*H*dk*dv*4 bytes per segment, twice that for

@@ -121,6 +121,28 @@ def lib() -> ctypes.CDLL:
         f.restype = i
     L.chela_shortlong_conv_bwd_workspace_bytes.argtypes = [i, i, i, i, i]
     L.chela_shortlong_conv_bwd_workspace_bytes.restype = sz
+    ll = ctypes.c_longlong
+    conv = [vp, ll, vp, i, vp, i]                                    # X, ldx, w, m, bias, silu
+    scan = [vp, ll, vp, ll, vp, vp, ll, vp, ll, vp, vp, ll, vp, i]   # U, delta, A, Bm, Cm, Dskip, Z, delta_bias, softplus
+    for sfx in ("", "_f32"):
+        for name, args in (("chela_short_conv_fwd", conv + [vp, i, i, i, vp, vp, vp, i, vp, vp]),
+                           ("chela_short_conv_bwd", conv + [vp, i, i, i, vp, vp, ll, vp, vp, vp, vp, vp, vp]),
+                           ("chela_short_conv_step", conv + [vp, vp, i, i, i, vp, vp]),
+                           ("chela_selscan_fwd", scan + [vp, i, i, i, i, i, vp, vp, vp, i, vp, vp, vp]),
+                           ("chela_selscan_bwd", scan + [vp, i, i, i, i, i, vp, vp, ll] + [vp] * 12),
+                           ("chela_selscan_step", scan + [vp, vp, i, i, i, i, i, vp, vp]),
+                           ("chela_block_norm_fwd", [vp] * 7 + [f32, f32, ll, i, i, vp]),
+                           ("chela_block_norm_bwd", [vp] * 12 + [f32, f32, ll, i, i, vp])):
+            f = getattr(L, name + sfx)
+            f.argtypes = args
+            f.restype = i
+    L.chela_short_conv_bwd_workspace_bytes.argtypes = [i, i, i, i]
+    L.chela_selscan_saved_bytes.argtypes = [i, i, i]
+    L.chela_selscan_workspace_bytes.argtypes = [i] * 6
+    L.chela_block_norm_bwd_workspace_bytes.argtypes = [ll, i]
+    for name in ("chela_short_conv_bwd", "chela_selscan", "chela_block_norm_bwd"):
+        getattr(L, name + "_workspace_bytes").restype = sz
+    L.chela_selscan_saved_bytes.restype = sz
     L.chela_linattn_step.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, vp]
     L.chela_linattn_step.restype = i
     L.chela_linattn_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
@@ -760,6 +782,292 @@ def chela_linattn_step_gated(q, k, v, g, S, eps, y=None, stream=None):
                                               _state_ptr(S, B, H, dk, dv, "S"), y.data_ptr(), float(eps), B, H, dk, dv,
                                               _stream_ptr(stream)))
     return y
+
+
+# ---- operators on rows: X [B, L, D] (B sequences of L tokens), or [T, D] with cu, the n_seq + 1 offsets of the sequences (int32, on the
+# device; None: one sequence).  Rows may be slices of a wider tensor: the last dimension has stride 1, the rows one stride.
+
+def _row_stride(t, like, name, dtype=None):
+    """(address, elements from a row to the next) of a tensor of rows with like's leading sizes."""
+    lead = like.shape[:-1]
+    if t.dim() < 2 or t.shape[:len(lead)] != lead or t.dtype != (dtype or like.dtype) or t.device != like.device:
+        raise ValueError("%s must have the rows, the dtype and the device of the first tensor" % name)
+    width = 1
+    for k in range(t.dim() - 1, len(lead) - 1, -1):
+        if t.shape[k] > 1 and t.stride(k) != width:
+            raise ValueError("%s: the elements of a row must be next to each other" % name)
+        width *= t.shape[k]
+    ld, rows = None, 1
+    for k in range(len(lead) - 1, -1, -1):
+        if t.shape[k] > 1:
+            if ld is None:
+                ld = t.stride(k)
+            elif t.stride(k) != ld * rows:
+                raise ValueError("%s: the rows must be evenly spaced" % name)
+            rows *= t.shape[k]
+    return t.data_ptr(), max(width, 1) if ld is None else ld
+
+
+def _sequences(X, cu, name):
+    """(offsets' address, sequences, rows, width) of the first tensor of a call on rows."""
+    if not X.is_cuda or X.dim() not in (2, 3):
+        raise ValueError("%s must be a device tensor [B, L, D] or [T, D]" % name)
+    if cu is None:
+        return None, (X.shape[0] if X.dim() == 3 else 1), X.shape[:-1].numel(), X.shape[-1]
+    if X.dim() != 2:
+        raise ValueError("with cu, %s is [T, D]" % name)
+    if cu.dim() != 1 or cu.shape[0] < 1 or cu.dtype != torch.int32 or cu.device != X.device or not cu.is_contiguous():
+        raise ValueError("cu must be a contiguous int32 device tensor of the sequences' n_seq + 1 offsets")
+    return cu.data_ptr(), cu.shape[0] - 1, X.shape[0], X.shape[1]
+
+
+def _dense(t, shape, dtype, device, name):
+    """The address of a contiguous tensor of that shape, None for None."""
+    if t is None:
+        return None
+    if t.shape != torch.Size(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor %s on the same device" % (name, str(dtype).replace("torch.", ""), list(shape)))
+    return t.data_ptr()
+
+
+def _slot_map(slots, n_seq, states, device):
+    """(address, states there are) for an optional map from sequences to states."""
+    if slots is None:
+        return None, n_seq
+    if slots.shape != (n_seq,) or slots.dtype != torch.int32 or slots.device != device or not slots.is_contiguous():
+        raise ValueError("slots must be a contiguous int32 device tensor with one entry per sequence")
+    if states is None:
+        raise ValueError("slots without states")
+    return slots.data_ptr(), states.shape[0]
+
+
+def chela_short_conv_fwd(X, w, bias=None, silu=True, cu=None, S_in=None, S_out=None, slots=None, Y=None, stream=None):
+    """Y = silu(bias + sum_j w[:, j] X[t - j]) over the tokens of each sequence (silu=False: without the activation).
+    w [D, m], bias [D] float32; S_in, S_out [n_slots, m-1, D] the last inputs in front of and behind the sequences (S_out may be S_in)."""
+    pcu, n_seq, T, D = _sequences(X, cu, "X")
+    sfx, _ = _suffix(X)
+    px, ldx = _row_stride(X, X, "X")
+    if w.dim() != 2:
+        raise ValueError("w must be [D, m]")
+    m, dev = w.shape[1], X.device
+    pslots, n_slots = _slot_map(slots, n_seq, S_in if S_in is not None else S_out, dev)
+    if Y is None:
+        Y = torch.empty(X.shape, dtype=X.dtype, device=dev)
+    st = (n_slots, m - 1, D)
+    with _on(X):
+        _check(getattr(lib(), "chela_short_conv_fwd" + sfx)(
+            px, ldx, _dense(w, (D, m), torch.float32, dev, "w"), m, _dense(bias, (D,), torch.float32, dev, "bias"), int(bool(silu)), pcu,
+            n_seq, T, D, _dense(S_in, st, X.dtype, dev, "S_in"), _dense(S_out, st, X.dtype, dev, "S_out"), pslots, n_slots,
+            _dense(Y, X.shape, X.dtype, dev, "Y"), _stream_ptr(stream)))
+    return Y
+
+
+def chela_short_conv_bwd(X, w, dY, bias=None, silu=True, cu=None, S_in=None, dS_out=None, want_dS_in=False, stream=None):
+    """(dX, dw, dbias, dS_in) of chela_short_conv_fwd (without slots) for the upstream gradients dY and dS_out; dbias is None without a
+    bias, dS_in unless asked for."""
+    pcu, n_seq, T, D = _sequences(X, cu, "X")
+    sfx, _ = _suffix(X)
+    px, ldx = _row_stride(X, X, "X")
+    if dY.shape != X.shape:
+        raise ValueError("dY must match X")
+    pdy, lddy = _row_stride(dY, X, "dY")
+    if w.dim() != 2:
+        raise ValueError("w must be [D, m]")
+    m, dev = w.shape[1], X.device
+    st = (n_seq, m - 1, D)
+    pw, pb = _dense(w, (D, m), torch.float32, dev, "w"), _dense(bias, (D,), torch.float32, dev, "bias")
+    ps, pds = _dense(S_in, st, X.dtype, dev, "S_in"), _dense(dS_out, st, X.dtype, dev, "dS_out")
+    dX = torch.empty(X.shape, dtype=X.dtype, device=dev)
+    dw = torch.empty((D, m), dtype=torch.float32, device=dev)
+    dbias = torch.empty(D, dtype=torch.float32, device=dev) if bias is not None else None
+    dS_in = torch.empty(st, dtype=X.dtype, device=dev) if want_dS_in else None
+    with _on(X):
+        _check(getattr(lib(), "chela_short_conv_bwd" + sfx)(
+            px, ldx, pw, m, pb, int(bool(silu)), pcu, n_seq, T, D, ps, pdy, lddy, pds, dX.data_ptr(), dw.data_ptr(), _ptr(dbias),
+            _ptr(dS_in), _stream_ptr(stream)))
+    return dX, dw, dbias, dS_in
+
+
+def chela_short_conv_step(x, w, S, bias=None, silu=True, slots=None, y=None, stream=None):
+    """One token for each of R requests, x [R, D]: y as chela_short_conv_fwd's, the states S [n_slots, m-1, D] move on in place.  A row
+    whose slot is not one of S's is left out: y keeps what it holds there."""
+    if not x.is_cuda or x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x must be a device tensor [R, D], w [D, m]")
+    R, D = x.shape
+    m, dev = w.shape[1], x.device
+    sfx, _ = _suffix(x)
+    px, ldx = _row_stride(x, x, "x")
+    pslots, n_slots = _slot_map(slots, R, S, dev)
+    if y is None:
+        y = torch.empty((R, D), dtype=x.dtype, device=dev)
+    with _on(x):
+        _check(getattr(lib(), "chela_short_conv_step" + sfx)(
+            px, ldx, _dense(w, (D, m), torch.float32, dev, "w"), m, _dense(bias, (D,), torch.float32, dev, "bias"), int(bool(silu)),
+            _dense(S, (n_slots, m - 1, D), x.dtype, dev, "S"), pslots, n_slots, R, D, _dense(y, (R, D), x.dtype, dev, "y"),
+            _stream_ptr(stream)))
+    return y
+
+
+def chela_short_conv_bwd_workspace_bytes(T, D, m, dtype) -> int:
+    return int(lib().chela_short_conv_bwd_workspace_bytes(T, D, m, int(dtype)))
+
+
+def _scan_inputs(U, delta, A, Bm, Cm, D, Z, delta_bias, softplus):
+    """The arguments that the three calls of the selective scan begin with, and (N, G)."""
+    dev, width = U.device, U.shape[-1]
+    if Bm.dim() < U.dim() or Bm.dim() > U.dim() + 1 or Cm.shape != Bm.shape:
+        raise ValueError("Bm and Cm must be [..., G, N] or [..., N] with U's rows")
+    N, G = Bm.shape[-1], Bm.shape[-2] if Bm.dim() == U.dim() + 1 else 1
+    args = [*_row_stride(U, U, "U")]
+    if delta.shape != U.shape or (Z is not None and Z.shape != U.shape):
+        raise ValueError("delta and Z must match U")
+    args += _row_stride(delta, U, "delta")
+    args.append(_dense(A, (N, width), torch.float32, dev, "A"))
+    args += _row_stride(Bm, U, "Bm")
+    args += _row_stride(Cm, U, "Cm")
+    args.append(_dense(D, (width,), torch.float32, dev, "D"))
+    args += _row_stride(Z, U, "Z") if Z is not None else (None, 0)
+    args += [_dense(delta_bias, (width,), torch.float32, dev, "delta_bias"), int(bool(softplus))]
+    return args, N, G
+
+
+def chela_selscan_fwd(U, delta, A, Bm, Cm, D=None, Z=None, delta_bias=None, softplus=True, cu=None, S_in=None, S_out=None, slots=None,
+                      want_saved=False, Y=None, stream=None):
+    """(Y, saved): the selective scan h[n] = exp(dl A[n]) h[n] + dl u B[n], y = sum_n C[n] h[n] + D u, gated with silu(Z), with
+    dl = softplus(delta + delta_bias).  A [N, D], D and delta_bias [D] float32; Bm, Cm [..., G, N] or [..., N]; states [n_slots, N, D]
+    float32.  saved is None unless asked for (for chela_selscan_bwd)."""
+    pcu, n_seq, T, width = _sequences(U, cu, "U")
+    sfx, _ = _suffix(U)
+    args, N, G = _scan_inputs(U, delta, A, Bm, Cm, D, Z, delta_bias, softplus)
+    dev = U.device
+    pslots, n_slots = _slot_map(slots, n_seq, S_in if S_in is not None else S_out, dev)
+    st = (n_slots, N, width)
+    ps_in, ps_out = _dense(S_in, st, torch.float32, dev, "S_in"), _dense(S_out, st, torch.float32, dev, "S_out")
+    if Y is None:
+        Y = torch.empty(U.shape, dtype=U.dtype, device=dev)
+    saved = None
+    if want_saved:
+        saved = torch.empty(max(chela_selscan_saved_bytes(T, width, N), 16) // 4, dtype=torch.float32, device=dev)
+    with _on(U):
+        _check(getattr(lib(), "chela_selscan_fwd" + sfx)(
+            *args, pcu, n_seq, T, width, N, G, ps_in, ps_out, pslots, n_slots, _dense(Y, U.shape, U.dtype, dev, "Y"), _ptr(saved),
+            _stream_ptr(stream)))
+    return Y, saved
+
+
+def chela_selscan_bwd(U, delta, A, Bm, Cm, dY, D=None, Z=None, delta_bias=None, softplus=True, cu=None, S_in=None, dS_out=None,
+                      want_dS_in=False, saved=None, stream=None):
+    """(dU, ddelta, dA, dB, dC, dD, dZ, ddelta_bias, dS_in) of chela_selscan_fwd (without slots) for the upstream gradients dY and dS_out;
+    None for what there is no input of, dS_in unless asked for.  saved: the forward call's on the same inputs, or None."""
+    pcu, n_seq, T, width = _sequences(U, cu, "U")
+    sfx, _ = _suffix(U)
+    args, N, G = _scan_inputs(U, delta, A, Bm, Cm, D, Z, delta_bias, softplus)
+    dev = U.device
+    if dY.shape != U.shape:
+        raise ValueError("dY must match U")
+    pdy, lddy = _row_stride(dY, U, "dY")
+    st = (n_seq, N, width)
+    ps, pds = _dense(S_in, st, torch.float32, dev, "S_in"), _dense(dS_out, st, torch.float32, dev, "dS_out")
+    if saved is not None and (saved.dtype != torch.float32 or saved.device != dev or not saved.is_contiguous()
+                              or saved.numel() * 4 < chela_selscan_saved_bytes(T, width, N)):
+        raise ValueError("saved must be what chela_selscan_fwd returned for these sizes")
+
+    def like(t, there=True):
+        return torch.empty(t.shape, dtype=t.dtype, device=dev) if there and t is not None else None
+
+    dU, ddelta, dA, dB, dC, dD, dZ, dbias = (like(t) for t in (U, delta, A, Bm, Cm, D, Z, delta_bias))
+    dS_in = torch.empty(st, dtype=torch.float32, device=dev) if want_dS_in else None
+    with _on(U):
+        _check(getattr(lib(), "chela_selscan_bwd" + sfx)(
+            *args, pcu, n_seq, T, width, N, G, ps, pdy, lddy, pds, _ptr(saved), dU.data_ptr(), ddelta.data_ptr(), dA.data_ptr(),
+            dB.data_ptr(), dC.data_ptr(), _ptr(dD), _ptr(dZ), _ptr(dbias), _ptr(dS_in), _stream_ptr(stream)))
+    return dU, ddelta, dA, dB, dC, dD, dZ, dbias, dS_in
+
+
+def chela_selscan_step(u, delta, A, Bm, Cm, S, D=None, z=None, delta_bias=None, softplus=True, slots=None, y=None, stream=None):
+    """One token for each of R requests, u [R, D]: y as chela_selscan_fwd's, the states S [n_slots, N, D] are updated in place.  A row
+    whose slot is not one of S's is left out: y keeps what it holds there."""
+    if not u.is_cuda or u.dim() != 2:
+        raise ValueError("u must be a device tensor [R, D]")
+    R, width = u.shape
+    sfx, _ = _suffix(u)
+    args, N, G = _scan_inputs(u, delta, A, Bm, Cm, D, z, delta_bias, softplus)
+    dev = u.device
+    pslots, n_slots = _slot_map(slots, R, S, dev)
+    if y is None:
+        y = torch.empty((R, width), dtype=u.dtype, device=dev)
+    with _on(u):
+        _check(getattr(lib(), "chela_selscan_step" + sfx)(
+            *args, _dense(S, (n_slots, N, width), torch.float32, dev, "S"), pslots, n_slots, R, width, N, G,
+            _dense(y, (R, width), u.dtype, dev, "y"), _stream_ptr(stream)))
+    return y
+
+
+def chela_selscan_saved_bytes(T, D, N) -> int:
+    return int(lib().chela_selscan_saved_bytes(T, D, N))
+
+
+def chela_selscan_workspace_bytes(T, D, N, G, is_bwd, has_saved=False) -> int:
+    return int(lib().chela_selscan_workspace_bytes(T, D, N, G, int(bool(is_bwd)), int(bool(has_saved))))
+
+
+def _norm_inputs(Y, X, gate, w_post, w_pre):
+    """(suffix, rows, D, whether X is fp32 beside bf16, addresses of Y, gate, X, w_post, w_pre)."""
+    if not X.is_cuda or X.dim() < 1 or not X.is_contiguous():
+        raise ValueError("X must be a contiguous device tensor [..., D]")
+    D, dev = X.shape[-1], X.device
+    io = Y.dtype if Y is not None else X.dtype
+    if io not in (torch.bfloat16, torch.float32) or X.dtype not in (io, torch.float32):
+        raise TypeError("block norm: tensors must be bfloat16 or float32, X float32 beside bfloat16")
+    if Y is None and (gate is not None or w_post is not None):
+        raise ValueError("gate and w_post need Y")
+    ptrs = (_dense(Y, X.shape, io, dev, "Y"), _dense(gate, X.shape, io, dev, "gate"), X.data_ptr(),
+            _dense(w_post, (D,), torch.float32, dev, "w_post"), _dense(w_pre, (D,), torch.float32, dev, "w_pre"))
+    return "" if io == torch.bfloat16 else "_f32", (X.numel() // D if D else 0), D, int(X.dtype != io), ptrs
+
+
+def chela_block_norm_fwd(Y, X, gate=None, w_post=None, w_pre=None, scale=1.0, eps=1e-5, X_out=None, Nrm=None, stream=None):
+    """(X_out, Nrm): X_out = X + scale * Norm(Y) * w_post * gate (w_post None: no norm of Y), Nrm = Norm(X_out) * w_pre (None without
+    w_pre) over the last dimension.  Y None: Nrm = Norm(X) * w_pre alone, and X_out is X.  X_out may be X."""
+    sfx, rows, D, x_f32, ptrs = _norm_inputs(Y, X, gate, w_post, w_pre)
+    dev, io = X.device, X.dtype if Y is None else Y.dtype
+    if Y is None:
+        X_out = X
+    elif X_out is None:
+        X_out = torch.empty_like(X)
+    if w_pre is None:
+        Nrm = None
+    elif Nrm is None:
+        Nrm = torch.empty(X.shape, dtype=io, device=dev)
+    with _on(X):
+        _check(getattr(lib(), "chela_block_norm_fwd" + sfx)(
+            *ptrs, _dense(X_out, X.shape, X.dtype, dev, "X_out"), _dense(Nrm, X.shape, io, dev, "Nrm"), float(scale), float(eps), rows, D,
+            x_f32, _stream_ptr(stream)))
+    return X_out, Nrm
+
+
+def chela_block_norm_bwd(Y, X_out, dX_out, dN, gate=None, w_post=None, w_pre=None, scale=1.0, eps=1e-5, in_place=False, stream=None):
+    """(dY, dgate, dX, dw_post, dw_pre) of chela_block_norm_fwd from its inputs and X_out, for the upstream gradients dX_out (None: zero)
+    and dN (only with w_pre); None for what there is no input of.  in_place=True writes dX over dX_out."""
+    sfx, rows, D, x_f32, ptrs = _norm_inputs(Y, X_out, gate, w_post, w_pre)
+    dev, io = X_out.device, X_out.dtype if Y is None else Y.dtype
+    pdx = _dense(dX_out, X_out.shape, X_out.dtype, dev, "dX_out")
+    if (dN is None) != (w_pre is None):
+        raise ValueError("dN goes with w_pre")
+    pdn = _dense(dN, X_out.shape, io, dev, "dN")
+    if in_place and dX_out is None:
+        raise ValueError("in_place needs dX_out")
+    dX = dX_out if in_place else torch.empty_like(X_out)
+    dY, dgate, dw_post, dw_pre = (torch.empty_like(t) if t is not None else None for t in (Y, gate, w_post, w_pre))
+    with _on(X_out):
+        _check(getattr(lib(), "chela_block_norm_bwd" + sfx)(
+            *ptrs, pdx, pdn, _ptr(dY), _ptr(dgate), dX.data_ptr(), _ptr(dw_post), _ptr(dw_pre), float(scale), float(eps), rows, D, x_f32,
+            _stream_ptr(stream)))
+    return dY, dgate, dX, dw_post, dw_pre
+
+
+def chela_block_norm_bwd_workspace_bytes(rows, D) -> int:
+    return int(lib().chela_block_norm_bwd_workspace_bytes(rows, D))
 
 
 def chela_linattn_workspace_bytes(B, H, N, dk, dv, chunk, is_bwd, dtype) -> int:

@@ -369,7 +369,8 @@ static const char* const kKernelNames[KID_COUNT] = {
     "bf16_seg_state_kernel", "scan_states_kernel", "bf16_fwd_sweep_kernel", "bf16_bwd_sweep_kernel",
     "f32_seg_state_kernel", "f32_sweep_kernel", "copy_probe_kernel", "bf16_step_kernel", "affine_grad_kernel",
     "bf16_apply_state_kernel", "longconv_spectrum_kernel", "shortlong_conv_kernel",
-    "shortconv_bwd_kernel", "longconv_bwd_kernel", "gate_norm_kernel", "stream_probe_kernel", "mfma_probe_kernel"};
+    "shortconv_bwd_kernel", "longconv_bwd_kernel", "gate_norm_kernel", "stream_probe_kernel", "mfma_probe_kernel",
+    "short_conv_kernel", "selscan_kernel", "selscan_bwd_kernel", "selscan_step_kernel", "block_norm_kernel"};
 
 ProfScope::ProfScope(int id, hipStream_t s) : slot(-1), st(s)
 {
@@ -1272,6 +1273,431 @@ int chela_linattn_step_gated(const void* q, const void* k, const void* v, const 
                              int B, int H, int dk, int dv, void* stream)
 {
     return step_common(q, k, v, g, true, eps, S, y, B, H, dk, dv, stream);
+}
+
+// ---- operators on rows
+// What a call reads and writes, for the checks that all of them make.  rows with a stride: elements' alignment; the rest: 16 bytes.
+struct Operands {
+    int rc = CHELA_OK;
+    int n_in = 0, n_out = 0;
+    Range in[16], out[12];
+    void check(const void* p, size_t bytes, size_t align)
+    {
+        if (rc != CHELA_OK || bytes == 0) return;
+        if (!p) rc = CHELA_ERR_NULL_POINTER;
+        else if ((uintptr_t)p & (align - 1)) rc = CHELA_ERR_MISALIGNED;
+    }
+    void read(const void* p, size_t bytes, size_t align = 16) { check(p, bytes, align); in[n_in++] = Range{(const char*)p, bytes}; }
+    void read_if(const void* p, size_t bytes, size_t align = 16) { if (p) read(p, bytes, align); }
+    // T rows of `width` elements
+    void rows(const void* p, long long ld, int T, size_t width, size_t es)
+    {
+        if (ld < (long long)width) { if (rc == CHELA_OK) rc = CHELA_ERR_BAD_SHAPE; return; }
+        if (ld > (1ll << 31)) { if (rc == CHELA_OK) rc = CHELA_ERR_BAD_SHAPE; return; }
+        read(p, T > 0 ? ((size_t)(T - 1) * (size_t)ld + width) * es : 0, es);
+    }
+    void write(const void* p, size_t bytes) { check(p, bytes, 16); out[n_out++] = Range{(const char*)p, bytes}; }
+    void write_if(const void* p, size_t bytes) { if (p) write(p, bytes); }
+    // no output on another, nor on an input but the one it may stand for
+    int done(const void* same_in = nullptr, const void* same_out = nullptr) const
+    {
+        if (rc != CHELA_OK) return rc;
+        for (int o = 0; o < n_out; ++o) {
+            for (int i = 0; i < n_in; ++i) {
+                if (same_in && out[o].p == same_out && in[i].p == same_in && same_in == same_out) continue;
+                if (overlap(out[o], in[i])) return CHELA_ERR_ALIASING;
+            }
+            for (int o2 = o + 1; o2 < n_out; ++o2) if (overlap(out[o], out[o2])) return CHELA_ERR_ALIASING;
+        }
+        return CHELA_OK;
+    }
+};
+
+constexpr int kMaxRows = 0x7fffffff - 4096;       // (the kernels count some rows beyond the last)
+// The sequences that T rows belong to, as a call names them.
+static int rows_of(const int* cu, int n_seq, int T, int D, const int* slots, int n_slots, Rows* out)
+{
+    if (T < 0 || n_seq < 0 || n_seq >= (1 << 24) || D < 0 || D > (1 << 20) || n_slots < 0 || T > kMaxRows) return CHELA_ERR_BAD_SHAPE;
+    if (cu == nullptr && T > 0 && (n_seq == 0 || T % n_seq != 0)) return CHELA_ERR_BAD_SHAPE;
+    if (slots == nullptr && n_slots != n_seq) return CHELA_ERR_BAD_SHAPE;
+    if (((uintptr_t)cu | (uintptr_t)slots) & 3u) return CHELA_ERR_MISALIGNED;
+    *out = Rows{cu, slots, n_seq, n_slots, T, cu == nullptr && n_seq > 0 ? T / n_seq : 0};
+    return CHELA_OK;
+}
+static int status_of(hipError_t e) { return e == hipSuccess ? CHELA_OK : CHELA_ERR_HIP; }
+static size_t esize(int dtype) { return dtype == CHELA_DTYPE_BF16 ? 2 : 4; }
+static int kind(int dtype) { return dtype == CHELA_DTYPE_BF16 ? 0 : 1; }
+// workgroups of a kernel with one per row and 64 channels stay below 2^31
+static bool too_many(int rows, int D) { return (unsigned long long)rows * (((unsigned long long)D + 63) / 64) > 0x7fffffffull; }
+
+static int short_conv_common(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,
+                             int T, int D, const void* S_in, void* S_out, const int* slots, int n_slots, void* Y, int dtype, void* stream)
+{
+    ShortConvArgs a{};
+    if (m < 1 || m > kShortConvMaxTaps) return CHELA_ERR_BAD_SHAPE;
+    int rc = rows_of(cu, n_seq, T, D, slots, n_slots, &a.rows);
+    if (rc != CHELA_OK) return rc;
+    if (too_many(T, D) || too_many(n_seq, D)) return CHELA_ERR_BAD_SHAPE;
+    if (D == 0 || (T == 0 && n_seq == 0)) return CHELA_OK;
+    if (m == 1) S_in = S_out = nullptr;
+    const size_t es = esize(dtype), st = (size_t)n_slots * (m - 1) * D * es;
+    Operands o;
+    o.rows(X, ldx, T, D, es);
+    o.read(w, (size_t)D * m * 4);
+    o.read_if(bias, (size_t)D * 4);
+    o.read_if(cu, ((size_t)n_seq + 1) * 4, 4);
+    o.read_if(slots, (size_t)n_seq * 4, 4);
+    o.read_if(S_in, st);
+    o.write_if(S_out, st);
+    o.write(Y, (size_t)T * D * es);
+    if ((rc = o.done(S_in, S_out)) != CHELA_OK) return rc;
+    a.X = X; a.ldx = ldx; a.w = w; a.m = m; a.bias = bias; a.silu = silu; a.D = D; a.S_in = S_in; a.S_out = S_out; a.Y = Y;
+    return status_of(launch_short_conv_fwd(a, kind(dtype), (hipStream_t)stream));
+}
+
+int chela_short_conv_fwd(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq, int T,
+                         int D, const void* S_in, void* S_out, const int* slots, int n_slots, void* Y, void* stream)
+{
+    return short_conv_common(X, ldx, w, m, bias, silu, cu, n_seq, T, D, S_in, S_out, slots, n_slots, Y, CHELA_DTYPE_BF16, stream);
+}
+
+int chela_short_conv_fwd_f32(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,
+                             int T, int D, const void* S_in, void* S_out, const int* slots, int n_slots, void* Y, void* stream)
+{
+    return short_conv_common(X, ldx, w, m, bias, silu, cu, n_seq, T, D, S_in, S_out, slots, n_slots, Y, CHELA_DTYPE_F32, stream);
+}
+
+size_t chela_short_conv_bwd_workspace_bytes(int T, int D, int m, int dtype)
+{
+    if (T < 0 || D <= 0 || D > (1 << 20) || m < 1 || m > kShortConvMaxTaps || (dtype != CHELA_DTYPE_BF16 && dtype != CHELA_DTYPE_F32)) return 0;
+    return (size_t)short_conv_bwd_parts(T, D, kind(dtype)) * (m + 1) * D * sizeof(float);
+}
+
+static int short_conv_bwd_common(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,
+                                 int T, int D, const void* S_in, const void* dY, long long lddy, const void* dS_out, void* dX, float* dw,
+                                 float* dbias, void* dS_in, int dtype, void* stream)
+{
+    ShortConvArgs a{};
+    if (m < 1 || m > kShortConvMaxTaps) return CHELA_ERR_BAD_SHAPE;
+    int rc = rows_of(cu, n_seq, T, D, nullptr, n_seq, &a.rows);
+    if (rc != CHELA_OK) return rc;
+    if (too_many(T, D)) return CHELA_ERR_BAD_SHAPE;
+    if (D == 0) return CHELA_OK;
+    if (m == 1) { S_in = dS_out = nullptr; dS_in = nullptr; }
+    const size_t es = esize(dtype), st = (size_t)n_seq * (m - 1) * D * es, rows = (size_t)T * D * es;
+    Operands o;
+    o.rows(X, ldx, T, D, es);
+    o.rows(dY, lddy, T, D, es);
+    o.read(w, (size_t)D * m * 4);
+    o.read_if(bias, (size_t)D * 4);
+    o.read_if(cu, ((size_t)n_seq + 1) * 4, 4);
+    o.read_if(S_in, st);
+    o.read_if(dS_out, st);
+    o.write(dX, rows);
+    o.write(dw, (size_t)D * m * 4);
+    if (bias) o.write(dbias, (size_t)D * 4);
+    o.write_if(dS_in, st);
+    if ((rc = o.done()) != CHELA_OK) return rc;
+    float* ws = nullptr;
+    rc = get_workspace(chela_short_conv_bwd_workspace_bytes(T, D, m, dtype), stream, &ws);
+    if (rc != CHELA_OK) return rc;
+    a.X = X; a.ldx = ldx; a.w = w; a.m = m; a.bias = bias; a.silu = silu; a.D = D; a.S_in = S_in; a.dY = dY; a.lddy = lddy;
+    a.dS_out = dS_out; a.dX = dX; a.dw = dw; a.dbias = bias ? dbias : nullptr; a.dS_in = dS_in; a.part = ws;
+    return status_of(launch_short_conv_bwd(a, kind(dtype), (hipStream_t)stream));
+}
+
+int chela_short_conv_bwd(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq, int T,
+                         int D, const void* S_in, const void* dY, long long lddy, const void* dS_out, void* dX, float* dw, float* dbias,
+                         void* dS_in, void* stream)
+{
+    return short_conv_bwd_common(X, ldx, w, m, bias, silu, cu, n_seq, T, D, S_in, dY, lddy, dS_out, dX, dw, dbias, dS_in,
+                                 CHELA_DTYPE_BF16, stream);
+}
+
+int chela_short_conv_bwd_f32(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,
+                             int T, int D, const void* S_in, const void* dY, long long lddy, const void* dS_out, void* dX, float* dw,
+                             float* dbias, void* dS_in, void* stream)
+{
+    return short_conv_bwd_common(X, ldx, w, m, bias, silu, cu, n_seq, T, D, S_in, dY, lddy, dS_out, dX, dw, dbias, dS_in,
+                                 CHELA_DTYPE_F32, stream);
+}
+
+static int short_conv_step_common(const void* x, long long ldx, const float* w, int m, const float* bias, int silu, void* S,
+                                  const int* slots, int n_slots, int R, int D, void* y, int dtype, void* stream)
+{
+    ShortConvArgs a{};
+    if (m < 1 || m > kShortConvMaxTaps || R < 0 || R >= (1 << 24)) return CHELA_ERR_BAD_SHAPE;
+    int rc = rows_of(nullptr, R, R, D, slots, n_slots, &a.rows);
+    if (rc != CHELA_OK) return rc;
+    if (too_many(R, D)) return CHELA_ERR_BAD_SHAPE;
+    if (R == 0 || D == 0) return CHELA_OK;
+    const size_t es = esize(dtype);
+    Operands o;
+    o.rows(x, ldx, R, D, es);
+    o.read(w, (size_t)D * m * 4);
+    o.read_if(bias, (size_t)D * 4);
+    o.read_if(slots, (size_t)R * 4, 4);
+    o.write(S, (size_t)n_slots * (m - 1) * D * es);
+    o.write(y, (size_t)R * D * es);
+    if ((rc = o.done()) != CHELA_OK) return rc;
+    a.X = x; a.ldx = ldx; a.w = w; a.m = m; a.bias = bias; a.silu = silu; a.D = D; a.S_out = S; a.Y = y;
+    return status_of(launch_short_conv_step(a, kind(dtype), (hipStream_t)stream));
+}
+
+int chela_short_conv_step(const void* x, long long ldx, const float* w, int m, const float* bias, int silu, void* S, const int* slots,
+                          int n_slots, int R, int D, void* y, void* stream)
+{
+    return short_conv_step_common(x, ldx, w, m, bias, silu, S, slots, n_slots, R, D, y, CHELA_DTYPE_BF16, stream);
+}
+
+int chela_short_conv_step_f32(const void* x, long long ldx, const float* w, int m, const float* bias, int silu, void* S, const int* slots,
+                              int n_slots, int R, int D, void* y, void* stream)
+{
+    return short_conv_step_common(x, ldx, w, m, bias, silu, S, slots, n_slots, R, D, y, CHELA_DTYPE_F32, stream);
+}
+
+static bool selscan_dims(int D, int N, int G) { return selscan_states_ok(N) && G >= 1 && D >= 0 && D % G == 0; }
+
+size_t chela_selscan_saved_bytes(int T, int D, int N)
+{
+    if (T <= 0 || D <= 0 || D > (1 << 20) || !selscan_states_ok(N)) return 0;
+    return ((size_t)T + kSelscanTile - 1) / kSelscanTile * N * D * sizeof(float);
+}
+
+size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int has_saved)
+{
+    if (T <= 0 || D <= 0 || D > (1 << 20) || !selscan_dims(D, N, G)) return 0;
+    return make_selscan_plan(T, D, N, G, is_bwd != 0, has_saved != 0).bytes;
+}
+
+// The arguments that the forward, the backward and the single-token call share.
+struct SelscanIn {
+    const void *U, *delta, *Bm, *Cm, *Z;
+    long long ldu, ldd, ldb, ldc, ldz;
+    const float *A, *Dskip, *delta_bias;
+    int softplus, D, N, G;
+};
+static void selscan_read(const SelscanIn& x, int T, size_t es, Operands* o, SelscanArgs* a)
+{
+    o->rows(x.U, x.ldu, T, x.D, es);
+    o->rows(x.delta, x.ldd, T, x.D, es);
+    o->rows(x.Bm, x.ldb, T, (size_t)x.G * x.N, es);
+    o->rows(x.Cm, x.ldc, T, (size_t)x.G * x.N, es);
+    if (x.Z) o->rows(x.Z, x.ldz, T, x.D, es);
+    o->read(x.A, (size_t)x.N * x.D * 4);
+    o->read_if(x.Dskip, (size_t)x.D * 4);
+    o->read_if(x.delta_bias, (size_t)x.D * 4);
+    o->read_if(a->rows.cu, ((size_t)a->rows.n_seq + 1) * 4, 4);
+    o->read_if(a->rows.slots, (size_t)a->rows.n_seq * 4, 4);
+    a->U = x.U; a->delta = x.delta; a->Bm = x.Bm; a->Cm = x.Cm; a->Z = x.Z;
+    a->ldu = x.ldu; a->ldd = x.ldd; a->ldb = x.ldb; a->ldc = x.ldc; a->ldz = x.Z ? x.ldz : 0;
+    a->A = x.A; a->Dskip = x.Dskip; a->delta_bias = x.delta_bias;
+    a->softplus = x.softplus; a->D = x.D; a->N = x.N; a->G = x.G;
+}
+
+static int selscan_fwd_common(const SelscanIn& x, const int* cu, int n_seq, int T, const float* S_in, float* S_out, const int* slots,
+                              int n_slots, void* Y, void* saved, int dtype, void* stream)
+{
+    SelscanArgs a{};
+    if (!selscan_states_ok(x.N)) return CHELA_ERR_UNSUPPORTED_DIM;
+    if (!selscan_dims(x.D, x.N, x.G)) return CHELA_ERR_BAD_SHAPE;
+    int rc = rows_of(cu, n_seq, T, x.D, slots, n_slots, &a.rows);
+    if (rc != CHELA_OK) return rc;
+    if (x.D == 0 || (T == 0 && n_seq == 0)) return CHELA_OK;
+    const size_t es = esize(dtype), st = (size_t)n_slots * x.N * x.D * 4;
+    Operands o;
+    selscan_read(x, T, es, &o, &a);
+    o.read_if(S_in, st);
+    o.write_if(S_out, st);
+    o.write(Y, (size_t)T * x.D * es);
+    o.write_if(saved, chela_selscan_saved_bytes(T, x.D, x.N));
+    if ((rc = o.done(S_in, S_out)) != CHELA_OK) return rc;
+    const SelscanPlan p = make_selscan_plan(T, x.D, x.N, x.G, false, false);
+    float* ws = nullptr;
+    if ((rc = get_workspace(p.bytes, stream, &ws)) != CHELA_OK) return rc;
+    a.S_in = S_in; a.S_out = S_out; a.Y = Y; a.saved = (float*)saved;
+    return status_of(launch_selscan_fwd(a, p, (char*)ws, kind(dtype), (hipStream_t)stream));
+}
+
+static int selscan_bwd_common(const SelscanIn& x, const int* cu, int n_seq, int T, const float* S_in, const void* dY, long long lddy,
+                              const float* dS_out, const void* saved, void* dU, void* ddelta, float* dA, void* dB, void* dC, float* dDskip,
+                              void* dZ, float* ddelta_bias, float* dS_in, int dtype, void* stream)
+{
+    SelscanArgs a{};
+    if (!selscan_states_ok(x.N)) return CHELA_ERR_UNSUPPORTED_DIM;
+    if (!selscan_dims(x.D, x.N, x.G)) return CHELA_ERR_BAD_SHAPE;
+    int rc = rows_of(cu, n_seq, T, x.D, nullptr, n_seq, &a.rows);
+    if (rc != CHELA_OK) return rc;
+    if (x.D == 0) return CHELA_OK;
+    const size_t es = esize(dtype), st = (size_t)n_seq * x.N * x.D * 4, rows = (size_t)T * x.D * es, maps = (size_t)T * x.G * x.N * es;
+    Operands o;
+    selscan_read(x, T, es, &o, &a);
+    o.read_if(S_in, st);
+    o.rows(dY, lddy, T, x.D, es);
+    o.read_if(dS_out, st);
+    o.read_if(saved, chela_selscan_saved_bytes(T, x.D, x.N));
+    o.write(dU, rows);
+    o.write(ddelta, rows);
+    o.write(dA, (size_t)x.N * x.D * 4);
+    o.write(dB, maps);
+    o.write(dC, maps);
+    if (x.Dskip) o.write(dDskip, (size_t)x.D * 4);
+    if (x.Z) o.write(dZ, rows);
+    if (x.delta_bias) o.write(ddelta_bias, (size_t)x.D * 4);
+    o.write_if(dS_in, st);
+    if ((rc = o.done()) != CHELA_OK) return rc;
+    const SelscanPlan p = make_selscan_plan(T, x.D, x.N, x.G, true, saved != nullptr);
+    float* ws = nullptr;
+    if ((rc = get_workspace(p.bytes, stream, &ws)) != CHELA_OK) return rc;
+    a.S_in = S_in; a.dY = dY; a.lddy = lddy; a.dS_out = dS_out; a.saved = (float*)saved;
+    a.dU = dU; a.ddelta = ddelta; a.dA = dA; a.dB = dB; a.dC = dC; a.dDskip = x.Dskip ? dDskip : nullptr; a.dZ = dZ;
+    a.dbias = x.delta_bias ? ddelta_bias : nullptr; a.dS_in = dS_in;
+    return status_of(launch_selscan_bwd(a, p, (char*)ws, kind(dtype), (hipStream_t)stream));
+}
+
+static int selscan_step_common(const SelscanIn& x, float* S, const int* slots, int n_slots, int R, void* y, int dtype, void* stream)
+{
+    SelscanArgs a{};
+    if (!selscan_states_ok(x.N)) return CHELA_ERR_UNSUPPORTED_DIM;
+    if (!selscan_dims(x.D, x.N, x.G) || R < 0 || R >= (1 << 24)) return CHELA_ERR_BAD_SHAPE;
+    int rc = rows_of(nullptr, R, R, x.D, slots, n_slots, &a.rows);
+    if (rc != CHELA_OK) return rc;
+    if (too_many(R, x.D)) return CHELA_ERR_BAD_SHAPE;
+    if (R == 0 || x.D == 0) return CHELA_OK;
+    const size_t es = esize(dtype);
+    Operands o;
+    selscan_read(x, R, es, &o, &a);
+    o.write(S, (size_t)n_slots * x.N * x.D * 4);
+    o.write(y, (size_t)R * x.D * es);
+    if ((rc = o.done()) != CHELA_OK) return rc;
+    a.S_out = S; a.Y = y;
+    return status_of(launch_selscan_step(a, kind(dtype), (hipStream_t)stream));
+}
+
+#define CHELA_SELSCAN_IN                                                                                              \
+    const void *U, long long ldu, const void *delta, long long ldd, const float *A, const void *Bm, long long ldb, const void *Cm,       \
+        long long ldc, const float *Dskip, const void *Z, long long ldz, const float *delta_bias, int softplus
+#define CHELA_SELSCAN_AS(D, N, G) SelscanIn{U, delta, Bm, Cm, Z, ldu, ldd, ldb, ldc, ldz, A, Dskip, delta_bias, softplus, D, N, G}
+#define CHELA_SELSCAN(SUFFIX, TYPE)                                                                                   \
+    int chela_selscan_fwd##SUFFIX(CHELA_SELSCAN_IN, const int* cu, int n_seq, int T, int D, int N, int G, const float* S_in, float* S_out, \
+                                  const int* slots, int n_slots, void* Y, void* saved, void* stream)                  \
+    {                                                                                                                 \
+        return selscan_fwd_common(CHELA_SELSCAN_AS(D, N, G), cu, n_seq, T, S_in, S_out, slots, n_slots, Y, saved, TYPE, stream); \
+    }                                                                                                                 \
+    int chela_selscan_bwd##SUFFIX(CHELA_SELSCAN_IN, const int* cu, int n_seq, int T, int D, int N, int G, const float* S_in,  \
+                                  const void* dY, long long lddy, const float* dS_out, const void* saved, void* dU, void* ddelta,  \
+                                  float* dA, void* dB, void* dC, float* dDskip, void* dZ, float* ddelta_bias, float* dS_in,   \
+                                  void* stream)                                                                       \
+    {                                                                                                                 \
+        return selscan_bwd_common(CHELA_SELSCAN_AS(D, N, G), cu, n_seq, T, S_in, dY, lddy, dS_out, saved, dU, ddelta, dA, dB, dC, dDskip, \
+                                  dZ, ddelta_bias, dS_in, TYPE, stream);                                              \
+    }                                                                                                                 \
+    int chela_selscan_step##SUFFIX(CHELA_SELSCAN_IN, float* S, const int* slots, int n_slots, int R, int D, int N, int G, void* y,  \
+                                   void* stream)                                                                      \
+    {                                                                                                                 \
+        return selscan_step_common(CHELA_SELSCAN_AS(D, N, G), S, slots, n_slots, R, y, TYPE, stream);                 \
+    }
+CHELA_SELSCAN(, CHELA_DTYPE_BF16)
+CHELA_SELSCAN(_f32, CHELA_DTYPE_F32)
+#undef CHELA_SELSCAN
+#undef CHELA_SELSCAN_AS
+#undef CHELA_SELSCAN_IN
+
+static int block_norm_check(const void* Y, const void* X, const float* w_pre, float scale, float eps, long long rows, int D)
+{
+    if (!(eps >= 0.f) || !std::isfinite(eps) || !std::isfinite(scale)) return CHELA_ERR_BAD_SHAPE;
+    if (rows < 0 || rows > 0x7fffffffll || D < 1) return CHELA_ERR_BAD_SHAPE;
+    if (D > kBlockNormMaxD) return CHELA_ERR_UNSUPPORTED_DIM;
+    if (!Y && !w_pre && rows > 0 && X) return CHELA_ERR_NULL_POINTER;      // neither of the two parts
+    return CHELA_OK;
+}
+
+static int block_norm_fwd_common(const void* Y, const void* gate, const void* X, const float* w_post, const float* w_pre, void* X_out,
+                                 void* Nrm, float scale, float eps, long long rows, int D, int x_f32, int dtype, void* stream)
+{
+    int rc = block_norm_check(Y, X, w_pre, scale, eps, rows, D);
+    if (rc != CHELA_OK) return rc;
+    if (rows == 0) return CHELA_OK;
+    if (!Y) { gate = nullptr; w_post = nullptr; X_out = nullptr; }
+    const size_t es = esize(dtype), n = (size_t)rows * D, xs = x_f32 ? 4 : es;
+    Operands o;
+    o.read(X, n * xs);
+    o.read_if(Y, n * es);
+    o.read_if(gate, n * es);
+    o.read_if(w_post, (size_t)D * 4);
+    o.read_if(w_pre, (size_t)D * 4);
+    if (Y) o.write(X_out, n * xs);
+    if (w_pre) o.write(Nrm, n * es);
+    if ((rc = o.done(X, X_out)) != CHELA_OK) return rc;
+    BlockNormArgs a{};
+    a.Y = Y; a.gate = gate; a.X = X; a.w_post = w_post; a.w_pre = w_pre; a.X_out = X_out; a.Nrm = Nrm;
+    a.scale = scale; a.eps = eps; a.rows = rows; a.D = D; a.x_f32 = x_f32;
+    return status_of(launch_block_norm_fwd(a, kind(dtype), (hipStream_t)stream));
+}
+
+size_t chela_block_norm_bwd_workspace_bytes(long long rows, int D)
+{
+    if (rows < 0 || rows > 0x7fffffffll || D < 1 || D > kBlockNormMaxD) return 0;
+    return (size_t)block_norm_bwd_parts((long)rows, D) * 2 * D * sizeof(float);
+}
+
+static int block_norm_bwd_common(const void* Y, const void* gate, const void* X, const float* w_post, const float* w_pre,
+                                 const void* dX_out, const void* dN, void* dY, void* dgate, void* dX, float* dw_post, float* dw_pre,
+                                 float scale, float eps, long long rows, int D, int x_f32, int dtype, void* stream)
+{
+    int rc = block_norm_check(Y, X, w_pre, scale, eps, rows, D);
+    if (rc != CHELA_OK) return rc;
+    if (!Y && rows > 0) { gate = nullptr; w_post = nullptr; }
+    const size_t es = esize(dtype), n = (size_t)rows * D, xs = x_f32 ? 4 : es;
+    Operands o;
+    o.read(X, n * xs);
+    o.read_if(Y, n * es);
+    o.read_if(gate, n * es);
+    o.read_if(w_post, (size_t)D * 4);
+    o.read_if(w_pre, (size_t)D * 4);
+    o.read_if(dX_out, n * xs);
+    if (w_pre) o.read(dN, n * es);
+    if (Y) o.write(dY, n * es);
+    if (gate) o.write(dgate, n * es);
+    o.write(dX, n * xs);
+    if (w_post) o.write(dw_post, (size_t)D * 4);
+    if (w_pre) o.write(dw_pre, (size_t)D * 4);
+    if ((rc = o.done(dX_out, dX)) != CHELA_OK) return rc;
+    float* ws = nullptr;
+    if ((rc = get_workspace(chela_block_norm_bwd_workspace_bytes(rows, D), stream, &ws)) != CHELA_OK) return rc;
+    BlockNormArgs a{};
+    a.Y = Y; a.gate = gate; a.X = X; a.w_post = w_post; a.w_pre = w_pre; a.dX_out = dX_out; a.dN = dN; a.dY = dY; a.dgate = dgate; a.dX = dX;
+    a.dw_post = w_post ? dw_post : nullptr; a.dw_pre = w_pre ? dw_pre : nullptr; a.part = ws;
+    a.scale = scale; a.eps = eps; a.rows = rows; a.D = D; a.x_f32 = x_f32;
+    return status_of(launch_block_norm_bwd(a, kind(dtype), (hipStream_t)stream));
+}
+
+int chela_block_norm_fwd(const void* Y, const void* gate, const void* X, const float* w_post, const float* w_pre, void* X_out, void* Nrm,
+                         float scale, float eps, long long rows, int D, int x_f32, void* stream)
+{
+    return block_norm_fwd_common(Y, gate, X, w_post, w_pre, X_out, Nrm, scale, eps, rows, D, x_f32, CHELA_DTYPE_BF16, stream);
+}
+
+int chela_block_norm_fwd_f32(const void* Y, const void* gate, const void* X, const float* w_post, const float* w_pre, void* X_out,
+                             void* Nrm, float scale, float eps, long long rows, int D, int x_f32, void* stream)
+{
+    return block_norm_fwd_common(Y, gate, X, w_post, w_pre, X_out, Nrm, scale, eps, rows, D, x_f32, CHELA_DTYPE_F32, stream);
+}
+
+int chela_block_norm_bwd(const void* Y, const void* gate, const void* X, const float* w_post, const float* w_pre, const void* dX_out,
+                         const void* dN, void* dY, void* dgate, void* dX, float* dw_post, float* dw_pre, float scale, float eps,
+                         long long rows, int D, int x_f32, void* stream)
+{
+    return block_norm_bwd_common(Y, gate, X, w_post, w_pre, dX_out, dN, dY, dgate, dX, dw_post, dw_pre, scale, eps, rows, D, x_f32,
+                                 CHELA_DTYPE_BF16, stream);
+}
+
+int chela_block_norm_bwd_f32(const void* Y, const void* gate, const void* X, const float* w_post, const float* w_pre, const void* dX_out,
+                             const void* dN, void* dY, void* dgate, void* dX, float* dw_post, float* dw_pre, float scale, float eps,
+                             long long rows, int D, int x_f32, void* stream)
+{
+    return block_norm_bwd_common(Y, gate, X, w_post, w_pre, dX_out, dN, dY, dgate, dX, dw_post, dw_pre, scale, eps, rows, D, x_f32,
+                                 CHELA_DTYPE_F32, stream);
 }
 
 size_t chela_linattn_workspace_bytes(int B, int H, int N, int dk, int dv, int chunk, int is_bwd, int dtype)

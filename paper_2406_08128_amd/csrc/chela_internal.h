@@ -216,9 +216,72 @@ hipError_t launch_shortlong_conv_bwd(const void* X, const float* w_short, int m,
                                      void* dX, float* dw, float* dk, float* ws_dV, int B, int d, int L, int dtype,
                                      hipStream_t st);
 
+// ---- operators on [T, D] rows (a token's channels next to each other)
+// Whose rows they are: sequence s has rows cu[s] .. cu[s+1], or L rows where cu is null.  slots: which state of the n_slots there are is
+// sequence s's (null: the s-th).
+struct Rows {
+    const int* cu;
+    const int* slots;
+    int n_seq, n_slots, T, L;
+};
+
+// Short causal convolution.  S_in, S_out: the last m - 1 inputs in front of and behind each sequence, [n_slots][m-1][D].
+struct ShortConvArgs {
+    Rows rows;
+    const void *X, *S_in, *dY, *dS_out;
+    long ldx, lddy;
+    const float *w, *bias;
+    void *S_out, *Y, *dX, *dS_in;
+    float *dw, *dbias, *part;
+    int m, D, silu;
+};
+constexpr int kShortConvMaxTaps = 8;
+int short_conv_bwd_parts(int T, int D, int dtype);              // partial sums of dw and dbias, [parts][m + 1][D] floats
+hipError_t launch_short_conv_fwd(const ShortConvArgs& a, int dtype, hipStream_t st);
+hipError_t launch_short_conv_bwd(const ShortConvArgs& a, int dtype, hipStream_t st);
+hipError_t launch_short_conv_step(const ShortConvArgs& a, int dtype, hipStream_t st);
+
+// Selective scan.  The rows are cut into n_chunk chunks of `chunk`, whichever sequences they belong to.
+struct SelscanPlan {
+    int chunk, n_chunk;
+    size_t bc, totals, sums, flags, fin, part_bc, part_A, part_D, saved, bytes;      // byte offsets into the scratch, and its size
+};
+struct SelscanArgs {
+    Rows rows;
+    const void *U, *delta, *Bm, *Cm, *Z, *dY;
+    long ldu, ldd, ldb, ldc, ldz, lddy;
+    const float *A, *Dskip, *delta_bias, *S_in, *dS_out;
+    float *S_out, *saved, *dS_in;
+    void *Y, *dU, *ddelta, *dB, *dC, *dZ;
+    float *dA, *dDskip, *dbias;
+    int D, N, G, softplus;
+};
+constexpr int kSelscanTile = 16;              // rows between two saved states
+bool selscan_states_ok(int N);
+SelscanPlan make_selscan_plan(int T, int D, int N, int G, bool is_bwd, bool has_saved);
+hipError_t launch_selscan_fwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, int dtype, hipStream_t st);
+hipError_t launch_selscan_bwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, int dtype, hipStream_t st);
+hipError_t launch_selscan_step(const SelscanArgs& a, int dtype, hipStream_t st);
+
+// Norms around a block.
+struct BlockNormArgs {
+    const void *Y, *gate, *X, *dX_out, *dN;            // (backward: X is the stream as the forward left it)
+    const float *w_post, *w_pre;
+    void *X_out, *Nrm, *dY, *dgate, *dX;
+    float *dw_post, *dw_pre, *part;
+    float scale, eps;
+    long rows;
+    int D, x_f32;                                      // x_f32: the stream and its gradients are fp32
+};
+constexpr int kBlockNormMaxD = 8192;
+int block_norm_bwd_parts(long rows, int D);            // partial sums of dw_post and dw_pre, [parts][2][D] floats
+hipError_t launch_block_norm_fwd(const BlockNormArgs& a, int dtype, hipStream_t st);
+hipError_t launch_block_norm_bwd(const BlockNormArgs& a, int dtype, hipStream_t st);
+
 // Kernel classes for the per-kernel timing aid.
 enum { KID_SEG_STATE_BF16 = 0, KID_SCAN = 1, KID_FWD_SWEEP_BF16 = 2, KID_BWD_SWEEP_BF16 = 3, KID_SEG_STATE_F32 = 4,
-       KID_SWEEP_F32 = 5, KID_COPY = 6, KID_STEP_BF16 = 7, KID_AFFINE_GRAD = 8, KID_APPLY_BF16 = 9, KID_CONV_SPECTRUM = 10, KID_CONV_FWD = 11, KID_CONV_SHORT_BWD = 12, KID_CONV_LONG_BWD = 13, KID_GATE_NORM = 14, KID_STREAM_PROBE = 15, KID_MFMA_PROBE = 16, KID_COUNT = 17 };
+       KID_SWEEP_F32 = 5, KID_COPY = 6, KID_STEP_BF16 = 7, KID_AFFINE_GRAD = 8, KID_APPLY_BF16 = 9, KID_CONV_SPECTRUM = 10, KID_CONV_FWD = 11, KID_CONV_SHORT_BWD = 12, KID_CONV_LONG_BWD = 13, KID_GATE_NORM = 14, KID_STREAM_PROBE = 15, KID_MFMA_PROBE = 16, KID_SHORT_CONV = 17, KID_SELSCAN = 18,
+       KID_SELSCAN_BWD = 19, KID_SELSCAN_STEP = 20, KID_BLOCK_NORM = 21, KID_COUNT = 22 };
 
 // Brackets one kernel launch with HIP events on its stream while profiling is enabled; otherwise does nothing.
 struct ProfScope {

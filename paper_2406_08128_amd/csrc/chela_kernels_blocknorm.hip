@@ -1,0 +1,288 @@
+// Norms before and after a block with its gate and residual, in one pass over the rows, gfx950.
+//
+//     p = Norm(Y) w_post gate   (w_post null: Y gate),   X' = X + scale p,   N = Norm(X') w_pre;   Norm(x) = x / sqrt(mean x^2 + eps)
+// Gradient, from Y, gate and X' (the norms are worked out again), with x^ = Norm(X'), v = dN w_pre, y^ = Norm(Y), s = 1 / sqrt(...):
+//     dX = dX' + s (v - x^ mean(v x^)),  dw_pre = sum dN x^;   dp = scale dX,  dgate = dp y^ w_post,  dw_post = sum dp y^ gate,
+//     dY = s (v - y^ mean(v y^)) with v = dp w_post gate.
+//
+// Memory-bound: a row stays in the registers of TPR threads between its two norms, so every tensor is read or written once.
+#include "chela_rows.h"
+
+namespace chela {
+
+// A thread's share of a row: NV pieces of 8 elements.  VEC: 16 bytes (bf16) or twice 16 (fp32) at a time; else element by element, the
+// threads' elements next to each other.
+template <typename T, int TPR, int NV, bool VEC>
+struct RowPart {
+    static constexpr int E = NV * 8;
+    static __device__ __forceinline__ int at(int tid, int e) { return VEC ? ((e >> 3) * TPR + tid) * 8 + (e & 7) : e * TPR + tid; }
+    static __device__ __forceinline__ void load(const T* row, int D, int tid, float (&x)[E])
+    {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if (VEC) {
+                const int i = (v * TPR + tid) * 8;
+                if (i < D) {
+                    struct alignas(16) { T e[8]; } t;
+                    const u32x4* p = reinterpret_cast<const u32x4*>(row + i);
+                    *reinterpret_cast<u32x4*>(&t) = p[0];
+                    if (sizeof(T) == 4) reinterpret_cast<u32x4*>(&t)[1 % (sizeof(t) / 16)] = p[1 % (sizeof(t) / 16)];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[v * 8 + j] = to_f(t.e[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[v * 8 + j] = 0.f;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int i = at(tid, v * 8 + j);
+                    x[v * 8 + j] = i < D ? to_f(row[i]) : 0.f;
+                }
+            }
+        }
+    }
+    static __device__ __forceinline__ void store(T* row, int D, int tid, const float (&x)[E])
+    {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if (VEC) {
+                const int i = (v * TPR + tid) * 8;
+                if (i >= D) continue;
+                struct alignas(16) { T e[8]; } t;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) t.e[j] = from_f<T>(x[v * 8 + j]);
+                u32x4* p = reinterpret_cast<u32x4*>(row + i);
+                p[0] = *reinterpret_cast<u32x4*>(&t);
+                if (sizeof(T) == 4) p[1 % (sizeof(t) / 16)] = reinterpret_cast<u32x4*>(&t)[1 % (sizeof(t) / 16)];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int i = at(tid, v * 8 + j);
+                    if (i < D) row[i] = from_f<T>(x[v * 8 + j]);
+                }
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+// Sums of K values over a row's threads; every thread returns with them.  s: room for K values per wave, not in use by the call before.
+template <int TPR, int K>
+__device__ __forceinline__ void row_sums(float (&x)[K], float (*s)[K])
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = wave_sum(x[k]);
+    if (TPR == 64) return;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k) s[threadIdx.x >> 6][k] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = 0.f;
+    for (int i = 0; i < TPR / 64; ++i)
+#pragma unroll
+        for (int k = 0; k < K; ++k) x[k] += s[i][k];
+}
+
+template <typename IO, typename XT, int TPR, int NV, bool VEC>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_kernel(BlockNormArgs a)
+{
+    typedef RowPart<IO, TPR, NV, VEC> P;
+    typedef RowPart<XT, TPR, NV, VEC> PX;
+    typedef RowPart<float, TPR, NV, VEC> PW;
+    constexpr int E = P::E, RPW = TPR < 256 ? 256 / TPR : 1;
+    __shared__ float s_a[16][1], s_b[16][1];
+    const int tid = threadIdx.x % TPR, D = a.D;
+    const long r = (long)blockIdx.x * RPW + threadIdx.x / TPR;
+    if (r >= a.rows) return;                                   // (whole rows leave: with several waves to a row there is one row)
+    float x[E], y[E], g[E], w[E], sum[1];
+    PX::load((const XT*)a.X + (size_t)r * D, D, tid, x);
+    if (a.Y) {
+        P::load((const IO*)a.Y + (size_t)r * D, D, tid, y);
+        if (a.gate) P::load((const IO*)a.gate + (size_t)r * D, D, tid, g);
+        if (a.w_post) {
+            PW::load(a.w_post, D, tid, w);
+            sum[0] = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[0] = fmaf(y[e], y[e], sum[0]);
+            row_sums<TPR, 1>(sum, s_a);
+            const float s = __builtin_amdgcn_rsqf(fmaf(sum[0], 1.f / (float)D, a.eps));
+#pragma unroll
+            for (int e = 0; e < E; ++e) y[e] *= s * w[e];
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = fmaf(a.scale, a.gate ? y[e] * g[e] : y[e], x[e]);
+        PX::store((XT*)a.X_out + (size_t)r * D, D, tid, x);
+    }
+    if (!a.w_pre) return;
+    PW::load(a.w_pre, D, tid, w);
+    sum[0] = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[0] = fmaf(x[e], x[e], sum[0]);
+    row_sums<TPR, 1>(sum, s_b);
+    const float s = __builtin_amdgcn_rsqf(fmaf(sum[0], 1.f / (float)D, a.eps));
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] *= s * w[e];
+    P::store((IO*)a.Nrm + (size_t)r * D, D, tid, x);
+}
+
+// A workgroup goes over every gridDim.x-th set of rows; the sums of the gains' gradients stay in registers and leave once.
+template <typename IO, typename XT, int TPR, int NV, bool VEC>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_bwd_kernel(BlockNormArgs a)
+{
+    typedef RowPart<IO, TPR, NV, VEC> P;
+    typedef RowPart<XT, TPR, NV, VEC> PX;
+    typedef RowPart<float, TPR, NV, VEC> PW;
+    constexpr int E = P::E, RPW = TPR < 256 ? 256 / TPR : 1;
+    __shared__ float s_a[16][3], s_b[16][1], s_w[2][RPW > 1 ? TPR * E : 1];
+    const int tid = threadIdx.x % TPR, D = a.D;
+    const float inv = 1.f / (float)D;
+    float wpost[E], wpre[E], dwpost[E], dwpre[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) { wpost[e] = 1.f; dwpost[e] = dwpre[e] = 0.f; wpre[e] = 0.f; }
+    if (a.w_post) PW::load(a.w_post, D, tid, wpost);
+    if (a.w_pre) PW::load(a.w_pre, D, tid, wpre);
+    for (long r = (long)blockIdx.x * RPW + threadIdx.x / TPR; r < a.rows; r += (long)gridDim.x * RPW) {
+        float x[E], y[E], g[E], d[E], sums[3] = {0.f, 0.f, 0.f}, sum[1] = {0.f};
+        PX::load((const XT*)a.X + (size_t)r * D, D, tid, x);
+        if (a.w_pre) P::load((const IO*)a.dN + (size_t)r * D, D, tid, d);
+        if (a.Y) P::load((const IO*)a.Y + (size_t)r * D, D, tid, y);
+        if (a.Y && a.gate) P::load((const IO*)a.gate + (size_t)r * D, D, tid, g);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (a.w_pre) {
+                sums[0] = fmaf(x[e], x[e], sums[0]);
+                sums[1] = fmaf(d[e] * wpre[e], x[e], sums[1]);
+            }
+            if (a.Y) sums[2] = fmaf(y[e], y[e], sums[2]);
+        }
+        row_sums<TPR, 3>(sums, s_a);
+        const float sx = __builtin_amdgcn_rsqf(fmaf(sums[0], inv, a.eps)), mx = sums[1] * inv * sx;
+        float dx[E];
+        if (a.dX_out) {
+            PX::load((const XT*)a.dX_out + (size_t)r * D, D, tid, dx);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) dx[e] = 0.f;
+        }
+        if (a.w_pre) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float n = x[e] * sx;
+                dwpre[e] = fmaf(d[e], n, dwpre[e]);
+                dx[e] = fmaf(sx, fmaf(-n, mx, d[e] * wpre[e]), dx[e]);
+            }
+        }
+        PX::store((XT*)a.dX + (size_t)r * D, D, tid, dx);
+        if (a.Y) {
+            const float sy = a.w_post ? __builtin_amdgcn_rsqf(fmaf(sums[2], inv, a.eps)) : 1.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float dp = a.scale * dx[e], n = y[e] * sy, gate = a.gate ? g[e] : 1.f;
+                dwpost[e] = fmaf(dp * n, gate, dwpost[e]);
+                g[e] = dp * n * wpost[e];                        // dgate
+                d[e] = dp * wpost[e] * gate;                     // v
+                y[e] = n;
+                sum[0] = fmaf(d[e], n, sum[0]);
+            }
+            if (a.gate) P::store((IO*)a.dgate + (size_t)r * D, D, tid, g);
+            if (a.w_post) {
+                row_sums<TPR, 1>(sum, s_b);
+                const float my = sum[0] * inv;
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[e] = sy * fmaf(-y[e], my, d[e]);
+            }
+            P::store((IO*)a.dY + (size_t)r * D, D, tid, d);
+        }
+        // (a wave writes its sums of the next row only after all waves have read those of this one)
+        if (TPR > 64) __syncthreads();
+    }
+    float* part = a.part + (size_t)blockIdx.x * 2 * D;
+    if (RPW > 1) {
+        // the waves of the workgroup, one after the other
+        for (int v = 0; v < RPW; ++v) {
+            if ((int)(threadIdx.x / TPR) == v) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    s_w[0][e * TPR + tid] = dwpost[e] + (v ? s_w[0][e * TPR + tid] : 0.f);
+                    s_w[1][e * TPR + tid] = dwpre[e] + (v ? s_w[1][e * TPR + tid] : 0.f);
+                }
+            }
+            __syncthreads();
+        }
+        if (threadIdx.x >= TPR) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e) { dwpost[e] = s_w[0][e * TPR + tid]; dwpre[e] = s_w[1][e * TPR + tid]; }
+    }
+    PW::store(part, D, tid, dwpost);
+    PW::store(part + D, D, tid, dwpre);
+}
+
+__global__ __launch_bounds__(256) void block_norm_sum_kernel(BlockNormArgs a, int parts)
+{
+    __shared__ float s_sum[4][64];
+    const int i = blockIdx.x * 64 + (threadIdx.x & 63), k = blockIdx.y, w = threadIdx.x >> 6;
+    float* to = k == 0 ? a.dw_post : a.dw_pre;
+    if (to == nullptr) return;
+    float x = 0.f;
+    for (int p = w; p < parts; p += 4) x += a.part[((size_t)p * 2 + k) * a.D + min(i, a.D - 1)];
+    s_sum[w][threadIdx.x & 63] = x;
+    __syncthreads();
+    if (w != 0 || i >= a.D) return;
+    x = 0.f;
+    for (int j = 0; j < 4; ++j) x += s_sum[j][threadIdx.x];
+    to[i] = x;
+}
+
+// -------------------------------------------------------------------------------------------------------------------- host
+static int rows_per_group(int D) { return D <= 1024 ? 4 : 1; }
+
+int block_norm_bwd_parts(long rows, int D)
+{
+    const long sets = (rows + rows_per_group(D) - 1) / rows_per_group(D);
+    return (int)(sets < 1 ? 1 : sets > 1024 ? 1024 : sets);
+}
+
+#define CHELA_ROWS(IO, XT, VEC)                                                                                       \
+    if (a.D <= 512) CHELA_F(IO, XT, 64, 1, VEC);                                                                      \
+    else if (a.D <= 1024) CHELA_F(IO, XT, 64, 2, VEC);                                                                \
+    else if (a.D <= 2048) CHELA_F(IO, XT, 256, 1, VEC);                                                               \
+    else if (a.D <= 4096) CHELA_F(IO, XT, 256, 2, VEC);                                                               \
+    else CHELA_F(IO, XT, 512, 2, VEC);
+#define CHELA_TYPES(VEC)                                                                                              \
+    if (dtype != 0) { CHELA_ROWS(float, float, VEC) }                                                                 \
+    else if (a.x_f32) { CHELA_ROWS(bf16, float, VEC) }                                                                \
+    else { CHELA_ROWS(bf16, bf16, VEC) }
+
+hipError_t launch_block_norm_fwd(const BlockNormArgs& a, int dtype, hipStream_t st)
+{
+    ProfScope prof(KID_BLOCK_NORM, st);
+    const dim3 grid((unsigned)((a.rows + rows_per_group(a.D) - 1) / rows_per_group(a.D)));
+#define CHELA_F(IO, XT, TPR, NV, VEC)                                                                                 \
+    hipLaunchKernelGGL((block_norm_kernel<IO, XT, TPR, NV, VEC>), grid, dim3(TPR < 256 ? 256 : TPR), 0, st, a)
+    if (a.D % 8 == 0) { CHELA_TYPES(true) } else { CHELA_TYPES(false) }
+#undef CHELA_F
+    return hipGetLastError();
+}
+
+hipError_t launch_block_norm_bwd(const BlockNormArgs& a, int dtype, hipStream_t st)
+{
+    ProfScope prof(KID_BLOCK_NORM, st);
+    const int parts = block_norm_bwd_parts(a.rows, a.D);
+    const dim3 grid(parts);
+#define CHELA_F(IO, XT, TPR, NV, VEC)                                                                                 \
+    hipLaunchKernelGGL((block_norm_bwd_kernel<IO, XT, TPR, NV, VEC>), grid, dim3(TPR < 256 ? 256 : TPR), 0, st, a)
+    if (a.D % 8 == 0) { CHELA_TYPES(true) } else { CHELA_TYPES(false) }
+#undef CHELA_F
+    hipLaunchKernelGGL(block_norm_sum_kernel, dim3((a.D + 63) / 64, 2), dim3(256), 0, st, a, parts);
+    return hipGetLastError();
+}
+
+}  // namespace chela

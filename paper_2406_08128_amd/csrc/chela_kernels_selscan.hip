@@ -1,0 +1,773 @@
+// Selective state space scan for gfx950: prompts, gradient, single tokens.
+//
+// Per channel c (of group g) and state n, with dl_t = softplus(delta_t + bias) or delta_t + bias:
+//     h_t[n] = exp(dl_t A[n]) h_{t-1}[n] + dl_t u_t B_t[n],   y_t = sum_n C_t[n] h_t[n] + D u_t,   out_t = y_t silu(z_t).
+// Gradient, with dy_t = dout_t silu(z_t), a_t[n] = exp(dl_t A[n]), q_t[n] = a_t[n] g_t[n] and p_t[n] = a_t[n] h_{t-1}[n]:
+//     g_t[n] = C_t[n] dy_t + q_{t+1}[n]                             (the gradient of h_t)
+//     dC_t[n] = sum_c dy_t h_t[n],   dB_t[n] = sum_c g_t[n] dl_t u_t,   dA[n] = sum_t dl_t g_t[n] p_t[n],   dD = sum_t dy_t u_t
+//     du_t = dl_t sum_n g_t[n] B_t[n] + D dy_t,   d(dl_t) = u_t sum_n g_t[n] B_t[n] + sum_n A[n] g_t[n] p_t[n]
+//     dz_t = dout_t y_t silu'(z_t);  d(delta_t) = d(dl_t) sigmoid(delta_t + bias) under the softplus.
+//
+// All of it is fp32 on the vector ALU: the decay differs from channel to channel and from state to state, so there is no matrix
+// product in it.
+//
+// Split.  A lane owns a channel, a wave 64 of one group.  The rows are cut into chunks wherever the sequences begin and end: a
+// first pass leaves, per chunk, what its rows add to the state behind them (the state itself, if a sequence begins in it) and the sum
+// of its step sizes, of which the chunk's decay is exp(A sum); a chunk's own workgroup then adds up the chunks since the last beginning.
+#include "chela_rows.h"
+
+namespace chela {
+
+struct ScanShape {
+    Rows rows;
+    int D, N, G, Dg, nb;              // channels per group, waves per group
+    int chunk, n_chunk, softplus, same_buffer;
+};
+
+struct ScanFwd {
+    ScanShape s;
+    const void *U, *delta, *Z;
+    long ldu, ldd, ldz;
+    const float *A, *bc, *Dskip, *dbias, *S_in;
+    float *S_out, *saved, *totals, *sums, *fin;
+    int* flags;
+    void* Y;
+};
+
+// The input and output maps of every row as fp32, next to each other: the scans read them through the scalar cache, whatever type,
+// stride or alignment they come with.  Sequences without rows hand their states (or, in the backward call, the states' gradients) on here.
+template <typename IO>
+__global__ __launch_bounds__(256) void selscan_pack_kernel(Rows rows, const IO* __restrict__ Bm, const IO* __restrict__ Cm, long ldb,
+                                                          long ldc, float* __restrict__ bc, const float* S_in, float* S_out, int D,
+                                                          int N, int G)
+{
+    const long n = (long)rows.T * G * 2 * N;
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
+        const int k = (int)(i % (2 * N));
+        const long tg = i / (2 * N), t = tg / G;
+        const int g = (int)(tg % G);
+        bc[i] = k < N ? to_f(Bm[t * ldb + (long)g * N + k]) : to_f(Cm[t * ldc + (long)g * N + k - N]);
+    }
+    if (S_out == nullptr || S_out == S_in) return;
+    for (int s = blockIdx.x; s < rows.n_seq; s += gridDim.x) {
+        if (seq_begin(rows, s) < seq_end(rows, s)) continue;
+        const int slot = slot_of(rows, s);
+        if (slot < 0) continue;
+        const size_t at = (size_t)slot * N * D;
+        for (long i = threadIdx.x; i < (long)N * D; i += 256) S_out[at + i] = S_in ? S_in[at + i] : 0.f;
+    }
+}
+
+// Behind a call that writes its states over those it reads: the sequences that end in another chunk than they begin in.
+__global__ __launch_bounds__(256) void selscan_finish_kernel(ScanShape s, const float* __restrict__ fin, float* __restrict__ S_out)
+{
+    const int c = blockIdx.y, t0 = c * s.chunk;
+    const int q = seq_of(s.rows, t0);
+    if (q < 0 || q >= s.rows.n_seq || seq_begin(s.rows, q) == t0 || seq_end(s.rows, q) > min(t0 + s.chunk, s.rows.T)) return;
+    const int slot = slot_of(s.rows, q);
+    if (slot < 0) return;
+    const long n = (long)s.N * s.D;
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) S_out[(size_t)slot * n + i] = fin[(size_t)c * n + i];
+}
+
+enum { SCAN_TOTALS = 0, SCAN_OUT = 1, SCAN_SAVE = 2 };        // what a walk leaves: the chunks' totals, the output, only the saved states
+constexpr int GT = 8;                                        // rows of a group: loaded together, one group ahead
+
+template <typename IO, int N, int MODE>
+__global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
+{
+    const ScanShape& s = a.s;
+    const Rows& R = s.rows;
+    const int lane = threadIdx.x;
+    const int g = blockIdx.x / s.nb, in_group = (blockIdx.x % s.nb) * 64 + lane;
+    const bool live = in_group < s.Dg;
+    const int ch = g * s.Dg + min(in_group, s.Dg - 1);       // (lanes behind the group's last channel walk that one and leave nothing)
+    const int c = blockIdx.y, t0 = c * s.chunk, t1 = min(t0 + s.chunk, R.T);
+    const size_t ND = (size_t)N * s.D;
+
+    float A2[N], h[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) { A2[n] = a.A[(size_t)n * s.D + ch] * kLog2e; h[n] = 0.f; }
+    const float bias = a.dbias ? a.dbias[ch] : 0.f, skip = a.Dskip ? a.Dskip[ch] : 0.f;
+
+    int q = seq_of(R, t0);                                   // the sequence the walk is in, and its rows
+    if (q < 0) q = 0;
+    int beg = q < R.n_seq ? seq_begin(R, q) : R.T, end = q < R.n_seq ? seq_end(R, q) : R.T;
+    if (MODE != SCAN_TOTALS && c > 0 && beg < t0 && q < R.n_seq) {
+        int k = c - 1;
+        while (k > 0 && a.flags[k] == 0) --k;
+        const float* H = a.totals + (size_t)k * ND + ch;
+#pragma unroll
+        for (int n = 0; n < N; ++n) h[n] = H[(size_t)n * s.D];
+        for (++k; k < c; ++k) {
+            const float sd = a.sums[(size_t)k * s.D + ch];
+            H = a.totals + (size_t)k * ND + ch;
+#pragma unroll
+            for (int n = 0; n < N; ++n) h[n] = fmaf(exp2_(sd * A2[n]), h[n], H[(size_t)n * s.D]);
+        }
+    }
+
+    const IO *U = (const IO*)a.U + ch, *De = (const IO*)a.delta + ch, *Z = a.Z && MODE == SCAN_OUT ? (const IO*)a.Z + ch : nullptr;
+    IO* Y = MODE == SCAN_OUT ? (IO*)a.Y + ch : nullptr;
+    IO nu[GT], nd[GT], nz[GT];
+    auto load = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < GT; ++i) {
+            const long r = min(t + i, R.T - 1);
+            nu[i] = U[r * a.ldu];
+            nd[i] = De[r * a.ldd];
+            if (Z) nz[i] = Z[r * a.ldz];
+        }
+    };
+    float sum = 0.f;
+    bool began = false;
+    auto row = [&](int t, float u, float d, float z) {
+        float dl = d + bias;
+        if (s.softplus) dl = softplus_(dl);
+        const float du = dl * u;
+        const float* bc = a.bc + ((size_t)t * s.G + g) * (2 * N);
+        float y = skip * u;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            h[n] = fmaf(exp2_(dl * A2[n]), h[n], du * bc[n]);
+            if (MODE == SCAN_OUT) y = fmaf(bc[N + n], h[n], y);
+        }
+        if (MODE == SCAN_TOTALS) sum += dl;
+        if (MODE == SCAN_OUT) {
+            if (Z) y *= z * sigmoid_(z);
+            if (live) Y[(size_t)t * s.D] = from_f<IO>(y);
+        }
+    };
+    auto save = [&](int t) {
+        if (MODE == SCAN_TOTALS || a.saved == nullptr || (t & (kSelscanTile - 1)) || !live) return;
+        float* to = a.saved + (size_t)(t / kSelscanTile) * ND + ch;
+#pragma unroll
+        for (int n = 0; n < N; ++n) to[(size_t)n * s.D] = h[n];
+    };
+
+    load(t0);
+    for (int t = t0; t < t1; t += GT) {
+        float u[GT], d[GT], z[GT];
+#pragma unroll
+        for (int i = 0; i < GT; ++i) { u[i] = to_f(nu[i]); d[i] = to_f(nd[i]); z[i] = Z ? to_f(nz[i]) : 0.f; }
+        if (t + GT < t1) load(t + GT);
+        save(t);
+        if (beg < t && t + GT < end && t + GT <= t1) {       // no sequence begins or ends here
+#pragma unroll
+            for (int i = 0; i < GT; ++i) row(t + i, u[i], d[i], z[i]);
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < GT; ++i) {
+            const int r = t + i;
+            while (q < R.n_seq && end <= r) {
+                ++q;
+                if (q < R.n_seq) { beg = seq_begin(R, q); end = seq_end(R, q); }
+            }
+            if (r >= t1 || q >= R.n_seq || r < beg) continue;
+            const int slot = a.S_in || a.S_out ? slot_of(R, q) : -1;
+            if (r == beg) {
+                began = true;
+#pragma unroll
+                for (int n = 0; n < N; ++n) h[n] = a.S_in && slot >= 0 ? a.S_in[(size_t)slot * ND + (size_t)n * s.D + ch] : 0.f;
+            }
+            row(r, u[i], d[i], z[i]);
+            if (MODE == SCAN_OUT && r == end - 1 && a.S_out && slot >= 0 && live) {
+                // (over the states that other workgroups of the sequence may still read: later, by selscan_finish_kernel)
+                float* to = s.same_buffer && beg < t0 ? a.fin + (size_t)c * ND + ch : a.S_out + (size_t)slot * ND + ch;
+#pragma unroll
+                for (int n = 0; n < N; ++n) to[(size_t)n * s.D] = h[n];
+            }
+        }
+    }
+    if (MODE == SCAN_TOTALS && live) {
+        float* H = a.totals + (size_t)c * ND + ch;
+#pragma unroll
+        for (int n = 0; n < N; ++n) H[(size_t)n * s.D] = h[n];
+        a.sums[(size_t)c * s.D + ch] = sum;
+        if (ch == 0) a.flags[c] = began;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- gradient
+struct ScanBwd {
+    ScanShape s;
+    const void *U, *delta, *Z, *dY;
+    long ldu, ldd, ldz, lddy;
+    const float *A, *bc, *Dskip, *dbias, *S_in, *dS_out, *saved;
+    float *dS_in, *totals, *sums, *part_bc, *part_A, *part_D;
+    int* flags;
+    void *dU, *ddelta, *dZ;
+};
+
+// What the rows of a chunk add to q in front of it (q itself, if a sequence ends in it), the walk going from the last row to the first.
+template <typename IO, int N>
+__global__ __launch_bounds__(64) void selscan_bwd_totals_kernel(ScanBwd a)
+{
+    const ScanShape& s = a.s;
+    const Rows& R = s.rows;
+    const int lane = threadIdx.x;
+    const int g = blockIdx.x / s.nb, in_group = (blockIdx.x % s.nb) * 64 + lane;
+    const bool live = in_group < s.Dg;
+    const int ch = g * s.Dg + min(in_group, s.Dg - 1);
+    const int c = blockIdx.y + 1, t0 = c * s.chunk, t1 = min(t0 + s.chunk, R.T);       // (nothing is in front of the first chunk)
+    const size_t ND = (size_t)N * s.D;
+
+    float A2[N], q[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) { A2[n] = a.A[(size_t)n * s.D + ch] * kLog2e; q[n] = 0.f; }
+    const float bias = a.dbias ? a.dbias[ch] : 0.f;
+    const IO *De = (const IO*)a.delta + ch, *dY = (const IO*)a.dY + ch, *Z = a.Z ? (const IO*)a.Z + ch : nullptr;
+    int sq = seq_of(R, t1 - 1), beg = 0, end = 0;
+    if (sq >= R.n_seq) sq = R.n_seq - 1;
+    if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
+    float sum = 0.f;
+    bool ended = false;
+    IO nd[GT], nz[GT], ny[GT];
+    auto load = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < GT; ++i) {
+            const long r = min(t + i, R.T - 1);
+            nd[i] = De[r * a.ldd];
+            ny[i] = dY[r * a.lddy];
+            if (Z) nz[i] = Z[r * a.ldz];
+        }
+    };
+    auto row = [&](int t, float d, float dy, float z) {
+        float dl = d + bias;
+        if (s.softplus) dl = softplus_(dl);
+        if (Z) dy *= z * sigmoid_(z);
+        const float* C = a.bc + ((size_t)t * s.G + g) * (2 * N) + N;
+#pragma unroll
+        for (int n = 0; n < N; ++n) q[n] = exp2_(dl * A2[n]) * fmaf(C[n], dy, q[n]);
+        sum += dl;
+    };
+    const int last = t0 + (t1 - 1 - t0) / GT * GT;
+    load(last);
+    for (int t = last; t >= t0; t -= GT) {
+        float d[GT], z[GT], y[GT];
+#pragma unroll
+        for (int i = 0; i < GT; ++i) { d[i] = to_f(nd[i]); y[i] = to_f(ny[i]); z[i] = Z ? to_f(nz[i]) : 0.f; }
+        if (t > t0) load(t - GT);
+        if (sq >= 0 && beg <= t && t + GT < end && t + GT <= t1) {
+#pragma unroll
+            for (int i = GT - 1; i >= 0; --i) row(t + i, d[i], y[i], z[i]);
+            continue;
+        }
+#pragma unroll
+        for (int i = GT - 1; i >= 0; --i) {
+            const int r = t + i;
+            while (sq >= 0 && beg > r) {
+                --sq;
+                if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
+            }
+            if (r >= t1 || sq < 0 || r >= end) continue;
+            if (r == end - 1) {
+                ended = true;
+                const int slot = slot_of(R, sq);
+#pragma unroll
+                for (int n = 0; n < N; ++n) q[n] = a.dS_out && slot >= 0 ? a.dS_out[(size_t)slot * ND + (size_t)n * s.D + ch] : 0.f;
+            }
+            row(r, d[i], y[i], z[i]);
+        }
+    }
+    if (live) {
+        float* Q = a.totals + (size_t)c * ND + ch;
+#pragma unroll
+        for (int n = 0; n < N; ++n) Q[(size_t)n * s.D] = q[n];
+        a.sums[(size_t)c * s.D + ch] = sum;
+        if (ch == 0) a.flags[c] = ended;
+    }
+}
+
+// Sums of eight values over the wave's lanes: lane l returns the sum of v[(l >> 3 & 7)'s value], see lane_value().
+__device__ __forceinline__ float lanes_swap_add32(float& x, float& y)      // x's sum over l, l + 32 in the lower half, y's in the upper
+{
+    u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float lanes_swap_add16(float x, float y)        // the same for rows of 16 lanes: x's in the even, y's in the odd ones
+{
+    u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x)
+{
+    return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x)
+{
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum8(float (&v)[8], int lane)
+{
+    float r[4], w[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = lanes_swap_add32(v[i], v[i + 4]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) w[i] = lanes_swap_add16(r[i], r[i + 2]);
+    const bool up = lane & 8;
+    const float keep = up ? w[1] : w[0], send = up ? w[0] : w[1];
+    float x = keep + dpp<0x128>(send);            // row_ror:8
+    x = dpp_add<0xB1>(x);                         // quad_perm 1,0,3,2
+    x = dpp_add<0x4E>(x);                         // quad_perm 2,3,0,1
+    return dpp_add<0x141>(x);                     // row_half_mirror
+}
+// Which of sum8()'s values lane l has.
+__device__ __forceinline__ int sum8_index(int lane) { return ((lane >> 3) & 1) + 2 * ((lane >> 4) & 1) + 4 * (lane >> 5); }
+
+constexpr int NPW = 4, TB = kSelscanTile;         // states of a wave, rows of a tile
+
+// A workgroup walks its chunk from the last tile to the first.  Wave w has states 4w .. 4w+3 of the same 64 channels: a tile's
+// decays and states then fit its registers.  The step sizes and the like of a tile are worked out once, by all waves, and shared.
+template <typename IO, int N>
+__global__ __launch_bounds__(N / NPW * 64) void selscan_bwd_kernel(ScanBwd a)
+{
+    constexpr int W = N / NPW, PER = TB / W > 0 ? TB / W : 1;      // waves; rows of a tile that a thread looks after
+    static_assert(TB % W == 0, "");
+    __shared__ float s_dl[TB][64], s_x[TB][64], s_dy[TB][64], s_part[W][3][TB][64];
+    const ScanShape& s = a.s;
+    const Rows& R = s.rows;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int g = blockIdx.x / s.nb, b = blockIdx.x % s.nb, in_group = b * 64 + lane;
+    const bool live = in_group < s.Dg;
+    const int ch = g * s.Dg + min(in_group, s.Dg - 1);
+    const int c = blockIdx.y, t0 = c * s.chunk, t1 = min(t0 + s.chunk, R.T);
+    const size_t ND = (size_t)N * s.D, mine = (size_t)(w * NPW) * s.D + ch;      // of a state's N * D floats, this lane's first
+
+    float A[NPW], A2[NPW], q[NPW], dA[NPW];
+#pragma unroll
+    for (int n = 0; n < NPW; ++n) {
+        A[n] = a.A[mine + (size_t)n * s.D];
+        A2[n] = A[n] * kLog2e;
+        q[n] = dA[n] = 0.f;
+    }
+    const float bias = a.dbias ? a.dbias[ch] : 0.f, skip = a.Dskip ? a.Dskip[ch] : 0.f;
+    const IO *U = (const IO*)a.U + ch, *De = (const IO*)a.delta + ch, *dY = (const IO*)a.dY + ch;
+    const IO* Z = a.Z ? (const IO*)a.Z + ch : nullptr;
+    IO *dU = (IO*)a.dU + ch, *dDe = (IO*)a.ddelta + ch, *dZ = a.Z ? (IO*)a.dZ + ch : nullptr;
+
+    int sq = seq_of(R, t1 - 1), beg = 0, end = 0;
+    const bool inside = sq >= 0 && sq < R.n_seq;
+    if (sq >= R.n_seq) sq = R.n_seq - 1;
+    if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
+    if (inside && end > t1) {                     // the sequence goes on in the chunks behind
+        int k = c + 1;
+        while (k + 1 < s.n_chunk && a.flags[k] == 0) ++k;
+        const float* Q = a.totals + (size_t)k * ND + mine;
+#pragma unroll
+        for (int n = 0; n < NPW; ++n) q[n] = Q[(size_t)n * s.D];
+        for (--k; k > c; --k) {
+            const float sd = a.sums[(size_t)k * s.D + ch];
+            Q = a.totals + (size_t)k * ND + mine;
+#pragma unroll
+            for (int n = 0; n < NPW; ++n) q[n] = fmaf(exp2_(sd * A2[n]), q[n], Q[(size_t)n * s.D]);
+        }
+    }
+
+    IO nu[PER], nd[PER], nz[PER], ny[PER];
+    float nh[NPW];
+    auto load = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const long r = min(t + w + i * W, R.T - 1);
+            nu[i] = U[r * a.ldu];
+            nd[i] = De[r * a.ldd];
+            ny[i] = dY[r * a.lddy];
+            if (Z) nz[i] = Z[r * a.ldz];
+        }
+        const float* from = a.saved + (size_t)(t / TB) * ND + mine;
+#pragma unroll
+        for (int n = 0; n < NPW; ++n) nh[n] = from[(size_t)n * s.D];
+    };
+    float dD = 0.f, dbias = 0.f;
+    const int last = t0 + (t1 - 1 - t0) / TB * TB;
+    load(last);
+    for (int t = last; t >= t0; t -= TB) {
+        float u[PER], x[PER], z[PER], dout[PER], dl[PER], h[NPW];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            u[i] = to_f(nu[i]);
+            x[i] = to_f(nd[i]) + bias;
+            dout[i] = to_f(ny[i]);
+            z[i] = Z ? to_f(nz[i]) : 0.f;
+            dl[i] = s.softplus ? softplus_(x[i]) : x[i];
+            const int k = w + i * W;
+            s_dl[k][lane] = dl[i];
+            s_x[k][lane] = dl[i] * u[i];
+            s_dy[k][lane] = Z ? dout[i] * z[i] * sigmoid_(z[i]) : dout[i];
+        }
+#pragma unroll
+        for (int n = 0; n < NPW; ++n) h[n] = nh[n];
+        if (t > t0) load(t - TB);
+        __syncthreads();
+        const bool whole = sq >= 0 && beg < t && t + TB < end && t + TB <= t1;
+        // forward: p and the decays of the tile
+        float p[TB][NPW], dec[TB][NPW];
+        int fq = sq, fb = beg;                     // (the sequence that the tile's first rows are in)
+        if (!whole) {
+            fq = seq_of(R, t);
+            if (fq < 0) fq = 0;
+            fb = fq < R.n_seq ? seq_begin(R, fq) : R.T;
+        }
+#pragma unroll
+        for (int i = 0; i < TB; ++i) {
+            const int r = t + i;
+            const float* bc = a.bc + ((size_t)min(r, R.T - 1) * s.G + g) * (2 * N) + w * NPW;
+            const float d = s_dl[i][lane], xu = s_x[i][lane];
+            if (!whole) {
+                while (fq < R.n_seq && seq_end(R, fq) <= r) {
+                    ++fq;
+                    fb = fq < R.n_seq ? seq_begin(R, fq) : R.T;
+                }
+                if (fq < R.n_seq && r == fb) {
+                    const int slot = a.S_in ? slot_of(R, fq) : -1;
+#pragma unroll
+                    for (int n = 0; n < NPW; ++n) h[n] = slot >= 0 ? a.S_in[(size_t)slot * ND + mine + (size_t)n * s.D] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NPW; ++n) {
+                dec[i][n] = exp2_(d * A2[n]);
+                p[i][n] = dec[i][n] * h[n];
+                h[n] = fmaf(xu, bc[n], p[i][n]);
+            }
+        }
+        // and back
+        float* part = a.part_bc + (size_t)b * R.T * s.G * (2 * N);
+#pragma unroll
+        for (int i = TB - 1; i >= 0; --i) {
+            const int r = t + i;
+            if (!whole) {
+                while (sq >= 0 && beg > r) {
+                    --sq;
+                    if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
+                }
+                if (r >= t1 || sq < 0 || r >= end) continue;
+                if (r == end - 1) {
+                    const int slot = a.dS_out ? slot_of(R, sq) : -1;
+#pragma unroll
+                    for (int n = 0; n < NPW; ++n) q[n] = slot >= 0 ? a.dS_out[(size_t)slot * ND + mine + (size_t)n * s.D] : 0.f;
+                }
+            }
+            const float* bc = a.bc + ((size_t)r * s.G + g) * (2 * N) + w * NPW;
+            const float d = s_dl[i][lane], xu = s_x[i][lane], dy = s_dy[i][lane];
+            float y = 0.f, s1 = 0.f, s2 = 0.f, v[8];
+#pragma unroll
+            for (int n = 0; n < NPW; ++n) {
+                const float hh = fmaf(xu, bc[n], p[i][n]), gg = fmaf(bc[N + n], dy, q[n]), gp = gg * p[i][n];
+                q[n] = dec[i][n] * gg;
+                y = fmaf(bc[N + n], hh, y);
+                s1 = fmaf(gg, bc[n], s1);
+                s2 = fmaf(A[n], gp, s2);
+                dA[n] = fmaf(d, gp, dA[n]);
+                v[n] = live ? gg * xu : 0.f;
+                v[4 + n] = live ? dy * hh : 0.f;
+            }
+            s_part[w][0][i][lane] = y;
+            s_part[w][1][i][lane] = s1;
+            s_part[w][2][i][lane] = s2;
+            const float total = sum8(v, lane);
+            if ((lane & 7) == 0) {
+                const int k = sum8_index(lane);
+                part[((size_t)r * s.G + g) * (2 * N) + (k >> 2) * N + w * NPW + (k & 3)] = total;
+            }
+            if (!whole && r == beg && a.dS_in && live) {
+                const int slot = slot_of(R, sq);
+                if (slot >= 0) {
+#pragma unroll
+                    for (int n = 0; n < NPW; ++n) a.dS_in[(size_t)slot * ND + mine + (size_t)n * s.D] = q[n];
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int k = w + i * W, r = t + k;
+            if (!whole) {
+                const int sr = r < t1 ? seq_of(R, r) : -1;
+                if (sr < 0 || sr >= R.n_seq) continue;
+            }
+            float y = 0.f, s1 = 0.f, s2 = 0.f;
+#pragma unroll
+            for (int j = 0; j < W; ++j) { y += s_part[j][0][k][lane]; s1 += s_part[j][1][k][lane]; s2 += s_part[j][2][k][lane]; }
+            y = fmaf(skip, u[i], y);
+            float dy = dout[i];
+            if (Z) {
+                const float sg = sigmoid_(z[i]), si = z[i] * sg;
+                dy *= si;
+                if (live) dZ[(size_t)r * s.D] = from_f<IO>(dout[i] * y * (sg + si * (1.f - sg)));
+            }
+            float dd = fmaf(u[i], s1, s2);
+            if (s.softplus) dd *= sigmoid_(x[i]);
+            dD = fmaf(dy, u[i], dD);
+            dbias += dd;
+            if (live) {
+                dU[(size_t)r * s.D] = from_f<IO>(fmaf(dl[i], s1, skip * dy));
+                dDe[(size_t)r * s.D] = from_f<IO>(dd);
+            }
+        }
+        // (the next tile's step sizes are written over this one's only after every wave has passed the barrier above)
+    }
+    __syncthreads();
+    if (live) {
+#pragma unroll
+        for (int n = 0; n < NPW; ++n) a.part_A[(size_t)c * ND + mine + (size_t)n * s.D] = dA[n];
+    }
+    s_part[w][0][0][lane] = dD;
+    s_part[w][1][0][lane] = dbias;
+    __syncthreads();
+    if (w == 0 && live) {
+        float x = 0.f, y = 0.f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) { x += s_part[j][0][0][lane]; y += s_part[j][1][0][lane]; }
+        a.part_D[(size_t)(2 * c) * s.D + ch] = x;
+        a.part_D[(size_t)(2 * c + 1) * s.D + ch] = y;
+    }
+}
+
+// The waves' sums over their channels, added up and rounded once; rows of no sequence are left as they are.
+template <typename IO>
+__global__ __launch_bounds__(256) void selscan_bc_kernel(Rows R, const float* __restrict__ part, int nb, int N, int G, IO* __restrict__ dB,
+                                                        IO* __restrict__ dC)
+{
+    const long n = (long)R.T * G * 2 * N;
+    const long first = R.n_seq > 0 ? (long)seq_begin(R, 0) * G * 2 * N : 0, stop = R.n_seq > 0 ? (long)seq_end(R, R.n_seq - 1) * G * 2 * N : 0;
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
+        if (i < first || i >= stop) continue;
+        float x = 0.f;
+        for (int b = 0; b < nb; ++b) x += part[(size_t)b * n + i];
+        const int k = (int)(i % (2 * N));
+        const long tg = i / (2 * N);
+        if (k < N) dB[tg * N + k] = from_f<IO>(x);
+        else dC[tg * N + k - N] = from_f<IO>(x);
+    }
+}
+
+// The chunks' sums of the parameters' gradients: rows 0 .. N-1 are dA's, N dD's and N+1 the bias's.
+__global__ __launch_bounds__(256) void selscan_params_kernel(const float* __restrict__ part_A, const float* __restrict__ part_D, int n_chunk,
+                                                            int N, int D, float* dA, float* dD, float* dbias)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x, n = blockIdx.y;
+    if (i >= D) return;
+    float* to = n < N ? dA + (size_t)n * D : n == N ? dD : dbias;
+    if (to == nullptr) return;
+    const float* from = n < N ? part_A + (size_t)n * D + i : part_D + (size_t)(n - N) * D + i;
+    const size_t step = n < N ? (size_t)N * D : (size_t)2 * D;
+    float x = 0.f;
+    for (int c = 0; c < n_chunk; ++c) x += from[(size_t)c * step];
+    to[i] = x;
+}
+
+// ------------------------------------------------------------------------------------------------------------ single tokens
+template <typename IO, int N>
+__global__ __launch_bounds__(64) void selscan_step_kernel(SelscanArgs a)
+{
+    const int nb = (a.D + 63) / 64, r = blockIdx.x / nb, Dg = a.D / a.G, ch = blockIdx.x % nb * 64 + threadIdx.x;
+    const int slot = slot_of(a.rows, r);
+    if (slot < 0 || ch >= a.D) return;
+    const int g = ch / Dg;
+    float* S = a.S_out + (size_t)slot * N * a.D + ch;
+    const IO *Bm = (const IO*)a.Bm + (size_t)r * a.ldb + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)r * a.ldc + (size_t)g * N;
+    const float u = to_f(((const IO*)a.U)[(size_t)r * a.ldu + ch]);
+    float dl = to_f(((const IO*)a.delta)[(size_t)r * a.ldd + ch]) + (a.delta_bias ? a.delta_bias[ch] : 0.f);
+    if (a.softplus) dl = softplus_(dl);
+    float y = a.Dskip ? a.Dskip[ch] * u : 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const float h = fmaf(exp2_(dl * kLog2e * a.A[(size_t)n * a.D + ch]), S[(size_t)n * a.D], dl * u * to_f(Bm[n]));
+        S[(size_t)n * a.D] = h;
+        y = fmaf(to_f(Cm[n]), h, y);
+    }
+    if (a.Z) {
+        const float z = to_f(((const IO*)a.Z)[(size_t)r * a.ldz + ch]);
+        y *= z * sigmoid_(z);
+    }
+    ((IO*)a.Y)[(size_t)r * a.D + ch] = from_f<IO>(y);
+}
+
+// -------------------------------------------------------------------------------------------------------------------- host
+bool selscan_states_ok(int N) { return N == 8 || N == 16 || N == 32; }
+
+static int waves_per_group(int D, int G) { return (D / G + 63) / 64; }
+
+// Chunks of whole tiles, as many as give `want` workgroups and no more than 64 of them.
+static void cut_rows(int T, long groups, long want, int* chunk, int* n_chunk)
+{
+    long n = groups > 0 ? (want + groups - 1) / groups : 1;
+    if (n > 64) n = 64;
+    long len = ((long)T + n - 1) / n;
+    len = (len + kSelscanTile - 1) / kSelscanTile * kSelscanTile;
+    if (len < 2 * kSelscanTile) len = 2 * kSelscanTile;
+    *chunk = (int)len;
+    *n_chunk = (int)(((long)T + len - 1) / len);
+}
+
+static SelscanPlan plan_of(int T, int D, int N, int G, bool is_bwd, bool has_saved)
+{
+    SelscanPlan p{};
+    const long groups = (long)G * waves_per_group(D, G);
+    cut_rows(T, groups, is_bwd ? 512 : 2048, &p.chunk, &p.n_chunk);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
+    const size_t ND = (size_t)N * D * sizeof(float);
+    p.bc = take((size_t)T * G * 2 * N * sizeof(float));
+    p.totals = take(ND * p.n_chunk);
+    p.sums = take((size_t)p.n_chunk * D * sizeof(float));
+    p.flags = take((size_t)p.n_chunk * sizeof(int));
+    if (!is_bwd) p.fin = take(ND * p.n_chunk);
+    if (is_bwd) {
+        p.part_bc = take((size_t)waves_per_group(D, G) * T * G * 2 * N * sizeof(float));
+        p.part_A = take(ND * p.n_chunk);
+        p.part_D = take((size_t)2 * p.n_chunk * D * sizeof(float));
+        if (!has_saved) p.saved = take(((size_t)T + kSelscanTile - 1) / kSelscanTile * ND);
+    }
+    p.bytes = at;
+    return p;
+}
+
+SelscanPlan make_selscan_plan(int T, int D, int N, int G, bool is_bwd, bool has_saved)
+{
+    if (T <= 0) return SelscanPlan{};
+    SelscanPlan p = plan_of(T, D, N, G, is_bwd, has_saved);
+    // (the states in front of the tiles are worked out by the forward's walk, with its chunks, before the scratch has anything else in it)
+    if (is_bwd && !has_saved) {
+        const SelscanPlan f = plan_of(T, D, N, G, false, false);
+        p.fin = p.bytes;
+        p.bytes += f.bytes;
+    }
+    return p;
+}
+
+static ScanShape shape_of(const SelscanArgs& a, int chunk, int n_chunk)
+{
+    ScanShape s{};
+    s.rows = a.rows;
+    s.D = a.D; s.N = a.N; s.G = a.G;
+    s.Dg = a.D / a.G;
+    s.nb = waves_per_group(a.D, a.G);
+    s.chunk = chunk; s.n_chunk = n_chunk; s.softplus = a.softplus;
+    return s;
+}
+
+template <typename IO>
+static void pack(const SelscanArgs& a, float* bc, const float* S_in, float* S_out, hipStream_t st)
+{
+    const long n = (long)a.rows.T * a.G * 2 * a.N;
+    long blocks = (n + 255) / 256;
+    if (blocks > 4096) blocks = 4096;
+    if (blocks < 1) blocks = 1;
+    if (S_out && blocks < 64) blocks = 64;
+    hipLaunchKernelGGL(selscan_pack_kernel<IO>, dim3((unsigned)blocks), dim3(256), 0, st, a.rows, (const IO*)a.Bm, (const IO*)a.Cm, a.ldb,
+                       a.ldc, bc, S_in, S_out, a.D, a.N, a.G);
+}
+
+static ScanFwd fwd_of(const SelscanArgs& a, const SelscanPlan& p, char* ws, const float* bc)
+{
+    ScanFwd f{};
+    f.s = shape_of(a, p.chunk, p.n_chunk);
+    f.U = a.U; f.delta = a.delta; f.Z = a.Z;
+    f.ldu = a.ldu; f.ldd = a.ldd; f.ldz = a.ldz;
+    f.A = a.A; f.bc = bc; f.Dskip = a.Dskip; f.dbias = a.delta_bias;
+    f.S_in = a.S_in; f.S_out = a.S_out; f.saved = a.saved;
+    f.totals = (float*)(ws + p.totals); f.sums = (float*)(ws + p.sums); f.flags = (int*)(ws + p.flags); f.fin = (float*)(ws + p.fin);
+    f.Y = a.Y;
+    f.s.same_buffer = a.S_out != nullptr && a.S_out == a.S_in && p.n_chunk > 1;
+    return f;
+}
+
+template <typename IO, int N>
+static void walk(const ScanFwd& f, bool out, hipStream_t st)
+{
+    const unsigned gx = (unsigned)(f.s.G * f.s.nb);
+    if (f.s.n_chunk > 1)
+        hipLaunchKernelGGL((selscan_fwd_kernel<IO, N, SCAN_TOTALS>), dim3(gx, f.s.n_chunk - 1), dim3(64), 0, st, f);
+    if (out) hipLaunchKernelGGL((selscan_fwd_kernel<IO, N, SCAN_OUT>), dim3(gx, f.s.n_chunk), dim3(64), 0, st, f);
+    else hipLaunchKernelGGL((selscan_fwd_kernel<IO, N, SCAN_SAVE>), dim3(gx, f.s.n_chunk), dim3(64), 0, st, f);
+}
+
+template <typename IO, int N>
+static hipError_t fwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, hipStream_t st)
+{
+    float* bc = (float*)(ws + p.bc);
+    ProfScope prof(KID_SELSCAN, st);
+    pack<IO>(a, bc, a.S_in, a.S_out, st);
+    if (a.rows.T > 0) {
+        const ScanFwd f = fwd_of(a, p, ws, bc);
+        walk<IO, N>(f, true, st);
+        if (f.s.same_buffer)
+            hipLaunchKernelGGL(selscan_finish_kernel, dim3((unsigned)(((long)N * a.D + 255) / 256), p.n_chunk), dim3(256), 0, st, f.s,
+                               f.fin, a.S_out);
+    }
+    return hipGetLastError();
+}
+
+template <typename IO, int N>
+static hipError_t bwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, hipStream_t st)
+{
+    ScanBwd b{};
+    float* bc = (float*)(ws + p.bc);
+    ProfScope prof(KID_SELSCAN_BWD, st);
+    pack<IO>(a, bc, a.dS_out, a.dS_in, st);
+    const float* saved = a.saved;
+    if (saved == nullptr && a.rows.T > 0) {
+        SelscanArgs again = a;
+        again.saved = (float*)(ws + p.saved);
+        again.S_out = nullptr;
+        const SelscanPlan fp = plan_of(a.rows.T, a.D, a.N, a.G, false, false);
+        const ScanFwd f = fwd_of(again, fp, ws + p.fin, bc);
+        walk<IO, N>(f, false, st);
+        saved = again.saved;
+    }
+    b.s = shape_of(a, p.chunk, p.n_chunk);
+    b.U = a.U; b.delta = a.delta; b.Z = a.Z; b.dY = a.dY;
+    b.ldu = a.ldu; b.ldd = a.ldd; b.ldz = a.ldz; b.lddy = a.lddy;
+    b.A = a.A; b.bc = bc; b.Dskip = a.Dskip; b.dbias = a.delta_bias; b.S_in = a.S_in; b.dS_out = a.dS_out; b.saved = saved;
+    b.dS_in = a.dS_in;
+    b.totals = (float*)(ws + p.totals); b.sums = (float*)(ws + p.sums); b.flags = (int*)(ws + p.flags);
+    b.part_bc = (float*)(ws + p.part_bc); b.part_A = (float*)(ws + p.part_A); b.part_D = (float*)(ws + p.part_D);
+    b.dU = a.dU; b.ddelta = a.ddelta; b.dZ = a.dZ;
+    const unsigned gx = (unsigned)(b.s.G * b.s.nb);
+    if (p.n_chunk > 1)
+        hipLaunchKernelGGL((selscan_bwd_totals_kernel<IO, N>), dim3(gx, p.n_chunk - 1), dim3(64), 0, st, b);
+    if (a.rows.T > 0) {
+        hipLaunchKernelGGL((selscan_bwd_kernel<IO, N>), dim3(gx, p.n_chunk), dim3(N / NPW * 64), 0, st, b);
+        const long n = (long)a.rows.T * a.G * 2 * N;
+        long blocks = (n + 255) / 256;
+        if (blocks > 8192) blocks = 8192;
+        hipLaunchKernelGGL(selscan_bc_kernel<IO>, dim3((unsigned)blocks), dim3(256), 0, st, a.rows, b.part_bc, b.s.nb, N, a.G, (IO*)a.dB,
+                           (IO*)a.dC);
+    }
+    hipLaunchKernelGGL(selscan_params_kernel, dim3((unsigned)((a.D + 255) / 256), N + 2), dim3(256), 0, st, b.part_A, b.part_D, p.n_chunk, N,
+                       a.D, a.dA, a.dDskip, a.dbias);
+    return hipGetLastError();
+}
+
+#define CHELA_SCAN(F, ...)                                                                                            \
+    if (dtype == 0) switch (a.N) {                                                                                    \
+        case 8: return F<bf16, 8>(__VA_ARGS__);                                                                       \
+        case 16: return F<bf16, 16>(__VA_ARGS__);                                                                     \
+        case 32: return F<bf16, 32>(__VA_ARGS__);                                                                     \
+    } else switch (a.N) {                                                                                             \
+        case 8: return F<float, 8>(__VA_ARGS__);                                                                      \
+        case 16: return F<float, 16>(__VA_ARGS__);                                                                    \
+        case 32: return F<float, 32>(__VA_ARGS__);                                                                    \
+    }                                                                                                                 \
+    return hipErrorInvalidValue;
+
+hipError_t launch_selscan_fwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, int dtype, hipStream_t st) { CHELA_SCAN(fwd, a, p, ws, st) }
+hipError_t launch_selscan_bwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, int dtype, hipStream_t st) { CHELA_SCAN(bwd, a, p, ws, st) }
+
+template <typename IO, int N>
+static hipError_t step(const SelscanArgs& a, hipStream_t st)
+{
+    ProfScope prof(KID_SELSCAN_STEP, st);
+    hipLaunchKernelGGL((selscan_step_kernel<IO, N>), dim3((unsigned)((a.D + 63) / 64) * (unsigned)a.rows.T), dim3(64), 0, st, a);
+    return hipGetLastError();
+}
+hipError_t launch_selscan_step(const SelscanArgs& a, int dtype, hipStream_t st) { CHELA_SCAN(step, a, st) }
+#undef CHELA_SCAN
+
+}  // namespace chela

@@ -1,0 +1,402 @@
+// Short causal convolution on [tokens, channels] rows, gfx950: sequences, gradient, single tokens.
+//
+//     u_t = bias + sum_{j<m} w[j] x_{t-j},  y_t = silu(u_t) or u_t;   x in front of a sequence: its state (the last m - 1 inputs), or 0.
+// Gradient, with du_t = dy_t silu'(u_t) (u_t is worked out again):
+//     dx_t = sum_j w[j] du_{t+j} (rows of the same sequence; the last m - 1 take d(state behind) too, and the state in front is a row like
+//     the others),  dw[j] = sum_t du_t x_{t-j},  dbias = sum_t du_t.
+//
+// Memory-bound: a thread owns V neighbouring channels, 16 bytes of them where the rows allow it, and walks a run of rows with the last
+// m - 1 inputs in registers, so a row is read once (and m - 1 rows more per run, from the L2).
+#include "chela_rows.h"
+
+namespace chela {
+
+template <typename IO, int V>
+__device__ __forceinline__ void load_row(const IO* p, float (&x)[V])
+{
+    if (V == 1) {
+        x[0] = to_f(p[0]);
+    } else if (sizeof(IO) == 2) {
+        const u32x4 t = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            x[2 * i] = __uint_as_float(t[i] << 16);
+            x[2 * i + 1] = __uint_as_float(t[i] & 0xffff0000u);
+        }
+    } else {
+        const u32x4 t = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = __uint_as_float(t[i]);
+    }
+}
+template <typename IO, int V>
+__device__ __forceinline__ void store_row(IO* p, const float (&x)[V])
+{
+    if (V == 1) {
+        p[0] = from_f<IO>(x[0]);
+    } else {
+        struct alignas(16) { IO e[V]; } t;
+#pragma unroll
+        for (int i = 0; i < V; ++i) t.e[i] = from_f<IO>(x[i]);
+        *reinterpret_cast<u32x4*>(p) = *reinterpret_cast<const u32x4*>(&t);
+    }
+}
+
+template <int V>
+__device__ __forceinline__ void activation(const float (&u)[V], int silu, float (&y)[V])
+{
+#pragma unroll
+    for (int e = 0; e < V; ++e) y[e] = silu ? u[e] * sigmoid_(u[e]) : u[e];
+}
+
+// Where in the sequence that row t belongs to: one look-up per run, then by counting.
+struct Where {
+    int q, beg, end;
+    __device__ __forceinline__ void start(const Rows& R, int t)
+    {
+        q = seq_of(R, t);
+        if (q < 0) q = 0;
+        set(R);
+    }
+    __device__ __forceinline__ void set(const Rows& R)
+    {
+        beg = q < R.n_seq ? seq_begin(R, q) : R.T;
+        end = q < R.n_seq ? seq_end(R, q) : R.T;
+    }
+    // false: row t is in no sequence
+    __device__ __forceinline__ bool at(const Rows& R, int t)
+    {
+        while (q < R.n_seq && end <= t) { ++q; set(R); }
+        return q < R.n_seq && t >= beg;
+    }
+};
+
+// The m - 1 inputs in front of row t of the sequence `at`: rows of it, or of its state, or 0.  back[j]: x_{t-1-j}.
+template <typename IO, int V, int M>
+__device__ __forceinline__ void history(const ShortConvArgs& a, const Where& at, int t, int ch, float (&back)[M > 1 ? M - 1 : 1][V])
+{
+    int slot = -2;
+#pragma unroll
+    for (int j = 0; j < M - 1; ++j) {
+        const int r = t - 1 - j;
+#pragma unroll
+        for (int e = 0; e < V; ++e) back[j][e] = 0.f;
+        if (r >= at.beg) {
+            load_row<IO, V>((const IO*)a.X + (size_t)r * a.ldx + ch, back[j]);
+        } else if (a.S_in) {
+            if (slot == -2) slot = slot_of(a.rows, at.q);
+            if (slot >= 0) load_row<IO, V>((const IO*)a.S_in + ((size_t)slot * (M - 1) + (M - 1 + r - at.beg)) * a.D + ch, back[j]);
+        }
+    }
+}
+
+template <int V, int M>
+__device__ __forceinline__ void weights(const ShortConvArgs& a, int ch, float (&w)[M][V], float (&bias)[V])
+{
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+#pragma unroll
+        for (int j = 0; j < M; ++j) w[j][e] = a.w[(size_t)(ch + e) * M + j];
+        bias[e] = a.bias ? a.bias[ch + e] : 0.f;
+    }
+}
+
+template <typename IO, int V, int M, int RUN>
+__global__ __launch_bounds__(256) void short_conv_kernel(ShortConvArgs a)
+{
+    const int across = (a.D + V * (int)blockDim.x - 1) / (V * (int)blockDim.x);          // workgroups that a run takes
+    const int ch = (blockIdx.x % across * blockDim.x + threadIdx.x) * V;
+    if (ch >= a.D) return;
+    const Rows& R = a.rows;
+    float w[M][V], bias[V], back[M > 1 ? M - 1 : 1][V];
+    weights<V, M>(a, ch, w, bias);
+    const int t0 = blockIdx.x / across * RUN, t1 = min(t0 + RUN, R.T);
+    Where at;
+    at.start(R, t0);
+    int known = -1;                                   // the sequence that `back` is of
+#pragma unroll 4
+    for (int t = t0; t < t1; ++t) {
+        if (!at.at(R, t)) continue;
+        if (known != at.q) { history<IO, V, M>(a, at, t, ch, back); known = at.q; }
+        float x[V], u[V], y[V];
+        load_row<IO, V>((const IO*)a.X + (size_t)t * a.ldx + ch, x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            u[e] = fmaf(w[0][e], x[e], bias[e]);
+#pragma unroll
+            for (int j = 1; j < M; ++j) u[e] = fmaf(w[j][e], back[j - 1][e], u[e]);
+        }
+        activation<V>(u, a.silu, y);
+        store_row<IO, V>((IO*)a.Y + (size_t)t * a.D + ch, y);
+#pragma unroll
+        for (int j = M - 2; j > 0; --j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) back[j][e] = back[j - 1][e];
+        if (M > 1)
+#pragma unroll
+            for (int e = 0; e < V; ++e) back[0][e] = x[e];
+    }
+}
+
+// The states behind the sequences.  A kernel of its own: over the states in front it has to come when those have been read, and a
+// thread reads all m - 1 rows of its channels before it writes one.
+template <typename IO, int M>
+__global__ __launch_bounds__(256) void short_conv_state_kernel(ShortConvArgs a)
+{
+    const int nb = (a.D + 255) / 256, q = blockIdx.x / nb, ch = blockIdx.x % nb * 256 + threadIdx.x;
+    if (ch >= a.D) return;
+    const int slot = slot_of(a.rows, q);
+    if (slot < 0) return;
+    Where at;
+    at.q = q;
+    at.set(a.rows);
+    if (at.end < at.beg) at.end = at.beg;
+    float back[M > 1 ? M - 1 : 1][1];
+    history<IO, 1, M>(a, at, at.end, ch, back);
+#pragma unroll
+    for (int j = 0; j < M - 1; ++j) ((IO*)a.S_out)[((size_t)slot * (M - 1) + (M - 2 - j)) * a.D + ch] = from_f<IO>(back[j][0]);
+}
+
+// One row for each of R requests: the states move on by one.
+template <typename IO, int V, int M>
+__global__ __launch_bounds__(64) void short_conv_step_kernel(ShortConvArgs a)
+{
+    const int nb = (a.D + 64 * V - 1) / (64 * V), r = blockIdx.x / nb, ch = (blockIdx.x % nb * 64 + threadIdx.x) * V;
+    if (ch >= a.D) return;
+    const int slot = slot_of(a.rows, r);
+    if (slot < 0) return;
+    IO* S = (IO*)a.S_out + (size_t)slot * (M - 1) * a.D + ch;
+    float w[M][V], bias[V], s[M > 1 ? M - 1 : 1][V], x[V], u[V], y[V];
+    load_row<IO, V>((const IO*)a.X + (size_t)r * a.ldx + ch, x);
+#pragma unroll
+    for (int j = 0; j < M - 1; ++j) load_row<IO, V>(S + (size_t)j * a.D, s[j]);
+    weights<V, M>(a, ch, w, bias);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        u[e] = fmaf(w[0][e], x[e], bias[e]);
+#pragma unroll
+        for (int j = 1; j < M; ++j) u[e] = fmaf(w[j][e], s[M - 1 - j][e], u[e]);
+    }
+    activation<V>(u, a.silu, y);
+    store_row<IO, V>((IO*)a.Y + (size_t)r * a.D + ch, y);
+#pragma unroll
+    for (int j = 0; j < M - 2; ++j) store_row<IO, V>(S + (size_t)j * a.D, s[j + 1]);
+    if (M > 1) store_row<IO, V>(S + (size_t)(M - 2) * a.D, x);
+}
+
+// Gradient.  A workgroup walks runs of rows; the sums of dw and dbias stay in its threads' registers and leave once, per workgroup, for
+// short_conv_sum_kernel to add up in a fixed order.  pend[k]: what dx of row t - k has so far.
+template <typename IO, int V, int M, int RUN>
+__global__ __launch_bounds__(256) void short_conv_bwd_kernel(ShortConvArgs a, int runs)
+{
+    const int ch = (blockIdx.x * blockDim.x + threadIdx.x) * V;
+    if (ch >= a.D) return;
+    const Rows& R = a.rows;
+    float w[M][V], bias[V], dw[M][V], db[V];
+    weights<V, M>(a, ch, w, bias);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        db[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < M; ++j) dw[j][e] = 0.f;
+    }
+    for (int run = blockIdx.y; run < runs; run += gridDim.y) {
+        const int t0 = run * RUN, t1 = min(t0 + RUN, R.T);
+        float back[M > 1 ? M - 1 : 1][V], pend[M][V];
+        Where at;
+        at.start(R, t0);
+        int known = -1;
+        // rows t1 .. t1 + m - 2 of the same sequence give to the rows of this run too
+        for (int t = t0; t - t1 < M - 1; ++t) {
+            if (t >= R.T || (t >= t1 && (known != at.q || t >= at.end))) break;
+            if (t < t1 && !at.at(R, t)) continue;
+            if (known != at.q) {
+                known = at.q;
+                history<IO, V, M>(a, at, t, ch, back);
+#pragma unroll
+                for (int k = 0; k < M; ++k)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) pend[k][e] = 0.f;
+            }
+            float x[V], dy[V], u[V];
+            load_row<IO, V>((const IO*)a.X + (size_t)t * a.ldx + ch, x);
+            load_row<IO, V>((const IO*)a.dY + (size_t)t * a.lddy + ch, dy);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                u[e] = fmaf(w[0][e], x[e], bias[e]);
+#pragma unroll
+                for (int j = 1; j < M; ++j) u[e] = fmaf(w[j][e], back[j - 1][e], u[e]);
+                float du = dy[e];
+                if (a.silu) {
+                    const float s = sigmoid_(u[e]);
+                    du *= s * fmaf(u[e], 1.f - s, 1.f);
+                }
+#pragma unroll
+                for (int j = 0; j < M; ++j) pend[j][e] = fmaf(w[j][e], du, pend[j][e]);
+                if (t < t1) {
+                    db[e] += du;
+                    dw[0][e] = fmaf(du, x[e], dw[0][e]);
+#pragma unroll
+                    for (int j = 1; j < M; ++j) dw[j][e] = fmaf(du, back[j - 1][e], dw[j][e]);
+                }
+            }
+            // what is complete: row t - (m - 1); behind the sequence's last row, all that are left
+            auto leave = [&](int k) {
+                const int r = t - k, behind = r - (at.end - (M - 1));        // place in the state behind the sequence
+                if (r >= at.beg ? (r < t0 || r >= t1) : (!a.dS_in || at.beg < t0 || at.beg >= t1 || r < at.beg - (M - 1))) return;
+                float g[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) g[e] = pend[k][e];
+                const int slot = (r < at.beg || (a.dS_out && behind >= 0)) ? slot_of(R, at.q) : -1;
+                if (a.dS_out && behind >= 0 && slot >= 0) {
+                    float d[V];
+                    load_row<IO, V>((const IO*)a.dS_out + ((size_t)slot * (M - 1) + behind) * a.D + ch, d);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) g[e] += d[e];
+                }
+                if (r >= at.beg) store_row<IO, V>((IO*)a.dX + (size_t)r * a.D + ch, g);
+                else if (slot >= 0) store_row<IO, V>((IO*)a.dS_in + ((size_t)slot * (M - 1) + (M - 1 + r - at.beg)) * a.D + ch, g);
+            };
+            leave(M - 1);
+            if (t == at.end - 1) {
+#pragma unroll
+                for (int k = M - 2; k >= 0; --k) leave(k);
+            }
+#pragma unroll
+            for (int j = M - 2; j > 0; --j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) back[j][e] = back[j - 1][e];
+#pragma unroll
+            for (int j = M - 1; j > 0; --j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) pend[j][e] = pend[j - 1][e];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                pend[0][e] = 0.f;
+                if (M > 1) back[0][e] = x[e];
+            }
+        }
+    }
+    float* part = a.part + (size_t)blockIdx.y * (M + 1) * a.D + ch;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+#pragma unroll
+        for (int j = 0; j < M; ++j) part[(size_t)j * a.D + e] = dw[j][e];
+        part[(size_t)M * a.D + e] = db[e];
+    }
+}
+
+__global__ __launch_bounds__(256) void short_conv_sum_kernel(ShortConvArgs a, int parts)
+{
+    __shared__ float s_sum[4][64];
+    const int ch = blockIdx.x * 64 + (threadIdx.x & 63), j = blockIdx.y, w = threadIdx.x >> 6;
+    const int c = min(ch, a.D - 1);
+    float x = 0.f;
+    for (int p = w; p < parts; p += 4) x += a.part[((size_t)p * (a.m + 1) + j) * a.D + c];
+    s_sum[w][threadIdx.x & 63] = x;
+    __syncthreads();
+    if (w != 0 || ch >= a.D) return;
+    x = 0.f;
+    for (int i = 0; i < 4; ++i) x += s_sum[i][threadIdx.x];
+    if (j < a.m) a.dw[(size_t)ch * a.m + j] = x;
+    else if (a.dbias) a.dbias[ch] = x;
+}
+
+// Sequences without rows hand the state's gradient on.
+template <typename IO>
+__global__ __launch_bounds__(256) void short_conv_empty_kernel(ShortConvArgs a)
+{
+    for (int s = blockIdx.x; s < a.rows.n_seq; s += gridDim.x) {
+        if (seq_begin(a.rows, s) < seq_end(a.rows, s)) continue;
+        const int slot = slot_of(a.rows, s);
+        if (slot < 0) continue;
+        const size_t n = (size_t)(a.m - 1) * a.D, at = n * slot;
+        for (size_t i = threadIdx.x; i < n; i += 256) ((IO*)a.dS_in)[at + i] = a.dS_out ? ((const IO*)a.dS_out)[at + i] : (IO)0.f;
+    }
+}
+
+// -------------------------------------------------------------------------------------------------------------------- host
+// 16 bytes of a row per thread, where every row begins on 16 bytes
+static bool wide(const ShortConvArgs& a, int dtype)
+{
+    const int V = dtype == 0 ? 8 : 4;
+    return a.D % V == 0 && a.ldx % V == 0 && a.lddy % V == 0 && (((uintptr_t)a.X | (uintptr_t)a.dY) & 15u) == 0;
+}
+static unsigned threads_for(int vectors) { return vectors >= 256 ? 256u : (unsigned)(vectors + 63) / 64 * 64; }
+
+#define CHELA_TAPS(F, IO, V)                                                                                          \
+    switch (a.m) {                                                                                                    \
+        case 1: F(IO, V, 1); break;                                                                                   \
+        case 2: F(IO, V, 2); break;                                                                                   \
+        case 3: F(IO, V, 3); break;                                                                                   \
+        case 4: F(IO, V, 4); break;                                                                                   \
+        case 5: F(IO, V, 5); break;                                                                                   \
+        case 6: F(IO, V, 6); break;                                                                                   \
+        case 7: F(IO, V, 7); break;                                                                                   \
+        case 8: F(IO, V, 8); break;                                                                                   \
+        default: return hipErrorInvalidValue;                                                                         \
+    }
+#define CHELA_TYPES(F)                                                                                                \
+    if (dtype == 0) { if (wide(a, dtype)) { CHELA_TAPS(F, bf16, 8) } else { CHELA_TAPS(F, bf16, 1) } }                \
+    else { if (wide(a, dtype)) { CHELA_TAPS(F, float, 4) } else { CHELA_TAPS(F, float, 1) } }
+
+constexpr int kRun = 16, kBwdRun = 32;
+
+hipError_t launch_short_conv_fwd(const ShortConvArgs& a, int dtype, hipStream_t st)
+{
+    ProfScope prof(KID_SHORT_CONV, st);
+    if (a.rows.T > 0) {
+        const int V = wide(a, dtype) ? (dtype == 0 ? 8 : 4) : 1, vectors = (a.D + V - 1) / V;
+        const unsigned threads = threads_for(vectors);
+        const dim3 grid(((vectors + threads - 1) / threads) * (unsigned)((a.rows.T + kRun - 1) / kRun));
+#define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_kernel<IO, V, M, kRun>), grid, dim3(threads), 0, st, a)
+        CHELA_TYPES(CHELA_F)
+#undef CHELA_F
+    }
+    if (a.S_out && a.m > 1 && a.rows.n_seq > 0) {
+        const dim3 grid((unsigned)((a.D + 255) / 256) * (unsigned)a.rows.n_seq);
+#define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_state_kernel<IO, M>), grid, dim3(256), 0, st, a)
+        if (dtype == 0) { CHELA_TAPS(CHELA_F, bf16, 1) } else { CHELA_TAPS(CHELA_F, float, 1) }
+#undef CHELA_F
+    }
+    return hipGetLastError();
+}
+
+int short_conv_bwd_parts(int T, int D, int dtype)
+{
+    (void)D; (void)dtype;
+    const int runs = (T + kBwdRun - 1) / kBwdRun;
+    return runs < 512 ? (runs > 0 ? runs : 1) : 512;
+}
+
+hipError_t launch_short_conv_bwd(const ShortConvArgs& a, int dtype, hipStream_t st)
+{
+    ProfScope prof(KID_SHORT_CONV, st);
+    const int V = wide(a, dtype) ? (dtype == 0 ? 8 : 4) : 1, vectors = (a.D + V - 1) / V;
+    const unsigned threads = threads_for(vectors);
+    const int runs = (a.rows.T + kBwdRun - 1) / kBwdRun, parts = short_conv_bwd_parts(a.rows.T, a.D, dtype);
+    const dim3 grid((vectors + threads - 1) / threads, parts);
+#define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_bwd_kernel<IO, V, M, kBwdRun>), grid, dim3(threads), 0, st, a, runs)
+    CHELA_TYPES(CHELA_F)
+#undef CHELA_F
+    hipLaunchKernelGGL(short_conv_sum_kernel, dim3((a.D + 63) / 64, a.m + 1), dim3(256), 0, st, a, parts);
+    if (a.dS_in && a.m > 1 && (a.rows.cu || a.rows.T == 0)) {
+        const dim3 g(a.rows.n_seq < 256 ? a.rows.n_seq : 256);
+        if (dtype == 0) hipLaunchKernelGGL(short_conv_empty_kernel<bf16>, g, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL(short_conv_empty_kernel<float>, g, dim3(256), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_short_conv_step(const ShortConvArgs& a, int dtype, hipStream_t st)
+{
+    ProfScope prof(KID_SHORT_CONV, st);
+    const int V = wide(a, dtype) ? (dtype == 0 ? 8 : 4) : 1, nb = (a.D + 64 * V - 1) / (64 * V);
+    const dim3 grid((unsigned)nb * (unsigned)a.rows.T);
+#define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_step_kernel<IO, V, M>), grid, dim3(64), 0, st, a)
+    CHELA_TYPES(CHELA_F)
+#undef CHELA_F
+    return hipGetLastError();
+}
+
+}  // namespace chela
