@@ -13,8 +13,10 @@
 //
 // Split.  A lane owns a channel, a wave 64 of one group.  The rows are cut into chunks wherever the sequences begin and end: a
 // first pass leaves, per chunk, what its rows add to the state behind them (the state itself, if a sequence begins in it) and the sum
-// of its step sizes, of which the chunk's decay is exp(A sum); a chunk's own workgroup then adds up the chunks since the last beginning.
+// of its step sizes, of which the chunk's decay is exp(A sum); a second one makes the state in front of each chunk of these, and a third
+// walks the chunks.
 #include "chela_rows.h"
+#include <type_traits>
 
 namespace chela {
 
@@ -26,35 +28,22 @@ struct ScanShape {
 
 struct ScanFwd {
     ScanShape s;
-    const void *U, *delta, *Z;
-    long ldu, ldd, ldz;
-    const float *A, *bc, *Dskip, *dbias, *S_in;
+    const void *U, *delta, *Z, *Bm, *Cm;
+    long ldu, ldd, ldz, ldb, ldc;
+    const float *A, *Dskip, *dbias, *S_in;
     float *S_out, *saved, *totals, *sums, *fin;
     int* flags;
     void* Y;
 };
 
-// The input and output maps of every row as fp32, next to each other: the scans read them through the scalar cache, whatever type,
-// stride or alignment they come with.  Sequences without rows hand their states (or, in the backward call, the states' gradients) on here.
-template <typename IO>
-__global__ __launch_bounds__(256) void selscan_pack_kernel(Rows rows, const IO* __restrict__ Bm, const IO* __restrict__ Cm, long ldb,
-                                                          long ldc, float* __restrict__ bc, const float* S_in, float* S_out, int D,
-                                                          int N, int G)
+// Sequences without rows hand their states (or, in the backward call, the states' gradients) on.
+__global__ __launch_bounds__(256) void selscan_empty_kernel(Rows rows, const float* from, float* to, long n)
 {
-    const long n = (long)rows.T * G * 2 * N;
-    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
-        const int k = (int)(i % (2 * N));
-        const long tg = i / (2 * N), t = tg / G;
-        const int g = (int)(tg % G);
-        bc[i] = k < N ? to_f(Bm[t * ldb + (long)g * N + k]) : to_f(Cm[t * ldc + (long)g * N + k - N]);
-    }
-    if (S_out == nullptr || S_out == S_in) return;
     for (int s = blockIdx.x; s < rows.n_seq; s += gridDim.x) {
         if (seq_begin(rows, s) < seq_end(rows, s)) continue;
         const int slot = slot_of(rows, s);
         if (slot < 0) continue;
-        const size_t at = (size_t)slot * N * D;
-        for (long i = threadIdx.x; i < (long)N * D; i += 256) S_out[at + i] = S_in ? S_in[at + i] : 0.f;
+        for (long i = threadIdx.x; i < n; i += 256) to[slot * n + i] = from ? from[slot * n + i] : 0.f;
     }
 }
 
@@ -70,18 +59,77 @@ __global__ __launch_bounds__(256) void selscan_finish_kernel(ScanShape s, const 
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) S_out[(size_t)slot * n + i] = fin[(size_t)c * n + i];
 }
 
+// The chunks' totals turned into what each chunk begins with, in place, in order (forward: from the first chunk on, state and decay; backward:
+// from the last chunk on).  A chunk with its flag set has a sequence's beginning (end) in it: what comes to it ends there.
+template <bool BWD>
+__global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restrict__ A, float* __restrict__ totals,
+                                                           const float* __restrict__ sums, const int* __restrict__ flags, int n_chunk, int D, long ND)
+{
+    const long i = (long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= ND) return;
+    const int ch = (int)(i % D);
+    const float A2 = A[i] * kLog2e;
+    float h = 0.f;
+    constexpr int AT = 8;                            // chunks whose totals are read together
+    for (int k = 0; k < n_chunk; k += AT) {
+        float H[AT], sd[AT];
+        int f[AT];
+#pragma unroll
+        for (int j = 0; j < AT; ++j) {
+            const int c = BWD ? n_chunk - 1 - min(k + j, n_chunk - 1) : min(k + j, n_chunk - 1);
+            // (the chunk that nothing comes behind has no totals)
+            const bool there = BWD ? c > 0 : c < n_chunk - 1;
+            H[j] = there ? totals[(size_t)c * ND + i] : 0.f;
+            sd[j] = there ? sums[(size_t)c * D + ch] : 0.f;
+            f[j] = there ? flags[c] : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < AT; ++j) {
+            if (k + j >= n_chunk) break;
+            const int c = BWD ? n_chunk - 1 - (k + j) : k + j;
+            totals[(size_t)c * ND + i] = h;
+            h = f[j] ? H[j] : fmaf(exp2_(sd[j] * A2), h, H[j]);
+        }
+    }
+}
+
 enum { SCAN_TOTALS = 0, SCAN_OUT = 1, SCAN_SAVE = 2 };        // what a walk leaves: the chunks' totals, the output, only the saved states
 constexpr int GT = 8;                                        // rows of a group: loaded together, one group ahead
+
+// A group's input and output maps: each lane loads N / 4 of its GT * 2N values, wherever they lie, and puts them into LDS as fp32, from where
+// every lane reads those of a row at one address.  (Through the scalar cache each row waited for them, and a scalar operand halves an
+// instruction's rate.)
+template <typename IO, int N>
+struct Maps {
+    static constexpr int PER = N / 4;
+    IO v[PER];
+    __device__ __forceinline__ void load(const IO* Bm, const IO* Cm, long ldb, long ldc, int t, int last, int lane)
+    {
+        const long r = min(t + (lane >> 3), last);
+        const int k = (lane & 3) * PER;
+        const IO* p = lane & 4 ? Cm + r * ldc + k : Bm + r * ldb + k;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = p[i];
+    }
+    __device__ __forceinline__ void put(float (*to)[2 * N], int lane) const
+    {
+        float* p = &to[lane >> 3][(lane & 7) * PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) p[i] = to_f(v[i]);
+    }
+};
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
 template <typename IO, int N, int MODE>
 __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
 {
+    __shared__ __align__(16) float s_bc[2][GT][2 * N];
     const ScanShape& s = a.s;
     const Rows& R = s.rows;
     const int lane = threadIdx.x;
-    const int g = blockIdx.x / s.nb, in_group = (blockIdx.x % s.nb) * 64 + lane;
-    const bool live = in_group < s.Dg;
-    const int ch = g * s.Dg + min(in_group, s.Dg - 1);       // (lanes behind the group's last channel walk that one and leave nothing)
+    const int g = blockIdx.x / s.nb;
+    const unsigned ch = g * s.Dg + min((int)(blockIdx.x % s.nb) * 64 + lane, s.Dg - 1);
+    // (lanes behind the group's last channel do what that one's lane does, and leave the same values in the same places)
     const int c = blockIdx.y, t0 = c * s.chunk, t1 = min(t0 + s.chunk, R.T);
     const size_t ND = (size_t)N * s.D;
 
@@ -94,70 +142,70 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
     if (q < 0) q = 0;
     int beg = q < R.n_seq ? seq_begin(R, q) : R.T, end = q < R.n_seq ? seq_end(R, q) : R.T;
     if (MODE != SCAN_TOTALS && c > 0 && beg < t0 && q < R.n_seq) {
-        int k = c - 1;
-        while (k > 0 && a.flags[k] == 0) --k;
-        const float* H = a.totals + (size_t)k * ND + ch;
+        const float* H = a.totals + (size_t)c * ND + ch;
 #pragma unroll
         for (int n = 0; n < N; ++n) h[n] = H[(size_t)n * s.D];
-        for (++k; k < c; ++k) {
-            const float sd = a.sums[(size_t)k * s.D + ch];
-            H = a.totals + (size_t)k * ND + ch;
-#pragma unroll
-            for (int n = 0; n < N; ++n) h[n] = fmaf(exp2_(sd * A2[n]), h[n], H[(size_t)n * s.D]);
-        }
     }
 
-    const IO *U = (const IO*)a.U + ch, *De = (const IO*)a.delta + ch, *Z = a.Z && MODE == SCAN_OUT ? (const IO*)a.Z + ch : nullptr;
-    IO* Y = MODE == SCAN_OUT ? (IO*)a.Y + ch : nullptr;
+    // (a row's address is the same in all lanes: scalar base, 32-bit lane offset)
+    const IO *U = (const IO*)a.U, *De = (const IO*)a.delta, *Z = MODE == SCAN_OUT ? (const IO*)a.Z : nullptr;
+    const IO *Bm = (const IO*)a.Bm + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)g * N;
+    IO* Y = (IO*)a.Y;
     IO nu[GT], nd[GT], nz[GT];
+    Maps<IO, N> maps;
     auto load = [&](int t) {
 #pragma unroll
         for (int i = 0; i < GT; ++i) {
             const long r = min(t + i, R.T - 1);
-            nu[i] = U[r * a.ldu];
-            nd[i] = De[r * a.ldd];
-            if (Z) nz[i] = Z[r * a.ldz];
+            nu[i] = (U + r * a.ldu)[ch];
+            nd[i] = (De + r * a.ldd)[ch];
+            if (Z) nz[i] = (Z + r * a.ldz)[ch];
         }
+        if (MODE == SCAN_OUT || (lane & 4) == 0) maps.load(Bm, Cm, a.ldb, a.ldc, t, R.T - 1, lane);
     };
     float sum = 0.f;
     bool began = false;
-    auto row = [&](int t, float u, float d, float z) {
-        float dl = d + bias;
-        if (s.softplus) dl = softplus_(dl);
+    auto row = [&](int t, const float* bc, float dl, float u, float gate) {
         const float du = dl * u;
-        const float* bc = a.bc + ((size_t)t * s.G + g) * (2 * N);
-        float y = skip * u;
+        float y[2] = {skip * u, 0.f};
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             h[n] = fmaf(exp2_(dl * A2[n]), h[n], du * bc[n]);
-            if (MODE == SCAN_OUT) y = fmaf(bc[N + n], h[n], y);
+            if (MODE == SCAN_OUT) y[n & 1] = fmaf(bc[N + n], h[n], y[n & 1]);
         }
         if (MODE == SCAN_TOTALS) sum += dl;
-        if (MODE == SCAN_OUT) {
-            if (Z) y *= z * sigmoid_(z);
-            if (live) Y[(size_t)t * s.D] = from_f<IO>(y);
-        }
-    };
-    auto save = [&](int t) {
-        if (MODE == SCAN_TOTALS || a.saved == nullptr || (t & (kSelscanTile - 1)) || !live) return;
-        float* to = a.saved + (size_t)(t / kSelscanTile) * ND + ch;
-#pragma unroll
-        for (int n = 0; n < N; ++n) to[(size_t)n * s.D] = h[n];
+        if (MODE == SCAN_OUT) (Y + (size_t)t * s.D)[ch] = from_f<IO>((y[0] + y[1]) * gate);
     };
 
     load(t0);
     for (int t = t0; t < t1; t += GT) {
-        float u[GT], d[GT], z[GT];
+        float u[GT], dl[GT], gate[GT];
+        float(*bc)[2 * N] = s_bc[(t / GT) & 1];
 #pragma unroll
-        for (int i = 0; i < GT; ++i) { u[i] = to_f(nu[i]); d[i] = to_f(nd[i]); z[i] = Z ? to_f(nz[i]) : 0.f; }
+        for (int i = 0; i < GT; ++i) { u[i] = to_f(nu[i]); dl[i] = to_f(nd[i]) + bias; gate[i] = Z ? to_f(nz[i]) : 1.f; }
+        if (MODE == SCAN_OUT || (lane & 4) == 0) maps.put(bc, lane);
+        wave_fence();
         if (t + GT < t1) load(t + GT);
-        save(t);
+        if (s.softplus)
+#pragma unroll
+            for (int i = 0; i < GT; ++i) dl[i] = softplus_(dl[i]);
+        if (Z)
+#pragma unroll
+            for (int i = 0; i < GT; ++i) gate[i] *= sigmoid_(gate[i]);
+        if (MODE != SCAN_TOTALS && a.saved && (t & (kSelscanTile - 1)) == 0) {
+            float* to = a.saved + (size_t)(t / kSelscanTile) * ND;
+#pragma unroll
+            for (int n = 0; n < N; ++n) (to + (size_t)n * s.D)[ch] = h[n];
+        }
         if (beg < t && t + GT < end && t + GT <= t1) {       // no sequence begins or ends here
 #pragma unroll
-            for (int i = 0; i < GT; ++i) row(t + i, u[i], d[i], z[i]);
+            for (int i = 0; i < GT; ++i) {
+                row(t + i, bc[i], dl[i], u[i], gate[i]);
+                __builtin_amdgcn_sched_barrier(0);           // (or all rows' maps are read into registers first)
+            }
             continue;
         }
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < GT; ++i) {
             const int r = t + i;
             while (q < R.n_seq && end <= r) {
@@ -171,8 +219,11 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
 #pragma unroll
                 for (int n = 0; n < N; ++n) h[n] = a.S_in && slot >= 0 ? a.S_in[(size_t)slot * ND + (size_t)n * s.D + ch] : 0.f;
             }
-            row(r, u[i], d[i], z[i]);
-            if (MODE == SCAN_OUT && r == end - 1 && a.S_out && slot >= 0 && live) {
+            float ui = u[0], di = dl[0], gi = gate[0];
+#pragma unroll
+            for (int j = 1; j < GT; ++j) if (i == j) { ui = u[j]; di = dl[j]; gi = gate[j]; }
+            row(r, bc[i], di, ui, gi);
+            if (MODE == SCAN_OUT && r == end - 1 && a.S_out && slot >= 0) {
                 // (over the states that other workgroups of the sequence may still read: later, by selscan_finish_kernel)
                 float* to = s.same_buffer && beg < t0 ? a.fin + (size_t)c * ND + ch : a.S_out + (size_t)slot * ND + ch;
 #pragma unroll
@@ -180,7 +231,7 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
             }
         }
     }
-    if (MODE == SCAN_TOTALS && live) {
+    if (MODE == SCAN_TOTALS) {
         float* H = a.totals + (size_t)c * ND + ch;
 #pragma unroll
         for (int n = 0; n < N; ++n) H[(size_t)n * s.D] = h[n];
@@ -192,9 +243,9 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
 // ---------------------------------------------------------------------------------------------------------------- gradient
 struct ScanBwd {
     ScanShape s;
-    const void *U, *delta, *Z, *dY;
-    long ldu, ldd, ldz, lddy;
-    const float *A, *bc, *Dskip, *dbias, *S_in, *dS_out, *saved;
+    const void *U, *delta, *Z, *dY, *Bm, *Cm;
+    long ldu, ldd, ldz, lddy, ldb, ldc;
+    const float *A, *Dskip, *dbias, *S_in, *dS_out, *saved;
     float *dS_in, *totals, *sums, *part_bc, *part_A, *part_D;
     int* flags;
     void *dU, *ddelta, *dZ;
@@ -204,12 +255,12 @@ struct ScanBwd {
 template <typename IO, int N>
 __global__ __launch_bounds__(64) void selscan_bwd_totals_kernel(ScanBwd a)
 {
+    __shared__ __align__(16) float s_bc[2][GT][2 * N];
     const ScanShape& s = a.s;
     const Rows& R = s.rows;
     const int lane = threadIdx.x;
-    const int g = blockIdx.x / s.nb, in_group = (blockIdx.x % s.nb) * 64 + lane;
-    const bool live = in_group < s.Dg;
-    const int ch = g * s.Dg + min(in_group, s.Dg - 1);
+    const int g = blockIdx.x / s.nb;
+    const unsigned ch = g * s.Dg + min((int)(blockIdx.x % s.nb) * 64 + lane, s.Dg - 1);
     const int c = blockIdx.y + 1, t0 = c * s.chunk, t1 = min(t0 + s.chunk, R.T);       // (nothing is in front of the first chunk)
     const size_t ND = (size_t)N * s.D;
 
@@ -217,44 +268,55 @@ __global__ __launch_bounds__(64) void selscan_bwd_totals_kernel(ScanBwd a)
 #pragma unroll
     for (int n = 0; n < N; ++n) { A2[n] = a.A[(size_t)n * s.D + ch] * kLog2e; q[n] = 0.f; }
     const float bias = a.dbias ? a.dbias[ch] : 0.f;
-    const IO *De = (const IO*)a.delta + ch, *dY = (const IO*)a.dY + ch, *Z = a.Z ? (const IO*)a.Z + ch : nullptr;
+    const IO *De = (const IO*)a.delta, *dY = (const IO*)a.dY, *Z = (const IO*)a.Z;
+    const IO *Bm = (const IO*)a.Bm + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)g * N;
     int sq = seq_of(R, t1 - 1), beg = 0, end = 0;
     if (sq >= R.n_seq) sq = R.n_seq - 1;
     if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
     float sum = 0.f;
     bool ended = false;
     IO nd[GT], nz[GT], ny[GT];
+    Maps<IO, N> maps;
     auto load = [&](int t) {
 #pragma unroll
         for (int i = 0; i < GT; ++i) {
             const long r = min(t + i, R.T - 1);
-            nd[i] = De[r * a.ldd];
-            ny[i] = dY[r * a.lddy];
-            if (Z) nz[i] = Z[r * a.ldz];
+            nd[i] = (De + r * a.ldd)[ch];
+            ny[i] = (dY + r * a.lddy)[ch];
+            if (Z) nz[i] = (Z + r * a.ldz)[ch];
         }
+        if (lane & 4) maps.load(Bm, Cm, a.ldb, a.ldc, t, R.T - 1, lane);
     };
-    auto row = [&](int t, float d, float dy, float z) {
-        float dl = d + bias;
-        if (s.softplus) dl = softplus_(dl);
-        if (Z) dy *= z * sigmoid_(z);
-        const float* C = a.bc + ((size_t)t * s.G + g) * (2 * N) + N;
+    auto row = [&](const float* bc, float dl, float dy) {
 #pragma unroll
-        for (int n = 0; n < N; ++n) q[n] = exp2_(dl * A2[n]) * fmaf(C[n], dy, q[n]);
+        for (int n = 0; n < N; ++n) q[n] = exp2_(dl * A2[n]) * fmaf(bc[N + n], dy, q[n]);
         sum += dl;
     };
     const int last = t0 + (t1 - 1 - t0) / GT * GT;
     load(last);
     for (int t = last; t >= t0; t -= GT) {
-        float d[GT], z[GT], y[GT];
+        float dl[GT], dy[GT];
+        float(*bc)[2 * N] = s_bc[(t / GT) & 1];
 #pragma unroll
-        for (int i = 0; i < GT; ++i) { d[i] = to_f(nd[i]); y[i] = to_f(ny[i]); z[i] = Z ? to_f(nz[i]) : 0.f; }
+        for (int i = 0; i < GT; ++i) { dl[i] = to_f(nd[i]) + bias; dy[i] = to_f(ny[i]); }
+        if (Z)
+#pragma unroll
+            for (int i = 0; i < GT; ++i) dy[i] *= to_f(nz[i]) * sigmoid_(to_f(nz[i]));
+        if (lane & 4) maps.put(bc, lane);
+        wave_fence();
         if (t > t0) load(t - GT);
+        if (s.softplus)
+#pragma unroll
+            for (int i = 0; i < GT; ++i) dl[i] = softplus_(dl[i]);
         if (sq >= 0 && beg <= t && t + GT < end && t + GT <= t1) {
 #pragma unroll
-            for (int i = GT - 1; i >= 0; --i) row(t + i, d[i], y[i], z[i]);
+            for (int i = GT - 1; i >= 0; --i) {
+                row(bc[i], dl[i], dy[i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             continue;
         }
-#pragma unroll
+#pragma unroll 1
         for (int i = GT - 1; i >= 0; --i) {
             const int r = t + i;
             while (sq >= 0 && beg > r) {
@@ -268,74 +330,73 @@ __global__ __launch_bounds__(64) void selscan_bwd_totals_kernel(ScanBwd a)
 #pragma unroll
                 for (int n = 0; n < N; ++n) q[n] = a.dS_out && slot >= 0 ? a.dS_out[(size_t)slot * ND + (size_t)n * s.D + ch] : 0.f;
             }
-            row(r, d[i], y[i], z[i]);
+            float di = dl[0], yi = dy[0];
+#pragma unroll
+            for (int j = 1; j < GT; ++j) if (i == j) { di = dl[j]; yi = dy[j]; }
+            row(bc[i], di, yi);
         }
     }
-    if (live) {
-        float* Q = a.totals + (size_t)c * ND + ch;
+    float* Q = a.totals + (size_t)c * ND + ch;
 #pragma unroll
-        for (int n = 0; n < N; ++n) Q[(size_t)n * s.D] = q[n];
-        a.sums[(size_t)c * s.D + ch] = sum;
-        if (ch == 0) a.flags[c] = ended;
-    }
+    for (int n = 0; n < N; ++n) Q[(size_t)n * s.D] = q[n];
+    a.sums[(size_t)c * s.D + ch] = sum;
+    if (ch == 0) a.flags[c] = ended;
 }
 
-// Sums of eight values over the wave's lanes: lane l returns the sum of v[(l >> 3 & 7)'s value], see lane_value().
-__device__ __forceinline__ float lanes_swap_add32(float& x, float& y)      // x's sum over l, l + 32 in the lower half, y's in the upper
-{
-    u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ __forceinline__ float lanes_swap_add16(float x, float y)        // the same for rows of 16 lanes: x's in the even, y's in the odd ones
-{
-    u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float x)
-{
-    return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
-}
+// Sums over the wave's lanes of many values at once: a step adds two lanes' worth and deals two values out to the two, so the values
+// get fewer as they get more complete.  Within rows of 16 lanes by DPP, across them by swaps (which take three times as long and come last).
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x)
 {
     return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
 }
-__device__ __forceinline__ float sum8(float (&v)[8], int lane)
+template <int CTRL>
+__device__ __forceinline__ float deal(float x, float y, bool second)       // x's partial sums to the lanes that are not `second`, y's to those that are
+{
+    const float keep = second ? y : x, send = second ? x : y;
+    return keep + dpp<CTRL>(send);
+}
+constexpr int ROR8 = 0x128, HALF_MIRROR = 0x141, XOR2 = 0x4E, XOR1 = 0xB1;
+__device__ __forceinline__ float deal32(float x, float y)      // x's to the lower half of the lanes, y's to the upper
+{
+    u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float deal16(float x, float y)      // x's to the even rows of 16 lanes, y's to the odd ones
+{
+    u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// Eight values' sums over rows of 16 lanes but for lanes that differ in bit 0: lane l has that of value 4 (bit 3) + 2 (bit 2) + (bit 1).
+__device__ __forceinline__ float sum8(const float (&v)[8], int lane)
 {
     float r[4], w[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = lanes_swap_add32(v[i], v[i + 4]);
+    for (int i = 0; i < 4; ++i) r[i] = deal<ROR8>(v[i], v[i + 4], lane & 8);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) w[i] = lanes_swap_add16(r[i], r[i + 2]);
-    const bool up = lane & 8;
-    const float keep = up ? w[1] : w[0], send = up ? w[0] : w[1];
-    float x = keep + dpp<0x128>(send);            // row_ror:8
-    x = dpp_add<0xB1>(x);                         // quad_perm 1,0,3,2
-    x = dpp_add<0x4E>(x);                         // quad_perm 2,3,0,1
-    return dpp_add<0x141>(x);                     // row_half_mirror
+    for (int i = 0; i < 2; ++i) w[i] = deal<HALF_MIRROR>(r[i], r[i + 2], lane & 4);
+    return deal<XOR2>(w[0], w[1], lane & 2);
 }
-// Which of sum8()'s values lane l has.
-__device__ __forceinline__ int sum8_index(int lane) { return ((lane >> 3) & 1) + 2 * ((lane >> 4) & 1) + 4 * (lane >> 5); }
 
 constexpr int NPW = 4, TB = kSelscanTile;         // states of a wave, rows of a tile
 
 // A workgroup walks its chunk from the last tile to the first.  Wave w has states 4w .. 4w+3 of the same 64 channels: a tile's
 // decays and states then fit its registers.  The step sizes and the like of a tile are worked out once, by all waves, and shared.
 template <typename IO, int N>
-__global__ __launch_bounds__(N / NPW * 64) void selscan_bwd_kernel(ScanBwd a)
+__global__ __launch_bounds__(N / NPW * 64, 2) void selscan_bwd_kernel(ScanBwd a)
 {
-    constexpr int W = N / NPW, PER = TB / W > 0 ? TB / W : 1;      // waves; rows of a tile that a thread looks after
+    constexpr int W = N / NPW, PER = TB / W;                       // waves; rows of a tile that a thread looks after
     static_assert(TB % W == 0, "");
     __shared__ float s_dl[TB][64], s_x[TB][64], s_dy[TB][64], s_part[W][3][TB][64];
+    __shared__ __align__(16) float s_bc[TB][2 * N];
     const ScanShape& s = a.s;
     const Rows& R = s.rows;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = blockIdx.x / s.nb, b = blockIdx.x % s.nb, in_group = b * 64 + lane;
     const bool live = in_group < s.Dg;
-    const int ch = g * s.Dg + min(in_group, s.Dg - 1);
+    const unsigned ch = g * s.Dg + min(in_group, s.Dg - 1);
     const int c = blockIdx.y, t0 = c * s.chunk, t1 = min(t0 + s.chunk, R.T);
-    const size_t ND = (size_t)N * s.D, mine = (size_t)(w * NPW) * s.D + ch;      // of a state's N * D floats, this lane's first
+    const size_t ND = (size_t)N * s.D, first = (size_t)(w * NPW) * s.D, mine = first + ch;      // of a state's N * D floats, this wave's first and this lane's
 
     float A[NPW], A2[NPW], q[NPW], dA[NPW];
 #pragma unroll
@@ -345,143 +406,170 @@ __global__ __launch_bounds__(N / NPW * 64) void selscan_bwd_kernel(ScanBwd a)
         q[n] = dA[n] = 0.f;
     }
     const float bias = a.dbias ? a.dbias[ch] : 0.f, skip = a.Dskip ? a.Dskip[ch] : 0.f;
-    const IO *U = (const IO*)a.U + ch, *De = (const IO*)a.delta + ch, *dY = (const IO*)a.dY + ch;
-    const IO* Z = a.Z ? (const IO*)a.Z + ch : nullptr;
-    IO *dU = (IO*)a.dU + ch, *dDe = (IO*)a.ddelta + ch, *dZ = a.Z ? (IO*)a.dZ + ch : nullptr;
+    const IO *U = (const IO*)a.U, *De = (const IO*)a.delta, *dY = (const IO*)a.dY, *Z = (const IO*)a.Z;
+    IO *dU = (IO*)a.dU, *dDe = (IO*)a.ddelta, *dZ = (IO*)a.dZ;
 
     int sq = seq_of(R, t1 - 1), beg = 0, end = 0;
     const bool inside = sq >= 0 && sq < R.n_seq;
     if (sq >= R.n_seq) sq = R.n_seq - 1;
     if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
     if (inside && end > t1) {                     // the sequence goes on in the chunks behind
-        int k = c + 1;
-        while (k + 1 < s.n_chunk && a.flags[k] == 0) ++k;
-        const float* Q = a.totals + (size_t)k * ND + mine;
+        const float* Q = a.totals + (size_t)c * ND + mine;
 #pragma unroll
         for (int n = 0; n < NPW; ++n) q[n] = Q[(size_t)n * s.D];
-        for (--k; k > c; --k) {
-            const float sd = a.sums[(size_t)k * s.D + ch];
-            Q = a.totals + (size_t)k * ND + mine;
-#pragma unroll
-            for (int n = 0; n < NPW; ++n) q[n] = fmaf(exp2_(sd * A2[n]), q[n], Q[(size_t)n * s.D]);
-        }
     }
 
-    IO nu[PER], nd[PER], nz[PER], ny[PER];
+    // a thread's two of the tile's TB * 2N map values
+    const int mt = threadIdx.x / N, mk = threadIdx.x % N * 2;
+    const IO* M = mk < N ? (const IO*)a.Bm + (size_t)g * N + mk : (const IO*)a.Cm + (size_t)g * N + mk - N;
+    const long ldm = mk < N ? a.ldb : a.ldc;
+    IO nu[PER], nd[PER], nz[PER], ny[PER], nm[2];
     float nh[NPW];
     auto load = [&](int t) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const long r = min(t + w + i * W, R.T - 1);
-            nu[i] = U[r * a.ldu];
-            nd[i] = De[r * a.ldd];
-            ny[i] = dY[r * a.lddy];
-            if (Z) nz[i] = Z[r * a.ldz];
+            nu[i] = (U + r * a.ldu)[ch];
+            nd[i] = (De + r * a.ldd)[ch];
+            ny[i] = (dY + r * a.lddy)[ch];
+            if (Z) nz[i] = (Z + r * a.ldz)[ch];
         }
-        const float* from = a.saved + (size_t)(t / TB) * ND + mine;
+        const IO* m = M + min(t + mt, R.T - 1) * ldm;
+        nm[0] = m[0];
+        nm[1] = m[1];
+        const float* from = a.saved + (size_t)(t / TB) * ND + first;
 #pragma unroll
-        for (int n = 0; n < NPW; ++n) nh[n] = from[(size_t)n * s.D];
+        for (int n = 0; n < NPW; ++n) nh[n] = (from + (size_t)n * s.D)[ch];
     };
     float dD = 0.f, dbias = 0.f;
+    // where sum8()'s value of this lane goes, of a row's 2N
+    float* part = a.part_bc + ((size_t)b * R.T * s.G + g) * (2 * N);
+    const int at = ((lane >> 3) & 1) * N + w * NPW + ((lane >> 2) & 1) * 2 + ((lane >> 1) & 1);
     const int last = t0 + (t1 - 1 - t0) / TB * TB;
     load(last);
     for (int t = last; t >= t0; t -= TB) {
-        float u[PER], x[PER], z[PER], dout[PER], dl[PER], h[NPW];
+        float u[PER], x[PER], z[PER], dout[PER], h[NPW], tA[NPW];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            u[i] = to_f(nu[i]);
+            // (lanes behind the group's last channel: nothing that reaches the sums over channels)
+            u[i] = live ? to_f(nu[i]) : 0.f;
             x[i] = to_f(nd[i]) + bias;
-            dout[i] = to_f(ny[i]);
+            dout[i] = live ? to_f(ny[i]) : 0.f;
             z[i] = Z ? to_f(nz[i]) : 0.f;
-            dl[i] = s.softplus ? softplus_(x[i]) : x[i];
+            const float dl = s.softplus ? softplus_(x[i]) : x[i];
             const int k = w + i * W;
-            s_dl[k][lane] = dl[i];
-            s_x[k][lane] = dl[i] * u[i];
+            s_dl[k][lane] = dl;
+            s_x[k][lane] = dl * u[i];
             s_dy[k][lane] = Z ? dout[i] * z[i] * sigmoid_(z[i]) : dout[i];
         }
+        s_bc[mt][mk] = to_f(nm[0]);
+        s_bc[mt][mk + 1] = to_f(nm[1]);
 #pragma unroll
-        for (int n = 0; n < NPW; ++n) h[n] = nh[n];
+        for (int n = 0; n < NPW; ++n) { h[n] = nh[n]; tA[n] = 0.f; }
         if (t > t0) load(t - TB);
         __syncthreads();
         const bool whole = sq >= 0 && beg < t && t + TB < end && t + TB <= t1;
-        // forward: p and the decays of the tile
-        float p[TB][NPW], dec[TB][NPW];
-        int fq = sq, fb = beg;                     // (the sequence that the tile's first rows are in)
-        if (!whole) {
-            fq = seq_of(R, t);
-            if (fq < 0) fq = 0;
-            fb = fq < R.n_seq ? seq_begin(R, fq) : R.T;
-        }
+        auto tile = [&](auto is_whole) {
+            constexpr bool WHOLE = decltype(is_whole)::value;
+            // forward: p and the decays of the tile
+            float p[TB][NPW], dec[TB][NPW];
+            int fq = 0, fb = 0;                    // (the sequence that the tile's first rows are in)
+            if (!WHOLE) {
+                fq = seq_of(R, t);
+                if (fq < 0) fq = 0;
+                fb = fq < R.n_seq ? seq_begin(R, fq) : R.T;
+            }
 #pragma unroll
-        for (int i = 0; i < TB; ++i) {
-            const int r = t + i;
-            const float* bc = a.bc + ((size_t)min(r, R.T - 1) * s.G + g) * (2 * N) + w * NPW;
-            const float d = s_dl[i][lane], xu = s_x[i][lane];
-            if (!whole) {
-                while (fq < R.n_seq && seq_end(R, fq) <= r) {
-                    ++fq;
-                    fb = fq < R.n_seq ? seq_begin(R, fq) : R.T;
+            for (int i = 0; i < TB; ++i) {
+                const int r = t + i;
+                const float* Bt = &s_bc[i][w * NPW];
+                const float d = s_dl[i][lane], xu = s_x[i][lane];
+                if (!WHOLE) {
+                    while (fq < R.n_seq && seq_end(R, fq) <= r) {
+                        ++fq;
+                        fb = fq < R.n_seq ? seq_begin(R, fq) : R.T;
+                    }
+                    if (fq < R.n_seq && r == fb) {
+                        const int slot = a.S_in ? slot_of(R, fq) : -1;
+#pragma unroll
+                        for (int n = 0; n < NPW; ++n) h[n] = slot >= 0 ? a.S_in[(size_t)slot * ND + mine + (size_t)n * s.D] : 0.f;
+                    }
                 }
-                if (fq < R.n_seq && r == fb) {
-                    const int slot = a.S_in ? slot_of(R, fq) : -1;
 #pragma unroll
-                    for (int n = 0; n < NPW; ++n) h[n] = slot >= 0 ? a.S_in[(size_t)slot * ND + mine + (size_t)n * s.D] : 0.f;
+                for (int n = 0; n < NPW; ++n) {
+                    dec[i][n] = exp2_(d * A2[n]);
+                    p[i][n] = dec[i][n] * h[n];
+                    h[n] = fmaf(xu, Bt[n], p[i][n]);
+                }
+                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+            // and back
+            float odd = 0.f, pair1 = 0.f, half1 = 0.f;
+#pragma unroll
+            for (int i = TB - 1; i >= 0; --i) {
+                const int r = t + i;
+                bool on = true;
+                if (!WHOLE) {
+                    while (sq >= 0 && beg > r) {
+                        --sq;
+                        if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
+                    }
+                    on = r < t1 && sq >= 0 && r < end;
+                    if (on && r == end - 1) {
+                        const int slot = a.dS_out ? slot_of(R, sq) : -1;
+#pragma unroll
+                        for (int n = 0; n < NPW; ++n) q[n] = slot >= 0 ? a.dS_out[(size_t)slot * ND + mine + (size_t)n * s.D] : 0.f;
+                    }
+                }
+                float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                if (on) {
+                    const float *Bt = &s_bc[i][w * NPW], *Ct = Bt + N;
+                    const float d = s_dl[i][lane], xu = s_x[i][lane], dy = s_dy[i][lane];
+                    float y = 0.f, s1 = 0.f, s2 = 0.f;
+#pragma unroll
+                    for (int n = 0; n < NPW; ++n) {
+                        const float hh = fmaf(xu, Bt[n], p[i][n]), gg = fmaf(Ct[n], dy, q[n]), gp = gg * p[i][n];
+                        q[n] = dec[i][n] * gg;
+                        y = fmaf(Ct[n], hh, y);
+                        s1 = fmaf(gg, Bt[n], s1);
+                        s2 = fmaf(A[n], gp, s2);
+                        tA[n] = fmaf(d, gp, tA[n]);
+                        v[n] = gg * xu;
+                        v[4 + n] = dy * hh;
+                    }
+                    s_part[w][0][i][lane] = y;
+                    s_part[w][1][i][lane] = s1;
+                    s_part[w][2][i][lane] = s2;
+                    if (!WHOLE && r == beg && a.dS_in && live) {
+                        const int slot = slot_of(R, sq);
+                        if (slot >= 0) {
+#pragma unroll
+                            for (int n = 0; n < NPW; ++n) a.dS_in[(size_t)slot * ND + mine + (size_t)n * s.D] = q[n];
+                        }
+                    }
+                }
+                const float x8 = sum8(v, lane);
+                if (i & 1) {
+                    odd = x8;
+                } else {
+                    const float pair = deal<XOR1>(x8, odd, lane & 1);
+                    if (i % 4 == 2) {
+                        pair1 = pair;
+                    } else if (i % 8 == 4) {
+                        half1 = deal32(pair, pair1);
+                    } else {
+                        const float sum = deal16(deal32(pair, pair1), half1);
+                        const int k = t + i + 4 * ((lane >> 4) & 1) + 2 * (lane >> 5) + (lane & 1);
+                        if (k < t1) (part + ((size_t)(t + i) * s.G) * (2 * N))[at + (k - t - i) * s.G * 2 * N] = sum;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
+        };
+        if (whole) tile(std::true_type{});
+        else tile(std::false_type{});
 #pragma unroll
-            for (int n = 0; n < NPW; ++n) {
-                dec[i][n] = exp2_(d * A2[n]);
-                p[i][n] = dec[i][n] * h[n];
-                h[n] = fmaf(xu, bc[n], p[i][n]);
-            }
-        }
-        // and back
-        float* part = a.part_bc + (size_t)b * R.T * s.G * (2 * N);
-#pragma unroll
-        for (int i = TB - 1; i >= 0; --i) {
-            const int r = t + i;
-            if (!whole) {
-                while (sq >= 0 && beg > r) {
-                    --sq;
-                    if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
-                }
-                if (r >= t1 || sq < 0 || r >= end) continue;
-                if (r == end - 1) {
-                    const int slot = a.dS_out ? slot_of(R, sq) : -1;
-#pragma unroll
-                    for (int n = 0; n < NPW; ++n) q[n] = slot >= 0 ? a.dS_out[(size_t)slot * ND + mine + (size_t)n * s.D] : 0.f;
-                }
-            }
-            const float* bc = a.bc + ((size_t)r * s.G + g) * (2 * N) + w * NPW;
-            const float d = s_dl[i][lane], xu = s_x[i][lane], dy = s_dy[i][lane];
-            float y = 0.f, s1 = 0.f, s2 = 0.f, v[8];
-#pragma unroll
-            for (int n = 0; n < NPW; ++n) {
-                const float hh = fmaf(xu, bc[n], p[i][n]), gg = fmaf(bc[N + n], dy, q[n]), gp = gg * p[i][n];
-                q[n] = dec[i][n] * gg;
-                y = fmaf(bc[N + n], hh, y);
-                s1 = fmaf(gg, bc[n], s1);
-                s2 = fmaf(A[n], gp, s2);
-                dA[n] = fmaf(d, gp, dA[n]);
-                v[n] = live ? gg * xu : 0.f;
-                v[4 + n] = live ? dy * hh : 0.f;
-            }
-            s_part[w][0][i][lane] = y;
-            s_part[w][1][i][lane] = s1;
-            s_part[w][2][i][lane] = s2;
-            const float total = sum8(v, lane);
-            if ((lane & 7) == 0) {
-                const int k = sum8_index(lane);
-                part[((size_t)r * s.G + g) * (2 * N) + (k >> 2) * N + w * NPW + (k & 3)] = total;
-            }
-            if (!whole && r == beg && a.dS_in && live) {
-                const int slot = slot_of(R, sq);
-                if (slot >= 0) {
-#pragma unroll
-                    for (int n = 0; n < NPW; ++n) a.dS_in[(size_t)slot * ND + mine + (size_t)n * s.D] = q[n];
-                }
-            }
-        }
+        for (int n = 0; n < NPW; ++n) dA[n] += tA[n];          // (a tile's sum first: thousands of rows in one sum would lose digits)
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -498,15 +586,15 @@ __global__ __launch_bounds__(N / NPW * 64) void selscan_bwd_kernel(ScanBwd a)
             if (Z) {
                 const float sg = sigmoid_(z[i]), si = z[i] * sg;
                 dy *= si;
-                if (live) dZ[(size_t)r * s.D] = from_f<IO>(dout[i] * y * (sg + si * (1.f - sg)));
+                if (live) (dZ + (size_t)r * s.D)[ch] = from_f<IO>(dout[i] * y * (sg + si * (1.f - sg)));
             }
             float dd = fmaf(u[i], s1, s2);
             if (s.softplus) dd *= sigmoid_(x[i]);
             dD = fmaf(dy, u[i], dD);
             dbias += dd;
             if (live) {
-                dU[(size_t)r * s.D] = from_f<IO>(fmaf(dl[i], s1, skip * dy));
-                dDe[(size_t)r * s.D] = from_f<IO>(dd);
+                (dU + (size_t)r * s.D)[ch] = from_f<IO>(fmaf(s_dl[k][lane], s1, skip * dy));
+                (dDe + (size_t)r * s.D)[ch] = from_f<IO>(dd);
             }
         }
         // (the next tile's step sizes are written over this one's only after every wave has passed the barrier above)
@@ -613,7 +701,6 @@ static SelscanPlan plan_of(int T, int D, int N, int G, bool is_bwd, bool has_sav
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
     const size_t ND = (size_t)N * D * sizeof(float);
-    p.bc = take((size_t)T * G * 2 * N * sizeof(float));
     p.totals = take(ND * p.n_chunk);
     p.sums = take((size_t)p.n_chunk * D * sizeof(float));
     p.flags = take((size_t)p.n_chunk * sizeof(int));
@@ -652,25 +739,28 @@ static ScanShape shape_of(const SelscanArgs& a, int chunk, int n_chunk)
     return s;
 }
 
-template <typename IO>
-static void pack(const SelscanArgs& a, float* bc, const float* S_in, float* S_out, hipStream_t st)
+// Sequences without rows, where the state behind them is not the one in front already.
+static void pass_on(const SelscanArgs& a, const float* from, float* to, hipStream_t st)
 {
-    const long n = (long)a.rows.T * a.G * 2 * a.N;
-    long blocks = (n + 255) / 256;
-    if (blocks > 4096) blocks = 4096;
-    if (blocks < 1) blocks = 1;
-    if (S_out && blocks < 64) blocks = 64;
-    hipLaunchKernelGGL(selscan_pack_kernel<IO>, dim3((unsigned)blocks), dim3(256), 0, st, a.rows, (const IO*)a.Bm, (const IO*)a.Cm, a.ldb,
-                       a.ldc, bc, S_in, S_out, a.D, a.N, a.G);
+    if (to == nullptr || to == from || a.rows.n_seq == 0 || (a.rows.cu == nullptr && a.rows.T > 0)) return;
+    hipLaunchKernelGGL(selscan_empty_kernel, dim3(a.rows.n_seq < 256 ? a.rows.n_seq : 256), dim3(256), 0, st, a.rows, from, to, (long)a.N * a.D);
 }
 
-static ScanFwd fwd_of(const SelscanArgs& a, const SelscanPlan& p, char* ws, const float* bc)
+template <bool BWD>
+static void carry(const SelscanArgs& a, float* totals, const float* sums, const int* flags, int n_chunk, hipStream_t st)
+{
+    const long ND = (long)a.N * a.D;
+    hipLaunchKernelGGL(selscan_carry_kernel<BWD>, dim3((unsigned)((ND + 255) / 256)), dim3(256), 0, st, a.A, totals, sums, flags, n_chunk, a.D, ND);
+}
+
+static ScanFwd fwd_of(const SelscanArgs& a, const SelscanPlan& p, char* ws)
 {
     ScanFwd f{};
     f.s = shape_of(a, p.chunk, p.n_chunk);
     f.U = a.U; f.delta = a.delta; f.Z = a.Z;
     f.ldu = a.ldu; f.ldd = a.ldd; f.ldz = a.ldz;
-    f.A = a.A; f.bc = bc; f.Dskip = a.Dskip; f.dbias = a.delta_bias;
+    f.Bm = a.Bm; f.Cm = a.Cm; f.ldb = a.ldb; f.ldc = a.ldc;
+    f.A = a.A; f.Dskip = a.Dskip; f.dbias = a.delta_bias;
     f.S_in = a.S_in; f.S_out = a.S_out; f.saved = a.saved;
     f.totals = (float*)(ws + p.totals); f.sums = (float*)(ws + p.sums); f.flags = (int*)(ws + p.flags); f.fin = (float*)(ws + p.fin);
     f.Y = a.Y;
@@ -679,11 +769,13 @@ static ScanFwd fwd_of(const SelscanArgs& a, const SelscanPlan& p, char* ws, cons
 }
 
 template <typename IO, int N>
-static void walk(const ScanFwd& f, bool out, hipStream_t st)
+static void walk(const SelscanArgs& a, const ScanFwd& f, bool out, hipStream_t st)
 {
     const unsigned gx = (unsigned)(f.s.G * f.s.nb);
-    if (f.s.n_chunk > 1)
+    if (f.s.n_chunk > 1) {
         hipLaunchKernelGGL((selscan_fwd_kernel<IO, N, SCAN_TOTALS>), dim3(gx, f.s.n_chunk - 1), dim3(64), 0, st, f);
+        carry<false>(a, f.totals, f.sums, f.flags, f.s.n_chunk, st);
+    }
     if (out) hipLaunchKernelGGL((selscan_fwd_kernel<IO, N, SCAN_OUT>), dim3(gx, f.s.n_chunk), dim3(64), 0, st, f);
     else hipLaunchKernelGGL((selscan_fwd_kernel<IO, N, SCAN_SAVE>), dim3(gx, f.s.n_chunk), dim3(64), 0, st, f);
 }
@@ -691,12 +783,11 @@ static void walk(const ScanFwd& f, bool out, hipStream_t st)
 template <typename IO, int N>
 static hipError_t fwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, hipStream_t st)
 {
-    float* bc = (float*)(ws + p.bc);
     ProfScope prof(KID_SELSCAN, st);
-    pack<IO>(a, bc, a.S_in, a.S_out, st);
+    pass_on(a, a.S_in, a.S_out, st);
     if (a.rows.T > 0) {
-        const ScanFwd f = fwd_of(a, p, ws, bc);
-        walk<IO, N>(f, true, st);
+        const ScanFwd f = fwd_of(a, p, ws);
+        walk<IO, N>(a, f, true, st);
         if (f.s.same_buffer)
             hipLaunchKernelGGL(selscan_finish_kernel, dim3((unsigned)(((long)N * a.D + 255) / 256), p.n_chunk), dim3(256), 0, st, f.s,
                                f.fin, a.S_out);
@@ -707,31 +798,29 @@ static hipError_t fwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, hipS
 template <typename IO, int N>
 static hipError_t bwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, hipStream_t st)
 {
-    ScanBwd b{};
-    float* bc = (float*)(ws + p.bc);
     ProfScope prof(KID_SELSCAN_BWD, st);
-    pack<IO>(a, bc, a.dS_out, a.dS_in, st);
-    const float* saved = a.saved;
-    if (saved == nullptr && a.rows.T > 0) {
+    pass_on(a, a.dS_out, a.dS_in, st);
+    ScanBwd b{};
+    b.saved = a.saved;
+    if (a.saved == nullptr && a.rows.T > 0) {
         SelscanArgs again = a;
         again.saved = (float*)(ws + p.saved);
         again.S_out = nullptr;
-        const SelscanPlan fp = plan_of(a.rows.T, a.D, a.N, a.G, false, false);
-        const ScanFwd f = fwd_of(again, fp, ws + p.fin, bc);
-        walk<IO, N>(f, false, st);
-        saved = again.saved;
+        walk<IO, N>(again, fwd_of(again, plan_of(a.rows.T, a.D, a.N, a.G, false, false), ws + p.fin), false, st);
+        b.saved = again.saved;
     }
     b.s = shape_of(a, p.chunk, p.n_chunk);
-    b.U = a.U; b.delta = a.delta; b.Z = a.Z; b.dY = a.dY;
-    b.ldu = a.ldu; b.ldd = a.ldd; b.ldz = a.ldz; b.lddy = a.lddy;
-    b.A = a.A; b.bc = bc; b.Dskip = a.Dskip; b.dbias = a.delta_bias; b.S_in = a.S_in; b.dS_out = a.dS_out; b.saved = saved;
-    b.dS_in = a.dS_in;
+    b.U = a.U; b.delta = a.delta; b.Z = a.Z; b.dY = a.dY; b.Bm = a.Bm; b.Cm = a.Cm;
+    b.ldu = a.ldu; b.ldd = a.ldd; b.ldz = a.ldz; b.lddy = a.lddy; b.ldb = a.ldb; b.ldc = a.ldc;
+    b.A = a.A; b.Dskip = a.Dskip; b.dbias = a.delta_bias; b.S_in = a.S_in; b.dS_out = a.dS_out; b.dS_in = a.dS_in;
     b.totals = (float*)(ws + p.totals); b.sums = (float*)(ws + p.sums); b.flags = (int*)(ws + p.flags);
     b.part_bc = (float*)(ws + p.part_bc); b.part_A = (float*)(ws + p.part_A); b.part_D = (float*)(ws + p.part_D);
     b.dU = a.dU; b.ddelta = a.ddelta; b.dZ = a.dZ;
     const unsigned gx = (unsigned)(b.s.G * b.s.nb);
-    if (p.n_chunk > 1)
+    if (p.n_chunk > 1) {
         hipLaunchKernelGGL((selscan_bwd_totals_kernel<IO, N>), dim3(gx, p.n_chunk - 1), dim3(64), 0, st, b);
+        carry<true>(a, b.totals, b.sums, b.flags, p.n_chunk, st);
+    }
     if (a.rows.T > 0) {
         hipLaunchKernelGGL((selscan_bwd_kernel<IO, N>), dim3(gx, p.n_chunk), dim3(N / NPW * 64), 0, st, b);
         const long n = (long)a.rows.T * a.G * 2 * N;

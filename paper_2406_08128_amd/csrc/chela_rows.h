@@ -17,13 +17,13 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // exp(x) for an argument that is already in units of ln 2
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float sigmoid_(float x) { return __builtin_amdgcn_rcpf(1.f + exp2_(-kLog2e * x)); }
-// log(1 + exp(x)): with e = exp(-|x|) and w = 1 + e as rounded, log(1 + e) = log(w) e / (w - 1) to an ulp or two for every e in (0, 1].
+// log(1 + exp(x)) = max(x, 0) + log(1 + e), e = exp(-|x|).  With w = 1 + e as rounded and r = e - (w - 1) what the rounding lost (exact, e
+// being no larger than 1), log(1 + e) = log(w) + r / w, and 2 - w does for 1 / w: r is below 2^-24 and 2 - w off by (w - 1)^2.
 // (log(w) alone loses all digits of a step size of 1e-6.)
 __device__ __forceinline__ float softplus_(float x)
 {
     const float e = exp2_(-kLog2e * fabsf(x)), w = 1.f + e;
-    const float l = w == 1.f ? e : __builtin_amdgcn_logf(w) * kLn2 * e * __builtin_amdgcn_rcpf(w - 1.f);
-    return fmaxf(x, 0.f) + l;
+    return fmaxf(x, 0.f) + fmaf(2.f - w, e - (w - 1.f), __builtin_amdgcn_logf(w) * kLn2);
 }
 
 // The sequences as the kernels see them (chela_internal.h: Rows).  Offsets out of [0, T] are taken for the nearest in it, so that whatever
