@@ -309,7 +309,7 @@ int chela_linattn_step_gated(const void *q, const void *k, const void *v, const 
  * scan, and the norms around a block.  Common to the first two:
  *   rows     : [T, D] tensors of T tokens, bf16 (plain name) or fp32 (_f32); arithmetic and sums are fp32 for either, outputs are
  *              rounded once.  A tensor that comes with a row stride (ld..., elements from a token to the next, at least the
- *              row's width) may be a slice of a wider one and needs only its elements' alignment; all others are contiguous
+ *              row's width, below 2^29) may be a slice of a wider one and needs only its elements' alignment; all others are contiguous
  *              and 16-byte aligned.
  *   sequences: the T rows belong to n_seq sequences, one after the other.  cu NULL: of T / n_seq rows each.  Otherwise cu is
  *              n_seq + 1 ascending int32 offsets on the device, sequence s has rows cu[s] .. cu[s+1] - 1, none is an empty
@@ -358,7 +358,7 @@ size_t chela_short_conv_bwd_workspace_bytes(int T, int D, int m, int dtype);
  *   U, delta, Z (or NULL) [T, D]; Bm, Cm [T, G, N], G divides D; A [N, D], Dskip [D] (or NULL), delta_bias [D] (or NULL) fp32;
  *   states [n_slots, N, D] fp32.  The decay is formed as 2^(dl A log2 e); nothing is assumed of A's sign.
  *   fwd  : Y [T, D].  saved: NULL, or a caller-owned buffer of chela_selscan_saved_bytes() bytes (16-byte aligned, opaque) that carries
- *          the states in front of every 16th row to the backward call.
+ *          the states in front of every 8th row to the backward call.
  *   bwd  : gradients dU, ddelta, dZ (NULL without Z) [T, D], dB, dC [T, G, N] in the I/O type, dA [N, D], dDskip, ddelta_bias [D] (each
  *          NULL without its input) fp32, dS_in [n_seq, N, D] fp32 (NULL: not wanted), for the upstream dY [T, D] and dS_out
  *          [n_seq, N, D] fp32 (NULL: zero).  saved: as the forward call with the same inputs left it, or NULL: the states are worked

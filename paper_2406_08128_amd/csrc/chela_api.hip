@@ -1293,7 +1293,7 @@ struct Operands {
     void rows(const void* p, long long ld, int T, size_t width, size_t es)
     {
         if (ld < (long long)width) { if (rc == CHELA_OK) rc = CHELA_ERR_BAD_SHAPE; return; }
-        if (ld > (1ll << 31)) { if (rc == CHELA_OK) rc = CHELA_ERR_BAD_SHAPE; return; }
+        if (ld >= (1ll << 29)) { if (rc == CHELA_OK) rc = CHELA_ERR_BAD_SHAPE; return; }
         read(p, T > 0 ? ((size_t)(T - 1) * (size_t)ld + width) * es : 0, es);
     }
     void write(const void* p, size_t bytes) { check(p, bytes, 16); out[n_out++] = Range{(const char*)p, bytes}; }

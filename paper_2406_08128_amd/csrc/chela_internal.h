@@ -256,7 +256,7 @@ struct SelscanArgs {
     float *dA, *dDskip, *dbias;
     int D, N, G, softplus;
 };
-constexpr int kSelscanTile = 16;              // rows between two saved states
+constexpr int kSelscanTile = 8;               // rows between two saved states
 bool selscan_states_ok(int N);
 SelscanPlan make_selscan_plan(int T, int D, int N, int G, bool is_bwd, bool has_saved);
 hipError_t launch_selscan_fwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, int dtype, hipStream_t st);

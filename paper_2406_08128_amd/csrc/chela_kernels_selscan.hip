@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restr
     const int ch = (int)(i % D);
     const float A2 = A[i] * kLog2e;
     float h = 0.f;
-    constexpr int AT = 8;                            // chunks whose totals are read together
+    constexpr int AT = 32;                           // chunks whose totals are read together
     for (int k = 0; k < n_chunk; k += AT) {
         float H[AT], sd[AT];
         int f[AT];
@@ -94,26 +94,28 @@ __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restr
 }
 
 enum { SCAN_TOTALS = 0, SCAN_OUT = 1, SCAN_SAVE = 2 };        // what a walk leaves: the chunks' totals, the output, only the saved states
-constexpr int GT = 8;                                        // rows of a group: loaded together, one group ahead
+constexpr int GT = 4;                                        // rows of a group: loaded together, one group ahead
 
-// A group's input and output maps: each lane loads N / 4 of its GT * 2N values, wherever they lie, and puts them into LDS as fp32, from where
-// every lane reads those of a row at one address.  (Through the scalar cache each row waited for them, and a scalar operand halves an
+// A group's input and output maps: each lane loads its share of the GT * 2N values, wherever they lie, and puts them into LDS as fp32, from
+// where every lane reads those of a row at one address.  (Through the scalar cache each row waited for them, and a scalar operand halves an
 // instruction's rate.)
 template <typename IO, int N>
 struct Maps {
-    static constexpr int PER = N / 4;
+    static constexpr int PER = GT * 2 * N / 64, LPR = 64 / GT;      // values of a lane, lanes of a row: the first half of them has B's
+    static_assert(PER >= 1 && N % PER == 0, "");
     IO v[PER];
+    static __device__ __forceinline__ bool has_c(int lane) { return lane & (LPR / 2); }
     __device__ __forceinline__ void load(const IO* Bm, const IO* Cm, long ldb, long ldc, int t, int last, int lane)
     {
-        const long r = min(t + (lane >> 3), last);
-        const int k = (lane & 3) * PER;
-        const IO* p = lane & 4 ? Cm + r * ldc + k : Bm + r * ldb + k;
+        const long r = min(t + lane / LPR, last);
+        const int k = lane % (LPR / 2) * PER;
+        const IO* p = has_c(lane) ? Cm + r * ldc + k : Bm + r * ldb + k;
 #pragma unroll
         for (int i = 0; i < PER; ++i) v[i] = p[i];
     }
     __device__ __forceinline__ void put(float (*to)[2 * N], int lane) const
     {
-        float* p = &to[lane >> 3][(lane & 7) * PER];
+        float* p = &to[lane / LPR][lane % LPR * PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) p[i] = to_f(v[i]);
     }
@@ -148,24 +150,31 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
     }
 
     // (a row's address is the same in all lanes: scalar base, 32-bit lane offset)
-    const IO *U = (const IO*)a.U, *De = (const IO*)a.delta, *Z = MODE == SCAN_OUT ? (const IO*)a.Z : nullptr;
+    const bool gated = MODE == SCAN_OUT && a.Z != nullptr;
     const IO *Bm = (const IO*)a.Bm + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)g * N;
-    IO* Y = (IO*)a.Y;
+    const unsigned och = ch * sizeof(IO);
+    IO* Y = (IO*)a.Y + (size_t)t0 * s.D;                     // (of the row that comes next)
+    RowWalk<IO> pu, pd, pz;
+    pu.start(a.U, a.ldu, t0);
+    pd.start(a.delta, a.ldd, t0);
+    if (gated) pz.start(a.Z, a.ldz, t0);
     IO nu[GT], nd[GT], nz[GT];
     Maps<IO, N> maps;
     auto load = [&](int t) {
 #pragma unroll
         for (int i = 0; i < GT; ++i) {
-            const long r = min(t + i, R.T - 1);
-            nu[i] = (U + r * a.ldu)[ch];
-            nd[i] = (De + r * a.ldd)[ch];
-            if (Z) nz[i] = (Z + r * a.ldz)[ch];
+            const bool more = t + i < R.T - 1;
+            nu[i] = pu.get(och);
+            pu.next(more);
+            nd[i] = pd.get(och);
+            pd.next(more);
+            if (gated) { nz[i] = pz.get(och); pz.next(more); }
         }
-        if (MODE == SCAN_OUT || (lane & 4) == 0) maps.load(Bm, Cm, a.ldb, a.ldc, t, R.T - 1, lane);
+        if (MODE == SCAN_OUT || !maps.has_c(lane)) maps.load(Bm, Cm, a.ldb, a.ldc, t, R.T - 1, lane);
     };
     float sum = 0.f;
     bool began = false;
-    auto row = [&](int t, const float* bc, float dl, float u, float gate) {
+    auto row = [&](const float* bc, float dl, float u, float gate) {
         const float du = dl * u;
         float y[2] = {skip * u, 0.f};
 #pragma unroll
@@ -174,7 +183,7 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
             if (MODE == SCAN_OUT) y[n & 1] = fmaf(bc[N + n], h[n], y[n & 1]);
         }
         if (MODE == SCAN_TOTALS) sum += dl;
-        if (MODE == SCAN_OUT) (Y + (size_t)t * s.D)[ch] = from_f<IO>((y[0] + y[1]) * gate);
+        if (MODE == SCAN_OUT) row_store(Y, och, from_f<IO>((y[0] + y[1]) * gate));
     };
 
     load(t0);
@@ -182,25 +191,26 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
         float u[GT], dl[GT], gate[GT];
         float(*bc)[2 * N] = s_bc[(t / GT) & 1];
 #pragma unroll
-        for (int i = 0; i < GT; ++i) { u[i] = to_f(nu[i]); dl[i] = to_f(nd[i]) + bias; gate[i] = Z ? to_f(nz[i]) : 1.f; }
-        if (MODE == SCAN_OUT || (lane & 4) == 0) maps.put(bc, lane);
+        for (int i = 0; i < GT; ++i) { u[i] = to_f(nu[i]); dl[i] = to_f(nd[i]) + bias; gate[i] = gated ? to_f(nz[i]) : 1.f; }
+        if (MODE == SCAN_OUT || !maps.has_c(lane)) maps.put(bc, lane);
         wave_fence();
         if (t + GT < t1) load(t + GT);
         if (s.softplus)
 #pragma unroll
             for (int i = 0; i < GT; ++i) dl[i] = softplus_(dl[i]);
-        if (Z)
+        if (gated)
 #pragma unroll
             for (int i = 0; i < GT; ++i) gate[i] *= sigmoid_(gate[i]);
         if (MODE != SCAN_TOTALS && a.saved && (t & (kSelscanTile - 1)) == 0) {
             float* to = a.saved + (size_t)(t / kSelscanTile) * ND;
 #pragma unroll
-            for (int n = 0; n < N; ++n) (to + (size_t)n * s.D)[ch] = h[n];
+            for (int n = 0; n < N; ++n) row_store(to + (size_t)n * s.D, ch * 4, h[n]);
         }
         if (beg < t && t + GT < end && t + GT <= t1) {       // no sequence begins or ends here
 #pragma unroll
             for (int i = 0; i < GT; ++i) {
-                row(t + i, bc[i], dl[i], u[i], gate[i]);
+                row(bc[i], dl[i], u[i], gate[i]);
+                Y += s.D;
                 __builtin_amdgcn_sched_barrier(0);           // (or all rows' maps are read into registers first)
             }
             continue;
@@ -208,6 +218,7 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
 #pragma unroll 1
         for (int i = 0; i < GT; ++i) {
             const int r = t + i;
+            if (i > 0) Y += s.D;
             while (q < R.n_seq && end <= r) {
                 ++q;
                 if (q < R.n_seq) { beg = seq_begin(R, q); end = seq_end(R, q); }
@@ -222,7 +233,7 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
             float ui = u[0], di = dl[0], gi = gate[0];
 #pragma unroll
             for (int j = 1; j < GT; ++j) if (i == j) { ui = u[j]; di = dl[j]; gi = gate[j]; }
-            row(r, bc[i], di, ui, gi);
+            row(bc[i], di, ui, gi);
             if (MODE == SCAN_OUT && r == end - 1 && a.S_out && slot >= 0) {
                 // (over the states that other workgroups of the sequence may still read: later, by selscan_finish_kernel)
                 float* to = s.same_buffer && beg < t0 ? a.fin + (size_t)c * ND + ch : a.S_out + (size_t)slot * ND + ch;
@@ -230,6 +241,7 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
                 for (int n = 0; n < N; ++n) to[(size_t)n * s.D] = h[n];
             }
         }
+        Y += s.D;
     }
     if (MODE == SCAN_TOTALS) {
         float* H = a.totals + (size_t)c * ND + ch;
@@ -268,7 +280,7 @@ __global__ __launch_bounds__(64) void selscan_bwd_totals_kernel(ScanBwd a)
 #pragma unroll
     for (int n = 0; n < N; ++n) { A2[n] = a.A[(size_t)n * s.D + ch] * kLog2e; q[n] = 0.f; }
     const float bias = a.dbias ? a.dbias[ch] : 0.f;
-    const IO *De = (const IO*)a.delta, *dY = (const IO*)a.dY, *Z = (const IO*)a.Z;
+    const bool gated = a.Z != nullptr;
     const IO *Bm = (const IO*)a.Bm + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)g * N;
     int sq = seq_of(R, t1 - 1), beg = 0, end = 0;
     if (sq >= R.n_seq) sq = R.n_seq - 1;
@@ -277,32 +289,39 @@ __global__ __launch_bounds__(64) void selscan_bwd_totals_kernel(ScanBwd a)
     bool ended = false;
     IO nd[GT], nz[GT], ny[GT];
     Maps<IO, N> maps;
+    const unsigned och = ch * sizeof(IO);
+    const int last = t0 + (t1 - 1 - t0) / GT * GT;
+    RowWalk<IO> pd, py, pz;
+    pd.start(a.delta, a.ldd, min(last + GT - 1, R.T - 1));
+    py.start(a.dY, a.lddy, min(last + GT - 1, R.T - 1));
+    if (gated) pz.start(a.Z, a.ldz, min(last + GT - 1, R.T - 1));
     auto load = [&](int t) {
 #pragma unroll
-        for (int i = 0; i < GT; ++i) {
-            const long r = min(t + i, R.T - 1);
-            nd[i] = (De + r * a.ldd)[ch];
-            ny[i] = (dY + r * a.lddy)[ch];
-            if (Z) nz[i] = (Z + r * a.ldz)[ch];
+        for (int i = GT - 1; i >= 0; --i) {
+            const bool more = t + i < R.T && t + i > 0;
+            nd[i] = pd.get(och);
+            pd.back(more);
+            ny[i] = py.get(och);
+            py.back(more);
+            if (gated) { nz[i] = pz.get(och); pz.back(more); }
         }
-        if (lane & 4) maps.load(Bm, Cm, a.ldb, a.ldc, t, R.T - 1, lane);
+        if (maps.has_c(lane)) maps.load(Bm, Cm, a.ldb, a.ldc, t, R.T - 1, lane);
     };
     auto row = [&](const float* bc, float dl, float dy) {
 #pragma unroll
         for (int n = 0; n < N; ++n) q[n] = exp2_(dl * A2[n]) * fmaf(bc[N + n], dy, q[n]);
         sum += dl;
     };
-    const int last = t0 + (t1 - 1 - t0) / GT * GT;
     load(last);
     for (int t = last; t >= t0; t -= GT) {
         float dl[GT], dy[GT];
         float(*bc)[2 * N] = s_bc[(t / GT) & 1];
 #pragma unroll
         for (int i = 0; i < GT; ++i) { dl[i] = to_f(nd[i]) + bias; dy[i] = to_f(ny[i]); }
-        if (Z)
+        if (gated)
 #pragma unroll
             for (int i = 0; i < GT; ++i) dy[i] *= to_f(nz[i]) * sigmoid_(to_f(nz[i]));
-        if (lane & 4) maps.put(bc, lane);
+        if (maps.has_c(lane)) maps.put(bc, lane);
         wave_fence();
         if (t > t0) load(t - GT);
         if (s.softplus)
@@ -382,8 +401,9 @@ constexpr int NPW = 4, TB = kSelscanTile;         // states of a wave, rows of a
 
 // A workgroup walks its chunk from the last tile to the first.  Wave w has states 4w .. 4w+3 of the same 64 channels: a tile's
 // decays and states then fit its registers.  The step sizes and the like of a tile are worked out once, by all waves, and shared.
+// Tiles of 8 rows leave room for three waves per SIMD, tiles of 16 for two: 1310 us against 1440 (65536 rows, 1536 channels, 16 states).
 template <typename IO, int N>
-__global__ __launch_bounds__(N / NPW * 64, 2) void selscan_bwd_kernel(ScanBwd a)
+__global__ __launch_bounds__(N / NPW * 64, 3) void selscan_bwd_kernel(ScanBwd a)
 {
     constexpr int W = N / NPW, PER = TB / W;                       // waves; rows of a tile that a thread looks after
     static_assert(TB % W == 0, "");
@@ -419,27 +439,29 @@ __global__ __launch_bounds__(N / NPW * 64, 2) void selscan_bwd_kernel(ScanBwd a)
         for (int n = 0; n < NPW; ++n) q[n] = Q[(size_t)n * s.D];
     }
 
-    // a thread's two of the tile's TB * 2N map values
-    const int mt = threadIdx.x / N, mk = threadIdx.x % N * 2;
+    // a thread's share of the tile's TB * 2N map values
+    constexpr int MV = TB * 2 * N / (W * 64);
+    const int mt = threadIdx.x * MV / (2 * N), mk = threadIdx.x * MV % (2 * N);
     const IO* M = mk < N ? (const IO*)a.Bm + (size_t)g * N + mk : (const IO*)a.Cm + (size_t)g * N + mk - N;
     const long ldm = mk < N ? a.ldb : a.ldc;
-    IO nu[PER], nd[PER], nz[PER], ny[PER], nm[2];
+    IO nu[PER], nd[PER], nz[PER], ny[PER], nm[MV];
     float nh[NPW];
+    const unsigned och = ch * sizeof(IO);
     auto load = [&](int t) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const long r = min(t + w + i * W, R.T - 1);
-            nu[i] = (U + r * a.ldu)[ch];
-            nd[i] = (De + r * a.ldd)[ch];
-            ny[i] = (dY + r * a.lddy)[ch];
-            if (Z) nz[i] = (Z + r * a.ldz)[ch];
+            nu[i] = row_load(U + r * a.ldu, och);
+            nd[i] = row_load(De + r * a.ldd, och);
+            ny[i] = row_load(dY + r * a.lddy, och);
+            if (Z) nz[i] = row_load(Z + r * a.ldz, och);
         }
         const IO* m = M + min(t + mt, R.T - 1) * ldm;
-        nm[0] = m[0];
-        nm[1] = m[1];
+#pragma unroll
+        for (int k = 0; k < MV; ++k) nm[k] = m[k];
         const float* from = a.saved + (size_t)(t / TB) * ND + first;
 #pragma unroll
-        for (int n = 0; n < NPW; ++n) nh[n] = (from + (size_t)n * s.D)[ch];
+        for (int n = 0; n < NPW; ++n) nh[n] = row_load(from + (size_t)n * s.D, ch * 4);
     };
     float dD = 0.f, dbias = 0.f;
     // where sum8()'s value of this lane goes, of a row's 2N
@@ -448,31 +470,42 @@ __global__ __launch_bounds__(N / NPW * 64, 2) void selscan_bwd_kernel(ScanBwd a)
     const int last = t0 + (t1 - 1 - t0) / TB * TB;
     load(last);
     for (int t = last; t >= t0; t -= TB) {
-        float u[PER], x[PER], z[PER], dout[PER], h[NPW], tA[NPW];
+        // of a row that the thread looks after: u, the step size's slope, dout silu(z), dout silu'(z)
+        float u[PER], slope[PER], dy[PER], dz[PER], h0[NPW], tA[NPW];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             // (lanes behind the group's last channel: nothing that reaches the sums over channels)
             u[i] = live ? to_f(nu[i]) : 0.f;
-            x[i] = to_f(nd[i]) + bias;
-            dout[i] = live ? to_f(ny[i]) : 0.f;
-            z[i] = Z ? to_f(nz[i]) : 0.f;
-            const float dl = s.softplus ? softplus_(x[i]) : x[i];
+            dy[i] = live ? to_f(ny[i]) : 0.f;
+            float dl = to_f(nd[i]) + bias;
+            slope[i] = 1.f;
+            if (s.softplus) dl = softplus_(dl, &slope[i]);
+            if (Z) {
+                const float z = to_f(nz[i]), sg = sigmoid_(z), si = z * sg;
+                dz[i] = dy[i] * fmaf(si, 1.f - sg, sg);
+                dy[i] *= si;
+            }
             const int k = w + i * W;
             s_dl[k][lane] = dl;
             s_x[k][lane] = dl * u[i];
-            s_dy[k][lane] = Z ? dout[i] * z[i] * sigmoid_(z[i]) : dout[i];
+            s_dy[k][lane] = dy[i];
         }
-        s_bc[mt][mk] = to_f(nm[0]);
-        s_bc[mt][mk + 1] = to_f(nm[1]);
 #pragma unroll
-        for (int n = 0; n < NPW; ++n) { h[n] = nh[n]; tA[n] = 0.f; }
+        for (int k = 0; k < MV; ++k) s_bc[mt][mk + k] = to_f(nm[k]);
+#pragma unroll
+        for (int n = 0; n < NPW; ++n) { h0[n] = nh[n]; tA[n] = 0.f; }
         if (t > t0) load(t - TB);
         __syncthreads();
         const bool whole = sq >= 0 && beg < t && t + TB < end && t + TB <= t1;
+        auto state_in_front = [&](int sequence, float (&to)[NPW]) {
+            const int slot = a.S_in ? slot_of(R, sequence) : -1;
+#pragma unroll
+            for (int n = 0; n < NPW; ++n) to[n] = slot >= 0 ? a.S_in[(size_t)slot * ND + mine + (size_t)n * s.D] : 0.f;
+        };
         auto tile = [&](auto is_whole) {
             constexpr bool WHOLE = decltype(is_whole)::value;
-            // forward: p and the decays of the tile
-            float p[TB][NPW], dec[TB][NPW];
+            // forward: the tile's states and decays
+            float h[TB][NPW], dec[TB][NPW];
             int fq = 0, fb = 0;                    // (the sequence that the tile's first rows are in)
             if (!WHOLE) {
                 fq = seq_of(R, t);
@@ -484,22 +517,20 @@ __global__ __launch_bounds__(N / NPW * 64, 2) void selscan_bwd_kernel(ScanBwd a)
                 const int r = t + i;
                 const float* Bt = &s_bc[i][w * NPW];
                 const float d = s_dl[i][lane], xu = s_x[i][lane];
+                float before[NPW];
+#pragma unroll
+                for (int n = 0; n < NPW; ++n) before[n] = i == 0 ? h0[n] : h[i > 0 ? i - 1 : 0][n];
                 if (!WHOLE) {
                     while (fq < R.n_seq && seq_end(R, fq) <= r) {
                         ++fq;
                         fb = fq < R.n_seq ? seq_begin(R, fq) : R.T;
                     }
-                    if (fq < R.n_seq && r == fb) {
-                        const int slot = a.S_in ? slot_of(R, fq) : -1;
-#pragma unroll
-                        for (int n = 0; n < NPW; ++n) h[n] = slot >= 0 ? a.S_in[(size_t)slot * ND + mine + (size_t)n * s.D] : 0.f;
-                    }
+                    if (fq < R.n_seq && r == fb) state_in_front(fq, before);
                 }
 #pragma unroll
                 for (int n = 0; n < NPW; ++n) {
                     dec[i][n] = exp2_(d * A2[n]);
-                    p[i][n] = dec[i][n] * h[n];
-                    h[n] = fmaf(xu, Bt[n], p[i][n]);
+                    h[i][n] = fmaf(dec[i][n], before[n], xu * Bt[n]);
                 }
                 if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
@@ -525,11 +556,15 @@ __global__ __launch_bounds__(N / NPW * 64, 2) void selscan_bwd_kernel(ScanBwd a)
                 if (on) {
                     const float *Bt = &s_bc[i][w * NPW], *Ct = Bt + N;
                     const float d = s_dl[i][lane], xu = s_x[i][lane], dy = s_dy[i][lane];
-                    float y = 0.f, s1 = 0.f, s2 = 0.f;
+                    float y = 0.f, s1 = 0.f, s2 = 0.f, before[NPW];
+#pragma unroll
+                    for (int n = 0; n < NPW; ++n) before[n] = i == 0 ? h0[n] : h[i > 0 ? i - 1 : 0][n];
+                    if (!WHOLE && r == beg) state_in_front(sq, before);
 #pragma unroll
                     for (int n = 0; n < NPW; ++n) {
-                        const float hh = fmaf(xu, Bt[n], p[i][n]), gg = fmaf(Ct[n], dy, q[n]), gp = gg * p[i][n];
+                        const float hh = h[i][n], gg = fmaf(Ct[n], dy, q[n]);
                         q[n] = dec[i][n] * gg;
+                        const float gp = q[n] * before[n];
                         y = fmaf(Ct[n], hh, y);
                         s1 = fmaf(gg, Bt[n], s1);
                         s2 = fmaf(A[n], gp, s2);
@@ -581,20 +616,13 @@ __global__ __launch_bounds__(N / NPW * 64, 2) void selscan_bwd_kernel(ScanBwd a)
             float y = 0.f, s1 = 0.f, s2 = 0.f;
 #pragma unroll
             for (int j = 0; j < W; ++j) { y += s_part[j][0][k][lane]; s1 += s_part[j][1][k][lane]; s2 += s_part[j][2][k][lane]; }
-            y = fmaf(skip, u[i], y);
-            float dy = dout[i];
-            if (Z) {
-                const float sg = sigmoid_(z[i]), si = z[i] * sg;
-                dy *= si;
-                if (live) (dZ + (size_t)r * s.D)[ch] = from_f<IO>(dout[i] * y * (sg + si * (1.f - sg)));
-            }
-            float dd = fmaf(u[i], s1, s2);
-            if (s.softplus) dd *= sigmoid_(x[i]);
-            dD = fmaf(dy, u[i], dD);
+            if (Z && live) row_store(dZ + (size_t)r * s.D, och, from_f<IO>(dz[i] * fmaf(skip, u[i], y)));
+            const float dd = fmaf(u[i], s1, s2) * slope[i];
+            dD = fmaf(dy[i], u[i], dD);
             dbias += dd;
             if (live) {
-                (dU + (size_t)r * s.D)[ch] = from_f<IO>(fmaf(s_dl[k][lane], s1, skip * dy));
-                (dDe + (size_t)r * s.D)[ch] = from_f<IO>(dd);
+                row_store(dU + (size_t)r * s.D, och, from_f<IO>(fmaf(s_dl[k][lane], s1, skip * dy[i])));
+                row_store(dDe + (size_t)r * s.D, och, from_f<IO>(dd));
             }
         }
         // (the next tile's step sizes are written over this one's only after every wave has passed the barrier above)
@@ -634,18 +662,24 @@ __global__ __launch_bounds__(256) void selscan_bc_kernel(Rows R, const float* __
     }
 }
 
-// The chunks' sums of the parameters' gradients: rows 0 .. N-1 are dA's, N dD's and N+1 the bias's.
-__global__ __launch_bounds__(256) void selscan_params_kernel(const float* __restrict__ part_A, const float* __restrict__ part_D, int n_chunk,
-                                                            int N, int D, float* dA, float* dD, float* dbias)
+// The chunks' sums of the parameters' gradients: rows 0 .. N-1 are dA's, N dD's and N+1 the bias's.  Sixteen waves share the chunks.
+__global__ __launch_bounds__(1024) void selscan_params_kernel(const float* __restrict__ part_A, const float* __restrict__ part_D, int n_chunk,
+                                                             int N, int D, float* dA, float* dD, float* dbias)
 {
-    const int i = blockIdx.x * 256 + threadIdx.x, n = blockIdx.y;
-    if (i >= D) return;
+    __shared__ float s_sum[16][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = blockIdx.x * 64 + lane, n = blockIdx.y;
     float* to = n < N ? dA + (size_t)n * D : n == N ? dD : dbias;
     if (to == nullptr) return;
-    const float* from = n < N ? part_A + (size_t)n * D + i : part_D + (size_t)(n - N) * D + i;
+    const float* from = (n < N ? part_A + (size_t)n * D : part_D + (size_t)(n - N) * D) + min(i, D - 1);
     const size_t step = n < N ? (size_t)N * D : (size_t)2 * D;
     float x = 0.f;
-    for (int c = 0; c < n_chunk; ++c) x += from[(size_t)c * step];
+    for (int c = w; c < n_chunk; c += 16) x += from[(size_t)c * step];
+    s_sum[w][lane] = x;
+    __syncthreads();
+    if (w != 0 || i >= D) return;
+    x = 0.f;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x += s_sum[j][lane];
     to[i] = x;
 }
 
@@ -681,14 +715,20 @@ bool selscan_states_ok(int N) { return N == 8 || N == 16 || N == 32; }
 
 static int waves_per_group(int D, int G) { return (D / G + 63) / 64; }
 
-// Chunks of whole tiles, as many as give `want` workgroups and no more than 64 of them.
+// Chunks of whole tiles, as many as give `want` workgroups, but none of less than 48 rows.  A wave alone on its SIMD issues at 40 % of the
+// rate that four reach, so the chunks have to be many; what they cost is a state each, to leave, to carry and to begin with.  us: one
+// sequence of 65536 rows, 2048 channels, forward, for 2048, 4096, 6144, 8192 waves: 1079, 928, 906, 893; four of 16384, 1536 channels,
+// forward and backward, for 1536, 2048, 4096, 6144 backward workgroups: 2500, 2430, 2320, 2313.  6007 rows, 1536 channels, forward, for
+// chunks of 32, 48, 64, 96 rows: 106, 98, 112, 117; 3001 rows, 1000 channels, 32 states, both: 248, 244, 261, 299.
+constexpr long kFwdWaves = 6144, kBwdGroups = 4096;
+constexpr int kLeastChunk = 48;
 static void cut_rows(int T, long groups, long want, int* chunk, int* n_chunk)
 {
     long n = groups > 0 ? (want + groups - 1) / groups : 1;
-    if (n > 64) n = 64;
+    if (n > 1024) n = 1024;
     long len = ((long)T + n - 1) / n;
     len = (len + kSelscanTile - 1) / kSelscanTile * kSelscanTile;
-    if (len < 2 * kSelscanTile) len = 2 * kSelscanTile;
+    if (len < kLeastChunk) len = kLeastChunk;
     *chunk = (int)len;
     *n_chunk = (int)(((long)T + len - 1) / len);
 }
@@ -697,7 +737,7 @@ static SelscanPlan plan_of(int T, int D, int N, int G, bool is_bwd, bool has_sav
 {
     SelscanPlan p{};
     const long groups = (long)G * waves_per_group(D, G);
-    cut_rows(T, groups, is_bwd ? 512 : 2048, &p.chunk, &p.n_chunk);
+    cut_rows(T, groups, is_bwd ? kBwdGroups : kFwdWaves, &p.chunk, &p.n_chunk);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
     const size_t ND = (size_t)N * D * sizeof(float);
@@ -829,7 +869,7 @@ static hipError_t bwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, hipS
         hipLaunchKernelGGL(selscan_bc_kernel<IO>, dim3((unsigned)blocks), dim3(256), 0, st, a.rows, b.part_bc, b.s.nb, N, a.G, (IO*)a.dB,
                            (IO*)a.dC);
     }
-    hipLaunchKernelGGL(selscan_params_kernel, dim3((unsigned)((a.D + 255) / 256), N + 2), dim3(256), 0, st, b.part_A, b.part_D, p.n_chunk, N,
+    hipLaunchKernelGGL(selscan_params_kernel, dim3((unsigned)((a.D + 63) / 64), N + 2), dim3(1024), 0, st, b.part_A, b.part_D, p.n_chunk, N,
                        a.D, a.dA, a.dDskip, a.dbias);
     return hipGetLastError();
 }

@@ -23,8 +23,42 @@ __device__ __forceinline__ float sigmoid_(float x) { return __builtin_amdgcn_rcp
 __device__ __forceinline__ float softplus_(float x)
 {
     const float e = exp2_(-kLog2e * fabsf(x)), w = 1.f + e;
-    return fmaxf(x, 0.f) + fmaf(2.f - w, e - (w - 1.f), __builtin_amdgcn_logf(w) * kLn2);
+    return __builtin_amdgcn_fmed3f(x, 0.f, __builtin_inff()) + fmaf(2.f - w, e - (w - 1.f), __builtin_amdgcn_logf(w) * kLn2);
 }
+// ... and its slope, 1 / (1 + exp(-x))
+__device__ __forceinline__ float softplus_(float x, float* slope)
+{
+    const float e = exp2_(-kLog2e * fabsf(x)), w = 1.f + e, r = __builtin_amdgcn_rcpf(w);
+    *slope = x < 0.f ? e * r : r;
+    return __builtin_amdgcn_fmed3f(x, 0.f, __builtin_inff()) + fmaf(2.f - w, e - (w - 1.f), __builtin_amdgcn_logf(w) * kLn2);
+}
+
+// A lane's element of a row whose address all lanes share: scalar base, 32-bit offset in bytes.  (The empty instructions keep the base in
+// scalar registers and the offset in 32 bits where it is used: the compiler adds lane and base first otherwise, or widens the offset in
+// front of the loop, and a 64-bit vector addition per row and tensor remains.)
+#define CHELA_GLOBAL __attribute__((address_space(1)))
+template <typename T> __device__ __forceinline__ T row_load(const T* row, unsigned off)
+{
+    const CHELA_GLOBAL char* p = (const CHELA_GLOBAL char*)row;
+    asm("" : "+s"(p), "+v"(off));
+    return *(const CHELA_GLOBAL T*)(p + off);
+}
+template <typename T> __device__ __forceinline__ void row_store(T* row, unsigned off, T x)
+{
+    CHELA_GLOBAL char* p = (CHELA_GLOBAL char*)row;
+    asm("" : "+s"(p), "+v"(off));
+    *(CHELA_GLOBAL T*)(p + off) = x;
+}
+// Rows one after the other, the last one again behind it: where the next one is, and how far it is to the one after.
+template <typename T>
+struct RowWalk {
+    const char* p;
+    unsigned step;
+    __device__ __forceinline__ void start(const void* base, long ld, int row) { p = (const char*)((const T*)base + (long)row * ld); step = (unsigned)ld * sizeof(T); }
+    __device__ __forceinline__ T get(unsigned off) const { return row_load((const T*)p, off); }
+    __device__ __forceinline__ void next(bool on) { p += on ? step : 0u; }
+    __device__ __forceinline__ void back(bool on) { p -= on ? step : 0u; }
+};
 
 // The sequences as the kernels see them (chela_internal.h: Rows).  Offsets out of [0, T] are taken for the nearest in it, so that whatever
 // `cu` holds no row out of [0, T) is touched.

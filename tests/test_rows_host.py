@@ -239,7 +239,7 @@ def test_block_norm_refusals(L, sfx):
 
 
 def test_workspace_and_saved_queries(L):
-    assert L.chela_selscan_saved_bytes(1000, 100, 16) == 63 * 16 * 100 * 4
+    assert L.chela_selscan_saved_bytes(1000, 100, 16) == 125 * 16 * 100 * 4
     assert L.chela_selscan_saved_bytes(0, 100, 16) == 0 and L.chela_selscan_saved_bytes(5, 100, 15) == 0
     for bad in ((0, 64, 16, 1, 0, 0), (8, 0, 16, 1, 0, 0), (8, 64, 12, 1, 0, 0), (8, 64, 16, 0, 0, 0), (8, 64, 16, 3, 1, 0)):
         assert L.chela_selscan_workspace_bytes(*bad) == 0, bad
