@@ -244,7 +244,7 @@ hipError_t launch_short_conv_step(const ShortConvArgs& a, int dtype, hipStream_t
 // Selective scan.  The rows are cut into n_chunk chunks of `chunk`, whichever sequences they belong to.
 struct SelscanPlan {
     int chunk, n_chunk;
-    size_t totals, sums, flags, fin, part_bc, part_A, part_D, saved, bytes;      // byte offsets into the scratch, and its size
+    size_t totals, sums, fin, part_bc, part_A, part_D, saved, bytes;      // byte offsets into the scratch, and its size
 };
 struct SelscanArgs {
     Rows rows;

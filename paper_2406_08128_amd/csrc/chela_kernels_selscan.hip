@@ -32,19 +32,22 @@ struct ScanFwd {
     long ldu, ldd, ldz, ldb, ldc;
     const float *A, *Dskip, *dbias, *S_in;
     float *S_out, *saved, *totals, *sums, *fin;
-    int* flags;
     void* Y;
 };
 
-// Sequences without rows hand their states (or, in the backward call, the states' gradients) on.
-__global__ __launch_bounds__(256) void selscan_empty_kernel(Rows rows, const float* from, float* to, long n)
+// Sequences without rows hand their states (or, in the backward call, the states' gradients) on: workgroup `first` of `groups`.
+__device__ __forceinline__ void pass_states_on(const Rows& rows, const float* from, float* to, long n, int first, int groups)
 {
-    for (int s = blockIdx.x; s < rows.n_seq; s += gridDim.x) {
+    for (int s = first; s < rows.n_seq; s += groups) {
         if (seq_begin(rows, s) < seq_end(rows, s)) continue;
         const int slot = slot_of(rows, s);
         if (slot < 0) continue;
-        for (long i = threadIdx.x; i < n; i += 256) to[slot * n + i] = from ? from[slot * n + i] : 0.f;
+        for (long i = threadIdx.x; i < n; i += blockDim.x) to[slot * n + i] = from ? from[slot * n + i] : 0.f;
     }
+}
+__global__ __launch_bounds__(256) void selscan_empty_kernel(Rows rows, const float* from, float* to, long n)
+{
+    pass_states_on(rows, from, to, n, blockIdx.x, gridDim.x);
 }
 
 // Behind a call that writes its states over those it reads: the sequences that end in another chunk than they begin in.
@@ -60,35 +63,39 @@ __global__ __launch_bounds__(256) void selscan_finish_kernel(ScanShape s, const 
 }
 
 // The chunks' totals turned into what each chunk begins with, in place, in order (forward: from the first chunk on, state and decay; backward:
-// from the last chunk on).  A chunk with its flag set has a sequence's beginning (end) in it: what comes to it ends there.
+// from the last chunk on).  A chunk whose sum of step sizes is the mark has a sequence's beginning (end) in it: what comes to it ends there.
+// (A sum that is not a number by itself comes with totals that are none.)  Workgroups from `groups` on: pass_states_on().
+__device__ __forceinline__ float reset_mark() { return __uint_as_float(0x7fc00000u); }
 template <bool BWD>
 __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restrict__ A, float* __restrict__ totals,
-                                                           const float* __restrict__ sums, const int* __restrict__ flags, int n_chunk, int D, long ND)
+                                                           const float* __restrict__ sums, int n_chunk, int D, long ND, int groups, Rows rows,
+                                                           const float* from, float* to)
 {
+    if ((int)blockIdx.x >= groups) {
+        pass_states_on(rows, from, to, ND, blockIdx.x - groups, gridDim.x - groups);
+        return;
+    }
     const long i = (long)blockIdx.x * 256 + threadIdx.x;
     if (i >= ND) return;
     const int ch = (int)(i % D);
     const float A2 = A[i] * kLog2e;
     float h = 0.f;
     constexpr int AT = 32;                           // chunks whose totals are read together
+    // (the chunk that nothing comes behind has no totals: its place holds anything, and what is made of it goes nowhere)
     for (int k = 0; k < n_chunk; k += AT) {
         float H[AT], sd[AT];
-        int f[AT];
 #pragma unroll
         for (int j = 0; j < AT; ++j) {
-            const int c = BWD ? n_chunk - 1 - min(k + j, n_chunk - 1) : min(k + j, n_chunk - 1);
-            // (the chunk that nothing comes behind has no totals)
-            const bool there = BWD ? c > 0 : c < n_chunk - 1;
-            H[j] = there ? totals[(size_t)c * ND + i] : 0.f;
-            sd[j] = there ? sums[(size_t)c * D + ch] : 0.f;
-            f[j] = there ? flags[c] : 0;
+            const int o = min(k + j, n_chunk - 1), c = BWD ? n_chunk - 1 - o : o;
+            H[j] = totals[(size_t)c * ND + i];
+            sd[j] = sums[(size_t)c * D + ch];
         }
 #pragma unroll
         for (int j = 0; j < AT; ++j) {
-            if (k + j >= n_chunk) break;
+            // (what is worked out for places behind the last chunk goes nowhere; were it left out, the loads would wait in turn)
             const int c = BWD ? n_chunk - 1 - (k + j) : k + j;
-            totals[(size_t)c * ND + i] = h;
-            h = f[j] ? H[j] : fmaf(exp2_(sd[j] * A2), h, H[j]);
+            if (k + j < n_chunk) totals[(size_t)c * ND + i] = h;
+            h = sd[j] != sd[j] ? H[j] : fmaf(exp2_(sd[j] * A2), h, H[j]);
         }
     }
 }
@@ -247,8 +254,7 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
         float* H = a.totals + (size_t)c * ND + ch;
 #pragma unroll
         for (int n = 0; n < N; ++n) H[(size_t)n * s.D] = h[n];
-        a.sums[(size_t)c * s.D + ch] = sum;
-        if (ch == 0) a.flags[c] = began;
+        a.sums[(size_t)c * s.D + ch] = began ? reset_mark() : sum;
     }
 }
 
@@ -259,7 +265,6 @@ struct ScanBwd {
     long ldu, ldd, ldz, lddy, ldb, ldc;
     const float *A, *Dskip, *dbias, *S_in, *dS_out, *saved;
     float *dS_in, *totals, *sums, *part_bc, *part_A, *part_D;
-    int* flags;
     void *dU, *ddelta, *dZ;
 };
 
@@ -358,8 +363,7 @@ __global__ __launch_bounds__(64) void selscan_bwd_totals_kernel(ScanBwd a)
     float* Q = a.totals + (size_t)c * ND + ch;
 #pragma unroll
     for (int n = 0; n < N; ++n) Q[(size_t)n * s.D] = q[n];
-    a.sums[(size_t)c * s.D + ch] = sum;
-    if (ch == 0) a.flags[c] = ended;
+    a.sums[(size_t)c * s.D + ch] = ended ? reset_mark() : sum;
 }
 
 // Sums over the wave's lanes of many values at once: a step adds two lanes' worth and deals two values out to the two, so the values
@@ -743,7 +747,6 @@ static SelscanPlan plan_of(int T, int D, int N, int G, bool is_bwd, bool has_sav
     const size_t ND = (size_t)N * D * sizeof(float);
     p.totals = take(ND * p.n_chunk);
     p.sums = take((size_t)p.n_chunk * D * sizeof(float));
-    p.flags = take((size_t)p.n_chunk * sizeof(int));
     if (!is_bwd) p.fin = take(ND * p.n_chunk);
     if (is_bwd) {
         p.part_bc = take((size_t)waves_per_group(D, G) * T * G * 2 * N * sizeof(float));
@@ -779,18 +782,25 @@ static ScanShape shape_of(const SelscanArgs& a, int chunk, int n_chunk)
     return s;
 }
 
-// Sequences without rows, where the state behind them is not the one in front already.
-static void pass_on(const SelscanArgs& a, const float* from, float* to, hipStream_t st)
+// Whether there may be sequences without rows whose state behind them is not the one in front already; with one chunk a kernel of its own
+// hands them on, else the carries' does.
+static bool to_pass_on(const SelscanArgs& a, const float* from, const float* to)
 {
-    if (to == nullptr || to == from || a.rows.n_seq == 0 || (a.rows.cu == nullptr && a.rows.T > 0)) return;
+    return to != nullptr && to != from && a.rows.n_seq > 0 && (a.rows.cu != nullptr || a.rows.T == 0);
+}
+static void pass_on(const SelscanArgs& a, const float* from, float* to, int n_chunk, hipStream_t st)
+{
+    if (n_chunk > 1 || !to_pass_on(a, from, to)) return;
     hipLaunchKernelGGL(selscan_empty_kernel, dim3(a.rows.n_seq < 256 ? a.rows.n_seq : 256), dim3(256), 0, st, a.rows, from, to, (long)a.N * a.D);
 }
 
 template <bool BWD>
-static void carry(const SelscanArgs& a, float* totals, const float* sums, const int* flags, int n_chunk, hipStream_t st)
+static void carry(const SelscanArgs& a, float* totals, const float* sums, int n_chunk, const float* from, float* to, hipStream_t st)
 {
     const long ND = (long)a.N * a.D;
-    hipLaunchKernelGGL(selscan_carry_kernel<BWD>, dim3((unsigned)((ND + 255) / 256)), dim3(256), 0, st, a.A, totals, sums, flags, n_chunk, a.D, ND);
+    const int groups = (int)((ND + 255) / 256), more = to_pass_on(a, from, to) ? (a.rows.n_seq < 256 ? a.rows.n_seq : 256) : 0;
+    hipLaunchKernelGGL(selscan_carry_kernel<BWD>, dim3(groups + more), dim3(256), 0, st, a.A, totals, sums, n_chunk, a.D, ND, groups, a.rows, from,
+                       to);
 }
 
 static ScanFwd fwd_of(const SelscanArgs& a, const SelscanPlan& p, char* ws)
@@ -802,7 +812,7 @@ static ScanFwd fwd_of(const SelscanArgs& a, const SelscanPlan& p, char* ws)
     f.Bm = a.Bm; f.Cm = a.Cm; f.ldb = a.ldb; f.ldc = a.ldc;
     f.A = a.A; f.Dskip = a.Dskip; f.dbias = a.delta_bias;
     f.S_in = a.S_in; f.S_out = a.S_out; f.saved = a.saved;
-    f.totals = (float*)(ws + p.totals); f.sums = (float*)(ws + p.sums); f.flags = (int*)(ws + p.flags); f.fin = (float*)(ws + p.fin);
+    f.totals = (float*)(ws + p.totals); f.sums = (float*)(ws + p.sums); f.fin = (float*)(ws + p.fin);
     f.Y = a.Y;
     f.s.same_buffer = a.S_out != nullptr && a.S_out == a.S_in && p.n_chunk > 1;
     return f;
@@ -814,7 +824,7 @@ static void walk(const SelscanArgs& a, const ScanFwd& f, bool out, hipStream_t s
     const unsigned gx = (unsigned)(f.s.G * f.s.nb);
     if (f.s.n_chunk > 1) {
         hipLaunchKernelGGL((selscan_fwd_kernel<IO, N, SCAN_TOTALS>), dim3(gx, f.s.n_chunk - 1), dim3(64), 0, st, f);
-        carry<false>(a, f.totals, f.sums, f.flags, f.s.n_chunk, st);
+        carry<false>(a, f.totals, f.sums, f.s.n_chunk, f.S_in, f.S_out, st);
     }
     if (out) hipLaunchKernelGGL((selscan_fwd_kernel<IO, N, SCAN_OUT>), dim3(gx, f.s.n_chunk), dim3(64), 0, st, f);
     else hipLaunchKernelGGL((selscan_fwd_kernel<IO, N, SCAN_SAVE>), dim3(gx, f.s.n_chunk), dim3(64), 0, st, f);
@@ -824,7 +834,7 @@ template <typename IO, int N>
 static hipError_t fwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, hipStream_t st)
 {
     ProfScope prof(KID_SELSCAN, st);
-    pass_on(a, a.S_in, a.S_out, st);
+    pass_on(a, a.S_in, a.S_out, p.n_chunk, st);
     if (a.rows.T > 0) {
         const ScanFwd f = fwd_of(a, p, ws);
         walk<IO, N>(a, f, true, st);
@@ -839,7 +849,7 @@ template <typename IO, int N>
 static hipError_t bwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, hipStream_t st)
 {
     ProfScope prof(KID_SELSCAN_BWD, st);
-    pass_on(a, a.dS_out, a.dS_in, st);
+    pass_on(a, a.dS_out, a.dS_in, p.n_chunk, st);
     ScanBwd b{};
     b.saved = a.saved;
     if (a.saved == nullptr && a.rows.T > 0) {
@@ -853,13 +863,13 @@ static hipError_t bwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, hipS
     b.U = a.U; b.delta = a.delta; b.Z = a.Z; b.dY = a.dY; b.Bm = a.Bm; b.Cm = a.Cm;
     b.ldu = a.ldu; b.ldd = a.ldd; b.ldz = a.ldz; b.lddy = a.lddy; b.ldb = a.ldb; b.ldc = a.ldc;
     b.A = a.A; b.Dskip = a.Dskip; b.dbias = a.delta_bias; b.S_in = a.S_in; b.dS_out = a.dS_out; b.dS_in = a.dS_in;
-    b.totals = (float*)(ws + p.totals); b.sums = (float*)(ws + p.sums); b.flags = (int*)(ws + p.flags);
+    b.totals = (float*)(ws + p.totals); b.sums = (float*)(ws + p.sums);
     b.part_bc = (float*)(ws + p.part_bc); b.part_A = (float*)(ws + p.part_A); b.part_D = (float*)(ws + p.part_D);
     b.dU = a.dU; b.ddelta = a.ddelta; b.dZ = a.dZ;
     const unsigned gx = (unsigned)(b.s.G * b.s.nb);
     if (p.n_chunk > 1) {
         hipLaunchKernelGGL((selscan_bwd_totals_kernel<IO, N>), dim3(gx, p.n_chunk - 1), dim3(64), 0, st, b);
-        carry<true>(a, b.totals, b.sums, b.flags, p.n_chunk, st);
+        carry<true>(a, b.totals, b.sums, p.n_chunk, a.dS_out, a.dS_in, st);
     }
     if (a.rows.T > 0) {
         hipLaunchKernelGGL((selscan_bwd_kernel<IO, N>), dim3(gx, p.n_chunk), dim3(N / NPW * 64), 0, st, b);

@@ -5,42 +5,42 @@
 //     dx_t = sum_j w[j] du_{t+j} (rows of the same sequence; the last m - 1 take d(state behind) too, and the state in front is a row like
 //     the others),  dw[j] = sum_t du_t x_{t-j},  dbias = sum_t du_t.
 //
-// Memory-bound: a thread owns V neighbouring channels, 16 bytes of them where the rows allow it, and walks a run of rows with the last
-// m - 1 inputs in registers, so a row is read once (and m - 1 rows more per run, from the L2).
+// Memory-bound: a thread owns two neighbouring channels where the rows allow it and walks a run of rows with the last m - 1 inputs in
+// registers, so a row is read once (and m - 1 rows more per run, from the L2).  65536 rows of 1536 channels, 4 taps, bf16: forward 74 us
+// (5.5 TB/s), gradient 138 + 8 us (4.3 TB/s).  Eight channels per thread, 16 bytes of a row, took 107 and 178: their weights lie 128
+// bytes apart from lane to lane, more lines than all the rows have.
 #include "chela_rows.h"
 
 namespace chela {
 
+// V neighbouring elements as they lie in memory
+template <int BYTES> struct Bits;
+template <> struct Bits<2> { typedef unsigned short type; };
+template <> struct Bits<4> { typedef unsigned type; };
+template <> struct Bits<8> { typedef u32x2 type; };
+template <> struct Bits<16> { typedef u32x4 type; };
+template <typename IO, int V> using Raw = typename Bits<V * (int)sizeof(IO)>::type;
+
 template <typename IO, int V>
-__device__ __forceinline__ void load_row(const IO* p, float (&x)[V])
+__device__ __forceinline__ void widen(Raw<IO, V> t, float (&x)[V])
 {
-    if (V == 1) {
-        x[0] = to_f(p[0]);
-    } else if (sizeof(IO) == 2) {
-        const u32x4 t = *reinterpret_cast<const u32x4*>(p);
+    struct Elements { IO e[V]; };
+    const Elements s = __builtin_bit_cast(Elements, t);
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            x[2 * i] = __uint_as_float(t[i] << 16);
-            x[2 * i + 1] = __uint_as_float(t[i] & 0xffff0000u);
-        }
-    } else {
-        const u32x4 t = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = __uint_as_float(t[i]);
-    }
+    for (int i = 0; i < V; ++i) x[i] = to_f(s.e[i]);
 }
 template <typename IO, int V>
-__device__ __forceinline__ void store_row(IO* p, const float (&x)[V])
+__device__ __forceinline__ Raw<IO, V> narrow(const float (&x)[V])
 {
-    if (V == 1) {
-        p[0] = from_f<IO>(x[0]);
-    } else {
-        struct alignas(16) { IO e[V]; } t;
+    struct Elements { IO e[V]; } s;
 #pragma unroll
-        for (int i = 0; i < V; ++i) t.e[i] = from_f<IO>(x[i]);
-        *reinterpret_cast<u32x4*>(p) = *reinterpret_cast<const u32x4*>(&t);
-    }
+    for (int i = 0; i < V; ++i) s.e[i] = from_f<IO>(x[i]);
+    return __builtin_bit_cast(Raw<IO, V>, s);
 }
+template <typename IO, int V>
+__device__ __forceinline__ void load_row(const IO* p, float (&x)[V]) { widen<IO, V>(*reinterpret_cast<const Raw<IO, V>*>(p), x); }
+template <typename IO, int V>
+__device__ __forceinline__ void store_row(IO* p, const float (&x)[V]) { *reinterpret_cast<Raw<IO, V>*>(p) = narrow<IO, V>(x); }
 
 template <int V>
 __device__ __forceinline__ void activation(const float (&u)[V], int silu, float (&y)[V])
@@ -101,20 +101,88 @@ __device__ __forceinline__ void weights(const ShortConvArgs& a, int ch, float (&
     }
 }
 
+// The states behind the sequences, 256 channels of sequence `q`.  A thread reads all m - 1 rows of a channel before it writes one, but the
+// rows of the sequences read the states in front too: where these are the same ones, the states come in a launch of their own, behind.
+template <typename IO, int M>
+__device__ __forceinline__ void state_behind(const ShortConvArgs& a, int q, int block)
+{
+    const int slot = slot_of(a.rows, q);
+    if (slot < 0) return;
+    Where at;
+    at.q = q;
+    at.set(a.rows);
+    if (at.end < at.beg) at.end = at.beg;
+    for (int ch = block * 256 + (int)threadIdx.x; ch < min(block * 256 + 256, a.D); ch += (int)blockDim.x) {
+        float back[M > 1 ? M - 1 : 1][1];
+        history<IO, 1, M>(a, at, at.end, ch, back);
+#pragma unroll
+        for (int j = 0; j < M - 1; ++j) ((IO*)a.S_out)[((size_t)slot * (M - 1) + (M - 2 - j)) * a.D + ch] = from_f<IO>(back[j][0]);
+    }
+}
+template <typename IO, int M>
+__global__ __launch_bounds__(256) void short_conv_state_kernel(ShortConvArgs a)
+{
+    const int nb = (a.D + 255) / 256;
+    state_behind<IO, M>(a, blockIdx.x / nb, blockIdx.x % nb);
+}
+
+// Workgroups go to the eight XCDs in turn: the neighbours in memory, which read each other's last rows, to one of them.
+__device__ __forceinline__ int xcd_neighbours(int i, int n)
+{
+    const int per = n / 8;
+    return i < per * 8 ? i % 8 * per + i / 8 : i;
+}
+
 template <typename IO, int V, int M, int RUN>
 __global__ __launch_bounds__(256) void short_conv_kernel(ShortConvArgs a)
 {
     const int across = (a.D + V * (int)blockDim.x - 1) / (V * (int)blockDim.x);          // workgroups that a run takes
+    const Rows& R = a.rows;
+    const int runs = (R.T + RUN - 1) / RUN;
+    if ((int)blockIdx.x >= runs * across) {
+        const int nb = (a.D + 255) / 256, i = blockIdx.x - runs * across;
+        state_behind<IO, M>(a, i / nb, i % nb);
+        return;
+    }
     const int ch = (blockIdx.x % across * blockDim.x + threadIdx.x) * V;
     if (ch >= a.D) return;
-    const Rows& R = a.rows;
+    const int t0 = xcd_neighbours(blockIdx.x / across, runs) * RUN, t1 = min(t0 + RUN, R.T);
     float w[M][V], bias[V], back[M > 1 ? M - 1 : 1][V];
-    weights<V, M>(a, ch, w, bias);
-    const int t0 = blockIdx.x / across * RUN, t1 = min(t0 + RUN, R.T);
     Where at;
     at.start(R, t0);
+    if (at.q < R.n_seq && t0 - (M - 1) >= at.beg && t0 + RUN <= at.end) {
+        // within one sequence: all rows on their way before the first is looked at
+        Raw<IO, V> x[RUN + M - 1];
+#pragma unroll
+        for (int i = 0; i < RUN + M - 1; ++i) x[i] = row_load((const Raw<IO, V>*)((const IO*)a.X + (size_t)(t0 - (M - 1) + i) * a.ldx), ch * sizeof(IO));
+        weights<V, M>(a, ch, w, bias);
+#pragma unroll
+        for (int j = 0; j < M - 1; ++j) widen<IO, V>(x[M - 2 - j], back[j]);
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            float now[V], u[V], y[V];
+            widen<IO, V>(x[i + M - 1], now);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                u[e] = fmaf(w[0][e], now[e], bias[e]);
+#pragma unroll
+                for (int j = 1; j < M; ++j) u[e] = fmaf(w[j][e], back[j - 1][e], u[e]);
+            }
+            activation<V>(u, a.silu, y);
+            row_store((Raw<IO, V>*)((IO*)a.Y + (size_t)(t0 + i) * a.D), ch * sizeof(IO), narrow<IO, V>(y));
+#pragma unroll
+            for (int j = M - 2; j > 0; --j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) back[j][e] = back[j - 1][e];
+            if (M > 1)
+#pragma unroll
+                for (int e = 0; e < V; ++e) back[0][e] = now[e];
+        }
+        return;
+    }
+    weights<V, M>(a, ch, w, bias);
     int known = -1;                                   // the sequence that `back` is of
-#pragma unroll 4
+#pragma unroll 1
     for (int t = t0; t < t1; ++t) {
         if (!at.at(R, t)) continue;
         if (known != at.q) { history<IO, V, M>(a, at, t, ch, back); known = at.q; }
@@ -136,25 +204,6 @@ __global__ __launch_bounds__(256) void short_conv_kernel(ShortConvArgs a)
 #pragma unroll
             for (int e = 0; e < V; ++e) back[0][e] = x[e];
     }
-}
-
-// The states behind the sequences.  A kernel of its own: over the states in front it has to come when those have been read, and a
-// thread reads all m - 1 rows of its channels before it writes one.
-template <typename IO, int M>
-__global__ __launch_bounds__(256) void short_conv_state_kernel(ShortConvArgs a)
-{
-    const int nb = (a.D + 255) / 256, q = blockIdx.x / nb, ch = blockIdx.x % nb * 256 + threadIdx.x;
-    if (ch >= a.D) return;
-    const int slot = slot_of(a.rows, q);
-    if (slot < 0) return;
-    Where at;
-    at.q = q;
-    at.set(a.rows);
-    if (at.end < at.beg) at.end = at.beg;
-    float back[M > 1 ? M - 1 : 1][1];
-    history<IO, 1, M>(a, at, at.end, ch, back);
-#pragma unroll
-    for (int j = 0; j < M - 1; ++j) ((IO*)a.S_out)[((size_t)slot * (M - 1) + (M - 2 - j)) * a.D + ch] = from_f<IO>(back[j][0]);
 }
 
 // One row for each of R requests: the states move on by one.
@@ -200,13 +249,65 @@ __global__ __launch_bounds__(256) void short_conv_bwd_kernel(ShortConvArgs a, in
 #pragma unroll
         for (int j = 0; j < M; ++j) dw[j][e] = 0.f;
     }
-    for (int run = blockIdx.y; run < runs; run += gridDim.y) {
+    // neighbouring runs, so that the rows that two runs share come from the L2
+    const int mine = (runs + (int)gridDim.y - 1) / (int)gridDim.y, first = (int)blockIdx.y * mine;
+    for (int run = first; run < min(first + mine, runs); ++run) {
         const int t0 = run * RUN, t1 = min(t0 + RUN, R.T);
         float back[M > 1 ? M - 1 : 1][V], pend[M][V];
         Where at;
         at.start(R, t0);
+        if (at.q < R.n_seq && t0 - (M - 1) >= at.beg && t0 + RUN + M - 1 <= at.end) {
+            // the run and all that it shares with others within one sequence, none of the last m - 1 rows in it
+            Raw<IO, V> xs[RUN + 2 * (M - 1)], dys[RUN + M - 1];
+#pragma unroll
+            for (int i = 0; i < RUN + 2 * (M - 1); ++i)
+                xs[i] = row_load((const Raw<IO, V>*)((const IO*)a.X + (size_t)(t0 - (M - 1) + i) * a.ldx), ch * sizeof(IO));
+#pragma unroll
+            for (int i = 0; i < RUN + M - 1; ++i)
+                dys[i] = row_load((const Raw<IO, V>*)((const IO*)a.dY + (size_t)(t0 + i) * a.lddy), ch * sizeof(IO));
+            float x[M][V];                            // x[j]: x_{t-j}
+#pragma unroll
+            for (int j = 1; j < M; ++j) widen<IO, V>(xs[M - 1 - j], x[j]);
+#pragma unroll
+            for (int k = 0; k < M; ++k)
+#pragma unroll
+                for (int e = 0; e < V; ++e) pend[k][e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < RUN + M - 1; ++i) {
+                float du[V];
+                widen<IO, V>(xs[i + M - 1], x[0]);
+                widen<IO, V>(dys[i], du);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    if (a.silu) {
+                        float u = bias[e];
+#pragma unroll
+                        for (int j = 0; j < M; ++j) u = fmaf(w[j][e], x[j][e], u);
+                        const float s = sigmoid_(u);
+                        du[e] *= s * fmaf(u, 1.f - s, 1.f);
+                    }
+#pragma unroll
+                    for (int j = 0; j < M; ++j) pend[j][e] = fmaf(w[j][e], du[e], pend[j][e]);
+                    if (i < RUN) {
+                        db[e] += du[e];
+#pragma unroll
+                        for (int j = 0; j < M; ++j) dw[j][e] = fmaf(du[e], x[j][e], dw[j][e]);
+                    }
+                }
+                if (i >= M - 1)
+                    row_store((Raw<IO, V>*)((IO*)a.dX + (size_t)(t0 + i - (M - 1)) * a.D), ch * sizeof(IO), narrow<IO, V>(pend[M - 1]));
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+#pragma unroll
+                    for (int j = M - 1; j > 0; --j) { x[j][e] = x[j - 1][e]; pend[j][e] = pend[j - 1][e]; }
+                    pend[0][e] = 0.f;
+                }
+            }
+            continue;
+        }
         int known = -1;
         // rows t1 .. t1 + m - 2 of the same sequence give to the rows of this run too
+#pragma unroll 1
         for (int t = t0; t - t1 < M - 1; ++t) {
             if (t >= R.T || (t >= t1 && (known != at.q || t >= at.end))) break;
             if (t < t1 && !at.at(R, t)) continue;
@@ -286,18 +387,21 @@ __global__ __launch_bounds__(256) void short_conv_bwd_kernel(ShortConvArgs a, in
     }
 }
 
-__global__ __launch_bounds__(256) void short_conv_sum_kernel(ShortConvArgs a, int parts)
+// The workgroups' sums, sixteen waves to 64 channels.
+__global__ __launch_bounds__(1024) void short_conv_sum_kernel(ShortConvArgs a, int parts)
 {
-    __shared__ float s_sum[4][64];
-    const int ch = blockIdx.x * 64 + (threadIdx.x & 63), j = blockIdx.y, w = threadIdx.x >> 6;
-    const int c = min(ch, a.D - 1);
+    __shared__ float s_sum[16][64];
+    const int lane = threadIdx.x & 63, ch = blockIdx.x * 64 + lane, j = blockIdx.y, w = threadIdx.x >> 6;
+    const float* from = a.part + (size_t)j * a.D + min(ch, a.D - 1);
     float x = 0.f;
-    for (int p = w; p < parts; p += 4) x += a.part[((size_t)p * (a.m + 1) + j) * a.D + c];
-    s_sum[w][threadIdx.x & 63] = x;
+#pragma unroll 8
+    for (int p = w; p < parts; p += 16) x += from[(size_t)p * (a.m + 1) * a.D];
+    s_sum[w][lane] = x;
     __syncthreads();
     if (w != 0 || ch >= a.D) return;
     x = 0.f;
-    for (int i = 0; i < 4; ++i) x += s_sum[i][threadIdx.x];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x += s_sum[i][lane];
     if (j < a.m) a.dw[(size_t)ch * a.m + j] = x;
     else if (a.dbias) a.dbias[ch] = x;
 }
@@ -316,11 +420,11 @@ __global__ __launch_bounds__(256) void short_conv_empty_kernel(ShortConvArgs a)
 }
 
 // -------------------------------------------------------------------------------------------------------------------- host
-// 16 bytes of a row per thread, where every row begins on 16 bytes
-static bool wide(const ShortConvArgs& a, int dtype)
+// Two neighbouring channels per thread, where every row begins on as many bytes
+static bool pairs(const ShortConvArgs& a, int dtype)
 {
-    const int V = dtype == 0 ? 8 : 4;
-    return a.D % V == 0 && a.ldx % V == 0 && a.lddy % V == 0 && (((uintptr_t)a.X | (uintptr_t)a.dY) & 15u) == 0;
+    const unsigned bytes = dtype == 0 ? 4 : 8;
+    return a.D % 2 == 0 && a.ldx % 2 == 0 && a.lddy % 2 == 0 && (((uintptr_t)a.X | (uintptr_t)a.dY) & (bytes - 1)) == 0;
 }
 static unsigned threads_for(int vectors) { return vectors >= 256 ? 256u : (unsigned)(vectors + 63) / 64 * 64; }
 
@@ -337,25 +441,33 @@ static unsigned threads_for(int vectors) { return vectors >= 256 ? 256u : (unsig
         default: return hipErrorInvalidValue;                                                                         \
     }
 #define CHELA_TYPES(F)                                                                                                \
-    if (dtype == 0) { if (wide(a, dtype)) { CHELA_TAPS(F, bf16, 8) } else { CHELA_TAPS(F, bf16, 1) } }                \
-    else { if (wide(a, dtype)) { CHELA_TAPS(F, float, 4) } else { CHELA_TAPS(F, float, 1) } }
+    if (dtype == 0) { if (V > 1) { CHELA_TAPS(F, bf16, 2) } else { CHELA_TAPS(F, bf16, 1) } }                         \
+    else { if (V > 1) { CHELA_TAPS(F, float, 2) } else { CHELA_TAPS(F, float, 1) } }
 
-constexpr int kRun = 16, kBwdRun = 32;
+// Rows of a run: the fewer, the more rows are read twice, the more, the fewer workgroups there are to read.  Forward, us, runs of 8, 16, 32
+// rows: 83, 74, 70 at 65536 rows, 13.7, 15.0, - at 6007 (the short ones below 2048 workgroups).  Gradient, runs of 8 in 512, 768, 1024
+// parts: 154, 138, 141, and 5, 8, 10 to add them up.
+constexpr int kRun = 16, kShortRun = 8, kBwdRun = 8, kBwdParts = 768;
 
 hipError_t launch_short_conv_fwd(const ShortConvArgs& a, int dtype, hipStream_t st)
 {
     ProfScope prof(KID_SHORT_CONV, st);
+    const unsigned states = a.S_out && a.m > 1 ? (unsigned)((a.D + 255) / 256) * (unsigned)a.rows.n_seq : 0;
+    const bool apart = a.S_out == a.S_in || a.rows.T == 0;
     if (a.rows.T > 0) {
-        const int V = wide(a, dtype) ? (dtype == 0 ? 8 : 4) : 1, vectors = (a.D + V - 1) / V;
-        const unsigned threads = threads_for(vectors);
-        const dim3 grid(((vectors + threads - 1) / threads) * (unsigned)((a.rows.T + kRun - 1) / kRun));
-#define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_kernel<IO, V, M, kRun>), grid, dim3(threads), 0, st, a)
+        const int V = pairs(a, dtype) ? 2 : 1, vectors = (a.D + V - 1) / V;
+        const unsigned threads = threads_for(vectors), across = (vectors + threads - 1) / threads;
+        const bool few = (long)((a.rows.T + kRun - 1) / kRun) * across < 2048;
+        const int run = few ? kShortRun : kRun;
+        const dim3 grid(across * (unsigned)((a.rows.T + run - 1) / run) + (apart ? 0 : states));
+#define CHELA_F(IO, V, M)                                                                                             \
+    if (few) hipLaunchKernelGGL((short_conv_kernel<IO, V, M, kShortRun>), grid, dim3(threads), 0, st, a);             \
+    else hipLaunchKernelGGL((short_conv_kernel<IO, V, M, kRun>), grid, dim3(threads), 0, st, a)
         CHELA_TYPES(CHELA_F)
 #undef CHELA_F
     }
-    if (a.S_out && a.m > 1 && a.rows.n_seq > 0) {
-        const dim3 grid((unsigned)((a.D + 255) / 256) * (unsigned)a.rows.n_seq);
-#define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_state_kernel<IO, M>), grid, dim3(256), 0, st, a)
+    if (states > 0 && apart) {
+#define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_state_kernel<IO, M>), dim3(states), dim3(256), 0, st, a)
         if (dtype == 0) { CHELA_TAPS(CHELA_F, bf16, 1) } else { CHELA_TAPS(CHELA_F, float, 1) }
 #undef CHELA_F
     }
@@ -366,20 +478,20 @@ int short_conv_bwd_parts(int T, int D, int dtype)
 {
     (void)D; (void)dtype;
     const int runs = (T + kBwdRun - 1) / kBwdRun;
-    return runs < 512 ? (runs > 0 ? runs : 1) : 512;
+    return runs < kBwdParts ? (runs > 0 ? runs : 1) : kBwdParts;
 }
 
 hipError_t launch_short_conv_bwd(const ShortConvArgs& a, int dtype, hipStream_t st)
 {
     ProfScope prof(KID_SHORT_CONV, st);
-    const int V = wide(a, dtype) ? (dtype == 0 ? 8 : 4) : 1, vectors = (a.D + V - 1) / V;
+    const int V = pairs(a, dtype) ? 2 : 1, vectors = (a.D + V - 1) / V;
     const unsigned threads = threads_for(vectors);
     const int runs = (a.rows.T + kBwdRun - 1) / kBwdRun, parts = short_conv_bwd_parts(a.rows.T, a.D, dtype);
     const dim3 grid((vectors + threads - 1) / threads, parts);
 #define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_bwd_kernel<IO, V, M, kBwdRun>), grid, dim3(threads), 0, st, a, runs)
     CHELA_TYPES(CHELA_F)
 #undef CHELA_F
-    hipLaunchKernelGGL(short_conv_sum_kernel, dim3((a.D + 63) / 64, a.m + 1), dim3(256), 0, st, a, parts);
+    hipLaunchKernelGGL(short_conv_sum_kernel, dim3((a.D + 63) / 64, a.m + 1), dim3(1024), 0, st, a, parts);
     if (a.dS_in && a.m > 1 && (a.rows.cu || a.rows.T == 0)) {
         const dim3 g(a.rows.n_seq < 256 ? a.rows.n_seq : 256);
         if (dtype == 0) hipLaunchKernelGGL(short_conv_empty_kernel<bf16>, g, dim3(256), 0, st, a);
@@ -391,7 +503,7 @@ hipError_t launch_short_conv_bwd(const ShortConvArgs& a, int dtype, hipStream_t 
 hipError_t launch_short_conv_step(const ShortConvArgs& a, int dtype, hipStream_t st)
 {
     ProfScope prof(KID_SHORT_CONV, st);
-    const int V = wide(a, dtype) ? (dtype == 0 ? 8 : 4) : 1, nb = (a.D + 64 * V - 1) / (64 * V);
+    const int V = pairs(a, dtype) ? 2 : 1, nb = (a.D + 64 * V - 1) / (64 * V);
     const dim3 grid((unsigned)nb * (unsigned)a.rows.T);
 #define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_step_kernel<IO, V, M>), grid, dim3(64), 0, st, a)
     CHELA_TYPES(CHELA_F)
