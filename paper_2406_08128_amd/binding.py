@@ -33,7 +33,9 @@ _host_module = None         # that module, None where there is none
 _fn = dict.fromkeys(("linattn_fwd", "linattn_fwd_f32", "linattn_fwd_state", "linattn_bwd", "linattn_bwd_f32", "linattn_fwd_gated",
                      "linattn_zfwd_gated", "linattn_saved_bytes", "gate_norm_bwd", "linattn_zbwd_saved", "linattn_noncausal_fwd_gated",
                      "linattn_noncausal_bwd", "longconv_spectrum", "longconv_spectrum_bytes", "shortlong_conv_fwd",
-                     "shortlong_conv_fwd_f32", "shortlong_conv_bwd", "shortlong_conv_bwd_f32"), 0)
+                     "shortlong_conv_fwd_f32", "shortlong_conv_bwd", "shortlong_conv_bwd_f32", "short_conv_fwd", "short_conv_fwd_f32",
+                     "short_conv_step", "short_conv_step_f32", "selscan_fwd", "selscan_fwd_f32", "selscan_step", "selscan_step_f32",
+                     "selscan_saved_bytes", "block_norm_fwd", "block_norm_fwd_f32"), 0)
 
 
 class ChelaError(RuntimeError):
@@ -844,6 +846,9 @@ def _slot_map(slots, n_seq, states, device):
 def chela_short_conv_fwd(X, w, bias=None, silu=True, cu=None, S_in=None, S_out=None, slots=None, Y=None, stream=None):
     """Y = silu(bias + sum_j w[:, j] X[t - j]) over the tokens of each sequence (silu=False: without the activation).
     w [D, m], bias [D] float32; S_in, S_out [n_slots, m-1, D] the last inputs in front of and behind the sequences (S_out may be S_in)."""
+    r = _host("short_conv_fwd")(_fn["short_conv_fwd"], _fn["short_conv_fwd_f32"], X, w, bias, silu, cu, S_in, S_out, slots, Y, stream)
+    if r is not None:
+        return _host_result(r)
     pcu, n_seq, T, D = _sequences(X, cu, "X")
     sfx, _ = _suffix(X)
     px, ldx = _row_stride(X, X, "X")
@@ -891,6 +896,9 @@ def chela_short_conv_bwd(X, w, dY, bias=None, silu=True, cu=None, S_in=None, dS_
 def chela_short_conv_step(x, w, S, bias=None, silu=True, slots=None, y=None, stream=None):
     """One token for each of R requests, x [R, D]: y as chela_short_conv_fwd's, the states S [n_slots, m-1, D] move on in place.  A row
     whose slot is not one of S's is left out: y keeps what it holds there."""
+    r = _host("short_conv_step")(_fn["short_conv_step"], _fn["short_conv_step_f32"], x, w, S, bias, silu, slots, y, stream)
+    if r is not None:
+        return _host_result(r)
     if not x.is_cuda or x.dim() != 2 or w.dim() != 2:
         raise ValueError("x must be a device tensor [R, D], w [D, m]")
     R, D = x.shape
@@ -936,6 +944,10 @@ def chela_selscan_fwd(U, delta, A, Bm, Cm, D=None, Z=None, delta_bias=None, soft
     """(Y, saved): the selective scan h[n] = exp(dl A[n]) h[n] + dl u B[n], y = sum_n C[n] h[n] + D u, gated with silu(Z), with
     dl = softplus(delta + delta_bias).  A [N, D], D and delta_bias [D] float32; Bm, Cm [..., G, N] or [..., N]; states [n_slots, N, D]
     float32.  saved is None unless asked for (for chela_selscan_bwd)."""
+    r = _host("selscan_fwd")(_fn["selscan_fwd"], _fn["selscan_fwd_f32"], _fn["selscan_saved_bytes"], U, delta, A, Bm, Cm, D, Z, delta_bias,
+                             softplus, cu, S_in, S_out, slots, want_saved, Y, stream)
+    if r is not None:
+        return _host_result(r)
     pcu, n_seq, T, width = _sequences(U, cu, "U")
     sfx, _ = _suffix(U)
     args, N, G = _scan_inputs(U, delta, A, Bm, Cm, D, Z, delta_bias, softplus)
@@ -987,6 +999,9 @@ def chela_selscan_bwd(U, delta, A, Bm, Cm, dY, D=None, Z=None, delta_bias=None, 
 def chela_selscan_step(u, delta, A, Bm, Cm, S, D=None, z=None, delta_bias=None, softplus=True, slots=None, y=None, stream=None):
     """One token for each of R requests, u [R, D]: y as chela_selscan_fwd's, the states S [n_slots, N, D] are updated in place.  A row
     whose slot is not one of S's is left out: y keeps what it holds there."""
+    r = _host("selscan_step")(_fn["selscan_step"], _fn["selscan_step_f32"], u, delta, A, Bm, Cm, S, D, z, delta_bias, softplus, slots, y, stream)
+    if r is not None:
+        return _host_result(r)
     if not u.is_cuda or u.dim() != 2:
         raise ValueError("u must be a device tensor [R, D]")
     R, width = u.shape
@@ -1029,6 +1044,10 @@ def _norm_inputs(Y, X, gate, w_post, w_pre):
 def chela_block_norm_fwd(Y, X, gate=None, w_post=None, w_pre=None, scale=1.0, eps=1e-5, X_out=None, Nrm=None, stream=None):
     """(X_out, Nrm): X_out = X + scale * Norm(Y) * w_post * gate (w_post None: no norm of Y), Nrm = Norm(X_out) * w_pre (None without
     w_pre) over the last dimension.  Y None: Nrm = Norm(X) * w_pre alone, and X_out is X.  X_out may be X."""
+    if X_out is None and Nrm is None and Y is not None:
+        r = _host("block_norm_fwd")(_fn["block_norm_fwd"], _fn["block_norm_fwd_f32"], Y, X, gate, w_post, w_pre, scale, eps, stream)
+        if r is not None:
+            return _host_result(r)
     sfx, rows, D, x_f32, ptrs = _norm_inputs(Y, X, gate, w_post, w_pre)
     dev, io = X.device, X.dtype if Y is None else Y.dtype
     if Y is None:

@@ -15,6 +15,11 @@
 //   zbwd_saved(f, Z, affine, V, dO, saved, stream) -> (dZ, d_affine, dV)
 //   spectrum(f, bytes, k_long, stream) -> spectrum
 //   conv_fwd(f, f32, X, w_short, spectrum, stream) -> Z;  conv_bwd(f, f32, X, w_short, spectrum, dZ, stream) -> (dX, d_w_short, d_k_long)
+//   short_conv_fwd(f, f32, X, w, bias, silu, cu, S_in, S_out, slots, Y, stream) -> Y
+//   short_conv_step(f, f32, x, w, S, bias, silu, slots, y, stream) -> y
+//   selscan_fwd(f, f32, saved_bytes, U, delta, A, Bm, Cm, D, Z, delta_bias, softplus, cu, S_in, S_out, slots, want_saved, Y, stream) -> (Y, saved)
+//   selscan_step(f, f32, u, delta, A, Bm, Cm, S, D, z, delta_bias, softplus, slots, y, stream) -> y
+//   block_norm_fwd(f, f32, Y, X, gate, w_post, w_pre, scale, eps, stream) -> (X_out, Nrm)
 // Host side of a call, us, the binding's own lines and these: forward, one launch, 8.5 and 4.4, two launches 9.7 and 6.2; with the
 // state 9.9 and 4.8, 12.1 and 7.2; backward, two launches, 11.4 and 7.5; the three calls of a gated layer's step, six launches, 39.6 and 23;
 // spectrum, forward and gradient of a convolution, 22.5 and 15.
@@ -425,10 +430,317 @@ PyObject* conv_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- operators on rows: tensors whose rows may be slices of wider ones
+typedef int (*short_conv_fwd_fn)(const void*, long long, const float*, int, const float*, int, const int*, int, int, int, const void*, void*,
+                                 const int*, int, void*, void*);
+typedef int (*short_conv_step_fn)(const void*, long long, const float*, int, const float*, int, void*, const int*, int, int, int, void*, void*);
+typedef int (*selscan_fwd_fn)(const void*, long long, const void*, long long, const float*, const void*, long long, const void*, long long,
+                              const float*, const void*, long long, const float*, int, const int*, int, int, int, int, int, const float*,
+                              float*, const int*, int, void*, void*, void*);
+typedef int (*selscan_step_fn)(const void*, long long, const void*, long long, const float*, const void*, long long, const void*, long long,
+                               const float*, const void*, long long, const float*, int, float*, const int*, int, int, int, int, int, void*, void*);
+typedef size_t (*selscan_saved_fn)(int, int, int);
+typedef int (*block_norm_fwd_fn)(const void*, const void*, const void*, const float*, const float*, void*, void*, float, float, long long, int,
+                                 int, void*);
+
+struct Rows {
+    c10::DeviceIndex dev;
+    at::ScalarType type;
+    int64_t lead[2], T, D;          // leading sizes (one or two), their product, the row's width
+    int dims;
+    int n_seq, n_slots;
+    const int *cu, *slots;
+
+    // a tensor of that type there, contiguous or not
+    bool there(PyObject* o, at::ScalarType t) const
+    {
+        if (!THPVariable_CheckExact(o)) return false;
+        const at::Tensor& x = THPVariable_Unpack(o);
+        return x.defined() && x.is_cuda() && x.layout() == at::kStrided && x.has_storage() && x.scalar_type() == t && x.get_device() == dev &&
+               !x.key_set().has_any(c10::DispatchKeySet({c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::FuncTorchGradWrapper,
+                                                         c10::DispatchKey::Functionalize, c10::DispatchKey::Python}));
+    }
+    // The first tensor, [B, L, D] or [T, D], and its sequences.
+    bool first(PyObject* o, PyObject* ocu, PyObject* ostream)
+    {
+        if (modes() || ostream != Py_None || !on_gpu(o)) return false;
+        const at::Tensor& x = THPVariable_Unpack(o);
+        type = x.scalar_type();
+        dev = c10::hip::current_device();
+        if ((type != at::kBFloat16 && type != at::kFloat) || !there(o, type)) return false;
+        dims = (int)x.dim() - 1;
+        if (dims < 1 || dims > 2) return false;
+        T = 1;
+        for (int i = 0; i < dims; ++i) {
+            lead[i] = x.size(i);
+            if (lead[i] > 0x7fffffff) return false;
+            T *= lead[i];
+        }
+        D = x.size(dims);
+        if (T > 0x7fffffff || D > 0x7fffffff) return false;
+        cu = slots = nullptr;
+        n_seq = dims == 2 ? (int)lead[0] : 1;
+        if (ocu != Py_None) {
+            if (dims != 1 || !plain(ocu, at::kInt, dev)) return false;
+            const at::Tensor& c = THPVariable_Unpack(ocu);
+            if (c.dim() != 1 || c.size(0) < 1 || c.size(0) > 0x7fffffff) return false;
+            n_seq = (int)c.size(0) - 1;
+            cu = (const int*)c.data_ptr();
+        }
+        n_slots = n_seq;
+        return true;
+    }
+    // A tensor with the first one's rows and `width` elements in each: address and stride of the rows.
+    bool rows(PyObject* o, int64_t width, const void** p, long long* ld) const
+    {
+        if (!there(o, type)) return false;
+        const at::Tensor& x = THPVariable_Unpack(o);
+        if (x.dim() < dims + 1) return false;
+        for (int i = 0; i < dims; ++i) if (x.size(i) != lead[i]) return false;
+        int64_t w = 1;
+        for (int k = (int)x.dim() - 1; k >= dims; --k) {
+            if (x.size(k) > 1 && x.stride(k) != w) return false;
+            w *= x.size(k);
+        }
+        if (w != width) return false;
+        int64_t step = -1, n = 1;
+        for (int k = dims - 1; k >= 0; --k) {
+            if (x.size(k) <= 1) continue;
+            if (step < 0) step = x.stride(k);
+            else if (x.stride(k) != step * n) return false;
+            n *= x.size(k);
+        }
+        *p = x.data_ptr();
+        *ld = step < 0 ? (width > 1 ? width : 1) : step;
+        return true;
+    }
+    template <typename T_>
+    bool dense(PyObject* o, at::ScalarType t, at::IntArrayRef sizes, bool optional, T_** p) const
+    {
+        *p = nullptr;
+        if (optional && o == Py_None) return true;
+        if (!plain(o, t, dev) || THPVariable_Unpack(o).sizes() != sizes) return false;
+        *p = (T_*)THPVariable_Unpack(o).data_ptr();
+        return true;
+    }
+    bool slot_map(PyObject* o, PyObject* states)
+    {
+        if (o == Py_None) return true;
+        if (states == Py_None || !THPVariable_CheckExact(states) || THPVariable_Unpack(states).dim() < 1) return false;
+        const int64_t n = THPVariable_Unpack(states).size(0);
+        if (n > 0x7fffffff || !dense(o, at::kInt, {n_seq}, false, &slots)) return false;
+        n_slots = (int)n;
+        return true;
+    }
+    PyObject* function(PyObject* const* a) const { return a[type == at::kFloat ? 1 : 0]; }
+};
+
+// True or False, or something else: -1
+int flag(PyObject* o) { return o == Py_True ? 1 : o == Py_False ? 0 : -1; }
+
+PyObject* given_or(PyObject* o, at::Tensor& made)
+{
+    if (o == Py_None) return THPVariable_Wrap(std::move(made));
+    Py_INCREF(o);
+    return o;
+}
+
+PyObject* short_conv_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 12) { PyErr_SetString(PyExc_TypeError, "short_conv_fwd takes twelve arguments"); return nullptr; }
+    Rows x;
+    const void *px, *pin;
+    long long ldx;
+    const float *pw, *pb;
+    void *pout, *py;
+    const int silu = flag(a[5]);
+    if (silu < 0 || !x.first(a[2], a[6], a[11]) || !x.rows(a[2], x.D, &px, &ldx) || !plain_sizes(a[3], at::kFloat, x.dev, 2)) Py_RETURN_NONE;
+    const int64_t m = THPVariable_Unpack(a[3]).size(1);
+    if (m < 1 || !x.dense(a[3], at::kFloat, {x.D, m}, false, &pw) || !x.dense(a[4], at::kFloat, {x.D}, true, &pb) ||
+        !x.slot_map(a[9], a[7] != Py_None ? a[7] : a[8]) || !x.dense(a[7], x.type, {x.n_slots, m - 1, x.D}, true, &pin) ||
+        !x.dense(a[8], x.type, {x.n_slots, m - 1, x.D}, true, &pout))
+        Py_RETURN_NONE;
+    const at::Tensor& X = THPVariable_Unpack(a[2]);
+    if (!x.dense(a[10], x.type, X.sizes(), true, &py)) Py_RETURN_NONE;
+    const auto f = address<short_conv_fwd_fn>(x.function(a));
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor y;
+    int rc;
+    {
+        const without_interpreter_lock free;
+        if (a[10] == Py_None) { y = at::empty(X.sizes(), like(X).memory_format(at::MemoryFormat::Contiguous)); py = y.data_ptr(); }
+        rc = f(px, ldx, pw, (int)m, pb, silu, x.cu, x.n_seq, (int)x.T, (int)x.D, pin, pout, x.slots, x.n_slots, py, stream_of(x.dev));
+    }
+    return rc != 0 ? PyLong_FromLong(rc) : given_or(a[10], y);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* short_conv_step(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 10) { PyErr_SetString(PyExc_TypeError, "short_conv_step takes ten arguments"); return nullptr; }
+    Rows x;
+    const void* px;
+    long long ldx;
+    const float *pw, *pb;
+    void *ps, *py;
+    const int silu = flag(a[6]);
+    if (silu < 0 || !x.first(a[2], Py_None, a[9]) || x.dims != 1 || !x.rows(a[2], x.D, &px, &ldx) || !plain_sizes(a[3], at::kFloat, x.dev, 2))
+        Py_RETURN_NONE;
+    x.n_seq = x.n_slots = (int)x.T;
+    const int64_t m = THPVariable_Unpack(a[3]).size(1);
+    if (m < 1 || !x.dense(a[3], at::kFloat, {x.D, m}, false, &pw) || !x.dense(a[5], at::kFloat, {x.D}, true, &pb) || !x.slot_map(a[7], a[4]) ||
+        !x.dense(a[4], x.type, {x.n_slots, m - 1, x.D}, false, &ps) || !x.dense(a[8], x.type, {x.T, x.D}, true, &py))
+        Py_RETURN_NONE;
+    const at::Tensor& X = THPVariable_Unpack(a[2]);
+    const auto f = address<short_conv_step_fn>(x.function(a));
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor y;
+    int rc;
+    {
+        const without_interpreter_lock free;
+        if (a[8] == Py_None) { y = at::empty({x.T, x.D}, like(X)); py = y.data_ptr(); }
+        rc = f(px, ldx, pw, (int)m, pb, silu, ps, x.slots, x.n_slots, (int)x.T, (int)x.D, py, stream_of(x.dev));
+    }
+    return rc != 0 ? PyLong_FromLong(rc) : given_or(a[8], y);
+    END_HANDLE_TH_ERRORS
+}
+
+// What the scan's calls have in common: U, delta, A, Bm, Cm and D, Z, delta_bias.
+struct Scan {
+    const void *U, *delta, *Bm, *Cm, *Z = nullptr;
+    long long ldu, ldd, ldb, ldc, ldz = 0;
+    const float *A, *D, *bias;
+    int64_t N, G;
+    bool read(const Rows& x, PyObject* const* five, PyObject* const* three)
+    {
+        if (!x.rows(five[0], x.D, &U, &ldu) || !x.rows(five[1], x.D, &delta, &ldd) || !THPVariable_CheckExact(five[3]) ||
+            !THPVariable_CheckExact(five[4]))
+            return false;
+        const at::Tensor &b = THPVariable_Unpack(five[3]), &c = THPVariable_Unpack(five[4]);
+        if (!b.defined() || !c.defined() || THPVariable_Unpack(five[1]).dim() != x.dims + 1 || b.dim() < x.dims + 1 || b.dim() > x.dims + 2 ||
+            b.sizes() != c.sizes())
+            return false;
+        N = b.size(-1);
+        G = b.dim() == x.dims + 2 ? b.size(-2) : 1;
+        if (N > 0x7fffffff || G > 0x7fffffff) return false;
+        if (three[1] != Py_None && (!x.rows(three[1], x.D, &Z, &ldz) || THPVariable_Unpack(three[1]).dim() != x.dims + 1)) return false;
+        return x.rows(five[3], N * G, &Bm, &ldb) && x.rows(five[4], N * G, &Cm, &ldc) && x.dense(five[2], at::kFloat, {N, x.D}, false, &A) &&
+               x.dense(three[0], at::kFloat, {x.D}, true, &D) && x.dense(three[2], at::kFloat, {x.D}, true, &bias);
+    }
+};
+
+PyObject* selscan_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 19) { PyErr_SetString(PyExc_TypeError, "selscan_fwd takes nineteen arguments"); return nullptr; }
+    Rows x;
+    Scan s;
+    const float* pin;
+    float* pout;
+    void* py;
+    const int softplus = flag(a[11]), want_saved = flag(a[16]);
+    if (softplus < 0 || want_saved < 0 || !x.first(a[3], a[12], a[18]) || !s.read(x, a + 3, a + 8) ||
+        !x.slot_map(a[15], a[13] != Py_None ? a[13] : a[14]) || !x.dense(a[13], at::kFloat, {x.n_slots, s.N, x.D}, true, &pin) ||
+        !x.dense(a[14], at::kFloat, {x.n_slots, s.N, x.D}, true, &pout))
+        Py_RETURN_NONE;
+    const at::Tensor& U = THPVariable_Unpack(a[3]);
+    if (!x.dense(a[17], x.type, U.sizes(), true, &py)) Py_RETURN_NONE;
+    const auto f = address<selscan_fwd_fn>(x.function(a));
+    const auto bytes = address<selscan_saved_fn>(a[2]);
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor y, saved;
+    int rc;
+    {
+        const without_interpreter_lock free;
+        if (a[17] == Py_None) { y = at::empty(U.sizes(), like(U).memory_format(at::MemoryFormat::Contiguous)); py = y.data_ptr(); }
+        if (want_saved) {
+            const size_t need = bytes((int)x.T, (int)x.D, (int)s.N);
+            saved = at::empty({(int64_t)(need < 16 ? 16 : need) / 4}, like(U).dtype(at::kFloat));
+        }
+        rc = f(s.U, s.ldu, s.delta, s.ldd, s.A, s.Bm, s.ldb, s.Cm, s.ldc, s.D, s.Z, s.ldz, s.bias, softplus, x.cu, x.n_seq, (int)x.T, (int)x.D,
+               (int)s.N, (int)s.G, pin, pout, x.slots, x.n_slots, py, want_saved ? saved.data_ptr() : nullptr, stream_of(x.dev));
+    }
+    if (rc != 0) return PyLong_FromLong(rc);
+    PyObject* both = PyTuple_New(2);
+    if (both == nullptr) return nullptr;
+    PyObject *first = given_or(a[17], y), *second = want_saved ? THPVariable_Wrap(std::move(saved)) : none();
+    if (first == nullptr || second == nullptr) { Py_XDECREF(first); Py_XDECREF(second); Py_DECREF(both); return nullptr; }
+    PyTuple_SET_ITEM(both, 0, first);
+    PyTuple_SET_ITEM(both, 1, second);
+    return both;
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* selscan_step(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 15) { PyErr_SetString(PyExc_TypeError, "selscan_step takes fifteen arguments"); return nullptr; }
+    Rows x;
+    Scan s;
+    float* ps;
+    void* py;
+    const int softplus = flag(a[11]);
+    if (softplus < 0 || !x.first(a[2], Py_None, a[14]) || x.dims != 1 || !s.read(x, a + 2, a + 8)) Py_RETURN_NONE;
+    x.n_seq = x.n_slots = (int)x.T;
+    if (!x.slot_map(a[12], a[7]) || !x.dense(a[7], at::kFloat, {x.n_slots, s.N, x.D}, false, &ps) || !x.dense(a[13], x.type, {x.T, x.D}, true, &py))
+        Py_RETURN_NONE;
+    const at::Tensor& U = THPVariable_Unpack(a[2]);
+    const auto f = address<selscan_step_fn>(x.function(a));
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor y;
+    int rc;
+    {
+        const without_interpreter_lock free;
+        if (a[13] == Py_None) { y = at::empty({x.T, x.D}, like(U)); py = y.data_ptr(); }
+        rc = f(s.U, s.ldu, s.delta, s.ldd, s.A, s.Bm, s.ldb, s.Cm, s.ldc, s.D, s.Z, s.ldz, s.bias, softplus, ps, x.slots, x.n_slots, (int)x.T,
+               (int)x.D, (int)s.N, (int)s.G, py, stream_of(x.dev));
+    }
+    return rc != 0 ? PyLong_FromLong(rc) : given_or(a[13], y);
+    END_HANDLE_TH_ERRORS
+}
+
+// (with Y: in front of the first block the binding's own lines)
+PyObject* block_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 10) { PyErr_SetString(PyExc_TypeError, "block_norm_fwd takes ten arguments"); return nullptr; }
+    if (modes() || a[9] != Py_None || !PyFloat_CheckExact(a[7]) || !PyFloat_CheckExact(a[8]) || !on_gpu(a[2]) || !on_gpu(a[3])) Py_RETURN_NONE;
+    Rows x;
+    x.dev = c10::hip::current_device();
+    x.type = THPVariable_Unpack(a[2]).scalar_type();
+    const at::Tensor& X = THPVariable_Unpack(a[3]);
+    const at::ScalarType xt = X.scalar_type();
+    if ((x.type != at::kBFloat16 && x.type != at::kFloat) || (xt != x.type && xt != at::kFloat) || X.dim() < 1) Py_RETURN_NONE;
+    const int64_t D = X.size(-1);
+    if (D < 1 || D > 0x7fffffff) Py_RETURN_NONE;
+    const void *pY, *pX, *pg;
+    const float *pp, *pn;
+    if (!x.dense(a[2], x.type, X.sizes(), false, &pY) || !x.dense(a[3], xt, X.sizes(), false, &pX) || !x.dense(a[4], x.type, X.sizes(), true, &pg) ||
+        !x.dense(a[5], at::kFloat, {D}, true, &pp) || !x.dense(a[6], at::kFloat, {D}, true, &pn))
+        Py_RETURN_NONE;
+    const auto f = address<block_norm_fwd_fn>(a[x.type == at::kFloat ? 1 : 0]);
+    if (PyErr_Occurred()) return nullptr;
+    const float scale = (float)PyFloat_AS_DOUBLE(a[7]), eps = (float)PyFloat_AS_DOUBLE(a[8]);
+    at::Tensor out[2];
+    int rc;
+    {
+        const without_interpreter_lock free;
+        out[0] = at::empty(X.sizes(), like(X));
+        if (pn != nullptr || a[6] != Py_None) out[1] = at::empty(X.sizes(), like(X).dtype(x.type));
+        rc = f(pY, pg, pX, pp, pn, out[0].data_ptr(), out[1].defined() ? out[1].data_ptr() : nullptr, scale, eps, (long long)(X.numel() / D), (int)D,
+               xt != x.type, stream_of(x.dev));
+    }
+    return rc != 0 ? PyLong_FromLong(rc) : wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
 #define CHELA_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CHELA_METHOD(step), CHELA_METHOD(forward), CHELA_METHOD(backward), CHELA_METHOD(gated),
                          CHELA_METHOD(gate_norm_bwd), CHELA_METHOD(zbwd_saved), CHELA_METHOD(spectrum), CHELA_METHOD(conv_fwd),
-                         CHELA_METHOD(conv_bwd), {nullptr, nullptr, 0, nullptr}};
+                         CHELA_METHOD(conv_bwd), CHELA_METHOD(short_conv_fwd), CHELA_METHOD(short_conv_step), CHELA_METHOD(selscan_fwd),
+                         CHELA_METHOD(selscan_step), CHELA_METHOD(block_norm_fwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_chela_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
