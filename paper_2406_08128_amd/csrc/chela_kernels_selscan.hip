@@ -147,16 +147,6 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
     for (int n = 0; n < N; ++n) { A2[n] = a.A[(size_t)n * s.D + ch] * kLog2e; h[n] = 0.f; }
     const float bias = a.dbias ? a.dbias[ch] : 0.f, skip = a.Dskip ? a.Dskip[ch] : 0.f;
 
-    int q = seq_of(R, t0);                                   // the sequence the walk is in, and its rows
-    if (q < 0) q = 0;
-    int beg = q < R.n_seq ? seq_begin(R, q) : R.T, end = q < R.n_seq ? seq_end(R, q) : R.T;
-    if (MODE != SCAN_TOTALS && c > 0 && beg < t0 && q < R.n_seq) {
-        const float* H = a.totals + (size_t)c * ND + ch;
-#pragma unroll
-        for (int n = 0; n < N; ++n) h[n] = H[(size_t)n * s.D];
-    }
-
-    // (a row's address is the same in all lanes: scalar base, 32-bit lane offset)
     const bool gated = MODE == SCAN_OUT && a.Z != nullptr;
     const IO *Bm = (const IO*)a.Bm + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)g * N;
     const unsigned och = ch * sizeof(IO);
@@ -179,6 +169,17 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
         }
         if (MODE == SCAN_OUT || !maps.has_c(lane)) maps.load(Bm, Cm, a.ldb, a.ldc, t, R.T - 1, lane);
     };
+    load(t0);                                                // (on their way while the sequence is looked for)
+    int q = seq_of_wave(R, t0, lane);                        // the sequence the walk is in, and its rows
+    if (q < 0) q = 0;
+    int beg = q < R.n_seq ? seq_begin(R, q) : R.T, end = q < R.n_seq ? seq_end(R, q) : R.T;
+    if (MODE != SCAN_TOTALS && c > 0 && beg < t0 && q < R.n_seq) {
+        const float* H = a.totals + (size_t)c * ND + ch;
+#pragma unroll
+        for (int n = 0; n < N; ++n) h[n] = H[(size_t)n * s.D];
+    }
+
+    // (a row's address is the same in all lanes: scalar base, 32-bit lane offset)
     float sum = 0.f;
     bool began = false;
     auto row = [&](const float* bc, float dl, float u, float gate) {
@@ -193,7 +194,6 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
         if (MODE == SCAN_OUT) row_store(Y, och, from_f<IO>((y[0] + y[1]) * gate));
     };
 
-    load(t0);
     for (int t = t0; t < t1; t += GT) {
         float u[GT], dl[GT], gate[GT];
         float(*bc)[2 * N] = s_bc[(t / GT) & 1];
@@ -287,9 +287,6 @@ __global__ __launch_bounds__(64) void selscan_bwd_totals_kernel(ScanBwd a)
     const float bias = a.dbias ? a.dbias[ch] : 0.f;
     const bool gated = a.Z != nullptr;
     const IO *Bm = (const IO*)a.Bm + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)g * N;
-    int sq = seq_of(R, t1 - 1), beg = 0, end = 0;
-    if (sq >= R.n_seq) sq = R.n_seq - 1;
-    if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
     float sum = 0.f;
     bool ended = false;
     IO nd[GT], nz[GT], ny[GT];
@@ -312,12 +309,15 @@ __global__ __launch_bounds__(64) void selscan_bwd_totals_kernel(ScanBwd a)
         }
         if (maps.has_c(lane)) maps.load(Bm, Cm, a.ldb, a.ldc, t, R.T - 1, lane);
     };
+    load(last);
+    int sq = seq_of_wave(R, t1 - 1, lane), beg = 0, end = 0;
+    if (sq >= R.n_seq) sq = R.n_seq - 1;
+    if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
     auto row = [&](const float* bc, float dl, float dy) {
 #pragma unroll
         for (int n = 0; n < N; ++n) q[n] = exp2_(dl * A2[n]) * fmaf(bc[N + n], dy, q[n]);
         sum += dl;
     };
-    load(last);
     for (int t = last; t >= t0; t -= GT) {
         float dl[GT], dy[GT];
         float(*bc)[2 * N] = s_bc[(t / GT) & 1];
@@ -433,16 +433,6 @@ __global__ __launch_bounds__(N / NPW * 64, 3) void selscan_bwd_kernel(ScanBwd a)
     const IO *U = (const IO*)a.U, *De = (const IO*)a.delta, *dY = (const IO*)a.dY, *Z = (const IO*)a.Z;
     IO *dU = (IO*)a.dU, *dDe = (IO*)a.ddelta, *dZ = (IO*)a.dZ;
 
-    int sq = seq_of(R, t1 - 1), beg = 0, end = 0;
-    const bool inside = sq >= 0 && sq < R.n_seq;
-    if (sq >= R.n_seq) sq = R.n_seq - 1;
-    if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
-    if (inside && end > t1) {                     // the sequence goes on in the chunks behind
-        const float* Q = a.totals + (size_t)c * ND + mine;
-#pragma unroll
-        for (int n = 0; n < NPW; ++n) q[n] = Q[(size_t)n * s.D];
-    }
-
     // a thread's share of the tile's TB * 2N map values
     constexpr int MV = TB * 2 * N / (W * 64);
     const int mt = threadIdx.x * MV / (2 * N), mk = threadIdx.x * MV % (2 * N);
@@ -473,6 +463,16 @@ __global__ __launch_bounds__(N / NPW * 64, 3) void selscan_bwd_kernel(ScanBwd a)
     const int at = ((lane >> 3) & 1) * N + w * NPW + ((lane >> 2) & 1) * 2 + ((lane >> 1) & 1);
     const int last = t0 + (t1 - 1 - t0) / TB * TB;
     load(last);
+    int sq = seq_of_wave(R, t1 - 1, lane), beg = 0, end = 0;
+    const bool inside = sq >= 0 && sq < R.n_seq;
+    if (sq >= R.n_seq) sq = R.n_seq - 1;
+    if (sq >= 0) { beg = seq_begin(R, sq); end = seq_end(R, sq); }
+    if (inside && end > t1) {                     // the sequence goes on in the chunks behind
+        const float* Q = a.totals + (size_t)c * ND + mine;
+#pragma unroll
+        for (int n = 0; n < NPW; ++n) q[n] = Q[(size_t)n * s.D];
+    }
+
     for (int t = last; t >= t0; t -= TB) {
         // of a row that the thread looks after: u, the step size's slope, dout silu(z), dout silu'(z)
         float u[PER], slope[PER], dy[PER], dz[PER], h0[NPW], tA[NPW];
@@ -688,30 +688,41 @@ __global__ __launch_bounds__(1024) void selscan_params_kernel(const float* __res
 }
 
 // ------------------------------------------------------------------------------------------------------------ single tokens
+// A wave has 64 channels of `each` requests: what a channel has once (16 decays, 4 KB a wave, as many bytes as its state) is read once.
 template <typename IO, int N>
-__global__ __launch_bounds__(64) void selscan_step_kernel(SelscanArgs a)
+__global__ __launch_bounds__(64) void selscan_step_kernel(SelscanArgs a, int each)
 {
-    const int nb = (a.D + 63) / 64, r = blockIdx.x / nb, Dg = a.D / a.G, ch = blockIdx.x % nb * 64 + threadIdx.x;
-    const int slot = slot_of(a.rows, r);
-    if (slot < 0 || ch >= a.D) return;
+    const int nb = (a.D + 63) / 64, Dg = a.D / a.G, ch = blockIdx.x % nb * 64 + threadIdx.x;
+    const int r0 = blockIdx.x / nb * each, r1 = min(r0 + each, a.rows.T);
+    if (ch >= a.D) return;
     const int g = ch / Dg;
-    float* S = a.S_out + (size_t)slot * N * a.D + ch;
-    const IO *Bm = (const IO*)a.Bm + (size_t)r * a.ldb + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)r * a.ldc + (size_t)g * N;
-    const float u = to_f(((const IO*)a.U)[(size_t)r * a.ldu + ch]);
-    float dl = to_f(((const IO*)a.delta)[(size_t)r * a.ldd + ch]) + (a.delta_bias ? a.delta_bias[ch] : 0.f);
-    if (a.softplus) dl = softplus_(dl);
-    float y = a.Dskip ? a.Dskip[ch] * u : 0.f;
+    const size_t ND = (size_t)N * a.D;
+    float A2[N];
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const float h = fmaf(exp2_(dl * kLog2e * a.A[(size_t)n * a.D + ch]), S[(size_t)n * a.D], dl * u * to_f(Bm[n]));
-        S[(size_t)n * a.D] = h;
-        y = fmaf(to_f(Cm[n]), h, y);
+    for (int n = 0; n < N; ++n) A2[n] = a.A[(size_t)n * a.D + ch] * kLog2e;
+    const float bias = a.delta_bias ? a.delta_bias[ch] : 0.f, skip = a.Dskip ? a.Dskip[ch] : 0.f;
+    for (int r = r0; r < r1; ++r) {
+        const int slot = slot_of(a.rows, r);
+        if (slot < 0) continue;
+        float* S = a.S_out + (size_t)slot * ND + ch;
+        const IO *Bm = (const IO*)a.Bm + (size_t)r * a.ldb + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)r * a.ldc + (size_t)g * N;
+        float h[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) h[n] = S[(size_t)n * a.D];
+        const float u = to_f(((const IO*)a.U)[(size_t)r * a.ldu + ch]);
+        const float z = a.Z ? to_f(((const IO*)a.Z)[(size_t)r * a.ldz + ch]) : 0.f;
+        float dl = to_f(((const IO*)a.delta)[(size_t)r * a.ldd + ch]) + bias;
+        if (a.softplus) dl = softplus_(dl);
+        float y = skip * u;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            h[n] = fmaf(exp2_(dl * A2[n]), h[n], dl * u * to_f(Bm[n]));
+            S[(size_t)n * a.D] = h[n];
+            y = fmaf(to_f(Cm[n]), h[n], y);
+        }
+        if (a.Z) y *= z * sigmoid_(z);
+        ((IO*)a.Y)[(size_t)r * a.D + ch] = from_f<IO>(y);
     }
-    if (a.Z) {
-        const float z = to_f(((const IO*)a.Z)[(size_t)r * a.ldz + ch]);
-        y *= z * sigmoid_(z);
-    }
-    ((IO*)a.Y)[(size_t)r * a.D + ch] = from_f<IO>(y);
 }
 
 // -------------------------------------------------------------------------------------------------------------------- host
@@ -903,7 +914,10 @@ template <typename IO, int N>
 static hipError_t step(const SelscanArgs& a, hipStream_t st)
 {
     ProfScope prof(KID_SELSCAN_STEP, st);
-    hipLaunchKernelGGL((selscan_step_kernel<IO, N>), dim3((unsigned)((a.D + 63) / 64) * (unsigned)a.rows.T), dim3(64), 0, st, a);
+    const long nb = (a.D + 63) / 64, R = a.rows.T;
+    // (256 requests, 1536 channels, for 1, 2, 4, 8 a wave: 8.7, 8.3, 9.2, 11.2 us; below four waves per SIMD one)
+    const int each = nb * R >= 4096 ? 2 : 1;
+    hipLaunchKernelGGL((selscan_step_kernel<IO, N>), dim3((unsigned)(nb * ((R + each - 1) / each))), dim3(64), 0, st, a, each);
     return hipGetLastError();
 }
 hipError_t launch_selscan_step(const SelscanArgs& a, int dtype, hipStream_t st) { CHELA_SCAN(step, a, st) }
