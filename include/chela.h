@@ -66,8 +66,8 @@ extern "C" {
 enum {
     CHELA_OK                  = 0,
     CHELA_ERR_NULL_POINTER    = -1, /* a tensor pointer is NULL while B*H*N > 0            */
-    CHELA_ERR_BAD_SHAPE       = -2, /* B, H or N negative, or element count overflows      */
-    CHELA_ERR_UNSUPPORTED_DIM = -3, /* dk or dv not in {64, 128}                           */
+    CHELA_ERR_BAD_SHAPE       = -2, /* B, H or N negative, element count overflows, sizes that do not go together */
+    CHELA_ERR_UNSUPPORTED_DIM = -3, /* dk or dv not in {64, 128}; selective scan: N not in {8, 16, 32}; block norm: D above 8192 */
     CHELA_ERR_BAD_CHUNK       = -4, /* chunk not in the supported set for this dtype       */
     CHELA_ERR_MISALIGNED      = -5, /* a tensor pointer is not 16-byte aligned             */
     CHELA_ERR_ALIASING        = -6, /* an output range overlaps an input or another output */
@@ -321,7 +321,7 @@ int chela_linattn_step_gated(const void *q, const void *k, const void *v, const 
  *              begins with nothing and leaves nothing, and in the single-token calls its output row is left as it is.  Two
  *              sequences of one call must not share a slot (their states would be unspecified).  S_out may be S_in (exactly
  *              the same pointer); states of slots that no sequence has are not touched.  An empty sequence hands its state on.
- * Limits: T < 2^31 - 4096; n_seq, R < 2^24; D <= 2^20; T D, n_seq D and R D below 2^37.  With T = 0 nothing is done but
+ * Limits: D <= 2^20; T ceil(D / 64) < 2^28; n_seq ceil(D / 64) and R ceil(D / 64) < 2^23.  With T = 0 nothing is done but
  * that states pass through and gradients of parameters are zeroed.  Everything else (streams, scratch, threads, errors) as for the
  * calls above; scratch: the _workspace_bytes queries (0 for invalid arguments).
  *

@@ -1313,11 +1313,15 @@ struct Operands {
     }
 };
 
-constexpr int kMaxRows = 0x7fffffff - 4096;       // (the kernels count some rows beyond the last)
+// Rows times 64 channels of them: the launches' threads have to stay below 2^32, of which the convolution's may take 8 a unit (256 for a
+// state), and a state's or a request's is 64 at least.
+static bool too_many(int rows, int D, long long units) { return (long long)rows * ((D + 63) / 64) >= units; }
+constexpr long long kRowUnits = 1ll << 28, kStateUnits = 1ll << 23;
 // The sequences that T rows belong to, as a call names them.
 static int rows_of(const int* cu, int n_seq, int T, int D, const int* slots, int n_slots, Rows* out)
 {
-    if (T < 0 || n_seq < 0 || n_seq >= (1 << 24) || D < 0 || D > (1 << 20) || n_slots < 0 || T > kMaxRows) return CHELA_ERR_BAD_SHAPE;
+    if (T < 0 || n_seq < 0 || D < 0 || D > (1 << 20) || n_slots < 0 || T >= kRowUnits || n_seq >= kStateUnits) return CHELA_ERR_BAD_SHAPE;
+    if (too_many(T, D, kRowUnits) || too_many(n_seq, D, kStateUnits)) return CHELA_ERR_BAD_SHAPE;
     if (cu == nullptr && T > 0 && (n_seq == 0 || T % n_seq != 0)) return CHELA_ERR_BAD_SHAPE;
     if (slots == nullptr && n_slots != n_seq) return CHELA_ERR_BAD_SHAPE;
     if (((uintptr_t)cu | (uintptr_t)slots) & 3u) return CHELA_ERR_MISALIGNED;
@@ -1327,8 +1331,6 @@ static int rows_of(const int* cu, int n_seq, int T, int D, const int* slots, int
 static int status_of(hipError_t e) { return e == hipSuccess ? CHELA_OK : CHELA_ERR_HIP; }
 static size_t esize(int dtype) { return dtype == CHELA_DTYPE_BF16 ? 2 : 4; }
 static int kind(int dtype) { return dtype == CHELA_DTYPE_BF16 ? 0 : 1; }
-// workgroups of a kernel with one per row and 64 channels stay below 2^31
-static bool too_many(int rows, int D) { return (unsigned long long)rows * (((unsigned long long)D + 63) / 64) > 0x7fffffffull; }
 
 static int short_conv_common(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,
                              int T, int D, const void* S_in, void* S_out, const int* slots, int n_slots, void* Y, int dtype, void* stream)
@@ -1337,7 +1339,6 @@ static int short_conv_common(const void* X, long long ldx, const float* w, int m
     if (m < 1 || m > kShortConvMaxTaps) return CHELA_ERR_BAD_SHAPE;
     int rc = rows_of(cu, n_seq, T, D, slots, n_slots, &a.rows);
     if (rc != CHELA_OK) return rc;
-    if (too_many(T, D) || too_many(n_seq, D)) return CHELA_ERR_BAD_SHAPE;
     if (D == 0 || (T == 0 && n_seq == 0)) return CHELA_OK;
     if (m == 1) S_in = S_out = nullptr;
     const size_t es = esize(dtype), st = (size_t)n_slots * (m - 1) * D * es;
@@ -1369,8 +1370,9 @@ int chela_short_conv_fwd_f32(const void* X, long long ldx, const float* w, int m
 
 size_t chela_short_conv_bwd_workspace_bytes(int T, int D, int m, int dtype)
 {
-    if (T < 0 || D <= 0 || D > (1 << 20) || m < 1 || m > kShortConvMaxTaps || (dtype != CHELA_DTYPE_BF16 && dtype != CHELA_DTYPE_F32)) return 0;
-    return (size_t)short_conv_bwd_parts(T, D, kind(dtype)) * (m + 1) * D * sizeof(float);
+    if (T < 0 || D <= 0 || D > (1 << 20) || too_many(T, D, kRowUnits) || m < 1 || m > kShortConvMaxTaps ||
+        (dtype != CHELA_DTYPE_BF16 && dtype != CHELA_DTYPE_F32)) return 0;
+    return (size_t)short_conv_bwd_parts(T) * (m + 1) * D * sizeof(float);
 }
 
 static int short_conv_bwd_common(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,
@@ -1381,7 +1383,6 @@ static int short_conv_bwd_common(const void* X, long long ldx, const float* w, i
     if (m < 1 || m > kShortConvMaxTaps) return CHELA_ERR_BAD_SHAPE;
     int rc = rows_of(cu, n_seq, T, D, nullptr, n_seq, &a.rows);
     if (rc != CHELA_OK) return rc;
-    if (too_many(T, D)) return CHELA_ERR_BAD_SHAPE;
     if (D == 0) return CHELA_OK;
     if (m == 1) { S_in = dS_out = nullptr; dS_in = nullptr; }
     const size_t es = esize(dtype), st = (size_t)n_seq * (m - 1) * D * es, rows = (size_t)T * D * es;
@@ -1426,10 +1427,9 @@ static int short_conv_step_common(const void* x, long long ldx, const float* w, 
                                   const int* slots, int n_slots, int R, int D, void* y, int dtype, void* stream)
 {
     ShortConvArgs a{};
-    if (m < 1 || m > kShortConvMaxTaps || R < 0 || R >= (1 << 24)) return CHELA_ERR_BAD_SHAPE;
+    if (m < 1 || m > kShortConvMaxTaps || R < 0) return CHELA_ERR_BAD_SHAPE;
     int rc = rows_of(nullptr, R, R, D, slots, n_slots, &a.rows);
     if (rc != CHELA_OK) return rc;
-    if (too_many(R, D)) return CHELA_ERR_BAD_SHAPE;
     if (R == 0 || D == 0) return CHELA_OK;
     const size_t es = esize(dtype);
     Operands o;
@@ -1460,13 +1460,13 @@ static bool selscan_dims(int D, int N, int G) { return selscan_states_ok(N) && G
 
 size_t chela_selscan_saved_bytes(int T, int D, int N)
 {
-    if (T <= 0 || D <= 0 || D > (1 << 20) || !selscan_states_ok(N)) return 0;
+    if (T <= 0 || D <= 0 || D > (1 << 20) || too_many(T, D, kRowUnits) || !selscan_states_ok(N)) return 0;
     return ((size_t)T + kSelscanTile - 1) / kSelscanTile * N * D * sizeof(float);
 }
 
 size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int has_saved)
 {
-    if (T <= 0 || D <= 0 || D > (1 << 20) || !selscan_dims(D, N, G)) return 0;
+    if (T <= 0 || D <= 0 || D > (1 << 20) || too_many(T, D, kRowUnits) || !selscan_dims(D, N, G)) return 0;
     return make_selscan_plan(T, D, N, G, is_bwd != 0, has_saved != 0).bytes;
 }
 
@@ -1559,10 +1559,9 @@ static int selscan_step_common(const SelscanIn& x, float* S, const int* slots, i
 {
     SelscanArgs a{};
     if (!selscan_states_ok(x.N)) return CHELA_ERR_UNSUPPORTED_DIM;
-    if (!selscan_dims(x.D, x.N, x.G) || R < 0 || R >= (1 << 24)) return CHELA_ERR_BAD_SHAPE;
+    if (!selscan_dims(x.D, x.N, x.G) || R < 0) return CHELA_ERR_BAD_SHAPE;
     int rc = rows_of(nullptr, R, R, x.D, slots, n_slots, &a.rows);
     if (rc != CHELA_OK) return rc;
-    if (too_many(R, x.D)) return CHELA_ERR_BAD_SHAPE;
     if (R == 0 || x.D == 0) return CHELA_OK;
     const size_t es = esize(dtype);
     Operands o;
@@ -1753,8 +1752,8 @@ const char* chela_status_string(int status)
     switch (status) {
         case CHELA_OK: return "CHELA_OK";
         case CHELA_ERR_NULL_POINTER: return "CHELA_ERR_NULL_POINTER: a tensor pointer is NULL";
-        case CHELA_ERR_BAD_SHAPE: return "CHELA_ERR_BAD_SHAPE: negative or overflowing B, H or N";
-        case CHELA_ERR_UNSUPPORTED_DIM: return "CHELA_ERR_UNSUPPORTED_DIM: dk and dv must be 64 or 128";
+        case CHELA_ERR_BAD_SHAPE: return "CHELA_ERR_BAD_SHAPE: negative or overflowing B, H or N, or sizes that do not go together";
+        case CHELA_ERR_UNSUPPORTED_DIM: return "CHELA_ERR_UNSUPPORTED_DIM: dk and dv must be 64 or 128; a selective scan's N 8, 16 or 32, a block norm's D at most 8192";
         case CHELA_ERR_BAD_CHUNK: return "CHELA_ERR_BAD_CHUNK: chunk must be 64/128 (bf16) or 16/32/64 (fp32)";
         case CHELA_ERR_MISALIGNED: return "CHELA_ERR_MISALIGNED: pointer not sufficiently aligned";
         case CHELA_ERR_ALIASING: return "CHELA_ERR_ALIASING: an output overlaps an input or another output";

@@ -474,9 +474,8 @@ hipError_t launch_short_conv_fwd(const ShortConvArgs& a, int dtype, hipStream_t 
     return hipGetLastError();
 }
 
-int short_conv_bwd_parts(int T, int D, int dtype)
+int short_conv_bwd_parts(int T)
 {
-    (void)D; (void)dtype;
     const int runs = (T + kBwdRun - 1) / kBwdRun;
     return runs < kBwdParts ? (runs > 0 ? runs : 1) : kBwdParts;
 }
@@ -486,7 +485,7 @@ hipError_t launch_short_conv_bwd(const ShortConvArgs& a, int dtype, hipStream_t 
     ProfScope prof(KID_SHORT_CONV, st);
     const int V = pairs(a, dtype) ? 2 : 1, vectors = (a.D + V - 1) / V;
     const unsigned threads = threads_for(vectors);
-    const int runs = (a.rows.T + kBwdRun - 1) / kBwdRun, parts = short_conv_bwd_parts(a.rows.T, a.D, dtype);
+    const int runs = (a.rows.T + kBwdRun - 1) / kBwdRun, parts = short_conv_bwd_parts(a.rows.T);
     const dim3 grid((vectors + threads - 1) / threads, parts);
 #define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_bwd_kernel<IO, V, M, kBwdRun>), grid, dim3(threads), 0, st, a, runs)
     CHELA_TYPES(CHELA_F)

@@ -146,6 +146,9 @@ def test_short_conv_refusals(L, sfx):
     assert f(n_slots=3) == SHAPE                              # three states for two sequences, and no map
     assert f(ldx=63) == SHAPE and f(ldx=1 << 40) == SHAPE
     assert f(T=2 ** 31 - 2) == SHAPE and f(T=2 ** 30, D=2 ** 20, ldx=2 ** 20) == SHAPE
+    # threads of a launch stay below 2^32: rows, sequences, requests times 64 channels of them
+    assert f(T=2 ** 28) == SHAPE and f(T=2 ** 24, D=1024, ldx=1024) == SHAPE and f(n_seq=2 ** 23, T=2 ** 23, n_slots=2 ** 23) == SHAPE
+    assert f(n_seq=2 ** 20, T=2 ** 20, D=512, ldx=512, n_slots=2 ** 20) == SHAPE
     assert f(X=at(0) + 1) == ALIGN and f(Y=at(5) + 8) == ALIGN and f(w=at(1) + 4) == ALIGN and f(S_in=at(3) + 2) == ALIGN
     assert f(cu=at(6) + 2) == ALIGN and f(slots=at(6) + 1) == ALIGN
     assert f(Y=at(0)) == ALIAS and f(Y=at(3)) == ALIAS and f(S_out=at(5)) == ALIAS and f(S_out=at(3) + 16) == ALIAS and f(Y=at(1)) == ALIAS
@@ -245,6 +248,8 @@ def test_workspace_and_saved_queries(L):
         assert L.chela_selscan_workspace_bytes(*bad) == 0, bad
     a, b = L.chela_selscan_workspace_bytes(4096, 512, 16, 1, 1, 1), L.chela_selscan_workspace_bytes(4096, 512, 16, 1, 1, 0)
     assert 0 < L.chela_selscan_workspace_bytes(4096, 512, 16, 1, 0, 0) < a < b      # the states in front of the tiles come on top
+    assert L.chela_selscan_workspace_bytes(2 ** 28, 64, 16, 1, 0, 0) == 0 and L.chela_selscan_saved_bytes(2 ** 24, 1024, 16) == 0
+    assert L.chela_short_conv_bwd_workspace_bytes(2 ** 28, 64, 4, 0) == 0
     assert L.chela_short_conv_bwd_workspace_bytes(64, 512, 4, 0) > 0 and L.chela_short_conv_bwd_workspace_bytes(64, 512, 9, 0) == 0
     assert L.chela_block_norm_bwd_workspace_bytes(10, 64) > 0 and L.chela_block_norm_bwd_workspace_bytes(10, 8193) == 0
 
