@@ -95,7 +95,8 @@ __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restr
             // (what is worked out for places behind the last chunk goes nowhere; were it left out, the loads would wait in turn)
             const int c = BWD ? n_chunk - 1 - (k + j) : k + j;
             if (k + j < n_chunk) totals[(size_t)c * ND + i] = h;
-            h = sd[j] != sd[j] ? H[j] : fmaf(exp2_(sd[j] * A2), h, H[j]);
+            // (a state of zero stays so however much growth has come together)
+            h = sd[j] != sd[j] || h == 0.f ? H[j] : fmaf(exp2_(sd[j] * A2), h, H[j]);
         }
     }
 }

@@ -338,6 +338,48 @@ def test_slots_and_rows_of_nobody(dtype):
             assert torch.equal(pool[k], before[k]) and torch.equal(conv_pool[k], cbefore[k])
 
 
+@pytest.mark.parametrize("n", [70, 300, 5000])
+def test_many_sequences(n):
+    # more of them than lanes, than 64 lanes' steps; short ones, many without rows, at the ends too
+    r, rng, D, N, m = gen(53), np.random.default_rng(n), 24, 8, 4
+    lens = rng.integers(0, 5, n) * rng.integers(0, 2, n)
+    lens[:3] = lens[-2:] = 0
+    first = 2
+    T, o = int(lens.sum()) + first + 3, offsets(lens, first)
+    cu = cu_of(lens, first)
+    u, delta, z, Bm, Cm, A, skip, bias = scan_inputs(r, T, D, N, 1, F32)
+    dY, w, S, dS = r(T, D), r(D, m), r(n, N, D), r(n, N, D)
+    C, dC = r(n, m - 1, D), r(n, m - 1, D)
+    kw = dict(D=skip, Z=z, delta_bias=bias, cu=cu)
+    S_out, C_out = torch.full_like(S, float("nan")), torch.full_like(C, float("nan"))
+    Y, saved = binding.chela_selscan_fwd(u, delta, A, Bm, Cm, S_in=S, S_out=S_out, want_saved=True, **kw)
+    S2 = S.clone()
+    Y2, _ = binding.chela_selscan_fwd(u, delta, A, Bm, Cm, S_in=S2, S_out=S2, **kw)
+    owned = slice(int(o[0]), int(o[-1]))
+    assert torch.equal(Y[owned], Y2[owned]) and torch.equal(S_out, S2)
+    g = binding.chela_selscan_bwd(u, delta, A, Bm, Cm, dY, S_in=S, dS_out=dS, want_dS_in=True, saved=saved, **kw)
+    y = binding.chela_short_conv_fwd(u, w, cu=cu, S_in=C, S_out=C_out)
+    h = binding.chela_short_conv_bwd(u, w, dY, cu=cu, S_in=C, dS_out=dC, want_dS_in=True)
+    n64 = [f64(t) for t in (u, delta, z, Bm, Cm, A, skip, bias)]
+    ref = scan_reference((*n64, True), f64(S), f64(dY), f64(dS), lens, first)
+    cref = conv_reference(n64[0], f64(w), None, True, f64(C), f64(dY), f64(dC), lens, first)
+    k = 8 * 4 + 128
+    cat = lambda parts, rows: np.concatenate(parts) if rows else np.stack(parts)  # noqa: E731
+    for name, got, rows in (("Y", Y[owned], True), ("S_out", S_out, False)):
+        check(name, got, cat([p[0][0][name] for p in ref], rows), cat([p[0][1][name] for p in ref], rows), k)
+    got = dict(zip(("dU", "ddelta", "dA", "dB", "dC", "dD", "dZ", "dbias", "dS_in"), g))
+    for name in ("dU", "ddelta", "dB", "dC", "dZ"):
+        check(name, got[name][owned], cat([p[1][0][name] for p in ref], True), cat([p[1][1][name] for p in ref], True), 2 * k + D)
+    check("dS_in", got["dS_in"], cat([p[1][0]["dS_in"] for p in ref], False), cat([p[1][1]["dS_in"] for p in ref], False), 2 * k)
+    for name in ("dA", "dD", "dbias"):
+        check(name, got[name], sum(p[1][0][name] for p in ref), sum(p[1][1][name] for p in ref), 2 * k + T)
+    check("y", y[owned], cat([p[0] for p in cref], True), cat([p[1] for p in cref], True), 64)
+    assert np.array_equal(f64(C_out), cat([p[2] for p in cref], False))
+    check("dX", h[0][owned], cat([p[3]["dX"] for p in cref], True), cat([p[4]["dX"] for p in cref], True), 64)
+    check("conv dS_in", h[3], cat([p[3]["dS_in"] for p in cref], False), cat([p[4]["dS_in"] for p in cref], False), 64)
+    check("dw", h[1], sum(p[3]["dw"] for p in cref), sum(p[4]["dw"] for p in cref), T + 64)
+
+
 def test_no_rows():
     D, N, m = 64, 16, 4
     S, C = torch.randn(2, N, D, device="cuda"), torch.randn(2, m - 1, D, device="cuda")
@@ -401,6 +443,25 @@ def test_selscan_extreme_steps_and_decays():
     check("Y", Y, f["Y"], mf["Y"], k)
     for i, name in enumerate(("dU", "ddelta", "dA", "dB", "dC")):
         check(name, g[i], v[name], mv[name], 2 * k)
+
+
+def test_selscan_growth_over_rows_that_bring_nothing():
+    # states of zero under a growth that no float holds over a chunk of rows, in front of the first input and behind the last gradient
+    r, D, N, L = gen(59), 64, 8, 600
+    u, delta, z, Bm, Cm, A, skip, bias = scan_inputs(r, L, D, N, 1, F32)
+    A = torch.linspace(0.25, 2.0, N, device="cuda")[:, None].expand(N, D).contiguous()
+    u[:590] = 0
+    delta[:] = 0.5413                                                   # steps of 1: up to e^2 a row, e^96 over 48 rows
+    Y, _ = binding.chela_selscan_fwd(u, delta, A, Bm, Cm)
+    f, mf = R.selscan_fwd(*[f64(t) for t in (u, delta, A, Bm, Cm)])
+    assert (Y[:590] == 0).all()
+    check("Y", Y, f["Y"], mf["Y"], 8 * 10 + 128)
+    u, dY = r(L, D), r(L, D)
+    dY[10:] = 0
+    g = binding.chela_selscan_bwd(u[:40], delta[:40], A, Bm[:40], Cm[:40], dY[:40])
+    far = binding.chela_selscan_bwd(u, delta, A, Bm, Cm, dY)
+    for k in (0, 3):                                                    # (what reaches back from the first ten rows)
+        assert torch.equal(far[k][:10], g[k][:10]) and (far[k][10:] == 0).all(), k
 
 
 # ------------------------------------------------------------------------------------------- norms around a block
@@ -579,6 +640,118 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for p, q in zip(out, want):
             assert torch.equal(p, q), k
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 33])
+def test_the_compiled_host_path_and_the_binding_do_the_same(dtype, D):
+    # (with a stream named, a call goes through the binding's own lines)
+    r, m, N, n, L = gen(61 + D), 4, 8, 3, 50
+    here = torch.cuda.current_stream()
+    u, delta, z, Bm, Cm, A, skip, bias = scan_inputs(r, n * L, D, N, 1, dtype)
+    w, cu = r(D, m), cu_of([20, 0, 100, 25])
+    slots, slots4 = torch.tensor([4, 0, -1], dtype=torch.int32, device="cuda"), torch.tensor([1, 3, 2, 0], dtype=torch.int32, device="cuda")
+    conv, pool = r(5, m - 1, D).to(dtype), r(5, N, D)
+    b3 = lambda t: t.view(n, L, t.shape[-1])  # noqa: E731
+    wide = wide_rows(u)
+
+    def both(f, *args, states=(), **kw):
+        out = []
+        for s in (None, here):
+            own = {k: v.clone() for k, v in states}
+            kw = {k: v.clone() if k in ("Y", "y") else v for k, v in kw.items()}
+            if "S_in" in own:
+                own["S_out"] = own["S_in"]
+            y = f(*args, stream=s, **own, **kw)
+            out.append([t for t in (y if isinstance(y, tuple) else (y,)) if t is not None] + list(own.values()))
+        bits = lambda t: t.contiguous().view(torch.int16 if t.dtype == BF else torch.int32)  # noqa: E731  (of what is no number, too)
+        for a, b in zip(*out):
+            assert a.shape == b.shape and a.dtype == b.dtype and torch.equal(bits(a), bits(b))
+
+    for x, kw in ((u, {}), (b3(u), {}), (wide, {}), (u, dict(cu=cu, silu=False)), (b3(u), dict(bias=bias, Y=torch.empty_like(b3(u))))):
+        both(binding.chela_short_conv_fwd, x, w, **kw)
+    both(binding.chela_short_conv_fwd, b3(u), w, states=[("S_in", conv)], slots=slots)
+    both(binding.chela_short_conv_fwd, u, w, cu=cu, states=[("S_in", conv)], slots=slots4)
+    both(binding.chela_short_conv_step, u[:3], w, states=[("S", conv)], slots=slots, bias=bias, y=torch.zeros_like(u[:3]))
+    both(binding.chela_short_conv_step, wide[:5], w, states=[("S", conv)], silu=False)
+    full = dict(D=skip, delta_bias=bias)
+    both(binding.chela_selscan_fwd, u, delta, A, Bm, Cm, cu=cu, **full, Z=z, states=[("S_in", pool)], slots=slots4,
+         Y=torch.zeros_like(u))
+    both(binding.chela_selscan_fwd, b3(u), b3(delta), A, b3(Bm.flatten(1)), b3(Cm.flatten(1)), want_saved=False, softplus=False)
+    both(binding.chela_selscan_fwd, wide, delta, A, Bm, Cm, cu=cu)
+    both(binding.chela_selscan_step, u[:3], delta[:3], A, Bm[:3], Cm[:3], states=[("S", pool)], z=z[:3], slots=slots, y=torch.zeros_like(u[:3]), **full)
+    both(binding.chela_selscan_step, wide[:5], delta[:5], A, Bm[:5], Cm[:5], states=[("S", pool)])
+    g1 = 1 + 0.1 * r(D)
+    for kw in (dict(w_pre=g1), dict(gate=z, w_post=g1, w_pre=g1, scale=0.5), dict(w_post=g1)):
+        both(binding.chela_block_norm_fwd, u, delta, **kw)
+    both(binding.chela_block_norm_fwd, None, b3(u), w_pre=g1)
+    x1, x2 = u.clone(), u.clone()
+    n1, n2 = torch.empty_like(u), torch.empty_like(u)
+    a = binding.chela_block_norm_fwd(delta, x1, w_pre=g1, X_out=x1, Nrm=n1)
+    b = binding.chela_block_norm_fwd(delta, x2, w_pre=g1, X_out=x2, Nrm=n2, stream=here)
+    assert a[0] is x1 and a[1] is n1 and torch.equal(x1, x2) and torch.equal(n1, n2) and not torch.equal(x1, u)
+    for bad in (dict(w=w.double()), dict(w=w[1:].contiguous()), dict(bias=bias[1:]), dict(S_in=conv), dict(cu=cu.long()), dict(Y=u[1:])):
+        for s in (None, here):
+            with pytest.raises(ValueError):
+                binding.chela_short_conv_fwd(u, **dict(dict(w=w, stream=s), **bad))
+
+
+def test_two_graphs_with_the_library_s_own_scratch():
+    runs = [_training_pass(256, 16, 4, 500, BF, 67), _training_pass(192, 8, 3, 700, F32, 71)]
+    s, graphs, outs = torch.cuda.Stream(), [], []
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for run, _ in runs:
+            run()                                          # (what the stream's scratch has to hold, before anything is captured)
+    torch.cuda.current_stream().wait_stream(s)
+    for run, _ in runs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append(run())
+        graphs.append(g)
+    other = gen(73)
+    for k in range(3):
+        for _, inputs in runs:
+            for t in inputs:
+                t.copy_(other(*t.shape).to(t.dtype))
+        want = [run() for run, _ in runs]
+        for out in outs:
+            for t in out:
+                t.fill_(float("nan"))
+        for g in graphs[::-1] if k % 2 else graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for out, w in zip(outs, want):
+            for p, q in zip(out, w):
+                assert torch.equal(p, q), k
+
+
+def test_two_threads_with_streams_of_their_own():
+    import threading
+    made = [_training_pass(256, 16, 4, 500, BF, 79), _training_pass(192, 8, 3, 700, F32, 83)]
+    want = [run() for run, _ in made]
+    torch.cuda.synchronize()
+    got, wrong = [None, None], []
+
+    def work(i):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                for _ in range(5):
+                    got[i] = made[i][0]()
+            s.synchronize()
+        except Exception as e:                             # (a thread's own would be lost)
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+    for a, b in zip(got, want):
+        for p, q in zip(a, b):
+            assert torch.equal(p, q)
 
 
 def test_offsets_beyond_32_bits():
