@@ -65,7 +65,11 @@ __global__ __launch_bounds__(256) void selscan_finish_kernel(ScanShape s, const 
 // The chunks' totals turned into what each chunk begins with, in place, in order (forward: from the first chunk on, state and decay; backward:
 // from the last chunk on).  A chunk whose sum of step sizes is the mark has a sequence's beginning (end) in it: what comes to it ends there.
 // (A sum that is not a number by itself comes with totals that are none.)  Workgroups from `groups` on: pass_states_on().
+// Latency-bound: four waves share the chunks of 64 elements, each makes one step of its 32, takes in what is in front of them from the
+// others, and goes over them again, all from registers.
 __device__ __forceinline__ float reset_mark() { return __uint_as_float(0x7fc00000u); }
+// (a state of zero stays so however much growth has come together)
+__device__ __forceinline__ float carried(float h, float sum, float A2, float H) { return sum != sum || h == 0.f ? H : fmaf(exp2_(sum * A2), h, H); }
 template <bool BWD>
 __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restrict__ A, float* __restrict__ totals,
                                                            const float* __restrict__ sums, int n_chunk, int D, long ND, int groups, Rows rows,
@@ -75,29 +79,45 @@ __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restr
         pass_states_on(rows, from, to, ND, blockIdx.x - groups, gridDim.x - groups);
         return;
     }
-    const long i = (long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= ND) return;
+    __shared__ float s_h[4][64], s_sum[4][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const bool live = (long)blockIdx.x * 64 + lane < ND;
+    const long i = live ? (long)blockIdx.x * 64 + lane : ND - 1;
     const int ch = (int)(i % D);
     const float A2 = A[i] * kLog2e;
-    float h = 0.f;
+    float base = 0.f;                                // what comes to the 4 * AT chunks
     constexpr int AT = 32;                           // chunks whose totals are read together
     // (the chunk that nothing comes behind has no totals: its place holds anything, and what is made of it goes nowhere)
-    for (int k = 0; k < n_chunk; k += AT) {
-        float H[AT], sd[AT];
+    for (int k = 0; k < n_chunk; k += 4 * AT) {
+        float H[AT], sd[AT], h = 0.f, sum = 0.f;
 #pragma unroll
         for (int j = 0; j < AT; ++j) {
-            const int o = min(k + j, n_chunk - 1), c = BWD ? n_chunk - 1 - o : o;
+            const int o = min(k + w * AT + j, n_chunk - 1), c = BWD ? n_chunk - 1 - o : o;
             H[j] = totals[(size_t)c * ND + i];
             sd[j] = sums[(size_t)c * D + ch];
         }
+        // (what is worked out for places behind the last chunk goes nowhere; were it left out, the loads would wait in turn)
 #pragma unroll
         for (int j = 0; j < AT; ++j) {
-            // (what is worked out for places behind the last chunk goes nowhere; were it left out, the loads would wait in turn)
-            const int c = BWD ? n_chunk - 1 - (k + j) : k + j;
-            if (k + j < n_chunk) totals[(size_t)c * ND + i] = h;
-            // (a state of zero stays so however much growth has come together)
-            h = sd[j] != sd[j] || h == 0.f ? H[j] : fmaf(exp2_(sd[j] * A2), h, H[j]);
+            h = carried(h, sd[j], A2, H[j]);
+            sum += sd[j];                            // (the mark stays)
         }
+        s_h[w][lane] = h;
+        s_sum[w][lane] = sum;
+        __syncthreads();
+        h = base;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            if (v < w) h = carried(h, s_sum[v][lane], A2, s_h[v][lane]);
+            base = carried(base, s_sum[v][lane], A2, s_h[v][lane]);
+        }
+#pragma unroll
+        for (int j = 0; j < AT; ++j) {
+            const int o = k + w * AT + j, c = BWD ? n_chunk - 1 - o : o;
+            if (o < n_chunk && live) totals[(size_t)c * ND + i] = h;
+            h = carried(h, sd[j], A2, H[j]);
+        }
+        __syncthreads();                             // (the sums have been read)
     }
 }
 
@@ -731,29 +751,42 @@ bool selscan_states_ok(int N) { return N == 8 || N == 16 || N == 32; }
 
 static int waves_per_group(int D, int G) { return (D / G + 63) / 64; }
 
-// Chunks of whole tiles, as many as give `want` workgroups, but none of less than 48 rows.  A wave alone on its SIMD issues at 40 % of the
-// rate that four reach, so the chunks have to be many; what they cost is a state each, to leave, to carry and to begin with.  us: one
-// sequence of 65536 rows, 2048 channels, forward, for 2048, 4096, 6144, 8192 waves: 1079, 928, 906, 893; four of 16384, 1536 channels,
-// forward and backward, for 1536, 2048, 4096, 6144 backward workgroups: 2500, 2430, 2320, 2313.  6007 rows, 1536 channels, forward, for
-// chunks of 32, 48, 64, 96 rows: 106, 98, 112, 117; 3001 rows, 1000 channels, 32 states, both: 248, 244, 261, 299.
-constexpr long kFwdWaves = 6144, kBwdGroups = 4096;
-constexpr int kLeastChunk = 48;
-static void cut_rows(int T, long groups, long want, int* chunk, int* n_chunk)
+// Chunks of whole tiles.  The more there are, the more waves, and the more states to leave, to carry and to begin with (as good as kExtra
+// rows each); and what counts is the fullest SIMD.  A kernel: `units`, its workgroups that bring every SIMD as many waves as one brings its
+// own; `slots`, how often that fits; `weight`, what its row costs.  kRate: what so many waves issue, of what four do; kUneven: how
+// much fuller the fullest SIMD is.
+struct ChunkCost { int units, slots; double weight; };
+constexpr int kLeastChunk = 24, kExtra = 8;
+constexpr double kRate[5] = {1, 0.45, 0.82, 0.93, 1}, kUneven = 0.7;
+static void cut_rows(int T, long groups, const ChunkCost (&kernels)[2], int* chunk, int* n_chunk)
 {
-    long n = groups > 0 ? (want + groups - 1) / groups : 1;
-    if (n > 1024) n = 1024;
-    long len = ((long)T + n - 1) / n;
-    len = (len + kSelscanTile - 1) / kSelscanTile * kSelscanTile;
-    if (len < kLeastChunk) len = kLeastChunk;
-    *chunk = (int)len;
-    *n_chunk = (int)(((long)T + len - 1) / len);
+    double least = 0;
+    for (int i = 1; i <= 24; ++i) {
+        long n = (long)i * kernels[0].units / groups;
+        n = n < 1 ? 1 : n > 1024 ? 1024 : n;
+        long len = ((long)T + n - 1) / n;
+        len = (len + kSelscanTile - 1) / kSelscanTile * kSelscanTile;
+        if (len < kLeastChunk) len = kLeastChunk;
+        n = ((long)T + len - 1) / len;
+        double cost = 0;
+        for (const ChunkCost& k : kernels) {
+            const long all = (n * groups + k.units - 1) / k.units;
+            cost += k.weight * (double)(len + kExtra) * ((double)all + kUneven) / kRate[all < k.slots ? all : k.slots];
+        }
+        if (i > 1 && cost >= least) continue;
+        least = cost;
+        *chunk = (int)len;
+        *n_chunk = (int)n;
+    }
 }
 
 static SelscanPlan plan_of(int T, int D, int N, int G, bool is_bwd, bool has_saved)
 {
     SelscanPlan p{};
     const long groups = (long)G * waves_per_group(D, G);
-    cut_rows(T, groups, is_bwd ? kBwdGroups : kFwdWaves, &p.chunk, &p.n_chunk);
+    const int slots = N == 32 ? 3 : 4;
+    const ChunkCost forward[2] = {{1024, slots, 1.0}, {1024, slots, 1.2}}, backward[2] = {{N == 32 ? 256 : 1024 / (N / NPW), N == 32 ? 1 : 3, 1.0}, {1024, slots, 1.15}};
+    cut_rows(T, groups, is_bwd ? backward : forward, &p.chunk, &p.n_chunk);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) & ~(size_t)255; return here; };
     const size_t ND = (size_t)N * D * sizeof(float);
@@ -810,7 +843,7 @@ template <bool BWD>
 static void carry(const SelscanArgs& a, float* totals, const float* sums, int n_chunk, const float* from, float* to, hipStream_t st)
 {
     const long ND = (long)a.N * a.D;
-    const int groups = (int)((ND + 255) / 256), more = to_pass_on(a, from, to) ? (a.rows.n_seq < 256 ? a.rows.n_seq : 256) : 0;
+    const int groups = (int)((ND + 63) / 64), more = to_pass_on(a, from, to) ? (a.rows.n_seq < 256 ? a.rows.n_seq : 256) : 0;
     hipLaunchKernelGGL(selscan_carry_kernel<BWD>, dim3(groups + more), dim3(256), 0, st, a.A, totals, sums, n_chunk, a.D, ND, groups, a.rows, from,
                        to);
 }
