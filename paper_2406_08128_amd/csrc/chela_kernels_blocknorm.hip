@@ -12,33 +12,41 @@
 
 namespace chela {
 
-// A thread's share of a row: NV pieces of four elements, 8 bytes (bf16) or 16 (fp32) at a time where VEC; else element by element, the
-// threads' elements next to each other.  Raw holds them as they lie in memory.
+// A thread's share of a row: NV pieces of four elements, 8 bytes (bf16) or 16 (fp32) at a time.  VEC: rows begin on a whole piece.  Otherwise
+// they begin on an element (loads and stores of global memory need no more), and the up to three elements behind the last whole piece go to
+// the row's first threads, one each: all loads stay on their way until they are needed.  (Element by element, the threads' next to each other,
+// both directions took 489, 2522, 1820 us at 40 million elements in bf16 rows of 941, 4506, 8191; so they take 227, 385, 330, and those
+// of 1000, 4096, 8192 200, 204, 222.)  Raw holds what was read as it lies in memory.
 template <typename T, int TPR, int NV, bool VEC>
 struct RowPart {
-    static constexpr int E = NV * 4;
-    struct alignas(VEC ? 4 * sizeof(T) : sizeof(T)) Piece { T e[4]; };
-    struct Raw { Piece p[NV]; };
-    static __device__ __forceinline__ int at(int tid, int e) { return VEC ? ((e >> 2) * TPR + tid) * 4 + (e & 3) : e * TPR + tid; }
+    static constexpr int E = NV * 4 + !VEC;
+    typedef unsigned Piece __attribute__((ext_vector_type(sizeof(T))));          // (words: single elements would take a register each)
+    struct __attribute__((packed, aligned(sizeof(T)))) Loose { Piece p; };
+    struct Elements { T e[4]; };
+    struct Raw { Piece p[NV]; T last; };
     static __device__ __forceinline__ void load(const T* row, int D, int tid, Raw& x)
     {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
+            const int k = (v * TPR + tid) * 4;
+            x.p[v] = Piece(0);
             if (VEC) {
-                if (at(tid, 4 * v) < D) x.p[v] = *reinterpret_cast<const Piece*>(row + at(tid, 4 * v));
-                else
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x.p[v].e[j] = (T)0.f;
+                if (k < D) x.p[v] = *reinterpret_cast<const Piece*>(row + k);
             } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x.p[v].e[j] = at(tid, 4 * v + j) < D ? row[at(tid, 4 * v + j)] : (T)0.f;
+                if (k + 4 <= D) x.p[v] = reinterpret_cast<const Loose*>(row + k)->p;
             }
         }
+        if (!VEC) x.last = tid < D % 4 ? row[D / 4 * 4 + tid] : (T)0.f;
     }
     static __device__ __forceinline__ void widen(const Raw& x, float (&to)[E])
     {
 #pragma unroll
-        for (int e = 0; e < E; ++e) to[e] = to_f(x.p[e >> 2].e[e & 3]);
+        for (int v = 0; v < NV; ++v) {
+            const Elements t = __builtin_bit_cast(Elements, x.p[v]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[4 * v + j] = to_f(t.e[j]);
+        }
+        if (!VEC) to[E - 1] = to_f(x.last);
     }
     static __device__ __forceinline__ void load(const T* row, int D, int tid, float (&x)[E])
     {
@@ -50,17 +58,17 @@ struct RowPart {
     {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
+            const int k = (v * TPR + tid) * 4;
+            Elements t;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t.e[j] = from_f<T>(x[4 * v + j]);
             if (VEC) {
-                Piece t;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) t.e[j] = from_f<T>(x[4 * v + j]);
-                if (at(tid, 4 * v) < D) *reinterpret_cast<Piece*>(row + at(tid, 4 * v)) = t;
+                if (k < D) *reinterpret_cast<Piece*>(row + k) = __builtin_bit_cast(Piece, t);
             } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (at(tid, 4 * v + j) < D) row[at(tid, 4 * v + j)] = from_f<T>(x[4 * v + j]);
+                if (k + 4 <= D) reinterpret_cast<Loose*>(row + k)->p = __builtin_bit_cast(Piece, t);
             }
         }
+        if (!VEC && tid < D % 4) row[D / 4 * 4 + tid] = from_f<T>(x[E - 1]);
     }
 };
 
@@ -167,7 +175,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void block_norm_bwd_kernel(B
     typedef RowPart<XT, TPR, NV, VEC> PX;
     typedef RowPart<float, TPR, NV, VEC> PW;
     constexpr int E = P::E, RPW = TPR < 256 ? 256 / TPR : 1;
-    constexpr bool AHEAD = E < 16 || (VEC && sizeof(IO) == 2); // (there are registers for the next row)
+    constexpr bool AHEAD = NV < 4 || sizeof(IO) == 2; // (there are registers for the next row)
     __shared__ float s_a[TPR / 64][3], s_b[TPR / 64][1], s_w[2][RPW > 1 ? TPR * E : 1];
     const int tid = threadIdx.x % TPR, D = a.D;
     const float inv = 1.f / (float)D;
