@@ -1372,7 +1372,7 @@ size_t chela_short_conv_bwd_workspace_bytes(int T, int D, int m, int dtype)
 {
     if (T < 0 || D <= 0 || D > (1 << 20) || too_many(T, D, kRowUnits) || m < 1 || m > kShortConvMaxTaps ||
         (dtype != CHELA_DTYPE_BF16 && dtype != CHELA_DTYPE_F32)) return 0;
-    return (size_t)short_conv_bwd_parts(T) * (m + 1) * D * sizeof(float);
+    return (size_t)short_conv_bwd_parts(T, D) * (m + 1) * D * sizeof(float);
 }
 
 static int short_conv_bwd_common(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,

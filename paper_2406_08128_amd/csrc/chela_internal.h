@@ -236,7 +236,7 @@ struct ShortConvArgs {
     int m, D, silu;
 };
 constexpr int kShortConvMaxTaps = 8;
-int short_conv_bwd_parts(int T);              // partial sums of dw and dbias, [parts][m + 1][D] floats
+int short_conv_bwd_parts(int T, int D);              // partial sums of dw and dbias, [parts][m + 1][D] floats
 hipError_t launch_short_conv_fwd(const ShortConvArgs& a, int dtype, hipStream_t st);
 hipError_t launch_short_conv_bwd(const ShortConvArgs& a, int dtype, hipStream_t st);
 hipError_t launch_short_conv_step(const ShortConvArgs& a, int dtype, hipStream_t st);

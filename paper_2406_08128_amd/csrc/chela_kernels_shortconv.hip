@@ -52,10 +52,9 @@ __device__ __forceinline__ void activation(const float (&u)[V], int silu, float 
 // Where in the sequence that row t belongs to: one look-up per run, then by counting.
 struct Where {
     int q, beg, end;
-    __device__ __forceinline__ void start(const Rows& R, int t)
+    __device__ __forceinline__ void start(const Rows& R, int sequence)
     {
-        q = seq_of(R, t);
-        if (q < 0) q = 0;
+        q = max(sequence, 0);
         set(R);
     }
     __device__ __forceinline__ void set(const Rows& R)
@@ -88,6 +87,28 @@ __device__ __forceinline__ void history(const ShortConvArgs& a, const Where& at,
             if (slot >= 0) load_row<IO, V>((const IO*)a.S_in + ((size_t)slot * (M - 1) + (M - 1 + r - at.beg)) * a.D + ch, back[j]);
         }
     }
+}
+
+// The same where the rows in front of row t are in `back` already, whatever sequence they are of.
+template <typename IO, int V, int M>
+__device__ __forceinline__ void in_front(const ShortConvArgs& a, const Where& at, int t, int ch, float (&back)[M > 1 ? M - 1 : 1][V])
+{
+    if (M == 1 || t - (M - 1) >= at.beg) return;
+    const int slot = a.S_in ? slot_of(a.rows, at.q) : -1;
+#pragma unroll
+    for (int j = 0; j < M - 1; ++j) {
+        const int r = t - 1 - j;
+        if (r >= at.beg) continue;
+#pragma unroll
+        for (int e = 0; e < V; ++e) back[j][e] = 0.f;
+        if (slot >= 0) load_row<IO, V>((const IO*)a.S_in + ((size_t)slot * (M - 1) + (M - 1 + r - at.beg)) * a.D + ch, back[j]);
+    }
+}
+// Row r as it lies in memory; in front of the first and behind the last, where nothing is made of it, the nearest there is.
+template <typename IO, int V>
+__device__ __forceinline__ Raw<IO, V> load_raw(const void* X, long ld, int r, int T, int ch)
+{
+    return row_load((const Raw<IO, V>*)((const IO*)X + (size_t)min(max(r, 0), T - 1) * ld), ch * sizeof(IO));
 }
 
 template <int V, int M>
@@ -144,65 +165,52 @@ __global__ __launch_bounds__(256) void short_conv_kernel(ShortConvArgs a)
         state_behind<IO, M>(a, i / nb, i % nb);
         return;
     }
-    const int ch = (blockIdx.x % across * blockDim.x + threadIdx.x) * V;
-    if (ch >= a.D) return;
+    const int mine = (blockIdx.x % across * blockDim.x + threadIdx.x) * V, ch = min(mine, a.D - V);
     const int t0 = xcd_neighbours(blockIdx.x / across, runs) * RUN, t1 = min(t0 + RUN, R.T);
+    // all rows on their way before the sequence is looked for and the first is looked at
+    Raw<IO, V> x[RUN + M - 1];
+#pragma unroll
+    for (int i = 0; i < RUN + M - 1; ++i) x[i] = load_raw<IO, V>(a.X, a.ldx, t0 - (M - 1) + i, R.T, ch);
     float w[M][V], bias[V], back[M > 1 ? M - 1 : 1][V];
-    Where at;
-    at.start(R, t0);
-    if (at.q < R.n_seq && t0 - (M - 1) >= at.beg && t0 + RUN <= at.end) {
-        // within one sequence: all rows on their way before the first is looked at
-        Raw<IO, V> x[RUN + M - 1];
-#pragma unroll
-        for (int i = 0; i < RUN + M - 1; ++i) x[i] = row_load((const Raw<IO, V>*)((const IO*)a.X + (size_t)(t0 - (M - 1) + i) * a.ldx), ch * sizeof(IO));
-        weights<V, M>(a, ch, w, bias);
-#pragma unroll
-        for (int j = 0; j < M - 1; ++j) widen<IO, V>(x[M - 2 - j], back[j]);
-#pragma unroll
-        for (int i = 0; i < RUN; ++i) {
-            float now[V], u[V], y[V];
-            widen<IO, V>(x[i + M - 1], now);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                u[e] = fmaf(w[0][e], now[e], bias[e]);
-#pragma unroll
-                for (int j = 1; j < M; ++j) u[e] = fmaf(w[j][e], back[j - 1][e], u[e]);
-            }
-            activation<V>(u, a.silu, y);
-            row_store((Raw<IO, V>*)((IO*)a.Y + (size_t)(t0 + i) * a.D), ch * sizeof(IO), narrow<IO, V>(y));
-#pragma unroll
-            for (int j = M - 2; j > 0; --j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) back[j][e] = back[j - 1][e];
-            if (M > 1)
-#pragma unroll
-                for (int e = 0; e < V; ++e) back[0][e] = now[e];
-        }
-        return;
-    }
     weights<V, M>(a, ch, w, bias);
-    int known = -1;                                   // the sequence that `back` is of
-#pragma unroll 1
-    for (int t = t0; t < t1; ++t) {
-        if (!at.at(R, t)) continue;
-        if (known != at.q) { history<IO, V, M>(a, at, t, ch, back); known = at.q; }
-        float x[V], u[V], y[V];
-        load_row<IO, V>((const IO*)a.X + (size_t)t * a.ldx + ch, x);
+    Where at;
+    at.start(R, seq_of_wave(R, t0, threadIdx.x & 63));
+    if (mine >= a.D) return;
+    const bool whole = at.q < R.n_seq && t0 - (M - 1) >= at.beg && t0 + RUN <= at.end;       // within one sequence
+#pragma unroll
+    for (int j = 0; j < M - 1; ++j) widen<IO, V>(x[M - 2 - j], back[j]);
+    auto row = [&](Raw<IO, V> raw, IO* to) {
+        float now[V], u[V], y[V];
+        widen<IO, V>(raw, now);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            u[e] = fmaf(w[0][e], x[e], bias[e]);
+            u[e] = fmaf(w[0][e], now[e], bias[e]);
 #pragma unroll
             for (int j = 1; j < M; ++j) u[e] = fmaf(w[j][e], back[j - 1][e], u[e]);
         }
         activation<V>(u, a.silu, y);
-        store_row<IO, V>((IO*)a.Y + (size_t)t * a.D + ch, y);
+        if (to) row_store((Raw<IO, V>*)to, ch * sizeof(IO), narrow<IO, V>(y));
 #pragma unroll
         for (int j = M - 2; j > 0; --j)
 #pragma unroll
             for (int e = 0; e < V; ++e) back[j][e] = back[j - 1][e];
         if (M > 1)
 #pragma unroll
-            for (int e = 0; e < V; ++e) back[0][e] = x[e];
+            for (int e = 0; e < V; ++e) back[0][e] = now[e];
+    };
+    if (whole) {
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) row(x[i + M - 1], (IO*)a.Y + (size_t)(t0 + i) * a.D);
+        return;
+    }
+    int known = -1;                                   // the sequence that `back` is of
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t) {
+        const bool on = at.at(R, t);
+        if (on && known != at.q) { in_front<IO, V, M>(a, at, t, ch, back); known = at.q; }
+        row(x[M - 1], on ? (IO*)a.Y + (size_t)t * a.D : nullptr);
+#pragma unroll
+        for (int i = M - 1; i < RUN + M - 2; ++i) x[i] = x[i + 1];
     }
 }
 
@@ -251,57 +259,73 @@ __global__ __launch_bounds__(256) void short_conv_bwd_kernel(ShortConvArgs a, in
     }
     // neighbouring runs, so that the rows that two runs share come from the L2
     const int mine = (runs + (int)gridDim.y - 1) / (int)gridDim.y, first = (int)blockIdx.y * mine;
+    Where at;                                         // (looked up once: for each run anew, 32 sequences cost 45 of 180 us)
+    at.start(R, seq_of(R, first * RUN));
     for (int run = first; run < min(first + mine, runs); ++run) {
         const int t0 = run * RUN, t1 = min(t0 + RUN, R.T);
+        // the run and all that it shares with others on their way before the sequence is looked for and the first row is looked at
+        Raw<IO, V> xs[RUN + 2 * (M - 1)], dys[RUN + M - 1];
+#pragma unroll
+        for (int i = 0; i < RUN + 2 * (M - 1); ++i) xs[i] = load_raw<IO, V>(a.X, a.ldx, t0 - (M - 1) + i, R.T, ch);
+#pragma unroll
+        for (int i = 0; i < RUN + M - 1; ++i) dys[i] = load_raw<IO, V>(a.dY, a.lddy, t0 + i, R.T, ch);
         float back[M > 1 ? M - 1 : 1][V], pend[M][V];
-        Where at;
-        at.start(R, t0);
-        if (at.q < R.n_seq && t0 - (M - 1) >= at.beg && t0 + RUN + M - 1 <= at.end) {
-            // the run and all that it shares with others within one sequence, none of the last m - 1 rows in it
-            Raw<IO, V> xs[RUN + 2 * (M - 1)], dys[RUN + M - 1];
+        at.at(R, t0);
+        // within one sequence, none of the last m - 1 rows in it?
+        const bool whole = at.q < R.n_seq && t0 - (M - 1) >= at.beg && t0 + RUN + M - 1 <= at.end;
 #pragma unroll
-            for (int i = 0; i < RUN + 2 * (M - 1); ++i)
-                xs[i] = row_load((const Raw<IO, V>*)((const IO*)a.X + (size_t)(t0 - (M - 1) + i) * a.ldx), ch * sizeof(IO));
+        for (int j = 0; j < M - 1; ++j) widen<IO, V>(xs[M - 2 - j], back[j]);
 #pragma unroll
-            for (int i = 0; i < RUN + M - 1; ++i)
-                dys[i] = row_load((const Raw<IO, V>*)((const IO*)a.dY + (size_t)(t0 + i) * a.lddy), ch * sizeof(IO));
-            float x[M][V];                            // x[j]: x_{t-j}
+        for (int k = 0; k < M; ++k)
 #pragma unroll
-            for (int j = 1; j < M; ++j) widen<IO, V>(xs[M - 1 - j], x[j]);
+            for (int e = 0; e < V; ++e) pend[k][e] = 0.f;
+        // a row's part in pend and, if it is one of the run's, in the sums
+        auto row = [&](Raw<IO, V> xr, Raw<IO, V> dyr, bool mine) {
+            float x[V], du[V];
+            widen<IO, V>(xr, x);
+            widen<IO, V>(dyr, du);
 #pragma unroll
-            for (int k = 0; k < M; ++k)
+            for (int e = 0; e < V; ++e) {
+                if (a.silu) {
+                    float u = fmaf(w[0][e], x[e], bias[e]);
 #pragma unroll
-                for (int e = 0; e < V; ++e) pend[k][e] = 0.f;
+                    for (int j = 1; j < M; ++j) u = fmaf(w[j][e], back[j - 1][e], u);
+                    const float s = sigmoid_(u);
+                    du[e] *= s * fmaf(u, 1.f - s, 1.f);
+                }
+#pragma unroll
+                for (int j = 0; j < M; ++j) pend[j][e] = fmaf(w[j][e], du[e], pend[j][e]);
+                if (mine) {
+                    db[e] += du[e];
+                    dw[0][e] = fmaf(du[e], x[e], dw[0][e]);
+#pragma unroll
+                    for (int j = 1; j < M; ++j) dw[j][e] = fmaf(du[e], back[j - 1][e], dw[j][e]);
+                }
+            }
+        };
+        auto next_x = [&](Raw<IO, V> xr) {
+#pragma unroll
+            for (int j = M - 2; j > 0; --j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) back[j][e] = back[j - 1][e];
+            if (M > 1) widen<IO, V>(xr, back[0]);
+        };
+        auto next_pend = [&]() {
+#pragma unroll
+            for (int j = M - 1; j > 0; --j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) pend[j][e] = pend[j - 1][e];
+#pragma unroll
+            for (int e = 0; e < V; ++e) pend[0][e] = 0.f;
+        };
+        if (whole) {
 #pragma unroll
             for (int i = 0; i < RUN + M - 1; ++i) {
-                float du[V];
-                widen<IO, V>(xs[i + M - 1], x[0]);
-                widen<IO, V>(dys[i], du);
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    if (a.silu) {
-                        float u = bias[e];
-#pragma unroll
-                        for (int j = 0; j < M; ++j) u = fmaf(w[j][e], x[j][e], u);
-                        const float s = sigmoid_(u);
-                        du[e] *= s * fmaf(u, 1.f - s, 1.f);
-                    }
-#pragma unroll
-                    for (int j = 0; j < M; ++j) pend[j][e] = fmaf(w[j][e], du[e], pend[j][e]);
-                    if (i < RUN) {
-                        db[e] += du[e];
-#pragma unroll
-                        for (int j = 0; j < M; ++j) dw[j][e] = fmaf(du[e], x[j][e], dw[j][e]);
-                    }
-                }
+                row(xs[i + M - 1], dys[i], i < RUN);
                 if (i >= M - 1)
                     row_store((Raw<IO, V>*)((IO*)a.dX + (size_t)(t0 + i - (M - 1)) * a.D), ch * sizeof(IO), narrow<IO, V>(pend[M - 1]));
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-#pragma unroll
-                    for (int j = M - 1; j > 0; --j) { x[j][e] = x[j - 1][e]; pend[j][e] = pend[j - 1][e]; }
-                    pend[0][e] = 0.f;
-                }
+                next_x(xs[i + M - 1]);
+                next_pend();
             }
             continue;
         }
@@ -310,44 +334,32 @@ __global__ __launch_bounds__(256) void short_conv_bwd_kernel(ShortConvArgs a, in
 #pragma unroll 1
         for (int t = t0; t - t1 < M - 1; ++t) {
             if (t >= R.T || (t >= t1 && (known != at.q || t >= at.end))) break;
-            if (t < t1 && !at.at(R, t)) continue;
+            const Raw<IO, V> xr = xs[M - 1], dyr = dys[0];
+#pragma unroll
+            for (int i = M - 1; i < RUN + 2 * (M - 1) - 1; ++i) xs[i] = xs[i + 1];
+#pragma unroll
+            for (int i = 0; i < RUN + M - 2; ++i) dys[i] = dys[i + 1];
+            if (t < t1 && !at.at(R, t)) { next_x(xr); continue; }
             if (known != at.q) {
                 known = at.q;
-                history<IO, V, M>(a, at, t, ch, back);
+                in_front<IO, V, M>(a, at, t, ch, back);
 #pragma unroll
                 for (int k = 0; k < M; ++k)
 #pragma unroll
                     for (int e = 0; e < V; ++e) pend[k][e] = 0.f;
             }
-            float x[V], dy[V], u[V];
-            load_row<IO, V>((const IO*)a.X + (size_t)t * a.ldx + ch, x);
-            load_row<IO, V>((const IO*)a.dY + (size_t)t * a.lddy + ch, dy);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                u[e] = fmaf(w[0][e], x[e], bias[e]);
-#pragma unroll
-                for (int j = 1; j < M; ++j) u[e] = fmaf(w[j][e], back[j - 1][e], u[e]);
-                float du = dy[e];
-                if (a.silu) {
-                    const float s = sigmoid_(u[e]);
-                    du *= s * fmaf(u[e], 1.f - s, 1.f);
-                }
-#pragma unroll
-                for (int j = 0; j < M; ++j) pend[j][e] = fmaf(w[j][e], du, pend[j][e]);
-                if (t < t1) {
-                    db[e] += du;
-                    dw[0][e] = fmaf(du, x[e], dw[0][e]);
-#pragma unroll
-                    for (int j = 1; j < M; ++j) dw[j][e] = fmaf(du, back[j - 1][e], dw[j][e]);
-                }
-            }
-            // what is complete: row t - (m - 1); behind the sequence's last row, all that are left
-            auto leave = [&](int k) {
-                const int r = t - k, behind = r - (at.end - (M - 1));        // place in the state behind the sequence
-                if (r >= at.beg ? (r < t0 || r >= t1) : (!a.dS_in || at.beg < t0 || at.beg >= t1 || r < at.beg - (M - 1))) return;
+            row(xr, dyr, t < t1);
+            next_x(xr);
+            // what is complete: row t - (m - 1); behind the sequence's last row, all that are left.  (One after the other: this code runs once in
+            // a while, and has to come from memory first)
+            const int rows = t == at.end - 1 ? M : 1;
+#pragma unroll 1
+            for (int i = 0; i < rows; ++i, next_pend()) {
+                const int r = t + i - (M - 1), behind = r - (at.end - (M - 1));        // place in the state behind the sequence
+                if (r >= at.beg ? (r < t0 || r >= t1) : (!a.dS_in || at.beg < t0 || at.beg >= t1 || r < at.beg - (M - 1))) continue;
                 float g[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) g[e] = pend[k][e];
+                for (int e = 0; e < V; ++e) g[e] = pend[M - 1][e];
                 const int slot = (r < at.beg || (a.dS_out && behind >= 0)) ? slot_of(R, at.q) : -1;
                 if (a.dS_out && behind >= 0 && slot >= 0) {
                     float d[V];
@@ -357,24 +369,6 @@ __global__ __launch_bounds__(256) void short_conv_bwd_kernel(ShortConvArgs a, in
                 }
                 if (r >= at.beg) store_row<IO, V>((IO*)a.dX + (size_t)r * a.D + ch, g);
                 else if (slot >= 0) store_row<IO, V>((IO*)a.dS_in + ((size_t)slot * (M - 1) + (M - 1 + r - at.beg)) * a.D + ch, g);
-            };
-            leave(M - 1);
-            if (t == at.end - 1) {
-#pragma unroll
-                for (int k = M - 2; k >= 0; --k) leave(k);
-            }
-#pragma unroll
-            for (int j = M - 2; j > 0; --j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) back[j][e] = back[j - 1][e];
-#pragma unroll
-            for (int j = M - 1; j > 0; --j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) pend[j][e] = pend[j - 1][e];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                pend[0][e] = 0.f;
-                if (M > 1) back[0][e] = x[e];
             }
         }
     }
@@ -445,9 +439,10 @@ static unsigned threads_for(int vectors) { return vectors >= 256 ? 256u : (unsig
     else { if (V > 1) { CHELA_TAPS(F, float, 2) } else { CHELA_TAPS(F, float, 1) } }
 
 // Rows of a run: the fewer, the more rows are read twice, the more, the fewer workgroups there are to read.  Forward, us, runs of 8, 16, 32
-// rows: 83, 74, 70 at 65536 rows, 13.7, 15.0, - at 6007 (the short ones below 2048 workgroups).  Gradient, runs of 8 in 512, 768, 1024
-// parts: 154, 138, 141, and 5, 8, 10 to add them up.
-constexpr int kRun = 16, kShortRun = 8, kBwdRun = 8, kBwdParts = 768;
+// rows: 83, 74, 70 at 65536 rows, 13.7, 15.0, - at 6007 (the short ones below 2048 workgroups).  Gradient, runs of 8 in as many parts as
+// make 768 * 768 threads, half and twice as many: 1536 channels 138, 148, 143 us, 4096 channels 133, -, 145 (what the parts leave has to be added
+// up); of few channels more of them fill the card: 101 channels, 768 and 1536 parts, 319 and 240.
+constexpr int kRun = 16, kShortRun = 8, kBwdRun = 8, kBwdThreads = 768 * 768, kLeastParts = 256, kMostParts = 1536;
 
 hipError_t launch_short_conv_fwd(const ShortConvArgs& a, int dtype, hipStream_t st)
 {
@@ -474,10 +469,11 @@ hipError_t launch_short_conv_fwd(const ShortConvArgs& a, int dtype, hipStream_t 
     return hipGetLastError();
 }
 
-int short_conv_bwd_parts(int T)
+int short_conv_bwd_parts(int T, int D)
 {
-    const int runs = (T + kBwdRun - 1) / kBwdRun;
-    return runs < kBwdParts ? (runs > 0 ? runs : 1) : kBwdParts;
+    const int threads = (D / (D % 2 ? 1 : 2) + 63) / 64 * 64, runs = (T + kBwdRun - 1) / kBwdRun;
+    const int want = kBwdThreads / threads, most = want > kMostParts ? kMostParts : want < kLeastParts ? kLeastParts : want;
+    return runs < most ? (runs > 0 ? runs : 1) : most;
 }
 
 hipError_t launch_short_conv_bwd(const ShortConvArgs& a, int dtype, hipStream_t st)
@@ -485,7 +481,7 @@ hipError_t launch_short_conv_bwd(const ShortConvArgs& a, int dtype, hipStream_t 
     ProfScope prof(KID_SHORT_CONV, st);
     const int V = pairs(a, dtype) ? 2 : 1, vectors = (a.D + V - 1) / V;
     const unsigned threads = threads_for(vectors);
-    const int runs = (a.rows.T + kBwdRun - 1) / kBwdRun, parts = short_conv_bwd_parts(a.rows.T);
+    const int runs = (a.rows.T + kBwdRun - 1) / kBwdRun, parts = short_conv_bwd_parts(a.rows.T, a.D);
     const dim3 grid((vectors + threads - 1) / threads, parts);
 #define CHELA_F(IO, V, M) hipLaunchKernelGGL((short_conv_bwd_kernel<IO, V, M, kBwdRun>), grid, dim3(threads), 0, st, a, runs)
     CHELA_TYPES(CHELA_F)
