@@ -35,7 +35,8 @@ _fn = dict.fromkeys(("linattn_fwd", "linattn_fwd_f32", "linattn_fwd_state", "lin
                      "linattn_noncausal_bwd", "longconv_spectrum", "longconv_spectrum_bytes", "shortlong_conv_fwd",
                      "shortlong_conv_fwd_f32", "shortlong_conv_bwd", "shortlong_conv_bwd_f32", "short_conv_fwd", "short_conv_fwd_f32",
                      "short_conv_step", "short_conv_step_f32", "selscan_fwd", "selscan_fwd_f32", "selscan_step", "selscan_step_f32",
-                     "selscan_saved_bytes", "block_norm_fwd", "block_norm_fwd_f32"), 0)
+                     "selscan_saved_bytes", "block_norm_fwd", "block_norm_fwd_f32", "short_conv_bwd", "short_conv_bwd_f32", "selscan_bwd",
+                     "selscan_bwd_f32", "block_norm_bwd", "block_norm_bwd_f32"), 0)
 
 
 class ChelaError(RuntimeError):
@@ -870,6 +871,9 @@ def chela_short_conv_fwd(X, w, bias=None, silu=True, cu=None, S_in=None, S_out=N
 def chela_short_conv_bwd(X, w, dY, bias=None, silu=True, cu=None, S_in=None, dS_out=None, want_dS_in=False, stream=None):
     """(dX, dw, dbias, dS_in) of chela_short_conv_fwd (without slots) for the upstream gradients dY and dS_out; dbias is None without a
     bias, dS_in unless asked for."""
+    r = _host("short_conv_bwd")(_fn["short_conv_bwd"], _fn["short_conv_bwd_f32"], X, w, dY, bias, silu, cu, S_in, dS_out, want_dS_in, stream)
+    if r is not None:
+        return _host_result(r)
     pcu, n_seq, T, D = _sequences(X, cu, "X")
     sfx, _ = _suffix(X)
     px, ldx = _row_stride(X, X, "X")
@@ -971,6 +975,10 @@ def chela_selscan_bwd(U, delta, A, Bm, Cm, dY, D=None, Z=None, delta_bias=None, 
                       want_dS_in=False, saved=None, stream=None):
     """(dU, ddelta, dA, dB, dC, dD, dZ, ddelta_bias, dS_in) of chela_selscan_fwd (without slots) for the upstream gradients dY and dS_out;
     None for what there is no input of, dS_in unless asked for.  saved: the forward call's on the same inputs, or None."""
+    r = _host("selscan_bwd")(_fn["selscan_bwd"], _fn["selscan_bwd_f32"], _fn["selscan_saved_bytes"], U, delta, A, Bm, Cm, dY, D, Z, delta_bias,
+                             softplus, cu, S_in, dS_out, want_dS_in, saved, stream)
+    if r is not None:
+        return _host_result(r)
     pcu, n_seq, T, width = _sequences(U, cu, "U")
     sfx, _ = _suffix(U)
     args, N, G = _scan_inputs(U, delta, A, Bm, Cm, D, Z, delta_bias, softplus)
@@ -1068,6 +1076,10 @@ def chela_block_norm_fwd(Y, X, gate=None, w_post=None, w_pre=None, scale=1.0, ep
 def chela_block_norm_bwd(Y, X_out, dX_out, dN, gate=None, w_post=None, w_pre=None, scale=1.0, eps=1e-5, in_place=False, stream=None):
     """(dY, dgate, dX, dw_post, dw_pre) of chela_block_norm_fwd from its inputs and X_out, for the upstream gradients dX_out (None: zero)
     and dN (only with w_pre); None for what there is no input of.  in_place=True writes dX over dX_out."""
+    r = _host("block_norm_bwd")(_fn["block_norm_bwd"], _fn["block_norm_bwd_f32"], Y, X_out, dX_out, dN, gate, w_post, w_pre, scale, eps, in_place,
+                                stream)
+    if r is not None:
+        return _host_result(r)
     sfx, rows, D, x_f32, ptrs = _norm_inputs(Y, X_out, gate, w_post, w_pre)
     dev, io = X_out.device, X_out.dtype if Y is None else Y.dtype
     pdx = _dense(dX_out, X_out.shape, X_out.dtype, dev, "dX_out")

@@ -20,9 +20,14 @@
 //   selscan_fwd(f, f32, saved_bytes, U, delta, A, Bm, Cm, D, Z, delta_bias, softplus, cu, S_in, S_out, slots, want_saved, Y, stream) -> (Y, saved)
 //   selscan_step(f, f32, u, delta, A, Bm, Cm, S, D, z, delta_bias, softplus, slots, y, stream) -> y
 //   block_norm_fwd(f, f32, Y, X, gate, w_post, w_pre, scale, eps, stream) -> (X_out, Nrm)
+//   short_conv_bwd(f, f32, X, w, dY, bias, silu, cu, S_in, dS_out, want_dS_in, stream) -> (dX, dw, dbias, dS_in)
+//   selscan_bwd(f, f32, saved_bytes, U, delta, A, Bm, Cm, dY, D, Z, delta_bias, softplus, cu, S_in, dS_out, want_dS_in, saved, stream)
+//       -> (dU, ddelta, dA, dB, dC, dD, dZ, ddelta_bias, dS_in)
+//   block_norm_bwd(f, f32, Y, X_out, dX_out, dN, gate, w_post, w_pre, scale, eps, in_place, stream) -> (dY, dgate, dX, dw_post, dw_pre)
 // Host side of a call, us, the binding's own lines and these: forward, one launch, 8.5 and 4.4, two launches 9.7 and 6.2; with the
 // state 9.9 and 4.8, 12.1 and 7.2; backward, two launches, 11.4 and 7.5; the three calls of a gated layer's step, six launches, 39.6 and 23;
-// spectrum, forward and gradient of a convolution, 22.5 and 15.
+// spectrum, forward and gradient of a convolution, 22.5 and 15; both directions on 64 rows of 512 channels: short convolution, four launches, 39 and
+// 21, selective scan, nine launches, 90 and 42, block norms 27 and 14.
 #include <Python.h>
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
@@ -442,6 +447,14 @@ typedef int (*selscan_step_fn)(const void*, long long, const void*, long long, c
 typedef size_t (*selscan_saved_fn)(int, int, int);
 typedef int (*block_norm_fwd_fn)(const void*, const void*, const void*, const float*, const float*, void*, void*, float, float, long long, int,
                                  int, void*);
+typedef int (*short_conv_bwd_fn)(const void*, long long, const float*, int, const float*, int, const int*, int, int, int, const void*, const void*,
+                                 long long, const void*, void*, float*, float*, void*, void*);
+typedef int (*selscan_bwd_fn)(const void*, long long, const void*, long long, const float*, const void*, long long, const void*, long long,
+                              const float*, const void*, long long, const float*, int, const int*, int, int, int, int, int, const float*,
+                              const void*, long long, const float*, const void*, void*, void*, float*, void*, void*, float*, void*, float*, float*,
+                              void*);
+typedef int (*block_norm_bwd_fn)(const void*, const void*, const void*, const float*, const float*, const void*, const void*, void*, void*, void*,
+                                 float*, float*, float, float, long long, int, int, void*);
 
 struct Rows {
     c10::DeviceIndex dev;
@@ -736,11 +749,143 @@ PyObject* block_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// A new contiguous tensor's address, where there is to be one.
+template <typename T_ = void>
+T_* make(at::Tensor& t, bool wanted, at::IntArrayRef sizes, const at::TensorOptions& o)
+{
+    if (!wanted) return nullptr;
+    t = at::empty(sizes, o);
+    return (T_*)t.data_ptr();
+}
+
+PyObject* short_conv_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 12) { PyErr_SetString(PyExc_TypeError, "short_conv_bwd takes twelve arguments"); return nullptr; }
+    Rows x;
+    const void *px, *pdy, *pin, *pds;
+    long long ldx, lddy;
+    const float *pw, *pb;
+    const int silu = flag(a[6]), want = flag(a[10]);
+    if (silu < 0 || want < 0 || !x.first(a[2], a[7], a[11]) || !x.rows(a[2], x.D, &px, &ldx) || !x.rows(a[4], x.D, &pdy, &lddy) ||
+        THPVariable_Unpack(a[4]).dim() != x.dims + 1 || !plain_sizes(a[3], at::kFloat, x.dev, 2))
+        Py_RETURN_NONE;
+    const int64_t m = THPVariable_Unpack(a[3]).size(1);
+    if (m < 1 || !x.dense(a[3], at::kFloat, {x.D, m}, false, &pw) || !x.dense(a[5], at::kFloat, {x.D}, true, &pb) ||
+        !x.dense(a[8], x.type, {x.n_seq, m - 1, x.D}, true, &pin) || !x.dense(a[9], x.type, {x.n_seq, m - 1, x.D}, true, &pds))
+        Py_RETURN_NONE;
+    const at::Tensor& X = THPVariable_Unpack(a[2]);
+    const auto f = address<short_conv_bwd_fn>(x.function(a));
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor out[4];
+    int rc;
+    {
+        const without_interpreter_lock free;
+        const at::TensorOptions io = like(X).memory_format(at::MemoryFormat::Contiguous), f32 = io.dtype(at::kFloat);
+        void* dx = make(out[0], true, X.sizes(), io);
+        float *dw = make<float>(out[1], true, {x.D, m}, f32), *db = make<float>(out[2], a[5] != Py_None, {x.D}, f32);
+        void* ds = make(out[3], want != 0, {x.n_seq, m - 1, x.D}, io);
+        rc = f(px, ldx, pw, (int)m, pb, silu, x.cu, x.n_seq, (int)x.T, (int)x.D, pin, pdy, lddy, pds, dx, dw, db, ds, stream_of(x.dev));
+    }
+    return rc != 0 ? PyLong_FromLong(rc) : wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* selscan_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 19) { PyErr_SetString(PyExc_TypeError, "selscan_bwd takes nineteen arguments"); return nullptr; }
+    Rows x;
+    Scan s;
+    const void *pdy, *psaved = nullptr;
+    long long lddy;
+    const float *pin, *pds;
+    const int softplus = flag(a[12]), want = flag(a[16]);
+    if (softplus < 0 || want < 0 || !x.first(a[3], a[13], a[18]) || !s.read(x, a + 3, a + 9) || !x.rows(a[8], x.D, &pdy, &lddy) ||
+        THPVariable_Unpack(a[8]).dim() != x.dims + 1 || !x.dense(a[14], at::kFloat, {x.n_seq, s.N, x.D}, true, &pin) ||
+        !x.dense(a[15], at::kFloat, {x.n_seq, s.N, x.D}, true, &pds))
+        Py_RETURN_NONE;
+    const auto f = address<selscan_bwd_fn>(x.function(a));
+    const auto bytes = address<selscan_saved_fn>(a[2]);
+    if (PyErr_Occurred()) return nullptr;
+    if (a[17] != Py_None) {
+        if (!plain(a[17], at::kFloat, x.dev)) Py_RETURN_NONE;
+        const at::Tensor& saved = THPVariable_Unpack(a[17]);
+        if ((size_t)saved.numel() * 4 < bytes((int)x.T, (int)x.D, (int)s.N)) Py_RETURN_NONE;
+        psaved = saved.data_ptr();
+    }
+    const at::Tensor &U = THPVariable_Unpack(a[3]), &B = THPVariable_Unpack(a[6]);
+    at::Tensor out[9];
+    int rc;
+    {
+        const without_interpreter_lock free;
+        const at::TensorOptions io = like(U).memory_format(at::MemoryFormat::Contiguous), f32 = io.dtype(at::kFloat);
+        void *du = make(out[0], true, U.sizes(), io), *dd = make(out[1], true, U.sizes(), io);
+        float* dA = make<float>(out[2], true, {s.N, x.D}, f32);
+        void *dB = make(out[3], true, B.sizes(), io), *dC = make(out[4], true, B.sizes(), io);
+        float* dD = make<float>(out[5], a[9] != Py_None, {x.D}, f32);
+        void* dZ = make(out[6], a[10] != Py_None, U.sizes(), io);
+        float *db = make<float>(out[7], a[11] != Py_None, {x.D}, f32), *ds = make<float>(out[8], want != 0, {x.n_seq, s.N, x.D}, f32);
+        rc = f(s.U, s.ldu, s.delta, s.ldd, s.A, s.Bm, s.ldb, s.Cm, s.ldc, s.D, s.Z, s.ldz, s.bias, softplus, x.cu, x.n_seq, (int)x.T, (int)x.D,
+               (int)s.N, (int)s.G, pin, pdy, lddy, pds, psaved, du, dd, dA, dB, dC, dD, dZ, db, ds, stream_of(x.dev));
+    }
+    return rc != 0 ? PyLong_FromLong(rc) : wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* block_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 13) { PyErr_SetString(PyExc_TypeError, "block_norm_bwd takes thirteen arguments"); return nullptr; }
+    const int in_place = flag(a[11]);
+    if (modes() || a[12] != Py_None || in_place < 0 || !PyFloat_CheckExact(a[9]) || !PyFloat_CheckExact(a[10]) || !on_gpu(a[2]) || !on_gpu(a[3]))
+        Py_RETURN_NONE;
+    Rows x;
+    x.dev = c10::hip::current_device();
+    x.type = THPVariable_Unpack(a[2]).scalar_type();
+    const at::Tensor& X = THPVariable_Unpack(a[3]);
+    const at::ScalarType xt = X.scalar_type();
+    if ((x.type != at::kBFloat16 && x.type != at::kFloat) || (xt != x.type && xt != at::kFloat) || X.dim() < 1) Py_RETURN_NONE;
+    const int64_t D = X.size(-1);
+    if (D < 1 || D > 0x7fffffff || (a[5] == Py_None) != (a[8] == Py_None) || (in_place && a[4] == Py_None)) Py_RETURN_NONE;
+    const void *pY, *pX, *pg, *pdn;
+    void* pdx;
+    const float *pp, *pn;
+    if (!x.dense(a[2], x.type, X.sizes(), false, &pY) || !x.dense(a[3], xt, X.sizes(), false, &pX) || !x.dense(a[4], xt, X.sizes(), true, &pdx) ||
+        !x.dense(a[5], x.type, X.sizes(), true, &pdn) || !x.dense(a[6], x.type, X.sizes(), true, &pg) ||
+        !x.dense(a[7], at::kFloat, {D}, true, &pp) || !x.dense(a[8], at::kFloat, {D}, true, &pn))
+        Py_RETURN_NONE;
+    const auto f = address<block_norm_bwd_fn>(a[x.type == at::kFloat ? 1 : 0]);
+    if (PyErr_Occurred()) return nullptr;
+    const float scale = (float)PyFloat_AS_DOUBLE(a[9]), eps = (float)PyFloat_AS_DOUBLE(a[10]);
+    at::Tensor out[5];
+    int rc;
+    {
+        const without_interpreter_lock free;
+        const at::TensorOptions io = like(X).dtype(x.type), f32 = like(X).dtype(at::kFloat);
+        void *dY = make(out[0], true, X.sizes(), io), *dg = make(out[1], a[6] != Py_None, X.sizes(), io);
+        void* dX = in_place ? pdx : make(out[2], true, X.sizes(), like(X));
+        float *dp = make<float>(out[3], a[7] != Py_None, {D}, f32), *dn = make<float>(out[4], a[8] != Py_None, {D}, f32);
+        rc = f(pY, pg, pX, pp, pn, pdx, pdn, dY, dg, dX, dp, dn, scale, eps, (long long)(X.numel() / D), (int)D, xt != x.type, stream_of(x.dev));
+    }
+    if (rc != 0) return PyLong_FromLong(rc);
+    PyObject* all = wrap(out);
+    if (all != nullptr && in_place) {
+        PyObject* was = PyTuple_GET_ITEM(all, 2);
+        Py_INCREF(a[4]);
+        PyTuple_SET_ITEM(all, 2, a[4]);
+        Py_DECREF(was);
+    }
+    return all;
+    END_HANDLE_TH_ERRORS
+}
+
 #define CHELA_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CHELA_METHOD(step), CHELA_METHOD(forward), CHELA_METHOD(backward), CHELA_METHOD(gated),
                          CHELA_METHOD(gate_norm_bwd), CHELA_METHOD(zbwd_saved), CHELA_METHOD(spectrum), CHELA_METHOD(conv_fwd),
                          CHELA_METHOD(conv_bwd), CHELA_METHOD(short_conv_fwd), CHELA_METHOD(short_conv_step), CHELA_METHOD(selscan_fwd),
-                         CHELA_METHOD(selscan_step), CHELA_METHOD(block_norm_fwd), {nullptr, nullptr, 0, nullptr}};
+                         CHELA_METHOD(selscan_step), CHELA_METHOD(block_norm_fwd), CHELA_METHOD(short_conv_bwd), CHELA_METHOD(selscan_bwd),
+                         CHELA_METHOD(block_norm_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_chela_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

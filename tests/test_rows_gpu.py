@@ -666,7 +666,10 @@ def test_the_compiled_host_path_and_the_binding_do_the_same(dtype, D):
             out.append([t for t in (y if isinstance(y, tuple) else (y,)) if t is not None] + list(own.values()))
         bits = lambda t: t.contiguous().view(torch.int16 if t.dtype == BF else torch.int32)  # noqa: E731  (of what is no number, too)
         for a, b in zip(*out):
-            assert a.shape == b.shape and a.dtype == b.dtype and torch.equal(bits(a), bits(b))
+            assert a.shape == b.shape and a.dtype == b.dtype
+            if "cu" in kw and a.shape[0] == n * L:
+                a, b = a[:145], b[:145]                                  # (the others are of no sequence: new tensors hold anything there)
+            assert torch.equal(bits(a), bits(b))
 
     for x, kw in ((u, {}), (b3(u), {}), (wide, {}), (u, dict(cu=cu, silu=False)), (b3(u), dict(bias=bias, Y=torch.empty_like(b3(u))))):
         both(binding.chela_short_conv_fwd, x, w, **kw)
@@ -685,6 +688,24 @@ def test_the_compiled_host_path_and_the_binding_do_the_same(dtype, D):
     for kw in (dict(w_pre=g1), dict(gate=z, w_post=g1, w_pre=g1, scale=0.5), dict(w_post=g1)):
         both(binding.chela_block_norm_fwd, u, delta, **kw)
     both(binding.chela_block_norm_fwd, None, b3(u), w_pre=g1)
+    dY, dS, dC = r(n * L, D).to(dtype), r(4, N, D), r(4, m - 1, D).to(dtype)
+    both(binding.chela_short_conv_bwd, u, w, dY, cu=cu, S_in=conv[:4], dS_out=dC, want_dS_in=True, bias=bias)
+    both(binding.chela_short_conv_bwd, b3(u), w, b3(dY), silu=False)
+    both(binding.chela_short_conv_bwd, wide, w, wide_rows(dY))
+    saved = binding.chela_selscan_fwd(u, delta, A, Bm, Cm, cu=cu, Z=z, S_in=pool[:4], want_saved=True, **full)[1]
+    both(binding.chela_selscan_bwd, u, delta, A, Bm, Cm, dY, cu=cu, Z=z, S_in=pool[:4], dS_out=dS, want_dS_in=True, saved=saved, **full)
+    both(binding.chela_selscan_bwd, b3(u), b3(delta), A, b3(Bm.flatten(1)), b3(Cm.flatten(1)), b3(dY))
+    for kw in (dict(w_pre=g1), dict(gate=z, w_post=g1, w_pre=g1, scale=0.5), dict(w_post=g1)):
+        both(binding.chela_block_norm_bwd, u, delta, dY, z if "w_pre" in kw else None, **kw)
+    both(binding.chela_block_norm_bwd, u, b3(delta).flatten(0, 1), None, z, w_pre=g1)
+    x1, x2 = dY.clone(), dY.clone()
+    a = binding.chela_block_norm_bwd(u, delta, x1, z, w_pre=g1, in_place=True)
+    b = binding.chela_block_norm_bwd(u, delta, x2, z, w_pre=g1, in_place=True, stream=here)
+    assert a[2] is x1 and b[2] is x2 and torch.equal(x1, x2) and not torch.equal(x1, dY) and a[1] is None and a[3] is None
+    for bad in (dict(saved=saved[:-4]), dict(saved=saved.double()), dict(dS_out=pool), dict(S_in=dS.double())):
+        for s in (None, here):
+            with pytest.raises(ValueError):
+                binding.chela_selscan_bwd(u, delta, A, Bm, Cm, dY, cu=cu, **dict(dict(stream=s), **bad))
     x1, x2 = u.clone(), u.clone()
     n1, n2 = torch.empty_like(u), torch.empty_like(u)
     a = binding.chela_block_norm_fwd(delta, x1, w_pre=g1, X_out=x1, Nrm=n1)
