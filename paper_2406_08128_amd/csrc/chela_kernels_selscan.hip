@@ -2,7 +2,7 @@
 //
 // Per channel c (of group g) and state n, with dl_t = softplus(delta_t + bias) or delta_t + bias:
 //     h_t[n] = exp(dl_t A[n]) h_{t-1}[n] + dl_t u_t B_t[n],   y_t = sum_n C_t[n] h_t[n] + D u_t,   out_t = y_t silu(z_t).
-// Gradient, with dy_t = dout_t silu(z_t), a_t[n] = exp(dl_t A[n]), q_t[n] = a_t[n] g_t[n] and p_t[n] = a_t[n] h_{t-1}[n]:
+// Gradient, with dy_t = dout_t silu(z_t), a_t[n] = exp(dl_t A[n]), q_t[n] = a_t[n] g_t[n] and p_t[n] = a_t[n] h_{t-1}[n], as the forward walk has them again:
 //     g_t[n] = C_t[n] dy_t + q_{t+1}[n]                             (the gradient of h_t)
 //     dC_t[n] = sum_c dy_t h_t[n],   dB_t[n] = sum_c g_t[n] dl_t u_t,   dA[n] = sum_t dl_t g_t[n] p_t[n],   dD = sum_t dy_t u_t
 //     du_t = dl_t sum_n g_t[n] B_t[n] + D dy_t,   d(dl_t) = u_t sum_n g_t[n] B_t[n] + sum_n A[n] g_t[n] p_t[n]
@@ -15,6 +15,11 @@
 // first pass leaves, per chunk, what its rows add to the state behind them (the state itself, if a sequence begins in it) and the sum
 // of its step sizes, of which the chunk's decay is exp(A sum); a second one makes the state in front of each chunk of these, and a third
 // walks the chunks.
+//
+// What bounds it is the vector ALU's issue.  A row of 16 states takes 48 operations and 16 exponentials in the first pass, 64 and 16 in the
+// third; alone, from registers, the latter keep a SIMD busy for 409 cycles (an operation 3, an exponential 12).  65536 rows in four sequences, 1536
+// channels, 16 states, bf16, us: first pass 304 (the issue's floor 224), third with its saved states 417 (262; 1.6 GB at 3.9 TB/s), gradient:
+// first pass 346, walk 1230, carries 25 and 16, sums of dB and dC over the channels' waves 59.
 #include "chela_rows.h"
 #include <type_traits>
 
@@ -709,7 +714,8 @@ __global__ __launch_bounds__(1024) void selscan_params_kernel(const float* __res
 }
 
 // ------------------------------------------------------------------------------------------------------------ single tokens
-// A wave has 64 channels of `each` requests: what a channel has once (16 decays, 4 KB a wave, as many bytes as its state) is read once.
+// A wave has 64 channels of `each` requests: what a channel has once (16 decays, 4 KB a wave, as many bytes as its state) is read once.  A request's
+// loads all come before its stores.  256 requests of 1536 channels, 16 states: 11.2 us, 4.8 TB/s of states read and written; one request 5.5.
 template <typename IO, int N>
 __global__ __launch_bounds__(64) void selscan_step_kernel(SelscanArgs a, int each)
 {
@@ -728,8 +734,11 @@ __global__ __launch_bounds__(64) void selscan_step_kernel(SelscanArgs a, int eac
         float* S = a.S_out + (size_t)slot * ND + ch;
         const IO *Bm = (const IO*)a.Bm + (size_t)r * a.ldb + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)r * a.ldc + (size_t)g * N;
         float h[N];
+        IO b[N], c[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) h[n] = S[(size_t)n * a.D];
+#pragma unroll
+        for (int n = 0; n < N; ++n) { b[n] = Bm[n]; c[n] = Cm[n]; }
         const float u = to_f(((const IO*)a.U)[(size_t)r * a.ldu + ch]);
         const float z = a.Z ? to_f(((const IO*)a.Z)[(size_t)r * a.ldz + ch]) : 0.f;
         float dl = to_f(((const IO*)a.delta)[(size_t)r * a.ldd + ch]) + bias;
@@ -737,10 +746,11 @@ __global__ __launch_bounds__(64) void selscan_step_kernel(SelscanArgs a, int eac
         float y = skip * u;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            h[n] = fmaf(exp2_(dl * A2[n]), h[n], dl * u * to_f(Bm[n]));
-            S[(size_t)n * a.D] = h[n];
-            y = fmaf(to_f(Cm[n]), h[n], y);
+            h[n] = fmaf(exp2_(dl * A2[n]), h[n], dl * u * to_f(b[n]));
+            y = fmaf(to_f(c[n]), h[n], y);
         }
+#pragma unroll
+        for (int n = 0; n < N; ++n) S[(size_t)n * a.D] = h[n];
         if (a.Z) y *= z * sigmoid_(z);
         ((IO*)a.Y)[(size_t)r * a.D + ch] = from_f<IO>(y);
     }
@@ -949,7 +959,7 @@ static hipError_t step(const SelscanArgs& a, hipStream_t st)
 {
     ProfScope prof(KID_SELSCAN_STEP, st);
     const long nb = (a.D + 63) / 64, R = a.rows.T;
-    // (256 requests, 1536 channels, for 1, 2, 4, 8 a wave: 8.7, 8.3, 9.2, 11.2 us; below four waves per SIMD one)
+    // (256 requests, 1536 channels, for 1, 2, 3 a wave: 12.3, 11.2, 11.9 us; below four waves per SIMD one)
     const int each = nb * R >= 4096 ? 2 : 1;
     hipLaunchKernelGGL((selscan_step_kernel<IO, N>), dim3((unsigned)(nb * ((R + each - 1) / each))), dim3(64), 0, st, a, each);
     return hipGetLastError();

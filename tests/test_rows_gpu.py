@@ -259,6 +259,31 @@ def test_selscan_many_chunks_pieces_and_single_tokens(dtype):
         check("S_out", S3[i], f["S_out"], mf["S_out"], 8 * L + 128)
 
 
+@pytest.mark.parametrize("lens", [[6700], [2300, 0, 4400]])
+def test_selscan_hundreds_of_chunks(lens):
+    # (so many that the carries take several rounds)
+    r, D, N, T, n = gen(89), 8, 8, sum(lens), len(lens)
+    u, delta, z, Bm, Cm, A, skip, bias = scan_inputs(r, T, D, N, 1, F32)
+    dY, S, dS = r(T, D), r(n, N, D), r(n, N, D)
+    kw = dict(D=skip, Z=z, delta_bias=bias - 3, cu=cu_of(lens), S_in=S)          # (steps small enough for states to last through chunks)
+    S_out = torch.empty_like(S)
+    Y, saved = binding.chela_selscan_fwd(u, delta, A, Bm, Cm, S_out=S_out, want_saved=True, **kw)
+    g = dict(zip(("dU", "ddelta", "dA", "dB", "dC", "dD", "dZ", "dbias", "dS_in"),
+                 binding.chela_selscan_bwd(u, delta, A, Bm, Cm, dY, dS_out=dS, want_dS_in=True, saved=saved, **kw)))
+    n64 = [f64(t) for t in (u, delta, z, Bm, Cm, A, skip, bias - 3)]
+    o, k = offsets(lens), 8 * max(lens) + 128
+    ref = scan_reference((*n64, True), f64(S), f64(dY), f64(dS), lens)
+    for i, ((f, mf), (v, mv)) in enumerate(ref):
+        rows = slice(o[i], o[i + 1])
+        check("Y", Y[rows], f["Y"], mf["Y"], k)
+        check("S_out", S_out[i], f["S_out"], mf["S_out"], k)
+        for name in ("dU", "ddelta", "dB", "dC", "dZ"):
+            check(name, g[name][rows], v[name], mv[name], 2 * k + D)
+        check("dS_in", g["dS_in"][i], v["dS_in"], mv["dS_in"], 2 * k)
+    for name in ("dA", "dD", "dbias"):
+        check(name, g[name], sum(p[1][0][name] for p in ref), sum(p[1][1][name] for p in ref), 2 * k + T)
+
+
 @pytest.mark.parametrize("N,G,D", [(16, 1, 64), (8, 2, 30), (32, 1, 200), (16, 4, 1000)])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_selscan_step_against_the_definition(dtype, N, G, D):
@@ -483,6 +508,11 @@ NORM = [  # rows, D, gate, w_post, w_pre, Y, fp32 stream
     (2100, 1100, True, True, True, True, False),
     (6, 768, False, False, True, False, False),
     (2, 300, False, False, True, False, True),
+    (5, 2, True, True, True, True, False),
+    (6, 3, True, True, True, True, True),
+    (3, 4095, True, True, True, True, True),
+    (2, 8190, True, True, True, True, False),
+    (2, 8191, True, True, True, True, True),
 ]
 
 

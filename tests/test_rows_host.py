@@ -22,9 +22,11 @@ def _differences(f, x, h=1e-6):
     return g
 
 
-def _close(a, b):
-    # central differences: truncation of the order h^2 = 1e-12, cancellation of the order 2^-52 / h = 2e-10, times the sums' size
-    assert np.allclose(a, b, rtol=1e-6, atol=1e-7), np.abs(a - b).max()
+def _close(a, b, size=0.0, h=1e-6):
+    # central differences: truncation of the order h^2 = 1e-12; and each of the two values whose difference is divided by 2 h has at most 168
+    # roundings (8 a row, 128 on top) of its terms' magnitudes, `size`.  (Without softplus half of the step sizes are negative and states
+    # grow: at a size of 5e9 a difference of two values, whose last digit alone is 1e-6, says nothing about less than 1.)
+    assert np.allclose(a, b, rtol=1e-6, atol=1e-7 + 168 * 2.0 ** -53 * size / h), np.abs(a - b).max()
 
 
 @pytest.mark.parametrize("act", [True, False])
@@ -57,11 +59,13 @@ def test_selscan_gradient_against_differences(rng, softplus, full, L):
         v, _ = R.selscan_fwd(u, delta, A, Bm, Cm, skip, z, b, softplus, s)
         return (v["Y"] * dY).sum() + (v["S_out"] * ds).sum()
 
+    f = R.selscan_fwd(u, delta, A, Bm, Cm, skip, z, b, softplus, s)[1]
+    size = (f["Y"] * np.abs(dY)).sum() + (f["S_out"] * np.abs(ds)).sum()
     v, mass = R.selscan_bwd(u, delta, A, Bm, Cm, dY, skip, z, b, softplus, s, ds)
     for k, t in (("dU", u), ("ddelta", delta), ("dA", A), ("dB", Bm), ("dC", Cm), ("dD", skip), ("dZ", z), ("dbias", b), ("dS_in", s)):
         if t is None:
             continue
-        _close(v[k], _differences(loss, t))
+        _close(v[k], _differences(loss, t), size)
         assert (np.abs(v[k]) <= mass[k] * (1 + 1e-12) + 1e-15).all(), k
 
 
