@@ -400,7 +400,7 @@ size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int
  *     Nrm   = Norm(X_out) * w_pre                       (w_pre NULL: not wanted, Nrm is not looked at)
  * with Norm(x) = x / sqrt(mean_j x_j^2 + eps) as defined above, over the row; eps >= 0 and scale are finite constants.  Y is the
  * block's output, X the residual stream, Nrm the next block's input.  Y NULL (in front of the first block; gate, w_post and X_out are
- * then not looked at): Nrm = Norm(X) * w_pre.  The second norm takes X_out before it is rounded.
+ * then not looked at): Nrm = Norm(X) * w_pre.  The second norm takes X_out before it is rounded.  Squares and their mean are fp32.
  *   Y, gate, Nrm: bf16 (plain name) or fp32 (_f32); X, X_out: the same, or fp32 beside bf16 (x_f32 != 0).  w_post, w_pre [D] fp32.
  *   X_out may be X (exactly the same pointer).
  *   bwd: from Y, gate and X, the stream as the forward call left it (its X_out; with Y NULL its X), for the upstream gradients dX_out (type
