@@ -314,11 +314,12 @@ int chela_linattn_step_gated(const void *q, const void *k, const void *v, const 
  *   sequences: the T rows belong to n_seq sequences, one after the other.  cu NULL: of T / n_seq rows each.  Otherwise cu is
  *              n_seq + 1 ascending int32 offsets on the device, sequence s has rows cu[s] .. cu[s+1] - 1, none is an empty
  *              sequence; rows in front of cu[0] and from cu[n_seq] on belong to nobody: they are not computed, and what the
- *              outputs hold there stays.  (Offsets outside [0, T] or not ascending give unspecified values in the outputs, nothing else.)
+ *              outputs hold there stays; the calls named _cleared write zeros there (for outputs in new memory: nobody's rows have a gradient
+ *              of zero).  (Offsets outside [0, T] or not ascending give unspecified values in the outputs, nothing else.)
  *   states   : what a sequence takes from the tokens in front of it (S_in, NULL: none) and hands to those behind it (S_out, NULL:
  *              not wanted).  slots NULL: sequence s has the s-th of n_slots = n_seq states.  Otherwise slots is n_seq int32
  *              on the device, sequence s has state slots[s] of a pool of n_slots; a sequence whose slot is not in [0, n_slots)
- *              begins with nothing and leaves nothing, and in the single-token calls its output row is left as it is.  Two
+ *              begins with nothing and leaves nothing, and in the single-token calls its output row is left as it is (_cleared: zeroed).  Two
  *              sequences of one call must not share a slot (their states would be unspecified).  S_out may be S_in (exactly
  *              the same pointer); states of slots that no sequence has are not touched.  An empty sequence hands its state on.
  * Limits: D <= 2^20; T ceil(D / 64) < 2^28; n_seq ceil(D / 64) and R ceil(D / 64) < 2^23.  With T = 0 nothing is done but
@@ -349,6 +350,24 @@ int chela_short_conv_step(const void *x, long long ldx, const float *w, int m, c
                           const int *slots, int n_slots, int R, int D, void *y, void *stream);
 int chela_short_conv_step_f32(const void *x, long long ldx, const float *w, int m, const float *bias, int silu, void *S,
                               const int *slots, int n_slots, int R, int D, void *y, void *stream);
+int chela_short_conv_fwd_cleared(const void *X, long long ldx, const float *w, int m, const float *bias, int silu,
+                                 const int *cu, int n_seq, int T, int D, const void *S_in, void *S_out,
+                                 const int *slots, int n_slots, void *Y, void *stream);
+int chela_short_conv_fwd_cleared_f32(const void *X, long long ldx, const float *w, int m, const float *bias, int silu,
+                                     const int *cu, int n_seq, int T, int D, const void *S_in, void *S_out,
+                                     const int *slots, int n_slots, void *Y, void *stream);
+int chela_short_conv_bwd_cleared(const void *X, long long ldx, const float *w, int m, const float *bias, int silu,
+                                 const int *cu, int n_seq, int T, int D, const void *S_in, const void *dY,
+                                 long long lddy, const void *dS_out, void *dX, float *dw, float *dbias, void *dS_in,
+                                 void *stream);
+int chela_short_conv_bwd_cleared_f32(const void *X, long long ldx, const float *w, int m, const float *bias, int silu,
+                                     const int *cu, int n_seq, int T, int D, const void *S_in, const void *dY,
+                                     long long lddy, const void *dS_out, void *dX, float *dw, float *dbias,
+                                     void *dS_in, void *stream);
+int chela_short_conv_step_cleared(const void *x, long long ldx, const float *w, int m, const float *bias, int silu,
+                                  void *S, const int *slots, int n_slots, int R, int D, void *y, void *stream);
+int chela_short_conv_step_cleared_f32(const void *x, long long ldx, const float *w, int m, const float *bias, int silu,
+                                      void *S, const int *slots, int n_slots, int R, int D, void *y, void *stream);
 size_t chela_short_conv_bwd_workspace_bytes(int T, int D, int m, int dtype);
 
 /* Selective scan: a state of N values per channel (N in {8, 16, 32}), whose decay, input and output maps depend on the token.
@@ -390,6 +409,37 @@ int chela_selscan_step_f32(const void *u, long long ldu, const void *delta, long
                            long long ldb, const void *Cm, long long ldc, const float *Dskip, const void *z, long long ldz,
                            const float *delta_bias, int softplus, float *S, const int *slots, int n_slots, int R, int D, int N,
                            int G, void *y, void *stream);
+int chela_selscan_fwd_cleared(const void *U, long long ldu, const void *delta, long long ldd, const float *A,
+                              const void *Bm, long long ldb, const void *Cm, long long ldc, const float *Dskip,
+                              const void *Z, long long ldz, const float *delta_bias, int softplus, const int *cu,
+                              int n_seq, int T, int D, int N, int G, const float *S_in, float *S_out, const int *slots,
+                              int n_slots, void *Y, void *saved, void *stream);
+int chela_selscan_fwd_cleared_f32(const void *U, long long ldu, const void *delta, long long ldd, const float *A,
+                                  const void *Bm, long long ldb, const void *Cm, long long ldc, const float *Dskip,
+                                  const void *Z, long long ldz, const float *delta_bias, int softplus, const int *cu,
+                                  int n_seq, int T, int D, int N, int G, const float *S_in, float *S_out,
+                                  const int *slots, int n_slots, void *Y, void *saved, void *stream);
+int chela_selscan_bwd_cleared(const void *U, long long ldu, const void *delta, long long ldd, const float *A,
+                              const void *Bm, long long ldb, const void *Cm, long long ldc, const float *Dskip,
+                              const void *Z, long long ldz, const float *delta_bias, int softplus, const int *cu,
+                              int n_seq, int T, int D, int N, int G, const float *S_in, const void *dY, long long lddy,
+                              const float *dS_out, const void *saved, void *dU, void *ddelta, float *dA, void *dB,
+                              void *dC, float *dDskip, void *dZ, float *ddelta_bias, float *dS_in, void *stream);
+int chela_selscan_bwd_cleared_f32(const void *U, long long ldu, const void *delta, long long ldd, const float *A,
+                                  const void *Bm, long long ldb, const void *Cm, long long ldc, const float *Dskip,
+                                  const void *Z, long long ldz, const float *delta_bias, int softplus, const int *cu,
+                                  int n_seq, int T, int D, int N, int G, const float *S_in, const void *dY,
+                                  long long lddy, const float *dS_out, const void *saved, void *dU, void *ddelta,
+                                  float *dA, void *dB, void *dC, float *dDskip, void *dZ, float *ddelta_bias,
+                                  float *dS_in, void *stream);
+int chela_selscan_step_cleared(const void *u, long long ldu, const void *delta, long long ldd, const float *A,
+                               const void *Bm, long long ldb, const void *Cm, long long ldc, const float *Dskip,
+                               const void *z, long long ldz, const float *delta_bias, int softplus, float *S,
+                               const int *slots, int n_slots, int R, int D, int N, int G, void *y, void *stream);
+int chela_selscan_step_cleared_f32(const void *u, long long ldu, const void *delta, long long ldd, const float *A,
+                                   const void *Bm, long long ldb, const void *Cm, long long ldc, const float *Dskip,
+                                   const void *z, long long ldz, const float *delta_bias, int softplus, float *S,
+                                   const int *slots, int n_slots, int R, int D, int N, int G, void *y, void *stream);
 size_t chela_selscan_saved_bytes(int T, int D, int N);
 /* is_bwd: of the backward call; has_saved: given `saved`. */
 size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int has_saved);

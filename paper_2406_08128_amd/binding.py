@@ -36,7 +36,9 @@ _fn = dict.fromkeys(("linattn_fwd", "linattn_fwd_f32", "linattn_fwd_state", "lin
                      "shortlong_conv_fwd_f32", "shortlong_conv_bwd", "shortlong_conv_bwd_f32", "short_conv_fwd", "short_conv_fwd_f32",
                      "short_conv_step", "short_conv_step_f32", "selscan_fwd", "selscan_fwd_f32", "selscan_step", "selscan_step_f32",
                      "selscan_saved_bytes", "block_norm_fwd", "block_norm_fwd_f32", "short_conv_bwd", "short_conv_bwd_f32", "selscan_bwd",
-                     "selscan_bwd_f32", "block_norm_bwd", "block_norm_bwd_f32"), 0)
+                     "selscan_bwd_f32", "block_norm_bwd", "block_norm_bwd_f32",
+                     *("%s_%s_cleared%s" % (op, call, sfx) for op in ("short_conv", "selscan") for call in ("fwd", "bwd", "step")
+                       for sfx in ("", "_f32"))), 0)
 
 
 class ChelaError(RuntimeError):
@@ -136,9 +138,10 @@ def lib() -> ctypes.CDLL:
                            ("chela_selscan_step", scan + [vp, vp, i, i, i, i, i, vp, vp]),
                            ("chela_block_norm_fwd", [vp] * 7 + [f32, f32, ll, i, i, vp]),
                            ("chela_block_norm_bwd", [vp] * 12 + [f32, f32, ll, i, i, vp])):
-            f = getattr(L, name + sfx)
-            f.argtypes = args
-            f.restype = i
+            for form in ("",) if "norm" in name else ("", "_cleared"):
+                f = getattr(L, name + form + sfx)
+                f.argtypes = args
+                f.restype = i
     L.chela_short_conv_bwd_workspace_bytes.argtypes = [i, i, i, i]
     L.chela_selscan_saved_bytes.argtypes = [i, i, i]
     L.chela_selscan_workspace_bytes.argtypes = [i] * 6
@@ -789,6 +792,8 @@ def chela_linattn_step_gated(q, k, v, g, S, eps, y=None, stream=None):
 
 # ---- operators on rows: X [B, L, D] (B sequences of L tokens), or [T, D] with cu, the n_seq + 1 offsets of the sequences (int32, on the
 # device; None: one sequence).  Rows may be slices of a wider tensor: the last dimension has stride 1, the rows one stride.
+# Rows in front of the first offset and behind the last are nobody's: in an output that the call allocates they are zero, one that it is
+# given keeps what it holds there.
 
 def _row_stride(t, like, name, dtype=None):
     """(address, elements from a row to the next) of a tensor of rows with like's leading sizes."""
@@ -846,8 +851,10 @@ def _slot_map(slots, n_seq, states, device):
 
 def chela_short_conv_fwd(X, w, bias=None, silu=True, cu=None, S_in=None, S_out=None, slots=None, Y=None, stream=None):
     """Y = silu(bias + sum_j w[:, j] X[t - j]) over the tokens of each sequence (silu=False: without the activation).
-    w [D, m], bias [D] float32; S_in, S_out [n_slots, m-1, D] the last inputs in front of and behind the sequences (S_out may be S_in)."""
-    r = _host("short_conv_fwd")(_fn["short_conv_fwd"], _fn["short_conv_fwd_f32"], X, w, bias, silu, cu, S_in, S_out, slots, Y, stream)
+    w [D, m], bias [D] float32; S_in, S_out [n_slots, m-1, D] the last inputs in front of and behind the sequences (S_out may be S_in).
+    Rows of no sequence: zero in a new Y, left as they are in one that is given."""
+    name = "short_conv_fwd" if cu is None or Y is not None else "short_conv_fwd_cleared"
+    r = _host("short_conv_fwd")(_fn[name], _fn[name + "_f32"], X, w, bias, silu, cu, S_in, S_out, slots, Y, stream)
     if r is not None:
         return _host_result(r)
     pcu, n_seq, T, D = _sequences(X, cu, "X")
@@ -861,7 +868,7 @@ def chela_short_conv_fwd(X, w, bias=None, silu=True, cu=None, S_in=None, S_out=N
         Y = torch.empty(X.shape, dtype=X.dtype, device=dev)
     st = (n_slots, m - 1, D)
     with _on(X):
-        _check(getattr(lib(), "chela_short_conv_fwd" + sfx)(
+        _check(getattr(lib(), "chela_" + name + sfx)(
             px, ldx, _dense(w, (D, m), torch.float32, dev, "w"), m, _dense(bias, (D,), torch.float32, dev, "bias"), int(bool(silu)), pcu,
             n_seq, T, D, _dense(S_in, st, X.dtype, dev, "S_in"), _dense(S_out, st, X.dtype, dev, "S_out"), pslots, n_slots,
             _dense(Y, X.shape, X.dtype, dev, "Y"), _stream_ptr(stream)))
@@ -870,8 +877,9 @@ def chela_short_conv_fwd(X, w, bias=None, silu=True, cu=None, S_in=None, S_out=N
 
 def chela_short_conv_bwd(X, w, dY, bias=None, silu=True, cu=None, S_in=None, dS_out=None, want_dS_in=False, stream=None):
     """(dX, dw, dbias, dS_in) of chela_short_conv_fwd (without slots) for the upstream gradients dY and dS_out; dbias is None without a
-    bias, dS_in unless asked for."""
-    r = _host("short_conv_bwd")(_fn["short_conv_bwd"], _fn["short_conv_bwd_f32"], X, w, dY, bias, silu, cu, S_in, dS_out, want_dS_in, stream)
+    bias, dS_in unless asked for.  dX is zero in rows of no sequence."""
+    name = "short_conv_bwd" if cu is None else "short_conv_bwd_cleared"
+    r = _host("short_conv_bwd")(_fn[name], _fn[name + "_f32"], X, w, dY, bias, silu, cu, S_in, dS_out, want_dS_in, stream)
     if r is not None:
         return _host_result(r)
     pcu, n_seq, T, D = _sequences(X, cu, "X")
@@ -891,7 +899,7 @@ def chela_short_conv_bwd(X, w, dY, bias=None, silu=True, cu=None, S_in=None, dS_
     dbias = torch.empty(D, dtype=torch.float32, device=dev) if bias is not None else None
     dS_in = torch.empty(st, dtype=X.dtype, device=dev) if want_dS_in else None
     with _on(X):
-        _check(getattr(lib(), "chela_short_conv_bwd" + sfx)(
+        _check(getattr(lib(), "chela_" + name + sfx)(
             px, ldx, pw, m, pb, int(bool(silu)), pcu, n_seq, T, D, ps, pdy, lddy, pds, dX.data_ptr(), dw.data_ptr(), _ptr(dbias),
             _ptr(dS_in), _stream_ptr(stream)))
     return dX, dw, dbias, dS_in
@@ -899,8 +907,9 @@ def chela_short_conv_bwd(X, w, dY, bias=None, silu=True, cu=None, S_in=None, dS_
 
 def chela_short_conv_step(x, w, S, bias=None, silu=True, slots=None, y=None, stream=None):
     """One token for each of R requests, x [R, D]: y as chela_short_conv_fwd's, the states S [n_slots, m-1, D] move on in place.  A row
-    whose slot is not one of S's is left out: y keeps what it holds there."""
-    r = _host("short_conv_step")(_fn["short_conv_step"], _fn["short_conv_step_f32"], x, w, S, bias, silu, slots, y, stream)
+    whose slot is not one of S's is left out: y keeps what it holds there, a new y is zero."""
+    name = "short_conv_step" if slots is None or y is not None else "short_conv_step_cleared"
+    r = _host("short_conv_step")(_fn[name], _fn[name + "_f32"], x, w, S, bias, silu, slots, y, stream)
     if r is not None:
         return _host_result(r)
     if not x.is_cuda or x.dim() != 2 or w.dim() != 2:
@@ -913,7 +922,7 @@ def chela_short_conv_step(x, w, S, bias=None, silu=True, slots=None, y=None, str
     if y is None:
         y = torch.empty((R, D), dtype=x.dtype, device=dev)
     with _on(x):
-        _check(getattr(lib(), "chela_short_conv_step" + sfx)(
+        _check(getattr(lib(), "chela_" + name + sfx)(
             px, ldx, _dense(w, (D, m), torch.float32, dev, "w"), m, _dense(bias, (D,), torch.float32, dev, "bias"), int(bool(silu)),
             _dense(S, (n_slots, m - 1, D), x.dtype, dev, "S"), pslots, n_slots, R, D, _dense(y, (R, D), x.dtype, dev, "y"),
             _stream_ptr(stream)))
@@ -947,8 +956,10 @@ def chela_selscan_fwd(U, delta, A, Bm, Cm, D=None, Z=None, delta_bias=None, soft
                       want_saved=False, Y=None, stream=None):
     """(Y, saved): the selective scan h[n] = exp(dl A[n]) h[n] + dl u B[n], y = sum_n C[n] h[n] + D u, gated with silu(Z), with
     dl = softplus(delta + delta_bias).  A [N, D], D and delta_bias [D] float32; Bm, Cm [..., G, N] or [..., N]; states [n_slots, N, D]
-    float32.  saved is None unless asked for (for chela_selscan_bwd)."""
-    r = _host("selscan_fwd")(_fn["selscan_fwd"], _fn["selscan_fwd_f32"], _fn["selscan_saved_bytes"], U, delta, A, Bm, Cm, D, Z, delta_bias,
+    float32.  saved is None unless asked for (for chela_selscan_bwd).  Rows of no sequence: zero in a new Y, left as they are in one that
+    is given."""
+    name = "selscan_fwd" if cu is None or Y is not None else "selscan_fwd_cleared"
+    r = _host("selscan_fwd")(_fn[name], _fn[name + "_f32"], _fn["selscan_saved_bytes"], U, delta, A, Bm, Cm, D, Z, delta_bias,
                              softplus, cu, S_in, S_out, slots, want_saved, Y, stream)
     if r is not None:
         return _host_result(r)
@@ -965,7 +976,7 @@ def chela_selscan_fwd(U, delta, A, Bm, Cm, D=None, Z=None, delta_bias=None, soft
     if want_saved:
         saved = torch.empty(max(chela_selscan_saved_bytes(T, width, N), 16) // 4, dtype=torch.float32, device=dev)
     with _on(U):
-        _check(getattr(lib(), "chela_selscan_fwd" + sfx)(
+        _check(getattr(lib(), "chela_" + name + sfx)(
             *args, pcu, n_seq, T, width, N, G, ps_in, ps_out, pslots, n_slots, _dense(Y, U.shape, U.dtype, dev, "Y"), _ptr(saved),
             _stream_ptr(stream)))
     return Y, saved
@@ -974,8 +985,10 @@ def chela_selscan_fwd(U, delta, A, Bm, Cm, D=None, Z=None, delta_bias=None, soft
 def chela_selscan_bwd(U, delta, A, Bm, Cm, dY, D=None, Z=None, delta_bias=None, softplus=True, cu=None, S_in=None, dS_out=None,
                       want_dS_in=False, saved=None, stream=None):
     """(dU, ddelta, dA, dB, dC, dD, dZ, ddelta_bias, dS_in) of chela_selscan_fwd (without slots) for the upstream gradients dY and dS_out;
-    None for what there is no input of, dS_in unless asked for.  saved: the forward call's on the same inputs, or None."""
-    r = _host("selscan_bwd")(_fn["selscan_bwd"], _fn["selscan_bwd_f32"], _fn["selscan_saved_bytes"], U, delta, A, Bm, Cm, dY, D, Z, delta_bias,
+    None for what there is no input of, dS_in unless asked for.  saved: the forward call's on the same inputs, or None.  Gradients of rows
+    of no sequence are zero."""
+    name = "selscan_bwd" if cu is None else "selscan_bwd_cleared"
+    r = _host("selscan_bwd")(_fn[name], _fn[name + "_f32"], _fn["selscan_saved_bytes"], U, delta, A, Bm, Cm, dY, D, Z, delta_bias,
                              softplus, cu, S_in, dS_out, want_dS_in, saved, stream)
     if r is not None:
         return _host_result(r)
@@ -998,7 +1011,7 @@ def chela_selscan_bwd(U, delta, A, Bm, Cm, dY, D=None, Z=None, delta_bias=None, 
     dU, ddelta, dA, dB, dC, dD, dZ, dbias = (like(t) for t in (U, delta, A, Bm, Cm, D, Z, delta_bias))
     dS_in = torch.empty(st, dtype=torch.float32, device=dev) if want_dS_in else None
     with _on(U):
-        _check(getattr(lib(), "chela_selscan_bwd" + sfx)(
+        _check(getattr(lib(), "chela_" + name + sfx)(
             *args, pcu, n_seq, T, width, N, G, ps, pdy, lddy, pds, _ptr(saved), dU.data_ptr(), ddelta.data_ptr(), dA.data_ptr(),
             dB.data_ptr(), dC.data_ptr(), _ptr(dD), _ptr(dZ), _ptr(dbias), _ptr(dS_in), _stream_ptr(stream)))
     return dU, ddelta, dA, dB, dC, dD, dZ, dbias, dS_in
@@ -1006,8 +1019,9 @@ def chela_selscan_bwd(U, delta, A, Bm, Cm, dY, D=None, Z=None, delta_bias=None, 
 
 def chela_selscan_step(u, delta, A, Bm, Cm, S, D=None, z=None, delta_bias=None, softplus=True, slots=None, y=None, stream=None):
     """One token for each of R requests, u [R, D]: y as chela_selscan_fwd's, the states S [n_slots, N, D] are updated in place.  A row
-    whose slot is not one of S's is left out: y keeps what it holds there."""
-    r = _host("selscan_step")(_fn["selscan_step"], _fn["selscan_step_f32"], u, delta, A, Bm, Cm, S, D, z, delta_bias, softplus, slots, y, stream)
+    whose slot is not one of S's is left out: y keeps what it holds there, a new y is zero."""
+    name = "selscan_step" if slots is None or y is not None else "selscan_step_cleared"
+    r = _host("selscan_step")(_fn[name], _fn[name + "_f32"], u, delta, A, Bm, Cm, S, D, z, delta_bias, softplus, slots, y, stream)
     if r is not None:
         return _host_result(r)
     if not u.is_cuda or u.dim() != 2:
@@ -1020,7 +1034,7 @@ def chela_selscan_step(u, delta, A, Bm, Cm, S, D=None, z=None, delta_bias=None, 
     if y is None:
         y = torch.empty((R, width), dtype=u.dtype, device=dev)
     with _on(u):
-        _check(getattr(lib(), "chela_selscan_step" + sfx)(
+        _check(getattr(lib(), "chela_" + name + sfx)(
             *args, _dense(S, (n_slots, N, width), torch.float32, dev, "S"), pslots, n_slots, R, width, N, G,
             _dense(y, (R, width), u.dtype, dev, "y"), _stream_ptr(stream)))
     return y

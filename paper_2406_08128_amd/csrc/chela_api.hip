@@ -1318,14 +1318,14 @@ struct Operands {
 static bool too_many(int rows, int D, long long units) { return (long long)rows * ((D + 63) / 64) >= units; }
 constexpr long long kRowUnits = 1ll << 28, kStateUnits = 1ll << 23;
 // The sequences that T rows belong to, as a call names them.
-static int rows_of(const int* cu, int n_seq, int T, int D, const int* slots, int n_slots, Rows* out)
+static int rows_of(const int* cu, int n_seq, int T, int D, const int* slots, int n_slots, bool clear, Rows* out)
 {
     if (T < 0 || n_seq < 0 || D < 0 || D > (1 << 20) || n_slots < 0 || T >= kRowUnits || n_seq >= kStateUnits) return CHELA_ERR_BAD_SHAPE;
     if (too_many(T, D, kRowUnits) || too_many(n_seq, D, kStateUnits)) return CHELA_ERR_BAD_SHAPE;
     if (cu == nullptr && T > 0 && (n_seq == 0 || T % n_seq != 0)) return CHELA_ERR_BAD_SHAPE;
     if (slots == nullptr && n_slots != n_seq) return CHELA_ERR_BAD_SHAPE;
     if (((uintptr_t)cu | (uintptr_t)slots) & 3u) return CHELA_ERR_MISALIGNED;
-    *out = Rows{cu, slots, n_seq, n_slots, T, cu == nullptr && n_seq > 0 ? T / n_seq : 0};
+    *out = Rows{cu, slots, n_seq, n_slots, T, cu == nullptr && n_seq > 0 ? T / n_seq : 0, clear};
     return CHELA_OK;
 }
 static int status_of(hipError_t e) { return e == hipSuccess ? CHELA_OK : CHELA_ERR_HIP; }
@@ -1333,11 +1333,12 @@ static size_t esize(int dtype) { return dtype == CHELA_DTYPE_BF16 ? 2 : 4; }
 static int kind(int dtype) { return dtype == CHELA_DTYPE_BF16 ? 0 : 1; }
 
 static int short_conv_common(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,
-                             int T, int D, const void* S_in, void* S_out, const int* slots, int n_slots, void* Y, int dtype, void* stream)
+                             int T, int D, const void* S_in, void* S_out, const int* slots, int n_slots, void* Y, int dtype, bool clear,
+                             void* stream)
 {
     ShortConvArgs a{};
     if (m < 1 || m > kShortConvMaxTaps) return CHELA_ERR_BAD_SHAPE;
-    int rc = rows_of(cu, n_seq, T, D, slots, n_slots, &a.rows);
+    int rc = rows_of(cu, n_seq, T, D, slots, n_slots, clear, &a.rows);
     if (rc != CHELA_OK) return rc;
     if (D == 0 || (T == 0 && n_seq == 0)) return CHELA_OK;
     if (m == 1) S_in = S_out = nullptr;
@@ -1356,18 +1357,6 @@ static int short_conv_common(const void* X, long long ldx, const float* w, int m
     return status_of(launch_short_conv_fwd(a, kind(dtype), (hipStream_t)stream));
 }
 
-int chela_short_conv_fwd(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq, int T,
-                         int D, const void* S_in, void* S_out, const int* slots, int n_slots, void* Y, void* stream)
-{
-    return short_conv_common(X, ldx, w, m, bias, silu, cu, n_seq, T, D, S_in, S_out, slots, n_slots, Y, CHELA_DTYPE_BF16, stream);
-}
-
-int chela_short_conv_fwd_f32(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,
-                             int T, int D, const void* S_in, void* S_out, const int* slots, int n_slots, void* Y, void* stream)
-{
-    return short_conv_common(X, ldx, w, m, bias, silu, cu, n_seq, T, D, S_in, S_out, slots, n_slots, Y, CHELA_DTYPE_F32, stream);
-}
-
 size_t chela_short_conv_bwd_workspace_bytes(int T, int D, int m, int dtype)
 {
     if (T < 0 || D <= 0 || D > (1 << 20) || too_many(T, D, kRowUnits) || m < 1 || m > kShortConvMaxTaps ||
@@ -1377,11 +1366,11 @@ size_t chela_short_conv_bwd_workspace_bytes(int T, int D, int m, int dtype)
 
 static int short_conv_bwd_common(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,
                                  int T, int D, const void* S_in, const void* dY, long long lddy, const void* dS_out, void* dX, float* dw,
-                                 float* dbias, void* dS_in, int dtype, void* stream)
+                                 float* dbias, void* dS_in, int dtype, bool clear, void* stream)
 {
     ShortConvArgs a{};
     if (m < 1 || m > kShortConvMaxTaps) return CHELA_ERR_BAD_SHAPE;
-    int rc = rows_of(cu, n_seq, T, D, nullptr, n_seq, &a.rows);
+    int rc = rows_of(cu, n_seq, T, D, nullptr, n_seq, clear, &a.rows);
     if (rc != CHELA_OK) return rc;
     if (D == 0) return CHELA_OK;
     if (m == 1) { S_in = dS_out = nullptr; dS_in = nullptr; }
@@ -1407,28 +1396,12 @@ static int short_conv_bwd_common(const void* X, long long ldx, const float* w, i
     return status_of(launch_short_conv_bwd(a, kind(dtype), (hipStream_t)stream));
 }
 
-int chela_short_conv_bwd(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq, int T,
-                         int D, const void* S_in, const void* dY, long long lddy, const void* dS_out, void* dX, float* dw, float* dbias,
-                         void* dS_in, void* stream)
-{
-    return short_conv_bwd_common(X, ldx, w, m, bias, silu, cu, n_seq, T, D, S_in, dY, lddy, dS_out, dX, dw, dbias, dS_in,
-                                 CHELA_DTYPE_BF16, stream);
-}
-
-int chela_short_conv_bwd_f32(const void* X, long long ldx, const float* w, int m, const float* bias, int silu, const int* cu, int n_seq,
-                             int T, int D, const void* S_in, const void* dY, long long lddy, const void* dS_out, void* dX, float* dw,
-                             float* dbias, void* dS_in, void* stream)
-{
-    return short_conv_bwd_common(X, ldx, w, m, bias, silu, cu, n_seq, T, D, S_in, dY, lddy, dS_out, dX, dw, dbias, dS_in,
-                                 CHELA_DTYPE_F32, stream);
-}
-
 static int short_conv_step_common(const void* x, long long ldx, const float* w, int m, const float* bias, int silu, void* S,
-                                  const int* slots, int n_slots, int R, int D, void* y, int dtype, void* stream)
+                                  const int* slots, int n_slots, int R, int D, void* y, int dtype, bool clear, void* stream)
 {
     ShortConvArgs a{};
     if (m < 1 || m > kShortConvMaxTaps || R < 0) return CHELA_ERR_BAD_SHAPE;
-    int rc = rows_of(nullptr, R, R, D, slots, n_slots, &a.rows);
+    int rc = rows_of(nullptr, R, R, D, slots, n_slots, clear, &a.rows);
     if (rc != CHELA_OK) return rc;
     if (R == 0 || D == 0) return CHELA_OK;
     const size_t es = esize(dtype);
@@ -1444,17 +1417,29 @@ static int short_conv_step_common(const void* x, long long ldx, const float* w, 
     return status_of(launch_short_conv_step(a, kind(dtype), (hipStream_t)stream));
 }
 
-int chela_short_conv_step(const void* x, long long ldx, const float* w, int m, const float* bias, int silu, void* S, const int* slots,
-                          int n_slots, int R, int D, void* y, void* stream)
-{
-    return short_conv_step_common(x, ldx, w, m, bias, silu, S, slots, n_slots, R, D, y, CHELA_DTYPE_BF16, stream);
-}
-
-int chela_short_conv_step_f32(const void* x, long long ldx, const float* w, int m, const float* bias, int silu, void* S, const int* slots,
-                              int n_slots, int R, int D, void* y, void* stream)
-{
-    return short_conv_step_common(x, ldx, w, m, bias, silu, S, slots, n_slots, R, D, y, CHELA_DTYPE_F32, stream);
-}
+#define CHELA_SHORT_CONV_IN const void *X, long long ldx, const float *w, int m, const float *bias, int silu
+#define CHELA_SHORT_CONV(FORM, SUFFIX, TYPE, CLEAR)                                                                   \
+    int chela_short_conv_fwd##FORM##SUFFIX(CHELA_SHORT_CONV_IN, const int* cu, int n_seq, int T, int D, const void* S_in, void* S_out, \
+                                           const int* slots, int n_slots, void* Y, void* stream)                      \
+    {                                                                                                                 \
+        return short_conv_common(X, ldx, w, m, bias, silu, cu, n_seq, T, D, S_in, S_out, slots, n_slots, Y, TYPE, CLEAR, stream); \
+    }                                                                                                                 \
+    int chela_short_conv_bwd##FORM##SUFFIX(CHELA_SHORT_CONV_IN, const int* cu, int n_seq, int T, int D, const void* S_in, const void* dY, \
+                                           long long lddy, const void* dS_out, void* dX, float* dw, float* dbias, void* dS_in, void* stream) \
+    {                                                                                                                 \
+        return short_conv_bwd_common(X, ldx, w, m, bias, silu, cu, n_seq, T, D, S_in, dY, lddy, dS_out, dX, dw, dbias, dS_in, TYPE, CLEAR, \
+                                     stream);                                                                         \
+    }                                                                                                                 \
+    int chela_short_conv_step##FORM##SUFFIX(CHELA_SHORT_CONV_IN, void* S, const int* slots, int n_slots, int R, int D, void* y, void* stream) \
+    {                                                                                                                 \
+        return short_conv_step_common(X, ldx, w, m, bias, silu, S, slots, n_slots, R, D, y, TYPE, CLEAR, stream);     \
+    }
+CHELA_SHORT_CONV(, , CHELA_DTYPE_BF16, false)
+CHELA_SHORT_CONV(, _f32, CHELA_DTYPE_F32, false)
+CHELA_SHORT_CONV(_cleared, , CHELA_DTYPE_BF16, true)
+CHELA_SHORT_CONV(_cleared, _f32, CHELA_DTYPE_F32, true)
+#undef CHELA_SHORT_CONV
+#undef CHELA_SHORT_CONV_IN
 
 static bool selscan_dims(int D, int N, int G) { return selscan_states_ok(N) && G >= 1 && D >= 0 && D % G == 0; }
 
@@ -1496,12 +1481,12 @@ static void selscan_read(const SelscanIn& x, int T, size_t es, Operands* o, Sels
 }
 
 static int selscan_fwd_common(const SelscanIn& x, const int* cu, int n_seq, int T, const float* S_in, float* S_out, const int* slots,
-                              int n_slots, void* Y, void* saved, int dtype, void* stream)
+                              int n_slots, void* Y, void* saved, int dtype, bool clear, void* stream)
 {
     SelscanArgs a{};
     if (!selscan_states_ok(x.N)) return CHELA_ERR_UNSUPPORTED_DIM;
     if (!selscan_dims(x.D, x.N, x.G)) return CHELA_ERR_BAD_SHAPE;
-    int rc = rows_of(cu, n_seq, T, x.D, slots, n_slots, &a.rows);
+    int rc = rows_of(cu, n_seq, T, x.D, slots, n_slots, clear, &a.rows);
     if (rc != CHELA_OK) return rc;
     if (x.D == 0 || (T == 0 && n_seq == 0)) return CHELA_OK;
     const size_t es = esize(dtype), st = (size_t)n_slots * x.N * x.D * 4;
@@ -1521,12 +1506,12 @@ static int selscan_fwd_common(const SelscanIn& x, const int* cu, int n_seq, int 
 
 static int selscan_bwd_common(const SelscanIn& x, const int* cu, int n_seq, int T, const float* S_in, const void* dY, long long lddy,
                               const float* dS_out, const void* saved, void* dU, void* ddelta, float* dA, void* dB, void* dC, float* dDskip,
-                              void* dZ, float* ddelta_bias, float* dS_in, int dtype, void* stream)
+                              void* dZ, float* ddelta_bias, float* dS_in, int dtype, bool clear, void* stream)
 {
     SelscanArgs a{};
     if (!selscan_states_ok(x.N)) return CHELA_ERR_UNSUPPORTED_DIM;
     if (!selscan_dims(x.D, x.N, x.G)) return CHELA_ERR_BAD_SHAPE;
-    int rc = rows_of(cu, n_seq, T, x.D, nullptr, n_seq, &a.rows);
+    int rc = rows_of(cu, n_seq, T, x.D, nullptr, n_seq, clear, &a.rows);
     if (rc != CHELA_OK) return rc;
     if (x.D == 0) return CHELA_OK;
     const size_t es = esize(dtype), st = (size_t)n_seq * x.N * x.D * 4, rows = (size_t)T * x.D * es, maps = (size_t)T * x.G * x.N * es;
@@ -1555,12 +1540,13 @@ static int selscan_bwd_common(const SelscanIn& x, const int* cu, int n_seq, int 
     return status_of(launch_selscan_bwd(a, p, (char*)ws, kind(dtype), (hipStream_t)stream));
 }
 
-static int selscan_step_common(const SelscanIn& x, float* S, const int* slots, int n_slots, int R, void* y, int dtype, void* stream)
+static int selscan_step_common(const SelscanIn& x, float* S, const int* slots, int n_slots, int R, void* y, int dtype, bool clear,
+                               void* stream)
 {
     SelscanArgs a{};
     if (!selscan_states_ok(x.N)) return CHELA_ERR_UNSUPPORTED_DIM;
     if (!selscan_dims(x.D, x.N, x.G) || R < 0) return CHELA_ERR_BAD_SHAPE;
-    int rc = rows_of(nullptr, R, R, x.D, slots, n_slots, &a.rows);
+    int rc = rows_of(nullptr, R, R, x.D, slots, n_slots, clear, &a.rows);
     if (rc != CHELA_OK) return rc;
     if (R == 0 || x.D == 0) return CHELA_OK;
     const size_t es = esize(dtype);
@@ -1574,30 +1560,32 @@ static int selscan_step_common(const SelscanIn& x, float* S, const int* slots, i
 }
 
 #define CHELA_SELSCAN_IN                                                                                              \
-    const void *U, long long ldu, const void *delta, long long ldd, const float *A, const void *Bm, long long ldb, const void *Cm,       \
+    const void *U, long long ldu, const void *delta, long long ldd, const float *A, const void *Bm, long long ldb, const void *Cm, \
         long long ldc, const float *Dskip, const void *Z, long long ldz, const float *delta_bias, int softplus
 #define CHELA_SELSCAN_AS(D, N, G) SelscanIn{U, delta, Bm, Cm, Z, ldu, ldd, ldb, ldc, ldz, A, Dskip, delta_bias, softplus, D, N, G}
-#define CHELA_SELSCAN(SUFFIX, TYPE)                                                                                   \
-    int chela_selscan_fwd##SUFFIX(CHELA_SELSCAN_IN, const int* cu, int n_seq, int T, int D, int N, int G, const float* S_in, float* S_out, \
+#define CHELA_SELSCAN(FORM, SUFFIX, TYPE, CLEAR)                                                                      \
+    int chela_selscan_fwd##FORM##SUFFIX(CHELA_SELSCAN_IN, const int* cu, int n_seq, int T, int D, int N, int G, const float* S_in, float* S_out, \
                                   const int* slots, int n_slots, void* Y, void* saved, void* stream)                  \
     {                                                                                                                 \
-        return selscan_fwd_common(CHELA_SELSCAN_AS(D, N, G), cu, n_seq, T, S_in, S_out, slots, n_slots, Y, saved, TYPE, stream); \
+        return selscan_fwd_common(CHELA_SELSCAN_AS(D, N, G), cu, n_seq, T, S_in, S_out, slots, n_slots, Y, saved, TYPE, CLEAR, stream); \
     }                                                                                                                 \
-    int chela_selscan_bwd##SUFFIX(CHELA_SELSCAN_IN, const int* cu, int n_seq, int T, int D, int N, int G, const float* S_in,  \
-                                  const void* dY, long long lddy, const float* dS_out, const void* saved, void* dU, void* ddelta,  \
-                                  float* dA, void* dB, void* dC, float* dDskip, void* dZ, float* ddelta_bias, float* dS_in,   \
+    int chela_selscan_bwd##FORM##SUFFIX(CHELA_SELSCAN_IN, const int* cu, int n_seq, int T, int D, int N, int G, const float* S_in, \
+                                  const void* dY, long long lddy, const float* dS_out, const void* saved, void* dU, void* ddelta, \
+                                  float* dA, void* dB, void* dC, float* dDskip, void* dZ, float* ddelta_bias, float* dS_in, \
                                   void* stream)                                                                       \
     {                                                                                                                 \
         return selscan_bwd_common(CHELA_SELSCAN_AS(D, N, G), cu, n_seq, T, S_in, dY, lddy, dS_out, saved, dU, ddelta, dA, dB, dC, dDskip, \
-                                  dZ, ddelta_bias, dS_in, TYPE, stream);                                              \
+                                  dZ, ddelta_bias, dS_in, TYPE, CLEAR, stream);                                       \
     }                                                                                                                 \
-    int chela_selscan_step##SUFFIX(CHELA_SELSCAN_IN, float* S, const int* slots, int n_slots, int R, int D, int N, int G, void* y,  \
+    int chela_selscan_step##FORM##SUFFIX(CHELA_SELSCAN_IN, float* S, const int* slots, int n_slots, int R, int D, int N, int G, void* y, \
                                    void* stream)                                                                      \
     {                                                                                                                 \
-        return selscan_step_common(CHELA_SELSCAN_AS(D, N, G), S, slots, n_slots, R, y, TYPE, stream);                 \
+        return selscan_step_common(CHELA_SELSCAN_AS(D, N, G), S, slots, n_slots, R, y, TYPE, CLEAR, stream);          \
     }
-CHELA_SELSCAN(, CHELA_DTYPE_BF16)
-CHELA_SELSCAN(_f32, CHELA_DTYPE_F32)
+CHELA_SELSCAN(, , CHELA_DTYPE_BF16, false)
+CHELA_SELSCAN(, _f32, CHELA_DTYPE_F32, false)
+CHELA_SELSCAN(_cleared, , CHELA_DTYPE_BF16, true)
+CHELA_SELSCAN(_cleared, _f32, CHELA_DTYPE_F32, true)
 #undef CHELA_SELSCAN
 #undef CHELA_SELSCAN_AS
 #undef CHELA_SELSCAN_IN

@@ -218,11 +218,11 @@ hipError_t launch_shortlong_conv_bwd(const void* X, const float* w_short, int m,
 
 // ---- operators on [T, D] rows (a token's channels next to each other)
 // Whose rows they are: sequence s has rows cu[s] .. cu[s+1], or L rows where cu is null.  slots: which state of the n_slots there are is
-// sequence s's (null: the s-th).
+// sequence s's (null: the s-th).  clear: the outputs' rows of no sequence (single tokens: without a state) are zeroed, else left as they are.
 struct Rows {
     const int* cu;
     const int* slots;
-    int n_seq, n_slots, T, L;
+    int n_seq, n_slots, T, L, clear;
 };
 
 // Short causal convolution.  S_in, S_out: the last m - 1 inputs in front of and behind each sequence, [n_slots][m-1][D].

@@ -256,7 +256,10 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
                 ++q;
                 if (q < R.n_seq) { beg = seq_begin(R, q); end = seq_end(R, q); }
             }
-            if (r >= t1 || q >= R.n_seq || r < beg) continue;
+            if (r >= t1 || q >= R.n_seq || r < beg) {
+                if (MODE == SCAN_OUT && R.clear && r < t1) row_store(Y, och, (IO)0.f);
+                continue;
+            }
             const int slot = a.S_in || a.S_out ? slot_of(R, q) : -1;
             if (r == beg) {
                 began = true;
@@ -641,7 +644,14 @@ __global__ __launch_bounds__(N / NPW * 64, 3) void selscan_bwd_kernel(ScanBwd a)
             const int k = w + i * W, r = t + k;
             if (!whole) {
                 const int sr = r < t1 ? seq_of(R, r) : -1;
-                if (sr < 0 || sr >= R.n_seq) continue;
+                if (sr < 0 || sr >= R.n_seq) {
+                    if (R.clear && r < t1 && live) {
+                        if (Z) row_store(dZ + (size_t)r * s.D, och, (IO)0.f);
+                        row_store(dU + (size_t)r * s.D, och, (IO)0.f);
+                        row_store(dDe + (size_t)r * s.D, och, (IO)0.f);
+                    }
+                    continue;
+                }
             }
             float y = 0.f, s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -674,7 +684,7 @@ __global__ __launch_bounds__(N / NPW * 64, 3) void selscan_bwd_kernel(ScanBwd a)
     }
 }
 
-// The waves' sums over their channels, added up and rounded once; rows of no sequence are left as they are.
+// The waves' sums over their channels, added up and rounded once; rows of no sequence are left as they are, or zeroed.
 template <typename IO>
 __global__ __launch_bounds__(256) void selscan_bc_kernel(Rows R, const float* __restrict__ part, int nb, int N, int G, IO* __restrict__ dB,
                                                         IO* __restrict__ dC)
@@ -682,9 +692,11 @@ __global__ __launch_bounds__(256) void selscan_bc_kernel(Rows R, const float* __
     const long n = (long)R.T * G * 2 * N;
     const long first = R.n_seq > 0 ? (long)seq_begin(R, 0) * G * 2 * N : 0, stop = R.n_seq > 0 ? (long)seq_end(R, R.n_seq - 1) * G * 2 * N : 0;
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
-        if (i < first || i >= stop) continue;
+        const bool on = i >= first && i < stop;
+        if (!on && !R.clear) continue;
         float x = 0.f;
-        for (int b = 0; b < nb; ++b) x += part[(size_t)b * n + i];
+        if (on)
+            for (int b = 0; b < nb; ++b) x += part[(size_t)b * n + i];
         const int k = (int)(i % (2 * N));
         const long tg = i / (2 * N);
         if (k < N) dB[tg * N + k] = from_f<IO>(x);
@@ -730,7 +742,10 @@ __global__ __launch_bounds__(64) void selscan_step_kernel(SelscanArgs a, int eac
     const float bias = a.delta_bias ? a.delta_bias[ch] : 0.f, skip = a.Dskip ? a.Dskip[ch] : 0.f;
     for (int r = r0; r < r1; ++r) {
         const int slot = slot_of(a.rows, r);
-        if (slot < 0) continue;
+        if (slot < 0) {
+            if (a.rows.clear) ((IO*)a.Y)[(size_t)r * a.D + ch] = (IO)0.f;
+            continue;
+        }
         float* S = a.S_out + (size_t)slot * ND + ch;
         const IO *Bm = (const IO*)a.Bm + (size_t)r * a.ldb + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)r * a.ldc + (size_t)g * N;
         float h[N];

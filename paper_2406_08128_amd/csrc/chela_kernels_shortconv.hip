@@ -209,6 +209,7 @@ __global__ __launch_bounds__(256) void short_conv_kernel(ShortConvArgs a)
         const bool on = at.at(R, t);
         if (on && known != at.q) { in_front<IO, V, M>(a, at, t, ch, back); known = at.q; }
         row(x[M - 1], on ? (IO*)a.Y + (size_t)t * a.D : nullptr);
+        if (!on && R.clear) row_store((Raw<IO, V>*)((IO*)a.Y + (size_t)t * a.D), ch * sizeof(IO), Raw<IO, V>(0));
 #pragma unroll
         for (int i = M - 1; i < RUN + M - 2; ++i) x[i] = x[i + 1];
     }
@@ -221,7 +222,10 @@ __global__ __launch_bounds__(64) void short_conv_step_kernel(ShortConvArgs a)
     const int nb = (a.D + 64 * V - 1) / (64 * V), r = blockIdx.x / nb, ch = (blockIdx.x % nb * 64 + threadIdx.x) * V;
     if (ch >= a.D) return;
     const int slot = slot_of(a.rows, r);
-    if (slot < 0) return;
+    if (slot < 0) {
+        if (a.rows.clear) row_store((Raw<IO, V>*)((IO*)a.Y + (size_t)r * a.D), ch * sizeof(IO), Raw<IO, V>(0));
+        return;
+    }
     IO* S = (IO*)a.S_out + (size_t)slot * (M - 1) * a.D + ch;
     float w[M][V], bias[V], s[M > 1 ? M - 1 : 1][V], x[V], u[V], y[V];
     load_row<IO, V>((const IO*)a.X + (size_t)r * a.ldx + ch, x);
@@ -339,7 +343,11 @@ __global__ __launch_bounds__(256) void short_conv_bwd_kernel(ShortConvArgs a, in
             for (int i = M - 1; i < RUN + 2 * (M - 1) - 1; ++i) xs[i] = xs[i + 1];
 #pragma unroll
             for (int i = 0; i < RUN + M - 2; ++i) dys[i] = dys[i + 1];
-            if (t < t1 && !at.at(R, t)) { next_x(xr); continue; }
+            if (t < t1 && !at.at(R, t)) {
+                if (R.clear) row_store((Raw<IO, V>*)((IO*)a.dX + (size_t)t * a.D), ch * sizeof(IO), Raw<IO, V>(0));
+                next_x(xr);
+                continue;
+            }
             if (known != at.q) {
                 known = at.q;
                 in_front<IO, V, M>(a, at, t, ch, back);

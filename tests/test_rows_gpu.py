@@ -363,6 +363,61 @@ def test_slots_and_rows_of_nobody(dtype):
             assert torch.equal(pool[k], before[k]) and torch.equal(conv_pool[k], cbefore[k])
 
 
+def poisoned(*shapes):
+    """What the allocator gives out next, for tensors of these (shape, dtype), holds no numbers."""
+    torch.cuda.synchronize()
+    held = [torch.full(s, float("nan"), dtype=t, device="cuda") for s, t in shapes for _ in range(8)]
+    torch.cuda.synchronize()
+    del held
+
+
+@pytest.mark.parametrize("named", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens,first,T", [([5, 0, 40, 1, 90], 3, 150), ([33, 7], 0, 1000), ([20], 901, 930), ([], 4, 70), ([0, 0], 0, 61)])
+def test_rows_of_nobody_are_zero_in_new_outputs(lens, first, T, dtype, named):
+    # (named: with a stream named a call goes through the binding's own lines, else through the compiled host path)
+    r, m, D, N, n = gen(101 + T), 4, 72, 16, len(lens)
+    kw = dict(stream=torch.cuda.current_stream()) if named else {}
+    cu = cu_of(lens, first)
+    owned = np.zeros(T, bool)
+    owned[first:first + sum(lens)] = True
+    own, bad = torch.tensor(owned, device="cuda"), torch.tensor(~owned, device="cuda")
+    u, delta, z, Bm, Cm, A, skip, bias = scan_inputs(r, T, D, N, 1, dtype)
+    dY, w = r(T, D).to(dtype), r(D, m)
+    for t in (u, delta, z, Bm, Cm, dY):
+        t[bad] = float("nan")
+    scan = dict(D=skip, Z=z, delta_bias=bias, cu=cu, **kw)
+    rows, maps = ((T, D), dtype), ((T, 1, N), dtype)
+    for run, new, given in (
+            (lambda **k: binding.chela_short_conv_fwd(u, w, cu=cu, **kw, **k), [rows], True),
+            (lambda **k: binding.chela_short_conv_fwd(wide_rows(u), w[:, :1].contiguous(), cu=cu, **kw, **k), [rows], True),
+            (lambda **k: binding.chela_selscan_fwd(u, delta, A, Bm, Cm, **scan, **k)[0], [rows], True),
+            (lambda: binding.chela_short_conv_bwd(u, w, dY, cu=cu, **kw)[:1], [rows], False),
+            (lambda: binding.chela_short_conv_bwd(u[:, :71], w[:71], dY[:, :71], cu=cu, **kw)[:1], [((T, 71), dtype)], False),
+            (lambda: [binding.chela_selscan_bwd(u, delta, A, Bm, Cm, dY, **scan)[k] for k in (0, 1, 3, 4, 6)], [rows, maps], False),
+            (lambda: [binding.chela_selscan_bwd(u, delta, A, Bm, Cm, dY, cu=cu, **kw)[k] for k in (0, 1, 3, 4)], [rows, maps], False)):
+        poisoned(*new)
+        got = run()
+        for t in (got,) if given else got:
+            assert (t[bad] == 0).all() and torch.isfinite(t).all()
+        if given:                                                        # one that the caller has keeps its rows
+            Y = torch.full((T, D), 7.0, dtype=dtype, device="cuda")
+            assert run(Y=Y) is Y and (Y[bad] == 7).all() and torch.equal(Y[own], got[own])
+    # single tokens: requests without a state
+    R, slots = 5, torch.tensor([2, -1, 0, 7, 4], dtype=torch.int32, device="cuda")
+    u, delta, z, Bm, Cm, A, skip, bias = scan_inputs(r, R, D, N, 1, dtype)
+    S, C = r(5, N, D), r(5, m - 1, D).to(dtype)
+    for run in (lambda **k: binding.chela_selscan_step(u, delta, A, Bm, Cm, S.clone(), z=z, slots=slots, **kw, **k),
+                lambda **k: binding.chela_short_conv_step(u, w, C.clone(), slots=slots, **kw, **k),
+                lambda **k: binding.chela_short_conv_step(wide_rows(u), w, C.clone(), slots=slots, **kw, **k)):
+        poisoned(((R, D), dtype))
+        y = run()
+        mine, none = [0, 2, 4], [1, 3]
+        assert (y[none] == 0).all() and torch.isfinite(y).all()
+        y2 = torch.full((R, D), 7.0, dtype=dtype, device="cuda")
+        assert run(y=y2) is y2 and (y2[none] == 7).all() and torch.equal(y2[mine], y[mine])
+
+
 @pytest.mark.parametrize("n", [70, 300, 5000])
 def test_many_sequences(n):
     # more of them than lanes, than 64 lanes' steps; short ones, many without rows, at the ends too

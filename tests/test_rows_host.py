@@ -245,6 +245,24 @@ def test_block_norm_refusals(L, sfx):
     assert bwd(dX=at(9) + 2) == ALIGN and bwd(dX=at(2)) == ALIAS and bwd(dY=at(8)) == ALIAS and bwd(dX=at(5) + 16) == ALIAS
 
 
+@pytest.mark.parametrize("sfx", ["", "_f32"])
+def test_the_calls_that_clear_refuse_the_same(L, sfx):
+    f, b, s = (getattr(L, "chela_short_conv_%s_cleared%s" % (k, sfx)) for k in ("fwd", "bwd", "step"))
+    conv = (at(0), 64, at(1), 4, None, 1)
+    assert f(*conv, None, 2, 8, 64, None, None, None, 2, None, None) == NULL and f(*conv, None, 2, 8, 64, None, None, None, 2, at(0), None) == ALIAS
+    assert b(*conv, None, 2, 9, 64, None, at(2), 64, None, at(3), at(4), None, None, None) == SHAPE
+    assert b(*conv, None, 2, 8, 64, None, at(2), 64, None, at(2), at(4), None, None, None) == ALIAS
+    assert s(*conv, at(2), None, 3, 3, 64, at(3) + 4, None) == ALIGN and s(*conv, at(2), None, 3, 2, 64, at(3), None) == SHAPE
+    f, b, s = (getattr(L, "chela_selscan_%s_cleared%s" % (k, sfx)) for k in ("fwd", "bwd", "step"))
+    scan = (at(0), 64, at(1), 64, at(2), at(3), 16, at(4), 16, None, None, 0, None, 1)
+    assert f(*scan, None, 2, 8, 64, 12, 1, None, None, None, 2, at(5), None, None) == DIM
+    assert f(*scan, None, 2, 8, 64, 16, 1, None, None, None, 2, None, None, None) == NULL
+    outs = (at(6), at(7), at(8), at(9), at(10), None, None, None, None, None)
+    assert b(*scan, None, 2, 7, 64, 16, 1, None, at(5), 64, None, None, *outs) == SHAPE
+    assert b(*scan, None, 2, 8, 64, 16, 1, None, at(6), 64, None, None, *outs) == ALIAS
+    assert s(*scan, at(5), None, 3, 3, 64, 16, 1, at(5), None) == ALIAS and s(*scan, at(5), None, 3, 3, 64, 16, 1, None, None) == NULL
+
+
 def test_workspace_and_saved_queries(L):
     assert L.chela_selscan_saved_bytes(1000, 100, 16) == 125 * 16 * 100 * 4
     assert L.chela_selscan_saved_bytes(0, 100, 16) == 0 and L.chela_selscan_saved_bytes(5, 100, 15) == 0
