@@ -495,7 +495,7 @@ hipError_t launch_short_conv_bwd(const ShortConvArgs& a, int dtype, hipStream_t 
     CHELA_TYPES(CHELA_F)
 #undef CHELA_F
     hipLaunchKernelGGL(short_conv_sum_kernel, dim3((a.D + 63) / 64, a.m + 1), dim3(1024), 0, st, a, parts);
-    if (a.dS_in && a.m > 1 && (a.rows.cu || a.rows.T == 0)) {
+    if (a.dS_in && a.m > 1 && a.rows.n_seq > 0 && (a.rows.cu || a.rows.T == 0)) {
         const dim3 g(a.rows.n_seq < 256 ? a.rows.n_seq : 256);
         if (dtype == 0) hipLaunchKernelGGL(short_conv_empty_kernel<bf16>, g, dim3(256), 0, st, a);
         else hipLaunchKernelGGL(short_conv_empty_kernel<float>, g, dim3(256), 0, st, a);

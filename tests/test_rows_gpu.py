@@ -478,6 +478,31 @@ def test_no_rows():
     assert (n[3] == 0).all() and (n[4] == 0).all()
 
 
+@pytest.mark.parametrize("sfx,dtype", [("", BF), ("_f32", F32)])
+@pytest.mark.parametrize("T,packed", [(0, False), (0, True), (9, True)])
+def test_no_sequences(sfx, dtype, T, packed):
+    # addresses of states all the same, as a caller from C may hand them over: there is nothing to pass on, and no error
+    L, D, N, m, st = binding.lib(), 64, 16, 4, torch.cuda.current_stream().cuda_stream
+    cu = torch.zeros(1, dtype=torch.int32, device="cuda")
+    pcu = cu.data_ptr() if packed else None
+    X, dX, dZ = (torch.full((9, D), 3.0, dtype=dtype, device="cuda") for _ in range(3))
+    Bm, dB, dC = (torch.full((9, N), 3.0, dtype=dtype, device="cuda") for _ in range(3))
+    w, dw, A, dA, b, db = (torch.full(s, 3.0, device="cuda") for s in ((D, m), (D, m), (N, D), (N, D), (D,), (D,)))
+    S, C, S2, C2 = (torch.full(s, 5.0, dtype=t, device="cuda") for s, t in ((((1, N, D)), F32), ((1, m - 1, D), dtype)) * 2)
+    x, p = X.data_ptr(), lambda t: t.data_ptr()  # noqa: E731
+    conv = (x, D, p(w), m, p(b), 1, pcu, 0, T, D)
+    scan = (x, D, x, D, p(A), p(Bm), N, p(Bm), N, None, None, 0, None, 1, pcu, 0, T, D, N, 1)
+    assert getattr(L, "chela_short_conv_bwd" + sfx)(*conv, p(C), x, D, p(C), p(dX), p(dw), p(db), p(C2), st) == 0
+    assert (dw == 0).all() and (db == 0).all()
+    assert getattr(L, "chela_selscan_bwd" + sfx)(*scan, p(S), x, D, p(S), None, p(dX), p(dZ), p(dA), p(dB), p(dC), None, None, None, p(S2), st) == 0
+    assert (dA == 0).all()
+    for in_place in (False, True):
+        assert getattr(L, "chela_short_conv_fwd" + sfx)(*conv, p(C), p(C if in_place else C2), None, 0, p(dX), st) == 0
+        assert getattr(L, "chela_selscan_fwd" + sfx)(*scan, p(S), p(S if in_place else S2), None, 0, p(dX), None, st) == 0
+    assert (dX == 3).all() and (dZ == 3).all() and (dB == 3).all() and (dC == 3).all()
+    assert all((t == 5).all() for t in (S, S2, C, C2))
+
+
 def test_what_is_not_finite_stays_in_its_sequence():
     r, D, N, m = gen(19), 64, 16, 4
     lens = [20, 30, 25]
