@@ -452,10 +452,11 @@ size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int
  * block's output, X the residual stream, Nrm the next block's input.  Y NULL (in front of the first block; gate, w_post and X_out are
  * then not looked at): Nrm = Norm(X) * w_pre.  The second norm takes X_out before it is rounded.  Squares and their mean are fp32.
  *   Y, gate, Nrm: bf16 (plain name) or fp32 (_f32); X, X_out: the same, or fp32 beside bf16 (x_f32 != 0).  w_post, w_pre [D] fp32.
- *   X_out may be X (exactly the same pointer).
+ *   X_out may be X (exactly the same pointer; then Y or gate may be there too where their type is X's).
  *   bwd: from Y, gate and X, the stream as the forward call left it (its X_out; with Y NULL its X), for the upstream gradients dX_out (type
- *   of X; NULL: zero) and dN (only with w_pre): dY, dgate, dX (type of X; may be dX_out, exactly the same pointer), dw_post and dw_pre [D] fp32,
- *   each only where there is its input.  Sums over rows are taken in a fixed order.  rows = 0: dw_post and dw_pre are zeroed. */
+ *   of X; NULL: zero) and dN (only with w_pre): dY, dgate, dX (type of X; may be dX_out, exactly the same pointer, where then X and, of X's
+ *   type, Y, gate and dN may be too), dw_post and dw_pre [D] fp32, each only where there is its input.  Sums over rows are taken in a fixed
+ *   order.  rows = 0: dw_post and dw_pre are zeroed. */
 int chela_block_norm_fwd(const void *Y, const void *gate, const void *X, const float *w_post, const float *w_pre, void *X_out,
                          void *Nrm, float scale, float eps, long long rows, int D, int x_f32, void *stream);
 int chela_block_norm_fwd_f32(const void *Y, const void *gate, const void *X, const float *w_post, const float *w_pre, void *X_out,

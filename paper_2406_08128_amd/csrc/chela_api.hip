@@ -1279,7 +1279,8 @@ int chela_linattn_step_gated(const void* q, const void* k, const void* v, const 
 // What a call reads and writes, for the checks that all of them make.  rows with a stride: elements' alignment; the rest: 16 bytes.
 struct Operands {
     int rc = CHELA_OK;
-    int n_in = 0, n_out = 0;
+    int n_in = 0, n_out = 0, under = -1, over = -1;           // the input that an output may stand for, and that output
+    unsigned alike = 0;                                       // inputs of which a thread reads what it writes, no more, before it does
     Range in[16], out[12];
     void check(const void* p, size_t bytes, size_t align)
     {
@@ -1298,13 +1299,19 @@ struct Operands {
     }
     void write(const void* p, size_t bytes) { check(p, bytes, 16); out[n_out++] = Range{(const char*)p, bytes}; }
     void write_if(const void* p, size_t bytes) { if (p) write(p, bytes); }
-    // no output on another, nor on an input but the one it may stand for
-    int done(const void* same_in = nullptr, const void* same_out = nullptr) const
+    void read_under(const void* p, size_t bytes) { under = n_in; read(p, bytes); }
+    void write_over(const void* p, size_t bytes) { over = n_out; write(p, bytes); }
+    void read_alike(const void* p, size_t bytes) { if (p) { alike |= 1u << n_in; read(p, bytes); } }
+    // no output on another, nor on an input, but the one that may be exactly where the other is.  (By their places here, not by the address: a
+    // third tensor there may be another workgroup's to read.  One of as many bytes that is read as the second is may be there too.)
+    int done() const
     {
         if (rc != CHELA_OK) return rc;
         for (int o = 0; o < n_out; ++o) {
             for (int i = 0; i < n_in; ++i) {
-                if (same_in && out[o].p == same_out && in[i].p == same_in && same_in == same_out) continue;
+                if (o == over && under >= 0 && in[under].p == out[o].p && in[i].p == out[o].p &&
+                    (i == under || ((alike >> i & 1) && in[i].n == out[o].n)))
+                    continue;
                 if (overlap(out[o], in[i])) return CHELA_ERR_ALIASING;
             }
             for (int o2 = o + 1; o2 < n_out; ++o2) if (overlap(out[o], out[o2])) return CHELA_ERR_ALIASING;
@@ -1349,10 +1356,10 @@ static int short_conv_common(const void* X, long long ldx, const float* w, int m
     o.read_if(bias, (size_t)D * 4);
     o.read_if(cu, ((size_t)n_seq + 1) * 4, 4);
     o.read_if(slots, (size_t)n_seq * 4, 4);
-    o.read_if(S_in, st);
-    o.write_if(S_out, st);
+    if (S_in) o.read_under(S_in, st);
+    if (S_out) o.write_over(S_out, st);
     o.write(Y, (size_t)T * D * es);
-    if ((rc = o.done(S_in, S_out)) != CHELA_OK) return rc;
+    if ((rc = o.done()) != CHELA_OK) return rc;
     a.X = X; a.ldx = ldx; a.w = w; a.m = m; a.bias = bias; a.silu = silu; a.D = D; a.S_in = S_in; a.S_out = S_out; a.Y = Y;
     return status_of(launch_short_conv_fwd(a, kind(dtype), (hipStream_t)stream));
 }
@@ -1492,11 +1499,11 @@ static int selscan_fwd_common(const SelscanIn& x, const int* cu, int n_seq, int 
     const size_t es = esize(dtype), st = (size_t)n_slots * x.N * x.D * 4;
     Operands o;
     selscan_read(x, T, es, &o, &a);
-    o.read_if(S_in, st);
-    o.write_if(S_out, st);
+    if (S_in) o.read_under(S_in, st);
+    if (S_out) o.write_over(S_out, st);
     o.write(Y, (size_t)T * x.D * es);
     o.write_if(saved, chela_selscan_saved_bytes(T, x.D, x.N));
-    if ((rc = o.done(S_in, S_out)) != CHELA_OK) return rc;
+    if ((rc = o.done()) != CHELA_OK) return rc;
     const SelscanPlan p = make_selscan_plan(T, x.D, x.N, x.G, false, false);
     float* ws = nullptr;
     if ((rc = get_workspace(p.bytes, stream, &ws)) != CHELA_OK) return rc;
@@ -1608,14 +1615,14 @@ static int block_norm_fwd_common(const void* Y, const void* gate, const void* X,
     if (!Y) { gate = nullptr; w_post = nullptr; X_out = nullptr; }
     const size_t es = esize(dtype), n = (size_t)rows * D, xs = x_f32 ? 4 : es;
     Operands o;
-    o.read(X, n * xs);
-    o.read_if(Y, n * es);
-    o.read_if(gate, n * es);
+    o.read_under(X, n * xs);
+    o.read_alike(Y, n * es);
+    o.read_alike(gate, n * es);
     o.read_if(w_post, (size_t)D * 4);
     o.read_if(w_pre, (size_t)D * 4);
-    if (Y) o.write(X_out, n * xs);
+    if (Y) o.write_over(X_out, n * xs);
     if (w_pre) o.write(Nrm, n * es);
-    if ((rc = o.done(X, X_out)) != CHELA_OK) return rc;
+    if ((rc = o.done()) != CHELA_OK) return rc;
     BlockNormArgs a{};
     a.Y = Y; a.gate = gate; a.X = X; a.w_post = w_post; a.w_pre = w_pre; a.X_out = X_out; a.Nrm = Nrm;
     a.scale = scale; a.eps = eps; a.rows = rows; a.D = D; a.x_f32 = x_f32;
@@ -1637,19 +1644,23 @@ static int block_norm_bwd_common(const void* Y, const void* gate, const void* X,
     if (!Y && rows > 0) { gate = nullptr; w_post = nullptr; }
     const size_t es = esize(dtype), n = (size_t)rows * D, xs = x_f32 ? 4 : es;
     Operands o;
-    o.read(X, n * xs);
-    o.read_if(Y, n * es);
-    o.read_if(gate, n * es);
+    o.check(X, n * xs, 16);
+    o.read_alike(X, n * xs);
+    o.read_alike(Y, n * es);
+    o.read_alike(gate, n * es);
     o.read_if(w_post, (size_t)D * 4);
     o.read_if(w_pre, (size_t)D * 4);
-    o.read_if(dX_out, n * xs);
-    if (w_pre) o.read(dN, n * es);
+    if (dX_out) o.read_under(dX_out, n * xs);
+    if (w_pre) {
+        o.check(dN, n * es, 16);
+        o.read_alike(dN, n * es);
+    }
     if (Y) o.write(dY, n * es);
     if (gate) o.write(dgate, n * es);
-    o.write(dX, n * xs);
+    o.write_over(dX, n * xs);
     if (w_post) o.write(dw_post, (size_t)D * 4);
     if (w_pre) o.write(dw_pre, (size_t)D * 4);
-    if ((rc = o.done(dX_out, dX)) != CHELA_OK) return rc;
+    if ((rc = o.done()) != CHELA_OK) return rc;
     float* ws = nullptr;
     if ((rc = get_workspace(chela_block_norm_bwd_workspace_bytes(rows, D), stream, &ws)) != CHELA_OK) return rc;
     BlockNormArgs a{};

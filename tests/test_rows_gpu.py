@@ -636,6 +636,28 @@ def test_block_norm(dtype, rows, D, gated, post, pre, block, x_f32):
             assert all([same(a, b) for a, b in zip(g, again)])
 
 
+@pytest.mark.parametrize("D", [768, 1531, 4506])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_block_norm_in_place_of_a_tensor_that_is_there_twice(dtype, D):
+    # one tensor as both upstream gradients, or as the block's output and the stream: a thread reads of it what it writes
+    r, n = gen(D), 300
+    Y, X, gate, d, wp, wn = r(n, D).to(dtype), r(n, D).to(dtype), r(n, D).to(dtype), r(n, D).to(dtype), 1 + 0.1 * r(D), 1 + 0.1 * r(D)
+    kw = dict(gate=gate, w_post=wp, w_pre=wn, scale=0.5)
+    want = binding.chela_block_norm_bwd(Y, X, d, d, **kw)
+    d2 = d.clone()
+    got = binding.chela_block_norm_bwd(Y, X, d2, d2, in_place=True, **kw)
+    assert got[2] is d2 and all([torch.equal(a, b) for a, b in zip(want, got)])
+    want = binding.chela_block_norm_fwd(X, X, **kw)
+    X2 = X.clone()
+    got = binding.chela_block_norm_fwd(X2, X2, X_out=X2, **kw)
+    assert got[0] is X2 and all([torch.equal(a, b) for a, b in zip(want, got)])
+    if dtype == BF:                                                      # rows of another size at one address: refused
+        whole = torch.zeros(n, D, device="cuda")
+        with pytest.raises(binding.ChelaError) as e:
+            binding.chela_block_norm_fwd(whole.view(-1).view(BF)[:n * D].view(n, D), whole, X_out=whole, w_pre=wn)
+        assert e.value.status == -6
+
+
 def test_block_norm_of_zeros():
     x = torch.zeros(3, 64, device="cuda")
     w = torch.ones(64, device="cuda")

@@ -263,6 +263,37 @@ def test_the_calls_that_clear_refuse_the_same(L, sfx):
     assert s(*scan, at(5), None, 3, 3, 64, 16, 1, at(5), None) == ALIAS and s(*scan, at(5), None, 3, 3, 64, 16, 1, None, None) == NULL
 
 
+@pytest.mark.parametrize("sfx", ["", "_f32"])
+def test_only_the_named_input_may_be_where_an_output_is(L, sfx):
+    # in place, and another input at the same address: other workgroups read it after one has written
+    S, X, w = at(0), at(1), at(2)
+    f = getattr(L, "chela_short_conv_fwd" + sfx)
+    for kw in (dict(w=S), dict(bias=S), dict(cu=S), dict(slots=S), dict(X=S)):
+        a = dict(dict(X=X, w=w, bias=None, cu=None, slots=None), **kw)
+        assert f(a["X"], 64, a["w"], 4, a["bias"], 1, a["cu"], 2, 8, 64, S, S, a["slots"], 2, at(3), None) == ALIAS, kw
+    f = getattr(L, "chela_selscan_fwd" + sfx)
+    names = ("U", "delta", "A", "Bm", "Cm", "skip", "Z", "bias", "cu", "slots")
+    for k in names:
+        a = dict({n: at(4 + i) for i, n in enumerate(names)}, cu=None, slots=None)
+        a[k] = S
+        assert f(a["U"], 64, a["delta"], 64, a["A"], a["Bm"], 16, a["Cm"], 16, a["skip"], a["Z"], 64, a["bias"], 1, a["cu"], 1, 8, 64, 16, 1, S, S,
+                 a["slots"], 1, at(3), None, None) == ALIAS, k
+    f, b = getattr(L, "chela_block_norm_fwd" + sfx), getattr(L, "chela_block_norm_bwd" + sfx)
+    for x_f32 in (0, 1):
+        for k in range(5):
+            a = [at(4), at(5), S, at(6), at(7)]              # Y, gate, X, w_post, w_pre
+            if k == 2 or (k < 2 and not (x_f32 and sfx == "")):
+                continue                                     # (rows of the stream's type, element by element where the stream's are)
+            a[k] = S
+            assert f(*a, S, at(8), 1.0, 1e-5, 4, 64, x_f32, None) == ALIAS, k
+            a[2] = X
+            assert b(*a, S, at(9), at(10), at(11), S, at(12), at(13), 1.0, 1e-5, 4, 64, x_f32, None) == ALIAS, k
+    if sfx == "":
+        assert b(at(4), at(5), X, at(6), at(7), S, S, at(10), at(11), S, at(12), at(13), 1.0, 1e-5, 4, 64, 1, None) == ALIAS
+    assert b(at(4), at(5), S, at(6), at(7), at(8), at(9), at(10), at(11), S, at(12), at(13), 1.0, 1e-5, 4, 64, 0, None) == ALIAS
+    assert b(at(4), at(5), S, at(6), at(7), None, at(9), at(10), at(11), S, at(12), at(13), 1.0, 1e-5, 4, 64, 0, None) == ALIAS
+
+
 def test_workspace_and_saved_queries(L):
     assert L.chela_selscan_saved_bytes(1000, 100, 16) == 125 * 16 * 100 * 4
     assert L.chela_selscan_saved_bytes(0, 100, 16) == 0 and L.chela_selscan_saved_bytes(5, 100, 15) == 0
