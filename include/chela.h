@@ -375,7 +375,8 @@ size_t chela_short_conv_bwd_workspace_bytes(int T, int D, int m, int dtype);
  *     h_t[n] = exp(dl_t A[n]) h_{t-1}[n] + dl_t u_t B_t[g,n],   y_t = sum_n C_t[g,n] h_t[n] + Dskip u_t,
  *     out_t = Z ? y_t z_t / (1 + exp(-z_t)) : y_t.
  *   U, delta, Z (or NULL) [T, D]; Bm, Cm [T, G, N], G divides D; A [N, D], Dskip [D] (or NULL), delta_bias [D] (or NULL) fp32;
- *   states [n_slots, N, D] fp32.  The decay is formed as 2^(dl A log2 e); nothing is assumed of A's sign.
+ *   states [n_slots, N, D] fp32.  The decay is formed as 2^(dl A log2 e); nothing is assumed of A's sign.  A row's decay has to be a number
+ *   that fp32 holds (from 2^128 on it is infinite, even of a state of zero); what many rows' decays make together has not.
  *   fwd  : Y [T, D].  saved: NULL, or a caller-owned buffer of chela_selscan_saved_bytes() bytes (16-byte aligned, opaque) that carries
  *          the states in front of every 8th row to the backward call.
  *   bwd  : gradients dU, ddelta, dZ (NULL without Z) [T, D], dB, dC [T, G, N] in the I/O type, dA [N, D], dDskip, ddelta_bias [D] (each

@@ -73,8 +73,13 @@ __global__ __launch_bounds__(256) void selscan_finish_kernel(ScanShape s, const 
 // Latency-bound: four waves share the chunks of 64 elements, each makes one step of its 32, takes in what is in front of them from the
 // others, and goes over them again, all from registers.
 __device__ __forceinline__ float reset_mark() { return __uint_as_float(0x7fc00000u); }
-// (a state of zero stays so however much growth has come together)
-__device__ __forceinline__ float carried(float h, float sum, float A2, float H) { return sum != sum || h == 0.f ? H : fmaf(exp2_(sum * A2), h, H); }
+// exp(A sum) h + H.  What the exponent has of whole powers of two is put on last: over many rows the decay itself may be nothing that a float
+// holds (2^-140, 2^160) where the state is, before and behind.  (Beyond 2^1000 either way nothing is left, of zero nothing comes.)
+__device__ __forceinline__ float carried(float h, float sum, float A2, float H)
+{
+    const float x = __builtin_amdgcn_fmed3f(sum * A2, -1000.f, 1000.f), k = rintf(x);
+    return sum != sum ? H : __builtin_ldexpf(exp2_(x - k) * h, (int)k) + H;
+}
 template <bool BWD>
 __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restrict__ A, float* __restrict__ totals,
                                                            const float* __restrict__ sums, int n_chunk, int D, long ND, int groups, Rows rows,

@@ -569,6 +569,33 @@ def test_selscan_growth_over_rows_that_bring_nothing():
         assert torch.equal(far[k][:10], g[k][:10]) and (far[k][10:] == 0).all(), k
 
 
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("T,first,D,N", [(2400, 768, 64, 8), (2400, 700, 64, 16), (700, 24, 64, 32), (3000, 0, 2100, 8)])
+def test_selscan_states_that_last_where_no_decay_does(T, first, D, N, sign):
+    # over 700 rows that bring nothing a state grows from 1e-12 by 2^140, or shrinks from 1e30 by as much: each row's state is a
+    # float, what the chunks' decays make together is none.  The same for the gradient on its way back.
+    r, rows = gen(97 + T + N), min(700, T - first)
+    A = torch.full((N, D), sign * 0.5, device="cuda")
+    delta = torch.zeros(T, D, device="cuda")
+    delta[first:first + rows] = 140 / rows / (0.5 * 1.4426950408889634)
+    u, dY = torch.zeros(T, D, device="cuda"), torch.zeros(T, D, device="cuda")
+    Bm, Cm = r(T, 1, N), r(T, 1, N)
+    S = (1e-12 if sign > 0 else 1e30) * (1 + r(1, N, D).abs())
+    kw = dict(softplus=False, S_in=S)
+    S_out = torch.empty_like(S)
+    Y, _ = binding.chela_selscan_fwd(u[None], delta[None], A, Bm[None], Cm[None], S_out=S_out, **kw)
+    n64 = [f64(t) for t in (u, delta, A, Bm, Cm)]
+    f, mf = R.selscan_fwd(*n64, softplus=False, state=f64(S)[0])
+    # (an exponent of 97, made of sums of 24 and of 32 step sizes: 97 * 60 roundings, fewer than these)
+    n = 8 * T + 128
+    check("Y", Y[0], f["Y"], mf["Y"], n)
+    check("S_out", S_out[0], f["S_out"], mf["S_out"], n)
+    g = binding.chela_selscan_bwd(u[None], delta[None], A, Bm[None], Cm[None], dY[None], softplus=False, dS_out=S, want_dS_in=True)
+    v, mv = R.selscan_bwd(*n64, f64(dY), softplus=False, dstate=f64(S)[0])
+    for name, t in (("dU", g[0][0]), ("ddelta", g[1][0]), ("dA", g[2]), ("dS_in", g[8][0])):
+        check(name, t, v[name], mv[name], 2 * n)
+
+
 # ------------------------------------------------------------------------------------------- norms around a block
 NORM = [  # rows, D, gate, w_post, w_pre, Y, fp32 stream
     (1, 64, True, True, True, True, False),
