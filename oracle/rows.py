@@ -157,6 +157,50 @@ def selscan_bwd(u, delta, A, Bm, Cm, dY, skip=None, z=None, delta_bias=None, sof
     return v, m
 
 
+def selscan_roundings(u, delta, A, Bm, Cm, dY, skip=None, z=None, delta_bias=None, softplus=True, state=None, dstate=None, once=128):
+    """For the outputs of selscan_fwd and selscan_bwd (but dA, dD, dbias): the sum over an output's terms of their magnitudes, each times the fp32
+    roundings that it goes through.  Times 2^-24 that is what the output may be off by, and it says more than the longest sequence's
+    roundings for all of them: a term that the decay has ended counts no more.
+
+    A row that a term passes costs it, walked row by row, the exponent's product (4 |x|, x = dl A, with what dl and A log2 e are off by), the
+    exponential and a multiply-add: 4 + 4 |x|.  Taken together with 24 other rows, and 32 such lots with one another, x is a part of a sum of step
+    sizes whose 56 additions are each off by half a step of the sum: 60 |x| on top.  So 8 + 64 |x|.  once: for what is not passed from row
+    to row, the input's products, the sum over at most 32 states, the activations."""
+    L, D = u.shape
+    N, G = A.shape[0], Bm.shape[1]
+    raw, dl, Be, Ce = _scan_setup(delta, A, Bm, Cm, delta_bias, softplus, D)
+    sk = np.zeros(D) if skip is None else np.abs(skip)
+    ms, ks = [np.zeros(A.shape) if state is None else np.abs(state)], [np.zeros(A.shape)]
+    out = {k: np.zeros((L, D)) for k in ("Y", "dU", "ddelta")}
+    for t in range(L):
+        a, w, b = np.exp(dl[t] * A), 8 + 64 * np.abs(dl[t] * A), np.abs(dl[t] * u[t] * Be[t])
+        ks.append(a * (ks[-1] + w * ms[-1]) + once * b)
+        ms.append(a * ms[-1] + b)
+        out["Y"][t] = (np.abs(Ce[t]) * (ks[-1] + once * ms[-1])).sum(0) + once * sk * np.abs(u[t])
+    out["S_out"] = ks[-1] + once * ms[-1]
+    mdy = np.abs(dY)
+    if z is not None:
+        gate = np.abs(silu(z)) * (1 + 0.1 * np.abs(z))
+        out["dZ"] = mdy * out["Y"] * dsilu(z)[1] * (1 + 0.1 * np.abs(z))
+        out["Y"], mdy = out["Y"] * gate, mdy * gate
+    out["dB"], out["dC"] = np.zeros((L, G, N)), np.zeros((L, G, N))
+    mq = np.zeros(A.shape) if dstate is None else np.abs(dstate)
+    kq = np.zeros(A.shape)
+    groups = lambda x: x.reshape(N, G, D // G).sum(2).T  # noqa: E731
+    for t in range(L - 1, -1, -1):
+        a, w = np.exp(dl[t] * A), 8 + 64 * np.abs(dl[t] * A)
+        mg, kg = np.abs(Ce[t]) * mdy[t] + mq, once * np.abs(Ce[t]) * mdy[t] + kq
+        out["dC"][t] = groups(mdy[t] * (ks[t + 1] + (once + D) * ms[t + 1]))
+        out["dB"][t] = groups((kg + (once + D) * mg) * np.abs(dl[t] * u[t]))
+        kq, mq = a * (kg + w * mg), a * mg
+        s1 = ((kg + once * mg) * np.abs(Be[t])).sum(0)
+        out["dU"][t] = np.abs(dl[t]) * s1 + once * sk * mdy[t]
+        f = (sigmoid(raw[t]) if softplus else 1.0) * (1 + 0.1 * np.abs(raw[t]))
+        out["ddelta"][t] = f * (np.abs(u[t]) * s1 + (np.abs(A) * (kq * ms[t] + mq * ks[t] + once * mq * ms[t])).sum(0))
+    out["dS_in"] = kq + once * mq
+    return out
+
+
 # ---- norms around a block: X' = X + scale Norm(Y) w_post gate, N = Norm(X') w_pre
 
 def _norm(x, eps):

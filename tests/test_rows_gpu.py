@@ -284,6 +284,34 @@ def test_selscan_hundreds_of_chunks(lens):
         check(name, g[name], sum(p[1][0][name] for p in ref), sum(p[1][1][name] for p in ref), 2 * k + T)
 
 
+@pytest.mark.parametrize("lasting", [False, True])
+@pytest.mark.parametrize("N,G,D,lens", [(8, 1, 8, [6700]), (8, 1, 8, [2300, 0, 4400]), (16, 2, 24, [3000]), (32, 1, 65, [700, 1900])])
+def test_selscan_chunks_hand_on_all_digits(N, G, D, lens, lasting):
+    # every term held to the roundings of the rows that it has passed (a carry in 16 bits is off by ten times that, see the host's tests)
+    r, T, n = gen(103 + N), sum(lens), len(lens)
+    u, delta, z, Bm, Cm, A, skip, bias = scan_inputs(r, T, D, N, G, F32)
+    bias = bias - 3
+    A = A / 64 if lasting else A                                        # (states that last for thousands of rows, or for tens)
+    dY, S, dS = r(T, D), r(n, N, D), r(n, N, D)
+    kw = dict(D=skip, Z=z, delta_bias=bias, cu=cu_of(lens), S_in=S)
+    S_out = torch.empty_like(S)
+    Y, saved = binding.chela_selscan_fwd(u, delta, A, Bm, Cm, S_out=S_out, want_saved=True, **kw)
+    g = dict(zip(("dU", "ddelta", "dA", "dB", "dC", "dD", "dZ", "dbias", "dS_in"),
+                 binding.chela_selscan_bwd(u, delta, A, Bm, Cm, dY, dS_out=dS, want_dS_in=True, saved=saved, **kw)))
+    n64 = [f64(t) for t in (u, delta, z, Bm, Cm, A, skip, bias)]
+    o = offsets(lens)
+    ref = scan_reference((*n64, True), f64(S), f64(dY), f64(dS), lens)
+    for i, ((f, _), (v, _)) in enumerate(ref):
+        rows = slice(o[i], o[i + 1])
+        k = R.selscan_roundings(n64[0][rows], n64[1][rows], n64[5], n64[3][rows], n64[4][rows], f64(dY)[rows], n64[6], n64[2][rows], n64[7], True,
+                                f64(S)[i], f64(dS)[i])
+        check("Y", Y[rows], f["Y"], k["Y"], 1)
+        check("S_out", S_out[i], f["S_out"], k["S_out"], 1)
+        for name in ("dU", "ddelta", "dB", "dC", "dZ"):
+            check(name, g[name][rows], v[name], k[name], 1)
+        check("dS_in", g["dS_in"][i], v["dS_in"], k["dS_in"], 1)
+
+
 @pytest.mark.parametrize("N,G,D", [(16, 1, 64), (8, 2, 30), (32, 1, 200), (16, 4, 1000)])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_selscan_step_against_the_definition(dtype, N, G, D):

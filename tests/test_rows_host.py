@@ -120,6 +120,43 @@ def test_selscan_without_decay_is_a_causal_sum(rng):
     assert np.allclose(v["Y"], P @ u) and np.allclose(v["S_out"], Bm[:, 0].T @ u)
 
 
+@pytest.mark.parametrize("lasting", [False, True])
+def test_the_scan_s_bound_tells_a_carry_of_fewer_bits(rng, lasting):
+    # a scan in fp32 by chunks of 24 rows: with what the chunks hand on in fp32 it is within the bound, in 16 bits of it it is not
+    L, D, N, chunk = 1200, 8, 8, 24
+    f4 = np.float32
+    u, delta, C, B = (rng.normal(size=s).astype(f4) for s in ((L, D), (L, D), (L, 1, N), (L, 1, N)))
+    A = (-np.exp(rng.normal(size=(N, D))) / (64 if lasting else 1)).astype(f4)
+    bias, S = (rng.normal(size=D) - 4).astype(f4), rng.normal(size=(N, D)).astype(f4)
+    dl = np.logaddexp(0, (delta + bias).astype(np.float64)).astype(f4)
+    b = (dl * u)[:, None] * B.transpose(0, 2, 1)
+
+    def walk(h, rows, out=None):
+        for t in rows:
+            h = np.exp(dl[t] * A) * h + b[t]
+            if out is not None:
+                out[t] = (C[t, 0][:, None] * h).sum(0)
+        return h
+
+    def scan(keep):
+        Y, h = np.zeros((L, D), f4), S
+        for t in range(0, L, chunk):
+            rows = range(t, min(t + chunk, L))
+            walk(h, rows, Y)
+            decay = np.exp(A * dl[rows.start:rows.stop].sum(0, dtype=f4))
+            h = keep(decay * h + walk(np.zeros((N, D), f4), rows))
+            assert h.dtype == f4
+        return Y
+
+    x = [t.astype(np.float64) for t in (u, delta, A, B, C)]
+    ref = R.selscan_fwd(*x, delta_bias=bias.astype(np.float64), state=S.astype(np.float64))[0]["Y"]
+    k = R.selscan_roundings(*x, np.ones((L, D)), delta_bias=bias.astype(np.float64), state=S.astype(np.float64))["Y"]
+    worst = lambda Y: float((np.abs(Y - ref) / R.tolerance(ref, k, 1, 2.0 ** -24)).max())  # noqa: E731
+    assert worst(scan(lambda h: h)) <= 1
+    assert worst(scan(lambda h: h.astype(np.float16).astype(f4))) > 2
+    assert worst(scan(lambda h: torch.from_numpy(h).bfloat16().float().numpy())) > 10
+
+
 # ------------------------------------------------------------------------------------------- refusals
 A0, SZ = 0x10000, 1 << 40      # made-up aligned addresses far apart: every call below has to be refused (or be empty) before they are used
 NULL, SHAPE, DIM, ALIGN, ALIAS, WS = -1, -2, -3, -5, -6, -7
