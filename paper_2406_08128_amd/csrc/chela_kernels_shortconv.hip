@@ -18,7 +18,6 @@ template <int BYTES> struct Bits;
 template <> struct Bits<2> { typedef unsigned short type; };
 template <> struct Bits<4> { typedef unsigned type; };
 template <> struct Bits<8> { typedef u32x2 type; };
-template <> struct Bits<16> { typedef u32x4 type; };
 template <typename IO, int V> using Raw = typename Bits<V * (int)sizeof(IO)>::type;
 
 template <typename IO, int V>

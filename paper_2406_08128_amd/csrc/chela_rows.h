@@ -5,7 +5,6 @@
 namespace chela {
 
 typedef __bf16 bf16;
-typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 
 __device__ __forceinline__ float to_f(float x) { return x; }
