@@ -19,7 +19,12 @@
 // What bounds it is the vector ALU's issue.  A row of 16 states takes 48 operations and 16 exponentials in the first pass, 64 and 16 in the
 // third; alone, from registers, the latter keep a SIMD busy for 409 cycles (an operation 3, an exponential 12).  65536 rows in four sequences, 1536
 // channels, 16 states, bf16, us: first pass 304 (the issue's floor 224), third with its saved states 417 (262; 1.6 GB at 3.9 TB/s), gradient:
-// first pass 346, walk 1230, carries 25 and 16, sums of dB and dC over the channels' waves 59.
+// first pass 346, walk 1230, carries 25 and 16, sums of dB and dC over the channels' waves 59.  By the counters the vector ALUs are at work
+// for all of the two passes' time and for 94 % of the gradient's walk: a row there takes 97 vector instructions per four states, 48 that the
+// formulas have, 24 for the sums over channels, 25 for what a row has once (softplus, gate, conversions, its results' sums over states).
+//
+// The states that a forward call saves for its gradient take 0.8 GB at that size.  Without them the gradient walks the rows forward itself:
+// 2080 us in all instead of 1500, and the forward call 676 instead of 693.
 #include "chela_rows.h"
 #include <type_traits>
 
@@ -73,12 +78,12 @@ __global__ __launch_bounds__(256) void selscan_finish_kernel(ScanShape s, const 
 // Latency-bound: four waves share the chunks of 64 elements, each makes one step of its 32, takes in what is in front of them from the
 // others, and goes over them again, all from registers.
 __device__ __forceinline__ float reset_mark() { return __uint_as_float(0x7fc00000u); }
-// exp(A sum) h + H.  What the exponent has of whole powers of two is put on last: over many rows the decay itself may be nothing that a float
-// holds (2^-140, 2^160) where the state is, before and behind.  (Beyond 2^1000 either way nothing is left, of zero nothing comes.)
-__device__ __forceinline__ float carried(float h, float sum, float A2, float H)
+// exp(A sum) h + H, half of the exponent at a time: over many rows the decay itself may be nothing that a float holds (2^-140, 2^160) where the
+// state is, before and behind.  half_A2: A / 2 in units of ln 2.  (A state of zero stays so however much growth has come together.)
+__device__ __forceinline__ float carried(float h, float sum, float half_A2, float H)
 {
-    const float x = __builtin_amdgcn_fmed3f(sum * A2, -1000.f, 1000.f), k = rintf(x);
-    return sum != sum ? H : __builtin_ldexpf(exp2_(x - k) * h, (int)k) + H;
+    const float e = exp2_(sum * half_A2);
+    return sum != sum || h == 0.f ? H : fmaf(e, e * h, H);
 }
 template <bool BWD>
 __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restrict__ A, float* __restrict__ totals,
@@ -94,7 +99,7 @@ __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restr
     const bool live = (long)blockIdx.x * 64 + lane < ND;
     const long i = live ? (long)blockIdx.x * 64 + lane : ND - 1;
     const int ch = (int)(i % D);
-    const float A2 = A[i] * kLog2e;
+    const float half_A2 = A[i] * (0.5f * kLog2e);
     float base = 0.f;                                // what comes to the 4 * AT chunks
     constexpr int AT = 32;                           // chunks whose totals are read together
     // (the chunk that nothing comes behind has no totals: its place holds anything, and what is made of it goes nowhere)
@@ -109,7 +114,7 @@ __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restr
         // (what is worked out for places behind the last chunk goes nowhere; were it left out, the loads would wait in turn)
 #pragma unroll
         for (int j = 0; j < AT; ++j) {
-            h = carried(h, sd[j], A2, H[j]);
+            h = carried(h, sd[j], half_A2, H[j]);
             sum += sd[j];                            // (the mark stays)
         }
         s_h[w][lane] = h;
@@ -118,14 +123,14 @@ __global__ __launch_bounds__(256) void selscan_carry_kernel(const float* __restr
         h = base;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            if (v < w) h = carried(h, s_sum[v][lane], A2, s_h[v][lane]);
-            base = carried(base, s_sum[v][lane], A2, s_h[v][lane]);
+            if (v < w) h = carried(h, s_sum[v][lane], half_A2, s_h[v][lane]);
+            base = carried(base, s_sum[v][lane], half_A2, s_h[v][lane]);
         }
 #pragma unroll
         for (int j = 0; j < AT; ++j) {
             const int o = k + w * AT + j, c = BWD ? n_chunk - 1 - o : o;
             if (o < n_chunk && live) totals[(size_t)c * ND + i] = h;
-            h = carried(h, sd[j], A2, H[j]);
+            h = carried(h, sd[j], half_A2, H[j]);
         }
         __syncthreads();                             // (the sums have been read)
     }
@@ -210,6 +215,14 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
         for (int n = 0; n < N; ++n) h[n] = H[(size_t)n * s.D];
     }
 
+    if (MODE == SCAN_OUT && R.clear) {                       // rows of no sequence
+        const int first = R.n_seq > 0 ? seq_begin(R, 0) : 0, stop = R.n_seq > 0 ? seq_end(R, R.n_seq - 1) : 0;
+        if (t0 < first || t1 > stop)
+#pragma unroll 1
+            for (int r = t0; r < t1; ++r)
+                if (r < first || r >= stop) row_store((IO*)a.Y + (size_t)r * s.D, och, (IO)0.f);
+    }
+
     // (a row's address is the same in all lanes: scalar base, 32-bit lane offset)
     float sum = 0.f;
     bool began = false;
@@ -261,10 +274,7 @@ __global__ __launch_bounds__(64) void selscan_fwd_kernel(ScanFwd a)
                 ++q;
                 if (q < R.n_seq) { beg = seq_begin(R, q); end = seq_end(R, q); }
             }
-            if (r >= t1 || q >= R.n_seq || r < beg) {
-                if (MODE == SCAN_OUT && R.clear && r < t1) row_store(Y, och, (IO)0.f);
-                continue;
-            }
+            if (r >= t1 || q >= R.n_seq || r < beg) continue;
             const int slot = a.S_in || a.S_out ? slot_of(R, q) : -1;
             if (r == beg) {
                 began = true;
@@ -440,6 +450,8 @@ constexpr int NPW = 4, TB = kSelscanTile;         // states of a wave, rows of a
 // A workgroup walks its chunk from the last tile to the first.  Wave w has states 4w .. 4w+3 of the same 64 channels: a tile's
 // decays and states then fit its registers.  The step sizes and the like of a tile are worked out once, by all waves, and shared.
 // Tiles of 8 rows leave room for three waves per SIMD, tiles of 16 for two: 1310 us against 1440 (65536 rows, 1536 channels, 16 states).
+// (With 32 states a workgroup is eight waves of 167 registers, of which a CU holds one: two waves per SIMD.  With 8 and 16 states three waves
+// are had at the price of 23 to 26 and 2 to 4 spilled registers.)
 template <typename IO, int N>
 __global__ __launch_bounds__(N / NPW * 64, 3) void selscan_bwd_kernel(ScanBwd a)
 {
@@ -649,14 +661,7 @@ __global__ __launch_bounds__(N / NPW * 64, 3) void selscan_bwd_kernel(ScanBwd a)
             const int k = w + i * W, r = t + k;
             if (!whole) {
                 const int sr = r < t1 ? seq_of(R, r) : -1;
-                if (sr < 0 || sr >= R.n_seq) {
-                    if (R.clear && r < t1 && live) {
-                        if (Z) row_store(dZ + (size_t)r * s.D, och, (IO)0.f);
-                        row_store(dU + (size_t)r * s.D, och, (IO)0.f);
-                        row_store(dDe + (size_t)r * s.D, och, (IO)0.f);
-                    }
-                    continue;
-                }
+                if (sr < 0 || sr >= R.n_seq) continue;
             }
             float y = 0.f, s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -689,19 +694,31 @@ __global__ __launch_bounds__(N / NPW * 64, 3) void selscan_bwd_kernel(ScanBwd a)
     }
 }
 
-// The waves' sums over their channels, added up and rounded once; rows of no sequence are left as they are, or zeroed.
+// The waves' sums over their channels, added up and rounded once; rows of no sequence are left as they are.  R.clear: all gradients of these are
+// zeroed here (in the walk that would be 1 % of its time, whether there are any or not).
 template <typename IO>
 __global__ __launch_bounds__(256) void selscan_bc_kernel(Rows R, const float* __restrict__ part, int nb, int N, int G, IO* __restrict__ dB,
-                                                        IO* __restrict__ dC)
+                                                        IO* __restrict__ dC, int D, IO* __restrict__ dU, IO* __restrict__ ddelta,
+                                                        IO* __restrict__ dZ)
 {
     const long n = (long)R.T * G * 2 * N;
-    const long first = R.n_seq > 0 ? (long)seq_begin(R, 0) * G * 2 * N : 0, stop = R.n_seq > 0 ? (long)seq_end(R, R.n_seq - 1) * G * 2 * N : 0;
+    const int begin = R.n_seq > 0 ? seq_begin(R, 0) : 0, end = R.n_seq > 0 ? seq_end(R, R.n_seq - 1) : 0;
+    const long first = (long)begin * G * 2 * N, stop = (long)end * G * 2 * N;
+    if (R.clear && (begin > 0 || end < R.T)) {
+        const long maps = (long)G * N;
+        for (int r = blockIdx.x; r < R.T; r += gridDim.x) {
+            if (r >= begin && r < end) continue;
+            for (long i = threadIdx.x; i < D; i += 256) {
+                dU[(size_t)r * D + i] = ddelta[(size_t)r * D + i] = (IO)0.f;
+                if (dZ) dZ[(size_t)r * D + i] = (IO)0.f;
+            }
+            for (long i = threadIdx.x; i < maps; i += 256) dB[(size_t)r * maps + i] = dC[(size_t)r * maps + i] = (IO)0.f;
+        }
+    }
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
-        const bool on = i >= first && i < stop;
-        if (!on && !R.clear) continue;
+        if (i < first || i >= stop) continue;
         float x = 0.f;
-        if (on)
-            for (int b = 0; b < nb; ++b) x += part[(size_t)b * n + i];
+        for (int b = 0; b < nb; ++b) x += part[(size_t)b * n + i];
         const int k = (int)(i % (2 * N));
         const long tg = i / (2 * N);
         if (k < N) dB[tg * N + k] = from_f<IO>(x);
@@ -745,12 +762,12 @@ __global__ __launch_bounds__(64) void selscan_step_kernel(SelscanArgs a, int eac
 #pragma unroll
     for (int n = 0; n < N; ++n) A2[n] = a.A[(size_t)n * a.D + ch] * kLog2e;
     const float bias = a.delta_bias ? a.delta_bias[ch] : 0.f, skip = a.Dskip ? a.Dskip[ch] : 0.f;
+    if (a.rows.clear)
+        for (int r = r0; r < r1; ++r)
+            if (slot_of(a.rows, r) < 0) ((IO*)a.Y)[(size_t)r * a.D + ch] = (IO)0.f;
     for (int r = r0; r < r1; ++r) {
         const int slot = slot_of(a.rows, r);
-        if (slot < 0) {
-            if (a.rows.clear) ((IO*)a.Y)[(size_t)r * a.D + ch] = (IO)0.f;
-            continue;
-        }
+        if (slot < 0) continue;
         float* S = a.S_out + (size_t)slot * ND + ch;
         const IO *Bm = (const IO*)a.Bm + (size_t)r * a.ldb + (size_t)g * N, *Cm = (const IO*)a.Cm + (size_t)r * a.ldc + (size_t)g * N;
         float h[N];
@@ -952,7 +969,7 @@ static hipError_t bwd(const SelscanArgs& a, const SelscanPlan& p, char* ws, hipS
         long blocks = (n + 255) / 256;
         if (blocks > 8192) blocks = 8192;
         hipLaunchKernelGGL(selscan_bc_kernel<IO>, dim3((unsigned)blocks), dim3(256), 0, st, a.rows, b.part_bc, b.s.nb, N, a.G, (IO*)a.dB,
-                           (IO*)a.dC);
+                           (IO*)a.dC, a.D, (IO*)a.dU, (IO*)a.ddelta, a.Z ? (IO*)a.dZ : nullptr);
     }
     hipLaunchKernelGGL(selscan_params_kernel, dim3((unsigned)((a.D + 63) / 64), N + 2), dim3(1024), 0, st, b.part_A, b.part_D, p.n_chunk, N,
                        a.D, a.dA, a.dDskip, a.dbias);

@@ -146,6 +146,18 @@ __global__ __launch_bounds__(256) void short_conv_state_kernel(ShortConvArgs a)
     state_behind<IO, M>(a, blockIdx.x / nb, blockIdx.x % nb);
 }
 
+// Rows t0 .. t1 - 1 of no sequence: those in front of `front`, which the walk from t0 began with, and where it has come past the last
+// sequence those behind it.  (Behind the walk: a store in it costs registers that it needs.)
+template <typename IO, int V>
+__device__ __forceinline__ void clear_rows(const Rows& R, int front, const Where& at, void* Y, int D, int t0, int t1, int ch)
+{
+    if (t0 >= front && at.q < R.n_seq) return;
+    const int stop = at.q < R.n_seq ? R.T : R.n_seq > 0 ? seq_end(R, R.n_seq - 1) : 0;
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t)
+        if (t < front || t >= stop) row_store((Raw<IO, V>*)((IO*)Y + (size_t)t * D), ch * sizeof(IO), Raw<IO, V>(0));
+}
+
 // Workgroups go to the eight XCDs in turn: the neighbours in memory, which read each other's last rows, to one of them.
 __device__ __forceinline__ int xcd_neighbours(int i, int n)
 {
@@ -203,15 +215,16 @@ __global__ __launch_bounds__(256) void short_conv_kernel(ShortConvArgs a)
         return;
     }
     int known = -1;                                   // the sequence that `back` is of
+    const int front = at.beg;
 #pragma unroll 1
     for (int t = t0; t < t1; ++t) {
         const bool on = at.at(R, t);
         if (on && known != at.q) { in_front<IO, V, M>(a, at, t, ch, back); known = at.q; }
         row(x[M - 1], on ? (IO*)a.Y + (size_t)t * a.D : nullptr);
-        if (!on && R.clear) row_store((Raw<IO, V>*)((IO*)a.Y + (size_t)t * a.D), ch * sizeof(IO), Raw<IO, V>(0));
 #pragma unroll
         for (int i = M - 1; i < RUN + M - 2; ++i) x[i] = x[i + 1];
     }
+    if (R.clear) clear_rows<IO, V>(R, front, at, a.Y, a.D, t0, t1, ch);
 }
 
 // One row for each of R requests: the states move on by one.
@@ -333,6 +346,7 @@ __global__ __launch_bounds__(256) void short_conv_bwd_kernel(ShortConvArgs a, in
             continue;
         }
         int known = -1;
+        const int front = at.beg;
         // rows t1 .. t1 + m - 2 of the same sequence give to the rows of this run too
 #pragma unroll 1
         for (int t = t0; t - t1 < M - 1; ++t) {
@@ -342,11 +356,7 @@ __global__ __launch_bounds__(256) void short_conv_bwd_kernel(ShortConvArgs a, in
             for (int i = M - 1; i < RUN + 2 * (M - 1) - 1; ++i) xs[i] = xs[i + 1];
 #pragma unroll
             for (int i = 0; i < RUN + M - 2; ++i) dys[i] = dys[i + 1];
-            if (t < t1 && !at.at(R, t)) {
-                if (R.clear) row_store((Raw<IO, V>*)((IO*)a.dX + (size_t)t * a.D), ch * sizeof(IO), Raw<IO, V>(0));
-                next_x(xr);
-                continue;
-            }
+            if (t < t1 && !at.at(R, t)) { next_x(xr); continue; }
             if (known != at.q) {
                 known = at.q;
                 in_front<IO, V, M>(a, at, t, ch, back);
@@ -378,6 +388,7 @@ __global__ __launch_bounds__(256) void short_conv_bwd_kernel(ShortConvArgs a, in
                 else if (slot >= 0) store_row<IO, V>((IO*)a.dS_in + ((size_t)slot * (M - 1) + (M - 1 + r - at.beg)) * a.D + ch, g);
             }
         }
+        if (R.clear) clear_rows<IO, V>(R, front, at, a.dX, a.D, t0, t1, ch);
     }
     float* part = a.part + (size_t)blockIdx.y * (M + 1) * a.D + ch;
 #pragma unroll
