@@ -7,7 +7,7 @@
 //
 // Memory-bound: a row stays in the registers of TPR threads between its two norms, so every tensor is read or written once.  65536 rows of
 // 768, bf16: forward 90 us (5.6 TB/s; one row per wave and the gains with every row: 106), gradient 145 us (5.5 TB/s; without the next
-// row on its way 271); 6007 rows of 1531, fp32: 34 and 53 us (5.5 TB/s).
+// row on its way 271), with the stream in fp32 125 and 219 us (5.6 and 5.1 TB/s); 6007 rows of 1531, fp32: 34 and 53 us (5.5 TB/s).
 #include "chela_rows.h"
 
 namespace chela {

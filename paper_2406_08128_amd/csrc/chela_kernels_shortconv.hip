@@ -7,8 +7,8 @@
 //
 // Memory-bound: a thread owns two neighbouring channels where the rows allow it and walks a run of rows with the last m - 1 inputs in
 // registers, so a row is read once (and m - 1 rows more per run, from the L2).  65536 rows of 1536 channels, 4 taps, bf16: forward 74 us
-// (5.5 TB/s), gradient 135 + 8 us (4.3 TB/s).  Eight channels per thread, 16 bytes of a row, took 107 and 178: their weights lie 128
-// bytes apart from lane to lane, more lines than all the rows have.
+// (5.5 TB/s), gradient 135 + 8 us (4.3 TB/s); fp32 146 us (5.5 TB/s) and 255 (4.7).  Eight channels per thread, 16 bytes of a row, took
+// 107 and 178 in bf16: their weights lie 128 bytes apart from lane to lane, more lines than all the rows have.
 #include "chela_rows.h"
 
 namespace chela {
