@@ -749,7 +749,7 @@ __global__ __launch_bounds__(1024) void selscan_params_kernel(const float* __res
 
 // ------------------------------------------------------------------------------------------------------------ single tokens
 // A wave has 64 channels of `each` requests: what a channel has once (16 decays, 4 KB a wave, as many bytes as its state) is read once.  A request's
-// loads all come before its stores.  256 requests of 1536 channels, 16 states: 11.2 us, 4.8 TB/s of states read and written; one request 5.5.
+// loads all come before its stores.  256 requests of 1536 channels, 16 states: 11.3 us, 4.7 TB/s of states read and written; one request 5.5.
 template <typename IO, int N>
 __global__ __launch_bounds__(64) void selscan_step_kernel(SelscanArgs a, int each)
 {
