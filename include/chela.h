@@ -67,7 +67,7 @@ enum {
     CHELA_OK                  = 0,
     CHELA_ERR_NULL_POINTER    = -1, /* a tensor pointer is NULL while B*H*N > 0            */
     CHELA_ERR_BAD_SHAPE       = -2, /* B, H or N negative, element count overflows, sizes that do not go together */
-    CHELA_ERR_UNSUPPORTED_DIM = -3, /* dk or dv not in {64, 128}; selective scan: N not in {8, 16, 32}; block norm: D above 8192 */
+    CHELA_ERR_UNSUPPORTED_DIM = -3, /* dk or dv not in {64, 128}; selective scan: N not in {8, 16, 32}; block and layer norm: D above 8192 */
     CHELA_ERR_BAD_CHUNK       = -4, /* chunk not in the supported set for this dtype       */
     CHELA_ERR_MISALIGNED      = -5, /* a tensor pointer is not 16-byte aligned             */
     CHELA_ERR_ALIASING        = -6, /* an output range overlaps an input or another output */
@@ -305,8 +305,8 @@ int chela_linattn_step_gated(const void *q, const void *k, const void *v, const 
                              int B, int H, int dk, int dv, void *stream);
 
 /* ---- operators on rows: a token's channels next to each other, as a projection leaves them ------------------------
- * Three operators of a selective state space block, the other linear-time token mixer: its short causal convolution, its
- * scan, and the norms around a block.  Common to the first two:
+ * Operators of two other linear-time token mixers: a selective scan and a gated delta rule, the short causal convolution in front of
+ * either, and the norms around a block.  Common to the first three:
  *   rows     : [T, D] tensors of T tokens, bf16 (plain name) or fp32 (_f32); arithmetic and sums are fp32 for either, outputs are
  *              rounded once.  A tensor that comes with a row stride (ld..., elements from a token to the next, at least the
  *              row's width, below 2^29) may be a slice of a wider one and needs only its elements' alignment; all others are contiguous
@@ -445,6 +445,78 @@ size_t chela_selscan_saved_bytes(int T, int D, int N);
 /* is_bwd: of the backward call; has_saved: given `saved`. */
 size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int has_saved);
 
+/* Gated delta rule: a state of dk x dv per value head that decays, and takes in of a token's value what it does not give back for the
+ * token's key already.  H value heads, Hk key heads, Hk divides H, value head h has key head h / (H / Hk); dk, dv in {64, 128}:
+ *     S' = e^(g_t) S_{t-1},   S_t = S' + beta_t k_t (v_t - S'^T k_t)^T,   o_t = scale S_t^T q_t.
+ * Nothing is normalised: keys of length one and beta in [0, 1] keep the state bounded (chela_block_norm_fwd with w_pre = dk^-1/2 makes rows of
+ * length one).  A log decay g of -infinity empties the state; one below -256 does the same.
+ *   Q, K [T, Hk, dk], V, O [T, H, dv], g (NULL: no decay), beta [T, H] in the I/O type, with row strides; states [n_slots, H, dk, dv] fp32; scale
+ *   is a finite constant.  Rows are taken 64 (bf16) or 32 (fp32) of a sequence at a time: what is not finite in one reaches the rows in front of
+ *   it in the same 64 or 32 too, and never another sequence.  bf16: the states, their gradients and everything that goes into them are held to 16
+ *   bits or more; for outputs and gradients in bf16 the matrix operands that they are made of (states, inner values, scores) are rounded to bf16.
+ *   fwd  : O.  saved: NULL, or a caller-owned buffer of chela_gated_delta_saved_bytes() bytes (16-byte aligned, opaque) that carries what the
+ *          backward call needs of the chunks (states and inverses).
+ *   bwd  : dQ, dK [T, Hk, dk] (sums over a key head's value heads), dV [T, H, dv], dg (NULL without g), dbeta [T, H] in the I/O type, dS_in
+ *          [n_seq, H, dk, dv] fp32 (NULL: not wanted), for the upstream dO [T, H, dv] and dS_out (fp32, NULL: zero).  saved: as the forward
+ *          call with the same inputs left it, or NULL: worked out again.  Sums are taken in a fixed order.
+ *   step : one row for each of R requests; S [n_slots, H, dk, dv] is updated in place.
+ * Limits beside those above (D: H dk): T H dk / 64 < 2^26, n_seq H dv / 16 and R H dv / 16 < 2^23.  `packed` in the queries: cu is given. */
+int chela_gated_delta_fwd(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                          const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                          const int *cu, int n_seq, int T, int H, int Hk, int dk, int dv, const float *S_in,
+                          float *S_out, const int *slots, int n_slots, void *O, void *saved, void *stream);
+int chela_gated_delta_bwd(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                          const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                          const int *cu, int n_seq, int T, int H, int Hk, int dk, int dv, const float *S_in,
+                          const void *dO, long long lddo, const float *dS_out, const void *saved, void *dQ, void *dK,
+                          void *dV, void *dg, void *dbeta, float *dS_in, void *stream);
+int chela_gated_delta_step(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                           const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                           float *S, const int *slots, int n_slots, int R, int H, int Hk, int dk, int dv, void *o,
+                           void *stream);
+int chela_gated_delta_fwd_f32(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                              const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                              const int *cu, int n_seq, int T, int H, int Hk, int dk, int dv, const float *S_in,
+                              float *S_out, const int *slots, int n_slots, void *O, void *saved, void *stream);
+int chela_gated_delta_bwd_f32(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                              const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                              const int *cu, int n_seq, int T, int H, int Hk, int dk, int dv, const float *S_in,
+                              const void *dO, long long lddo, const float *dS_out, const void *saved, void *dQ, void *dK,
+                              void *dV, void *dg, void *dbeta, float *dS_in, void *stream);
+int chela_gated_delta_step_f32(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                               const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                               float *S, const int *slots, int n_slots, int R, int H, int Hk, int dk, int dv, void *o,
+                               void *stream);
+int chela_gated_delta_fwd_cleared(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                                  const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                                  const int *cu, int n_seq, int T, int H, int Hk, int dk, int dv, const float *S_in,
+                                  float *S_out, const int *slots, int n_slots, void *O, void *saved, void *stream);
+int chela_gated_delta_bwd_cleared(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                                  const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                                  const int *cu, int n_seq, int T, int H, int Hk, int dk, int dv, const float *S_in,
+                                  const void *dO, long long lddo, const float *dS_out, const void *saved, void *dQ, void *dK,
+                                  void *dV, void *dg, void *dbeta, float *dS_in, void *stream);
+int chela_gated_delta_step_cleared(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                                   const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                                   float *S, const int *slots, int n_slots, int R, int H, int Hk, int dk, int dv, void *o,
+                                   void *stream);
+int chela_gated_delta_fwd_cleared_f32(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                                      const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                                      const int *cu, int n_seq, int T, int H, int Hk, int dk, int dv, const float *S_in,
+                                      float *S_out, const int *slots, int n_slots, void *O, void *saved, void *stream);
+int chela_gated_delta_bwd_cleared_f32(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                                      const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                                      const int *cu, int n_seq, int T, int H, int Hk, int dk, int dv, const float *S_in,
+                                      const void *dO, long long lddo, const float *dS_out, const void *saved, void *dQ, void *dK,
+                                      void *dV, void *dg, void *dbeta, float *dS_in, void *stream);
+int chela_gated_delta_step_cleared_f32(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
+                                       const void *g, long long ldg, const void *beta, long long ldb, float scale,
+                                       float *S, const int *slots, int n_slots, int R, int H, int Hk, int dk, int dv, void *o,
+                                       void *stream);
+size_t chela_gated_delta_saved_bytes(int T, int n_seq, int packed, int H, int dk, int dv, int dtype);
+size_t chela_gated_delta_workspace_bytes(int T, int n_seq, int packed, int H, int dk, int dv, int dtype, int is_bwd,
+                                         int has_saved);
+
 /* Norms before and after a block, with its gate and the residual, in one pass over `rows` contiguous rows of D features
  * (1 <= D <= 8192):
  *     X_out = X + scale * Norm(Y) * w_post * gate      (w_post NULL: scale * Y * gate; gate NULL: 1)
@@ -469,6 +541,25 @@ int chela_block_norm_bwd_f32(const void *Y, const void *gate, const void *X, con
                              const void *dX_out, const void *dN, void *dY, void *dgate, void *dX, float *dw_post, float *dw_pre,
                              float scale, float eps, long long rows, int D, int x_f32, void *stream);
 size_t chela_block_norm_bwd_workspace_bytes(long long rows, int D);
+
+/* Layer norm of `rows` contiguous rows of D features (1 <= D <= 8192), behind the addition of a block's output to the residual stream:
+ *     X_out = X + Y   (Y NULL: X, and X_out is not looked at),
+ *     Nrm = (X_out - m) / sqrt(mean_j (X_out_j - m)^2 + eps) * w + b,   m = mean_j X_out_j   (w NULL: 1; b NULL: 0)
+ * over the row; eps >= 0 is a finite constant.  Statistics are fp32, the squares are taken behind the mean, and of X_out before it is rounded.
+ *   Y, Nrm: bf16 (plain name) or fp32 (_f32); X, X_out: the same, or fp32 beside bf16 (x_f32 != 0).  w, b [D] fp32.  X_out may be X (exactly
+ *   the same pointer; then Y may be there too where its type is X's).
+ *   bwd: from X, the stream as the forward call left it (its X_out; without Y its X), for the upstream gradients dX_out (type of X; NULL: zero) and
+ *   dN: dX (type of X; the gradient of X and of Y; may be dX_out, exactly the same pointer, where then X and, of X's type, dN may be too), dw
+ *   and db [D] fp32 (each NULL: not wanted).  Sums over rows are taken in a fixed order.  rows = 0: dw and db are zeroed. */
+int chela_layer_norm_fwd(const void *X, const void *Y, const float *w, const float *b, void *X_out, void *Nrm, float eps,
+                         long long rows, int D, int x_f32, void *stream);
+int chela_layer_norm_bwd(const void *X, const float *w, const void *dX_out, const void *dN, void *dX, float *dw, float *db,
+                         float eps, long long rows, int D, int x_f32, void *stream);
+int chela_layer_norm_fwd_f32(const void *X, const void *Y, const float *w, const float *b, void *X_out, void *Nrm, float eps,
+                             long long rows, int D, int x_f32, void *stream);
+int chela_layer_norm_bwd_f32(const void *X, const float *w, const void *dX_out, const void *dN, void *dX, float *dw, float *db,
+                             float eps, long long rows, int D, int x_f32, void *stream);
+size_t chela_layer_norm_bwd_workspace_bytes(long long rows, int D);
 
 /* Bytes of device scratch one call with these arguments needs, with or without
  * carried states (0 if the arguments are invalid; the training pair has its own query,

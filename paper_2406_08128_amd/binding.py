@@ -36,8 +36,10 @@ _fn = dict.fromkeys(("linattn_fwd", "linattn_fwd_f32", "linattn_fwd_state", "lin
                      "shortlong_conv_fwd_f32", "shortlong_conv_bwd", "shortlong_conv_bwd_f32", "short_conv_fwd", "short_conv_fwd_f32",
                      "short_conv_step", "short_conv_step_f32", "selscan_fwd", "selscan_fwd_f32", "selscan_step", "selscan_step_f32",
                      "selscan_saved_bytes", "block_norm_fwd", "block_norm_fwd_f32", "short_conv_bwd", "short_conv_bwd_f32", "selscan_bwd",
-                     "selscan_bwd_f32", "block_norm_bwd", "block_norm_bwd_f32",
-                     *("%s_%s_cleared%s" % (op, call, sfx) for op in ("short_conv", "selscan") for call in ("fwd", "bwd", "step")
+                     "selscan_bwd_f32", "block_norm_bwd", "block_norm_bwd_f32", "gated_delta_saved_bytes",
+                     *("%s_%s%s" % (op, call, sfx) for op, calls in (("gated_delta", ("fwd", "bwd", "step")), ("layer_norm", ("fwd", "bwd")))
+                       for call in calls for sfx in ("", "_f32")),
+                     *("%s_%s_cleared%s" % (op, call, sfx) for op in ("short_conv", "selscan", "gated_delta") for call in ("fwd", "bwd", "step")
                        for sfx in ("", "_f32"))), 0)
 
 
@@ -129,6 +131,7 @@ def lib() -> ctypes.CDLL:
     ll = ctypes.c_longlong
     conv = [vp, ll, vp, i, vp, i]                                    # X, ldx, w, m, bias, silu
     scan = [vp, ll, vp, ll, vp, vp, ll, vp, ll, vp, vp, ll, vp, i]   # U, delta, A, Bm, Cm, Dskip, Z, delta_bias, softplus
+    delta = [vp, ll] * 5 + [f32]                                     # Q, K, V, g, beta, scale
     for sfx in ("", "_f32"):
         for name, args in (("chela_short_conv_fwd", conv + [vp, i, i, i, vp, vp, vp, i, vp, vp]),
                            ("chela_short_conv_bwd", conv + [vp, i, i, i, vp, vp, ll, vp, vp, vp, vp, vp, vp]),
@@ -136,6 +139,11 @@ def lib() -> ctypes.CDLL:
                            ("chela_selscan_fwd", scan + [vp, i, i, i, i, i, vp, vp, vp, i, vp, vp, vp]),
                            ("chela_selscan_bwd", scan + [vp, i, i, i, i, i, vp, vp, ll] + [vp] * 12),
                            ("chela_selscan_step", scan + [vp, vp, i, i, i, i, i, vp, vp]),
+                           ("chela_gated_delta_fwd", delta + [vp, i, i, i, i, i, i, vp, vp, vp, i, vp, vp, vp]),
+                           ("chela_gated_delta_bwd", delta + [vp, i, i, i, i, i, i, vp, vp, ll] + [vp] * 9),
+                           ("chela_gated_delta_step", delta + [vp, vp, i, i, i, i, i, i, vp, vp]),
+                           ("chela_layer_norm_fwd", [vp] * 6 + [f32, ll, i, i, vp]),
+                           ("chela_layer_norm_bwd", [vp] * 7 + [f32, ll, i, i, vp]),
                            ("chela_block_norm_fwd", [vp] * 7 + [f32, f32, ll, i, i, vp]),
                            ("chela_block_norm_bwd", [vp] * 12 + [f32, f32, ll, i, i, vp])):
             for form in ("",) if "norm" in name else ("", "_cleared"):
@@ -146,7 +154,11 @@ def lib() -> ctypes.CDLL:
     L.chela_selscan_saved_bytes.argtypes = [i, i, i]
     L.chela_selscan_workspace_bytes.argtypes = [i] * 6
     L.chela_block_norm_bwd_workspace_bytes.argtypes = [ll, i]
-    for name in ("chela_short_conv_bwd", "chela_selscan", "chela_block_norm_bwd"):
+    L.chela_gated_delta_saved_bytes.argtypes = [i] * 7
+    L.chela_gated_delta_saved_bytes.restype = sz
+    L.chela_gated_delta_workspace_bytes.argtypes = [i] * 9
+    L.chela_layer_norm_bwd_workspace_bytes.argtypes = [ll, i]
+    for name in ("chela_short_conv_bwd", "chela_selscan", "chela_block_norm_bwd", "chela_gated_delta", "chela_layer_norm_bwd"):
         getattr(L, name + "_workspace_bytes").restype = sz
     L.chela_selscan_saved_bytes.restype = sz
     L.chela_linattn_step.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, vp]
@@ -824,9 +836,14 @@ def _sequences(X, cu, name):
         return None, (X.shape[0] if X.dim() == 3 else 1), X.shape[:-1].numel(), X.shape[-1]
     if X.dim() != 2:
         raise ValueError("with cu, %s is [T, D]" % name)
+    return (*_offsets(cu, X), X.shape[0], X.shape[1])
+
+
+def _offsets(cu, X):
+    """(offsets' address, sequences) of packed rows."""
     if cu.dim() != 1 or cu.shape[0] < 1 or cu.dtype != torch.int32 or cu.device != X.device or not cu.is_contiguous():
         raise ValueError("cu must be a contiguous int32 device tensor of the sequences' n_seq + 1 offsets")
-    return cu.data_ptr(), cu.shape[0] - 1, X.shape[0], X.shape[1]
+    return cu.data_ptr(), cu.shape[0] - 1
 
 
 def _dense(t, shape, dtype, device, name):
@@ -1048,6 +1065,116 @@ def chela_selscan_workspace_bytes(T, D, N, G, is_bwd, has_saved=False) -> int:
     return int(lib().chela_selscan_workspace_bytes(T, D, N, G, int(bool(is_bwd)), int(bool(has_saved))))
 
 
+def _delta_inputs(Q, K, V, g, beta, scale, cu):
+    """The arguments that the three calls of the gated delta rule begin with, then (lead, offsets' address, sequences, rows, H, Hk, dk, dv)."""
+    if not V.is_cuda or V.dim() not in (3, 4) or (cu is not None and V.dim() != 3):
+        raise ValueError("V must be a device tensor [B, L, H, dv], or [T, H, dv] with cu or of one sequence")
+    lead, (H, dv) = V.shape[:-2], V.shape[-2:]
+    if Q.dim() != V.dim() or Q.shape[:-2] != lead or K.shape != Q.shape:
+        raise ValueError("Q and K must be [..., Hk, dk] with V's rows")
+    Hk, dk = Q.shape[-2:]
+    if beta.shape != lead + (H,) or (g is not None and g.shape != lead + (H,)):
+        raise ValueError("g and beta must be [..., H] with V's rows")
+    if Hk < 1 or H % Hk != 0:
+        raise ValueError("the key heads must divide the value heads")
+    args = []
+    for t, name in ((Q, "Q"), (K, "K"), (V, "V"), (g, "g"), (beta, "beta")):
+        args += _row_stride(t, beta, name, V.dtype) if t is not None else (None, 0)
+    args.append(float(scale))
+    if cu is None:
+        pcu, n_seq = None, lead[0] if len(lead) == 2 else 1
+    else:
+        pcu, n_seq = _offsets(cu, V)
+    return args, lead, pcu, n_seq, lead.numel(), H, Hk, dk, dv
+
+
+def chela_gated_delta_fwd(Q, K, V, g, beta, scale=1.0, cu=None, S_in=None, S_out=None, slots=None, want_saved=False, O=None, stream=None):
+    """(O, saved): the gated delta rule S = exp(g) S, S += beta k (v - S^T k)^T, o = scale S^T q over the tokens of each sequence.
+    Q, K [..., Hk, dk], V [..., H, dv], g (None: no decay) and beta [..., H]; Hk divides H; states [n_slots, H, dk, dv] float32.  saved is None
+    unless asked for (for chela_gated_delta_bwd).  Rows of no sequence: zero in a new O, left as they are in one that is given."""
+    name = "gated_delta_fwd" if cu is None or O is not None else "gated_delta_fwd_cleared"
+    r = _host("gated_delta_fwd")(_fn[name], _fn[name + "_f32"], _fn["gated_delta_saved_bytes"], Q, K, V, g, beta, scale, cu, S_in, S_out,
+                                 slots, want_saved, O, stream)
+    if r is not None:
+        return _host_result(r)
+    args, lead, pcu, n_seq, T, H, Hk, dk, dv = _delta_inputs(Q, K, V, g, beta, scale, cu)
+    sfx, kind = _suffix(V)
+    dev = V.device
+    pslots, n_slots = _slot_map(slots, n_seq, S_in if S_in is not None else S_out, dev)
+    st = (n_slots, H, dk, dv)
+    ps_in, ps_out = _dense(S_in, st, torch.float32, dev, "S_in"), _dense(S_out, st, torch.float32, dev, "S_out")
+    if O is None:
+        O = torch.empty(V.shape, dtype=V.dtype, device=dev)
+    saved = None
+    if want_saved:
+        saved = torch.empty(max(chela_gated_delta_saved_bytes(T, n_seq, cu is not None, H, dk, dv, kind), 16) // 4, dtype=torch.float32,
+                            device=dev)
+    with _on(V):
+        _check(getattr(lib(), "chela_" + name + sfx)(
+            *args, pcu, n_seq, T, H, Hk, dk, dv, ps_in, ps_out, pslots, n_slots, _dense(O, V.shape, V.dtype, dev, "O"), _ptr(saved),
+            _stream_ptr(stream)))
+    return O, saved
+
+
+def chela_gated_delta_bwd(Q, K, V, g, beta, dO, scale=1.0, cu=None, S_in=None, dS_out=None, want_dS_in=False, saved=None, stream=None):
+    """(dQ, dK, dV, dg, dbeta, dS_in) of chela_gated_delta_fwd (without slots) for the upstream gradients dO and dS_out; dg is None without
+    g, dS_in unless asked for.  saved: the forward call's on the same inputs, or None.  Gradients of rows of no sequence are zero."""
+    name = "gated_delta_bwd" if cu is None else "gated_delta_bwd_cleared"
+    r = _host("gated_delta_bwd")(_fn[name], _fn[name + "_f32"], _fn["gated_delta_saved_bytes"], Q, K, V, g, beta, dO, scale, cu, S_in, dS_out,
+                                 want_dS_in, saved, stream)
+    if r is not None:
+        return _host_result(r)
+    args, lead, pcu, n_seq, T, H, Hk, dk, dv = _delta_inputs(Q, K, V, g, beta, scale, cu)
+    sfx, kind = _suffix(V)
+    dev = V.device
+    if dO.shape != V.shape:
+        raise ValueError("dO must match V")
+    pdo, lddo = _row_stride(dO, beta, "dO", V.dtype)
+    st = (n_seq, H, dk, dv)
+    ps, pds = _dense(S_in, st, torch.float32, dev, "S_in"), _dense(dS_out, st, torch.float32, dev, "dS_out")
+    if saved is not None and (saved.dtype != torch.float32 or saved.device != dev or not saved.is_contiguous()
+                              or saved.numel() * 4 < chela_gated_delta_saved_bytes(T, n_seq, cu is not None, H, dk, dv, kind)):
+        raise ValueError("saved must be what chela_gated_delta_fwd returned for these sizes")
+    dQ, dK, dV, dg, dbeta = (torch.empty(t.shape, dtype=t.dtype, device=dev) if t is not None else None for t in (Q, K, V, g, beta))
+    dS_in = torch.empty(st, dtype=torch.float32, device=dev) if want_dS_in else None
+    with _on(V):
+        _check(getattr(lib(), "chela_" + name + sfx)(
+            *args, pcu, n_seq, T, H, Hk, dk, dv, ps, pdo, lddo, pds, _ptr(saved), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), _ptr(dg),
+            dbeta.data_ptr(), _ptr(dS_in), _stream_ptr(stream)))
+    return dQ, dK, dV, dg, dbeta, dS_in
+
+
+def chela_gated_delta_step(q, k, v, g, beta, S, scale=1.0, slots=None, o=None, stream=None):
+    """One token for each of R requests, q, k [R, Hk, dk], v [R, H, dv], g (or None), beta [R, H]: o as chela_gated_delta_fwd's, the states
+    S [n_slots, H, dk, dv] are updated in place.  A row whose slot is not one of S's is left out: o keeps what it holds there, a new o is zero."""
+    name = "gated_delta_step" if slots is None or o is not None else "gated_delta_step_cleared"
+    r = _host("gated_delta_step")(_fn[name], _fn[name + "_f32"], q, k, v, g, beta, S, scale, slots, o, stream)
+    if r is not None:
+        return _host_result(r)
+    if not v.is_cuda or v.dim() != 3:
+        raise ValueError("v must be a device tensor [R, H, dv]")
+    args, lead, _, _, R, H, Hk, dk, dv = _delta_inputs(q, k, v, g, beta, scale, None)
+    sfx, _ = _suffix(v)
+    dev = v.device
+    pslots, n_slots = _slot_map(slots, R, S, dev)
+    if o is None:
+        o = torch.empty((R, H, dv), dtype=v.dtype, device=dev)
+    with _on(v):
+        _check(getattr(lib(), "chela_" + name + sfx)(
+            *args, _dense(S, (n_slots, H, dk, dv), torch.float32, dev, "S"), pslots, n_slots, R, H, Hk, dk, dv,
+            _dense(o, (R, H, dv), v.dtype, dev, "o"), _stream_ptr(stream)))
+    return o
+
+
+def chela_gated_delta_saved_bytes(T, n_seq, packed, H, dk, dv, dtype) -> int:
+    return int(lib().chela_gated_delta_saved_bytes(T, n_seq, int(bool(packed)), H, dk, dv, int(dtype)))
+
+
+def chela_gated_delta_workspace_bytes(T, n_seq, packed, H, dk, dv, dtype, is_bwd, has_saved=False) -> int:
+    return int(lib().chela_gated_delta_workspace_bytes(T, n_seq, int(bool(packed)), H, dk, dv, int(dtype), int(bool(is_bwd)),
+                                                       int(bool(has_saved))))
+
+
 def _norm_inputs(Y, X, gate, w_post, w_pre):
     """(suffix, rows, D, whether X is fp32 beside bf16, addresses of Y, gate, X, w_post, w_pre)."""
     if not X.is_cuda or X.dim() < 1 or not X.is_contiguous():
@@ -1113,6 +1240,65 @@ def chela_block_norm_bwd(Y, X_out, dX_out, dN, gate=None, w_post=None, w_pre=Non
 
 def chela_block_norm_bwd_workspace_bytes(rows, D) -> int:
     return int(lib().chela_block_norm_bwd_workspace_bytes(rows, D))
+
+
+def _layer_norm_inputs(X, io, w, b):
+    """(suffix, rows, D, whether X is fp32 beside bf16, addresses of w and b)."""
+    if not X.is_cuda or X.dim() < 1 or not X.is_contiguous():
+        raise ValueError("X must be a contiguous device tensor [..., D]")
+    D, dev = X.shape[-1], X.device
+    if io not in (torch.bfloat16, torch.float32) or X.dtype not in (io, torch.float32):
+        raise TypeError("layer norm: tensors must be bfloat16 or float32, X float32 beside bfloat16")
+    return ("" if io == torch.bfloat16 else "_f32", (X.numel() // D if D else 0), D, int(X.dtype != io),
+            _dense(w, (D,), torch.float32, dev, "w"), _dense(b, (D,), torch.float32, dev, "b"))
+
+
+def chela_layer_norm_fwd(X, w=None, b=None, Y=None, eps=1e-5, X_out=None, Nrm=None, stream=None):
+    """(X_out, Nrm): X_out = X + Y (Y None: X itself), Nrm = (X_out - mean) / sqrt(var + eps) * w + b over the last dimension, in Y's dtype or,
+    without Y, in Nrm's or X's.  w, b [D] float32 or None.  X_out may be X."""
+    if X_out is None and Nrm is None:
+        r = _host("layer_norm_fwd")(_fn["layer_norm_fwd"], _fn["layer_norm_fwd_f32"], X, w, b, Y, eps, stream)
+        if r is not None:
+            return _host_result(r)
+    io = Y.dtype if Y is not None else Nrm.dtype if Nrm is not None else X.dtype
+    sfx, rows, D, x_f32, pw, pb = _layer_norm_inputs(X, io, w, b)
+    dev = X.device
+    py = _dense(Y, X.shape, io, dev, "Y")
+    if Y is None:
+        X_out = X
+    elif X_out is None:
+        X_out = torch.empty_like(X)
+    if Nrm is None:
+        Nrm = torch.empty(X.shape, dtype=io, device=dev)
+    with _on(X):
+        _check(getattr(lib(), "chela_layer_norm_fwd" + sfx)(
+            X.data_ptr(), py, pw, pb, _dense(X_out, X.shape, X.dtype, dev, "X_out"), _dense(Nrm, X.shape, io, dev, "Nrm"), float(eps), rows, D,
+            x_f32, _stream_ptr(stream)))
+    return X_out, Nrm
+
+
+def chela_layer_norm_bwd(X_out, dN, w=None, want_db=False, dX_out=None, eps=1e-5, in_place=False, stream=None):
+    """(dX, dw, db) of chela_layer_norm_fwd from its X_out (without Y: its X), for the upstream gradients dN and dX_out (None: zero); dX is the
+    gradient of X and of Y; dw is None without w, db unless asked for.  in_place=True writes dX over dX_out."""
+    r = _host("layer_norm_bwd")(_fn["layer_norm_bwd"], _fn["layer_norm_bwd_f32"], X_out, dN, w, want_db, dX_out, eps, in_place, stream)
+    if r is not None:
+        return _host_result(r)
+    sfx, rows, D, x_f32, pw, _ = _layer_norm_inputs(X_out, dN.dtype, w, None)
+    dev = X_out.device
+    pdn, pdx = _dense(dN, X_out.shape, dN.dtype, dev, "dN"), _dense(dX_out, X_out.shape, X_out.dtype, dev, "dX_out")
+    if in_place and dX_out is None:
+        raise ValueError("in_place needs dX_out")
+    dX = dX_out if in_place else torch.empty_like(X_out)
+    dw = torch.empty_like(w) if w is not None else None
+    db = torch.empty(D, dtype=torch.float32, device=dev) if want_db else None
+    with _on(X_out):
+        _check(getattr(lib(), "chela_layer_norm_bwd" + sfx)(
+            X_out.data_ptr(), pw, pdx, pdn, dX.data_ptr(), _ptr(dw), _ptr(db), float(eps), rows, D, x_f32, _stream_ptr(stream)))
+    return dX, dw, db
+
+
+def chela_layer_norm_bwd_workspace_bytes(rows, D) -> int:
+    return int(lib().chela_layer_norm_bwd_workspace_bytes(rows, D))
 
 
 def chela_linattn_workspace_bytes(B, H, N, dk, dv, chunk, is_bwd, dtype) -> int:

@@ -13,7 +13,8 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libchela.so")
 HOST_MODULE = os.path.join(HERE, "_chela_host.so")
 SOURCES = ["chela_api.hip", "chela_kernels_f32.hip", "chela_kernels_bf16.hip", "chela_kernels_conv.hip",
-           "chela_kernels_convmx.hip", "chela_kernels_selscan.hip", "chela_kernels_shortconv.hip", "chela_kernels_blocknorm.hip"]
+           "chela_kernels_convmx.hip", "chela_kernels_selscan.hip", "chela_kernels_shortconv.hip", "chela_kernels_blocknorm.hip",
+           "chela_kernels_delta.hip", "chela_kernels_delta_bwd.hip", "chela_kernels_layernorm.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 VALU forms are switched off for every device compile (they have given wrong results on this chip now and then)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

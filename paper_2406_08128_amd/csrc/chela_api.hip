@@ -370,7 +370,8 @@ static const char* const kKernelNames[KID_COUNT] = {
     "f32_seg_state_kernel", "f32_sweep_kernel", "copy_probe_kernel", "bf16_step_kernel", "affine_grad_kernel",
     "bf16_apply_state_kernel", "longconv_spectrum_kernel", "shortlong_conv_kernel",
     "shortconv_bwd_kernel", "longconv_bwd_kernel", "gate_norm_kernel", "stream_probe_kernel", "mfma_probe_kernel",
-    "short_conv_kernel", "selscan_kernel", "selscan_bwd_kernel", "selscan_step_kernel", "block_norm_kernel"};
+    "short_conv_kernel", "selscan_kernel", "selscan_bwd_kernel", "selscan_step_kernel", "block_norm_kernel",
+    "delta_kernels", "delta_bwd_kernels", "delta_step_kernel", "layer_norm_kernel"};
 
 ProfScope::ProfScope(int id, hipStream_t s) : slot(-1), st(s)
 {
@@ -1597,6 +1598,157 @@ CHELA_SELSCAN(_cleared, _f32, CHELA_DTYPE_F32, true)
 #undef CHELA_SELSCAN_AS
 #undef CHELA_SELSCAN_IN
 
+// The arguments that the forward, the backward and the single-token call of the gated delta rule share.
+struct DeltaIn {
+    const void *Q, *K, *V, *g, *beta;
+    long long ldq, ldk, ldv, ldg, ldb;
+    float scale;
+    int H, Hk, dk, dv;
+};
+static int delta_check(const DeltaIn& x, const int* cu, int n_seq, int T, const int* slots, int n_slots, bool clear, Rows* rows)
+{
+    if (!delta_dims_ok(x.dk, x.dv)) return CHELA_ERR_UNSUPPORTED_DIM;
+    if (x.H < 0 || x.H > (1 << 20) / (x.dk > x.dv ? x.dk : x.dv) || x.Hk < 1 || x.H % x.Hk != 0 || !std::isfinite(x.scale)) return CHELA_ERR_BAD_SHAPE;
+    const int rc = rows_of(cu, n_seq, T, x.H * x.dk, slots, n_slots, clear, rows);
+    if (rc != CHELA_OK) return rc;
+    if (too_many(T, x.H * x.dk, kRowUnits / 4) || (long long)n_seq * x.H * (x.dv / 16) >= kStateUnits) return CHELA_ERR_BAD_SHAPE;
+    return CHELA_OK;
+}
+static void delta_read(const DeltaIn& x, int T, size_t es, Operands* o, DeltaArgs* a)
+{
+    o->rows(x.Q, x.ldq, T, (size_t)x.Hk * x.dk, es);
+    o->rows(x.K, x.ldk, T, (size_t)x.Hk * x.dk, es);
+    o->rows(x.V, x.ldv, T, (size_t)x.H * x.dv, es);
+    if (x.g) o->rows(x.g, x.ldg, T, x.H, es);
+    o->rows(x.beta, x.ldb, T, x.H, es);
+    o->read_if(a->rows.cu, ((size_t)a->rows.n_seq + 1) * 4, 4);
+    o->read_if(a->rows.slots, (size_t)a->rows.n_seq * 4, 4);
+    a->Q = x.Q; a->K = x.K; a->V = x.V; a->g = x.g; a->beta = x.beta;
+    a->ldq = x.ldq; a->ldk = x.ldk; a->ldv = x.ldv; a->ldg = x.g ? x.ldg : 0; a->ldb = x.ldb;
+    a->scale = x.scale; a->H = x.H; a->Hk = x.Hk;
+}
+
+static int delta_fwd_common(const DeltaIn& x, const int* cu, int n_seq, int T, const float* S_in, float* S_out, const int* slots,
+                            int n_slots, void* O, void* saved, int dtype, bool clear, void* stream)
+{
+    DeltaArgs a{};
+    int rc = delta_check(x, cu, n_seq, T, slots, n_slots, clear, &a.rows);
+    if (rc != CHELA_OK) return rc;
+    if (x.H == 0 || (T == 0 && n_seq == 0)) return CHELA_OK;
+    const size_t es = esize(dtype), st = (size_t)n_slots * x.H * x.dk * x.dv * 4;
+    const DeltaPlan p = make_delta_plan(T, n_seq, cu != nullptr, x.H, x.dk, x.dv, kind(dtype), false, saved != nullptr);
+    Operands o;
+    delta_read(x, T, es, &o, &a);
+    if (S_in) o.read_under(S_in, st);
+    if (S_out) o.write_over(S_out, st);
+    o.write(O, (size_t)T * x.H * x.dv * es);
+    o.write_if(saved, p.saved_bytes);
+    if ((rc = o.done()) != CHELA_OK) return rc;
+    float* ws = nullptr;
+    if ((rc = get_workspace(p.bytes, stream, &ws)) != CHELA_OK) return rc;
+    a.S_in = S_in; a.S_out = S_out; a.O = O;
+    return status_of(launch_delta_fwd(a, p, (char*)ws, (char*)saved, x.dk, x.dv, kind(dtype), (hipStream_t)stream));
+}
+
+static int delta_bwd_common(const DeltaIn& x, const int* cu, int n_seq, int T, const float* S_in, const void* dO, long long lddo,
+                            const float* dS_out, const void* saved, void* dQ, void* dK, void* dV, void* dg, void* dbeta, float* dS_in,
+                            int dtype, bool clear, void* stream)
+{
+    DeltaArgs a{};
+    int rc = delta_check(x, cu, n_seq, T, nullptr, n_seq, clear, &a.rows);
+    if (rc != CHELA_OK) return rc;
+    if (x.H == 0 || (T == 0 && n_seq == 0)) return CHELA_OK;
+    const size_t es = esize(dtype), st = (size_t)n_seq * x.H * x.dk * x.dv * 4;
+    const size_t qk = (size_t)T * x.Hk * x.dk * es, v = (size_t)T * x.H * x.dv * es, one = (size_t)T * x.H * es;
+    const DeltaPlan p = make_delta_plan(T, n_seq, cu != nullptr, x.H, x.dk, x.dv, kind(dtype), true, saved != nullptr);
+    Operands o;
+    delta_read(x, T, es, &o, &a);
+    o.read_if(S_in, st);
+    o.rows(dO, lddo, T, (size_t)x.H * x.dv, es);
+    o.read_if(dS_out, st);
+    o.read_if(saved, p.saved_bytes);
+    o.write(dQ, qk);
+    o.write(dK, qk);
+    o.write(dV, v);
+    if (x.g) o.write(dg, one);
+    o.write(dbeta, one);
+    o.write_if(dS_in, st);
+    if ((rc = o.done()) != CHELA_OK) return rc;
+    float* ws = nullptr;
+    if ((rc = get_workspace(p.bytes, stream, &ws)) != CHELA_OK) return rc;
+    a.S_in = S_in; a.dO = dO; a.lddo = lddo; a.dS_out = dS_out;
+    a.dQ = dQ; a.dK = dK; a.dV = dV; a.dg = x.g ? dg : nullptr; a.dbeta = dbeta; a.dS_in = dS_in;
+    return status_of(launch_delta_bwd(a, p, (char*)ws, (char*)const_cast<void*>(saved), saved != nullptr, x.dk, x.dv, kind(dtype),
+                                      (hipStream_t)stream));
+}
+
+static int delta_step_common(const DeltaIn& x, float* S, const int* slots, int n_slots, int R, void* out, int dtype, bool clear, void* stream)
+{
+    DeltaArgs a{};
+    if (R < 0) return CHELA_ERR_BAD_SHAPE;
+    int rc = delta_check(x, nullptr, R, R, slots, n_slots, clear, &a.rows);
+    if (rc != CHELA_OK) return rc;
+    if (R == 0 || x.H == 0) return CHELA_OK;
+    const size_t es = esize(dtype);
+    Operands o;
+    delta_read(x, R, es, &o, &a);
+    o.write(S, (size_t)n_slots * x.H * x.dk * x.dv * 4);
+    o.write(out, (size_t)R * x.H * x.dv * es);
+    if ((rc = o.done()) != CHELA_OK) return rc;
+    a.S_out = S; a.O = out;
+    return status_of(launch_delta_step(a, x.dk, x.dv, kind(dtype), (hipStream_t)stream));
+}
+
+static bool delta_sizes_ok(int T, int n_seq, int packed, int H, int dk, int dv)
+{
+    Rows rows;
+    const DeltaIn x{nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0, 0, 0, 0, 1.f, H, 1, dk, dv};
+    static const int offsets = 0;                             // (only its being there is looked at)
+    return delta_check(x, packed ? &offsets : nullptr, n_seq, T, nullptr, n_seq, false, &rows) == CHELA_OK;
+}
+size_t chela_gated_delta_saved_bytes(int T, int n_seq, int packed, int H, int dk, int dv, int dtype)
+{
+    if (!delta_sizes_ok(T, n_seq, packed, H, dk, dv)) return 0;
+    return make_delta_plan(T, n_seq, packed != 0, H, dk, dv, kind(dtype), false, true).saved_bytes;
+}
+size_t chela_gated_delta_workspace_bytes(int T, int n_seq, int packed, int H, int dk, int dv, int dtype, int is_bwd, int has_saved)
+{
+    if (!delta_sizes_ok(T, n_seq, packed, H, dk, dv)) return 0;
+    return make_delta_plan(T, n_seq, packed != 0, H, dk, dv, kind(dtype), is_bwd != 0, has_saved != 0).bytes;
+}
+
+#define CHELA_DELTA_IN                                                                                                \
+    const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv, const void *g, long long ldg, \
+        const void *beta, long long ldb, float scale
+#define CHELA_DELTA_AS DeltaIn{Q, K, V, g, beta, ldq, ldk, ldv, ldg, ldb, scale, H, Hk, dk, dv}
+#define CHELA_DELTA_CALLS(FORM, SUFFIX, TYPE, CLEAR)                                                                  \
+    int chela_gated_delta_fwd##FORM##SUFFIX(CHELA_DELTA_IN, const int* cu, int n_seq, int T, int H, int Hk, int dk, int dv, \
+                                            const float* S_in, float* S_out, const int* slots, int n_slots, void* O, void* saved, \
+                                            void* stream)                                                             \
+    {                                                                                                                 \
+        return delta_fwd_common(CHELA_DELTA_AS, cu, n_seq, T, S_in, S_out, slots, n_slots, O, saved, TYPE, CLEAR, stream); \
+    }                                                                                                                 \
+    int chela_gated_delta_bwd##FORM##SUFFIX(CHELA_DELTA_IN, const int* cu, int n_seq, int T, int H, int Hk, int dk, int dv, \
+                                            const float* S_in, const void* dO, long long lddo, const float* dS_out,   \
+                                            const void* saved, void* dQ, void* dK, void* dV, void* dg, void* dbeta,   \
+                                            float* dS_in, void* stream)                                               \
+    {                                                                                                                 \
+        return delta_bwd_common(CHELA_DELTA_AS, cu, n_seq, T, S_in, dO, lddo, dS_out, saved, dQ, dK, dV, dg, dbeta, dS_in, TYPE, CLEAR, \
+                                stream);                                                                              \
+    }                                                                                                                 \
+    int chela_gated_delta_step##FORM##SUFFIX(CHELA_DELTA_IN, float* S, const int* slots, int n_slots, int R, int H, int Hk, int dk, int dv, \
+                                             void* o, void* stream)                                                   \
+    {                                                                                                                 \
+        return delta_step_common(CHELA_DELTA_AS, S, slots, n_slots, R, o, TYPE, CLEAR, stream);                       \
+    }
+CHELA_DELTA_CALLS(, , CHELA_DTYPE_BF16, false)
+CHELA_DELTA_CALLS(, _f32, CHELA_DTYPE_F32, false)
+CHELA_DELTA_CALLS(_cleared, , CHELA_DTYPE_BF16, true)
+CHELA_DELTA_CALLS(_cleared, _f32, CHELA_DTYPE_F32, true)
+#undef CHELA_DELTA_CALLS
+#undef CHELA_DELTA_AS
+#undef CHELA_DELTA_IN
+
 static int block_norm_check(const void* Y, const void* X, const float* w_pre, float scale, float eps, long long rows, int D)
 {
     if (!(eps >= 0.f) || !std::isfinite(eps) || !std::isfinite(scale)) return CHELA_ERR_BAD_SHAPE;
@@ -1697,6 +1849,79 @@ int chela_block_norm_bwd_f32(const void* Y, const void* gate, const void* X, con
     return block_norm_bwd_common(Y, gate, X, w_post, w_pre, dX_out, dN, dY, dgate, dX, dw_post, dw_pre, scale, eps, rows, D, x_f32,
                                  CHELA_DTYPE_F32, stream);
 }
+
+static int layer_norm_check(float eps, long long rows, int D)
+{
+    if (!(eps >= 0.f) || !std::isfinite(eps) || rows < 0 || rows > 0x7fffffffll || D < 1) return CHELA_ERR_BAD_SHAPE;
+    return D > kLayerNormMaxD ? CHELA_ERR_UNSUPPORTED_DIM : CHELA_OK;
+}
+
+static int layer_norm_fwd_common(const void* X, const void* Y, const float* w, const float* b, void* X_out, void* Nrm, float eps,
+                                 long long rows, int D, int x_f32, int dtype, void* stream)
+{
+    int rc = layer_norm_check(eps, rows, D);
+    if (rc != CHELA_OK || rows == 0) return rc;
+    if (!Y) X_out = nullptr;
+    const size_t es = esize(dtype), n = (size_t)rows * D, xs = x_f32 ? 4 : es;
+    Operands o;
+    o.read_under(X, n * xs);
+    o.read_alike(Y, n * es);
+    o.read_if(w, (size_t)D * 4);
+    o.read_if(b, (size_t)D * 4);
+    if (Y) o.write_over(X_out, n * xs);
+    o.write(Nrm, n * es);
+    if ((rc = o.done()) != CHELA_OK) return rc;
+    LayerNormArgs a{};
+    a.X = X; a.Y = Y; a.w = w; a.b = b; a.X_out = X_out; a.Nrm = Nrm; a.eps = eps; a.rows = rows; a.D = D; a.x_f32 = x_f32;
+    return status_of(launch_layer_norm_fwd(a, kind(dtype), (hipStream_t)stream));
+}
+
+size_t chela_layer_norm_bwd_workspace_bytes(long long rows, int D)
+{
+    if (rows < 0 || rows > 0x7fffffffll || D < 1 || D > kLayerNormMaxD) return 0;
+    return (size_t)layer_norm_bwd_parts((long)rows, D) * 2 * D * sizeof(float);
+}
+
+static int layer_norm_bwd_common(const void* X, const float* w, const void* dX_out, const void* dN, void* dX, float* dw, float* db, float eps,
+                                 long long rows, int D, int x_f32, int dtype, void* stream)
+{
+    int rc = layer_norm_check(eps, rows, D);
+    if (rc != CHELA_OK) return rc;
+    const size_t es = esize(dtype), n = (size_t)rows * D, xs = x_f32 ? 4 : es;
+    Operands o;
+    o.check(X, n * xs, 16);
+    o.check(dN, n * es, 16);
+    o.read_alike(X, n * xs);
+    o.read_alike(dN, n * es);
+    o.read_if(w, (size_t)D * 4);
+    if (dX_out) o.read_under(dX_out, n * xs);
+    o.write_over(dX, n * xs);
+    o.write_if(dw, (size_t)D * 4);
+    o.write_if(db, (size_t)D * 4);
+    if ((rc = o.done()) != CHELA_OK) return rc;
+    float* ws = nullptr;
+    if ((dw || db) && (rc = get_workspace(chela_layer_norm_bwd_workspace_bytes(rows, D), stream, &ws)) != CHELA_OK) return rc;
+    LayerNormArgs a{};
+    a.X = X; a.w = w; a.dX_out = dX_out; a.dN = dN; a.dX = dX; a.dw = dw; a.db = db; a.part = ws;
+    a.eps = eps; a.rows = rows; a.D = D; a.x_f32 = x_f32;
+    if (rows == 0 && ws == nullptr) return CHELA_OK;
+    return status_of(launch_layer_norm_bwd(a, kind(dtype), (hipStream_t)stream));
+}
+
+#define CHELA_LAYER_NORM(SUFFIX, TYPE)                                                                                \
+    int chela_layer_norm_fwd##SUFFIX(const void* X, const void* Y, const float* w, const float* b, void* X_out, void* Nrm, float eps, \
+                                     long long rows, int D, int x_f32, void* stream)                                  \
+    {                                                                                                                 \
+        return layer_norm_fwd_common(X, Y, w, b, X_out, Nrm, eps, rows, D, x_f32, TYPE, stream);                      \
+    }                                                                                                                 \
+    int chela_layer_norm_bwd##SUFFIX(const void* X, const float* w, const void* dX_out, const void* dN, void* dX, float* dw, float* db, \
+                                     float eps, long long rows, int D, int x_f32, void* stream)                       \
+    {                                                                                                                 \
+        return layer_norm_bwd_common(X, w, dX_out, dN, dX, dw, db, eps, rows, D, x_f32, TYPE, stream);                \
+    }
+CHELA_LAYER_NORM(, CHELA_DTYPE_BF16)
+CHELA_LAYER_NORM(_f32, CHELA_DTYPE_F32)
+#undef CHELA_LAYER_NORM
 
 size_t chela_linattn_workspace_bytes(int B, int H, int N, int dk, int dv, int chunk, int is_bwd, int dtype)
 {

@@ -1,0 +1,306 @@
+// What the kernels of the gated delta rule share: operands of the matrix instructions in either type, tiles in LDS, and the chunks that
+// the sequences are cut into.
+#pragma once
+#include "chela_rows.h"
+
+namespace chela {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(4))) bf16 bf16x4;
+typedef __attribute__((ext_vector_type(8))) bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+
+// Tokens of a chunk.  (fp32: a chunk's rows take twice the room in LDS.)
+template <typename E> struct DeltaChunk { static constexpr int C = sizeof(E) == 2 ? kDeltaChunkBf16 : kDeltaChunkF32; };
+// Elements behind each row of a tile in LDS: 16 rows' pieces of 8 (bf16) or 16 (fp32) bytes then fall on all banks alike.
+template <typename E> constexpr int kPad = sizeof(E) == 2 ? 8 : 4;
+
+// A 16 x 32 operand.  All products are 16 x 16 tiles over 32 terms, D[m][n] += sum_k A[m][k] B[n][k]: lane 16 q + c has row c of A (of B)
+// at eight k, and of D the column n = c at the rows m = 4 q + i.  Which eight is free as long as A and B agree; here they are
+//     k = 16 (j / 4) + 4 q + j % 4,  j = 0..7,
+// the rows that two accumulator tiles, one above the other, have in this lane: a result is the next product's operand as it lies in the
+// registers, summed over its rows.
+// P parts: a value that was worked out in fp32 is rounded to bf16 (P = 1, off by 2^-9) or kept as a sum of two (P = 2, 2^-18).  What the caller
+// gave in bf16 has one part.  fp32 operands have all bits, and their products are fp32: eight instructions over four terms each.
+template <typename E, int P> struct Op;
+template <> struct Op<bf16, 1> { bf16x8 h; };
+template <> struct Op<bf16, 2> { bf16x8 h, l; };
+template <int P> struct Op<float, P> { f32x8 v; };
+
+template <int PA, int PB>
+__device__ __forceinline__ f32x4 mma(const Op<bf16, PA>& a, const Op<bf16, PB>& b, f32x4 c)
+{
+    if constexpr (PA == 2) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.l, b.h, c, 0, 0, 0);
+    if constexpr (PB == 2) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.h, b.l, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.h, b.h, c, 0, 0, 0);
+}
+template <int PA, int PB>
+__device__ __forceinline__ f32x4 mma(const Op<float, PA>& a, const Op<float, PB>& b, f32x4 c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+    return c;
+}
+
+// Two accumulator tiles as an operand.
+template <typename E, int P>
+__device__ __forceinline__ Op<E, P> operand(f32x4 lo, f32x4 hi)
+{
+    const f32x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    Op<E, P> o;
+    if constexpr (sizeof(E) == 4) {
+        o.v = x;
+    } else {
+        o.h = __builtin_convertvector(x, bf16x8);
+        if constexpr (P == 2) o.l = __builtin_convertvector(x - __builtin_convertvector(o.h, f32x8), bf16x8);
+    }
+    return o;
+}
+template <typename E>
+__device__ __forceinline__ Op<E, 1> first_part(const Op<E, 2>& x)
+{
+    if constexpr (sizeof(E) == 4) return Op<E, 1>{x.v};
+    else return Op<E, 1>{x.h};
+}
+
+template <typename E> using Vec4 = typename std::conditional<sizeof(E) == 2, bf16x4, f32x4>::type;
+template <typename E> using Vec8 = typename std::conditional<sizeof(E) == 2, bf16x8, f32x8>::type;
+
+// The operand that is X[row0 + c][k0 ..], rows of a tile, summed over its columns.
+template <typename E>
+__device__ __forceinline__ Op<E, 1> rows_op(const E* X, int ld, int row0, int k0, int lane)
+{
+    const E* p = X + (row0 + (lane & 15)) * ld + k0 + 4 * (lane >> 4);
+    const Vec4<E> a = *(const Vec4<E>*)p, b = *(const Vec4<E>*)(p + 16);
+    return Op<E, 1>{__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
+}
+// The operand that is X[k0 ..][col0 + c], columns of a tile, summed over its rows.  bf16: within 16 lanes the transposing read hands lane p
+// the column p of a 4 x 16 block whose rows the lanes address as p / 4, and 8-byte pieces as p % 4.
+template <typename E>
+__device__ __forceinline__ Op<E, 1> cols_op(const E* X, int ld, int k0, int col0, int lane)
+{
+    const int q = lane >> 4, c = lane & 15;
+    if constexpr (sizeof(E) == 2) {
+        const bf16* p = X + (k0 + 4 * q + (c >> 2)) * ld + col0 + 4 * (c & 3);
+        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
+        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 16 * ld));
+        return Op<E, 1>{__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
+    } else {
+        const float* p = X + (k0 + 4 * q) * ld + col0 + c;
+        Op<E, 1> o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { o.v[j] = p[j * ld]; o.v[4 + j] = p[(16 + j) * ld]; }
+        return o;
+    }
+}
+
+// A matrix of fp32 values in LDS in the form of operands: one part, or two a plane apart.
+template <typename E, int P>
+struct Planes {
+    E* h;
+    int ld, plane;                             // (plane: elements from the first parts to the second)
+    __device__ __forceinline__ void put(int row, int col, float x) const
+    {
+        if constexpr (sizeof(E) == 4) {
+            h[row * ld + col] = x;
+        } else {
+            const bf16 a = (bf16)x;
+            h[row * ld + col] = a;
+            if constexpr (P == 2) h[plane + row * ld + col] = (bf16)(x - (float)a);
+        }
+    }
+    __device__ __forceinline__ void put4(int row, int col, f32x4 x) const          // col, col + 1, ...
+    {
+        if constexpr (sizeof(E) == 4) {
+            *(f32x4*)(h + row * ld + col) = x;
+        } else {
+            const bf16x4 a = __builtin_convertvector(x, bf16x4);
+            *(bf16x4*)(h + row * ld + col) = a;
+            if constexpr (P == 2) *(bf16x4*)(h + plane + row * ld + col) = __builtin_convertvector(x - __builtin_convertvector(a, f32x4), bf16x4);
+        }
+    }
+    __device__ __forceinline__ Op<E, P> rows(int row0, int k0, int lane) const
+    {
+        if constexpr (sizeof(E) == 2 && P == 2)
+            return Op<E, P>{rows_op(h, ld, row0, k0, lane).h, rows_op(h + plane, ld, row0, k0, lane).h};
+        else if constexpr (sizeof(E) == 4)
+            return Op<E, P>{rows_op(h, ld, row0, k0, lane).v};
+        else
+            return rows_op(h, ld, row0, k0, lane);
+    }
+    __device__ __forceinline__ Op<E, P> cols(int k0, int col0, int lane) const
+    {
+        if constexpr (sizeof(E) == 2 && P == 2)
+            return Op<E, P>{cols_op(h, ld, k0, col0, lane).h, cols_op(h + plane, ld, k0, col0, lane).h};
+        else if constexpr (sizeof(E) == 4)
+            return Op<E, P>{cols_op(h, ld, k0, col0, lane).v};
+        else
+            return cols_op(h, ld, k0, col0, lane);
+    }
+};
+
+// An operand as it lies in memory, lanes next to each other: 16 bytes (bf16) or 32 (fp32) of a lane, the second parts behind the first.
+template <typename E, int P> constexpr int kOpElems = 64 * 8 * (sizeof(E) == 2 ? P : 1);
+template <typename E, int P>
+__device__ __forceinline__ void store_op(E* to, const Op<E, P>& x, int lane)
+{
+    if constexpr (sizeof(E) == 4) {
+        *(f32x8*)(to + 8 * lane) = x.v;
+    } else {
+        *(bf16x8*)(to + 8 * lane) = x.h;
+        if constexpr (P == 2) *(bf16x8*)(to + 512 + 8 * lane) = x.l;
+    }
+}
+template <typename E, int P>
+__device__ __forceinline__ Op<E, P> load_op(const E* from, int lane)
+{
+    if constexpr (sizeof(E) == 4) {
+        return Op<E, P>{*(const f32x8*)(from + 8 * lane)};
+    } else {
+        Op<E, P> o;
+        o.h = *(const bf16x8*)(from + 8 * lane);
+        if constexpr (P == 2) o.l = *(const bf16x8*)(from + 512 + 8 * lane);
+        return o;
+    }
+}
+
+__device__ __forceinline__ f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+__device__ __forceinline__ f32x4 splat4(float x) { return f32x4{x, x, x, x}; }
+
+// ---- chunks.  A sequence's rows are cut into chunks of C, the last one shorter.  The places of all chunks in the scratch: sequence s begins at
+// cu[s] / C + s.  (A sequence of n rows has at most floor(n / C) + 1 chunks and the next one begins at least as much further on, so that no
+// two chunks share a place, and there are T / C + n_seq places; no prefix sum is needed.)
+__device__ __forceinline__ int chunk_key(const Rows& r, int C, int s)
+{
+    return r.cu == nullptr ? s * ((r.L + C - 1) / C) : seq_begin(r, s) / C + s;
+}
+__device__ __forceinline__ int chunks_in(const Rows& r, int C, int s)
+{
+    const int n = r.cu == nullptr ? r.L : seq_end(r, s) - seq_begin(r, s);
+    return n > 0 ? (n + C - 1) / C : 0;
+}
+struct Chunk { int seq, index, row, n; };      // its sequence, which of that one's chunks, its first row, its rows (0: nothing is here)
+// All 64 lanes of a wave together, 64 sequences at a time.
+__device__ __forceinline__ Chunk chunk_at(const Rows& r, int C, int place, int lane)
+{
+    Chunk c{0, 0, 0, 0};
+    if (r.cu == nullptr) {
+        const int per = (r.L + C - 1) / C;
+        if (per == 0) return c;
+        c.seq = place / per;
+        c.index = place - c.seq * per;
+    } else {
+        int first = 0, n = r.n_seq;
+        while (n > 64) {
+            const int step = (n + 63) / 64, i = lane * step;
+            const int below = __popcll(__ballot(i < n && chunk_key(r, C, first + min(i, n - 1)) <= place));
+            if (below == 0) return c;
+            const int skip = min((below - 1) * step, n - 1);
+            first += skip;
+            n = min(step, n - skip);
+        }
+        const int below = n > 0 ? __popcll(__ballot(lane < n && chunk_key(r, C, first + min(lane, n - 1)) <= place)) : 0;
+        if (below == 0) return c;
+        c.seq = first + below - 1;
+        c.index = place - chunk_key(r, C, c.seq);
+    }
+    if (c.seq >= r.n_seq || c.index >= chunks_in(r, C, c.seq)) return c;
+    c.row = (r.cu == nullptr ? c.seq * r.L : seq_begin(r, c.seq)) + c.index * C;
+    c.n = min(C, (r.cu == nullptr ? (c.seq + 1) * r.L : seq_end(r, c.seq)) - c.row);
+    return c;
+}
+
+// ---- what a chunk's tokens have of their own: beta, and the running sum of the log decays, gamma.  Sums of 64 bits, held as two floats: two
+// tokens' difference has to be good to fp32's last digits behind any number of strong decays.  A log decay below -256 (infinite ones
+// too) stands for none of the state being left, which fp32 makes of -104 already.
+template <int C>
+struct ChunkSteps {
+    alignas(16) float hi[C], lo[C], beta[C], up[C], down[C], bu[C];     // up: e^gamma, down: e^(gamma of the last token - gamma), bu: -beta up
+    float whole;                                                       // e^(gamma of the last token)
+    __device__ __forceinline__ float decay(int t, int s) const { return exp2_(kLog2e * ((hi[t] - hi[s]) + (lo[t] - lo[s]))); }
+};
+// By the first wave; n rows there are, the rest as if they were not (no decay, beta of zero).
+template <typename E, int C>
+__device__ __forceinline__ void load_steps(ChunkSteps<C>& st, const E* g, long ldg, const E* beta, long ldb, int row, int h, int n, int tid)
+{
+    if (tid < 64) {
+        const int t = tid;
+        const bool on = t < n;
+        float x = on && g != nullptr ? to_f(g[(size_t)(row + (on ? t : 0)) * ldg + h]) : 0.f;
+        const float b = on ? to_f(beta[(size_t)(row + t) * ldb + h]) : 0.f;
+        if (x < -256.f) x = -256.f;
+        double s = (double)x;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const double y = __shfl_up(s, d);
+            if (t >= d) s += y;
+        }
+        const double last = __shfl(s, 63);
+        if (t < C) {
+            const float hi = (float)s;
+            st.hi[t] = hi;
+            st.lo[t] = (float)(s - (double)hi);
+            st.beta[t] = b;
+            const float up = exp2_(kLog2e * (float)s);
+            st.up[t] = up;
+            st.bu[t] = -b * up;
+            st.down[t] = exp2_(kLog2e * (float)(last - s));
+            if (t == 0) st.whole = exp2_(kLog2e * (float)last);
+        }
+    }
+}
+
+// The same operand with each of its eight terms times a factor: f[k0 ..], one for each row of the tile that it was read from.
+template <typename E, int P>
+__device__ __forceinline__ Op<E, P> scaled(const Op<E, 1>& x, const float* f, int k0, int lane)
+{
+    const f32x4 a = *(const f32x4*)(f + k0 + 4 * (lane >> 4)), b = *(const f32x4*)(f + k0 + 16 + 4 * (lane >> 4));
+    f32x8 v;
+    if constexpr (sizeof(E) == 4) v = x.v;
+    else v = __builtin_convertvector(x.h, f32x8);
+    v *= __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    return operand<E, P>(__builtin_shufflevector(v, v, 0, 1, 2, 3), __builtin_shufflevector(v, v, 4, 5, 6, 7));
+}
+
+// A chunk's rows of one head into LDS, zeros behind the n there are.  (Rows begin on an element: loads of global memory need no more.)
+template <typename E, int C, int D>
+__device__ __forceinline__ void load_tile(E* to, int ld, const E* from, long ldf, int row, int n, int tid, int threads)
+{
+    constexpr int W = 16 / sizeof(E);
+    typedef unsigned Piece __attribute__((ext_vector_type(4)));
+    struct __attribute__((packed, aligned(sizeof(E)))) Loose { Piece p; };
+#pragma unroll
+    for (int i = tid; i < C * (D / W); i += threads) {
+        const int t = i / (D / W), k = i % (D / W) * W;
+        Piece x = Piece(0);
+        if (t < n) {
+            x = ((const Loose*)(from + (size_t)(row + t) * ldf + k))->p;
+        }
+        *(Piece*)(to + t * ld + k) = x;
+    }
+}
+
+// Rows of no sequence: zeros in all of `width` elements of each, sixty-four rows to a workgroup.
+template <typename E>
+__device__ __forceinline__ void clear_rows(const Rows& r, int block, E* to, int width)
+{
+    if (to == nullptr) return;
+    const int lo = r.n_seq > 0 ? seq_begin(r, 0) : r.T, hi = r.n_seq > 0 ? seq_begin(r, r.n_seq) : r.T;
+    const int end = min(r.T, 64 * block + 64);
+    for (int t = 64 * block; t < end; ++t) {
+        if (t >= lo && t < hi) continue;
+        E* row = to + (size_t)t * width;
+        for (int i = threadIdx.x; i < width; i += 256) row[i] = (E)0.f;
+    }
+}
+
+// RUN(element type, DK, DV) for a call's.
+#define CHELA_DELTA(RUN)                                                                                              \
+    if (dtype != 0) { if (dk == 64) { if (dv == 64) RUN(float, 64, 64); else RUN(float, 64, 128); }                   \
+                      else { if (dv == 64) RUN(float, 128, 64); else RUN(float, 128, 128); } }                        \
+    else { if (dk == 64) { if (dv == 64) RUN(bf16, 64, 64); else RUN(bf16, 64, 128); }                                \
+           else { if (dv == 64) RUN(bf16, 128, 64); else RUN(bf16, 128, 128); } }
+
+}  // namespace chela

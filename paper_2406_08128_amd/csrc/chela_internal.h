@@ -278,10 +278,54 @@ int block_norm_bwd_parts(long rows, int D);            // partial sums of dw_pos
 hipError_t launch_block_norm_fwd(const BlockNormArgs& a, int dtype, hipStream_t st);
 hipError_t launch_block_norm_bwd(const BlockNormArgs& a, int dtype, hipStream_t st);
 
+// Gated delta rule.  A sequence's rows are cut into chunks (of kDeltaChunkBf16 or kDeltaChunkF32 tokens); `places` is how many there may be,
+// and each has room for what the kernels hand to each other, per head.
+struct DeltaPlan {
+    int chunk, places, parts;             // parts: of the operands that a state goes through (1, or 2 in bf16)
+    size_t N, Z, bytes;                   // byte offsets into the scratch, and its size
+    size_t T, S0, whole, saved_bytes;     // ... into `saved` (without one: this many bytes of the scratch from `saved_at` on)
+    size_t saved_at, dS;
+};
+struct DeltaArgs {
+    Rows rows;
+    const void *Q, *K, *V, *g, *beta, *dO;
+    long ldq, ldk, ldv, ldg, ldb, lddo;
+    const float *S_in, *dS_out;
+    float *S_out, *dS_in;
+    void *O, *dQ, *dK, *dV, *dg, *dbeta;
+    float scale;
+    int H, Hk, places;
+    void *N, *T, *S0, *dS;                // between the kernels, [places][H] of each
+    float *Z, *whole;
+};
+constexpr int kDeltaChunkBf16 = 64, kDeltaChunkF32 = 32;
+bool delta_dims_ok(int dk, int dv);
+DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved);
+hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st);
+hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st);
+hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int dk, int dv, int dtype, hipStream_t st);
+hipError_t launch_delta_bwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, bool has_saved, int dk, int dv, int dtype, hipStream_t st);
+hipError_t launch_delta_step(const DeltaArgs& a, int dk, int dv, int dtype, hipStream_t st);
+
+// Layer norm with the residual.
+struct LayerNormArgs {
+    const void *X, *Y, *dX_out, *dN;                   // (backward: X is the stream as the forward left it)
+    const float *w, *b;
+    void *X_out, *Nrm, *dX;
+    float *dw, *db, *part;                             // part: null where neither is wanted
+    float eps;
+    long rows;
+    int D, x_f32;                                      // x_f32: the stream and its gradients are fp32
+};
+constexpr int kLayerNormMaxD = 8192;
+int layer_norm_bwd_parts(long rows, int D);            // partial sums of dw and db, [parts][2][D] floats
+hipError_t launch_layer_norm_fwd(const LayerNormArgs& a, int dtype, hipStream_t st);
+hipError_t launch_layer_norm_bwd(const LayerNormArgs& a, int dtype, hipStream_t st);
+
 // Kernel classes for the per-kernel timing aid.
 enum { KID_SEG_STATE_BF16 = 0, KID_SCAN = 1, KID_FWD_SWEEP_BF16 = 2, KID_BWD_SWEEP_BF16 = 3, KID_SEG_STATE_F32 = 4,
        KID_SWEEP_F32 = 5, KID_COPY = 6, KID_STEP_BF16 = 7, KID_AFFINE_GRAD = 8, KID_APPLY_BF16 = 9, KID_CONV_SPECTRUM = 10, KID_CONV_FWD = 11, KID_CONV_SHORT_BWD = 12, KID_CONV_LONG_BWD = 13, KID_GATE_NORM = 14, KID_STREAM_PROBE = 15, KID_MFMA_PROBE = 16, KID_SHORT_CONV = 17, KID_SELSCAN = 18,
-       KID_SELSCAN_BWD = 19, KID_SELSCAN_STEP = 20, KID_BLOCK_NORM = 21, KID_COUNT = 22 };
+       KID_SELSCAN_BWD = 19, KID_SELSCAN_STEP = 20, KID_BLOCK_NORM = 21, KID_DELTA = 22, KID_DELTA_BWD = 23, KID_DELTA_STEP = 24, KID_LAYER_NORM = 25, KID_COUNT = 26 };
 
 // Brackets one kernel launch with HIP events on its stream while profiling is enabled; otherwise does nothing.
 struct ProfScope {

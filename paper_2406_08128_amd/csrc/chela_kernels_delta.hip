@@ -1,0 +1,476 @@
+// Gated delta rule, forward and single tokens, gfx950.
+//
+// Per head, with a state S of dk x dv, alpha = e^g:
+//     S' = alpha_t S_{t-1},   u_t = beta_t (v_t - S'^T k_t),   S_t = S' + k_t u_t^T,   o_t = scale S_t^T q_t.
+// A chunk of C tokens at once, gamma the running sum of g in it, S the state in front of it, D_ts = e^(gamma_t - gamma_s):
+//     (1 + A) U = beta (V - e^gamma K S),  A_ts = beta_t D_ts k_t . k_s for s < t, 0 otherwise;   T = (1 + A)^-1,
+//     O = scale e^gamma Q S + P U,  P_ts = scale D_ts q_t . k_s for s <= t,
+//     S_next = e^(gamma_C) S + K~^T U = e^(gamma_C) S - N S + Z,   K~_s = e^(gamma_C - gamma_s) k_s,
+//     N = K~^T T (beta e^gamma K),   Z = K~^T T (beta V).
+// Three launches: one works N, Z and T out for all chunks at once, one walks the chunks with the states, a product each, one makes all
+// outputs from the states in front of the chunks.
+#include "chela_delta.h"
+
+namespace chela {
+
+// ---- a chunk's T, N and Z
+template <typename E, int DK, int DV, int P>
+__global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a)
+{
+    constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>, LA = C + 4, LD = 20;
+    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[2 * C * LT];
+    __shared__ __align__(16) float sA[C * LA], sD[C * LD];
+    __shared__ ChunkSteps<C> st;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
+    const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
+    const Chunk ch = chunk_at(a.rows, C, place, lane);
+    if (ch.n <= 0) return;
+    load_tile<E, C, DK>(sK, LK, (const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid, 256);
+    load_tile<E, C, DV>(sV, LV, (const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid, 256);
+    load_steps<E, C>(st, (const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, tid);
+    __syncthreads();
+    // A, sixteen tokens to a wave
+    if (w < NB) {
+        const int t = 16 * w + c;
+        for (int sb = 0; sb <= w; ++sb) {
+            f32x4 x = zero4();
+#pragma unroll
+            for (int ks = 0; ks < DK / 32; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sK, LK, 16 * w, 32 * ks, lane), x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int s = 16 * sb + 4 * q + i;
+                x[i] = s < t ? st.beta[t] * st.decay(t, s) * x[i] : 0.f;
+            }
+            *(f32x4*)(sA + t * LA + 16 * sb + 4 * q) = x;
+        }
+    }
+    __syncthreads();
+    // the inverses of 1 + A's blocks on the diagonal, a lane to a column: x_i = e_i - sum_{j<i} A_ij x_j
+    if (tid < C) {
+        const float* A = sA + 16 * q * LA + 16 * q;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float s = i == c ? 1.f : 0.f;
+#pragma unroll
+            for (int j4 = 0; j4 < (i + 3) / 4; ++j4) {
+                const f32x4 r = *(const f32x4*)(A + i * LA + 4 * j4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (4 * j4 + j < i) s = fmaf(-r[j], x[4 * j4 + j], s);
+            }
+            x[i] = s;
+            sD[(16 * q + i) * LD + c] = s;
+        }
+    }
+    __syncthreads();
+    // the blocks below it, a wave to a column of blocks: T_rj = -T_rr sum_{j<=b<r} A_rb T_bj, fp32 products
+    f32x4 t[NB];
+    if (w < NB) {
+#pragma unroll
+        for (int r = 0; r < NB; ++r) {
+            t[r] = zero4();
+            if (r == w) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[r][i] = sD[(16 * r + 4 * q + i) * LD + c];
+            } else if (r > w) {
+                f32x4 x = zero4();
+#pragma unroll
+                for (int b = 0; b < r; ++b)
+                    if (b >= w) {
+                        const f32x4 m = *(const f32x4*)(sA + (16 * r + c) * LA + 16 * b + 4 * q);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(m[i], t[b][i], x, 0, 0, 0);
+                    }
+                const f32x4 m = *(const f32x4*)(sD + (16 * r + c) * LD + 4 * q);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(-m[i], x[i], t[r], 0, 0, 0);
+            }
+        }
+        const Planes<E, 2> T{sT, LT, C * LT};
+#pragma unroll
+        for (int r = 0; r < NB; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) T.put(16 * r + 4 * q + i, 16 * w + c, t[r][i]);
+    }
+    __syncthreads();
+    const size_t at = (size_t)place * a.H + h;
+    {
+        // T for the kernels behind, its first parts and (bf16) its second
+        constexpr int W = 16 / sizeof(E), PT = sizeof(E) == 2 ? 2 : 1;
+        E* to = (E*)a.T + at * (PT * C * C);
+#pragma unroll
+        for (int i = tid; i < PT * C * (C / W); i += 256) {
+            const int part = i / (C * (C / W)), r = i % (C * (C / W)) / (C / W), k = i % (C / W) * W;
+            *(u32x4*)(to + part * C * C + r * C + k) = *(const u32x4*)(sT + part * C * LT + r * LT + k);
+        }
+        if (tid == 0) a.whole[at] = st.whole;
+    }
+    // T (beta e^gamma K), T (beta V), thirty-two columns at a time, and what K~ makes of them
+    const Planes<E, P> T{sT, LT, C * LT};
+    for (int p = w; p < (DK + DV) / 32; p += 4) {
+        const bool of_k = p < DK / 32;
+        const int col = 32 * (of_k ? p : p - DK / 32);
+        const E* X = of_k ? sK : sV;
+        const int ldx = of_k ? LK : LV;
+        const float* f = of_k ? st.bu : st.beta;          // (N is kept with its sign changed)
+        f32x4 y[NB][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) y[b][0] = y[b][1] = zero4();
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) {
+            const Op<E, P> x0 = scaled<E, P>(cols_op(X, ldx, 32 * ks, col, lane), f, 32 * ks, lane);
+            const Op<E, P> x1 = scaled<E, P>(cols_op(X, ldx, 32 * ks, col + 16, lane), f, 32 * ks, lane);
+#pragma unroll
+            for (int b = 2 * ks; b < NB; ++b) {
+                const Op<E, P> m = T.rows(16 * b, 32 * ks, lane);
+                y[b][0] = mma(m, x0, y[b][0]);
+                y[b][1] = mma(m, x1, y[b][1]);
+            }
+        }
+        Op<E, P> yo[KC][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const f32x4 d = *(const f32x4*)(st.down + 16 * b + 4 * q);
+            y[b][0] *= d;
+            y[b][1] *= d;
+        }
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) {
+            yo[ks][0] = operand<E, P>(y[2 * ks][0], y[2 * ks + 1][0]);
+            yo[ks][1] = operand<E, P>(y[2 * ks][1], y[2 * ks + 1][1]);
+        }
+#pragma unroll
+        for (int n = 0; n < DK / 16; ++n) {
+            f32x4 r0 = zero4(), r1 = zero4();
+#pragma unroll
+            for (int ks = 0; ks < KC; ++ks) {
+                const Op<E, 1> k = cols_op(sK, LK, 32 * ks, 16 * n, lane);
+                if (of_k) { r0 = mma(yo[ks][0], k, r0); r1 = mma(yo[ks][1], k, r1); }
+                else { r0 = mma(k, yo[ks][0], r0); r1 = mma(k, yo[ks][1], r1); }
+            }
+            if (of_k) {
+                store_op<E, P>((E*)a.N + (at * (DK / 16 * (DK / 32)) + n * (DK / 32) + p) * kOpElems<E, P>, operand<E, P>(r0, r1), lane);
+            } else {
+                float* z = a.Z + at * (DK * DV) + (size_t)(col / 16 * (DK / 16) + n) * 256 + 4 * lane;
+                *(f32x4*)z = r0;
+                *(f32x4*)(z + DK / 16 * 256) = r1;
+            }
+        }
+    }
+}
+
+// ---- the walk: S <- whole S + Z - N S from chunk to chunk (N comes negated), sixteen of S's columns to a workgroup, a quarter of its rows to
+// a wave.  Each wave keeps its rows in fp32 and hands them to the others as operands, through LDS; what the next chunks need is on its way
+// meanwhile.  REV: from the last chunk to the first, with the states' gradients.
+template <typename E, int DK, int P, bool REV>
+__global__ __launch_bounds__(256) void delta_walk_kernel(DeltaArgs a, int DV)
+{
+    constexpr int C = DeltaChunk<E>::C, TW = DK / 64, KS = DK / 32, OE = kOpElems<E, P>;
+    constexpr int AHEAD = (DK == 64 ? 4 : 2);
+    __shared__ __align__(16) E sS[2][KS * OE];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
+    const int groups = DV / 16;
+    const int eg = blockIdx.x % groups, h = blockIdx.x / groups % a.H, seq = blockIdx.x / groups / a.H;
+    const int first = chunk_key(a.rows, C, seq), n = min(chunks_in(a.rows, C, seq), a.places - first);
+    const int slot = slot_of(a.rows, seq);
+    const float* from = REV ? a.dS_out : a.S_in;
+    float* to = REV ? a.dS_in : a.S_out;
+    E* keep = (E*)(REV ? a.dS : a.S0);
+    f32x4 S[TW];
+    const size_t mine = (((size_t)max(slot, 0) * a.H + h) * DK + 16 * TW * w + 4 * q) * DV + 16 * eg + c;
+#pragma unroll
+    for (int i = 0; i < TW; ++i) {
+        S[i] = zero4();
+        if (from != nullptr && slot >= 0)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[i][j] = from[mine + (size_t)(16 * i + j) * DV];
+    }
+    Op<E, P> N[AHEAD][TW][KS];
+    f32x4 Z[AHEAD][TW];
+    float whole[AHEAD];
+    auto load = [&](int u, int k) {
+        k = min(k, n - 1);
+        const size_t at = (size_t)(first + (REV ? n - 1 - k : k)) * a.H + h;
+        whole[u] = a.whole[at];
+#pragma unroll
+        for (int i = 0; i < TW; ++i) {
+            Z[u][i] = *(const f32x4*)(a.Z + at * ((size_t)DK * DV) + (size_t)(eg * (DK / 16) + TW * w + i) * 256 + 4 * lane);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                N[u][i][ks] = load_op<E, P>((const E*)a.N + (at * (DK / 16 * KS) + (TW * w + i) * KS + ks) * OE, lane);
+        }
+    };
+    if (n > 0) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) load(u, u);
+    }
+    for (int k0 = 0; k0 < n; k0 += AHEAD) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int k = k0 + u;
+            if (k >= n) break;
+            E* x = sS[u & 1];
+            const size_t at = (size_t)(first + (REV ? n - 1 - k : k)) * a.H + h;
+            E* out = keep + at * ((size_t)DK * DV) + (size_t)eg * (DK * 16);
+            if constexpr (TW == 2) {
+                const Op<E, P> o = operand<E, P>(S[0], S[1]);
+                store_op<E, P>(x + w * OE, o, lane);
+                store_op<E, 1>(out + w * 512, [&] { if constexpr (sizeof(E) == 4) return Op<E, 1>{o.v}; else return Op<E, 1>{o.h}; }(), lane);
+            } else {
+                E* half = x + (w >> 1) * OE + 8 * lane + 4 * (w & 1);
+                E* out_half = out + (w >> 1) * 512 + 8 * lane + 4 * (w & 1);
+                if constexpr (sizeof(E) == 4) {
+                    *(f32x4*)half = S[0];
+                    *(f32x4*)out_half = S[0];
+                } else {
+                    const bf16x4 hi = __builtin_convertvector(S[0], bf16x4);
+                    *(bf16x4*)half = hi;
+                    *(bf16x4*)out_half = hi;
+                    if constexpr (P == 2) *(bf16x4*)(half + 512) = __builtin_convertvector(S[0] - __builtin_convertvector(hi, f32x4), bf16x4);
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < TW; ++i) S[i] = S[i] * whole[u] + Z[u][i];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const Op<E, P> o = load_op<E, P>(x + ks * OE, lane);
+#pragma unroll
+                for (int i = 0; i < TW; ++i) S[i] = mma(N[u][i][ks], o, S[i]);
+            }
+            load(u, k + AHEAD);
+        }
+    }
+    if (to != nullptr && slot >= 0)
+#pragma unroll
+        for (int i = 0; i < TW; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[mine + (size_t)(16 * i + j) * DV] = S[i][j];
+}
+
+// ---- the outputs
+template <typename E, int DK, int DV>
+__global__ __launch_bounds__(256) void delta_out_kernel(DeltaArgs a)
+{
+    constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
+    __shared__ __align__(16) E sK[C * LK], sQ[C * LK], sV[C * LV], sT[C * LT], sP[C * LT];
+    __shared__ ChunkSteps<C> st;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
+    const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
+    if (place >= a.places) {
+        clear_rows(a.rows, blockIdx.x - a.places * a.H, (E*)a.O, a.H * DV);
+        return;
+    }
+    const Chunk ch = chunk_at(a.rows, C, place, lane);
+    if (ch.n <= 0) return;
+    const size_t at = (size_t)place * a.H + h;
+    load_tile<E, C, DK>(sK, LK, (const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid, 256);
+    load_tile<E, C, DK>(sQ, LK, (const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid, 256);
+    load_tile<E, C, DV>(sV, LV, (const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid, 256);
+    load_tile<E, C, C>(sT, LT, (const E*)a.T + at * ((sizeof(E) == 2 ? 2 : 1) * C * C), C, 0, C, tid, 256);
+    load_steps<E, C>(st, (const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, tid);
+    __syncthreads();
+    if (w < NB) {
+        const Planes<E, 1> Pm{sP, LT, 0};
+        const int t = 16 * w + c;
+        for (int sb = 0; sb <= (w | 1); ++sb) {
+            f32x4 x = zero4();
+            if (sb <= w) {
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sQ, LK, 16 * w, 32 * ks, lane), x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int s = 16 * sb + 4 * q + i;
+                    x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
+                }
+            }
+            Pm.put4(t, 16 * sb + 4 * q, x);
+        }
+    }
+    __syncthreads();
+    const E* S0 = (const E*)a.S0 + at * (DK * DV);
+    for (int eg = w; eg < DV / 16; eg += 4) {
+        Op<E, 1> so[KS], ro[KC], uo[KC];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) so[ks] = load_op<E, 1>(S0 + (eg * KS + ks) * 512, lane);
+        f32x4 x[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            x[b] = zero4();
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) x[b] = mma(rows_op(sK, LK, 16 * b, 32 * ks, lane), so[ks], x[b]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = 16 * b + 4 * q + i;
+                x[b][i] = st.beta[t] * fmaf(-st.up[t], x[b][i], to_f(sV[t * LV + 16 * eg + c]));
+            }
+        }
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 1>(x[2 * ks], x[2 * ks + 1]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            x[b] = zero4();
+#pragma unroll
+            for (int ks = 0; ks <= b / 2; ++ks) x[b] = mma(rows_op(sT, LT, 16 * b, 32 * ks, lane), ro[ks], x[b]);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) uo[ks] = operand<E, 1>(x[2 * ks], x[2 * ks + 1]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int t = 16 * b + c;
+            f32x4 o = zero4();
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) o = mma(so[ks], rows_op(sQ, LK, 16 * b, 32 * ks, lane), o);
+            o *= splat4(a.scale * st.up[t]);
+#pragma unroll
+            for (int ks = 0; ks <= b / 2; ++ks) o = mma(uo[ks], rows_op(sP, LT, 16 * b, 32 * ks, lane), o);
+            if (t < ch.n)
+                *(Vec4<E>*)((E*)a.O + (size_t)(ch.row + t) * (a.H * DV) + h * DV + 16 * eg + 4 * q) = __builtin_convertvector(o, Vec4<E>);
+        }
+    }
+}
+
+// ---- a single token of each request: the state is read and written once, four columns and DK / R rows to a thread
+template <typename E, int DK, int DV>
+__global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a)
+{
+    constexpr int L = DV / 4, R = 256 / L, M = DK / R;                // threads to a row, rows at a time, rows to a thread
+    __shared__ float sk[DK], sq[DK];
+    __shared__ __align__(16) f32x4 s_r[R][L], s_p[R][L];
+    __shared__ float s_qk[4];
+    const int tid = threadIdx.x, r = blockIdx.x / a.H, h = blockIdx.x - r * a.H, hk = h / (a.H / a.Hk);
+    const int l = tid % L, j = tid / L;
+    const int slot = slot_of(a.rows, r);
+    E* o = (E*)a.O + ((size_t)r * a.H + h) * DV;
+    if (slot < 0) {
+        if (a.rows.clear) for (int i = tid; i < DV; i += 256) o[i] = (E)0.f;
+        return;
+    }
+    float* S = a.S_out + ((size_t)slot * a.H + h) * (DK * DV) + 4 * l;
+    f32x4 x[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) x[m] = *(const f32x4*)(S + (size_t)(m * R + j) * DV);
+    float alpha = 1.f;
+    if (a.g != nullptr) alpha = exp2_(kLog2e * to_f(((const E*)a.g)[(size_t)r * a.ldg + h]));
+    const float beta = to_f(((const E*)a.beta)[(size_t)r * a.ldb + h]);
+    const E* v = (const E*)a.V + (size_t)r * a.ldv + h * DV + 4 * l;
+    f32x4 vv;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vv[i] = to_f(v[i]);
+    float qk = 0.f;
+    for (int i = tid; i < DK; i += 256) {
+        const float k = to_f(((const E*)a.K)[(size_t)r * a.ldk + hk * DK + i]), y = to_f(((const E*)a.Q)[(size_t)r * a.ldq + hk * DK + i]);
+        sk[i] = k;
+        sq[i] = y;
+        qk = k * y;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) qk += __shfl_xor(qk, d);
+    if ((tid & 63) == 0) s_qk[tid >> 6] = qk;
+    __syncthreads();
+    f32x4 rd = zero4(), p = zero4();
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+        x[m] *= splat4(alpha);
+        rd += x[m] * splat4(sk[m * R + j]);
+        p += x[m] * splat4(sq[m * R + j]);
+    }
+    s_r[j][l] = rd;
+    s_p[j][l] = p;
+    __syncthreads();
+    rd = p = zero4();
+#pragma unroll
+    for (int i = 0; i < R; ++i) { rd += s_r[i][l]; p += s_p[i][l]; }
+    const f32x4 u = splat4(beta) * (vv - rd);
+#pragma unroll
+    for (int m = 0; m < M; ++m) *(f32x4*)(S + (size_t)(m * R + j) * DV) = x[m] + splat4(sk[m * R + j]) * u;
+    if (j == 0) {
+        const f32x4 y = splat4(a.scale) * (p + splat4(s_qk[0] + s_qk[1]) * u);
+        *(Vec4<E>*)(o + 4 * l) = __builtin_convertvector(y, Vec4<E>);
+    }
+}
+
+// -------------------------------------------------------------------------------------------------------------------- host
+bool delta_dims_ok(int dk, int dv) { return (dk == 64 || dk == 128) && (dv == 64 || dv == 128); }
+
+DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved)
+{
+    DeltaPlan p{};
+    const size_t es = dtype != 0 ? 4 : 2;
+    p.parts = dtype != 0 ? 1 : 2;
+    p.chunk = dtype != 0 ? kDeltaChunkF32 : kDeltaChunkBf16;
+    const int len = n_seq > 0 ? T / n_seq : 0;
+    p.places = T <= 0 || n_seq <= 0 ? 0 : packed ? T / p.chunk + n_seq : n_seq * ((len + p.chunk - 1) / p.chunk);
+    const size_t n = (size_t)p.places * H;
+    auto room = [](size_t& at, size_t bytes) { const size_t was = at; at += (bytes + 255) & ~(size_t)255; return was; };
+    p.T = room(p.saved_bytes, n * p.parts * p.chunk * p.chunk * es);
+    p.S0 = room(p.saved_bytes, n * dk * dv * es);
+    p.whole = room(p.saved_bytes, n * sizeof(float));
+    p.N = room(p.bytes, n * p.parts * dk * dk * es);
+    p.Z = room(p.bytes, n * dk * dv * sizeof(float));
+    if (is_bwd) p.dS = room(p.bytes, n * dk * dv * es);
+    p.saved_at = p.bytes;
+    if (!has_saved) p.bytes += p.saved_bytes;
+    return p;
+}
+
+hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int dk, int dv, int dtype, hipStream_t st)
+{
+    if (a.rows.n_seq == 0) return hipSuccess;
+    const dim3 grid((unsigned)((size_t)a.rows.n_seq * a.H * (dv / 16)));
+#define CHELA_W(E, DK, P)                                                                                             \
+    if (reverse) hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, true>), grid, dim3(256), 0, st, a, dv);              \
+    else hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, false>), grid, dim3(256), 0, st, a, dv)
+    if (dtype != 0) { if (dk == 64) { CHELA_W(float, 64, 1); } else { CHELA_W(float, 128, 1); } }
+    else { if (dk == 64) { CHELA_W(bf16, 64, 2); } else { CHELA_W(bf16, 128, 2); } }
+#undef CHELA_W
+    return hipGetLastError();
+}
+
+// The states in front of all chunks, and T.
+hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st)
+{
+    if (saved == nullptr) saved = ws + p.saved_at;
+    a.places = p.places;
+    a.N = ws + p.N;
+    a.Z = (float*)(ws + p.Z);
+    a.T = saved + p.T;
+    a.S0 = saved + p.S0;
+    a.whole = (float*)(saved + p.whole);
+    if (p.places > 0) {
+        const dim3 grid((unsigned)((size_t)p.places * a.H));
+#define CHELA_RUN(E, DK, DV) hipLaunchKernelGGL((delta_prep_kernel<E, DK, DV, sizeof(E) == 2 ? 2 : 1>), grid, dim3(256), 0, st, a)
+        CHELA_DELTA(CHELA_RUN)
+#undef CHELA_RUN
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return launch_delta_walk(a, false, dk, dv, dtype, st);
+}
+
+hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st)
+{
+    ProfScope prof(KID_DELTA, st);
+    const hipError_t e = launch_delta_states(a, p, ws, saved, dk, dv, dtype, st);
+    if (e != hipSuccess) return e;
+    const bool clear = a.rows.clear && a.rows.cu != nullptr;
+    const size_t blocks = (size_t)p.places * a.H + (clear ? (a.rows.T + 63) / 64 : 0);
+    if (blocks == 0) return hipSuccess;
+    const dim3 grid((unsigned)blocks);
+#define CHELA_RUN(E, DK, DV) hipLaunchKernelGGL((delta_out_kernel<E, DK, DV>), grid, dim3(256), 0, st, a)
+    CHELA_DELTA(CHELA_RUN)
+#undef CHELA_RUN
+    return hipGetLastError();
+}
+
+hipError_t launch_delta_step(const DeltaArgs& a, int dk, int dv, int dtype, hipStream_t st)
+{
+    ProfScope prof(KID_DELTA_STEP, st);
+    const dim3 grid((unsigned)((size_t)a.rows.n_seq * a.H));
+#define CHELA_RUN(E, DK, DV) hipLaunchKernelGGL((delta_step_kernel<E, DK, DV>), grid, dim3(256), 0, st, a)
+    CHELA_DELTA(CHELA_RUN)
+#undef CHELA_RUN
+    return hipGetLastError();
+}
+
+}  // namespace chela
