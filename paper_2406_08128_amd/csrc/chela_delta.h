@@ -22,7 +22,7 @@ template <typename E> constexpr int kPad = sizeof(E) == 2 ? 8 : 4;
 //     k = 16 (j / 4) + 4 q + j % 4,  j = 0..7,
 // the rows that two accumulator tiles, one above the other, have in this lane: a result is the next product's operand as it lies in the
 // registers, summed over its rows.
-// P parts: a value that was worked out in fp32 is rounded to bf16 (P = 1, off by 2^-9) or kept as a sum of two (P = 2, 2^-18).  What the caller
+// P parts: a value that was worked out in fp32 is rounded to bf16 (P = 1, off by 2^-8 at most) or kept as a sum of two (P = 2, 2^-16).  What the caller
 // gave in bf16 has one part.  fp32 operands have all bits, and their products are fp32: eight instructions over four terms each.
 template <typename E, int P> struct Op;
 template <> struct Op<bf16, 1> { bf16x8 h; };

@@ -24,6 +24,12 @@
 //   selscan_bwd(f, f32, saved_bytes, U, delta, A, Bm, Cm, dY, D, Z, delta_bias, softplus, cu, S_in, dS_out, want_dS_in, saved, stream)
 //       -> (dU, ddelta, dA, dB, dC, dD, dZ, ddelta_bias, dS_in)
 //   block_norm_bwd(f, f32, Y, X_out, dX_out, dN, gate, w_post, w_pre, scale, eps, in_place, stream) -> (dY, dgate, dX, dw_post, dw_pre)
+//   gated_delta_fwd(f, f32, saved_bytes, Q, K, V, g, beta, scale, cu, S_in, S_out, slots, want_saved, O, stream) -> (O, saved)
+//   gated_delta_bwd(f, f32, saved_bytes, Q, K, V, g, beta, dO, scale, cu, S_in, dS_out, want_dS_in, saved, stream)
+//       -> (dQ, dK, dV, dg, dbeta, dS_in)
+//   gated_delta_step(f, f32, q, k, v, g, beta, S, scale, slots, o, stream) -> o
+//   layer_norm_fwd(f, f32, X, w, b, Y, eps, stream) -> (X_out, Nrm)
+//   layer_norm_bwd(f, f32, X_out, dN, w, want_db, dX_out, eps, in_place, stream) -> (dX, dw, db)
 // Host side of a call, us, the binding's own lines and these: forward, one launch, 8.5 and 4.4, two launches 9.7 and 6.2; with the
 // state 9.9 and 4.8, 12.1 and 7.2; backward, two launches, 11.4 and 7.5; the three calls of a gated layer's step, six launches, 39.6 and 23;
 // spectrum, forward and gradient of a convolution, 22.5 and 15; both directions on 64 rows of 512 channels: short convolution, four launches, 39 and
@@ -456,6 +462,16 @@ typedef int (*selscan_bwd_fn)(const void*, long long, const void*, long long, co
 typedef int (*block_norm_bwd_fn)(const void*, const void*, const void*, const float*, const float*, const void*, const void*, void*, void*, void*,
                                  float*, float*, float, float, long long, int, int, void*);
 
+#define CHELA_DELTA_IN                                                                                                \
+    const void*, long long, const void*, long long, const void*, long long, const void*, long long, const void*, long long, float
+typedef int (*delta_fwd_fn)(CHELA_DELTA_IN, const int*, int, int, int, int, int, int, const float*, float*, const int*, int, void*, void*, void*);
+typedef int (*delta_bwd_fn)(CHELA_DELTA_IN, const int*, int, int, int, int, int, int, const float*, const void*, long long, const float*,
+                            const void*, void*, void*, void*, void*, void*, float*, void*);
+typedef int (*delta_step_fn)(CHELA_DELTA_IN, float*, const int*, int, int, int, int, int, int, void*, void*);
+typedef size_t (*delta_saved_fn)(int, int, int, int, int, int, int);
+typedef int (*layer_norm_fwd_fn)(const void*, const void*, const float*, const float*, void*, void*, float, long long, int, int, void*);
+typedef int (*layer_norm_bwd_fn)(const void*, const float*, const void*, const void*, void*, float*, float*, float, long long, int, int, void*);
+
 struct Rows {
     c10::DeviceIndex dev;
     at::ScalarType type;
@@ -880,12 +896,238 @@ PyObject* block_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// What the gated delta rule's calls have in common: Q, K, V, g, beta, scale.
+struct Delta {
+    const void *Q, *K, *V, *g = nullptr, *beta;
+    long long ldq, ldk, ldv, ldg = 0, ldb;
+    int64_t H, Hk, dk, dv;
+    float scale;
+    bool read(Rows& x, PyObject* const* five, PyObject* oscale, PyObject* ocu, PyObject* ostream)
+    {
+        if (!PyFloat_CheckExact(oscale) || !x.first(five[4], ocu, ostream) || !x.there(five[0], x.type) || !x.there(five[1], x.type) ||
+            !x.there(five[2], x.type))
+            return false;
+        const at::Tensor &q = THPVariable_Unpack(five[0]), &k = THPVariable_Unpack(five[1]), &v = THPVariable_Unpack(five[2]);
+        if (q.dim() != x.dims + 2 || v.dim() != x.dims + 2 || k.sizes() != q.sizes()) return false;
+        H = x.D;
+        Hk = q.size(-2);
+        dk = q.size(-1);
+        dv = v.size(-1);
+        scale = (float)PyFloat_AS_DOUBLE(oscale);
+        if (v.size(-2) != H || Hk < 1 || H % Hk != 0 || Hk > 0x7fffffff || dk > 0x7fffffff || dv > 0x7fffffff) return false;
+        if (five[3] != Py_None && (!x.rows(five[3], H, &g, &ldg) || THPVariable_Unpack(five[3]).dim() != x.dims + 1)) return false;
+        return x.rows(five[0], Hk * dk, &Q, &ldq) && x.rows(five[1], Hk * dk, &K, &ldk) && x.rows(five[2], H * dv, &V, &ldv) &&
+               x.rows(five[4], H, &beta, &ldb);
+    }
+};
+
+PyObject* gated_delta_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 16) { PyErr_SetString(PyExc_TypeError, "gated_delta_fwd takes sixteen arguments"); return nullptr; }
+    Rows x;
+    Delta s;
+    const float* pin;
+    float* pout;
+    void* po;
+    const int want_saved = flag(a[13]);
+    if (want_saved < 0 || !s.read(x, a + 3, a[8], a[9], a[15]) || !x.slot_map(a[12], a[10] != Py_None ? a[10] : a[11]) ||
+        !x.dense(a[10], at::kFloat, {x.n_slots, s.H, s.dk, s.dv}, true, &pin) ||
+        !x.dense(a[11], at::kFloat, {x.n_slots, s.H, s.dk, s.dv}, true, &pout))
+        Py_RETURN_NONE;
+    const at::Tensor& V = THPVariable_Unpack(a[5]);
+    if (!x.dense(a[14], x.type, V.sizes(), true, &po)) Py_RETURN_NONE;
+    const auto f = address<delta_fwd_fn>(x.function(a));
+    const auto bytes = address<delta_saved_fn>(a[2]);
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor o, saved;
+    int rc;
+    {
+        const without_interpreter_lock free;
+        if (a[14] == Py_None) { o = at::empty(V.sizes(), like(V).memory_format(at::MemoryFormat::Contiguous)); po = o.data_ptr(); }
+        if (want_saved) {
+            const size_t need = bytes((int)x.T, x.n_seq, x.cu != nullptr, (int)s.H, (int)s.dk, (int)s.dv, x.type == at::kFloat);
+            saved = at::empty({(int64_t)(need < 16 ? 16 : need) / 4}, like(V).dtype(at::kFloat));
+        }
+        rc = f(s.Q, s.ldq, s.K, s.ldk, s.V, s.ldv, s.g, s.ldg, s.beta, s.ldb, s.scale, x.cu, x.n_seq, (int)x.T, (int)s.H, (int)s.Hk, (int)s.dk,
+               (int)s.dv, pin, pout, x.slots, x.n_slots, po, want_saved ? saved.data_ptr() : nullptr, stream_of(x.dev));
+    }
+    if (rc != 0) return PyLong_FromLong(rc);
+    PyObject* both = PyTuple_New(2);
+    if (both == nullptr) return nullptr;
+    PyObject *first = given_or(a[14], o), *second = want_saved ? THPVariable_Wrap(std::move(saved)) : none();
+    if (first == nullptr || second == nullptr) { Py_XDECREF(first); Py_XDECREF(second); Py_DECREF(both); return nullptr; }
+    PyTuple_SET_ITEM(both, 0, first);
+    PyTuple_SET_ITEM(both, 1, second);
+    return both;
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* gated_delta_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 16) { PyErr_SetString(PyExc_TypeError, "gated_delta_bwd takes sixteen arguments"); return nullptr; }
+    Rows x;
+    Delta s;
+    const void *pdo, *psaved = nullptr;
+    long long lddo;
+    const float *pin, *pds;
+    const int want = flag(a[13]);
+    if (want < 0 || !s.read(x, a + 3, a[9], a[10], a[15]) || !x.rows(a[8], s.H * s.dv, &pdo, &lddo) ||
+        THPVariable_Unpack(a[8]).sizes() != THPVariable_Unpack(a[5]).sizes() ||
+        !x.dense(a[11], at::kFloat, {x.n_seq, s.H, s.dk, s.dv}, true, &pin) || !x.dense(a[12], at::kFloat, {x.n_seq, s.H, s.dk, s.dv}, true, &pds))
+        Py_RETURN_NONE;
+    const auto f = address<delta_bwd_fn>(x.function(a));
+    const auto bytes = address<delta_saved_fn>(a[2]);
+    if (PyErr_Occurred()) return nullptr;
+    if (a[14] != Py_None) {
+        if (!plain(a[14], at::kFloat, x.dev)) Py_RETURN_NONE;
+        const at::Tensor& saved = THPVariable_Unpack(a[14]);
+        if ((size_t)saved.numel() * 4 < bytes((int)x.T, x.n_seq, x.cu != nullptr, (int)s.H, (int)s.dk, (int)s.dv, x.type == at::kFloat)) Py_RETURN_NONE;
+        psaved = saved.data_ptr();
+    }
+    const at::Tensor &Q = THPVariable_Unpack(a[3]), &V = THPVariable_Unpack(a[5]), &beta = THPVariable_Unpack(a[7]);
+    at::Tensor out[6];
+    int rc;
+    {
+        const without_interpreter_lock free;
+        const at::TensorOptions io = like(V).memory_format(at::MemoryFormat::Contiguous);
+        void *dQ = make(out[0], true, Q.sizes(), io), *dK = make(out[1], true, Q.sizes(), io), *dV = make(out[2], true, V.sizes(), io);
+        void *dg = make(out[3], a[6] != Py_None, beta.sizes(), io), *db = make(out[4], true, beta.sizes(), io);
+        float* ds = make<float>(out[5], want != 0, {x.n_seq, s.H, s.dk, s.dv}, io.dtype(at::kFloat));
+        rc = f(s.Q, s.ldq, s.K, s.ldk, s.V, s.ldv, s.g, s.ldg, s.beta, s.ldb, s.scale, x.cu, x.n_seq, (int)x.T, (int)s.H, (int)s.Hk, (int)s.dk,
+               (int)s.dv, pin, pdo, lddo, pds, psaved, dQ, dK, dV, dg, db, ds, stream_of(x.dev));
+    }
+    return rc != 0 ? PyLong_FromLong(rc) : wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* gated_delta_step(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 12) { PyErr_SetString(PyExc_TypeError, "gated_delta_step takes twelve arguments"); return nullptr; }
+    Rows x;
+    Delta s;
+    float* ps;
+    void* po;
+    if (!s.read(x, a + 2, a[8], Py_None, a[11]) || x.dims != 1) Py_RETURN_NONE;
+    x.n_seq = x.n_slots = (int)x.T;
+    if (!x.slot_map(a[9], a[7]) || !x.dense(a[7], at::kFloat, {x.n_slots, s.H, s.dk, s.dv}, false, &ps) ||
+        !x.dense(a[10], x.type, {x.T, s.H, s.dv}, true, &po))
+        Py_RETURN_NONE;
+    const auto f = address<delta_step_fn>(x.function(a));
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor o;
+    int rc;
+    {
+        const without_interpreter_lock free;
+        if (a[10] == Py_None) { o = at::empty({x.T, s.H, s.dv}, like(THPVariable_Unpack(a[4]))); po = o.data_ptr(); }
+        rc = f(s.Q, s.ldq, s.K, s.ldk, s.V, s.ldv, s.g, s.ldg, s.beta, s.ldb, s.scale, ps, x.slots, x.n_slots, (int)x.T, (int)s.H, (int)s.Hk,
+               (int)s.dk, (int)s.dv, po, stream_of(x.dev));
+    }
+    return rc != 0 ? PyLong_FromLong(rc) : given_or(a[10], o);
+    END_HANDLE_TH_ERRORS
+}
+
+// The stream X, and beside it a tensor of the I/O type (or X's own).
+struct Stream {
+    Rows x;
+    at::ScalarType type;             // X's
+    int64_t D;
+    const void* pX;
+    bool read(PyObject* oX, PyObject* beside, PyObject* oeps, PyObject* ostream)
+    {
+        if (modes() || ostream != Py_None || !PyFloat_CheckExact(oeps) || !on_gpu(oX) || (beside != Py_None && !on_gpu(beside))) return false;
+        x.dev = c10::hip::current_device();
+        const at::Tensor& X = THPVariable_Unpack(oX);
+        type = X.scalar_type();
+        x.type = beside != Py_None ? THPVariable_Unpack(beside).scalar_type() : type;
+        if ((x.type != at::kBFloat16 && x.type != at::kFloat) || (type != x.type && type != at::kFloat) || X.dim() < 1) return false;
+        D = X.size(-1);
+        return D >= 1 && D <= 0x7fffffff && x.dense(oX, type, X.sizes(), false, &pX);
+    }
+};
+
+PyObject* layer_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 8) { PyErr_SetString(PyExc_TypeError, "layer_norm_fwd takes eight arguments"); return nullptr; }
+    Stream s;
+    const void* pY;
+    const float *pw, *pb;
+    if (!s.read(a[2], a[5], a[6], a[7])) Py_RETURN_NONE;
+    const at::Tensor& X = THPVariable_Unpack(a[2]);
+    if (!s.x.dense(a[5], s.x.type, X.sizes(), true, &pY) || !s.x.dense(a[3], at::kFloat, {s.D}, true, &pw) ||
+        !s.x.dense(a[4], at::kFloat, {s.D}, true, &pb))
+        Py_RETURN_NONE;
+    const auto f = address<layer_norm_fwd_fn>(s.x.function(a));
+    if (PyErr_Occurred()) return nullptr;
+    const float eps = (float)PyFloat_AS_DOUBLE(a[6]);
+    at::Tensor out[2];
+    int rc;
+    {
+        const without_interpreter_lock free;
+        void* px = make(out[0], a[5] != Py_None, X.sizes(), like(X));
+        void* pn = make(out[1], true, X.sizes(), like(X).dtype(s.x.type));
+        rc = f(s.pX, pY, pw, pb, px, pn, eps, (long long)(X.numel() / s.D), (int)s.D, s.type != s.x.type, stream_of(s.x.dev));
+    }
+    if (rc != 0) return PyLong_FromLong(rc);
+    PyObject* both = wrap(out);
+    if (both != nullptr && a[5] == Py_None) {
+        PyObject* was = PyTuple_GET_ITEM(both, 0);
+        Py_INCREF(a[2]);
+        PyTuple_SET_ITEM(both, 0, a[2]);
+        Py_DECREF(was);
+    }
+    return both;
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject* layer_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 10) { PyErr_SetString(PyExc_TypeError, "layer_norm_bwd takes ten arguments"); return nullptr; }
+    const int want_db = flag(a[5]), in_place = flag(a[8]);
+    Stream s;
+    const void* pdn;
+    void* pdx;
+    const float* pw;
+    if (want_db < 0 || in_place < 0 || (in_place && a[6] == Py_None) || !s.read(a[2], a[3], a[7], a[9]) || a[3] == Py_None) Py_RETURN_NONE;
+    const at::Tensor& X = THPVariable_Unpack(a[2]);
+    if (!s.x.dense(a[3], s.x.type, X.sizes(), false, &pdn) || !s.x.dense(a[6], s.type, X.sizes(), true, &pdx) ||
+        !s.x.dense(a[4], at::kFloat, {s.D}, true, &pw))
+        Py_RETURN_NONE;
+    const auto f = address<layer_norm_bwd_fn>(s.x.function(a));
+    if (PyErr_Occurred()) return nullptr;
+    const float eps = (float)PyFloat_AS_DOUBLE(a[7]);
+    at::Tensor out[3];
+    int rc;
+    {
+        const without_interpreter_lock free;
+        const at::TensorOptions f32 = like(X).dtype(at::kFloat);
+        void* dX = in_place ? pdx : make(out[0], true, X.sizes(), like(X));
+        float *dw = make<float>(out[1], a[4] != Py_None, {s.D}, f32), *db = make<float>(out[2], want_db != 0, {s.D}, f32);
+        rc = f(s.pX, pw, pdx, pdn, dX, dw, db, eps, (long long)(X.numel() / s.D), (int)s.D, s.type != s.x.type, stream_of(s.x.dev));
+    }
+    if (rc != 0) return PyLong_FromLong(rc);
+    PyObject* all = wrap(out);
+    if (all != nullptr && in_place) {
+        PyObject* was = PyTuple_GET_ITEM(all, 0);
+        Py_INCREF(a[6]);
+        PyTuple_SET_ITEM(all, 0, a[6]);
+        Py_DECREF(was);
+    }
+    return all;
+    END_HANDLE_TH_ERRORS
+}
+
 #define CHELA_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CHELA_METHOD(step), CHELA_METHOD(forward), CHELA_METHOD(backward), CHELA_METHOD(gated),
                          CHELA_METHOD(gate_norm_bwd), CHELA_METHOD(zbwd_saved), CHELA_METHOD(spectrum), CHELA_METHOD(conv_fwd),
                          CHELA_METHOD(conv_bwd), CHELA_METHOD(short_conv_fwd), CHELA_METHOD(short_conv_step), CHELA_METHOD(selscan_fwd),
                          CHELA_METHOD(selscan_step), CHELA_METHOD(block_norm_fwd), CHELA_METHOD(short_conv_bwd), CHELA_METHOD(selscan_bwd),
-                         CHELA_METHOD(block_norm_bwd), {nullptr, nullptr, 0, nullptr}};
+                         CHELA_METHOD(block_norm_bwd), CHELA_METHOD(gated_delta_fwd), CHELA_METHOD(gated_delta_bwd),
+                         CHELA_METHOD(gated_delta_step), CHELA_METHOD(layer_norm_fwd), CHELA_METHOD(layer_norm_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_chela_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -4,7 +4,8 @@
 // Gradient, from X' (its statistics are worked out again), with v = dN w:
 //     dX = dX' + s (v - mean v - n mean(v n)),   dw = sum dN n,   db = sum dN.
 // Memory-bound: a row stays in the registers of TPR threads, so every tensor is read or written once; the squares are taken behind the mean, from
-// what is left of the row without it (a difference of two sums would lose the digits that a stream far from zero has in common).
+// what is left of the row without it (a difference of two sums would lose the digits that a stream far from zero has in common), and what of
+// the mean is left there, off as it is by its own rounding, goes with the same sums.
 #include "chela_rowparts.h"
 
 namespace chela {
@@ -31,7 +32,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void layer_norm_kernel(Layer
     typedef RowPart<XT, TPR, NV, VEC> PX;
     typedef RowPart<float, TPR, NV, VEC> PW;
     constexpr int E = P::E, RPW = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float s_a[TPR / 64][1], s_b[TPR / 64][1];
+    __shared__ float s_a[TPR / 64][1], s_b[TPR / 64][2];
     const int tid = threadIdx.x % TPR, D = a.D;
     const float inv = 1.f / (float)D;
     float w[E], b[E];
@@ -68,13 +69,16 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void layer_norm_kernel(Layer
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] -= m;
         only_in_row<TPR, NV, VEC>(D, tid, x);
-        sum[0] = 0.f;
+        float sums[2] = {0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum[0] = fmaf(x[e], x[e], sum[0]);
-        row_sums<TPR, 1>(sum, s_b);
-        const float s = __builtin_amdgcn_rsqf(fmaf(sum[0], inv, a.eps));
+        for (int e = 0; e < E; ++e) {
+            sums[0] += x[e];
+            sums[1] = fmaf(x[e], x[e], sums[1]);
+        }
+        row_sums<TPR, 2>(sums, s_b);
+        const float left = sums[0] * inv, s = __builtin_amdgcn_rsqf(fmaxf(fmaf(sums[1], inv, -left * left), 0.f) + a.eps);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = fmaf(x[e] * s, w[e], b[e]);
+        for (int e = 0; e < E; ++e) x[e] = fmaf((x[e] - left) * s, w[e], b[e]);
         P::store((IO*)a.Nrm + (size_t)r * D, D, tid, x);
         // (a wave writes its sums of the next row only after all waves have read those of this one)
         if (TPR > 64) __syncthreads();
@@ -90,7 +94,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void layer_norm_bwd_kernel(L
     typedef RowPart<float, TPR, NV, VEC> PW;
     constexpr int E = P::E, RPW = TPR < 256 ? 256 / TPR : 1;
     constexpr bool AHEAD = NV < 4 || sizeof(IO) == 2; // (there are registers for the next row)
-    __shared__ float s_a[TPR / 64][2], s_b[TPR / 64][2], s_w[2][RPW > 1 ? TPR * E : 1];
+    __shared__ float s_a[TPR / 64][2], s_b[TPR / 64][3], s_w[2][RPW > 1 ? TPR * E : 1];
     const int tid = threadIdx.x % TPR, D = a.D;
     const float inv = 1.f / (float)D;
     float w[E], dw[E], db[E];
@@ -130,17 +134,19 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void layer_norm_bwd_kernel(L
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] -= m;
         only_in_row<TPR, NV, VEC>(D, tid, x);
-        sums[0] = sums[1] = 0.f;
+        float three[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            sums[0] = fmaf(x[e], x[e], sums[0]);
-            sums[1] = fmaf(d[e] * w[e], x[e], sums[1]);
+            three[0] += x[e];
+            three[1] = fmaf(x[e], x[e], three[1]);
+            three[2] = fmaf(d[e] * w[e], x[e], three[2]);
         }
-        row_sums<TPR, 2>(sums, s_b);
-        const float s = __builtin_amdgcn_rsqf(fmaf(sums[0], inv, a.eps)), mvn = sums[1] * inv * s;
+        row_sums<TPR, 3>(three, s_b);
+        const float left = three[0] * inv, s = __builtin_amdgcn_rsqf(fmaxf(fmaf(three[1], inv, -left * left), 0.f) + a.eps);
+        const float mvn = fmaf(three[2], inv, -left * mv) * s;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float n = x[e] * s;
+            const float n = (x[e] - left) * s;
             dw[e] = fmaf(d[e], n, dw[e]);
             db[e] += d[e];
             dx[e] = fmaf(s, fmaf(-n, mvn, fmaf(d[e], w[e], -mv)), dx[e]);
