@@ -24,6 +24,10 @@ template <typename E> constexpr int kPad = sizeof(E) == 2 ? 8 : 4;
 // registers, summed over its rows.
 // P parts: a value that was worked out in fp32 is rounded to bf16 (P = 1, off by 2^-8 at most) or kept as a sum of two (P = 2, 2^-16).  What the caller
 // gave in bf16 has one part.  fp32 operands have all bits, and their products are fp32: eight instructions over four terms each.
+// Operands that stay in registers have two parts where the result goes into a state, or through the inverse: they cost matrix instructions, of
+// which there are enough.  Those that go through memory (N, T, the states that the outputs are made of) have one, and N and T two in calls that
+// take or return states in fp32: with one part each everywhere bf16 outputs are 4.1e-3 to 5.0e-3 off (root mean square, relative, of
+// which 1.7e-3 are their own rounding; one head of 64, 4096 tokens without decay), so 3.0e-3 to 3.7e-3, with N and T in two 2.7e-3 to 3.4e-3.
 template <typename E, int P> struct Op;
 template <> struct Op<bf16, 1> { bf16x8 h; };
 template <> struct Op<bf16, 2> { bf16x8 h, l; };
@@ -166,6 +170,8 @@ __device__ __forceinline__ Op<E, P> load_op(const E* from, int lane)
     }
 }
 
+// LDS is read again behind this: operands that one column group after the other needs would otherwise all be kept in registers.
+__device__ __forceinline__ void read_afresh() { asm volatile("" ::: "memory"); }
 __device__ __forceinline__ f32x4 zero4() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
 __device__ __forceinline__ f32x4 splat4(float x) { return f32x4{x, x, x, x}; }
 
@@ -221,29 +227,48 @@ struct ChunkSteps {
     float whole;                                                       // e^(gamma of the last token)
     __device__ __forceinline__ float decay(int t, int s) const { return exp2_(kLog2e * ((hi[t] - hi[s]) + (lo[t] - lo[s]))); }
 };
-// By the first wave; n rows there are, the rest as if they were not (no decay, beta of zero).
-template <typename E, int C>
-__device__ __forceinline__ void load_steps(ChunkSteps<C>& st, const E* g, long ldg, const E* beta, long ldb, int row, int h, int n, int tid)
+// Sums over the lanes up to each, by DPP: within rows of 16 lanes, then the rows' totals.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double plus_dpp(double x)
+{
+    typedef __attribute__((ext_vector_type(2))) int i32x2;
+    const i32x2 v = __builtin_bit_cast(i32x2, x);
+    const i32x2 y{__builtin_amdgcn_update_dpp(0, v[0], CTRL, ROWS, 0xf, false), __builtin_amdgcn_update_dpp(0, v[1], CTRL, ROWS, 0xf, false)};
+    return x + __builtin_bit_cast(double, y);
+}
+__device__ __forceinline__ double running_sum(double x)
+{
+    x = plus_dpp<0x111, 0xf>(x);
+    x = plus_dpp<0x112, 0xf>(x);
+    x = plus_dpp<0x114, 0xf>(x);
+    x = plus_dpp<0x118, 0xf>(x);
+    x = plus_dpp<0x142, 0xa>(x);           // lane 15's to the second row, 47's to the fourth
+    return plus_dpp<0x143, 0xc>(x);        // lane 31's to the upper two
+}
+// The log decay and beta of this lane's token, on their way; n rows there are, the rest are as if they were not (no decay, beta of zero).
+struct Steps { float g, beta; };
+template <typename E>
+__device__ __forceinline__ Steps fetch_steps(const E* g, long ldg, const E* beta, long ldb, int row, int h, int n, int lane)
+{
+    const size_t t = (size_t)row + min(lane, n - 1);
+    return Steps{g != nullptr ? to_f(g[t * ldg + h]) : 0.f, to_f(beta[t * ldb + h])};
+}
+// By the first wave.
+template <int C>
+__device__ __forceinline__ void put_steps(ChunkSteps<C>& st, const Steps& x, int n, int tid)
 {
     if (tid < 64) {
         const int t = tid;
-        const bool on = t < n;
-        float x = on && g != nullptr ? to_f(g[(size_t)(row + (on ? t : 0)) * ldg + h]) : 0.f;
-        const float b = on ? to_f(beta[(size_t)(row + t) * ldb + h]) : 0.f;
-        if (x < -256.f) x = -256.f;
-        double s = (double)x;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const double y = __shfl_up(s, d);
-            if (t >= d) s += y;
-        }
-        const double last = __shfl(s, 63);
+        const float b = t < n ? x.beta : 0.f, g = t < n ? (x.g < -256.f ? -256.f : x.g) : 0.f;
+        const double s = running_sum((double)g);
+        typedef __attribute__((ext_vector_type(2))) int i32x2;
+        const i32x2 v = __builtin_bit_cast(i32x2, s);
+        const double last = __builtin_bit_cast(double, i32x2{__builtin_amdgcn_readlane(v[0], 63), __builtin_amdgcn_readlane(v[1], 63)});
         if (t < C) {
-            const float hi = (float)s;
+            const float hi = (float)s, up = exp2_(kLog2e * hi);
             st.hi[t] = hi;
             st.lo[t] = (float)(s - (double)hi);
             st.beta[t] = b;
-            const float up = exp2_(kLog2e * (float)s);
             st.up[t] = up;
             st.bu[t] = -b * up;
             st.down[t] = exp2_(kLog2e * (float)(last - s));
@@ -264,23 +289,31 @@ __device__ __forceinline__ Op<E, P> scaled(const Op<E, 1>& x, const float* f, in
     return operand<E, P>(__builtin_shufflevector(v, v, 0, 1, 2, 3), __builtin_shufflevector(v, v, 4, 5, 6, 7));
 }
 
-// A chunk's rows of one head into LDS, zeros behind the n there are.  (Rows begin on an element: loads of global memory need no more.)
+// A chunk's rows of one head, C of D elements, from memory to LDS by way of the registers of 256 threads, zeros behind the n there are (the last
+// row again is what is read for them: no load waits for a comparison).  Rows begin on an element: loads of global memory need no more.
 template <typename E, int C, int D>
-__device__ __forceinline__ void load_tile(E* to, int ld, const E* from, long ldf, int row, int n, int tid, int threads)
-{
-    constexpr int W = 16 / sizeof(E);
-    typedef unsigned Piece __attribute__((ext_vector_type(4)));
-    struct __attribute__((packed, aligned(sizeof(E)))) Loose { Piece p; };
+struct Tile {
+    static constexpr int W = 16 / sizeof(E), M = C * (D / W) / 256;
+    static_assert(C * (D / W) % 256 == 0, "whole pieces for all threads");
+    u32x4 x[M];
+    __device__ __forceinline__ void fetch(const E* from, long ld, int row, int n, int tid)
+    {
+        struct __attribute__((packed, aligned(sizeof(E)))) Loose { u32x4 p; };
 #pragma unroll
-    for (int i = tid; i < C * (D / W); i += threads) {
-        const int t = i / (D / W), k = i % (D / W) * W;
-        Piece x = Piece(0);
-        if (t < n) {
-            x = ((const Loose*)(from + (size_t)(row + t) * ldf + k))->p;
+        for (int m = 0; m < M; ++m) {
+            const int i = m * 256 + tid, t = i / (D / W), k = i % (D / W) * W;
+            x[m] = ((const Loose*)(from + (size_t)(row + min(t, n - 1)) * ld + k))->p;
         }
-        *(Piece*)(to + t * ld + k) = x;
     }
-}
+    __device__ __forceinline__ void put(E* to, int ldt, int n, int tid) const
+    {
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const int i = m * 256 + tid, t = i / (D / W), k = i % (D / W) * W;
+            *(u32x4*)(to + t * ldt + k) = t < n ? x[m] : u32x4{0, 0, 0, 0};
+        }
+    }
+};
 
 // Rows of no sequence: zeros in all of `width` elements of each, sixty-four rows to a workgroup.
 template <typename E>
@@ -294,6 +327,78 @@ __device__ __forceinline__ void clear_rows(const Rows& r, int block, E* to, int 
         E* row = to + (size_t)t * width;
         for (int i = threadIdx.x; i < width; i += 256) row[i] = (E)0.f;
     }
+}
+
+// T = (1 + A)^-1 of a chunk, A_ts = beta_t e^(gamma_t - gamma_s) k_t . k_s below the diagonal, from its keys in LDS; all 256 threads, sA [C][C + 4] and sD
+// [C][20] are room for them.  fp32 throughout: blocks of 16 on the diagonal row by row, those below by products with them.
+template <typename E, int DK, int P, int C>
+__device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSteps<C>& st, float* sA, float* sD, const Planes<E, P>& T, int tid)
+{
+    constexpr int NB = C / 16, LA = C + 4, LD = 20;
+    const int lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
+    // A, sixteen tokens to a wave
+    if (w < NB) {
+        const int t = 16 * w + c;
+        for (int sb = 0; sb <= w; ++sb) {
+            f32x4 x = zero4();
+#pragma unroll
+            for (int ks = 0; ks < DK / 32; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sK, LK, 16 * w, 32 * ks, lane), x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int s = 16 * sb + 4 * q + i;
+                x[i] = s < t ? st.beta[t] * st.decay(t, s) * x[i] : 0.f;
+            }
+            *(f32x4*)(sA + t * LA + 16 * sb + 4 * q) = x;
+        }
+    }
+    __syncthreads();
+    // the inverses of 1 + A's blocks on the diagonal, a lane to a column: x_i = e_i - sum_{j<i} A_ij x_j
+    if (tid < C) {
+        const float* A = sA + 16 * q * LA + 16 * q;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float s = i == c ? 1.f : 0.f;
+#pragma unroll
+            for (int j4 = 0; j4 < (i + 3) / 4; ++j4) {
+                const f32x4 r = *(const f32x4*)(A + i * LA + 4 * j4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (4 * j4 + j < i) s = fmaf(-r[j], x[4 * j4 + j], s);
+            }
+            x[i] = s;
+            sD[(16 * q + i) * LD + c] = s;
+        }
+    }
+    __syncthreads();
+    // the blocks below it, a wave to a column of blocks: T_rj = -T_rr sum_{j<=b<r} A_rb T_bj, fp32 products
+    f32x4 t[NB];
+    if (w < NB) {
+#pragma unroll
+        for (int r = 0; r < NB; ++r) {
+            t[r] = zero4();
+            if (r == w) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[r][i] = sD[(16 * r + 4 * q + i) * LD + c];
+            } else if (r > w) {
+                f32x4 x = zero4();
+#pragma unroll
+                for (int b = 0; b < r; ++b)
+                    if (b >= w) {
+                        const f32x4 m = *(const f32x4*)(sA + (16 * r + c) * LA + 16 * b + 4 * q);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(m[i], t[b][i], x, 0, 0, 0);
+                    }
+                const f32x4 m = *(const f32x4*)(sD + (16 * r + c) * LD + 4 * q);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(-m[i], x[i], t[r], 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < NB; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) T.put(16 * r + 4 * q + i, 16 * w + c, t[r][i]);
+    }
+    __syncthreads();
 }
 
 // RUN(element type, DK, DV) for a call's.

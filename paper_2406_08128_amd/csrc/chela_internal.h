@@ -279,7 +279,7 @@ hipError_t launch_block_norm_fwd(const BlockNormArgs& a, int dtype, hipStream_t 
 hipError_t launch_block_norm_bwd(const BlockNormArgs& a, int dtype, hipStream_t st);
 
 // Gated delta rule.  A sequence's rows are cut into chunks (of kDeltaChunkBf16 or kDeltaChunkF32 tokens); `places` is how many there may be,
-// and each has room for what the kernels hand to each other, per head.
+// and each has room for what the kernels hand to each other, per head.  states: of a call with states or their gradients, given or wanted.
 struct DeltaPlan {
     int chunk, places, parts;             // parts: of the operands that a state goes through (1, or 2 in bf16)
     size_t N, Z, bytes;                   // byte offsets into the scratch, and its size
@@ -300,10 +300,10 @@ struct DeltaArgs {
 };
 constexpr int kDeltaChunkBf16 = 64, kDeltaChunkF32 = 32;
 bool delta_dims_ok(int dk, int dv);
-DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved);
+DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states);
 hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st);
-hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int dk, int dv, int dtype, hipStream_t st);
+hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int parts, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_bwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, bool has_saved, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_step(const DeltaArgs& a, int dk, int dv, int dtype, hipStream_t st);
 

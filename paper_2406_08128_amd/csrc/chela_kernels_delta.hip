@@ -15,99 +15,42 @@ namespace chela {
 
 // ---- a chunk's T, N and Z
 template <typename E, int DK, int DV, int P>
-__global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a)
+__global__ __launch_bounds__(256, 2) void delta_prep_kernel(DeltaArgs a)
 {
-    constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>, LA = C + 4, LD = 20;
-    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[2 * C * LT];
-    __shared__ __align__(16) float sA[C * LA], sD[C * LD];
+    constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
+    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[P * C * LT];
+    __shared__ __align__(16) float sA[C * (C + 4)], sD[C * 20];
     __shared__ ChunkSteps<C> st;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
     const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
     const Chunk ch = chunk_at(a.rows, C, place, lane);
     if (ch.n <= 0) return;
-    load_tile<E, C, DK>(sK, LK, (const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid, 256);
-    load_tile<E, C, DV>(sV, LV, (const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid, 256);
-    load_steps<E, C>(st, (const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, tid);
-    __syncthreads();
-    // A, sixteen tokens to a wave
-    if (w < NB) {
-        const int t = 16 * w + c;
-        for (int sb = 0; sb <= w; ++sb) {
-            f32x4 x = zero4();
-#pragma unroll
-            for (int ks = 0; ks < DK / 32; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sK, LK, 16 * w, 32 * ks, lane), x);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int s = 16 * sb + 4 * q + i;
-                x[i] = s < t ? st.beta[t] * st.decay(t, s) * x[i] : 0.f;
-            }
-            *(f32x4*)(sA + t * LA + 16 * sb + 4 * q) = x;
-        }
+    {
+        Tile<E, C, DK> k;
+        Tile<E, C, DV> v;
+        const Steps s = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, lane);
+        k.fetch((const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid);
+        v.fetch((const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid);
+        put_steps(st, s, ch.n, tid);
+        k.put(sK, LK, ch.n, tid);
+        v.put(sV, LV, ch.n, tid);
     }
     __syncthreads();
-    // the inverses of 1 + A's blocks on the diagonal, a lane to a column: x_i = e_i - sum_{j<i} A_ij x_j
-    if (tid < C) {
-        const float* A = sA + 16 * q * LA + 16 * q;
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float s = i == c ? 1.f : 0.f;
-#pragma unroll
-            for (int j4 = 0; j4 < (i + 3) / 4; ++j4) {
-                const f32x4 r = *(const f32x4*)(A + i * LA + 4 * j4);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) if (4 * j4 + j < i) s = fmaf(-r[j], x[4 * j4 + j], s);
-            }
-            x[i] = s;
-            sD[(16 * q + i) * LD + c] = s;
-        }
-    }
-    __syncthreads();
-    // the blocks below it, a wave to a column of blocks: T_rj = -T_rr sum_{j<=b<r} A_rb T_bj, fp32 products
-    f32x4 t[NB];
-    if (w < NB) {
-#pragma unroll
-        for (int r = 0; r < NB; ++r) {
-            t[r] = zero4();
-            if (r == w) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) t[r][i] = sD[(16 * r + 4 * q + i) * LD + c];
-            } else if (r > w) {
-                f32x4 x = zero4();
-#pragma unroll
-                for (int b = 0; b < r; ++b)
-                    if (b >= w) {
-                        const f32x4 m = *(const f32x4*)(sA + (16 * r + c) * LA + 16 * b + 4 * q);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(m[i], t[b][i], x, 0, 0, 0);
-                    }
-                const f32x4 m = *(const f32x4*)(sD + (16 * r + c) * LD + 4 * q);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) t[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(-m[i], x[i], t[r], 0, 0, 0);
-            }
-        }
-        const Planes<E, 2> T{sT, LT, C * LT};
-#pragma unroll
-        for (int r = 0; r < NB; ++r)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) T.put(16 * r + 4 * q + i, 16 * w + c, t[r][i]);
-    }
-    __syncthreads();
+    const Planes<E, P> T{sT, LT, C * LT};
+    chunk_inverse<E, DK>(sK, LK, st, sA, sD, T, tid);
     const size_t at = (size_t)place * a.H + h;
     {
-        // T for the kernels behind, its first parts and (bf16) its second
-        constexpr int W = 16 / sizeof(E), PT = sizeof(E) == 2 ? 2 : 1;
-        E* to = (E*)a.T + at * (PT * C * C);
+        // T for the kernels behind
+        constexpr int W = 16 / sizeof(E);
+        E* to = (E*)a.T + at * (C * C);
 #pragma unroll
-        for (int i = tid; i < PT * C * (C / W); i += 256) {
-            const int part = i / (C * (C / W)), r = i % (C * (C / W)) / (C / W), k = i % (C / W) * W;
-            *(u32x4*)(to + part * C * C + r * C + k) = *(const u32x4*)(sT + part * C * LT + r * LT + k);
-        }
+        for (int i = tid; i < C * (C / W); i += 256) *(u32x4*)(to + i * W) = *(const u32x4*)(sT + i / (C / W) * LT + i % (C / W) * W);
         if (tid == 0) a.whole[at] = st.whole;
     }
     // T (beta e^gamma K), T (beta V), thirty-two columns at a time, and what K~ makes of them
-    const Planes<E, P> T{sT, LT, C * LT};
+#pragma unroll 1
     for (int p = w; p < (DK + DV) / 32; p += 4) {
+        read_afresh();
         const bool of_k = p < DK / 32;
         const int col = 32 * (of_k ? p : p - DK / 32);
         const E* X = of_k ? sK : sV;
@@ -118,8 +61,8 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a)
         for (int b = 0; b < NB; ++b) y[b][0] = y[b][1] = zero4();
 #pragma unroll
         for (int ks = 0; ks < KC; ++ks) {
-            const Op<E, P> x0 = scaled<E, P>(cols_op(X, ldx, 32 * ks, col, lane), f, 32 * ks, lane);
-            const Op<E, P> x1 = scaled<E, P>(cols_op(X, ldx, 32 * ks, col + 16, lane), f, 32 * ks, lane);
+            const Op<E, 2> x0 = scaled<E, 2>(cols_op(X, ldx, 32 * ks, col, lane), f, 32 * ks, lane);
+            const Op<E, 2> x1 = scaled<E, 2>(cols_op(X, ldx, 32 * ks, col + 16, lane), f, 32 * ks, lane);
 #pragma unroll
             for (int b = 2 * ks; b < NB; ++b) {
                 const Op<E, P> m = T.rows(16 * b, 32 * ks, lane);
@@ -127,7 +70,7 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a)
                 y[b][1] = mma(m, x1, y[b][1]);
             }
         }
-        Op<E, P> yo[KC][2];
+        Op<E, 2> yo[KC][2];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             const f32x4 d = *(const f32x4*)(st.down + 16 * b + 4 * q);
@@ -136,8 +79,8 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a)
         }
 #pragma unroll
         for (int ks = 0; ks < KC; ++ks) {
-            yo[ks][0] = operand<E, P>(y[2 * ks][0], y[2 * ks + 1][0]);
-            yo[ks][1] = operand<E, P>(y[2 * ks][1], y[2 * ks + 1][1]);
+            yo[ks][0] = operand<E, 2>(y[2 * ks][0], y[2 * ks + 1][0]);
+            yo[ks][1] = operand<E, 2>(y[2 * ks][1], y[2 * ks + 1][1]);
         }
 #pragma unroll
         for (int n = 0; n < DK / 16; ++n) {
@@ -165,12 +108,14 @@ __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaArgs a)
 template <typename E, int DK, int P, bool REV>
 __global__ __launch_bounds__(256) void delta_walk_kernel(DeltaArgs a, int DV)
 {
-    constexpr int C = DeltaChunk<E>::C, TW = DK / 64, KS = DK / 32, OE = kOpElems<E, P>;
+    constexpr int C = DeltaChunk<E>::C, TW = DK / 64, KS = DK / 32, NE = kOpElems<E, P>, OE = kOpElems<E, 2>;
     constexpr int AHEAD = (DK == 64 ? 4 : 2);
     __shared__ __align__(16) E sS[2][KS * OE];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
-    const int groups = DV / 16;
-    const int eg = blockIdx.x % groups, h = blockIdx.x / groups % a.H, seq = blockIdx.x / groups / a.H;
+    // (workgroups go to the eight L2s in turn: those of one head, which read the same N, to one of them)
+    const int groups = DV / 16, all = a.rows.n_seq * a.H * groups, id = (int)(blockIdx.x & 7) * ((all + 7) / 8) + (int)(blockIdx.x >> 3);
+    if (id >= all) return;
+    const int eg = id % groups, h = id / groups % a.H, seq = id / groups / a.H;
     const int first = chunk_key(a.rows, C, seq), n = min(chunks_in(a.rows, C, seq), a.places - first);
     const int slot = slot_of(a.rows, seq);
     const float* from = REV ? a.dS_out : a.S_in;
@@ -197,7 +142,7 @@ __global__ __launch_bounds__(256) void delta_walk_kernel(DeltaArgs a, int DV)
             Z[u][i] = *(const f32x4*)(a.Z + at * ((size_t)DK * DV) + (size_t)(eg * (DK / 16) + TW * w + i) * 256 + 4 * lane);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
-                N[u][i][ks] = load_op<E, P>((const E*)a.N + (at * (DK / 16 * KS) + (TW * w + i) * KS + ks) * OE, lane);
+                N[u][i][ks] = load_op<E, P>((const E*)a.N + (at * (DK / 16 * KS) + (TW * w + i) * KS + ks) * NE, lane);
         }
     };
     if (n > 0) {
@@ -213,9 +158,9 @@ __global__ __launch_bounds__(256) void delta_walk_kernel(DeltaArgs a, int DV)
             const size_t at = (size_t)(first + (REV ? n - 1 - k : k)) * a.H + h;
             E* out = keep + at * ((size_t)DK * DV) + (size_t)eg * (DK * 16);
             if constexpr (TW == 2) {
-                const Op<E, P> o = operand<E, P>(S[0], S[1]);
-                store_op<E, P>(x + w * OE, o, lane);
-                store_op<E, 1>(out + w * 512, [&] { if constexpr (sizeof(E) == 4) return Op<E, 1>{o.v}; else return Op<E, 1>{o.h}; }(), lane);
+                const Op<E, 2> o = operand<E, 2>(S[0], S[1]);
+                store_op<E, 2>(x + w * OE, o, lane);
+                store_op<E, 1>(out + w * 512, first_part(o), lane);
             } else {
                 E* half = x + (w >> 1) * OE + 8 * lane + 4 * (w & 1);
                 E* out_half = out + (w >> 1) * 512 + 8 * lane + 4 * (w & 1);
@@ -226,7 +171,7 @@ __global__ __launch_bounds__(256) void delta_walk_kernel(DeltaArgs a, int DV)
                     const bf16x4 hi = __builtin_convertvector(S[0], bf16x4);
                     *(bf16x4*)half = hi;
                     *(bf16x4*)out_half = hi;
-                    if constexpr (P == 2) *(bf16x4*)(half + 512) = __builtin_convertvector(S[0] - __builtin_convertvector(hi, f32x4), bf16x4);
+                    *(bf16x4*)(half + 512) = __builtin_convertvector(S[0] - __builtin_convertvector(hi, f32x4), bf16x4);
                 }
             }
             __syncthreads();
@@ -234,7 +179,7 @@ __global__ __launch_bounds__(256) void delta_walk_kernel(DeltaArgs a, int DV)
             for (int i = 0; i < TW; ++i) S[i] = S[i] * whole[u] + Z[u][i];
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                const Op<E, P> o = load_op<E, P>(x + ks * OE, lane);
+                const Op<E, 2> o = load_op<E, 2>(x + ks * OE, lane);
 #pragma unroll
                 for (int i = 0; i < TW; ++i) S[i] = mma(N[u][i][ks], o, S[i]);
             }
@@ -250,7 +195,7 @@ __global__ __launch_bounds__(256) void delta_walk_kernel(DeltaArgs a, int DV)
 
 // ---- the outputs
 template <typename E, int DK, int DV>
-__global__ __launch_bounds__(256) void delta_out_kernel(DeltaArgs a)
+__global__ __launch_bounds__(256, DK + DV == 128 ? 3 : 2) void delta_out_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
     __shared__ __align__(16) E sK[C * LK], sQ[C * LK], sV[C * LV], sT[C * LT], sP[C * LT];
@@ -264,11 +209,25 @@ __global__ __launch_bounds__(256) void delta_out_kernel(DeltaArgs a)
     const Chunk ch = chunk_at(a.rows, C, place, lane);
     if (ch.n <= 0) return;
     const size_t at = (size_t)place * a.H + h;
-    load_tile<E, C, DK>(sK, LK, (const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid, 256);
-    load_tile<E, C, DK>(sQ, LK, (const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid, 256);
-    load_tile<E, C, DV>(sV, LV, (const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid, 256);
-    load_tile<E, C, C>(sT, LT, (const E*)a.T + at * ((sizeof(E) == 2 ? 2 : 1) * C * C), C, 0, C, tid, 256);
-    load_steps<E, C>(st, (const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, tid);
+    const E* S0 = (const E*)a.S0 + at * (DK * DV);
+    Op<E, 1> so[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) so[ks] = load_op<E, 1>(S0 + (w * KS + ks) * 512, lane);      // (of the wave's first columns)
+    {
+        Tile<E, C, DK> k, y;
+        Tile<E, C, DV> v;
+        Tile<E, C, C> m;
+        const Steps s = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, lane);
+        k.fetch((const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid);
+        y.fetch((const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid);
+        v.fetch((const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid);
+        m.fetch((const E*)a.T + at * (C * C), C, 0, C, tid);
+        put_steps(st, s, ch.n, tid);
+        k.put(sK, LK, ch.n, tid);
+        y.put(sQ, LK, ch.n, tid);
+        v.put(sV, LV, ch.n, tid);
+        m.put(sT, LT, C, tid);
+    }
     __syncthreads();
     if (w < NB) {
         const Planes<E, 1> Pm{sP, LT, 0};
@@ -288,11 +247,10 @@ __global__ __launch_bounds__(256) void delta_out_kernel(DeltaArgs a)
         }
     }
     __syncthreads();
-    const E* S0 = (const E*)a.S0 + at * (DK * DV);
+#pragma unroll 1
     for (int eg = w; eg < DV / 16; eg += 4) {
-        Op<E, 1> so[KS], ro[KC], uo[KC];
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) so[ks] = load_op<E, 1>(S0 + (eg * KS + ks) * 512, lane);
+        read_afresh();
+        Op<E, 2> ro[KC], uo[KC];
         f32x4 x[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -306,7 +264,7 @@ __global__ __launch_bounds__(256) void delta_out_kernel(DeltaArgs a)
             }
         }
 #pragma unroll
-        for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 1>(x[2 * ks], x[2 * ks + 1]);
+        for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             x[b] = zero4();
@@ -314,7 +272,7 @@ __global__ __launch_bounds__(256) void delta_out_kernel(DeltaArgs a)
             for (int ks = 0; ks <= b / 2; ++ks) x[b] = mma(rows_op(sT, LT, 16 * b, 32 * ks, lane), ro[ks], x[b]);
         }
 #pragma unroll
-        for (int ks = 0; ks < KC; ++ks) uo[ks] = operand<E, 1>(x[2 * ks], x[2 * ks + 1]);
+        for (int ks = 0; ks < KC; ++ks) uo[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             const int t = 16 * b + c;
@@ -327,6 +285,9 @@ __global__ __launch_bounds__(256) void delta_out_kernel(DeltaArgs a)
             if (t < ch.n)
                 *(Vec4<E>*)((E*)a.O + (size_t)(ch.row + t) * (a.H * DV) + h * DV + 16 * eg + 4 * q) = __builtin_convertvector(o, Vec4<E>);
         }
+        if (eg + 4 < DV / 16)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) so[ks] = load_op<E, 1>(S0 + ((eg + 4) * KS + ks) * 512, lane);
     }
 }
 
@@ -393,17 +354,17 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a)
 // -------------------------------------------------------------------------------------------------------------------- host
 bool delta_dims_ok(int dk, int dv) { return (dk == 64 || dk == 128) && (dv == 64 || dv == 128); }
 
-DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved)
+DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states)
 {
     DeltaPlan p{};
     const size_t es = dtype != 0 ? 4 : 2;
-    p.parts = dtype != 0 ? 1 : 2;
+    p.parts = dtype == 0 && states ? 2 : 1;
     p.chunk = dtype != 0 ? kDeltaChunkF32 : kDeltaChunkBf16;
     const int len = n_seq > 0 ? T / n_seq : 0;
     p.places = T <= 0 || n_seq <= 0 ? 0 : packed ? T / p.chunk + n_seq : n_seq * ((len + p.chunk - 1) / p.chunk);
     const size_t n = (size_t)p.places * H;
     auto room = [](size_t& at, size_t bytes) { const size_t was = at; at += (bytes + 255) & ~(size_t)255; return was; };
-    p.T = room(p.saved_bytes, n * p.parts * p.chunk * p.chunk * es);
+    p.T = room(p.saved_bytes, n * p.chunk * p.chunk * es);
     p.S0 = room(p.saved_bytes, n * dk * dv * es);
     p.whole = room(p.saved_bytes, n * sizeof(float));
     p.N = room(p.bytes, n * p.parts * dk * dk * es);
@@ -414,15 +375,16 @@ DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, 
     return p;
 }
 
-hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int dk, int dv, int dtype, hipStream_t st)
+hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int parts, int dk, int dv, int dtype, hipStream_t st)
 {
     if (a.rows.n_seq == 0) return hipSuccess;
-    const dim3 grid((unsigned)((size_t)a.rows.n_seq * a.H * (dv / 16)));
+    const dim3 grid((unsigned)(((size_t)a.rows.n_seq * a.H * (dv / 16) + 7) / 8 * 8));
 #define CHELA_W(E, DK, P)                                                                                             \
     if (reverse) hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, true>), grid, dim3(256), 0, st, a, dv);              \
     else hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, false>), grid, dim3(256), 0, st, a, dv)
     if (dtype != 0) { if (dk == 64) { CHELA_W(float, 64, 1); } else { CHELA_W(float, 128, 1); } }
-    else { if (dk == 64) { CHELA_W(bf16, 64, 2); } else { CHELA_W(bf16, 128, 2); } }
+    else if (parts == 2) { if (dk == 64) { CHELA_W(bf16, 64, 2); } else { CHELA_W(bf16, 128, 2); } }
+    else { if (dk == 64) { CHELA_W(bf16, 64, 1); } else { CHELA_W(bf16, 128, 1); } }
 #undef CHELA_W
     return hipGetLastError();
 }
@@ -439,13 +401,17 @@ hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, char* ws, char*
     a.whole = (float*)(saved + p.whole);
     if (p.places > 0) {
         const dim3 grid((unsigned)((size_t)p.places * a.H));
-#define CHELA_RUN(E, DK, DV) hipLaunchKernelGGL((delta_prep_kernel<E, DK, DV, sizeof(E) == 2 ? 2 : 1>), grid, dim3(256), 0, st, a)
+#define CHELA_RUN(E, DK, DV)                                                                                          \
+    do {                                                                                                              \
+        if (sizeof(E) == 2 && p.parts == 2) hipLaunchKernelGGL((delta_prep_kernel<E, DK, DV, 3 - sizeof(E) / 2>), grid, dim3(256), 0, st, a); \
+        else hipLaunchKernelGGL((delta_prep_kernel<E, DK, DV, 1>), grid, dim3(256), 0, st, a);                        \
+    } while (0)
         CHELA_DELTA(CHELA_RUN)
 #undef CHELA_RUN
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    return launch_delta_walk(a, false, dk, dv, dtype, st);
+    return launch_delta_walk(a, false, p.parts, dk, dv, dtype, st);
 }
 
 hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st)

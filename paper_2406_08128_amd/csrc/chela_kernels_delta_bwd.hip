@@ -14,11 +14,11 @@
 namespace chela {
 
 template <typename E, int DK, int DV, int P>
-__global__ __launch_bounds__(256) void delta_bwd_prep_kernel(DeltaArgs a)
+__global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
-    constexpr int PT = sizeof(E) == 2 ? 2 : 1;
-    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sO[C * LV], sT[PT * C * LT], sP[PT * C * LT];
+    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sO[C * LV], sT[P * C * LT], sP[P * C * LT];
+    __shared__ __align__(16) float s_inv[P == 2 ? C * (C + 4) + C * 20 : 1];
     __shared__ ChunkSteps<C> st;
     __shared__ __align__(16) float s_qu[C];                        // scale e^gamma
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
@@ -26,13 +26,24 @@ __global__ __launch_bounds__(256) void delta_bwd_prep_kernel(DeltaArgs a)
     const Chunk ch = chunk_at(a.rows, C, place, lane);
     if (ch.n <= 0) return;
     const size_t at = (size_t)place * a.H + h;
-    load_tile<E, C, DK>(sQ, LK, (const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid, 256);
-    load_tile<E, C, DK>(sK, LK, (const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid, 256);
-    load_tile<E, C, DV>(sO, LV, (const E*)a.dO + h * DV, a.lddo, ch.row, ch.n, tid, 256);
-    load_tile<E, PT * C, C>(sT, LT, (const E*)a.T + at * (PT * C * C), C, 0, PT * C, tid, 256);
-    load_steps<E, C>(st, (const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, tid);
+    {
+        Tile<E, C, DK> y, k;
+        Tile<E, C, DV> o;
+        Tile<E, C, C> m;
+        const Steps s = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, lane);
+        y.fetch((const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid);
+        k.fetch((const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid);
+        o.fetch((const E*)a.dO + h * DV, a.lddo, ch.row, ch.n, tid);
+        if (P == 1) m.fetch((const E*)a.T + at * (C * C), C, 0, C, tid);
+        put_steps(st, s, ch.n, tid);
+        y.put(sQ, LK, ch.n, tid);
+        k.put(sK, LK, ch.n, tid);
+        o.put(sO, LV, ch.n, tid);
+        if (P == 1) m.put(sT, LT, C, tid);
+    }
     __syncthreads();
     const Planes<E, P> T{sT, LT, C * LT}, Pt{sP, LT, C * LT};
+    if (P == 2) chunk_inverse<E, DK>(sK, LK, st, s_inv, s_inv + C * (C + 4), T, tid);       // (what was kept of it has one part)
     if (w < NB) {                                                  // P's transpose, sixteen of its rows to a wave
         const int s = 16 * w + c;
         for (int tb = w & ~1; tb < NB; ++tb) {
@@ -51,22 +62,24 @@ __global__ __launch_bounds__(256) void delta_bwd_prep_kernel(DeltaArgs a)
     }
     if (tid < C) s_qu[tid] = a.scale * st.up[tid];
     __syncthreads();
+#pragma unroll 1
     for (int p = w; p < (DK + DV) / 16; p += 4) {
+        read_afresh();
         f32x4 x[NB];
-        Op<E, P> xo[KC];
+        Op<E, 2> xo[KC];
         if (p < DV / 16) {
-            Op<E, P> qo[KC];
+            Op<E, 2> qo[KC];
 #pragma unroll
             for (int b = 0; b < NB; ++b) x[b] = zero4();
 #pragma unroll
             for (int ks = 0; ks < KC; ++ks) {
                 const Op<E, 1> o = cols_op(sO, LV, 32 * ks, 16 * p, lane);
-                qo[ks] = scaled<E, P>(o, s_qu, 32 * ks, lane);
+                qo[ks] = scaled<E, 2>(o, s_qu, 32 * ks, lane);
 #pragma unroll
                 for (int b = 0; b <= 2 * ks + 1; ++b) x[b] = mma(Pt.rows(16 * b, 32 * ks, lane), o, x[b]);
             }
 #pragma unroll
-            for (int ks = 0; ks < KC; ++ks) xo[ks] = operand<E, P>(x[2 * ks], x[2 * ks + 1]);
+            for (int ks = 0; ks < KC; ++ks) xo[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 x[b] = zero4();
@@ -75,7 +88,7 @@ __global__ __launch_bounds__(256) void delta_bwd_prep_kernel(DeltaArgs a)
                 x[b] *= *(const f32x4*)(st.bu + 16 * b + 4 * q);
             }
 #pragma unroll
-            for (int ks = 0; ks < KC; ++ks) xo[ks] = operand<E, P>(x[2 * ks], x[2 * ks + 1]);
+            for (int ks = 0; ks < KC; ++ks) xo[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
 #pragma unroll
             for (int n = 0; n < DK / 16; ++n) {
                 f32x4 z = zero4();
@@ -92,14 +105,14 @@ __global__ __launch_bounds__(256) void delta_bwd_prep_kernel(DeltaArgs a)
             for (int b = 0; b < NB; ++b) x[b] = zero4();
 #pragma unroll
             for (int ks = 0; ks < KC; ++ks) {
-                const Op<E, P> k = scaled<E, P>(cols_op(sK, LK, 32 * ks, 16 * g, lane), st.bu, 32 * ks, lane);
+                const Op<E, 2> k = scaled<E, 2>(cols_op(sK, LK, 32 * ks, 16 * g, lane), st.bu, 32 * ks, lane);
 #pragma unroll
                 for (int b = 2 * ks; b < NB; ++b) x[b] = mma(T.rows(16 * b, 32 * ks, lane), k, x[b]);
             }
 #pragma unroll
             for (int b = 0; b < NB; ++b) x[b] *= *(const f32x4*)(st.down + 16 * b + 4 * q);
 #pragma unroll
-            for (int ks = 0; ks < KC; ++ks) xo[ks] = operand<E, P>(x[2 * ks], x[2 * ks + 1]);
+            for (int ks = 0; ks < KC; ++ks) xo[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
 #pragma unroll
             for (int n = 0; n < KS; ++n) {
                 f32x4 r0 = zero4(), r1 = zero4();
@@ -124,7 +137,7 @@ __device__ __forceinline__ float column_sum(float x)
 }
 // A workgroup has a chunk and a key head, and goes over that one's value heads: the sums of dQ and dK over them stay in registers.
 template <typename E, int DK, int DV>
-__global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a)
+__global__ __launch_bounds__(256, DK + DV == 128 ? 2 : 1) void delta_grad_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, VS = DV / 32, LK = DK + kPad<E>, LV = DV + kPad<E>;
     constexpr int LT = C + kPad<E>, LS = 64 + kPad<E>;
@@ -144,8 +157,9 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a)
     }
     const Chunk ch = chunk_at(a.rows, C, place, lane);
     if (ch.n <= 0) return;
-    load_tile<E, C, DK>(sQ, LK, (const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid, 256);
-    load_tile<E, C, DK>(sK, LK, (const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid, 256);
+    Tile<E, C, DK> ty, tk;
+    ty.fetch((const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid);
+    tk.fetch((const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid);
     const Planes<E, 1> Pm{sP, LT, 0}, Tm{sT, LT, 0}, Um{sU, LV, 0}, Rm{sV, LV, 0};
     f32x4 sumQ[DK / 16], sumK[DK / 16];
 #pragma unroll
@@ -153,11 +167,33 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a)
     for (int hh = 0; hh < share; ++hh) {
         const int h = hk * share + hh;
         const size_t at = (size_t)place * a.H + h;
-        if (hh > 0) __syncthreads();
-        load_tile<E, C, DV>(sV, LV, (const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid, 256);
-        load_tile<E, C, DV>(sO, LV, (const E*)a.dO + h * DV, a.lddo, ch.row, ch.n, tid, 256);
-        load_tile<E, C, C>(sT, LT, (const E*)a.T + at * ((sizeof(E) == 2 ? 2 : 1) * C * C), C, 0, C, tid, 256);
-        load_steps<E, C>(st, (const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, tid);
+        const E *S0 = (const E*)a.S0 + at * (DK * DV), *dS = (const E*)a.dS + at * (DK * DV);
+        Op<E, 1> so[KS], bo[KS];                                       // the states' operands, of the wave's next columns
+        auto next = [&](int eg) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                so[ks] = load_op<E, 1>(S0 + (eg * KS + ks) * 512, lane);
+                bo[ks] = load_op<E, 1>(dS + (eg * KS + ks) * 512, lane);
+            }
+        };
+        {
+            Tile<E, C, DV> v, o;
+            Tile<E, C, C> m;
+            const Steps s = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, lane);
+            v.fetch((const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid);
+            o.fetch((const E*)a.dO + h * DV, a.lddo, ch.row, ch.n, tid);
+            m.fetch((const E*)a.T + at * (C * C), C, 0, C, tid);
+            next(w);
+            if (hh > 0) __syncthreads();
+            put_steps(st, s, ch.n, tid);
+            if (hh == 0) {
+                ty.put(sQ, LK, ch.n, tid);
+                tk.put(sK, LK, ch.n, tid);
+            }
+            v.put(sV, LV, ch.n, tid);
+            o.put(sO, LV, ch.n, tid);
+            m.put(sT, LT, C, tid);
+        }
         __syncthreads();
         if (w < NB) {                                                  // P's transpose
             const int s = 16 * w + c;
@@ -177,18 +213,19 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a)
         }
         __syncthreads();
         // U and dR, sixteen value columns at a time
-        const E *S0 = (const E*)a.S0 + at * (DK * DV), *dS = (const E*)a.dS + at * (DK * DV);
         float db[NB], ss = 0.f;
 #pragma unroll
         for (int b = 0; b < NB; ++b) db[b] = 0.f;
+#pragma unroll 1
         for (int eg = w; eg < DV / 16; eg += 4) {
-            Op<E, 1> so[KS], ro[KC];
+            read_afresh();
+            Op<E, 2> ro[KC];
             f32x4 x[NB], y[NB];
 #pragma unroll
             for (int b = 0; b < NB; ++b) x[b] = y[b] = zero4();
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                const Op<E, 1> s = load_op<E, 1>(S0 + (eg * KS + ks) * 512, lane), d = load_op<E, 1>(dS + (eg * KS + ks) * 512, lane);
+                const Op<E, 1> s = so[ks], d = bo[ks];
                 f32x8 sf, df;
                 if constexpr (sizeof(E) == 4) { sf = s.v; df = d.v; }
                 else { sf = __builtin_convertvector(s.h, f32x8); df = __builtin_convertvector(d.h, f32x8); }
@@ -211,7 +248,9 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a)
                 y[b] *= *(const f32x4*)(st.down + 16 * b + 4 * q);
             }
 #pragma unroll
-            for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 1>(x[2 * ks], x[2 * ks + 1]);
+            for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
+            if (eg + 4 < DV / 16) next(eg + 4);
+            read_afresh();
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 f32x4 u = zero4();
@@ -219,6 +258,7 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a)
                 for (int ks = 0; ks <= b / 2; ++ks) u = mma(ro[ks], Tm.rows(16 * b, 32 * ks, lane), u);
                 Um.put4(16 * b + c, 16 * eg + 4 * q, u);
             }
+            read_afresh();
 #pragma unroll
             for (int ks = 0; ks < KC; ++ks) {
                 const Op<E, 1> o = cols_op(sO, LV, 32 * ks, 16 * eg, lane);
@@ -226,7 +266,8 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a)
                 for (int b = 0; b <= 2 * ks + 1; ++b) y[b] = mma(Pm.rows(16 * b, 32 * ks, lane), o, y[b]);
             }
 #pragma unroll
-            for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 1>(y[2 * ks], y[2 * ks + 1]);
+            for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(y[2 * ks], y[2 * ks + 1]);
+            read_afresh();
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const int t = 16 * b + c;
@@ -248,6 +289,26 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a)
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) ss += __shfl_xor(ss, d);
         if (lane == 0) s_ss[w] = ss;
+        Op<E, 1> s0[DV / 32], s1[DV / 32];                             // S and dS_next, sixty-four of a row's columns, on their way to LDS
+        auto fetch = [&](Op<E, 1>(&to)[DV / 32], const E* from, int half) {
+#pragma unroll
+            for (int i = 0; i < DV / 32; ++i) to[i] = load_op<E, 1>(from + (((w + 4 * i) >> 1) * KS + 2 * half + (w & 1)) * 512, lane);
+        };
+        auto put = [&](const Op<E, 1>(&x)[DV / 32]) {
+#pragma unroll
+            for (int i = 0; i < DV / 32; ++i) {
+                E* to = sS + (16 * ((w + 4 * i) >> 1) + c) * LS + 32 * (w & 1) + 4 * q;
+                if constexpr (sizeof(E) == 4) {
+                    *(f32x4*)to = __builtin_shufflevector(x[i].v, x[i].v, 0, 1, 2, 3);
+                    *(f32x4*)(to + 16) = __builtin_shufflevector(x[i].v, x[i].v, 4, 5, 6, 7);
+                } else {
+                    *(bf16x4*)to = __builtin_shufflevector(x[i].h, x[i].h, 0, 1, 2, 3);
+                    *(bf16x4*)(to + 16) = __builtin_shufflevector(x[i].h, x[i].h, 4, 5, 6, 7);
+                }
+            }
+        };
+        fetch(s0, S0, 0);
+        fetch(s1, dS, 0);
         __syncthreads();
         // X and beta Y, sixteen tokens to a wave
         const int t = 16 * w + c;
@@ -281,26 +342,13 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a)
 #pragma unroll
         for (int half = 0; half < DK / 64; ++half) {
             f32x4 dq[4], rd[4];
-            auto stage = [&](const E* from) {
-                for (int p = w; p < DV / 16 * 2; p += 4) {
-                    const int eg = p >> 1, ks = p & 1;
-                    const Op<E, 1> o = load_op<E, 1>(from + (eg * KS + 2 * half + ks) * 512, lane);
-                    E* to = sS + (16 * eg + c) * LS + 32 * ks + 4 * q;
-                    if constexpr (sizeof(E) == 4) {
-                        *(f32x4*)to = __builtin_shufflevector(o.v, o.v, 0, 1, 2, 3);
-                        *(f32x4*)(to + 16) = __builtin_shufflevector(o.v, o.v, 4, 5, 6, 7);
-                    } else {
-                        *(bf16x4*)to = __builtin_shufflevector(o.h, o.h, 0, 1, 2, 3);
-                        *(bf16x4*)(to + 16) = __builtin_shufflevector(o.h, o.h, 4, 5, 6, 7);
-                    }
-                }
-            };
             if (half > 0) __syncthreads();
-            stage(S0);
+            put(s0);
             __syncthreads();
             if (w < NB) {
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
+                    read_afresh();
                     const int col = 64 * half + 16 * d;
                     f32x4 x = zero4(), y = zero4();
 #pragma unroll
@@ -324,11 +372,16 @@ __global__ __launch_bounds__(256) void delta_grad_kernel(DeltaArgs a)
                 }
             }
             __syncthreads();
-            stage(dS);
+            put(s1);
+            if (half + 1 < DK / 64) {
+                fetch(s0, S0, half + 1);
+                fetch(s1, dS, half + 1);
+            }
             __syncthreads();
             if (w < NB) {
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
+                    read_afresh();
                     const int col = 64 * half + 16 * d;
                     f32x4 x = zero4(), y = zero4();
 #pragma unroll
@@ -403,12 +456,16 @@ hipError_t launch_delta_bwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* sav
     a.dS = ws + p.dS;
     if (p.places > 0) {
         const dim3 grid((unsigned)((size_t)p.places * a.H));
-#define CHELA_RUN(E, DK, DV) hipLaunchKernelGGL((delta_bwd_prep_kernel<E, DK, DV, sizeof(E) == 2 ? 2 : 1>), grid, dim3(256), 0, st, a)
+#define CHELA_RUN(E, DK, DV)                                                                                          \
+    do {                                                                                                              \
+        if (sizeof(E) == 2 && p.parts == 2) hipLaunchKernelGGL((delta_bwd_prep_kernel<E, DK, DV, 3 - sizeof(E) / 2>), grid, dim3(256), 0, st, a); \
+        else hipLaunchKernelGGL((delta_bwd_prep_kernel<E, DK, DV, 1>), grid, dim3(256), 0, st, a);                    \
+    } while (0)
         CHELA_DELTA(CHELA_RUN)
 #undef CHELA_RUN
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    if ((e = launch_delta_walk(a, true, dk, dv, dtype, st)) != hipSuccess) return e;
+    if ((e = launch_delta_walk(a, true, p.parts, dk, dv, dtype, st)) != hipSuccess) return e;
     const bool clear = a.rows.clear && a.rows.cu != nullptr;
     const size_t blocks = (size_t)p.places * a.Hk + (clear ? (a.rows.T + 63) / 64 : 0);
     if (blocks == 0) return hipSuccess;
