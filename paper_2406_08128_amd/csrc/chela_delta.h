@@ -187,6 +187,7 @@ __device__ __forceinline__ int chunks_in(const Rows& r, int C, int s)
     const int n = r.cu == nullptr ? r.L : seq_end(r, s) - seq_begin(r, s);
     return n > 0 ? (n + C - 1) / C : 0;
 }
+// The same holds for runs of several chunks: C is then a run's tokens.
 struct Chunk { int seq, index, row, n; };      // its sequence, which of that one's chunks, its first row, its rows (0: nothing is here)
 // All 64 lanes of a wave together, 64 sequences at a time.
 __device__ __forceinline__ Chunk chunk_at(const Rows& r, int C, int place, int lane)
@@ -223,9 +224,10 @@ __device__ __forceinline__ Chunk chunk_at(const Rows& r, int C, int place, int l
 // too) stands for none of the state being left, which fp32 makes of -104 already.
 template <int C>
 struct ChunkSteps {
-    alignas(16) float hi[C], lo[C], beta[C], up[C], down[C], bu[C];     // up: e^gamma, down: e^(gamma of the last token - gamma), bu: -beta up
+    // (hi + lo: gamma in units of ln 2); up: e^gamma, down: e^(gamma of the last token - gamma), bu: -beta up
+    alignas(16) float hi[C], lo[C], beta[C], up[C], down[C], bu[C];
     float whole;                                                       // e^(gamma of the last token)
-    __device__ __forceinline__ float decay(int t, int s) const { return exp2_(kLog2e * ((hi[t] - hi[s]) + (lo[t] - lo[s]))); }
+    __device__ __forceinline__ float decay(int t, int s) const { return exp2_((hi[t] - hi[s]) + (lo[t] - lo[s])); }
 };
 // Sums over the lanes up to each, by DPP: within rows of 16 lanes, then the rows' totals.
 template <int CTRL, int ROWS>
@@ -245,6 +247,18 @@ __device__ __forceinline__ double running_sum(double x)
     x = plus_dpp<0x142, 0xa>(x);           // lane 15's to the second row, 47's to the fourth
     return plus_dpp<0x143, 0xc>(x);        // lane 31's to the upper two
 }
+// Four rows of a tile in LDS from row0 + 4 q on, of column col0 + c: as an accumulator tile has them.
+template <typename E>
+__device__ __forceinline__ f32x4 tile_of(const E* X, int ld, int row0, int col0, int lane)
+{
+    const int q = lane >> 4, c = lane & 15;
+    if constexpr (sizeof(E) == 2) {
+        return __builtin_convertvector(__builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(X + (row0 + 4 * q + (c >> 2)) * ld + col0 + 4 * (c & 3))), f32x4);
+    } else {
+        const float* p = X + (row0 + 4 * q) * ld + col0 + c;
+        return f32x4{p[0], p[ld], p[2 * ld], p[3 * ld]};
+    }
+}
 // The log decay and beta of this lane's token, on their way; n rows there are, the rest are as if they were not (no decay, beta of zero).
 struct Steps { float g, beta; };
 template <typename E>
@@ -260,19 +274,19 @@ __device__ __forceinline__ void put_steps(ChunkSteps<C>& st, const Steps& x, int
     if (tid < 64) {
         const int t = tid;
         const float b = t < n ? x.beta : 0.f, g = t < n ? (x.g < -256.f ? -256.f : x.g) : 0.f;
-        const double s = running_sum((double)g);
+        const double s = running_sum((double)g) * 1.4426950408889634074;
         typedef __attribute__((ext_vector_type(2))) int i32x2;
         const i32x2 v = __builtin_bit_cast(i32x2, s);
         const double last = __builtin_bit_cast(double, i32x2{__builtin_amdgcn_readlane(v[0], 63), __builtin_amdgcn_readlane(v[1], 63)});
         if (t < C) {
-            const float hi = (float)s, up = exp2_(kLog2e * hi);
+            const float hi = (float)s, up = exp2_(hi);
             st.hi[t] = hi;
             st.lo[t] = (float)(s - (double)hi);
             st.beta[t] = b;
             st.up[t] = up;
             st.bu[t] = -b * up;
-            st.down[t] = exp2_(kLog2e * (float)(last - s));
-            if (t == 0) st.whole = exp2_(kLog2e * (float)last);
+            st.down[t] = exp2_((float)(last - s));
+            if (t == 0) st.whole = exp2_((float)last);
         }
     }
 }
@@ -289,19 +303,18 @@ __device__ __forceinline__ Op<E, P> scaled(const Op<E, 1>& x, const float* f, in
     return operand<E, P>(__builtin_shufflevector(v, v, 0, 1, 2, 3), __builtin_shufflevector(v, v, 4, 5, 6, 7));
 }
 
-// A chunk's rows of one head, C of D elements, from memory to LDS by way of the registers of 256 threads, zeros behind the n there are (the last
+// A chunk's rows of one head, C of D elements, from memory to LDS by way of the registers of NT threads, zeros behind the n there are (the last
 // row again is what is read for them: no load waits for a comparison).  Rows begin on an element: loads of global memory need no more.
-template <typename E, int C, int D>
+template <typename E, int C, int D, int NT = 256>
 struct Tile {
-    static constexpr int W = 16 / sizeof(E), M = C * (D / W) / 256;
-    static_assert(C * (D / W) % 256 == 0, "whole pieces for all threads");
+    static constexpr int W = 16 / sizeof(E), ALL = C * (D / W), M = (ALL + NT - 1) / NT;
     u32x4 x[M];
     __device__ __forceinline__ void fetch(const E* from, long ld, int row, int n, int tid)
     {
         struct __attribute__((packed, aligned(sizeof(E)))) Loose { u32x4 p; };
 #pragma unroll
         for (int m = 0; m < M; ++m) {
-            const int i = m * 256 + tid, t = i / (D / W), k = i % (D / W) * W;
+            const int i = min(m * NT + tid, ALL - 1), t = i / (D / W), k = i % (D / W) * W;
             x[m] = ((const Loose*)(from + (size_t)(row + min(t, n - 1)) * ld + k))->p;
         }
     }
@@ -309,7 +322,8 @@ struct Tile {
     {
 #pragma unroll
         for (int m = 0; m < M; ++m) {
-            const int i = m * 256 + tid, t = i / (D / W), k = i % (D / W) * W;
+            const int i = m * NT + tid, t = i / (D / W), k = i % (D / W) * W;
+            if (ALL % NT != 0 && i >= ALL) break;
             *(u32x4*)(to + t * ldt + k) = t < n ? x[m] : u32x4{0, 0, 0, 0};
         }
     }
@@ -325,7 +339,7 @@ __device__ __forceinline__ void clear_rows(const Rows& r, int block, E* to, int 
     for (int t = 64 * block; t < end; ++t) {
         if (t >= lo && t < hi) continue;
         E* row = to + (size_t)t * width;
-        for (int i = threadIdx.x; i < width; i += 256) row[i] = (E)0.f;
+        for (int i = threadIdx.x; i < width; i += blockDim.x) row[i] = (E)0.f;
     }
 }
 
@@ -335,7 +349,7 @@ template <typename E, int DK, int P, int C>
 __device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSteps<C>& st, float* sA, float* sD, const Planes<E, P>& T, int tid)
 {
     constexpr int NB = C / 16, LA = C + 4, LD = 20;
-    const int lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
+    const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
     // A, sixteen tokens to a wave
     if (w < NB) {
         const int t = 16 * w + c;

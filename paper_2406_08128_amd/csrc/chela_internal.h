@@ -279,9 +279,10 @@ hipError_t launch_block_norm_fwd(const BlockNormArgs& a, int dtype, hipStream_t 
 hipError_t launch_block_norm_bwd(const BlockNormArgs& a, int dtype, hipStream_t st);
 
 // Gated delta rule.  A sequence's rows are cut into chunks (of kDeltaChunkBf16 or kDeltaChunkF32 tokens); `places` is how many there may be,
-// and each has room for what the kernels hand to each other, per head.  states: of a call with states or their gradients, given or wanted.
+// and each has room for what the kernels hand to each other, per head.  states: of a call with states or their gradients, given or wanted.  kept: a
+// gradient is to be had from what each chunk leaves.
 struct DeltaPlan {
-    int chunk, places, parts;             // parts: of the operands that a state goes through (1, or 2 in bf16)
+    int chunk, run, places, parts, t_parts;     // run: chunks that share a place; t_parts: of T; parts: of the operands that a state goes through (1, or 2 in bf16)
     size_t N, Z, bytes;                   // byte offsets into the scratch, and its size
     size_t T, S0, whole, saved_bytes;     // ... into `saved` (without one: this many bytes of the scratch from `saved_at` on)
     size_t saved_at, dS;
@@ -294,13 +295,13 @@ struct DeltaArgs {
     float *S_out, *dS_in;
     void *O, *dQ, *dK, *dV, *dg, *dbeta;
     float scale;
-    int H, Hk, places;
+    int H, Hk, places, run, t_parts;
     void *N, *T, *S0, *dS;                // between the kernels, [places][H] of each
     float *Z, *whole;
 };
 constexpr int kDeltaChunkBf16 = 64, kDeltaChunkF32 = 32;
 bool delta_dims_ok(int dk, int dv);
-DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states);
+DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states, bool kept);
 hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int parts, int dk, int dv, int dtype, hipStream_t st);

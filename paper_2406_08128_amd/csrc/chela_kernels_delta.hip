@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256, 2) void delta_prep_kernel(DeltaArgs a)
     __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[P * C * LT];
     __shared__ __align__(16) float sA[C * (C + 4)], sD[C * 20];
     __shared__ ChunkSteps<C> st;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
     const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
     const Chunk ch = chunk_at(a.rows, C, place, lane);
     if (ch.n <= 0) return;
@@ -102,48 +102,222 @@ __global__ __launch_bounds__(256, 2) void delta_prep_kernel(DeltaArgs a)
     }
 }
 
-// ---- the walk: S <- whole S + Z - N S from chunk to chunk (N comes negated), sixteen of S's columns to a workgroup, a quarter of its rows to
-// a wave.  Each wave keeps its rows in fp32 and hands them to the others as operands, through LDS; what the next chunks need is on its way
-// meanwhile.  REV: from the last chunk to the first, with the states' gradients.
-template <typename E, int DK, int P, bool REV>
-__global__ __launch_bounds__(256) void delta_walk_kernel(DeltaArgs a, int DV)
+// ---- T alone, of all chunks, for runs of them
+template <typename E, int DK, int P>
+__global__ __launch_bounds__(256) void delta_inverse_kernel(DeltaArgs a)
 {
-    constexpr int C = DeltaChunk<E>::C, TW = DK / 64, KS = DK / 32, NE = kOpElems<E, P>, OE = kOpElems<E, 2>;
-    constexpr int AHEAD = (DK == 64 ? 4 : 2);
-    __shared__ __align__(16) E sS[2][KS * OE];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
+    constexpr int C = DeltaChunk<E>::C, LK = DK + kPad<E>, LT = C + kPad<E>, W = 16 / sizeof(E);
+    __shared__ __align__(16) E sK[C * LK], sT[P * C * LT];
+    __shared__ __align__(16) float sA[C * (C + 4)], sD[C * 20];
+    __shared__ ChunkSteps<C> st;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int i = blockIdx.x / a.H, h = blockIdx.x - i * a.H, hk = h / (a.H / a.Hk);
+    const Chunk ch = chunk_at(a.rows, C * a.run, i / a.run, lane);
+    const int row = ch.row + i % a.run * C, n = min(C, ch.n - i % a.run * C);
+    if (n <= 0) return;
+    Tile<E, C, DK> k;
+    const Steps s = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, row, h, n, lane);
+    k.fetch((const E*)a.K + hk * DK, a.ldk, row, n, tid);
+    put_steps(st, s, n, tid);
+    k.put(sK, LK, n, tid);
+    __syncthreads();
+    chunk_inverse<E, DK>(sK, LK, st, sA, sD, Planes<E, P>{sT, LT, C * LT}, tid);
+    E* to = (E*)a.T + ((size_t)i * a.H + h) * (P * C * C);
+#pragma unroll
+    for (int j = tid; j < P * C * (C / W); j += 256) *(u32x4*)(to + j * W) = *(const u32x4*)(sT + j / (C / W) * LT + j % (C / W) * W);
+}
+
+// ---- the same for a run of chunks: one N and one Z for all of them, so that the walk has fewer steps and less to read.  The state behind the
+// run's first chunks is taken through the next as the walk does it, Z beside what is left of the identity (X = M - e^Gamma, M the transition so far,
+// Gamma the sum of all log decays so far), thirty-two columns to a wave:
+//     U = T (beta V) - W Z,   or of X's columns  -e^Gamma W - W X;   X <- e^gamma X + K~^T U,   W = T (beta e^gamma K).
+template <typename E, int DK, int DV, int P>
+__global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs a)
+{
+    constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
+    constexpr int NT = (DK + DV) * 2;
+    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[P * C * LT], sW[(sizeof(E) == 2 ? 2 : 1) * C * LK];
+    __shared__ ChunkSteps<C> st;
+    const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6);
+    const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
+    const Chunk ch = chunk_at(a.rows, C * a.run, place, lane0);
+    if (ch.n <= 0) return;
+    const size_t at = (size_t)place * a.H + h;
+    const bool of_k = w < DK / 32;
+    const int col = 32 * (of_k ? w : w - DK / 32);
+    Tile<E, C, DK, NT> tk;
+    Tile<E, C, DV, NT> tv;
+    Tile<E, P * C, C, NT> tt;
+    Steps ts;
+    auto fetch = [&](int r, int tid, int lane) {
+        const int row = ch.row + r * C, n = min(C, ch.n - r * C);
+        ts = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, row, h, n, lane);
+        tk.fetch((const E*)a.K + hk * DK, a.ldk, row, n, tid);
+        tv.fetch((const E*)a.V + h * DV, a.ldv, row, n, tid);
+        tt.fetch((const E*)a.T + (((size_t)place * a.run + r) * a.H + h) * (P * C * C), C, 0, P * C, tid);
+    };
+    fetch(0, tid0, lane0);
+    const Planes<E, P> T{sT, LT, C * LT};
+    const Planes<E, 2> W{sW, LK, C * LK};
+    f32x4 X[DK / 16][2];
+    float before = 1.f;
+    for (int r = 0; r * C < ch.n; ++r) {
+        const int n = min(C, ch.n - r * C);
+        const bool last = (r + 1) * C >= ch.n;
+        int lane = lane0;
+        asm volatile("" : "+v"(lane));             // (addresses are worked out where they are used: kept over the chunks, they fill the registers)
+        const int tid = 64 * w + lane, q = lane >> 4, c = lane & 15;
+        if (r > 0) __syncthreads();
+        put_steps(st, ts, n, tid);
+        tk.put(sK, LK, n, tid);
+        tv.put(sV, LV, n, tid);
+        tt.put(sT, LT, P * C, tid);
+        if (!last) fetch(r + 1, tid, lane);
+        __syncthreads();
+        const float* f = of_k ? st.bu : st.beta;          // (W and X are kept with their signs changed)
+        f32x4 y[NB][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) y[b][0] = y[b][1] = zero4();
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) {
+            const Op<E, 2> x0 = scaled<E, 2>(cols_op(of_k ? sK : sV, of_k ? LK : LV, 32 * ks, col, lane), f, 32 * ks, lane);
+            const Op<E, 2> x1 = scaled<E, 2>(cols_op(of_k ? sK : sV, of_k ? LK : LV, 32 * ks, col + 16, lane), f, 32 * ks, lane);
+#pragma unroll
+            for (int b = 2 * ks; b < NB; ++b) {
+                const Op<E, P> m = T.rows(16 * b, 32 * ks, lane);
+                y[b][0] = mma(m, x0, y[b][0]);
+                y[b][1] = mma(m, x1, y[b][1]);
+            }
+        }
+        if (r > 0) {
+            if (of_k) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) W.put(16 * b + 4 * q + i, col + 16 * g + c, y[b][g][i]);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                y[b][0] *= splat4(of_k ? before : 1.f);
+                y[b][1] *= splat4(of_k ? before : 1.f);
+            }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                read_afresh();
+                const Op<E, 2> x0 = operand<E, 2>(X[2 * ks][0], X[2 * ks + 1][0]), x1 = operand<E, 2>(X[2 * ks][1], X[2 * ks + 1][1]);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const Op<E, 2> m = W.rows(16 * b, 32 * ks, lane);
+                    y[b][0] = mma(m, x0, y[b][0]);
+                    y[b][1] = mma(m, x1, y[b][1]);
+                }
+            }
+        }
+        Op<E, 2> yo[KC][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const f32x4 d = *(const f32x4*)(st.down + 16 * b + 4 * q);
+            y[b][0] *= d;
+            y[b][1] *= d;
+        }
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) {
+            yo[ks][0] = operand<E, 2>(y[2 * ks][0], y[2 * ks + 1][0]);
+            yo[ks][1] = operand<E, 2>(y[2 * ks][1], y[2 * ks + 1][1]);
+        }
+        const float whole = st.whole;
+#pragma unroll
+        for (int n0 = 0; n0 < DK / 16; n0 += 2) {
+            read_afresh();
+            f32x4 z[2][2];                                 // [row of tiles][columns]
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) z[i][g] = r > 0 ? X[n0 + i][g] * splat4(whole) : zero4();
+            if (last && of_k) {
+                // as N is read, the columns of X down the rows of a tile: its old part by products with the identity
+                const Op<E, 2> x0 = operand<E, 2>(z[0][0], z[1][0]), x1 = operand<E, 2>(z[0][1], z[1][1]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    f32x4 lo = zero4(), hi = zero4();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) lo[j] = 4 * q + j == c ? 1.f : 0.f;
+                    const Op<E, 1> one = i == 0 ? operand<E, 1>(lo, hi) : operand<E, 1>(hi, lo);
+                    f32x4 r0 = mma(x0, one, zero4()), r1 = mma(x1, one, zero4());
+#pragma unroll
+                    for (int ks = 0; ks < KC; ++ks) {
+                        const Op<E, 1> k = cols_op(sK, LK, 32 * ks, 16 * (n0 + i), lane);
+                        r0 = mma(yo[ks][0], k, r0);
+                        r1 = mma(yo[ks][1], k, r1);
+                    }
+                    store_op<E, P>((E*)a.N + (at * (DK / 16 * KS) + (n0 + i) * KS + w) * kOpElems<E, P>, operand<E, P>(r0, r1), lane);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int ks = 0; ks < KC; ++ks) {
+                        const Op<E, 1> k = cols_op(sK, LK, 32 * ks, 16 * (n0 + i), lane);
+                        z[i][0] = mma(k, yo[ks][0], z[i][0]);
+                        z[i][1] = mma(k, yo[ks][1], z[i][1]);
+                    }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        X[n0 + i][g] = z[i][g];
+                        if (last) *(f32x4*)(a.Z + at * (DK * DV) + (size_t)((col / 16 + g) * (DK / 16) + n0 + i) * 256 + 4 * lane) = z[i][g];
+                    }
+            }
+        }
+        before *= whole;
+    }
+    if (tid0 == 0) a.whole[at] = before;
+}
+
+// ---- the walk: S <- whole S + Z - N S from chunk to chunk (N comes negated), 16 G of S's columns to a workgroup, sixteen of its rows to a wave.
+// Each wave keeps its rows in fp32 and hands them to the others as operands, through LDS; what the next chunks need is on its way
+// meanwhile.  REV: from the last chunk to the first, with the states' gradients.
+template <typename E, int DK, int P, int G, bool REV>
+__global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
+{
+    constexpr int C = DeltaChunk<E>::C, KS = DK / 32, NE = kOpElems<E, P>, OE = kOpElems<E, 2>, AHEAD = 4;
+    __shared__ __align__(16) E sS[2][G][KS * OE];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
     // (workgroups go to the eight L2s in turn: those of one head, which read the same N, to one of them)
-    const int groups = DV / 16, all = a.rows.n_seq * a.H * groups, id = (int)(blockIdx.x & 7) * ((all + 7) / 8) + (int)(blockIdx.x >> 3);
+    const int groups = DV / (16 * G), all = a.rows.n_seq * a.H * groups, id = (int)(blockIdx.x & 7) * ((all + 7) / 8) + (int)(blockIdx.x >> 3);
     if (id >= all) return;
-    const int eg = id % groups, h = id / groups % a.H, seq = id / groups / a.H;
-    const int first = chunk_key(a.rows, C, seq), n = min(chunks_in(a.rows, C, seq), a.places - first);
+    const int eg = id % groups * G, h = id / groups % a.H, seq = id / groups / a.H;
+    const int first = chunk_key(a.rows, C * a.run, seq), n = min(chunks_in(a.rows, C * a.run, seq), a.places - first);
     const int slot = slot_of(a.rows, seq);
     const float* from = REV ? a.dS_out : a.S_in;
     float* to = REV ? a.dS_in : a.S_out;
-    E* keep = (E*)(REV ? a.dS : a.S0);
-    f32x4 S[TW];
-    const size_t mine = (((size_t)max(slot, 0) * a.H + h) * DK + 16 * TW * w + 4 * q) * DV + 16 * eg + c;
+    E* keep = (E*)(REV ? a.dS : a.S0) + (size_t)eg * (DK * 16) + (w >> 1) * 512 + 8 * lane + 4 * (w & 1);
+    const float* z = a.Z + (size_t)(eg * (DK / 16) + w) * 256 + 4 * lane;
+    const E* nn = (const E*)a.N + (size_t)w * KS * NE;
+    f32x4 S[G];
+    const size_t mine = (((size_t)max(slot, 0) * a.H + h) * DK + 16 * w + 4 * q) * DV + 16 * eg + c;
 #pragma unroll
-    for (int i = 0; i < TW; ++i) {
-        S[i] = zero4();
+    for (int g = 0; g < G; ++g) {
+        S[g] = zero4();
         if (from != nullptr && slot >= 0)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) S[i][j] = from[mine + (size_t)(16 * i + j) * DV];
+            for (int j = 0; j < 4; ++j) S[g][j] = from[mine + (size_t)j * DV + 16 * g];
     }
-    Op<E, P> N[AHEAD][TW][KS];
-    f32x4 Z[AHEAD][TW];
+    Op<E, P> N[AHEAD][KS];
+    f32x4 Z[AHEAD][G];
     float whole[AHEAD];
     auto load = [&](int u, int k) {
         k = min(k, n - 1);
         const size_t at = (size_t)(first + (REV ? n - 1 - k : k)) * a.H + h;
         whole[u] = a.whole[at];
 #pragma unroll
-        for (int i = 0; i < TW; ++i) {
-            Z[u][i] = *(const f32x4*)(a.Z + at * ((size_t)DK * DV) + (size_t)(eg * (DK / 16) + TW * w + i) * 256 + 4 * lane);
+        for (int ks = 0; ks < KS; ++ks) N[u][ks] = load_op<E, P>(nn + at * (DK / 16 * KS * NE) + ks * NE, lane);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                N[u][i][ks] = load_op<E, P>((const E*)a.N + (at * (DK / 16 * KS) + (TW * w + i) * KS + ks) * NE, lane);
-        }
+        for (int g = 0; g < G; ++g) Z[u][g] = *(const f32x4*)(z + at * ((size_t)DK * DV) + g * (DK * 16));
     };
     if (n > 0) {
 #pragma unroll
@@ -154,114 +328,114 @@ __global__ __launch_bounds__(256) void delta_walk_kernel(DeltaArgs a, int DV)
         for (int u = 0; u < AHEAD; ++u) {
             const int k = k0 + u;
             if (k >= n) break;
-            E* x = sS[u & 1];
-            const size_t at = (size_t)(first + (REV ? n - 1 - k : k)) * a.H + h;
-            E* out = keep + at * ((size_t)DK * DV) + (size_t)eg * (DK * 16);
-            if constexpr (TW == 2) {
-                const Op<E, 2> o = operand<E, 2>(S[0], S[1]);
-                store_op<E, 2>(x + w * OE, o, lane);
-                store_op<E, 1>(out + w * 512, first_part(o), lane);
-            } else {
-                E* half = x + (w >> 1) * OE + 8 * lane + 4 * (w & 1);
-                E* out_half = out + (w >> 1) * 512 + 8 * lane + 4 * (w & 1);
+            E* out = keep + ((size_t)(first + (REV ? n - 1 - k : k)) * a.H + h) * ((size_t)DK * DV);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                // (the wave's rows are one half of an operand's terms)
+                E* half = sS[u & 1][g] + (w >> 1) * OE + 8 * lane + 4 * (w & 1);
                 if constexpr (sizeof(E) == 4) {
-                    *(f32x4*)half = S[0];
-                    *(f32x4*)out_half = S[0];
+                    *(f32x4*)half = S[g];
+                    *(f32x4*)(out + g * (DK * 16)) = S[g];
                 } else {
-                    const bf16x4 hi = __builtin_convertvector(S[0], bf16x4);
+                    const bf16x4 hi = __builtin_convertvector(S[g], bf16x4);
                     *(bf16x4*)half = hi;
-                    *(bf16x4*)out_half = hi;
-                    *(bf16x4*)(half + 512) = __builtin_convertvector(S[0] - __builtin_convertvector(hi, f32x4), bf16x4);
+                    *(bf16x4*)(half + 512) = __builtin_convertvector(S[g] - __builtin_convertvector(hi, f32x4), bf16x4);
+                    *(bf16x4*)(out + g * (DK * 16)) = hi;
                 }
             }
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < TW; ++i) S[i] = S[i] * whole[u] + Z[u][i];
+            for (int g = 0; g < G; ++g) S[g] = S[g] * whole[u] + Z[u][g];
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const Op<E, 2> o = load_op<E, 2>(x + ks * OE, lane);
+            for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int i = 0; i < TW; ++i) S[i] = mma(N[u][i][ks], o, S[i]);
-            }
+                for (int g = 0; g < G; ++g) S[g] = mma(N[u][ks], load_op<E, 2>(sS[u & 1][g] + ks * OE, lane), S[g]);
             load(u, k + AHEAD);
         }
     }
     if (to != nullptr && slot >= 0)
 #pragma unroll
-        for (int i = 0; i < TW; ++i)
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) to[mine + (size_t)(16 * i + j) * DV] = S[i][j];
+            for (int j = 0; j < 4; ++j) to[mine + (size_t)j * DV + 16 * g] = S[g][j];
 }
 
 // ---- the outputs
+// Sixteen value columns to a wave; a run's chunks one after the other, the state from chunk to chunk in the wave's registers.
 template <typename E, int DK, int DV>
-__global__ __launch_bounds__(256, DK + DV == 128 ? 3 : 2) void delta_out_kernel(DeltaArgs a)
+__global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 ? 3 : 2) : 2) void delta_out_kernel(DeltaArgs a)
 {
-    constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
+    constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>, NT = DV * 4;
     __shared__ __align__(16) E sK[C * LK], sQ[C * LK], sV[C * LV], sT[C * LT], sP[C * LT];
     __shared__ ChunkSteps<C> st;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
+    const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6);
     const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
     if (place >= a.places) {
         clear_rows(a.rows, blockIdx.x - a.places * a.H, (E*)a.O, a.H * DV);
         return;
     }
-    const Chunk ch = chunk_at(a.rows, C, place, lane);
+    const Chunk ch = chunk_at(a.rows, C * a.run, place, lane0);
     if (ch.n <= 0) return;
-    const size_t at = (size_t)place * a.H + h;
-    const E* S0 = (const E*)a.S0 + at * (DK * DV);
+    const E* S0 = (const E*)a.S0 + ((size_t)place * a.H + h) * (DK * DV) + (size_t)w * (KS * 512);
+    Tile<E, C, DK, NT> tk, tq;
+    Tile<E, C, DV, NT> tv;
+    Tile<E, C, C, NT> tt;
+    Steps ts;
+    auto fetch = [&](int r, int tid, int lane) {
+        const int row = ch.row + r * C, n = min(C, ch.n - r * C);
+        ts = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, row, h, n, lane);
+        tk.fetch((const E*)a.K + hk * DK, a.ldk, row, n, tid);
+        tq.fetch((const E*)a.Q + hk * DK, a.ldq, row, n, tid);
+        tv.fetch((const E*)a.V + h * DV, a.ldv, row, n, tid);
+        tt.fetch((const E*)a.T + (((size_t)place * a.run + r) * a.H + h) * (a.t_parts * C * C), C, 0, C, tid);
+    };
     Op<E, 1> so[KS];
+    f32x4 S[DK / 16];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) so[ks] = load_op<E, 1>(S0 + (w * KS + ks) * 512, lane);      // (of the wave's first columns)
-    {
-        Tile<E, C, DK> k, y;
-        Tile<E, C, DV> v;
-        Tile<E, C, C> m;
-        const Steps s = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, lane);
-        k.fetch((const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid);
-        y.fetch((const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid);
-        v.fetch((const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid);
-        m.fetch((const E*)a.T + at * (C * C), C, 0, C, tid);
-        put_steps(st, s, ch.n, tid);
-        k.put(sK, LK, ch.n, tid);
-        y.put(sQ, LK, ch.n, tid);
-        v.put(sV, LV, ch.n, tid);
-        m.put(sT, LT, C, tid);
-    }
-    __syncthreads();
-    if (w < NB) {
-        const Planes<E, 1> Pm{sP, LT, 0};
-        const int t = 16 * w + c;
-        for (int sb = 0; sb <= (w | 1); ++sb) {
-            f32x4 x = zero4();
-            if (sb <= w) {
+    for (int ks = 0; ks < KS; ++ks) so[ks] = load_op<E, 1>(S0 + ks * 512, lane0);
+    constexpr bool AHEAD = DV == 64;                       // (with eight waves to a workgroup there are no registers for it)
+    if (AHEAD) fetch(0, tid0, lane0);
+    for (int r = 0; r * C < ch.n; ++r) {
+        const int n = min(C, ch.n - r * C);
+        const bool last = (r + 1) * C >= ch.n;
+        int lane = lane0;
+        asm volatile("" : "+v"(lane));             // (addresses are worked out where they are used: kept over the chunks, they fill the registers)
+        const int tid = 64 * w + lane, q = lane >> 4, c = lane & 15;
+        if (!AHEAD) fetch(r, tid, lane);
+        if (r > 0) __syncthreads();
+        put_steps(st, ts, n, tid);
+        tk.put(sK, LK, n, tid);
+        tq.put(sQ, LK, n, tid);
+        tv.put(sV, LV, n, tid);
+        tt.put(sT, LT, C, tid);
+        if (AHEAD && !last) fetch(r + 1, tid, lane);
+        __syncthreads();
+        if (w < NB) {
+            const Planes<E, 1> Pm{sP, LT, 0};
+            const int t = 16 * w + c;
+            for (int sb = 0; sb <= (w | 1); ++sb) {
+                f32x4 x = zero4();
+                if (sb <= w) {
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sQ, LK, 16 * w, 32 * ks, lane), x);
+                    for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sQ, LK, 16 * w, 32 * ks, lane), x);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int s = 16 * sb + 4 * q + i;
-                    x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
+                    for (int i = 0; i < 4; ++i) {
+                        const int s = 16 * sb + 4 * q + i;
+                        x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
+                    }
                 }
+                Pm.put4(t, 16 * sb + 4 * q, x);
             }
-            Pm.put4(t, 16 * sb + 4 * q, x);
         }
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int eg = w; eg < DV / 16; eg += 4) {
-        read_afresh();
         Op<E, 2> ro[KC], uo[KC];
         f32x4 x[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
+            if (b % 2 == 0) read_afresh();
             x[b] = zero4();
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) x[b] = mma(rows_op(sK, LK, 16 * b, 32 * ks, lane), so[ks], x[b]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = 16 * b + 4 * q + i;
-                x[b][i] = st.beta[t] * fmaf(-st.up[t], x[b][i], to_f(sV[t * LV + 16 * eg + c]));
-            }
+            x[b] = x[b] * *(const f32x4*)(st.bu + 16 * b + 4 * q) + *(const f32x4*)(st.beta + 16 * b + 4 * q) * tile_of(sV, LV, 16 * b, 16 * w, lane);
         }
 #pragma unroll
         for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
@@ -273,8 +447,10 @@ __global__ __launch_bounds__(256, DK + DV == 128 ? 3 : 2) void delta_out_kernel(
         }
 #pragma unroll
         for (int ks = 0; ks < KC; ++ks) uo[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
+        __syncthreads();
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
+            if (b % 2 == 0) read_afresh();
             const int t = 16 * b + c;
             f32x4 o = zero4();
 #pragma unroll
@@ -282,12 +458,35 @@ __global__ __launch_bounds__(256, DK + DV == 128 ? 3 : 2) void delta_out_kernel(
             o *= splat4(a.scale * st.up[t]);
 #pragma unroll
             for (int ks = 0; ks <= b / 2; ++ks) o = mma(uo[ks], rows_op(sP, LT, 16 * b, 32 * ks, lane), o);
-            if (t < ch.n)
-                *(Vec4<E>*)((E*)a.O + (size_t)(ch.row + t) * (a.H * DV) + h * DV + 16 * eg + 4 * q) = __builtin_convertvector(o, Vec4<E>);
+            if (t < n)
+                *(Vec4<E>*)((E*)a.O + (size_t)(ch.row + r * C + t) * (a.H * DV) + h * DV + 16 * w + 4 * q) = __builtin_convertvector(o, Vec4<E>);
         }
-        if (eg + 4 < DV / 16)
+        if (last) break;
+        // the state in front of the next chunk
+        const float whole = st.whole;
+        if (r == 0) {
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) so[ks] = load_op<E, 1>(S0 + ((eg + 4) * KS + ks) * 512, lane);
+            for (int ks = 0; ks < KS; ++ks) {
+                f32x8 v;
+                if constexpr (sizeof(E) == 4) v = so[ks].v;
+                else v = __builtin_convertvector(so[ks].h, f32x8);
+                S[2 * ks] = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+                S[2 * ks + 1] = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) x[b] *= *(const f32x4*)(st.down + 16 * b + 4 * q);
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) uo[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
+#pragma unroll
+        for (int d = 0; d < DK / 16; ++d) {
+            if (d % 4 == 0) read_afresh();
+            S[d] *= splat4(whole);
+#pragma unroll
+            for (int ks = 0; ks < KC; ++ks) S[d] = mma(cols_op(sK, LK, 32 * ks, 16 * d, lane), uo[ks], S[d]);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) so[ks] = operand<E, 1>(S[2 * ks], S[2 * ks + 1]);
     }
 }
 
@@ -354,17 +553,31 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a)
 // -------------------------------------------------------------------------------------------------------------------- host
 bool delta_dims_ok(int dk, int dv) { return (dk == 64 || dk == 128) && (dv == 64 || dv == 128); }
 
-DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states)
+// Chunks to a run, a power of two, where nothing is kept of each for a gradient.  A run's chunks are one after the other in a workgroup, the runs of
+// a sequence in the walk: R c + n w / R for n chunks, c and w the times that a chunk takes of either, is least where R^2 = n w / c.  w / c is about
+// 1/16 with heads of 64, 1/8 where there are heads of 128 (0.5 us of 8, 1.3 of 12).  Measured (us; R = 1, 2, 4, 8, 16), bf16, 12 heads of 64, one
+// sequence of 2048 tokens 41 44 57 89 157, of 8192 102 92 90 108 173, of 32768 328 275 235 220 255; 8 of 1024 60 69 76 99 163; 16 heads of
+// 128, 2048 tokens 78 74 93 149 269, 8192 355 254 205 207 312, 65536 2475 2057 1621 1401 1299.
+static int chunks_to_a_run(long n, int dk, int dv)
+{
+    int r = 1;
+    while (r < 16 && (long)r * r * (dk + dv > 128 ? 8 : 16) < n) r *= 2;
+    return r;
+}
+DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states, bool kept)
 {
     DeltaPlan p{};
     const size_t es = dtype != 0 ? 4 : 2;
     p.parts = dtype == 0 && states ? 2 : 1;
     p.chunk = dtype != 0 ? kDeltaChunkF32 : kDeltaChunkBf16;
     const int len = n_seq > 0 ? T / n_seq : 0;
-    p.places = T <= 0 || n_seq <= 0 ? 0 : packed ? T / p.chunk + n_seq : n_seq * ((len + p.chunk - 1) / p.chunk);
+    auto places = [&](int tokens) { return T <= 0 || n_seq <= 0 ? 0 : packed ? T / tokens + n_seq : n_seq * ((len + tokens - 1) / tokens); };
+    p.run = kept ? 1 : chunks_to_a_run(((long)len + p.chunk - 1) / p.chunk, dk, dv);
+    p.places = places(p.chunk * p.run);
     const size_t n = (size_t)p.places * H;
     auto room = [](size_t& at, size_t bytes) { const size_t was = at; at += (bytes + 255) & ~(size_t)255; return was; };
-    p.T = room(p.saved_bytes, n * p.chunk * p.chunk * es);
+    p.t_parts = p.run > 1 ? p.parts : 1;
+    p.T = room(p.saved_bytes, n * p.run * p.t_parts * p.chunk * p.chunk * es);
     p.S0 = room(p.saved_bytes, n * dk * dv * es);
     p.whole = room(p.saved_bytes, n * sizeof(float));
     p.N = room(p.bytes, n * p.parts * dk * dk * es);
@@ -378,10 +591,11 @@ DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, 
 hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int parts, int dk, int dv, int dtype, hipStream_t st)
 {
     if (a.rows.n_seq == 0) return hipSuccess;
-    const dim3 grid((unsigned)(((size_t)a.rows.n_seq * a.H * (dv / 16) + 7) / 8 * 8));
+    const int G = 1;
+    const dim3 grid((unsigned)(((size_t)a.rows.n_seq * a.H * (dv / (16 * G)) + 7) / 8 * 8));
 #define CHELA_W(E, DK, P)                                                                                             \
-    if (reverse) hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, true>), grid, dim3(256), 0, st, a, dv);              \
-    else hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, false>), grid, dim3(256), 0, st, a, dv)
+    if (reverse) hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, 1, true>), grid, dim3(DK * 4), 0, st, a, dv);        \
+    else hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, 1, false>), grid, dim3(DK * 4), 0, st, a, dv)
     if (dtype != 0) { if (dk == 64) { CHELA_W(float, 64, 1); } else { CHELA_W(float, 128, 1); } }
     else if (parts == 2) { if (dk == 64) { CHELA_W(bf16, 64, 2); } else { CHELA_W(bf16, 128, 2); } }
     else { if (dk == 64) { CHELA_W(bf16, 64, 1); } else { CHELA_W(bf16, 128, 1); } }
@@ -394,6 +608,8 @@ hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, char* ws, char*
 {
     if (saved == nullptr) saved = ws + p.saved_at;
     a.places = p.places;
+    a.run = p.run;
+    a.t_parts = p.t_parts;
     a.N = ws + p.N;
     a.Z = (float*)(ws + p.Z);
     a.T = saved + p.T;
@@ -403,8 +619,17 @@ hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, char* ws, char*
         const dim3 grid((unsigned)((size_t)p.places * a.H));
 #define CHELA_RUN(E, DK, DV)                                                                                          \
     do {                                                                                                              \
-        if (sizeof(E) == 2 && p.parts == 2) hipLaunchKernelGGL((delta_prep_kernel<E, DK, DV, 3 - sizeof(E) / 2>), grid, dim3(256), 0, st, a); \
-        else hipLaunchKernelGGL((delta_prep_kernel<E, DK, DV, 1>), grid, dim3(256), 0, st, a);                        \
+        constexpr int P2 = sizeof(E) == 2 ? 2 : 1;                                                                    \
+        if (p.run > 1) {                                                                                              \
+            const dim3 chunks((unsigned)((size_t)p.places * p.run * a.H));                                            \
+            if (p.parts == 2) hipLaunchKernelGGL((delta_inverse_kernel<E, DK, P2>), chunks, dim3(256), 0, st, a);     \
+            else hipLaunchKernelGGL((delta_inverse_kernel<E, DK, 1>), chunks, dim3(256), 0, st, a);                   \
+            if (p.parts == 2) hipLaunchKernelGGL((delta_prep_run_kernel<E, DK, DV, P2>), grid, dim3((DK + DV) * 2), 0, st, a); \
+            else hipLaunchKernelGGL((delta_prep_run_kernel<E, DK, DV, 1>), grid, dim3((DK + DV) * 2), 0, st, a);       \
+        } else {                                                                                                      \
+            if (p.parts == 2) hipLaunchKernelGGL((delta_prep_kernel<E, DK, DV, P2>), grid, dim3(256), 0, st, a);      \
+            else hipLaunchKernelGGL((delta_prep_kernel<E, DK, DV, 1>), grid, dim3(256), 0, st, a);                    \
+        }                                                                                                             \
     } while (0)
         CHELA_DELTA(CHELA_RUN)
 #undef CHELA_RUN
@@ -423,7 +648,7 @@ hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* sav
     const size_t blocks = (size_t)p.places * a.H + (clear ? (a.rows.T + 63) / 64 : 0);
     if (blocks == 0) return hipSuccess;
     const dim3 grid((unsigned)blocks);
-#define CHELA_RUN(E, DK, DV) hipLaunchKernelGGL((delta_out_kernel<E, DK, DV>), grid, dim3(256), 0, st, a)
+#define CHELA_RUN(E, DK, DV) hipLaunchKernelGGL((delta_out_kernel<E, DK, DV>), grid, dim3(DV * 4), 0, st, a)
     CHELA_DELTA(CHELA_RUN)
 #undef CHELA_RUN
     return hipGetLastError();

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
     __shared__ __align__(16) float s_inv[P == 2 ? C * (C + 4) + C * 20 : 1];
     __shared__ ChunkSteps<C> st;
     __shared__ __align__(16) float s_qu[C];                        // scale e^gamma
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
     const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
     const Chunk ch = chunk_at(a.rows, C, place, lane);
     if (ch.n <= 0) return;
@@ -135,16 +135,21 @@ __device__ __forceinline__ float column_sum(float x)
     x += __shfl_xor(x, 16);
     return x + __shfl_xor(x, 32);
 }
-// A workgroup has a chunk and a key head, and goes over that one's value heads: the sums of dQ and dK over them stay in registers.
+// A workgroup has a chunk and a key head, and goes over that one's value heads: the sums of dQ and dK over them stay in registers.  Sixteen value
+// columns to a wave for U and dR; then sixteen tokens, as queries and as keys, and a part of the key columns.  X and Y are worked out twice, by the wave
+// of the query's tokens and by that of the key's: as the operands of its own products they then lie in a wave's registers as they are.
 template <typename E, int DK, int DV>
-__global__ __launch_bounds__(256, DK + DV == 128 ? 2 : 1) void delta_grad_kernel(DeltaArgs a)
+__global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, VS = DV / 32, LK = DK + kPad<E>, LV = DV + kPad<E>;
-    constexpr int LT = C + kPad<E>, LS = 64 + kPad<E>;
-    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sV[C * LV], sO[C * LV], sU[C * LV], sT[C * LT], sP[C * LT], sS[DV * LS];
+    // (rows of S without padding where 160 KB are too few otherwise)
+    constexpr int LT = C + kPad<E>, LS = 64 + (sizeof(E) == 4 && DK + DV == 256 ? 0 : kPad<E>), NW = DV / 16, NT = DV * 4, GI = NW / NB, DT = 4 / GI;      // (DT: tiles of 64 key columns to a wave)
+    constexpr bool SHARED = DV * LS <= C * LT;                  // (the states' operands fit where P and T were)
+    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sV[C * LV], sO[C * LV], sU[C * LV], sT[C * LT], sP[C * LT], sS[SHARED ? 8 : 2 * DV * LS];
     __shared__ ChunkSteps<C> st;
-    __shared__ float s_db[4][C], s_dg[C], s_kc[4], s_ss[4];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, c = lane & 15;
+    __shared__ float s_db[NW][C], s_db2[GI][C], s_dg[GI][C], s_kc[NW], s_ss[NW];
+    E *const sS0 = SHARED ? sP : sS, *const sdS = SHARED ? sT : sS + DV * LS;
+    const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6), tw = w % NB, gi = w / NB;
     const int place = blockIdx.x / a.Hk, hk = blockIdx.x - place * a.Hk, share = a.H / a.Hk;
     if (place >= a.places) {
         const int b = blockIdx.x - a.places * a.Hk;
@@ -155,285 +160,299 @@ __global__ __launch_bounds__(256, DK + DV == 128 ? 2 : 1) void delta_grad_kernel
         clear_rows(a.rows, b, (E*)a.dbeta, a.H);
         return;
     }
-    const Chunk ch = chunk_at(a.rows, C, place, lane);
+    const Chunk ch = chunk_at(a.rows, C, place, lane0);
     if (ch.n <= 0) return;
-    Tile<E, C, DK> ty, tk;
-    ty.fetch((const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid);
-    tk.fetch((const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid);
-    const Planes<E, 1> Pm{sP, LT, 0}, Tm{sT, LT, 0}, Um{sU, LV, 0}, Rm{sV, LV, 0};
-    f32x4 sumQ[DK / 16], sumK[DK / 16];
+    constexpr bool AHEAD = DV == 128;                           // (two workgroups to a compute unit have no registers for the next head)
+    Tile<E, C, DV, NT> tv, to;
+    Tile<E, C, C, NT> tt;
+    Steps ts;
+    Op<E, 1> so[KS], bo[KS];                                    // the states' operands, of the wave's value columns
+    auto fetch = [&](int h, int tid, int lane) {
+        const size_t at = (size_t)place * a.H + h;
+        ts = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, lane);
+        tv.fetch((const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid);
+        to.fetch((const E*)a.dO + h * DV, a.lddo, ch.row, ch.n, tid);
+        tt.fetch((const E*)a.T + at * (C * C), C, 0, C, tid);
 #pragma unroll
-    for (int d = 0; d < DK / 16; ++d) sumQ[d] = sumK[d] = zero4();
+        for (int ks = 0; ks < KS; ++ks) {
+            so[ks] = load_op<E, 1>((const E*)a.S0 + at * (DK * DV) + (w * KS + ks) * 512, lane);
+            bo[ks] = load_op<E, 1>((const E*)a.dS + at * (DK * DV) + (w * KS + ks) * 512, lane);
+        }
+    };
+    {
+        Tile<E, C, DK, NT> ty, tk;
+        ty.fetch((const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid0);
+        tk.fetch((const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid0);
+        if (AHEAD) fetch(hk * share, tid0, lane0);
+        ty.put(sQ, LK, ch.n, tid0);
+        tk.put(sK, LK, ch.n, tid0);
+    }
+    const Planes<E, 1> Pm{sP, LT, 0}, Tm{sT, LT, 0}, Um{sU, LV, 0}, Rm{sV, LV, 0};
+    f32x4 sumQ[DK / 64 * DT], sumK[DK / 64 * DT];
+#pragma unroll
+    for (int d = 0; d < DK / 64 * DT; ++d) sumQ[d] = sumK[d] = zero4();
     for (int hh = 0; hh < share; ++hh) {
         const int h = hk * share + hh;
-        const size_t at = (size_t)place * a.H + h;
-        const E *S0 = (const E*)a.S0 + at * (DK * DV), *dS = (const E*)a.dS + at * (DK * DV);
-        Op<E, 1> so[KS], bo[KS];                                       // the states' operands, of the wave's next columns
-        auto next = [&](int eg) {
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                so[ks] = load_op<E, 1>(S0 + (eg * KS + ks) * 512, lane);
-                bo[ks] = load_op<E, 1>(dS + (eg * KS + ks) * 512, lane);
-            }
-        };
-        {
-            Tile<E, C, DV> v, o;
-            Tile<E, C, C> m;
-            const Steps s = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, lane);
-            v.fetch((const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid);
-            o.fetch((const E*)a.dO + h * DV, a.lddo, ch.row, ch.n, tid);
-            m.fetch((const E*)a.T + at * (C * C), C, 0, C, tid);
-            next(w);
-            if (hh > 0) __syncthreads();
-            put_steps(st, s, ch.n, tid);
-            if (hh == 0) {
-                ty.put(sQ, LK, ch.n, tid);
-                tk.put(sK, LK, ch.n, tid);
-            }
-            v.put(sV, LV, ch.n, tid);
-            o.put(sO, LV, ch.n, tid);
-            m.put(sT, LT, C, tid);
-        }
+        int lane = lane0;
+        asm volatile("" : "+v"(lane));             // (addresses are worked out where they are used: kept over the heads, they fill the registers)
+        const int tid = 64 * w + lane, q = lane >> 4, c = lane & 15, t = 16 * tw + c;
+        if (!AHEAD) fetch(h, tid, lane);
+        if (hh > 0) __syncthreads();
+        put_steps(st, ts, ch.n, tid);
+        tv.put(sV, LV, ch.n, tid);
+        to.put(sO, LV, ch.n, tid);
+        tt.put(sT, LT, C, tid);
         __syncthreads();
-        if (w < NB) {                                                  // P's transpose
-            const int s = 16 * w + c;
-            for (int tb = w & ~1; tb < NB; ++tb) {
-                f32x4 x = zero4();
-                if (tb >= w) {
+        // P's transpose, sixteen of its rows to a wave
+        for (int tb = (tw & ~1) + gi; tb < NB; tb += GI) {
+            f32x4 x = zero4();
+            if (tb >= tw) {
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sQ, LK, 16 * tb, 32 * ks, lane), rows_op(sK, LK, 16 * w, 32 * ks, lane), x);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int t = 16 * tb + 4 * q + i;
-                        x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
-                    }
-                }
-                Pm.put4(s, 16 * tb + 4 * q, x);
-            }
-        }
-        __syncthreads();
-        // U and dR, sixteen value columns at a time
-        float db[NB], ss = 0.f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) db[b] = 0.f;
-#pragma unroll 1
-        for (int eg = w; eg < DV / 16; eg += 4) {
-            read_afresh();
-            Op<E, 2> ro[KC];
-            f32x4 x[NB], y[NB];
-#pragma unroll
-            for (int b = 0; b < NB; ++b) x[b] = y[b] = zero4();
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const Op<E, 1> s = so[ks], d = bo[ks];
-                f32x8 sf, df;
-                if constexpr (sizeof(E) == 4) { sf = s.v; df = d.v; }
-                else { sf = __builtin_convertvector(s.h, f32x8); df = __builtin_convertvector(d.h, f32x8); }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) ss = fmaf(sf[j], df[j], ss);
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const Op<E, 1> k = rows_op(sK, LK, 16 * b, 32 * ks, lane);
-                    x[b] = mma(k, s, x[b]);
-                    y[b] = mma(k, d, y[b]);
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
+                for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sQ, LK, 16 * tb, 32 * ks, lane), rows_op(sK, LK, 16 * tw, 32 * ks, lane), x);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int t = 16 * b + 4 * q + i;
-                    x[b][i] = st.beta[t] * fmaf(-st.up[t], x[b][i], to_f(sV[t * LV + 16 * eg + c]));
+                    const int u = 16 * tb + 4 * q + i;
+                    x[i] = t <= u ? a.scale * st.decay(u, t) * x[i] : 0.f;
                 }
-                y[b] *= *(const f32x4*)(st.down + 16 * b + 4 * q);
             }
+            Pm.put4(t, 16 * tb + 4 * q, x);
+        }
+        // U and dR, sixteen value columns to a wave
+        float ss = 0.f;
+        f32x4 x[NB], y[NB];
 #pragma unroll
-            for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
-            if (eg + 4 < DV / 16) next(eg + 4);
-            read_afresh();
+        for (int b = 0; b < NB; ++b) x[b] = y[b] = zero4();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            f32x8 sf, df;
+            if constexpr (sizeof(E) == 4) { sf = so[ks].v; df = bo[ks].v; }
+            else { sf = __builtin_convertvector(so[ks].h, f32x8); df = __builtin_convertvector(bo[ks].h, f32x8); }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) ss = fmaf(sf[j], df[j], ss);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                f32x4 u = zero4();
-#pragma unroll
-                for (int ks = 0; ks <= b / 2; ++ks) u = mma(ro[ks], Tm.rows(16 * b, 32 * ks, lane), u);
-                Um.put4(16 * b + c, 16 * eg + 4 * q, u);
-            }
-            read_afresh();
-#pragma unroll
-            for (int ks = 0; ks < KC; ++ks) {
-                const Op<E, 1> o = cols_op(sO, LV, 32 * ks, 16 * eg, lane);
-#pragma unroll
-                for (int b = 0; b <= 2 * ks + 1; ++b) y[b] = mma(Pm.rows(16 * b, 32 * ks, lane), o, y[b]);
-            }
-#pragma unroll
-            for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(y[2 * ks], y[2 * ks + 1]);
-            read_afresh();
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const int t = 16 * b + c;
-                f32x4 r = zero4();
-#pragma unroll
-                for (int ks = b / 2; ks < KC; ++ks) r = mma(ro[ks], Tm.cols(32 * ks, 16 * b, lane), r);
-                db[b] += dot4(r, wide4(sV + t * LV + 16 * eg + 4 * q));
-                Rm.put4(t, 16 * eg + 4 * q, r);                       // (dR where the value was: no other lane reads that one)
-                if (t < ch.n)
-                    *(Vec4<E>*)((E*)a.dV + (size_t)(ch.row + t) * (a.H * DV) + h * DV + 16 * eg + 4 * q) =
-                        __builtin_convertvector(r * splat4(st.beta[t]), Vec4<E>);
+                const Op<E, 1> k = rows_op(sK, LK, 16 * b, 32 * ks, lane);
+                x[b] = mma(k, so[ks], x[b]);
+                y[b] = mma(k, bo[ks], y[b]);
             }
         }
+        Op<E, 2> ro[KC];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const float x = column_sum(db[b]);
-            if (q == 0) s_db[w][16 * b + c] = x;
+            x[b] = x[b] * *(const f32x4*)(st.bu + 16 * b + 4 * q) + *(const f32x4*)(st.beta + 16 * b + 4 * q) * tile_of(sV, LV, 16 * b, 16 * w, lane);
+            y[b] *= *(const f32x4*)(st.down + 16 * b + 4 * q);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            f32x4 u = zero4();
+#pragma unroll
+            for (int ks = 0; ks <= b / 2; ++ks) u = mma(ro[ks], Tm.rows(16 * b, 32 * ks, lane), u);
+            Um.put4(16 * b + c, 16 * w + 4 * q, u);
         }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) ss += __shfl_xor(ss, d);
         if (lane == 0) s_ss[w] = ss;
-        Op<E, 1> s0[DV / 32], s1[DV / 32];                             // S and dS_next, sixty-four of a row's columns, on their way to LDS
-        auto fetch = [&](Op<E, 1>(&to)[DV / 32], const E* from, int half) {
+        __syncthreads();                                               // (P is there)
 #pragma unroll
-            for (int i = 0; i < DV / 32; ++i) to[i] = load_op<E, 1>(from + (((w + 4 * i) >> 1) * KS + 2 * half + (w & 1)) * 512, lane);
-        };
-        auto put = [&](const Op<E, 1>(&x)[DV / 32]) {
+        for (int ks = 0; ks < KC; ++ks) {
+            const Op<E, 1> o = cols_op(sO, LV, 32 * ks, 16 * w, lane);
 #pragma unroll
-            for (int i = 0; i < DV / 32; ++i) {
-                E* to = sS + (16 * ((w + 4 * i) >> 1) + c) * LS + 32 * (w & 1) + 4 * q;
+            for (int b = 0; b <= 2 * ks + 1; ++b) y[b] = mma(Pm.rows(16 * b, 32 * ks, lane), o, y[b]);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(y[2 * ks], y[2 * ks + 1]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int r0 = 16 * b + c;
+            f32x4 r = zero4();
+#pragma unroll
+            for (int ks = b / 2; ks < KC; ++ks) r = mma(ro[ks], Tm.cols(32 * ks, 16 * b, lane), r);
+            const float db = column_sum(dot4(r, wide4(sV + r0 * LV + 16 * w + 4 * q)));
+            if (q == 0) s_db[w][r0] = db;
+            Rm.put4(r0, 16 * w + 4 * q, r);                            // (dR where the value was: no other lane reads that one)
+            if (r0 < ch.n)
+                *(Vec4<E>*)((E*)a.dV + (size_t)(ch.row + r0) * (a.H * DV) + h * DV + 16 * w + 4 * q) =
+                    __builtin_convertvector(r * splat4(st.beta[r0]), Vec4<E>);
+        }
+        __syncthreads();
+        // S and dS_next so that their rows are summed over, sixty-four columns of them; what the next head needs is on its way
+        auto put = [&](int half) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int at = (16 * w + c) * LS + 32 * i + 4 * q;
                 if constexpr (sizeof(E) == 4) {
-                    *(f32x4*)to = __builtin_shufflevector(x[i].v, x[i].v, 0, 1, 2, 3);
-                    *(f32x4*)(to + 16) = __builtin_shufflevector(x[i].v, x[i].v, 4, 5, 6, 7);
+                    const f32x8 s = so[2 * half + i].v, b = bo[2 * half + i].v;
+                    *(f32x4*)(sS0 + at) = __builtin_shufflevector(s, s, 0, 1, 2, 3);
+                    *(f32x4*)(sS0 + at + 16) = __builtin_shufflevector(s, s, 4, 5, 6, 7);
+                    *(f32x4*)(sdS + at) = __builtin_shufflevector(b, b, 0, 1, 2, 3);
+                    *(f32x4*)(sdS + at + 16) = __builtin_shufflevector(b, b, 4, 5, 6, 7);
                 } else {
-                    *(bf16x4*)to = __builtin_shufflevector(x[i].h, x[i].h, 0, 1, 2, 3);
-                    *(bf16x4*)(to + 16) = __builtin_shufflevector(x[i].h, x[i].h, 4, 5, 6, 7);
+                    const bf16x8 s = so[2 * half + i].h, b = bo[2 * half + i].h;
+                    *(bf16x4*)(sS0 + at) = __builtin_shufflevector(s, s, 0, 1, 2, 3);
+                    *(bf16x4*)(sS0 + at + 16) = __builtin_shufflevector(s, s, 4, 5, 6, 7);
+                    *(bf16x4*)(sdS + at) = __builtin_shufflevector(b, b, 0, 1, 2, 3);
+                    *(bf16x4*)(sdS + at + 16) = __builtin_shufflevector(b, b, 4, 5, 6, 7);
                 }
             }
         };
-        fetch(s0, S0, 0);
-        fetch(s1, dS, 0);
-        __syncthreads();
-        // X and beta Y, sixteen tokens to a wave
-        const int t = 16 * w + c;
+        put(0);
+        if (AHEAD && DK == 64 && hh + 1 < share) fetch(h + 1, tid, lane);
+        // X and beta Y of the wave's tokens as queries, then as keys
         float dbeta = 0.f, dgamma = 0.f, kc = 0.f;
-        if (w < NB) {
-            for (int sb = 0; sb <= (w | 1); ++sb) {
-                f32x4 x = zero4(), y = zero4(), g = zero4();
-                if (sb <= w) {
+        Op<E, 1> xq[KC], yq[KC], xk[KC], yk[KC];
+        {
+            Op<E, 1> o[VS], r[VS], u[VS];
+#pragma unroll
+            for (int ks = 0; ks < VS; ++ks) {
+                o[ks] = rows_op(sO, LV, 16 * tw, 32 * ks, lane);
+                r[ks] = rows_op(sV, LV, 16 * tw, 32 * ks, lane);
+                u[ks] = rows_op(sU, LV, 16 * tw, 32 * ks, lane);
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                x[b] = y[b] = zero4();
+                read_afresh();
+                if (b <= tw) {                                         // keys b
+                    f32x4 g = zero4();
 #pragma unroll
                     for (int ks = 0; ks < VS; ++ks) {
-                        const Op<E, 1> u = rows_op(sU, LV, 16 * sb, 32 * ks, lane);
-                        x = mma(u, rows_op(sO, LV, 16 * w, 32 * ks, lane), x);
-                        y = mma(u, rows_op(sV, LV, 16 * w, 32 * ks, lane), y);
+                        const Op<E, 1> m = rows_op(sU, LV, 16 * b, 32 * ks, lane);
+                        x[b] = mma(m, o[ks], x[b]);
+                        y[b] = mma(m, r[ks], y[b]);
                     }
+                    if (gi == 0)
 #pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) g = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sK, LK, 16 * w, 32 * ks, lane), g);
+                        for (int ks = 0; ks < KS; ++ks) g = mma(rows_op(sK, LK, 16 * b, 32 * ks, lane), rows_op(sK, LK, 16 * tw, 32 * ks, lane), g);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int s = 16 * sb + 4 * q + i;
+                        const int s = 16 * b + 4 * q + i;
                         const float d = s <= t ? st.decay(t, s) : 0.f;
-                        x[i] = s <= t ? a.scale * d * x[i] : 0.f;
-                        y[i] = s < t ? d * y[i] : 0.f;
-                        dbeta = s < t ? fmaf(-y[i], g[i], dbeta) : dbeta;
+                        x[b][i] = s <= t ? a.scale * d * x[b][i] : 0.f;
+                        y[b][i] = s < t ? d * y[b][i] : 0.f;
+                        dbeta = gi == 0 && s < t ? fmaf(-y[b][i], g[i], dbeta) : dbeta;
                     }
+                    y[b] *= splat4(st.beta[t]);
                 }
-                Pm.put4(t, 16 * sb + 4 * q, x);
-                Tm.put4(t, 16 * sb + 4 * q, y * splat4(st.beta[t]));
             }
-        }
-        // the gradients of queries and keys, sixty-four columns at a time
 #pragma unroll
-        for (int half = 0; half < DK / 64; ++half) {
-            f32x4 dq[4], rd[4];
-            if (half > 0) __syncthreads();
-            put(s0);
-            __syncthreads();
-            if (w < NB) {
+            for (int ks = 0; ks < KC; ++ks) {
+                xq[ks] = operand<E, 1>(x[2 * ks], x[2 * ks + 1]);
+                yq[ks] = operand<E, 1>(y[2 * ks], y[2 * ks + 1]);
+            }
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    read_afresh();
-                    const int col = 64 * half + 16 * d;
-                    f32x4 x = zero4(), y = zero4();
+            for (int b = 0; b < NB; ++b) {
+                x[b] = y[b] = zero4();
+                read_afresh();
+                if (b >= tw) {                                         // queries b
 #pragma unroll
                     for (int ks = 0; ks < VS; ++ks) {
-                        const Op<E, 1> s = cols_op(sS, LS, 32 * ks, 16 * d, lane);
-                        x = mma(s, rows_op(sO, LV, 16 * w, 32 * ks, lane), x);
-                        y = mma(s, rows_op(sV, LV, 16 * w, 32 * ks, lane), y);
+                        x[b] = mma(rows_op(sO, LV, 16 * b, 32 * ks, lane), u[ks], x[b]);
+                        y[b] = mma(rows_op(sV, LV, 16 * b, 32 * ks, lane), u[ks], y[b]);
                     }
-                    x *= splat4(a.scale * st.up[t]);
-                    y *= splat4(st.up[t]);
-                    dbeta -= dot4(y, wide4(sK + t * LK + col + 4 * q));
-                    y *= splat4(st.beta[t]);
-                    for (int ks = 0; ks <= w / 2; ++ks) {
-                        const Op<E, 1> k = cols_op(sK, LK, 32 * ks, col, lane);
-                        x = mma(k, Pm.rows(16 * w, 32 * ks, lane), x);
-                        y = mma(k, Tm.rows(16 * w, 32 * ks, lane), y);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int s = 16 * b + 4 * q + i;
+                        const float d = t <= s ? st.decay(s, t) : 0.f;
+                        x[b][i] = t <= s ? a.scale * d * x[b][i] : 0.f;
+                        y[b][i] = t < s ? d * y[b][i] : 0.f;
                     }
-                    dgamma += dot4(x, wide4(sQ + t * LK + col + 4 * q)) - dot4(y, wide4(sK + t * LK + col + 4 * q));
-                    dq[d] = x;
-                    rd[d] = y;
+                    y[b] *= *(const f32x4*)(st.beta + 16 * b + 4 * q);
                 }
             }
-            __syncthreads();
-            put(s1);
-            if (half + 1 < DK / 64) {
-                fetch(s0, S0, half + 1);
-                fetch(s1, dS, half + 1);
-            }
-            __syncthreads();
-            if (w < NB) {
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    read_afresh();
-                    const int col = 64 * half + 16 * d;
-                    f32x4 x = zero4(), y = zero4();
-#pragma unroll
-                    for (int ks = 0; ks < VS; ++ks) x = mma(cols_op(sS, LS, 32 * ks, 16 * d, lane), rows_op(sU, LV, 16 * w, 32 * ks, lane), x);
-                    x *= splat4(st.down[t]);
-                    const f32x4 k = wide4(sK + t * LK + col + 4 * q);
-                    kc += dot4(x, k);
-                    for (int ks = w / 2; ks < KC; ++ks) {
-                        x = mma(cols_op(sQ, LK, 32 * ks, col, lane), Pm.cols(32 * ks, 16 * w, lane), x);
-                        y = mma(cols_op(sK, LK, 32 * ks, col, lane), Tm.cols(32 * ks, 16 * w, lane), y);
-                    }
-                    x -= y;
-                    dgamma -= dot4(x, k);
-                    sumQ[4 * half + d] += dq[d];
-                    sumK[4 * half + d] += x - rd[d];
-                }
+            for (int ks = 0; ks < KC; ++ks) {
+                xk[ks] = operand<E, 1>(x[2 * ks], x[2 * ks + 1]);
+                yk[ks] = operand<E, 1>(y[2 * ks], y[2 * ks + 1]);
             }
         }
-        if (w < NB) {
-            dbeta = column_sum(dbeta);
-            dgamma = column_sum(dgamma);
-            if (q == 0) {
-                if (t < ch.n)
-                    ((E*)a.dbeta)[(size_t)(ch.row + t) * a.H + h] = from_f<E>(dbeta + ((s_db[0][t] + s_db[1][t]) + (s_db[2][t] + s_db[3][t])));
-                s_dg[t] = dgamma;
+        // the gradients of queries and keys
+#pragma unroll
+        for (int half = 0; half < DK / 64; ++half) {
+            if (half > 0) {
+                __syncthreads();
+                put(half);
+                if (AHEAD && half + 1 == DK / 64 && hh + 1 < share) fetch(h + 1, tid, lane);
             }
+            __syncthreads();
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const int n = DT * gi + d, col = 64 * half + 16 * n;
+                read_afresh();
+                f32x4 xx = zero4(), yy = zero4(), zz = zero4();
+#pragma unroll
+                for (int ks = 0; ks < VS; ++ks) {
+                    const Op<E, 1> s = cols_op(sS0, LS, 32 * ks, 16 * n, lane);
+                    xx = mma(s, rows_op(sO, LV, 16 * tw, 32 * ks, lane), xx);
+                    yy = mma(s, rows_op(sV, LV, 16 * tw, 32 * ks, lane), yy);
+                    zz = mma(cols_op(sdS, LS, 32 * ks, 16 * n, lane), rows_op(sU, LV, 16 * tw, 32 * ks, lane), zz);
+                }
+                const f32x4 k4 = wide4(sK + t * LK + col + 4 * q), q4 = wide4(sQ + t * LK + col + 4 * q);
+                xx *= splat4(a.scale * st.up[t]);
+                yy *= splat4(st.up[t]);
+                zz *= splat4(st.down[t]);
+                dbeta -= dot4(yy, k4);
+                kc += dot4(zz, k4);
+                yy *= splat4(st.beta[t]);
+                f32x4 vv = zero4();
+#pragma unroll
+                for (int ks = 0; ks < KC; ++ks) {
+                    const Op<E, 1> k = cols_op(sK, LK, 32 * ks, col, lane);
+                    if (ks <= tw / 2) {
+                        xx = mma(k, xq[ks], xx);
+                        yy = mma(k, yq[ks], yy);
+                    }
+                    if (ks >= tw / 2) {
+                        zz = mma(cols_op(sQ, LK, 32 * ks, col, lane), xk[ks], zz);
+                        vv = mma(k, yk[ks], vv);
+                    }
+                }
+                zz -= vv;
+                dgamma += dot4(xx, q4) - dot4(yy + zz, k4);
+                sumQ[DT * half + d] += xx;
+                sumK[DT * half + d] += zz - yy;
+            }
+        }
+        dbeta = column_sum(dbeta);
+        dgamma = column_sum(dgamma);
+        if (q == 0) {
+            s_db2[gi][t] = dbeta;
+            s_dg[gi][t] = dgamma;
         }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) kc += __shfl_xor(kc, d);
         if (lane == 0) s_kc[w] = kc;
         __syncthreads();
-        if (a.g != nullptr && tid < 64) {
-            float x = tid < C ? s_dg[tid] : 0.f;
-            if (tid == C - 1) x += st.whole * ((s_ss[0] + s_ss[1]) + (s_ss[2] + s_ss[3])) + ((s_kc[0] + s_kc[1]) + (s_kc[2] + s_kc[3]));
+        if (tid < 64) {
+            float x = 0.f, b = 0.f, ends = 0.f, sums = 0.f;
+            if (tid < C) {
+#pragma unroll
+                for (int i = 0; i < GI; ++i) { x += s_dg[i][tid]; b += s_db2[i][tid]; }
+#pragma unroll
+                for (int i = 0; i < NW; ++i) b += s_db[i][tid];
+                if (tid < ch.n) ((E*)a.dbeta)[(size_t)(ch.row + tid) * a.H + h] = from_f<E>(b);
+            }
+#pragma unroll
+            for (int i = 0; i < NW; ++i) { ends += s_ss[i]; sums += s_kc[i]; }
+            if (tid == C - 1) x += st.whole * ends + sums;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
-                const float y = __shfl_down(x, d);
-                if (tid + d < 64) x += y;
+                const float y1 = __shfl_down(x, d);
+                if (tid + d < 64) x += y1;
             }
-            if (tid < ch.n) ((E*)a.dg)[(size_t)(ch.row + tid) * a.H + h] = from_f<E>(x);
+            if (a.g != nullptr && tid < ch.n) ((E*)a.dg)[(size_t)(ch.row + tid) * a.H + h] = from_f<E>(x);
         }
     }
-    if (w < NB) {
-        const int t = 16 * w + c;
-        if (t < ch.n) {
-            E* dq = (E*)a.dQ + (size_t)(ch.row + t) * (a.Hk * DK) + hk * DK + 4 * q;
-            E* dk = (E*)a.dK + (size_t)(ch.row + t) * (a.Hk * DK) + hk * DK + 4 * q;
+    const int q = lane0 >> 4, t = 16 * tw + (lane0 & 15);
+    if (t < ch.n) {
+        E* dq = (E*)a.dQ + (size_t)(ch.row + t) * (a.Hk * DK) + hk * DK + 4 * q;
+        E* dk = (E*)a.dK + (size_t)(ch.row + t) * (a.Hk * DK) + hk * DK + 4 * q;
 #pragma unroll
-            for (int d = 0; d < DK / 16; ++d) {
-                *(Vec4<E>*)(dq + 16 * d) = __builtin_convertvector(sumQ[d], Vec4<E>);
-                *(Vec4<E>*)(dk + 16 * d) = __builtin_convertvector(sumK[d], Vec4<E>);
-            }
+        for (int i = 0; i < DK / 64 * DT; ++i) {
+            const int col = 64 * (i / DT) + 16 * (DT * gi + i % DT);
+            *(Vec4<E>*)(dq + col) = __builtin_convertvector(sumQ[i], Vec4<E>);
+            *(Vec4<E>*)(dk + col) = __builtin_convertvector(sumK[i], Vec4<E>);
         }
     }
 }
@@ -447,6 +466,7 @@ hipError_t launch_delta_bwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* sav
         if ((e = launch_delta_states(a, p, ws, nullptr, dk, dv, dtype, st)) != hipSuccess) return e;
     } else {
         a.places = p.places;
+        a.run = p.run;
         a.N = ws + p.N;
         a.Z = (float*)(ws + p.Z);
         a.T = saved + p.T;
@@ -470,7 +490,7 @@ hipError_t launch_delta_bwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* sav
     const size_t blocks = (size_t)p.places * a.Hk + (clear ? (a.rows.T + 63) / 64 : 0);
     if (blocks == 0) return hipSuccess;
     const dim3 grid((unsigned)blocks);
-#define CHELA_RUN(E, DK, DV) hipLaunchKernelGGL((delta_grad_kernel<E, DK, DV>), grid, dim3(256), 0, st, a)
+#define CHELA_RUN(E, DK, DV) hipLaunchKernelGGL((delta_grad_kernel<E, DK, DV>), grid, dim3(DV * 4), 0, st, a)
     CHELA_DELTA(CHELA_RUN)
 #undef CHELA_RUN
     return hipGetLastError();
