@@ -343,12 +343,13 @@ __device__ __forceinline__ void clear_rows(const Rows& r, int block, E* to, int 
     }
 }
 
-// T = (1 + A)^-1 of a chunk, A_ts = beta_t e^(gamma_t - gamma_s) k_t . k_s below the diagonal, from its keys in LDS; all 256 threads, sA [C][C + 4] and sD
-// [C][20] are room for them.  fp32 throughout: blocks of 16 on the diagonal row by row, those below by products with them.
+// T = (1 + A)^-1 of a chunk, A_ts = beta_t e^(gamma_t - gamma_s) k_t . k_s below the diagonal, from its keys in LDS; the first 256 threads of a workgroup
+// work, all have to call.  sA: room for C (C + 4) floats, where T may be too.  fp32 throughout: blocks of 16 on the diagonal row by row, in place,
+// those below by products with them.
 template <typename E, int DK, int P, int C>
-__device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSteps<C>& st, float* sA, float* sD, const Planes<E, P>& T, int tid)
+__device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSteps<C>& st, float* sA, const Planes<E, P>& T, int tid)
 {
-    constexpr int NB = C / 16, LA = C + 4, LD = 20;
+    constexpr int NB = C / 16, LA = C + 4;
     const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
     // A, sixteen tokens to a wave
     if (w < NB) {
@@ -366,9 +367,10 @@ __device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSt
         }
     }
     __syncthreads();
-    // the inverses of 1 + A's blocks on the diagonal, a lane to a column: x_i = e_i - sum_{j<i} A_ij x_j
+    // the inverses of 1 + A's blocks on the diagonal, a lane to a column: x_i = e_i - sum_{j<i} A_ij x_j.  (One wave: a row is written when it has
+    // been read for the last time.)
     if (tid < C) {
-        const float* A = sA + 16 * q * LA + 16 * q;
+        float* A = sA + 16 * q * LA + 16 * q;
         float x[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -380,8 +382,10 @@ __device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSt
                 for (int j = 0; j < 4; ++j) if (4 * j4 + j < i) s = fmaf(-r[j], x[4 * j4 + j], s);
             }
             x[i] = s;
-            sD[(16 * q + i) * LD + c] = s;
         }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) A[i * LA + c] = x[i];
     }
     __syncthreads();
     // the blocks below it, a wave to a column of blocks: T_rj = -T_rr sum_{j<=b<r} A_rb T_bj, fp32 products
@@ -392,7 +396,7 @@ __device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSt
             t[r] = zero4();
             if (r == w) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) t[r][i] = sD[(16 * r + 4 * q + i) * LD + c];
+                for (int i = 0; i < 4; ++i) t[r][i] = sA[(16 * r + 4 * q + i) * LA + 16 * r + c];
             } else if (r > w) {
                 f32x4 x = zero4();
 #pragma unroll
@@ -402,17 +406,26 @@ __device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSt
 #pragma unroll
                         for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(m[i], t[b][i], x, 0, 0, 0);
                     }
-                const f32x4 m = *(const f32x4*)(sD + (16 * r + c) * LD + 4 * q);
+                const f32x4 m = *(const f32x4*)(sA + (16 * r + c) * LA + 16 * r + 4 * q);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) t[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(-m[i], x[i], t[r], 0, 0, 0);
             }
         }
+    }
+    __syncthreads();
+    if (w < NB) {
 #pragma unroll
         for (int r = 0; r < NB; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i) T.put(16 * r + 4 * q + i, 16 * w + c, t[r][i]);
     }
     __syncthreads();
+}
+// Room for either, in elements.
+template <typename E, int P> constexpr int inverse_room()
+{
+    constexpr int C = DeltaChunk<E>::C, t = P * C * (C + kPad<E>), a = C * (C + 4) * 4 / sizeof(E);
+    return t > a ? t : a;
 }
 
 // RUN(element type, DK, DV) for a call's.

@@ -15,11 +15,10 @@ namespace chela {
 
 // ---- a chunk's T, N and Z
 template <typename E, int DK, int DV, int P>
-__global__ __launch_bounds__(256, 2) void delta_prep_kernel(DeltaArgs a)
+__global__ __launch_bounds__(256, DK + DV == 128 ? 4 : 2) void delta_prep_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
-    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[P * C * LT];
-    __shared__ __align__(16) float sA[C * (C + 4)], sD[C * 20];
+    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[inverse_room<E, P>()];
     __shared__ ChunkSteps<C> st;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
     const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
@@ -37,7 +36,7 @@ __global__ __launch_bounds__(256, 2) void delta_prep_kernel(DeltaArgs a)
     }
     __syncthreads();
     const Planes<E, P> T{sT, LT, C * LT};
-    chunk_inverse<E, DK>(sK, LK, st, sA, sD, T, tid);
+    chunk_inverse<E, DK>(sK, LK, st, (float*)sT, T, tid);
     const size_t at = (size_t)place * a.H + h;
     {
         // T for the kernels behind
@@ -104,11 +103,10 @@ __global__ __launch_bounds__(256, 2) void delta_prep_kernel(DeltaArgs a)
 
 // ---- T alone, of all chunks, for runs of them
 template <typename E, int DK, int P>
-__global__ __launch_bounds__(256) void delta_inverse_kernel(DeltaArgs a)
+__global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, LK = DK + kPad<E>, LT = C + kPad<E>, W = 16 / sizeof(E);
-    __shared__ __align__(16) E sK[C * LK], sT[P * C * LT];
-    __shared__ __align__(16) float sA[C * (C + 4)], sD[C * 20];
+    __shared__ __align__(16) E sK[C * LK], sT[inverse_room<E, P>()];
     __shared__ ChunkSteps<C> st;
     const int tid = threadIdx.x, lane = tid & 63;
     const int i = blockIdx.x / a.H, h = blockIdx.x - i * a.H, hk = h / (a.H / a.Hk);
@@ -121,7 +119,7 @@ __global__ __launch_bounds__(256) void delta_inverse_kernel(DeltaArgs a)
     put_steps(st, s, n, tid);
     k.put(sK, LK, n, tid);
     __syncthreads();
-    chunk_inverse<E, DK>(sK, LK, st, sA, sD, Planes<E, P>{sT, LT, C * LT}, tid);
+    chunk_inverse<E, DK>(sK, LK, st, (float*)sT, Planes<E, P>{sT, LT, C * LT}, tid);
     E* to = (E*)a.T + ((size_t)i * a.H + h) * (P * C * C);
 #pragma unroll
     for (int j = tid; j < P * C * (C / W); j += 256) *(u32x4*)(to + j * W) = *(const u32x4*)(sT + j / (C / W) * LT + j % (C / W) * W);
@@ -284,7 +282,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
 template <typename E, int DK, int P, int G, bool REV>
 __global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
 {
-    constexpr int C = DeltaChunk<E>::C, KS = DK / 32, NE = kOpElems<E, P>, OE = kOpElems<E, 2>, AHEAD = 4;
+    constexpr int C = DeltaChunk<E>::C, KS = DK / 32, NE = kOpElems<E, P>, OE = kOpElems<E, 2>, AHEAD = DK == 64 && P == 1 ? 8 : 4;
     __shared__ __align__(16) E sS[2][G][KS * OE];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
     // (workgroups go to the eight L2s in turn: those of one head, which read the same N, to one of them)

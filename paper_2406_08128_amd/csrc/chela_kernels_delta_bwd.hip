@@ -17,8 +17,7 @@ template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
-    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sO[C * LV], sT[P * C * LT], sP[P * C * LT];
-    __shared__ __align__(16) float s_inv[P == 2 ? C * (C + 4) + C * 20 : 1];
+    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sO[C * LV], sT[P == 2 ? inverse_room<E, P>() : C * LT], sP[P * C * LT];
     __shared__ ChunkSteps<C> st;
     __shared__ __align__(16) float s_qu[C];                        // scale e^gamma
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
@@ -43,7 +42,7 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
     }
     __syncthreads();
     const Planes<E, P> T{sT, LT, C * LT}, Pt{sP, LT, C * LT};
-    if (P == 2) chunk_inverse<E, DK>(sK, LK, st, s_inv, s_inv + C * (C + 4), T, tid);       // (what was kept of it has one part)
+    if (P == 2) chunk_inverse<E, DK>(sK, LK, st, (float*)sT, T, tid);       // (what was kept of it has one part)
     if (w < NB) {                                                  // P's transpose, sixteen of its rows to a wave
         const int s = 16 * w + c;
         for (int tb = w & ~1; tb < NB; ++tb) {
