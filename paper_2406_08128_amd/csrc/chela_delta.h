@@ -213,10 +213,16 @@ __device__ __forceinline__ Chunk chunk_at(const Rows& r, int C, int place, int l
         c.seq = first + below - 1;
         c.index = place - chunk_key(r, C, c.seq);
     }
-    if (c.seq >= r.n_seq || c.index >= chunks_in(r, C, c.seq)) return c;
+    if (c.seq >= r.n_seq || c.index < 0 || c.index >= chunks_in(r, C, c.seq)) return c;       // (below 0: offsets out of order)
     c.row = (r.cu == nullptr ? c.seq * r.L : seq_begin(r, c.seq)) + c.index * C;
     c.n = min(C, (r.cu == nullptr ? (c.seq + 1) * r.L : seq_end(r, c.seq)) - c.row);
     return c;
+}
+
+// The place of the k-th chunk of a run among all chunks, whatever runs there are.
+__device__ __forceinline__ int chunk_place(const Rows& r, int C, const Chunk& run, int chunks_to_a_run, int k)
+{
+    return chunk_key(r, C, run.seq) + run.index * chunks_to_a_run + k;
 }
 
 // ---- what a chunk's tokens have of their own: beta, and the running sum of the log decays, gamma.  Sums of 64 bits, held as two floats: two
@@ -293,13 +299,13 @@ __device__ __forceinline__ void put_steps(ChunkSteps<C>& st, const Steps& x, int
 
 // The same operand with each of its eight terms times a factor: f[k0 ..], one for each row of the tile that it was read from.
 template <typename E, int P>
-__device__ __forceinline__ Op<E, P> scaled(const Op<E, 1>& x, const float* f, int k0, int lane)
+__device__ __forceinline__ Op<E, P> scaled(const Op<E, 1>& x, const float* f, int k0, int lane, float by = 1.f)
 {
     const f32x4 a = *(const f32x4*)(f + k0 + 4 * (lane >> 4)), b = *(const f32x4*)(f + k0 + 16 + 4 * (lane >> 4));
     f32x8 v;
     if constexpr (sizeof(E) == 4) v = x.v;
     else v = __builtin_convertvector(x.h, f32x8);
-    v *= __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    v *= __builtin_shufflevector(a * by, b * by, 0, 1, 2, 3, 4, 5, 6, 7);
     return operand<E, P>(__builtin_shufflevector(v, v, 0, 1, 2, 3), __builtin_shufflevector(v, v, 4, 5, 6, 7));
 }
 

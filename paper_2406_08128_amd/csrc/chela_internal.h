@@ -278,14 +278,15 @@ int block_norm_bwd_parts(long rows, int D);            // partial sums of dw_pos
 hipError_t launch_block_norm_fwd(const BlockNormArgs& a, int dtype, hipStream_t st);
 hipError_t launch_block_norm_bwd(const BlockNormArgs& a, int dtype, hipStream_t st);
 
-// Gated delta rule.  A sequence's rows are cut into chunks (of kDeltaChunkBf16 or kDeltaChunkF32 tokens); `places` is how many there may be,
-// and each has room for what the kernels hand to each other, per head.  states: of a call with states or their gradients, given or wanted.  kept: a
-// gradient is to be had from what each chunk leaves.
+// Gated delta rule.  A sequence's rows are cut into chunks (of kDeltaChunkBf16 or kDeltaChunkF32 tokens), and these into runs of `run` chunks that the
+// states are walked by; `chunks` and `places` are how many there may be, and each has room for what the kernels hand to each other, per head.
 struct DeltaPlan {
-    int chunk, run, places, parts, t_parts;     // run: chunks that share a place; t_parts: of T; parts: of the operands that a state goes through (1, or 2 in bf16)
-    size_t N, Z, bytes;                   // byte offsets into the scratch, and its size
-    size_t T, S0, whole, saved_bytes;     // ... into `saved` (without one: this many bytes of the scratch from `saved_at` on)
-    size_t saved_at, dS;
+    int chunk, chunks, run, places;
+    int parts, t_parts;                   // of the operands in memory that a state goes through (1, or 2 in bf16), of T
+    size_t N, Z, whole, S0, dS, bytes;    // byte offsets into the scratch, and its size.  S0: per run (`own_states`), where the chunks' are not the same
+    size_t T, S0c, saved_bytes;           // ... into `saved` (without one: this many bytes of the scratch from `saved_at` on)
+    size_t saved_at;
+    bool own_states;
 };
 struct DeltaArgs {
     Rows rows;
@@ -296,14 +297,16 @@ struct DeltaArgs {
     void *O, *dQ, *dK, *dV, *dg, *dbeta;
     float scale;
     int H, Hk, places, run, t_parts;
-    void *N, *T, *S0, *dS;                // between the kernels, [places][H] of each
+    void *N, *T, *S0, *S0c, *dS;          // between the kernels, [places][H] of each; T and S0c, the states in front of all chunks (or null), [chunks][H]
     float *Z, *whole;
 };
 constexpr int kDeltaChunkBf16 = 64, kDeltaChunkF32 = 32;
 bool delta_dims_ok(int dk, int dv);
-DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states, bool kept);
+// is_bwd, has_saved: of the gradient, given `saved` (of the forward: wanting it).  states: of a call with states or their gradients, given or
+// wanted.
+DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int Hk, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states);
 hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st);
-hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st);
+hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int parts, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_bwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, bool has_saved, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_step(const DeltaArgs& a, int dk, int dv, int dtype, hipStream_t st);

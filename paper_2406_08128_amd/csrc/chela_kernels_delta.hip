@@ -110,14 +110,13 @@ __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
     __shared__ ChunkSteps<C> st;
     const int tid = threadIdx.x, lane = tid & 63;
     const int i = blockIdx.x / a.H, h = blockIdx.x - i * a.H, hk = h / (a.H / a.Hk);
-    const Chunk ch = chunk_at(a.rows, C * a.run, i / a.run, lane);
-    const int row = ch.row + i % a.run * C, n = min(C, ch.n - i % a.run * C);
-    if (n <= 0) return;
+    const Chunk ch = chunk_at(a.rows, C, i, lane);
+    if (ch.n <= 0) return;
     Tile<E, C, DK> k;
-    const Steps s = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, row, h, n, lane);
-    k.fetch((const E*)a.K + hk * DK, a.ldk, row, n, tid);
-    put_steps(st, s, n, tid);
-    k.put(sK, LK, n, tid);
+    const Steps s = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, lane);
+    k.fetch((const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid);
+    put_steps(st, s, ch.n, tid);
+    k.put(sK, LK, ch.n, tid);
     __syncthreads();
     chunk_inverse<E, DK>(sK, LK, st, (float*)sT, Planes<E, P>{sT, LT, C * LT}, tid);
     E* to = (E*)a.T + ((size_t)i * a.H + h) * (P * C * C);
@@ -141,6 +140,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
     const Chunk ch = chunk_at(a.rows, C * a.run, place, lane0);
     if (ch.n <= 0) return;
     const size_t at = (size_t)place * a.H + h;
+    const int chunk0 = chunk_place(a.rows, C, ch, a.run, 0);
     const bool of_k = w < DK / 32;
     const int col = 32 * (of_k ? w : w - DK / 32);
     Tile<E, C, DK, NT> tk;
@@ -152,7 +152,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
         ts = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, row, h, n, lane);
         tk.fetch((const E*)a.K + hk * DK, a.ldk, row, n, tid);
         tv.fetch((const E*)a.V + h * DV, a.ldv, row, n, tid);
-        tt.fetch((const E*)a.T + (((size_t)place * a.run + r) * a.H + h) * (P * C * C), C, 0, P * C, tid);
+        tt.fetch((const E*)a.T + ((size_t)(chunk0 + r) * a.H + h) * (P * C * C), C, 0, P * C, tid);
     };
     fetch(0, tid0, lane0);
     const Planes<E, P> T{sT, LT, C * LT};
@@ -276,19 +276,19 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
     if (tid0 == 0) a.whole[at] = before;
 }
 
-// ---- the walk: S <- whole S + Z - N S from chunk to chunk (N comes negated), 16 G of S's columns to a workgroup, sixteen of its rows to a wave.
+// ---- the walk: S <- whole S + Z - N S from chunk to chunk (N comes negated), sixteen of S's columns to a workgroup, sixteen of its rows to a wave.
 // Each wave keeps its rows in fp32 and hands them to the others as operands, through LDS; what the next chunks need is on its way
 // meanwhile.  REV: from the last chunk to the first, with the states' gradients.
-template <typename E, int DK, int P, int G, bool REV>
+template <typename E, int DK, int P, bool REV>
 __global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
 {
     constexpr int C = DeltaChunk<E>::C, KS = DK / 32, NE = kOpElems<E, P>, OE = kOpElems<E, 2>, AHEAD = DK == 64 && P == 1 ? 8 : 4;
-    __shared__ __align__(16) E sS[2][G][KS * OE];
+    __shared__ __align__(16) E sS[2][KS * OE];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
     // (workgroups go to the eight L2s in turn: those of one head, which read the same N, to one of them)
-    const int groups = DV / (16 * G), all = a.rows.n_seq * a.H * groups, id = (int)(blockIdx.x & 7) * ((all + 7) / 8) + (int)(blockIdx.x >> 3);
+    const int groups = DV / 16, all = a.rows.n_seq * a.H * groups, id = (int)(blockIdx.x & 7) * ((all + 7) / 8) + (int)(blockIdx.x >> 3);
     if (id >= all) return;
-    const int eg = id % groups * G, h = id / groups % a.H, seq = id / groups / a.H;
+    const int eg = id % groups, h = id / groups % a.H, seq = id / groups / a.H;
     const int first = chunk_key(a.rows, C * a.run, seq), n = min(chunks_in(a.rows, C * a.run, seq), a.places - first);
     const int slot = slot_of(a.rows, seq);
     const float* from = REV ? a.dS_out : a.S_in;
@@ -296,17 +296,13 @@ __global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
     E* keep = (E*)(REV ? a.dS : a.S0) + (size_t)eg * (DK * 16) + (w >> 1) * 512 + 8 * lane + 4 * (w & 1);
     const float* z = a.Z + (size_t)(eg * (DK / 16) + w) * 256 + 4 * lane;
     const E* nn = (const E*)a.N + (size_t)w * KS * NE;
-    f32x4 S[G];
+    f32x4 S = zero4();
     const size_t mine = (((size_t)max(slot, 0) * a.H + h) * DK + 16 * w + 4 * q) * DV + 16 * eg + c;
+    if (from != nullptr && slot >= 0)
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-        S[g] = zero4();
-        if (from != nullptr && slot >= 0)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) S[g][j] = from[mine + (size_t)j * DV + 16 * g];
-    }
+        for (int j = 0; j < 4; ++j) S[j] = from[mine + (size_t)j * DV];
     Op<E, P> N[AHEAD][KS];
-    f32x4 Z[AHEAD][G];
+    f32x4 Z[AHEAD];
     float whole[AHEAD];
     auto load = [&](int u, int k) {
         k = min(k, n - 1);
@@ -314,8 +310,7 @@ __global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
         whole[u] = a.whole[at];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) N[u][ks] = load_op<E, P>(nn + at * (DK / 16 * KS * NE) + ks * NE, lane);
-#pragma unroll
-        for (int g = 0; g < G; ++g) Z[u][g] = *(const f32x4*)(z + at * ((size_t)DK * DV) + g * (DK * 16));
+        Z[u] = *(const f32x4*)(z + at * ((size_t)DK * DV));
     };
     if (n > 0) {
 #pragma unroll
@@ -327,35 +322,27 @@ __global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
             const int k = k0 + u;
             if (k >= n) break;
             E* out = keep + ((size_t)(first + (REV ? n - 1 - k : k)) * a.H + h) * ((size_t)DK * DV);
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                // (the wave's rows are one half of an operand's terms)
-                E* half = sS[u & 1][g] + (w >> 1) * OE + 8 * lane + 4 * (w & 1);
-                if constexpr (sizeof(E) == 4) {
-                    *(f32x4*)half = S[g];
-                    *(f32x4*)(out + g * (DK * 16)) = S[g];
-                } else {
-                    const bf16x4 hi = __builtin_convertvector(S[g], bf16x4);
-                    *(bf16x4*)half = hi;
-                    *(bf16x4*)(half + 512) = __builtin_convertvector(S[g] - __builtin_convertvector(hi, f32x4), bf16x4);
-                    *(bf16x4*)(out + g * (DK * 16)) = hi;
-                }
+            // (the wave's rows are one half of an operand's terms)
+            E* half = sS[u & 1] + (w >> 1) * OE + 8 * lane + 4 * (w & 1);
+            if constexpr (sizeof(E) == 4) {
+                *(f32x4*)half = S;
+                *(f32x4*)out = S;
+            } else {
+                const bf16x4 hi = __builtin_convertvector(S, bf16x4);
+                *(bf16x4*)half = hi;
+                *(bf16x4*)(half + 512) = __builtin_convertvector(S - __builtin_convertvector(hi, f32x4), bf16x4);
+                *(bf16x4*)out = hi;
             }
             __syncthreads();
+            S = S * whole[u] + Z[u];
 #pragma unroll
-            for (int g = 0; g < G; ++g) S[g] = S[g] * whole[u] + Z[u][g];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                for (int g = 0; g < G; ++g) S[g] = mma(N[u][ks], load_op<E, 2>(sS[u & 1][g] + ks * OE, lane), S[g]);
+            for (int ks = 0; ks < KS; ++ks) S = mma(N[u][ks], load_op<E, 2>(sS[u & 1] + ks * OE, lane), S);
             load(u, k + AHEAD);
         }
     }
     if (to != nullptr && slot >= 0)
 #pragma unroll
-        for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) to[mine + (size_t)j * DV + 16 * g] = S[g][j];
+        for (int j = 0; j < 4; ++j) to[mine + (size_t)j * DV] = S[j];
 }
 
 // ---- the outputs
@@ -375,6 +362,7 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
     const Chunk ch = chunk_at(a.rows, C * a.run, place, lane0);
     if (ch.n <= 0) return;
     const E* S0 = (const E*)a.S0 + ((size_t)place * a.H + h) * (DK * DV) + (size_t)w * (KS * 512);
+    const int chunk0 = chunk_place(a.rows, C, ch, a.run, 0);
     Tile<E, C, DK, NT> tk, tq;
     Tile<E, C, DV, NT> tv;
     Tile<E, C, C, NT> tt;
@@ -385,7 +373,7 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
         tk.fetch((const E*)a.K + hk * DK, a.ldk, row, n, tid);
         tq.fetch((const E*)a.Q + hk * DK, a.ldq, row, n, tid);
         tv.fetch((const E*)a.V + h * DV, a.ldv, row, n, tid);
-        tt.fetch((const E*)a.T + (((size_t)place * a.run + r) * a.H + h) * (a.t_parts * C * C), C, 0, C, tid);
+        tt.fetch((const E*)a.T + ((size_t)(chunk0 + r) * a.H + h) * (a.t_parts * C * C), C, 0, C, tid);
     };
     Op<E, 1> so[KS];
     f32x4 S[DK / 16];
@@ -408,6 +396,10 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
         tt.put(sT, LT, C, tid);
         if (AHEAD && !last) fetch(r + 1, tid, lane);
         __syncthreads();
+        if (a.S0c != nullptr)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                store_op<E, 1>((E*)a.S0c + ((size_t)(chunk0 + r) * a.H + h) * (DK * DV) + (w * KS + ks) * 512, so[ks], lane);
         if (w < NB) {
             const Planes<E, 1> Pm{sP, LT, 0};
             const int t = 16 * w + c;
@@ -551,18 +543,23 @@ __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a)
 // -------------------------------------------------------------------------------------------------------------------- host
 bool delta_dims_ok(int dk, int dv) { return (dk == 64 || dk == 128) && (dv == 64 || dv == 128); }
 
-// Chunks to a run, a power of two, where nothing is kept of each for a gradient.  A run's chunks are one after the other in a workgroup, the runs of
-// a sequence in the walk: R c + n w / R for n chunks, c and w the times that a chunk takes of either, is least where R^2 = n w / c.  w / c is about
-// 1/16 with heads of 64, 1/8 where there are heads of 128 (0.5 us of 8, 1.3 of 12).  Measured (us; R = 1, 2, 4, 8, 16), bf16, 12 heads of 64, one
+// Chunks to a run, a power of two.  A run's chunks are one after the other in a workgroup, the runs of a sequence in the walk: R c + n w / R for n
+// chunks, c and w the times that a chunk takes of either, is least where R^2 = n w / c.  w / c is about 1/16 with heads of 64, 1/8 where there are
+// heads of 128 (0.5 us of 8, 1.3 of 12), 1/32 with fp32's shorter chunks.  Measured (us; R = 1, 2, 4, 8, 16), bf16, nothing kept, 12 heads of 64, one
 // sequence of 2048 tokens 41 44 57 89 157, of 8192 102 92 90 108 173, of 32768 328 275 235 220 255; 8 of 1024 60 69 76 99 163; 16 heads of
-// 128, 2048 tokens 78 74 93 149 269, 8192 355 254 205 207 312, 65536 2475 2057 1621 1401 1299.
-static int chunks_to_a_run(long n, int dk, int dv)
+// 128, 2048 tokens 78 74 93 149 269, 8192 355 254 205 207 312, 65536 2475 2057 1621 1401 1299.  With what a gradient needs kept, and the gradient
+// (R = 1, 2, 4, 8): 12 heads of 64, one sequence of 4096 48 51 56 85, 69 68 89 158, of 16384 147 136 117 134, 216 185 184 206, 4 of 8192 220 204
+// 193 188, 344 322 311 337; 16 heads of 128, 8 of 4096 730 697 616 582, 1270 1393 1268 1220; fp32, 12 heads of 64, 8 of 1024 107 119 114 136, 250
+// 250 239 302, one of 4096 104 91 88 93, 170 150 169 169.
+static int chunks_to_a_run(long n, int dk, int dv, int dtype)
 {
+    const int w = dk + dv > 128 ? 8 : dtype != 0 ? 32 : 16;
     int r = 1;
-    while (r < 16 && (long)r * r * (dk + dv > 128 ? 8 : 16) < n) r *= 2;
+    while (r < 16 && (long)r * r * w < n) r *= 2;
     return r;
 }
-DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states, bool kept)
+
+DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int Hk, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states)
 {
     DeltaPlan p{};
     const size_t es = dtype != 0 ? 4 : 2;
@@ -570,17 +567,23 @@ DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, 
     p.chunk = dtype != 0 ? kDeltaChunkF32 : kDeltaChunkBf16;
     const int len = n_seq > 0 ? T / n_seq : 0;
     auto places = [&](int tokens) { return T <= 0 || n_seq <= 0 ? 0 : packed ? T / tokens + n_seq : n_seq * ((len + tokens - 1) / tokens); };
-    p.run = kept ? 1 : chunks_to_a_run(((long)len + p.chunk - 1) / p.chunk, dk, dv);
+    p.run = chunks_to_a_run(((long)len + p.chunk - 1) / p.chunk, dk, dv, dtype);
+    // (T is kept in one part; a gradient walks the runs with a state for one value head)
+    if (((is_bwd || has_saved) && p.parts == 2) || (is_bwd && H != Hk)) p.run = 1;
+    p.chunks = places(p.chunk);
     p.places = places(p.chunk * p.run);
-    const size_t n = (size_t)p.places * H;
+    const size_t all = (size_t)p.chunks * H, n = is_bwd && !has_saved ? all : (size_t)p.places * H;      // (the states are then walked chunk by chunk)
     auto room = [](size_t& at, size_t bytes) { const size_t was = at; at += (bytes + 255) & ~(size_t)255; return was; };
-    p.t_parts = p.run > 1 ? p.parts : 1;
-    p.T = room(p.saved_bytes, n * p.run * p.t_parts * p.chunk * p.chunk * es);
-    p.S0 = room(p.saved_bytes, n * dk * dv * es);
-    p.whole = room(p.saved_bytes, n * sizeof(float));
+    p.t_parts = is_bwd || has_saved || p.run == 1 ? 1 : p.parts;
+    p.own_states = !is_bwd && p.run > 1;
+    p.T = room(p.saved_bytes, all * p.t_parts * p.chunk * p.chunk * es);
+    p.S0c = p.saved_bytes;
+    if (is_bwd || has_saved || !p.own_states) room(p.saved_bytes, all * dk * dv * es);
     p.N = room(p.bytes, n * p.parts * dk * dk * es);
     p.Z = room(p.bytes, n * dk * dv * sizeof(float));
-    if (is_bwd) p.dS = room(p.bytes, n * dk * dv * es);
+    p.whole = room(p.bytes, n * sizeof(float));
+    if (p.own_states) p.S0 = room(p.bytes, n * dk * dv * es);
+    if (is_bwd) p.dS = room(p.bytes, (size_t)p.places * H * dk * dv * es);
     p.saved_at = p.bytes;
     if (!has_saved) p.bytes += p.saved_bytes;
     return p;
@@ -589,11 +592,10 @@ DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int dk, int dv, 
 hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int parts, int dk, int dv, int dtype, hipStream_t st)
 {
     if (a.rows.n_seq == 0) return hipSuccess;
-    const int G = 1;
-    const dim3 grid((unsigned)(((size_t)a.rows.n_seq * a.H * (dv / (16 * G)) + 7) / 8 * 8));
+    const dim3 grid((unsigned)(((size_t)a.rows.n_seq * a.H * (dv / 16) + 7) / 8 * 8));
 #define CHELA_W(E, DK, P)                                                                                             \
-    if (reverse) hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, 1, true>), grid, dim3(DK * 4), 0, st, a, dv);        \
-    else hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, 1, false>), grid, dim3(DK * 4), 0, st, a, dv)
+    if (reverse) hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, true>), grid, dim3(DK * 4), 0, st, a, dv);        \
+    else hipLaunchKernelGGL((delta_walk_kernel<E, DK, P, false>), grid, dim3(DK * 4), 0, st, a, dv)
     if (dtype != 0) { if (dk == 64) { CHELA_W(float, 64, 1); } else { CHELA_W(float, 128, 1); } }
     else if (parts == 2) { if (dk == 64) { CHELA_W(bf16, 64, 2); } else { CHELA_W(bf16, 128, 2); } }
     else { if (dk == 64) { CHELA_W(bf16, 64, 1); } else { CHELA_W(bf16, 128, 1); } }
@@ -601,25 +603,15 @@ hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int parts, int dk
     return hipGetLastError();
 }
 
-// The states in front of all chunks, and T.
-hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st)
+// T of all chunks, the states in front of all runs.
+hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, int dk, int dv, int dtype, hipStream_t st)
 {
-    if (saved == nullptr) saved = ws + p.saved_at;
-    a.places = p.places;
-    a.run = p.run;
-    a.t_parts = p.t_parts;
-    a.N = ws + p.N;
-    a.Z = (float*)(ws + p.Z);
-    a.T = saved + p.T;
-    a.S0 = saved + p.S0;
-    a.whole = (float*)(saved + p.whole);
     if (p.places > 0) {
-        const dim3 grid((unsigned)((size_t)p.places * a.H));
+        const dim3 grid((unsigned)((size_t)a.places * a.H)), chunks((unsigned)((size_t)p.chunks * a.H));
 #define CHELA_RUN(E, DK, DV)                                                                                          \
     do {                                                                                                              \
         constexpr int P2 = sizeof(E) == 2 ? 2 : 1;                                                                    \
-        if (p.run > 1) {                                                                                              \
-            const dim3 chunks((unsigned)((size_t)p.places * p.run * a.H));                                            \
+        if (a.run > 1) {                                                                                              \
             if (p.parts == 2) hipLaunchKernelGGL((delta_inverse_kernel<E, DK, P2>), chunks, dim3(256), 0, st, a);     \
             else hipLaunchKernelGGL((delta_inverse_kernel<E, DK, 1>), chunks, dim3(256), 0, st, a);                   \
             if (p.parts == 2) hipLaunchKernelGGL((delta_prep_run_kernel<E, DK, DV, P2>), grid, dim3((DK + DV) * 2), 0, st, a); \
@@ -640,7 +632,18 @@ hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, char* ws, char*
 hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st)
 {
     ProfScope prof(KID_DELTA, st);
-    const hipError_t e = launch_delta_states(a, p, ws, saved, dk, dv, dtype, st);
+    const bool kept = saved != nullptr;
+    if (!kept) saved = ws + p.saved_at;
+    a.places = p.places;
+    a.run = p.run;
+    a.t_parts = p.t_parts;
+    a.N = ws + p.N;
+    a.Z = (float*)(ws + p.Z);
+    a.whole = (float*)(ws + p.whole);
+    a.T = saved + p.T;
+    a.S0 = p.own_states ? ws + p.S0 : saved + p.S0c;
+    a.S0c = p.own_states && kept ? saved + p.S0c : nullptr;
+    const hipError_t e = launch_delta_states(a, p, dk, dv, dtype, st);
     if (e != hipSuccess) return e;
     const bool clear = a.rows.clear && a.rows.cu != nullptr;
     const size_t blocks = (size_t)p.places * a.H + (clear ? (a.rows.T + 63) / 64 : 0);

@@ -41,6 +41,7 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
         if (P == 1) m.put(sT, LT, C, tid);
     }
     __syncthreads();
+    if (tid == 0) a.whole[at] = st.whole;
     const Planes<E, P> T{sT, LT, C * LT}, Pt{sP, LT, C * LT};
     if (P == 2) chunk_inverse<E, DK>(sK, LK, st, (float*)sT, T, tid);       // (what was kept of it has one part)
     if (w < NB) {                                                  // P's transpose, sixteen of its rows to a wave
@@ -126,6 +127,187 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
     }
 }
 
+// ---- the same for a run of chunks, from its last to its first: one N^T and one Z' for all of them.  What a chunk makes of a state's gradient,
+//     dS <- e^gamma dS + scale (e^gamma Q)^T dO - (beta e^gamma K)^T T^T (P^T dO + K~ dS),
+// with Z' beside what is left of the identity (X = M^T - e^Gamma, without the terms in dO), thirty-two columns to a wave.
+template <typename E, int DK, int DV>
+__global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(DeltaArgs a)
+{
+    constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
+    constexpr int NT = (DK + DV) * 2, NW = NT / 64;
+    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sO[C * LV], sT[C * LT], sP[C * LT];
+    __shared__ ChunkSteps<C> st;
+    const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6);
+    const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
+    const Chunk ch = chunk_at(a.rows, C * a.run, place, lane0);
+    if (ch.n <= 0) return;
+    const size_t at = (size_t)place * a.H + h;
+    const int chunk0 = chunk_place(a.rows, C, ch, a.run, 0), n_chunks = (ch.n + C - 1) / C;
+    const bool of_k = w < DK / 32;
+    const int col = 32 * (of_k ? w : w - DK / 32);
+    Tile<E, C, DK, NT> tq, tk;
+    Tile<E, C, DV, NT> to;
+    Tile<E, C, C, NT> tt;
+    Steps ts;
+    auto fetch = [&](int r, int tid, int lane) {
+        const int row = ch.row + r * C, n = min(C, ch.n - r * C);
+        ts = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, row, h, n, lane);
+        tq.fetch((const E*)a.Q + hk * DK, a.ldq, row, n, tid);
+        tk.fetch((const E*)a.K + hk * DK, a.ldk, row, n, tid);
+        to.fetch((const E*)a.dO + h * DV, a.lddo, row, n, tid);
+        tt.fetch((const E*)a.T + ((size_t)(chunk0 + r) * a.H + h) * (C * C), C, 0, C, tid);
+    };
+    fetch(n_chunks - 1, tid0, lane0);
+    const Planes<E, 1> T{sT, LT, 0}, Pt{sP, LT, 0};
+    f32x4 X[DK / 16][2];
+#pragma unroll
+    for (int d = 0; d < DK / 16; ++d) X[d][0] = X[d][1] = zero4();
+    float before = 1.f;
+    for (int r = n_chunks - 1; r >= 0; --r) {
+        const int n = min(C, ch.n - r * C);
+        const bool first = r == n_chunks - 1;
+        int lane = lane0;
+        asm volatile("" : "+v"(lane));             // (addresses are worked out where they are used)
+        const int tid = 64 * w + lane, q = lane >> 4, c = lane & 15;
+        if (!first) __syncthreads();
+        put_steps(st, ts, n, tid);
+        tq.put(sQ, LK, n, tid);
+        tk.put(sK, LK, n, tid);
+        to.put(sO, LV, n, tid);
+        tt.put(sT, LT, C, tid);
+        if (r > 0) fetch(r - 1, tid, lane);
+        __syncthreads();
+        {
+            constexpr int GI = NW / NB > 0 ? NW / NB : 1;
+            const int tw = w % NB, gi = w / NB, s = 16 * tw + c;
+            if (gi < GI)
+                for (int tb = (tw & ~1) + gi; tb < NB; tb += GI) {     // P's transpose, sixteen of its rows to a wave
+                    f32x4 x = zero4();
+                    if (tb >= tw) {
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sQ, LK, 16 * tb, 32 * ks, lane), rows_op(sK, LK, 16 * tw, 32 * ks, lane), x);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int t = 16 * tb + 4 * q + i;
+                            x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
+                        }
+                    }
+                    Pt.put4(s, 16 * tb + 4 * q, x);
+                }
+        }
+        f32x4 y[NB][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) y[b][g] = of_k ? splat4(before) * tile_of(sK, LK, 16 * b, col + 16 * g, lane) : zero4();
+        if (!first)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                read_afresh();
+                const Op<E, 2> x0 = operand<E, 2>(X[2 * ks][0], X[2 * ks + 1][0]), x1 = operand<E, 2>(X[2 * ks][1], X[2 * ks + 1][1]);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const Op<E, 1> k = rows_op(sK, LK, 16 * b, 32 * ks, lane);
+                    y[b][0] = mma(k, x0, y[b][0]);
+                    y[b][1] = mma(k, x1, y[b][1]);
+                }
+            }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const f32x4 d = *(const f32x4*)(st.down + 16 * b + 4 * q);
+            y[b][0] *= d;
+            y[b][1] *= d;
+        }
+        __syncthreads();
+        if (!of_k)
+#pragma unroll
+            for (int ks = 0; ks < KC; ++ks) {
+                const Op<E, 1> o0 = cols_op(sO, LV, 32 * ks, col, lane), o1 = cols_op(sO, LV, 32 * ks, col + 16, lane);
+#pragma unroll
+                for (int b = 0; b <= 2 * ks + 1; ++b) {
+                    const Op<E, 1> m = Pt.rows(16 * b, 32 * ks, lane);
+                    y[b][0] = mma(m, o0, y[b][0]);
+                    y[b][1] = mma(m, o1, y[b][1]);
+                }
+            }
+        Op<E, 2> yo[KC][2];
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) yo[ks][g] = operand<E, 2>(y[2 * ks][g], y[2 * ks + 1][g]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            y[b][0] = y[b][1] = zero4();
+#pragma unroll
+            for (int ks = b / 2; ks < KC; ++ks) {
+                const Op<E, 1> m = T.cols(32 * ks, 16 * b, lane);
+                y[b][0] = mma(m, yo[ks][0], y[b][0]);
+                y[b][1] = mma(m, yo[ks][1], y[b][1]);
+            }
+            const f32x4 f = *(const f32x4*)(st.bu + 16 * b + 4 * q);
+            y[b][0] *= f;
+            y[b][1] *= f;
+        }
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) yo[ks][g] = operand<E, 2>(y[2 * ks][g], y[2 * ks + 1][g]);
+        const float whole = st.whole;
+#pragma unroll
+        for (int d = 0; d < DK / 16; ++d) {
+            if (d % 2 == 0) read_afresh();
+            X[d][0] *= splat4(whole);
+            X[d][1] *= splat4(whole);
+#pragma unroll
+            for (int ks = 0; ks < KC; ++ks) {
+                const Op<E, 1> k = cols_op(sK, LK, 32 * ks, 16 * d, lane);
+                X[d][0] = mma(k, yo[ks][0], X[d][0]);
+                X[d][1] = mma(k, yo[ks][1], X[d][1]);
+            }
+        }
+        if (!of_k) {
+            Op<E, 2> qo[KC][2];
+#pragma unroll
+            for (int ks = 0; ks < KC; ++ks)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) qo[ks][g] = scaled<E, 2>(cols_op(sO, LV, 32 * ks, col + 16 * g, lane), st.up, 32 * ks, lane, a.scale);
+#pragma unroll
+            for (int d = 0; d < DK / 16; ++d) {
+                if (d % 2 == 0) read_afresh();
+#pragma unroll
+                for (int ks = 0; ks < KC; ++ks) {
+                    const Op<E, 1> k = cols_op(sQ, LK, 32 * ks, 16 * d, lane);
+                    X[d][0] = mma(k, qo[ks][0], X[d][0]);
+                    X[d][1] = mma(k, qo[ks][1], X[d][1]);
+                }
+            }
+        }
+        before *= whole;
+    }
+    if (of_k) {
+        // as it is read, the columns of X down the rows of a tile: by products with the identity
+        const int q = lane0 >> 4, c = lane0 & 15;
+#pragma unroll
+        for (int n = 0; n < DK / 16; n += 2) {
+            const Op<E, 2> x0 = operand<E, 2>(X[n][0], X[n + 1][0]), x1 = operand<E, 2>(X[n][1], X[n + 1][1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f32x4 lo = zero4(), hi = zero4();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) lo[j] = 4 * q + j == c ? 1.f : 0.f;
+                const Op<E, 1> one = i == 0 ? operand<E, 1>(lo, hi) : operand<E, 1>(hi, lo);
+                store_op<E, 1>((E*)a.N + (at * (DK / 16 * KS) + (n + i) * KS + w) * 512, operand<E, 1>(mma(x0, one, zero4()), mma(x1, one, zero4())), lane0);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int d = 0; d < DK / 16; ++d)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) *(f32x4*)(a.Z + at * (DK * DV) + (size_t)((col / 16 + g) * (DK / 16) + d) * 256 + 4 * lane0) = X[d][g];
+    }
+    if (tid0 == 0) a.whole[at] = before;
+}
+
 __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) { return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3]))); }
 template <typename E> __device__ __forceinline__ f32x4 wide4(const E* p) { return __builtin_convertvector(*(const Vec4<E>*)p, f32x4); }
 // over the four lanes that have a column of a tile
@@ -134,10 +316,11 @@ __device__ __forceinline__ float column_sum(float x)
     x += __shfl_xor(x, 16);
     return x + __shfl_xor(x, 32);
 }
-// A workgroup has a chunk and a key head, and goes over that one's value heads: the sums of dQ and dK over them stay in registers.  Sixteen value
+// A workgroup has a chunk and a key head, and goes over that one's value heads: the sums of dQ and dK over them stay in registers.  RUN: a run of chunks
+// and a head, from the last chunk to the first with the gradient of the state behind each in registers, sixteen value columns to a wave.  Sixteen value
 // columns to a wave for U and dR; then sixteen tokens, as queries and as keys, and a part of the key columns.  X and Y are worked out twice, by the wave
 // of the query's tokens and by that of the key's: as the operands of its own products they then lie in a wave's registers as they are.
-template <typename E, int DK, int DV>
+template <typename E, int DK, int DV, bool RUN>
 __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, VS = DV / 32, LK = DK + kPad<E>, LV = DV + kPad<E>;
@@ -149,7 +332,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
     __shared__ float s_db[NW][C], s_db2[GI][C], s_dg[GI][C], s_kc[NW], s_ss[NW];
     E *const sS0 = SHARED ? sP : sS, *const sdS = SHARED ? sT : sS + DV * LS;
     const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6), tw = w % NB, gi = w / NB;
-    const int place = blockIdx.x / a.Hk, hk = blockIdx.x - place * a.Hk, share = a.H / a.Hk;
+    const int place = blockIdx.x / a.Hk, hk = blockIdx.x - place * a.Hk, share = RUN ? 1 : a.H / a.Hk;
     if (place >= a.places) {
         const int b = blockIdx.x - a.places * a.Hk;
         clear_rows(a.rows, b, (E*)a.dQ, a.Hk * DK);
@@ -159,30 +342,52 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         clear_rows(a.rows, b, (E*)a.dbeta, a.H);
         return;
     }
-    const Chunk ch = chunk_at(a.rows, C, place, lane0);
-    if (ch.n <= 0) return;
-    constexpr bool AHEAD = DV == 128;                           // (two workgroups to a compute unit have no registers for the next head)
+    const Chunk run = chunk_at(a.rows, C * a.run, place, lane0);
+    if (run.n <= 0) return;
+    const int chunk0 = chunk_place(a.rows, C, run, a.run, 0), n_chunks = RUN ? (run.n + C - 1) / C : 1;
+    Chunk ch = run;
+    // What the next head needs, or (NEXT) the next chunk, on its way during this one, where there are registers for it: 12 heads of 64, 16 sequences of
+    // 2048 tokens, the gradient 332 us without, 324 with; 16 heads of 64 and 128, 8 of 2048, 415 and 422; of 128 and 128, 1083 and 1105.
+    constexpr bool AHEAD = DV == 128, NEXT = RUN && DK + DV == 128;
     Tile<E, C, DV, NT> tv, to;
     Tile<E, C, C, NT> tt;
     Steps ts;
     Op<E, 1> so[KS], bo[KS];                                    // the states' operands, of the wave's value columns
-    auto fetch = [&](int h, int tid, int lane) {
-        const size_t at = (size_t)place * a.H + h;
-        ts = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, lane);
-        tv.fetch((const E*)a.V + h * DV, a.ldv, ch.row, ch.n, tid);
-        to.fetch((const E*)a.dO + h * DV, a.lddo, ch.row, ch.n, tid);
+    auto fetch = [&](int h, int chunk, int row, int n, int tid, int lane) {
+        const size_t at = (size_t)chunk * a.H + h;
+        ts = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, row, h, n, lane);
+        tv.fetch((const E*)a.V + h * DV, a.ldv, row, n, tid);
+        to.fetch((const E*)a.dO + h * DV, a.lddo, row, n, tid);
         tt.fetch((const E*)a.T + at * (C * C), C, 0, C, tid);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            so[ks] = load_op<E, 1>((const E*)a.S0 + at * (DK * DV) + (w * KS + ks) * 512, lane);
-            bo[ks] = load_op<E, 1>((const E*)a.dS + at * (DK * DV) + (w * KS + ks) * 512, lane);
+            so[ks] = load_op<E, 1>((const E*)a.S0c + at * (DK * DV) + (w * KS + ks) * 512, lane);
+            if (!RUN) bo[ks] = load_op<E, 1>((const E*)a.dS + at * (DK * DV) + (w * KS + ks) * 512, lane);
         }
     };
+    f32x4 B[RUN ? DK / 16 : 1];
+    if (RUN) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            bo[ks] = load_op<E, 1>((const E*)a.dS + ((size_t)place * a.H + hk) * (DK * DV) + (w * KS + ks) * 512, lane0);
+            f32x8 v;
+            if constexpr (sizeof(E) == 4) v = bo[ks].v;
+            else v = __builtin_convertvector(bo[ks].h, f32x8);
+            B[2 * ks] = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+            B[2 * ks + 1] = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+        }
+    }
+    for (int rc = n_chunks - 1; rc >= 0; --rc) {
+    if (RUN) {
+        if (rc < n_chunks - 1) __syncthreads();
+        ch.row = run.row + rc * C;
+        ch.n = min(C, run.n - rc * C);
+    }
     {
         Tile<E, C, DK, NT> ty, tk;
         ty.fetch((const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid0);
         tk.fetch((const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid0);
-        if (AHEAD) fetch(hk * share, tid0, lane0);
+        if (AHEAD) fetch(hk * share, chunk0 + rc, ch.row, ch.n, tid0, lane0);
         ty.put(sQ, LK, ch.n, tid0);
         tk.put(sK, LK, ch.n, tid0);
     }
@@ -195,7 +400,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         int lane = lane0;
         asm volatile("" : "+v"(lane));             // (addresses are worked out where they are used: kept over the heads, they fill the registers)
         const int tid = 64 * w + lane, q = lane >> 4, c = lane & 15, t = 16 * tw + c;
-        if (!AHEAD) fetch(h, tid, lane);
+        if (NEXT ? rc == n_chunks - 1 : !AHEAD) fetch(h, chunk0 + rc, ch.row, ch.n, tid, lane);
         if (hh > 0) __syncthreads();
         put_steps(st, ts, ch.n, tid);
         tv.put(sV, LV, ch.n, tid);
@@ -297,7 +502,8 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
             }
         };
         put(0);
-        if (AHEAD && DK == 64 && hh + 1 < share) fetch(h + 1, tid, lane);
+        if (AHEAD && DK == 64 && hh + 1 < share) fetch(h + 1, chunk0, ch.row, ch.n, tid, lane);
+        if (NEXT && rc > 0) fetch(h, chunk0 + rc - 1, ch.row - C, C, tid, lane);
         // X and beta Y of the wave's tokens as queries, then as keys
         float dbeta = 0.f, dgamma = 0.f, kc = 0.f;
         Op<E, 1> xq[KC], yq[KC], xk[KC], yk[KC];
@@ -372,7 +578,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
             if (half > 0) {
                 __syncthreads();
                 put(half);
-                if (AHEAD && half + 1 == DK / 64 && hh + 1 < share) fetch(h + 1, tid, lane);
+                if (AHEAD && half + 1 == DK / 64 && hh + 1 < share) fetch(h + 1, chunk0, ch.row, ch.n, tid, lane);
             }
             __syncthreads();
 #pragma unroll
@@ -443,6 +649,29 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
             if (a.g != nullptr && tid < ch.n) ((E*)a.dg)[(size_t)(ch.row + tid) * a.H + h] = from_f<E>(x);
         }
     }
+    if (RUN && rc > 0) {
+        // the gradient of the state in front: dS <- e^gamma dS + scale (e^gamma Q)^T dO - (beta e^gamma K)^T dR
+        int lane = lane0;
+        asm volatile("" : "+v"(lane));
+        Op<E, 2> qo[KC], ro[KC];
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) {
+            qo[ks] = scaled<E, 2>(cols_op(sO, LV, 32 * ks, 16 * w, lane), st.up, 32 * ks, lane, a.scale);
+            ro[ks] = scaled<E, 2>(cols_op(sV, LV, 32 * ks, 16 * w, lane), st.bu, 32 * ks, lane);
+        }
+#pragma unroll
+        for (int d = 0; d < DK / 16; ++d) {
+            if (d % 2 == 0) read_afresh();
+            B[d] *= splat4(st.whole);
+#pragma unroll
+            for (int ks = 0; ks < KC; ++ks) {
+                B[d] = mma(cols_op(sQ, LK, 32 * ks, 16 * d, lane), qo[ks], B[d]);
+                B[d] = mma(cols_op(sK, LK, 32 * ks, 16 * d, lane), ro[ks], B[d]);
+            }
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) bo[ks] = operand<E, 1>(B[2 * ks], B[2 * ks + 1]);
+    }
     const int q = lane0 >> 4, t = 16 * tw + (lane0 & 15);
     if (t < ch.n) {
         E* dq = (E*)a.dQ + (size_t)(ch.row + t) * (a.Hk * DK) + hk * DK + 4 * q;
@@ -454,6 +683,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
             *(Vec4<E>*)(dk + col) = __builtin_convertvector(sumK[i], Vec4<E>);
         }
     }
+    }
 }
 
 // -------------------------------------------------------------------------------------------------------------------- host
@@ -461,23 +691,27 @@ hipError_t launch_delta_bwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* sav
 {
     ProfScope prof(KID_DELTA_BWD, st);
     hipError_t e = hipSuccess;
+    if (!has_saved) saved = ws + p.saved_at;
+    a.t_parts = p.t_parts;
+    a.N = ws + p.N;
+    a.Z = (float*)(ws + p.Z);
+    a.whole = (float*)(ws + p.whole);
+    a.T = saved + p.T;
+    a.S0 = a.S0c = saved + p.S0c;
     if (!has_saved) {
-        if ((e = launch_delta_states(a, p, ws, nullptr, dk, dv, dtype, st)) != hipSuccess) return e;
-    } else {
-        a.places = p.places;
-        a.run = p.run;
-        a.N = ws + p.N;
-        a.Z = (float*)(ws + p.Z);
-        a.T = saved + p.T;
-        a.S0 = saved + p.S0;
-        a.whole = (float*)(saved + p.whole);
+        a.places = p.chunks;
+        a.run = 1;
+        if ((e = launch_delta_states(a, p, dk, dv, dtype, st)) != hipSuccess) return e;
     }
+    a.places = p.places;
+    a.run = p.run;
     a.dS = ws + p.dS;
     if (p.places > 0) {
         const dim3 grid((unsigned)((size_t)p.places * a.H));
 #define CHELA_RUN(E, DK, DV)                                                                                          \
     do {                                                                                                              \
-        if (sizeof(E) == 2 && p.parts == 2) hipLaunchKernelGGL((delta_bwd_prep_kernel<E, DK, DV, 3 - sizeof(E) / 2>), grid, dim3(256), 0, st, a); \
+        if (p.run > 1) hipLaunchKernelGGL((delta_bwd_prep_run_kernel<E, DK, DV>), grid, dim3((DK + DV) * 2), 0, st, a); \
+        else if (sizeof(E) == 2 && p.parts == 2) hipLaunchKernelGGL((delta_bwd_prep_kernel<E, DK, DV, 3 - sizeof(E) / 2>), grid, dim3(256), 0, st, a); \
         else hipLaunchKernelGGL((delta_bwd_prep_kernel<E, DK, DV, 1>), grid, dim3(256), 0, st, a);                    \
     } while (0)
         CHELA_DELTA(CHELA_RUN)
@@ -489,7 +723,11 @@ hipError_t launch_delta_bwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* sav
     const size_t blocks = (size_t)p.places * a.Hk + (clear ? (a.rows.T + 63) / 64 : 0);
     if (blocks == 0) return hipSuccess;
     const dim3 grid((unsigned)blocks);
-#define CHELA_RUN(E, DK, DV) hipLaunchKernelGGL((delta_grad_kernel<E, DK, DV>), grid, dim3(DV * 4), 0, st, a)
+#define CHELA_RUN(E, DK, DV)                                                                                          \
+    do {                                                                                                              \
+        if (p.run > 1) hipLaunchKernelGGL((delta_grad_kernel<E, DK, DV, true>), grid, dim3(DV * 4), 0, st, a);        \
+        else hipLaunchKernelGGL((delta_grad_kernel<E, DK, DV, false>), grid, dim3(DV * 4), 0, st, a);                 \
+    } while (0)
     CHELA_DELTA(CHELA_RUN)
 #undef CHELA_RUN
     return hipGetLastError();

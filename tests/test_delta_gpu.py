@@ -164,6 +164,35 @@ def test_many_chunks(dtype, dk, dv):
     check_all(dict(got, O=out.flatten(0, 1), S_out=S_out, dS_in=grads[5]), x, S, dS, [L, L], 0.1, dtype, bounds=False)
 
 
+RUNS = [  # lengths long enough for runs of several chunks; sequences whose last run is short or ends inside a chunk, that have less than one run
+    (1, 1, 64, 64, [1100]),
+    (2, 2, 64, 128, [1400, 3]),
+    (2, 1, 128, 64, [577, 1090, 0, 1029]),
+    (1, 1, 128, 128, [2305]),
+    (2, 2, 64, 64, [4200, 5]),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("states", [False, True])
+@pytest.mark.parametrize("H,Hk,dk,dv,lens", RUNS)
+def test_runs_of_chunks(dtype, states, H, Hk, dk, dv, lens):
+    # nothing kept, kept for a gradient, a gradient that has nothing kept; decays that keep a state over many chunks
+    r, T, n = gen(dk + dv + len(lens)), sum(lens), len(lens)
+    x = inputs(r, T, H, Hk, dk, dv, dtype, decay=5.0)
+    S, dS = (0.3 * r(n, H, dk, dv), 0.3 * r(n, H, dk, dv)) if states else (None, None)
+    kw = dict(scale=0.1, cu=cu_of(lens), S_in=S)
+    S_out = torch.empty(n, H, dk, dv, device="cuda") if states else None
+    O0, _ = binding.chela_gated_delta_fwd(*x[:5], S_out=S_out, **kw)
+    check_all(dict(O=O0, S_out=S_out), x, S, dS, lens, 0.1, dtype, bounds=False)
+    O1, saved = binding.chela_gated_delta_fwd(*x[:5], S_out=S_out, want_saved=True, **kw)
+    grads = binding.chela_gated_delta_bwd(*x[:5], x[5], dS_out=dS, want_dS_in=states, saved=saved, **kw)
+    again = binding.chela_gated_delta_bwd(*x[:5], x[5], dS_out=dS, want_dS_in=states, **kw)
+    names = ("dQ", "dK", "dV", "dg", "dbeta", "dS_in")
+    check_all(dict(zip(names, grads), O=O1, S_out=S_out), x, S, dS, lens, 0.1, dtype, bounds=False)
+    check_all(dict(zip(names, again)), x, S, dS, lens, 0.1, dtype, bounds=False)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_in_place_states_pieces_and_single_tokens(dtype):
     r, H, Hk, dk, dv, n, L = gen(5), 4, 2, 64, 64, 3, 150
@@ -276,6 +305,27 @@ def test_many_sequences(n):
         check_all(got, one, S[i:i + 1], None, [lens[i]], 1.0, F32)
     empty = torch.tensor([m == 0 for m in lens], device="cuda")
     assert torch.equal(S_out[empty], S[empty])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cu", [[0, 900, 300, 1200, 700, 1500], [1500, 0, 1500, 0], [-70, 400, 399, 2000, 2000, 0, 1 << 30]])
+def test_offsets_out_of_order_stay_inside(dtype, cu):
+    # what they give is not specified; nothing in front of or behind the tensors is touched, and calls behind these are right
+    r, T, H, n, pad = gen(3), 1500, 2, len(cu) - 1, 4096
+    x = inputs(r, T, H, H, 64, 64, dtype)
+    cu = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    S = 0.1 * r(n, H, 64, 64)
+    room = torch.full((T * H * 64 + 2 * pad,), 7.0, dtype=dtype, device="cuda")
+    O = room[pad:-pad].view(T, H, 64)
+    for states in (False, True):
+        kw = dict(cu=cu, S_in=S if states else None)
+        _, saved = binding.chela_gated_delta_fwd(*x[:5], S_out=torch.empty_like(S) if states else None, want_saved=True, O=O, **kw)
+        binding.chela_gated_delta_fwd(*x[:5], O=O, **kw)
+        binding.chela_gated_delta_bwd(*x, saved=saved, **kw)
+        binding.chela_gated_delta_bwd(*x, **kw)
+    assert (room[:pad] == 7).all() and (room[-pad:] == 7).all()
+    out, _ = binding.chela_gated_delta_fwd(*x[:5], cu=cu_of([T]))
+    check_all(dict(O=out), x, None, None, [T], 1.0, dtype, bounds=False)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)

@@ -244,9 +244,9 @@ def test_workspace_and_saved_queries(L):
                 (1 << 27, 1, 0, 16, 64, 64, 0)):
         assert saved(*bad) == 0, bad
         assert ws(*bad, 0, 0) == 0 and ws(*bad, 1, 1) == 0, bad
-    # per chunk and head: the inverse in two parts and the state in bf16, e^gamma; the transition in two parts and the state's part in fp32
-    assert saved(128, 1, 0, 1, 64, 64, 0) == 2 * (2 * 64 * 64 * 2 + 64 * 64 * 2) + 256
-    assert ws(128, 1, 0, 1, 64, 64, 0, 0, 1) == 2 * (2 * 64 * 64 * 2 + 64 * 64 * 4)
+    # per chunk and head: the inverse and the state in bf16; the transition in two parts, the state's part in fp32, e^gamma
+    assert saved(128, 1, 0, 1, 64, 64, 0) == 2 * (64 * 64 * 2 + 64 * 64 * 2)
+    assert ws(128, 1, 0, 1, 64, 64, 0, 0, 1) == 2 * (2 * 64 * 64 * 2 + 64 * 64 * 4) + 256
     assert ws(128, 1, 0, 1, 64, 64, 0, 0, 0) == ws(128, 1, 0, 1, 64, 64, 0, 0, 1) + saved(128, 1, 0, 1, 64, 64, 0)
     assert saved(128, 4, 1, 2, 64, 128, 1) > saved(128, 1, 1, 2, 64, 128, 1) > saved(128, 1, 0, 2, 64, 128, 1) > 0
     assert ws(128, 1, 0, 1, 64, 64, 0, 1, 1) > ws(128, 1, 0, 1, 64, 64, 0, 0, 1)
