@@ -646,7 +646,9 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                 const float y1 = __shfl_down(x, d);
                 if (tid + d < 64) x += y1;
             }
-            if (a.g != nullptr && tid < ch.n) ((E*)a.dg)[(size_t)(ch.row + tid) * a.H + h] = from_f<E>(x);
+            // (nothing is in front of a sequence's first token that it could let decay: its sum is the roundings' rest)
+            const bool none = tid == 0 && rc == 0 && run.index == 0 && a.S_in == nullptr;
+            if (a.g != nullptr && tid < ch.n) ((E*)a.dg)[(size_t)(ch.row + tid) * a.H + h] = from_f<E>(none ? 0.f : x);
         }
     }
     if (RUN && rc > 0) {

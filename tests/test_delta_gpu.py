@@ -194,6 +194,16 @@ def test_runs_of_chunks(dtype, states, H, Hk, dk, dv, lens):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lens", [[1] * 10, [1100, 3, 0, 64, 1]])
+def test_a_first_token_lets_nothing_decay(dtype, lens):
+    r, T, H = gen(8), sum(lens), 2
+    x = inputs(r, T, H, H, 64, 64, dtype)
+    dg = binding.chela_gated_delta_bwd(*x, cu=cu_of(lens))[3]
+    starts = torch.tensor([a for a, n in zip(offsets(lens), lens) if n], device="cuda")
+    assert (dg[starts] == 0).all() and (T == len(starts) or (dg != 0).sum() >= (T - len(starts)) * H // 2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_in_place_states_pieces_and_single_tokens(dtype):
     r, H, Hk, dk, dv, n, L = gen(5), 4, 2, 64, 64, 3, 150
     x = inputs(r, n * L, H, Hk, dk, dv, dtype)
