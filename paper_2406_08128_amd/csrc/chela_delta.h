@@ -9,12 +9,13 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef __attribute__((ext_vector_type(4))) bf16 bf16x4;
 typedef __attribute__((ext_vector_type(8))) bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
 // Tokens of a chunk.  (fp32: a chunk's rows take twice the room in LDS.)
 template <typename E> struct DeltaChunk { static constexpr int C = sizeof(E) == 2 ? kDeltaChunkBf16 : kDeltaChunkF32; };
-// Elements behind each row of a tile in LDS: 16 rows' pieces of 8 (bf16) or 16 (fp32) bytes then fall on all banks alike.
+// Elements behind each row of a tile in LDS: 16 rows' pieces of 16 bytes then fall on all banks alike.
 template <typename E> constexpr int kPad = sizeof(E) == 2 ? 8 : 4;
 
 // A 16 x 32 operand.  All products are 16 x 16 tiles over 32 terms, D[m][n] += sum_k A[m][k] B[n][k]: lane 16 q + c has row c of A (of B)
@@ -72,13 +73,28 @@ __device__ __forceinline__ Op<E, 1> first_part(const Op<E, 2>& x)
 template <typename E> using Vec4 = typename std::conditional<sizeof(E) == 2, bf16x4, f32x4>::type;
 template <typename E> using Vec8 = typename std::conditional<sizeof(E) == 2, bf16x8, f32x8>::type;
 
+// Where column `col` of a tile lies in its row in LDS.  bf16: within 32 columns the two fours that a lane's eight k are come one behind the other, so that
+// it reads them at once: 16 bytes of 64 lanes take 8 cycles (6 with 32 bytes behind each row), two times 8 bytes 16.
+template <typename E>
+__device__ __forceinline__ constexpr int place_of(int col)
+{
+    return sizeof(E) == 4 ? col : (col & ~31) | (col & 12) * 2 | (col & 16) / 4 | (col & 3);
+}
+// Four columns beginning with col0 + 4 q, col0 a multiple of 16.
+template <typename E>
+__device__ __forceinline__ int four_of(int col0, int q) { return sizeof(E) == 4 ? col0 + 4 * q : (col0 & ~31) + (col0 & 16) / 4 + 8 * q; }
+
 // The operand that is X[row0 + c][k0 ..], rows of a tile, summed over its columns.
 template <typename E>
 __device__ __forceinline__ Op<E, 1> rows_op(const E* X, int ld, int row0, int k0, int lane)
 {
-    const E* p = X + (row0 + (lane & 15)) * ld + k0 + 4 * (lane >> 4);
-    const Vec4<E> a = *(const Vec4<E>*)p, b = *(const Vec4<E>*)(p + 16);
-    return Op<E, 1>{__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
+    if constexpr (sizeof(E) == 2) {
+        return Op<E, 1>{*(const bf16x8*)(X + (row0 + (lane & 15)) * ld + k0 + 8 * (lane >> 4))};
+    } else {
+        const E* p = X + (row0 + (lane & 15)) * ld + k0 + 4 * (lane >> 4);
+        const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 16);
+        return Op<E, 1>{__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
+    }
 }
 // The operand that is X[k0 ..][col0 + c], columns of a tile, summed over its rows.  bf16: within 16 lanes the transposing read hands lane p
 // the column p of a 4 x 16 block whose rows the lanes address as p / 4, and 8-byte pieces as p % 4.
@@ -87,7 +103,7 @@ __device__ __forceinline__ Op<E, 1> cols_op(const E* X, int ld, int k0, int col0
 {
     const int q = lane >> 4, c = lane & 15;
     if constexpr (sizeof(E) == 2) {
-        const bf16* p = X + (k0 + 4 * q + (c >> 2)) * ld + col0 + 4 * (c & 3);
+        const bf16* p = X + (k0 + 4 * q + (c >> 2)) * ld + four_of<E>(col0, c & 3);
         const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
         const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 16 * ld));
         return Op<E, 1>{__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
@@ -107,22 +123,24 @@ struct Planes {
     int ld, plane;                             // (plane: elements from the first parts to the second)
     __device__ __forceinline__ void put(int row, int col, float x) const
     {
+        E* p = h + row * ld + place_of<E>(col);
         if constexpr (sizeof(E) == 4) {
-            h[row * ld + col] = x;
+            *p = x;
         } else {
             const bf16 a = (bf16)x;
-            h[row * ld + col] = a;
-            if constexpr (P == 2) h[plane + row * ld + col] = (bf16)(x - (float)a);
+            *p = a;
+            if constexpr (P == 2) p[plane] = (bf16)(x - (float)a);
         }
     }
-    __device__ __forceinline__ void put4(int row, int col, f32x4 x) const          // col, col + 1, ...
+    __device__ __forceinline__ void put4(int row, int col0, int q, f32x4 x) const          // columns col0 + 4 q ..
     {
+        E* p = h + row * ld + four_of<E>(col0, q);
         if constexpr (sizeof(E) == 4) {
-            *(f32x4*)(h + row * ld + col) = x;
+            *(f32x4*)p = x;
         } else {
             const bf16x4 a = __builtin_convertvector(x, bf16x4);
-            *(bf16x4*)(h + row * ld + col) = a;
-            if constexpr (P == 2) *(bf16x4*)(h + plane + row * ld + col) = __builtin_convertvector(x - __builtin_convertvector(a, f32x4), bf16x4);
+            *(bf16x4*)p = a;
+            if constexpr (P == 2) *(bf16x4*)(p + plane) = __builtin_convertvector(x - __builtin_convertvector(a, f32x4), bf16x4);
         }
     }
     __device__ __forceinline__ Op<E, P> rows(int row0, int k0, int lane) const
@@ -259,7 +277,7 @@ __device__ __forceinline__ f32x4 tile_of(const E* X, int ld, int row0, int col0,
 {
     const int q = lane >> 4, c = lane & 15;
     if constexpr (sizeof(E) == 2) {
-        return __builtin_convertvector(__builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(X + (row0 + 4 * q + (c >> 2)) * ld + col0 + 4 * (c & 3))), f32x4);
+        return __builtin_convertvector(__builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(X + (row0 + 4 * q + (c >> 2)) * ld + four_of<E>(col0, c & 3))), f32x4);
     } else {
         const float* p = X + (row0 + 4 * q) * ld + col0 + c;
         return f32x4{p[0], p[ld], p[2 * ld], p[3 * ld]};
@@ -324,13 +342,22 @@ struct Tile {
             x[m] = ((const Loose*)(from + (size_t)(row + min(t, n - 1)) * ld + k))->p;
         }
     }
+    // (AS_IS: what was written as it lay in LDS)
+    template <bool AS_IS = false>
     __device__ __forceinline__ void put(E* to, int ldt, int n, int tid) const
     {
 #pragma unroll
         for (int m = 0; m < M; ++m) {
             const int i = m * NT + tid, t = i / (D / W), k = i % (D / W) * W;
             if (ALL % NT != 0 && i >= ALL) break;
-            *(u32x4*)(to + t * ldt + k) = t < n ? x[m] : u32x4{0, 0, 0, 0};
+            const u32x4 v = t < n ? x[m] : u32x4{0, 0, 0, 0};
+            if constexpr (AS_IS || sizeof(E) == 4) {
+                *(u32x4*)(to + t * ldt + k) = v;
+            } else {
+                E* p = to + t * ldt + place_of<E>(k);
+                *(u32x2*)p = u32x2{v[0], v[1]};
+                *(u32x2*)(p + 8) = u32x2{v[2], v[3]};
+            }
         }
     }
 };

@@ -169,7 +169,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
         put_steps(st, ts, n, tid);
         tk.put(sK, LK, n, tid);
         tv.put(sV, LV, n, tid);
-        tt.put(sT, LT, P * C, tid);
+        tt.template put<true>(sT, LT, P * C, tid);
         if (!last) fetch(r + 1, tid, lane);
         __syncthreads();
         const float* f = of_k ? st.bu : st.beta;          // (W and X are kept with their signs changed)
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
         tk.put(sK, LK, n, tid);
         tq.put(sQ, LK, n, tid);
         tv.put(sV, LV, n, tid);
-        tt.put(sT, LT, C, tid);
+        tt.template put<true>(sT, LT, C, tid);
         if (AHEAD && !last) fetch(r + 1, tid, lane);
         __syncthreads();
         if (a.S0c != nullptr)
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
                         x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
                     }
                 }
-                Pm.put4(t, 16 * sb + 4 * q, x);
+                Pm.put4(t, 16 * sb, q, x);
             }
         }
         Op<E, 2> ro[KC], uo[KC];

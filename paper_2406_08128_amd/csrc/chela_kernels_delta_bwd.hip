@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
         y.put(sQ, LK, ch.n, tid);
         k.put(sK, LK, ch.n, tid);
         o.put(sO, LV, ch.n, tid);
-        if (P == 1) m.put(sT, LT, C, tid);
+        if (P == 1) m.template put<true>(sT, LT, C, tid);
     }
     __syncthreads();
     if (tid == 0) a.whole[at] = st.whole;
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
                     x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
                 }
             }
-            Pt.put4(s, 16 * tb + 4 * q, x);
+            Pt.put4(s, 16 * tb, q, x);
         }
     }
     if (tid < C) s_qu[tid] = a.scale * st.up[tid];
@@ -174,7 +174,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
         tq.put(sQ, LK, n, tid);
         tk.put(sK, LK, n, tid);
         to.put(sO, LV, n, tid);
-        tt.put(sT, LT, C, tid);
+        tt.template put<true>(sT, LT, C, tid);
         if (r > 0) fetch(r - 1, tid, lane);
         __syncthreads();
         {
@@ -192,7 +192,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
                             x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
                         }
                     }
-                    Pt.put4(s, 16 * tb + 4 * q, x);
+                    Pt.put4(s, 16 * tb, q, x);
                 }
         }
         f32x4 y[NB][2];
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         put_steps(st, ts, ch.n, tid);
         tv.put(sV, LV, ch.n, tid);
         to.put(sO, LV, ch.n, tid);
-        tt.put(sT, LT, C, tid);
+        tt.template put<true>(sT, LT, C, tid);
         __syncthreads();
         // P's transpose, sixteen of its rows to a wave
         for (int tb = (tw & ~1) + gi; tb < NB; tb += GI) {
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                     x[i] = t <= u ? a.scale * st.decay(u, t) * x[i] : 0.f;
                 }
             }
-            Pm.put4(t, 16 * tb + 4 * q, x);
+            Pm.put4(t, 16 * tb, q, x);
         }
         // U and dR, sixteen value columns to a wave
         float ss = 0.f;
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
             f32x4 u = zero4();
 #pragma unroll
             for (int ks = 0; ks <= b / 2; ++ks) u = mma(ro[ks], Tm.rows(16 * b, 32 * ks, lane), u);
-            Um.put4(16 * b + c, 16 * w + 4 * q, u);
+            Um.put4(16 * b + c, 16 * w, q, u);
         }
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) ss += __shfl_xor(ss, d);
@@ -473,9 +473,9 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
             f32x4 r = zero4();
 #pragma unroll
             for (int ks = b / 2; ks < KC; ++ks) r = mma(ro[ks], Tm.cols(32 * ks, 16 * b, lane), r);
-            const float db = column_sum(dot4(r, wide4(sV + r0 * LV + 16 * w + 4 * q)));
+            const float db = column_sum(dot4(r, wide4(sV + r0 * LV + four_of<E>(16 * w, q))));
             if (q == 0) s_db[w][r0] = db;
-            Rm.put4(r0, 16 * w + 4 * q, r);                            // (dR where the value was: no other lane reads that one)
+            Rm.put4(r0, 16 * w, q, r);                            // (dR where the value was: no other lane reads that one)
             if (r0 < ch.n)
                 *(Vec4<E>*)((E*)a.dV + (size_t)(ch.row + r0) * (a.H * DV) + h * DV + 16 * w + 4 * q) =
                     __builtin_convertvector(r * splat4(st.beta[r0]), Vec4<E>);
@@ -485,19 +485,16 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         auto put = [&](int half) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int at = (16 * w + c) * LS + 32 * i + 4 * q;
+                E *const p = sS0 + (16 * w + c) * LS + 32 * i, *const r = sdS + (16 * w + c) * LS + 32 * i;
                 if constexpr (sizeof(E) == 4) {
                     const f32x8 s = so[2 * half + i].v, b = bo[2 * half + i].v;
-                    *(f32x4*)(sS0 + at) = __builtin_shufflevector(s, s, 0, 1, 2, 3);
-                    *(f32x4*)(sS0 + at + 16) = __builtin_shufflevector(s, s, 4, 5, 6, 7);
-                    *(f32x4*)(sdS + at) = __builtin_shufflevector(b, b, 0, 1, 2, 3);
-                    *(f32x4*)(sdS + at + 16) = __builtin_shufflevector(b, b, 4, 5, 6, 7);
+                    *(f32x4*)(p + 4 * q) = __builtin_shufflevector(s, s, 0, 1, 2, 3);
+                    *(f32x4*)(p + 16 + 4 * q) = __builtin_shufflevector(s, s, 4, 5, 6, 7);
+                    *(f32x4*)(r + 4 * q) = __builtin_shufflevector(b, b, 0, 1, 2, 3);
+                    *(f32x4*)(r + 16 + 4 * q) = __builtin_shufflevector(b, b, 4, 5, 6, 7);
                 } else {
-                    const bf16x8 s = so[2 * half + i].h, b = bo[2 * half + i].h;
-                    *(bf16x4*)(sS0 + at) = __builtin_shufflevector(s, s, 0, 1, 2, 3);
-                    *(bf16x4*)(sS0 + at + 16) = __builtin_shufflevector(s, s, 4, 5, 6, 7);
-                    *(bf16x4*)(sdS + at) = __builtin_shufflevector(b, b, 0, 1, 2, 3);
-                    *(bf16x4*)(sdS + at + 16) = __builtin_shufflevector(b, b, 4, 5, 6, 7);
+                    *(bf16x8*)(p + 8 * q) = so[2 * half + i].h;
+                    *(bf16x8*)(r + 8 * q) = bo[2 * half + i].h;
                 }
             }
         };
@@ -593,7 +590,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                     yy = mma(s, rows_op(sV, LV, 16 * tw, 32 * ks, lane), yy);
                     zz = mma(cols_op(sdS, LS, 32 * ks, 16 * n, lane), rows_op(sU, LV, 16 * tw, 32 * ks, lane), zz);
                 }
-                const f32x4 k4 = wide4(sK + t * LK + col + 4 * q), q4 = wide4(sQ + t * LK + col + 4 * q);
+                const f32x4 k4 = wide4(sK + t * LK + four_of<E>(col, q)), q4 = wide4(sQ + t * LK + four_of<E>(col, q));
                 xx *= splat4(a.scale * st.up[t]);
                 yy *= splat4(st.up[t]);
                 zz *= splat4(st.down[t]);
