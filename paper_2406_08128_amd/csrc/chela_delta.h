@@ -251,7 +251,18 @@ struct ChunkSteps {
     // (hi + lo: gamma in units of ln 2); up: e^gamma, down: e^(gamma of the last token - gamma), bu: -beta up
     alignas(16) float hi[C], lo[C], beta[C], up[C], down[C], bu[C];
     float whole;                                                       // e^(gamma of the last token)
-    __device__ __forceinline__ float decay(int t, int s) const { return exp2_((hi[t] - hi[s]) + (lo[t] - lo[s])); }
+    // e^(gamma_t - gamma_s) of one token t and four s from s0 on; of four t from t0 on and one s.  (Where s > t it is not wanted and may be infinite: what
+    // it is a factor of is chosen away there.  Worked out for all lanes alike: with a branch around each of them, a wave waits for LDS at each.)
+    __device__ __forceinline__ f32x4 decays_from(int t, int s0) const
+    {
+        const f32x4 d = (splat4(hi[t]) - *(const f32x4*)(hi + s0)) + (splat4(lo[t]) - *(const f32x4*)(lo + s0));
+        return f32x4{exp2_(d[0]), exp2_(d[1]), exp2_(d[2]), exp2_(d[3])};
+    }
+    __device__ __forceinline__ f32x4 decays_to(int t0, int s) const
+    {
+        const f32x4 d = (*(const f32x4*)(hi + t0) - splat4(hi[s])) + (*(const f32x4*)(lo + t0) - splat4(lo[s]));
+        return f32x4{exp2_(d[0]), exp2_(d[1]), exp2_(d[2]), exp2_(d[3])};
+    }
 };
 // Sums over the lanes up to each, by DPP: within rows of 16 lanes, then the rows' totals.
 template <int CTRL, int ROWS>
@@ -391,11 +402,9 @@ __device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSt
             f32x4 x = zero4();
 #pragma unroll
             for (int ks = 0; ks < DK / 32; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sK, LK, 16 * w, 32 * ks, lane), x);
+            x *= splat4(st.beta[t]) * st.decays_from(t, 16 * sb + 4 * q);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int s = 16 * sb + 4 * q + i;
-                x[i] = s < t ? st.beta[t] * st.decay(t, s) * x[i] : 0.f;
-            }
+            for (int i = 0; i < 4; ++i) x[i] = 16 * sb + 4 * q + i < t ? x[i] : 0.f;
             *(f32x4*)(sA + t * LA + 16 * sb + 4 * q) = x;
         }
     }

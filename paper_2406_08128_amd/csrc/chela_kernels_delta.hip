@@ -408,11 +408,9 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
                 if (sb <= w) {
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sQ, LK, 16 * w, 32 * ks, lane), x);
+                    x *= splat4(a.scale) * st.decays_from(t, 16 * sb + 4 * q);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int s = 16 * sb + 4 * q + i;
-                        x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
-                    }
+                    for (int i = 0; i < 4; ++i) x[i] = 16 * sb + 4 * q + i <= t ? x[i] : 0.f;
                 }
                 Pm.put4(t, 16 * sb, q, x);
             }

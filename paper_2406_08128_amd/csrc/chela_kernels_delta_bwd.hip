@@ -51,11 +51,9 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
             if (tb >= w) {
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sQ, LK, 16 * tb, 32 * ks, lane), rows_op(sK, LK, 16 * w, 32 * ks, lane), x);
+                x *= splat4(a.scale) * st.decays_to(16 * tb + 4 * q, s);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = 16 * tb + 4 * q + i;
-                    x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
-                }
+                for (int i = 0; i < 4; ++i) x[i] = s <= 16 * tb + 4 * q + i ? x[i] : 0.f;
             }
             Pt.put4(s, 16 * tb, q, x);
         }
@@ -186,11 +184,9 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
                     if (tb >= tw) {
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sQ, LK, 16 * tb, 32 * ks, lane), rows_op(sK, LK, 16 * tw, 32 * ks, lane), x);
+                        x *= splat4(a.scale) * st.decays_to(16 * tb + 4 * q, s);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int t = 16 * tb + 4 * q + i;
-                            x[i] = s <= t ? a.scale * st.decay(t, s) * x[i] : 0.f;
-                        }
+                        for (int i = 0; i < 4; ++i) x[i] = s <= 16 * tb + 4 * q + i ? x[i] : 0.f;
                     }
                     Pt.put4(s, 16 * tb, q, x);
                 }
@@ -413,11 +409,9 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
             if (tb >= tw) {
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sQ, LK, 16 * tb, 32 * ks, lane), rows_op(sK, LK, 16 * tw, 32 * ks, lane), x);
+                x *= splat4(a.scale) * st.decays_to(16 * tb + 4 * q, t);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int u = 16 * tb + 4 * q + i;
-                    x[i] = t <= u ? a.scale * st.decay(u, t) * x[i] : 0.f;
-                }
+                for (int i = 0; i < 4; ++i) x[i] = t <= 16 * tb + 4 * q + i ? x[i] : 0.f;
             }
             Pm.put4(t, 16 * tb, q, x);
         }
@@ -527,14 +521,16 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                     if (gi == 0)
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) g = mma(rows_op(sK, LK, 16 * b, 32 * ks, lane), rows_op(sK, LK, 16 * tw, 32 * ks, lane), g);
+                    const f32x4 d = st.decays_from(t, 16 * b + 4 * q);
+                    x[b] *= splat4(a.scale) * d;
+                    y[b] *= d;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int s = 16 * b + 4 * q + i;
-                        const float d = s <= t ? st.decay(t, s) : 0.f;
-                        x[b][i] = s <= t ? a.scale * d * x[b][i] : 0.f;
-                        y[b][i] = s < t ? d * y[b][i] : 0.f;
-                        dbeta = gi == 0 && s < t ? fmaf(-y[b][i], g[i], dbeta) : dbeta;
+                        x[b][i] = s <= t ? x[b][i] : 0.f;
+                        y[b][i] = s < t ? y[b][i] : 0.f;
                     }
+                    dbeta -= dot4(y[b], g);
                     y[b] *= splat4(st.beta[t]);
                 }
             }
@@ -553,12 +549,14 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                         x[b] = mma(rows_op(sO, LV, 16 * b, 32 * ks, lane), u[ks], x[b]);
                         y[b] = mma(rows_op(sV, LV, 16 * b, 32 * ks, lane), u[ks], y[b]);
                     }
+                    const f32x4 d = st.decays_to(16 * b + 4 * q, t);
+                    x[b] *= splat4(a.scale) * d;
+                    y[b] *= d;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int s = 16 * b + 4 * q + i;
-                        const float d = t <= s ? st.decay(s, t) : 0.f;
-                        x[b][i] = t <= s ? a.scale * d * x[b][i] : 0.f;
-                        y[b][i] = t < s ? d * y[b][i] : 0.f;
+                        x[b][i] = t <= s ? x[b][i] : 0.f;
+                        y[b][i] = t < s ? y[b][i] : 0.f;
                     }
                     y[b] *= *(const f32x4*)(st.beta + 16 * b + 4 * q);
                 }
