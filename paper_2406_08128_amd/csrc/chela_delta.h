@@ -49,6 +49,17 @@ __device__ __forceinline__ f32x4 mma(const Op<float, PA>& a, const Op<float, PB>
     return c;
 }
 
+// What has been rounded to bf16, in fp32 again.  (Out of the packed pairs: where the compiler sees the rounding it does it a second time, one by one.)
+__device__ __forceinline__ f32x4 widen(bf16x4 x)
+{
+    const u32x2 u = __builtin_bit_cast(u32x2, x);
+    return __builtin_bit_cast(f32x4, u32x4{u[0] << 16, u[0] & 0xffff0000u, u[1] << 16, u[1] & 0xffff0000u});
+}
+__device__ __forceinline__ f32x8 widen(bf16x8 x)
+{
+    return __builtin_shufflevector(widen(__builtin_shufflevector(x, x, 0, 1, 2, 3)), widen(__builtin_shufflevector(x, x, 4, 5, 6, 7)), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 // Two accumulator tiles as an operand.
 template <typename E, int P>
 __device__ __forceinline__ Op<E, P> operand(f32x4 lo, f32x4 hi)
@@ -59,7 +70,7 @@ __device__ __forceinline__ Op<E, P> operand(f32x4 lo, f32x4 hi)
         o.v = x;
     } else {
         o.h = __builtin_convertvector(x, bf16x8);
-        if constexpr (P == 2) o.l = __builtin_convertvector(x - __builtin_convertvector(o.h, f32x8), bf16x8);
+        if constexpr (P == 2) o.l = __builtin_convertvector(x - widen(o.h), bf16x8);
     }
     return o;
 }
@@ -140,7 +151,7 @@ struct Planes {
         } else {
             const bf16x4 a = __builtin_convertvector(x, bf16x4);
             *(bf16x4*)p = a;
-            if constexpr (P == 2) *(bf16x4*)(p + plane) = __builtin_convertvector(x - __builtin_convertvector(a, f32x4), bf16x4);
+            if constexpr (P == 2) *(bf16x4*)(p + plane) = __builtin_convertvector(x - widen(a), bf16x4);
         }
     }
     __device__ __forceinline__ Op<E, P> rows(int row0, int k0, int lane) const

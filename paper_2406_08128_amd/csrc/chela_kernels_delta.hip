@@ -127,13 +127,14 @@ __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 // ---- the same for a run of chunks: one N and one Z for all of them, so that the walk has fewer steps and less to read.  The state behind the
 // run's first chunks is taken through the next as the walk does it, Z beside what is left of the identity (X = M - e^Gamma, M the transition so far,
 // Gamma the sum of all log decays so far), thirty-two columns to a wave:
-//     U = T (beta V) - W Z,   or of X's columns  -e^Gamma W - W X;   X <- e^gamma X + K~^T U,   W = T (beta e^gamma K).
+//     U = T (beta V - beta e^gamma K Z),   or of X's columns  -T beta e^gamma K (X + e^Gamma);   X <- e^gamma X + K~^T U.
+// (K is what the caller gave and has one part, T K of the chunk alone would have two.)
 template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
     constexpr int NT = (DK + DV) * 2;
-    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[P * C * LT], sW[(sizeof(E) == 2 ? 2 : 1) * C * LK];
+    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[P * C * LT];
     __shared__ ChunkSteps<C> st;
     const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6);
     const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
@@ -156,7 +157,6 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
     };
     fetch(0, tid0, lane0);
     const Planes<E, P> T{sT, LT, C * LT};
-    const Planes<E, 2> W{sW, LK, C * LK};
     f32x4 X[DK / 16][2];
     float before = 1.f;
     for (int r = 0; r * C < ch.n; ++r) {
@@ -172,60 +172,59 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
         tt.template put<true>(sT, LT, P * C, tid);
         if (!last) fetch(r + 1, tid, lane);
         __syncthreads();
-        const float* f = of_k ? st.bu : st.beta;          // (W and X are kept with their signs changed)
+        // beta V - beta e^gamma K Z, or of the transition the same without V
         f32x4 y[NB][2];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) y[b][0] = y[b][1] = zero4();
-#pragma unroll
-        for (int ks = 0; ks < KC; ++ks) {
-            const Op<E, 2> x0 = scaled<E, 2>(cols_op(of_k ? sK : sV, of_k ? LK : LV, 32 * ks, col, lane), f, 32 * ks, lane);
-            const Op<E, 2> x1 = scaled<E, 2>(cols_op(of_k ? sK : sV, of_k ? LK : LV, 32 * ks, col + 16, lane), f, 32 * ks, lane);
-#pragma unroll
-            for (int b = 2 * ks; b < NB; ++b) {
-                const Op<E, P> m = T.rows(16 * b, 32 * ks, lane);
-                y[b][0] = mma(m, x0, y[b][0]);
-                y[b][1] = mma(m, x1, y[b][1]);
-            }
+        for (int b = 0; b < NB; ++b) {
+            y[b][0] = of_k ? splat4(before) * tile_of(sK, LK, 16 * b, col, lane) : zero4();
+            y[b][1] = of_k ? splat4(before) * tile_of(sK, LK, 16 * b, col + 16, lane) : zero4();
         }
-        if (r > 0) {
-            if (of_k) {
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int g = 0; g < 2; ++g)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) W.put(16 * b + 4 * q + i, col + 16 * g + c, y[b][g][i]);
-            }
-            __syncthreads();
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                y[b][0] *= splat4(of_k ? before : 1.f);
-                y[b][1] *= splat4(of_k ? before : 1.f);
-            }
+        if (r > 0)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 read_afresh();
                 const Op<E, 2> x0 = operand<E, 2>(X[2 * ks][0], X[2 * ks + 1][0]), x1 = operand<E, 2>(X[2 * ks][1], X[2 * ks + 1][1]);
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
-                    const Op<E, 2> m = W.rows(16 * b, 32 * ks, lane);
-                    y[b][0] = mma(m, x0, y[b][0]);
-                    y[b][1] = mma(m, x1, y[b][1]);
+                    const Op<E, 1> k = rows_op(sK, LK, 16 * b, 32 * ks, lane);
+                    y[b][0] = mma(k, x0, y[b][0]);
+                    y[b][1] = mma(k, x1, y[b][1]);
                 }
+            }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const f32x4 f = *(const f32x4*)(st.bu + 16 * b + 4 * q);
+            y[b][0] *= f;
+            y[b][1] *= f;
+            if (!of_k) {
+                const f32x4 be = *(const f32x4*)(st.beta + 16 * b + 4 * q);
+                y[b][0] += be * tile_of(sV, LV, 16 * b, col, lane);
+                y[b][1] += be * tile_of(sV, LV, 16 * b, col + 16, lane);
             }
         }
         Op<E, 2> yo[KC][2];
 #pragma unroll
+        for (int ks = 0; ks < KC; ++ks)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) yo[ks][g] = operand<E, 2>(y[2 * ks][g], y[2 * ks + 1][g]);
+        // what the tokens write, T of it
+#pragma unroll
         for (int b = 0; b < NB; ++b) {
+            y[b][0] = y[b][1] = zero4();
+#pragma unroll
+            for (int ks = 0; ks <= b / 2; ++ks) {
+                const Op<E, P> m = T.rows(16 * b, 32 * ks, lane);
+                y[b][0] = mma(m, yo[ks][0], y[b][0]);
+                y[b][1] = mma(m, yo[ks][1], y[b][1]);
+            }
             const f32x4 d = *(const f32x4*)(st.down + 16 * b + 4 * q);
             y[b][0] *= d;
             y[b][1] *= d;
         }
 #pragma unroll
-        for (int ks = 0; ks < KC; ++ks) {
-            yo[ks][0] = operand<E, 2>(y[2 * ks][0], y[2 * ks + 1][0]);
-            yo[ks][1] = operand<E, 2>(y[2 * ks][1], y[2 * ks + 1][1]);
-        }
+        for (int ks = 0; ks < KC; ++ks)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) yo[ks][g] = operand<E, 2>(y[2 * ks][g], y[2 * ks + 1][g]);
         const float whole = st.whole;
 #pragma unroll
         for (int n0 = 0; n0 < DK / 16; n0 += 2) {
@@ -330,7 +329,7 @@ __global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
             } else {
                 const bf16x4 hi = __builtin_convertvector(S, bf16x4);
                 *(bf16x4*)half = hi;
-                *(bf16x4*)(half + 512) = __builtin_convertvector(S - __builtin_convertvector(hi, f32x4), bf16x4);
+                *(bf16x4*)(half + 512) = __builtin_convertvector(S - widen(hi), bf16x4);
                 *(bf16x4*)out = hi;
             }
             __syncthreads();

@@ -320,8 +320,10 @@ template <typename E, int DK, int DV, bool RUN>
 __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, VS = DV / 32, LK = DK + kPad<E>, LV = DV + kPad<E>;
-    // (rows of S without padding where 160 KB are too few otherwise)
-    constexpr int LT = C + kPad<E>, LS = 64 + (sizeof(E) == 4 && DK + DV == 256 ? 0 : kPad<E>), NW = DV / 16, NT = DV * 4, GI = NW / NB, DT = 4 / GI;      // (DT: tiles of 64 key columns to a wave)
+    // Key columns of S and dS_next at a time, and tiles of them to a wave.  (fp32, 64 value columns: with 64 of them two workgroups would not fit in a compute
+    // unit's LDS: 3000 tokens, 6 heads of 64, 74 us, with 32 69.  Rows without padding where 160 KB are too few otherwise.)
+    constexpr int NW = DV / 16, NT = DV * 4, GI = NW / NB, CW = sizeof(E) == 4 && DV == 64 ? 32 : 64, DT = CW / 16 / GI;
+    constexpr int LT = C + kPad<E>, LS = CW + (sizeof(E) == 4 && DK + DV == 256 ? 0 : kPad<E>);
     constexpr bool SHARED = DV * LS <= C * LT;                  // (the states' operands fit where P and T were)
     __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sV[C * LV], sO[C * LV], sU[C * LV], sT[C * LT], sP[C * LT], sS[SHARED ? 8 : 2 * DV * LS];
     __shared__ ChunkSteps<C> st;
@@ -344,7 +346,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
     Chunk ch = run;
     // What the next head needs, or (NEXT) the next chunk, on its way during this one, where there are registers for it: 12 heads of 64, 16 sequences of
     // 2048 tokens, the gradient 332 us without, 324 with; 16 heads of 64 and 128, 8 of 2048, 415 and 422; of 128 and 128, 1083 and 1105.
-    constexpr bool AHEAD = DV == 128, NEXT = RUN && DK + DV == 128;
+    constexpr bool AHEAD = DV == 128, NEXT = RUN && DK + DV == 128 && DK == CW;
     Tile<E, C, DV, NT> tv, to;
     Tile<E, C, C, NT> tt;
     Steps ts;
@@ -388,9 +390,9 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         tk.put(sK, LK, ch.n, tid0);
     }
     const Planes<E, 1> Pm{sP, LT, 0}, Tm{sT, LT, 0}, Um{sU, LV, 0}, Rm{sV, LV, 0};
-    f32x4 sumQ[DK / 64 * DT], sumK[DK / 64 * DT];
+    f32x4 sumQ[DK / CW * DT], sumK[DK / CW * DT];
 #pragma unroll
-    for (int d = 0; d < DK / 64 * DT; ++d) sumQ[d] = sumK[d] = zero4();
+    for (int d = 0; d < DK / CW * DT; ++d) sumQ[d] = sumK[d] = zero4();
     for (int hh = 0; hh < share; ++hh) {
         const int h = hk * share + hh;
         int lane = lane0;
@@ -475,25 +477,25 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                     __builtin_convertvector(r * splat4(st.beta[r0]), Vec4<E>);
         }
         __syncthreads();
-        // S and dS_next so that their rows are summed over, sixty-four columns of them; what the next head needs is on its way
+        // S and dS_next so that their rows are summed over, CW columns of them; what the next head needs is on its way
         auto put = [&](int half) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < CW / 32; ++i) {
                 E *const p = sS0 + (16 * w + c) * LS + 32 * i, *const r = sdS + (16 * w + c) * LS + 32 * i;
                 if constexpr (sizeof(E) == 4) {
-                    const f32x8 s = so[2 * half + i].v, b = bo[2 * half + i].v;
+                    const f32x8 s = so[CW / 32 * half + i].v, b = bo[CW / 32 * half + i].v;
                     *(f32x4*)(p + 4 * q) = __builtin_shufflevector(s, s, 0, 1, 2, 3);
                     *(f32x4*)(p + 16 + 4 * q) = __builtin_shufflevector(s, s, 4, 5, 6, 7);
                     *(f32x4*)(r + 4 * q) = __builtin_shufflevector(b, b, 0, 1, 2, 3);
                     *(f32x4*)(r + 16 + 4 * q) = __builtin_shufflevector(b, b, 4, 5, 6, 7);
                 } else {
-                    *(bf16x8*)(p + 8 * q) = so[2 * half + i].h;
-                    *(bf16x8*)(r + 8 * q) = bo[2 * half + i].h;
+                    *(bf16x8*)(p + 8 * q) = so[CW / 32 * half + i].h;
+                    *(bf16x8*)(r + 8 * q) = bo[CW / 32 * half + i].h;
                 }
             }
         };
         put(0);
-        if (AHEAD && DK == 64 && hh + 1 < share) fetch(h + 1, chunk0, ch.row, ch.n, tid, lane);
+        if (AHEAD && DK == CW && hh + 1 < share) fetch(h + 1, chunk0, ch.row, ch.n, tid, lane);
         if (NEXT && rc > 0) fetch(h, chunk0 + rc - 1, ch.row - C, C, tid, lane);
         // X and beta Y of the wave's tokens as queries, then as keys
         float dbeta = 0.f, dgamma = 0.f, kc = 0.f;
@@ -569,16 +571,16 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         }
         // the gradients of queries and keys
 #pragma unroll
-        for (int half = 0; half < DK / 64; ++half) {
+        for (int half = 0; half < DK / CW; ++half) {
             if (half > 0) {
                 __syncthreads();
                 put(half);
-                if (AHEAD && half + 1 == DK / 64 && hh + 1 < share) fetch(h + 1, chunk0, ch.row, ch.n, tid, lane);
+                if (AHEAD && half + 1 == DK / CW && hh + 1 < share) fetch(h + 1, chunk0, ch.row, ch.n, tid, lane);
             }
             __syncthreads();
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                const int n = DT * gi + d, col = 64 * half + 16 * n;
+                const int n = DT * gi + d, col = CW * half + 16 * n;
                 read_afresh();
                 f32x4 xx = zero4(), yy = zero4(), zz = zero4();
 #pragma unroll
@@ -674,8 +676,8 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         E* dq = (E*)a.dQ + (size_t)(ch.row + t) * (a.Hk * DK) + hk * DK + 4 * q;
         E* dk = (E*)a.dK + (size_t)(ch.row + t) * (a.Hk * DK) + hk * DK + 4 * q;
 #pragma unroll
-        for (int i = 0; i < DK / 64 * DT; ++i) {
-            const int col = 64 * (i / DT) + 16 * (DT * gi + i % DT);
+        for (int i = 0; i < DK / CW * DT; ++i) {
+            const int col = CW * (i / DT) + 16 * (DT * gi + i % DT);
             *(Vec4<E>*)(dq + col) = __builtin_convertvector(sumQ[i], Vec4<E>);
             *(Vec4<E>*)(dk + col) = __builtin_convertvector(sumK[i], Vec4<E>);
         }
