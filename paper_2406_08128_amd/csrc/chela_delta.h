@@ -15,8 +15,9 @@ typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
 // Tokens of a chunk.  (fp32: a chunk's rows take twice the room in LDS.)
 template <typename E> struct DeltaChunk { static constexpr int C = sizeof(E) == 2 ? kDeltaChunkBf16 : kDeltaChunkF32; };
-// Elements behind each row of a tile in LDS: 16 rows' pieces of 16 bytes then fall on all banks alike.
-template <typename E> constexpr int kPad = sizeof(E) == 2 ? 8 : 4;
+// Elements behind each row of a tile in LDS: 32 bytes (bf16), so that the pieces that a read takes from eight or sixteen rows fall on all banks alike,
+// the transposed ones too.  (16 bytes: outputs of 16 heads of 128, 65536 tokens, 342 us, with 32 318; gradients of heads of 64 and 128 311 and 298.)
+template <typename E> constexpr int kPad = sizeof(E) == 2 ? 16 : 4;
 
 // A 16 x 32 operand.  All products are 16 x 16 tiles over 32 terms, D[m][n] += sum_k A[m][k] B[n][k]: lane 16 q + c has row c of A (of B)
 // at eight k, and of D the column n = c at the rows m = 4 q + i.  Which eight is free as long as A and B agree; here they are
