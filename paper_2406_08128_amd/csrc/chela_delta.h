@@ -27,8 +27,8 @@ template <typename E> constexpr int kPad = sizeof(E) == 2 ? 16 : 4;
 // P parts: a value that was worked out in fp32 is rounded to bf16 (P = 1, off by 2^-8 at most) or kept as a sum of two (P = 2, 2^-16).  What the caller
 // gave in bf16 has one part.  fp32 operands have all bits, and their products are fp32: eight instructions over four terms each.
 // Operands that stay in registers have two parts where the result goes into a state, or through the inverse: they cost matrix instructions, of
-// which there are enough.  Those that go through memory (N, T, the states that the outputs are made of) have one, and N and T two in calls that
-// take or return states in fp32: with one part each everywhere bf16 outputs are 4.1e-3 to 5.0e-3 off (root mean square, relative, of
+// which there are enough.  Those that go through memory (N, T, the states that the outputs are made of) have one, but N, and T where it goes into N, two in
+// calls that take or return states in fp32: with one part each everywhere bf16 outputs are 4.1e-3 to 5.0e-3 off (root mean square, relative, of
 // which 1.7e-3 are their own rounding; one head of 64, 4096 tokens without decay), so 3.0e-3 to 3.7e-3, with N and T in two 2.7e-3 to 3.4e-3.
 template <typename E, int P> struct Op;
 template <> struct Op<bf16, 1> { bf16x8 h; };

@@ -8,12 +8,15 @@
 //     S_next = e^(gamma_C) S + K~^T U = e^(gamma_C) S - N S + Z,   K~_s = e^(gamma_C - gamma_s) k_s,
 //     N = K~^T T (beta e^gamma K),   Z = K~^T T (beta V).
 // Three launches: one works N, Z and T out for all chunks at once, one walks the chunks with the states, a product each, one makes all
-// outputs from the states in front of the chunks.
+// outputs from the states in front of the chunks.  In long sequences the first and the last take runs of chunks (chunks_to_a_run), T comes in a
+// launch of its own, and the walk has a step to a run.
+// Times below: us, 65536 tokens in 4 sequences, 12 heads of 64, bf16 without states (a), or 1 sequence, 16 heads of 128, with states (b).
 #include "chela_delta.h"
 
 namespace chela {
 
-// ---- a chunk's T, N and Z
+// ---- a chunk's T, N and Z.  All of it on what is in LDS, thirty-two columns of N or Z to a wave.  6007 tokens in 11 sequences, 12 heads of 64, with
+// states: 22, a round and a half of workgroups, each of which waits for its tiles, then for the inverse, a row after the other.
 template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__(256, DK + DV == 128 ? 4 : 2) void delta_prep_kernel(DeltaArgs a)
 {
@@ -101,7 +104,8 @@ __global__ __launch_bounds__(256, DK + DV == 128 ? 4 : 2) void delta_prep_kernel
     }
 }
 
-// ---- T alone, of all chunks, for runs of them
+// ---- T alone, of all chunks, for runs of them (within a run's workgroup it would be one chunk's after the other: (b) 890 for both kernels in one, 820 in
+// two).  (a) 68, 200 MB, where the copy's rate would give 39: the inverse's steps wait for each other; five workgroups to a compute unit.
 template <typename E, int DK, int P>
 __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 {
@@ -128,7 +132,8 @@ __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 // run's first chunks is taken through the next as the walk does it, Z beside what is left of the identity (X = M - e^Gamma, M the transition so far,
 // Gamma the sum of all log decays so far), thirty-two columns to a wave:
 //     U = T (beta V - beta e^gamma K Z),   or of X's columns  -T beta e^gamma K (X + e^Gamma);   X <- e^gamma X + K~^T U.
-// (K is what the caller gave and has one part, T K of the chunk alone would have two.)
+// (K is what the caller gave and has one part, T K of the chunk alone would have two: 119 and 574 so.)  (a) 100, 400 MB at 4.0 TB/s; (b) 470, matrix
+// instructions: 340 GFLOP with all parts counted, at 0.72 PFLOP/s where a large product reaches 1.24; 193 registers, two waves to a SIMD.
 template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs a)
 {
@@ -277,7 +282,9 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
 
 // ---- the walk: S <- whole S + Z - N S from chunk to chunk (N comes negated), sixteen of S's columns to a workgroup, sixteen of its rows to a wave.
 // Each wave keeps its rows in fp32 and hands them to the others as operands, through LDS; what the next chunks need is on its way
-// meanwhile.  REV: from the last chunk to the first, with the states' gradients.
+// meanwhile.  REV: from the last chunk to the first, with the states' gradients.  (a) 32 for 64 runs: a step is one wave's turn to LDS, a barrier and
+// a product.  Chunk by chunk 110; 32768 tokens in 8 sequences, 12 heads of 64 and 128, so 89: 690 MB through the L2s, each head's N to all groups of
+// columns.  (Thirty-two columns to a workgroup, which halves that, leaves too few of them: slower.)
 template <typename E, int DK, int P, bool REV>
 __global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
 {
@@ -345,7 +352,8 @@ __global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
 }
 
 // ---- the outputs
-// Sixteen value columns to a wave; a run's chunks one after the other, the state from chunk to chunk in the wave's registers.
+// Sixteen value columns to a wave; a run's chunks one after the other, the state from chunk to chunk in the wave's registers.  (a) 130, 600 MB at
+// 4.6 TB/s, the states for the gradient among them; (b) 318, 1.0 GB at 3.1: operands from LDS, each wave all of K, Q and T.
 template <typename E, int DK, int DV>
 __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 ? 3 : 2) : 2) void delta_out_kernel(DeltaArgs a)
 {
@@ -477,7 +485,8 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
     }
 }
 
-// ---- a single token of each request: the state is read and written once, four columns and DK / R rows to a thread
+// ---- a single token of each request: the state is read and written once, four columns and DK / R rows to a thread.  256 requests, 12 heads of
+// 64: 18, 102 MB at 5.7 TB/s; one request 4, a launch.
 template <typename E, int DK, int DV>
 __global__ __launch_bounds__(256) void delta_step_kernel(DeltaArgs a)
 {
