@@ -170,6 +170,8 @@ RUNS = [  # lengths long enough for runs of several chunks; sequences whose last
     (2, 1, 128, 64, [577, 1090, 0, 1029]),
     (1, 1, 128, 128, [2305]),
     (2, 2, 64, 64, [4200, 5]),
+    (2, 2, 128, 64, [1100, 577]),
+    (1, 1, 64, 128, [8300]),
 ]
 
 
@@ -422,6 +424,24 @@ def test_what_is_not_finite_stays_in_its_sequence(dtype):
     assert torch.equal(c[:front], a[0][:front]) and not torch.isfinite(c[150:]).any()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_what_is_not_finite_stays_on_its_side_of_its_chunk(dtype):
+    # in runs of several chunks too: values reach no chunk in front, upstream gradients none behind
+    C, T, H = 64 if dtype == BF else 32, 1400, 2
+    x = inputs(gen(31), T, H, H, 64, 64, dtype)
+    y = [t.clone() for t in x]
+    y[2][1000], y[1][1003], y[4][1001] = float("nan"), float("inf"), float("nan")
+    for kept in (False, True):
+        a, b = (binding.chela_gated_delta_fwd(*t[:5], want_saved=kept) for t in (x, y))
+        front = 1000 // C * C
+        assert torch.equal(a[0][:front], b[0][:front]) and not torch.isfinite(b[0][1003:]).any()
+    z = [t.clone() for t in x]
+    z[5][500] = float("nan")
+    behind = (500 // C + 1) * C
+    for p, q in zip(binding.chela_gated_delta_bwd(*x)[:5], binding.chela_gated_delta_bwd(*z)[:5]):
+        assert torch.equal(p[behind:], q[behind:])
+
+
 # ------------------------------------------------------------------------------------------- layer norm
 def check(name, got, ref, mass, n):
     tol = O.tolerance(ref, mass, n, HALF[got.dtype])
@@ -645,6 +665,35 @@ def test_captured_and_replayed(own_scratch):
         for out, w in zip(outs, want):
             for p, q in zip(out, w):
                 assert torch.equal(p, q), k
+
+
+def test_runs_captured_and_replayed_with_other_offsets():
+    T, H = 1600, 2
+    x = inputs(gen(37), T, H, H, 64, 64, BF)
+    cu = cu_of([1500, 100])
+
+    def run():
+        out, saved = binding.chela_gated_delta_fwd(*x[:5], cu=cu, want_saved=True)
+        return [out, *binding.chela_gated_delta_bwd(*x, cu=cu, saved=saved)[:5], *binding.chela_gated_delta_bwd(*x, cu=cu)[:5],
+                binding.chela_gated_delta_fwd(*x[:5], cu=cu)[0]]
+
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        run()
+    torch.cuda.current_stream().wait_stream(s)
+    with torch.cuda.graph(g, stream=s):
+        got = run()
+    for lens in ([800, 800], [1600, 0], [3, 1590], [1500, 100], [0, 1]):
+        cu.copy_(cu_of(lens))
+        want = run()
+        for t in got:
+            t.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        for p, q in zip(got, want):
+            assert torch.equal(p, q), lens
+        check_all(dict(O=got[0], dV=got[3], dK=got[2]), x, None, None, lens, 1.0, BF, bounds=False)
 
 
 def test_two_threads_with_streams_of_their_own():
