@@ -132,8 +132,9 @@ __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 // run's first chunks is taken through the next as the walk does it, Z beside what is left of the identity (X = M - e^Gamma, M the transition so far,
 // Gamma the sum of all log decays so far), thirty-two columns to a wave:
 //     U = T (beta V - beta e^gamma K Z),   or of X's columns  -T beta e^gamma K (X + e^Gamma);   X <- e^gamma X + K~^T U.
-// (K is what the caller gave and has one part, T K of the chunk alone would have two: 119 and 574 so.)  (a) 100, 400 MB at 4.0 TB/s; (b) 470, matrix
-// instructions: 340 GFLOP with all parts counted, at 0.72 PFLOP/s where a large product reaches 1.24; 193 registers, two waves to a SIMD.
+// (K is what the caller gave and has one part, T K of the chunk alone would have two: 119 and 574 so.)  (a) 100, 400 MB at 4.0 TB/s; (b) 470,
+// instruction issue: vector instructions 57 % of the time (values split into two parts, scaled), matrix instructions 34 (340 GFLOP with all
+// parts, 0.72 PFLOP/s); 193 registers, two waves to a SIMD.
 template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs a)
 {
@@ -353,7 +354,7 @@ __global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
 
 // ---- the outputs
 // Sixteen value columns to a wave; a run's chunks one after the other, the state from chunk to chunk in the wave's registers.  (a) 130, 600 MB at
-// 4.6 TB/s, the states for the gradient among them; (b) 318, 1.0 GB at 3.1: operands from LDS, each wave all of K, Q and T.
+// 4.6 TB/s, the states for the gradient among them; (b) 318, 1.0 GB at 3.1: vector instructions 55 % of the time, matrix instructions 31.
 template <typename E, int DK, int DV>
 __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 ? 3 : 2) : 2) void delta_out_kernel(DeltaArgs a)
 {

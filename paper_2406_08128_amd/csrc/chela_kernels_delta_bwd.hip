@@ -319,8 +319,8 @@ __device__ __forceinline__ float column_sum(float x)
 // columns to a wave for U and dR; then sixteen tokens, as queries and as keys, and a part of the key columns.  X and Y are worked out twice, by the wave
 // of the query's tokens and by that of the key's: as the operands of its own products they then lie in a wave's registers as they are.
 // 65536 tokens in 4 sequences, 12 heads of 64: 350 us, 900 MB at 2.6 TB/s; 32768 in 8, 12 heads of 64 and 128 with 4 key heads: 298.  Registers bound it:
-// 203 to 247 leave two waves to a SIMD, which wait for LDS and each other half the time (eight barriers to a chunk; matrix instructions 12 % of
-// the time, vector instructions 40 %, LDS 54 %, before its reads went by 16 bytes).
+// 203 to 247 leave two waves to a SIMD, which wait for LDS and each other half the time (eight barriers to a chunk; vector instructions 45 % of the
+// time, LDS 38, matrix instructions 15).
 template <typename E, int DK, int DV, bool RUN>
 __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
 {
