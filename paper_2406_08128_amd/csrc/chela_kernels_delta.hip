@@ -164,6 +164,8 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
     fetch(0, tid0, lane0);
     const Planes<E, P> T{sT, LT, C * LT};
     f32x4 X[DK / 16][2];
+#pragma unroll
+    for (int d = 0; d < DK / 16; ++d) X[d][0] = X[d][1] = zero4();
     float before = 1.f;
     for (int r = 0; r * C < ch.n; ++r) {
         const int n = min(C, ch.n - r * C);
@@ -181,10 +183,13 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
         // beta V - beta e^gamma K Z, or of the transition the same without V
         f32x4 y[NB][2];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            y[b][0] = of_k ? splat4(before) * tile_of(sK, LK, 16 * b, col, lane) : zero4();
-            y[b][1] = of_k ? splat4(before) * tile_of(sK, LK, 16 * b, col + 16, lane) : zero4();
-        }
+        for (int b = 0; b < NB; ++b) y[b][0] = y[b][1] = zero4();
+        if (of_k)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                y[b][0] = splat4(before) * tile_of(sK, LK, 16 * b, col, lane);
+                y[b][1] = splat4(before) * tile_of(sK, LK, 16 * b, col + 16, lane);
+            }
         if (r > 0)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -239,7 +244,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int g = 0; g < 2; ++g) z[i][g] = r > 0 ? X[n0 + i][g] * splat4(whole) : zero4();
+                for (int g = 0; g < 2; ++g) z[i][g] = X[n0 + i][g] * splat4(whole);
             if (last && of_k) {
                 // as N is read, the columns of X down the rows of a tile: its old part by products with the identity
                 const Op<E, 2> x0 = operand<E, 2>(z[0][0], z[1][0]), x1 = operand<E, 2>(z[0][1], z[1][1]);

@@ -195,9 +195,12 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
         }
         f32x4 y[NB][2];
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NB; ++b) y[b][0] = y[b][1] = zero4();
+        if (of_k)
 #pragma unroll
-            for (int g = 0; g < 2; ++g) y[b][g] = of_k ? splat4(before) * tile_of(sK, LK, 16 * b, col + 16 * g, lane) : zero4();
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) y[b][g] = splat4(before) * tile_of(sK, LK, 16 * b, col + 16 * g, lane);
         if (!first)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
