@@ -415,8 +415,9 @@ __device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSt
 #pragma unroll
             for (int ks = 0; ks < DK / 32; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sK, LK, 16 * w, 32 * ks, lane), x);
             x *= splat4(st.beta[t]) * st.decays_from(t, 16 * sb + 4 * q);
+            if (sb == w)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = 16 * sb + 4 * q + i < t ? x[i] : 0.f;
+                for (int i = 0; i < 4; ++i) x[i] = 4 * q + i < c ? x[i] : 0.f;
             *(f32x4*)(sA + t * LA + 16 * sb + 4 * q) = x;
         }
     }

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 // run's first chunks is taken through the next as the walk does it, Z beside what is left of the identity (X = M - e^Gamma, M the transition so far,
 // Gamma the sum of all log decays so far), thirty-two columns to a wave:
 //     U = T (beta V - beta e^gamma K Z),   or of X's columns  -T beta e^gamma K (X + e^Gamma);   X <- e^gamma X + K~^T U.
-// (K is what the caller gave and has one part, T K of the chunk alone would have two: 119 and 574 so.)  (a) 100, 400 MB at 4.0 TB/s; (b) 470,
+// (K is what the caller gave and has one part, T K of the chunk alone would have two: 119 and 574 so.)  (a) 97, 400 MB at 4.1 TB/s; (b) 465,
 // instruction issue: vector instructions 57 % of the time (values split into two parts, scaled), matrix instructions 34 (340 GFLOP with all
 // parts, 0.72 PFLOP/s); 193 registers, two waves to a SIMD.
 template <typename E, int DK, int DV, int P>
@@ -422,8 +422,9 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sQ, LK, 16 * w, 32 * ks, lane), x);
                     x *= splat4(a.scale) * st.decays_from(t, 16 * sb + 4 * q);
+                    if (sb == w)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = 16 * sb + 4 * q + i <= t ? x[i] : 0.f;
+                        for (int i = 0; i < 4; ++i) x[i] = 4 * q + i <= c ? x[i] : 0.f;
                 }
                 Pm.put4(t, 16 * sb, q, x);
             }

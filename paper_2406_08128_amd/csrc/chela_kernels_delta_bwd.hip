@@ -13,7 +13,7 @@
 
 namespace chela {
 
-// ---- a chunk's N^T and Z'.  32768 tokens in 8 sequences, 12 heads of 64 and 128 (4 key heads): 113 us, 440 MB at 3.9 TB/s.
+// ---- a chunk's N^T and Z'.  32768 tokens in 8 sequences, 12 heads of 64 and 128 (4 key heads): 111 us, 440 MB at 4.0 TB/s.
 template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 {
@@ -53,8 +53,9 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sQ, LK, 16 * tb, 32 * ks, lane), rows_op(sK, LK, 16 * w, 32 * ks, lane), x);
                 x *= splat4(a.scale) * st.decays_to(16 * tb + 4 * q, s);
+                if (tb == w)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = s <= 16 * tb + 4 * q + i ? x[i] : 0.f;
+                    for (int i = 0; i < 4; ++i) x[i] = c <= 4 * q + i ? x[i] : 0.f;
             }
             Pt.put4(s, 16 * tb, q, x);
         }
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 // ---- the same for a run of chunks, from its last to its first: one N^T and one Z' for all of them.  What a chunk makes of a state's gradient,
 //     dS <- e^gamma dS + scale (e^gamma Q)^T dO - (beta e^gamma K)^T T^T (P^T dO + K~ dS),
 // with Z' beside what is left of the identity (X = M^T - e^Gamma, without the terms in dO), thirty-two columns to a wave.  65536 tokens in 4
-// sequences, 12 heads of 64: 139 us, 400 MB at 2.9 TB/s: products in a chain, two waves to a SIMD (150 registers and more).
+// sequences, 12 heads of 64: 134 us, 400 MB at 3.0 TB/s: products in a chain, two waves to a SIMD (150 registers and more).
 template <typename E, int DK, int DV>
 __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(DeltaArgs a)
 {
@@ -187,8 +188,9 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sQ, LK, 16 * tb, 32 * ks, lane), rows_op(sK, LK, 16 * tw, 32 * ks, lane), x);
                         x *= splat4(a.scale) * st.decays_to(16 * tb + 4 * q, s);
+                        if (tb == tw)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[i] = s <= 16 * tb + 4 * q + i ? x[i] : 0.f;
+                            for (int i = 0; i < 4; ++i) x[i] = c <= 4 * q + i ? x[i] : 0.f;
                     }
                     Pt.put4(s, 16 * tb, q, x);
                 }
@@ -321,7 +323,7 @@ __device__ __forceinline__ float column_sum(float x)
 // and a head, from the last chunk to the first with the gradient of the state behind each in registers, sixteen value columns to a wave.  Sixteen value
 // columns to a wave for U and dR; then sixteen tokens, as queries and as keys, and a part of the key columns.  X and Y are worked out twice, by the wave
 // of the query's tokens and by that of the key's: as the operands of its own products they then lie in a wave's registers as they are.
-// 65536 tokens in 4 sequences, 12 heads of 64: 350 us, 900 MB at 2.6 TB/s; 32768 in 8, 12 heads of 64 and 128 with 4 key heads: 298.  Registers bound it:
+// 65536 tokens in 4 sequences, 12 heads of 64: 340 us, 900 MB at 2.6 TB/s; 32768 in 8, 12 heads of 64 and 128 with 4 key heads: 298.  Registers bound it:
 // 203 to 247 leave two waves to a SIMD, which wait for LDS and each other half the time (eight barriers to a chunk; vector instructions 45 % of the
 // time, LDS 38, matrix instructions 15).
 template <typename E, int DK, int DV, bool RUN>
@@ -420,8 +422,9 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sQ, LK, 16 * tb, 32 * ks, lane), rows_op(sK, LK, 16 * tw, 32 * ks, lane), x);
                 x *= splat4(a.scale) * st.decays_to(16 * tb + 4 * q, t);
+                if (tb == tw)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = t <= 16 * tb + 4 * q + i ? x[i] : 0.f;
+                    for (int i = 0; i < 4; ++i) x[i] = c <= 4 * q + i ? x[i] : 0.f;
             }
             Pm.put4(t, 16 * tb, q, x);
         }
@@ -534,12 +537,12 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                     const f32x4 d = st.decays_from(t, 16 * b + 4 * q);
                     x[b] *= splat4(a.scale) * d;
                     y[b] *= d;
+                    if (b == tw)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int s = 16 * b + 4 * q + i;
-                        x[b][i] = s <= t ? x[b][i] : 0.f;
-                        y[b][i] = s < t ? y[b][i] : 0.f;
-                    }
+                        for (int i = 0; i < 4; ++i) {
+                            x[b][i] = 4 * q + i <= c ? x[b][i] : 0.f;
+                            y[b][i] = 4 * q + i < c ? y[b][i] : 0.f;
+                        }
                     dbeta -= dot4(y[b], g);
                     y[b] *= splat4(st.beta[t]);
                 }
@@ -562,12 +565,12 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                     const f32x4 d = st.decays_to(16 * b + 4 * q, t);
                     x[b] *= splat4(a.scale) * d;
                     y[b] *= d;
+                    if (b == tw)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int s = 16 * b + 4 * q + i;
-                        x[b][i] = t <= s ? x[b][i] : 0.f;
-                        y[b][i] = t < s ? y[b][i] : 0.f;
-                    }
+                        for (int i = 0; i < 4; ++i) {
+                            x[b][i] = c <= 4 * q + i ? x[b][i] : 0.f;
+                            y[b][i] = c < 4 * q + i ? y[b][i] : 0.f;
+                        }
                     y[b] *= *(const f32x4*)(st.beta + 16 * b + 4 * q);
                 }
             }
