@@ -1090,8 +1090,8 @@ def _delta_inputs(Q, K, V, g, beta, scale, cu):
 
 def chela_gated_delta_fwd(Q, K, V, g, beta, scale=1.0, cu=None, S_in=None, S_out=None, slots=None, want_saved=False, O=None, stream=None):
     """(O, saved): the gated delta rule S = exp(g) S, S += beta k (v - S^T k)^T, o = scale S^T q over the tokens of each sequence.
-    Q, K [..., Hk, dk], V [..., H, dv], g (None: no decay) and beta [..., H]; Hk divides H; states [n_slots, H, dk, dv] float32.  saved is None
-    unless asked for (for chela_gated_delta_bwd).  Rows of no sequence: zero in a new O, left as they are in one that is given."""
+    Q, K [..., Hk, dk], V [..., H, dv], g (None: no decay; above 0, where it lets a state grow, roundings count for more by as much as
+    64 tokens grow) and beta [..., H]; Hk divides H; states [n_slots, H, dk, dv] float32.  saved is None unless asked for (for chela_gated_delta_bwd).  Rows of no sequence: zero in a new O, left as they are in one that is given."""
     name = "gated_delta_fwd" if cu is None or O is not None else "gated_delta_fwd_cleared"
     r = _host("gated_delta_fwd")(_fn[name], _fn[name + "_f32"], _fn["gated_delta_saved_bytes"], Q, K, V, g, beta, scale, cu, S_in, S_out,
                                  slots, want_saved, O, stream)

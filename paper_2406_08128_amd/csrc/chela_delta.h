@@ -338,6 +338,20 @@ __device__ __forceinline__ void put_steps(ChunkSteps<C>& st, const Steps& x, int
     }
 }
 
+// What a chunk or a run makes of a state is kept as M - w, w times the identity beside it, w = e^Gamma (Gamma the sum of its log decays) where that
+// is below 1, so that a state without decay goes through as it is.  Above 1 it is not: keys that replace what grows leave M far below e^Gamma, and what
+// is kept would be rounded relative to that, to no digit of M in the end.  w is 1 there, from chunk to chunk w <- min(1, e^gamma w), and what is left of
+// e^gamma w comes into M - w.  (What is not a number stays it.)
+__device__ __forceinline__ float no_growth(float x) { return x > 1.f ? 1.f : x; }
+// x on the diagonal of a tile, added to an accumulator
+__device__ __forceinline__ f32x4 plus_diagonal(f32x4 a, float x, int lane)
+{
+    const int q = lane >> 4, c = lane & 15;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] += 4 * q + i == c ? x : 0.f;
+    return a;
+}
+
 // The same operand with each of its eight terms times a factor: f[k0 ..], one for each row of the tile that it was read from.
 template <typename E, int P>
 __device__ __forceinline__ Op<E, P> scaled(const Op<E, 1>& x, const float* f, int k0, int lane, float by = 1.f)

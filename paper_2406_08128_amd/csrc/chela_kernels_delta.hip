@@ -5,8 +5,8 @@
 // A chunk of C tokens at once, gamma the running sum of g in it, S the state in front of it, D_ts = e^(gamma_t - gamma_s):
 //     (1 + A) U = beta (V - e^gamma K S),  A_ts = beta_t D_ts k_t . k_s for s < t, 0 otherwise;   T = (1 + A)^-1,
 //     O = scale e^gamma Q S + P U,  P_ts = scale D_ts q_t . k_s for s <= t,
-//     S_next = e^(gamma_C) S + K~^T U = e^(gamma_C) S - N S + Z,   K~_s = e^(gamma_C - gamma_s) k_s,
-//     N = K~^T T (beta e^gamma K),   Z = K~^T T (beta V).
+//     S_next = e^(gamma_C) S + K~^T U = w S - N S + Z,   K~_s = e^(gamma_C - gamma_s) k_s,
+//     N = K~^T T (beta e^gamma K) + w - e^(gamma_C),   Z = K~^T T (beta V),   w = min(1, e^(gamma_C)).
 // Three launches: one works N, Z and T out for all chunks at once, one walks the chunks with the states, a product each, one makes all
 // outputs from the states in front of the chunks.  In long sequences the first and the last take runs of chunks (chunks_to_a_run), T comes in a
 // launch of its own, and the walk has a step to a run.
@@ -47,8 +47,9 @@ __global__ __launch_bounds__(256, DK + DV == 128 ? 4 : 2) void delta_prep_kernel
         E* to = (E*)a.T + at * (C * C);
 #pragma unroll
         for (int i = tid; i < C * (C / W); i += 256) *(u32x4*)(to + i * W) = *(const u32x4*)(sT + i / (C / W) * LT + i % (C / W) * W);
-        if (tid == 0) a.whole[at] = st.whole;
+        if (tid == 0) a.whole[at] = no_growth(st.whole);
     }
+    const float grown = st.whole - no_growth(st.whole);
     // T (beta e^gamma K), T (beta V), thirty-two columns at a time, and what K~ makes of them
 #pragma unroll 1
     for (int p = w; p < (DK + DV) / 32; p += 4) {
@@ -87,6 +88,10 @@ __global__ __launch_bounds__(256, DK + DV == 128 ? 4 : 2) void delta_prep_kernel
 #pragma unroll
         for (int n = 0; n < DK / 16; ++n) {
             f32x4 r0 = zero4(), r1 = zero4();
+            if (of_k && n / 2 == p) {
+                if (n % 2 == 0) r0 = plus_diagonal(r0, grown, lane);
+                else r1 = plus_diagonal(r1, grown, lane);
+            }
 #pragma unroll
             for (int ks = 0; ks < KC; ++ks) {
                 const Op<E, 1> k = cols_op(sK, LK, 32 * ks, 16 * n, lane);
@@ -129,9 +134,9 @@ __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 }
 
 // ---- the same for a run of chunks: one N and one Z for all of them, so that the walk has fewer steps and less to read.  The state behind the
-// run's first chunks is taken through the next as the walk does it, Z beside what is left of the identity (X = M - e^Gamma, M the transition so far,
-// Gamma the sum of all log decays so far), thirty-two columns to a wave:
-//     U = T (beta V - beta e^gamma K Z),   or of X's columns  -T beta e^gamma K (X + e^Gamma);   X <- e^gamma X + K~^T U.
+// run's first chunks is taken through the next as the walk does it, Z beside what is left of the identity (X = M - w, M the transition so far,
+// w = e^(sum of all log decays so far), held to 1), thirty-two columns to a wave:
+//     U = T (beta V - beta e^gamma K Z),   or of X's columns  -T beta e^gamma K (X + w);   X <- e^gamma X + K~^T U + e^gamma w - w_next.
 // (K is what the caller gave and has one part, T K of the chunk alone would have two: 119 and 574 so.)  (a) 97, 400 MB at 4.1 TB/s; (b) 465,
 // instruction issue: vector instructions 57 % of the time (values split into two parts, scaled), matrix instructions 34 (340 GFLOP with all
 // parts, 0.72 PFLOP/s); 193 registers, two waves to a SIMD.
@@ -236,7 +241,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
         for (int ks = 0; ks < KC; ++ks)
 #pragma unroll
             for (int g = 0; g < 2; ++g) yo[ks][g] = operand<E, 2>(y[2 * ks][g], y[2 * ks + 1][g]);
-        const float whole = st.whole;
+        const float whole = st.whole, after = no_growth(before * whole), grown = before * whole - after;
 #pragma unroll
         for (int n0 = 0; n0 < DK / 16; n0 += 2) {
             read_afresh();
@@ -245,6 +250,10 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int g = 0; g < 2; ++g) z[i][g] = X[n0 + i][g] * splat4(whole);
+            if (n0 / 2 == w) {                             // (only of X, whose waves come first)
+                z[0][0] = plus_diagonal(z[0][0], grown, lane);
+                z[1][1] = plus_diagonal(z[1][1], grown, lane);
+            }
             if (last && of_k) {
                 // as N is read, the columns of X down the rows of a tile: its old part by products with the identity
                 const Op<E, 2> x0 = operand<E, 2>(z[0][0], z[1][0]), x1 = operand<E, 2>(z[0][1], z[1][1]);
@@ -281,12 +290,12 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
                     }
             }
         }
-        before *= whole;
+        before = after;
     }
     if (tid0 == 0) a.whole[at] = before;
 }
 
-// ---- the walk: S <- whole S + Z - N S from chunk to chunk (N comes negated), sixteen of S's columns to a workgroup, sixteen of its rows to a wave.
+// ---- the walk: S <- w S + Z - N S from chunk to chunk (N comes negated), sixteen of S's columns to a workgroup, sixteen of its rows to a wave.
 // Each wave keeps its rows in fp32 and hands them to the others as operands, through LDS; what the next chunks need is on its way
 // meanwhile.  REV: from the last chunk to the first, with the states' gradients.  (a) 32 for 64 runs: a step is one wave's turn to LDS, a barrier and
 // a product.  Chunk by chunk 110; 32768 tokens in 8 sequences, 12 heads of 64 and 128, so 89: 690 MB through the L2s, each head's N to all groups of

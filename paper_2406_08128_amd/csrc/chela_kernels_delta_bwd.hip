@@ -7,7 +7,7 @@
 //     dbeta_t = dR_t . v_t - k_t . (e^gamma_t S dR_t) - sum_s Y_ts k_t . k_s,
 //     dgamma_t = q_t . dQ_t + k_t . read_t - k_t . write_t, at the chunk's last token + e^gamma_C <S, dS_next> + sum_s k_s . carry_s,
 //     dg_t = sum of dgamma from t to the chunk's end   (every pair of tokens on one side of t cancels: both take it from the same X, Y),
-//     dS = e^gamma_C dS_next - N^T dS_next + Z',   Z' = scale (e^gamma Q)^T dO - (beta e^gamma K)^T T^T P^T dO.
+//     dS = w dS_next - N^T dS_next + Z' (w and N as forward),   Z' = scale (e^gamma Q)^T dO - (beta e^gamma K)^T T^T P^T dO.
 // Three launches, as forward: N^T and Z' of all chunks, the walk from the last chunk to the first, all gradients.
 #include "chela_delta.h"
 
@@ -42,7 +42,8 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
         if (P == 1) m.template put<true>(sT, LT, C, tid);
     }
     __syncthreads();
-    if (tid == 0) a.whole[at] = st.whole;
+    if (tid == 0) a.whole[at] = no_growth(st.whole);
+    const float grown = st.whole - no_growth(st.whole);
     const Planes<E, P> T{sT, LT, C * LT}, Pt{sP, LT, C * LT};
     if (P == 2) chunk_inverse<E, DK>(sK, LK, st, (float*)sT, T, tid);       // (what was kept of it has one part)
     if (w < NB) {                                                  // P's transpose, sixteen of its rows to a wave
@@ -116,6 +117,10 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 #pragma unroll
             for (int n = 0; n < KS; ++n) {
                 f32x4 r0 = zero4(), r1 = zero4();
+                if (n == g / 2) {
+                    if (g % 2 == 0) r0 = plus_diagonal(r0, grown, lane);
+                    else r1 = plus_diagonal(r1, grown, lane);
+                }
 #pragma unroll
                 for (int ks = 0; ks < KC; ++ks) {
                     r0 = mma(cols_op(sK, LK, 32 * ks, 32 * n, lane), xo[ks], r0);
@@ -129,7 +134,7 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 
 // ---- the same for a run of chunks, from its last to its first: one N^T and one Z' for all of them.  What a chunk makes of a state's gradient,
 //     dS <- e^gamma dS + scale (e^gamma Q)^T dO - (beta e^gamma K)^T T^T (P^T dO + K~ dS),
-// with Z' beside what is left of the identity (X = M^T - e^Gamma, without the terms in dO), thirty-two columns to a wave.  65536 tokens in 4
+// with Z' beside what is left of the identity (X = M^T - w, as forward, without the terms in dO), thirty-two columns to a wave.  65536 tokens in 4
 // sequences, 12 heads of 64: 134 us, 400 MB at 3.0 TB/s: products in a chain, two waves to a SIMD (150 registers and more).
 template <typename E, int DK, int DV>
 __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(DeltaArgs a)
@@ -255,12 +260,13 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
         for (int ks = 0; ks < KC; ++ks)
 #pragma unroll
             for (int g = 0; g < 2; ++g) yo[ks][g] = operand<E, 2>(y[2 * ks][g], y[2 * ks + 1][g]);
-        const float whole = st.whole;
+        const float whole = st.whole, after = no_growth(before * whole), grown = before * whole - after;
 #pragma unroll
         for (int d = 0; d < DK / 16; ++d) {
             if (d % 2 == 0) read_afresh();
             X[d][0] *= splat4(whole);
             X[d][1] *= splat4(whole);
+            if (d / 2 == w) X[d][d % 2] = plus_diagonal(X[d][d % 2], grown, lane);        // (only of X, whose waves come first)
 #pragma unroll
             for (int ks = 0; ks < KC; ++ks) {
                 const Op<E, 1> k = cols_op(sK, LK, 32 * ks, 16 * d, lane);
@@ -285,7 +291,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
                 }
             }
         }
-        before *= whole;
+        before = after;
     }
     if (of_k) {
         // as it is read, the columns of X down the rows of a tile: by products with the identity
