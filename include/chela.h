@@ -462,7 +462,8 @@ size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int
  *          backward call needs of the chunks (states and inverses).
  *   bwd  : dQ, dK [T, Hk, dk] (sums over a key head's value heads), dV [T, H, dv], dg (NULL without g), dbeta [T, H] in the I/O type, dS_in
  *          [n_seq, H, dk, dv] fp32 (NULL: not wanted), for the upstream dO [T, H, dv] and dS_out (fp32, NULL: zero).  saved: as the forward
- *          call with the same inputs left it, or NULL: worked out again.  Sums are taken in a fixed order.
+ *          call with the same inputs left it, or NULL: worked out again.  Sums are taken in a fixed order.  dg_t is added up of terms
+ *          with the factor e^(g_t) each: as exact relative to what a token lets through as the others are, and zero where it empties the state.
  *   step : one row for each of R requests; S [n_slots, H, dk, dv] is updated in place.
  * Limits beside those above (D: H dk): T H dk / 64 < 2^26, n_seq H dv / 16 and R H dv / 16 < 2^23.  `packed` in the queries: cu is given. */
 int chela_gated_delta_fwd(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,

@@ -129,12 +129,12 @@ def delta_bounds(q, k, v, g, beta, dO, chunk, once, twice, scale=1.0, state=None
         R = _times(_plus(_exact(p["V"]), (-KS[0], KS[1])), p["be"])
         p["U"] = _mm(p["T1"], _rounded(R, once))
         P = _mm(_exact(p["Q"]), _exact(p["K"].T))
-        p["P0"], p["P"] = P[0], _times(P, scale * p["D"], p["erel"])
+        p["QK"], p["P"] = P, _times(P, scale * p["D"], p["erel"])
         QS = _times(_mm(_exact(p["Q"]), p["S"]), scale * p["up"], p["grel"])
         out["O"][p["a"]:p["b"]] = _onto(QS, _mm(_rounded(p["P"], once), _rounded(p["U"], once)), p["b"] - p["a"])[1]
     if dO is None:
         return out
-    out.update(dQ=np.zeros(q.shape), dK=np.zeros(k.shape), dV=np.zeros(v.shape), dg=np.zeros(L), dbeta=np.zeros(L), dg_sums=np.zeros(L))
+    out.update(dQ=np.zeros(q.shape), dK=np.zeros(k.shape), dV=np.zeros(v.shape), dg=np.zeros(L), dbeta=np.zeros(L), dg_sums=np.zeros(L), dg_divided=np.zeros(L))
     dS = _exact(zero if dstate is None else dstate)
     for p in parts[::-1]:
         a, b, K, Q, be, up, down, grel, D, erel = (p[x] for x in ("a", "b", "K", "Q", "be", "up", "down", "grel", "D", "erel"))
@@ -163,7 +163,7 @@ def delta_bounds(q, k, v, g, beta, dO, chunk, once, twice, scale=1.0, state=None
         out["dbeta"][a:b] = dot(p["V"], dR, dv) + dot(K, into, dk) + dot(Y[0], p["G"], b - a) + (Y[1] * np.abs(p["G"][0])).sum(1)
         # Decays: a pair of tokens on one side of t goes into dgamma twice, from the same rounded X and Y, and cancels but for sums' roundings (512
         # of them on any way); what X and Y are off by comes in through the pairs that t divides.
-        QK = np.abs(p["P0"])
+        QK = np.abs(p["QK"][0])
         pair = X1[1] * QK + Yb[1] * np.abs(p["G"][0])
         size = np.abs(X1[0]) * QK + np.abs(Yb[0]) * np.abs(p["G"][0])
         oS = _times(_mm(_exact(d), _t(p["S"])), scale * up, grel)
@@ -173,6 +173,16 @@ def delta_bounds(q, k, v, g, beta, dO, chunk, once, twice, scale=1.0, state=None
         for t in range(b - a):
             out["dg_sums"][a + t] = 512 * F * sums              # (of it what is left where all of it cancels, a first token's without a state)
             out["dg"][a + t] = pair[t:, :t].sum() + near[t:].sum() + far[:t].sum() + p["whole"] * SB + 512 * F * sums
+        # ... and where only the pairs that t divides are added up, with what comes from the state in front to t and later tokens, what tokens in front of t
+        # hand to the one behind, and what goes through: each term has the factor e^g_t, so the bound has it too.  X and Y need not be rounded for it.
+        Ye = _times(Y, be)
+        pair = X[1] * QK + np.abs(X[0]) * p["QK"][1] + Ye[1] * np.abs(p["G"][0]) + np.abs(Ye[0]) * p["G"][1]
+        size = np.abs(X[0]) * QK + np.abs(Ye[0]) * np.abs(p["G"][0])
+        onear, ofar = np.abs(Q * oS[0]).sum(1) + np.abs(K * into[0] * be).sum(1), np.abs(K * carry[0]).sum(1)
+        through = p["whole"] * np.abs(p["S"][0] * B[0]).sum()
+        for t in range(b - a):
+            mags = size[t:, :t].sum() + onear[t:].sum() + ofar[:t].sum() + through * (1 + abs(np.log(max(p["whole"], 1e-100))))
+            out["dg_divided"][a + t] = pair[t:, :t].sum() + near[t:].sum() + far[:t].sum() + p["whole"] * SB + (2 * (b - a) + 32) * F * mags
         # and of the state in front
         x = _rounded(_mm(_t(_rounded(p["P"], twice)), _exact(d)), twice)
         y = _rounded(_times(_mm(_t(p["T2"]), x), be * up, grel), twice)

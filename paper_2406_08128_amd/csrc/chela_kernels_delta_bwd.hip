@@ -5,8 +5,10 @@
 //     dQ = scale e^gamma dO S^T + X K,   read = -beta (e^gamma dR S^T + Y K),   carry = e^(gamma_C - gamma) U dS_next^T,
 //     write = carry + X^T Q - (beta Y)^T K,   dK = read + write,
 //     dbeta_t = dR_t . v_t - k_t . (e^gamma_t S dR_t) - sum_s Y_ts k_t . k_s,
-//     dgamma_t = q_t . dQ_t + k_t . read_t - k_t . write_t, at the chunk's last token + e^gamma_C <S, dS_next> + sum_s k_s . carry_s,
-//     dg_t = sum of dgamma from t to the chunk's end   (every pair of tokens on one side of t cancels: both take it from the same X, Y),
+//     dg_t = e^gamma_C <S, dS_next> + sum_{u >= t} near_u + sum_{s < t} k_s . carry_s + sum_{s < t <= u} W_us,
+//         near_u = q_u . (scale e^gamma dO S^T)_u - beta_u k_u . (e^gamma dR S^T)_u,   W_us = X_us q_u . k_s - beta_u Y_us k_u . k_s.
+// (The same dg_t is a sum over all tokens from t on of q . dQ, and so on, in which pairs on one side of t cancel but for roundings.  Of those that t divides,
+// each has the factor e^g_t: where little is let through little is added up, and nothing where nothing is.)
 //     dS = w dS_next - N^T dS_next + Z' (w and N as forward),   Z' = scale (e^gamma Q)^T dO - (beta e^gamma K)^T T^T P^T dO.
 // Three launches, as forward: N^T and Z' of all chunks, the walk from the last chunk to the first, all gradients.
 #include "chela_delta.h"
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
     constexpr bool SHARED = DV * LS <= C * LT;                  // (the states' operands fit where P and T were)
     __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sV[C * LV], sO[C * LV], sU[C * LV], sT[C * LT], sP[C * LT], sS[SHARED ? 8 : 2 * DV * LS];
     __shared__ ChunkSteps<C> st;
-    __shared__ float s_db[NW][C], s_db2[GI][C], s_dg[GI][C], s_kc[NW], s_ss[NW];
+    __shared__ float s_db[NW][C], s_db2[GI][C], s_near[GI][C], s_far[GI][C], s_pairs[NB][C], s_ss[NW];
     E *const sS0 = SHARED ? sP : sS, *const sdS = SHARED ? sT : sS + DV * LS;
     const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6), tw = w % NB, gi = w / NB;
     const int place = blockIdx.x / a.Hk, hk = blockIdx.x - place * a.Hk, share = RUN ? 1 : a.H / a.Hk;
@@ -515,7 +517,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         if (AHEAD && DK == CW && hh + 1 < share) fetch(h + 1, chunk0, ch.row, ch.n, tid, lane);
         if (NEXT && rc > 0) fetch(h, chunk0 + rc - 1, ch.row - C, C, tid, lane);
         // X and beta Y of the wave's tokens as queries, then as keys
-        float dbeta = 0.f, dgamma = 0.f, kc = 0.f;
+        float dbeta = 0.f, near = 0.f, far = 0.f;
         Op<E, 1> xq[KC], yq[KC], xk[KC], yk[KC];
         {
             Op<E, 1> o[VS], r[VS], u[VS];
@@ -523,14 +525,14 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
             for (int ks = 0; ks < VS; ++ks) {
                 o[ks] = rows_op(sO, LV, 16 * tw, 32 * ks, lane);
                 r[ks] = rows_op(sV, LV, 16 * tw, 32 * ks, lane);
-                u[ks] = rows_op(sU, LV, 16 * tw, 32 * ks, lane);
             }
+            f32x4 rest = zero4();                                      // of W, the sums over the keys of the blocks in front, u down the rows, in all columns
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 x[b] = y[b] = zero4();
                 read_afresh();
                 if (b <= tw) {                                         // keys b
-                    f32x4 g = zero4();
+                    f32x4 g = zero4(), p = zero4();
 #pragma unroll
                     for (int ks = 0; ks < VS; ++ks) {
                         const Op<E, 1> m = rows_op(sU, LV, 16 * b, 32 * ks, lane);
@@ -539,7 +541,11 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                     }
                     if (gi == 0)
 #pragma unroll
-                        for (int ks = 0; ks < KS; ++ks) g = mma(rows_op(sK, LK, 16 * b, 32 * ks, lane), rows_op(sK, LK, 16 * tw, 32 * ks, lane), g);
+                        for (int ks = 0; ks < KS; ++ks) {
+                            const Op<E, 1> k = rows_op(sK, LK, 16 * b, 32 * ks, lane);
+                            g = mma(k, rows_op(sK, LK, 16 * tw, 32 * ks, lane), g);
+                            p = mma(k, rows_op(sQ, LK, 16 * tw, 32 * ks, lane), p);
+                        }
                     const f32x4 d = st.decays_from(t, 16 * b + 4 * q);
                     x[b] *= splat4(a.scale) * d;
                     y[b] *= d;
@@ -551,6 +557,21 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                         }
                     dbeta -= dot4(y[b], g);
                     y[b] *= splat4(st.beta[t]);
+                    if (gi == 0) {
+                        // sum of W_us over s < t for the t of the keys' block, by a product with ones below the diagonal; then over the wave's u, u >= t
+                        const f32x4 W = x[b] * p - y[b] * g;
+                        f32x4 v = rest;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v = __builtin_amdgcn_mfma_f32_16x16x4f32(W[j], 4 * q + j < c ? 1.f : 0.f, v, 0, 0, 0);
+                        if (b == tw)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) v[i] = 4 * q + i >= c ? v[i] : 0.f;
+                        else
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) rest = __builtin_amdgcn_mfma_f32_16x16x4f32(W[j], 1.f, rest, 0, 0, 0);
+                        const float sum = column_sum((v[0] + v[1]) + (v[2] + v[3]));
+                        if (q == 0) s_pairs[tw][16 * b + c] = sum;
+                    }
                 }
             }
 #pragma unroll
@@ -558,6 +579,8 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                 xq[ks] = operand<E, 1>(x[2 * ks], x[2 * ks + 1]);
                 yq[ks] = operand<E, 1>(y[2 * ks], y[2 * ks + 1]);
             }
+#pragma unroll
+            for (int ks = 0; ks < VS; ++ks) u[ks] = rows_op(sU, LV, 16 * tw, 32 * ks, lane);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 x[b] = y[b] = zero4();
@@ -611,8 +634,10 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                 xx *= splat4(a.scale * st.up[t]);
                 yy *= splat4(st.up[t]);
                 zz *= splat4(st.down[t]);
-                dbeta -= dot4(yy, k4);
-                kc += dot4(zz, k4);
+                const float read = dot4(yy, k4);
+                dbeta -= read;
+                near += fmaf(-st.beta[t], read, dot4(xx, q4));
+                far += dot4(zz, k4);
                 yy *= splat4(st.beta[t]);
                 f32x4 vv = zero4();
 #pragma unroll
@@ -628,41 +653,41 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                     }
                 }
                 zz -= vv;
-                dgamma += dot4(xx, q4) - dot4(yy + zz, k4);
                 sumQ[DT * half + d] += xx;
                 sumK[DT * half + d] += zz - yy;
             }
         }
         dbeta = column_sum(dbeta);
-        dgamma = column_sum(dgamma);
+        near = column_sum(near);
+        far = column_sum(far);
         if (q == 0) {
             s_db2[gi][t] = dbeta;
-            s_dg[gi][t] = dgamma;
+            s_near[gi][t] = near;
+            s_far[gi][t] = far;
         }
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) kc += __shfl_xor(kc, d);
-        if (lane == 0) s_kc[w] = kc;
         __syncthreads();
         if (tid < 64) {
-            float x = 0.f, b = 0.f, ends = 0.f, sums = 0.f;
+            float b = 0.f, behind = 0.f, front = 0.f, pairs = 0.f, ends = 0.f;
             if (tid < C) {
 #pragma unroll
-                for (int i = 0; i < GI; ++i) { x += s_dg[i][tid]; b += s_db2[i][tid]; }
+                for (int i = 0; i < GI; ++i) { b += s_db2[i][tid]; behind += s_near[i][tid]; front += s_far[i][tid]; }
+#pragma unroll
+                for (int i = 0; i < NB; ++i) pairs += i >= tid / 16 ? s_pairs[i][tid] : 0.f;
 #pragma unroll
                 for (int i = 0; i < NW; ++i) b += s_db[i][tid];
                 if (tid < ch.n) ((E*)a.dbeta)[(size_t)(ch.row + tid) * a.H + h] = from_f<E>(b);
             }
 #pragma unroll
-            for (int i = 0; i < NW; ++i) { ends += s_ss[i]; sums += s_kc[i]; }
-            if (tid == C - 1) x += st.whole * ends + sums;
+            for (int i = 0; i < NW; ++i) ends += s_ss[i];
+            front = __shfl_up(front, 1);                                 // (of the tokens in front, t itself not among them)
+            if (tid == 0) front = 0.f;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
-                const float y1 = __shfl_down(x, d);
-                if (tid + d < 64) x += y1;
+                const float x = __shfl_down(behind, d), y1 = __shfl_up(front, d);
+                if (tid + d < 64) behind += x;
+                if (tid >= d) front += y1;
             }
-            // (nothing is in front of a sequence's first token that it could let decay: its sum is the roundings' rest)
-            const bool none = tid == 0 && rc == 0 && run.index == 0 && a.S_in == nullptr;
-            if (a.g != nullptr && tid < ch.n) ((E*)a.dg)[(size_t)(ch.row + tid) * a.H + h] = from_f<E>(none ? 0.f : x);
+            if (a.g != nullptr && tid < ch.n) ((E*)a.dg)[(size_t)(ch.row + tid) * a.H + h] = from_f<E>(st.whole * ends + behind + front + pairs);
         }
     }
     if (RUN && rc > 0) {
