@@ -465,7 +465,7 @@ size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int
  *          call with the same inputs left it, or NULL: worked out again.  Sums are taken in a fixed order.  dg_t is added up of terms
  *          with the factor e^(g_t) each: as exact relative to what a token lets through as the others are, and zero where it empties the state.
  *   step : one row for each of R requests; S [n_slots, H, dk, dv] is updated in place.
- * Limits beside those above (D: H dk): T H dk / 64 < 2^26, n_seq H dv / 16 and R H dv / 16 < 2^23.  `packed` in the queries: cu is given. */
+ * Limits beside those above (D: H dk): T H dk / 64 < 2^26, n_seq H dv / 16 and R H dv / 16 <= 2^23 - 8.  `packed` in the queries: cu is given. */
 int chela_gated_delta_fwd(const void *Q, long long ldq, const void *K, long long ldk, const void *V, long long ldv,
                           const void *g, long long ldg, const void *beta, long long ldb, float scale,
                           const int *cu, int n_seq, int T, int H, int Hk, int dk, int dv, const float *S_in,

@@ -1611,7 +1611,8 @@ static int delta_check(const DeltaIn& x, const int* cu, int n_seq, int T, const 
     if (x.H < 0 || x.H > (1 << 20) / (x.dk > x.dv ? x.dk : x.dv) || x.Hk < 1 || x.H % x.Hk != 0 || !std::isfinite(x.scale)) return CHELA_ERR_BAD_SHAPE;
     const int rc = rows_of(cu, n_seq, T, x.H * x.dk, slots, n_slots, clear, rows);
     if (rc != CHELA_OK) return rc;
-    if (too_many(T, x.H * x.dk, kRowUnits / 4) || (long long)n_seq * x.H * (x.dv / 16) >= kStateUnits) return CHELA_ERR_BAD_SHAPE;
+    // (the walk takes up to 512 threads to sixteen columns of a state, and eight such workgroups at a time)
+    if (too_many(T, x.H * x.dk, kRowUnits / 4) || ((long long)n_seq * x.H * (x.dv / 16) + 7) / 8 * 8 >= kStateUnits) return CHELA_ERR_BAD_SHAPE;
     return CHELA_OK;
 }
 static void delta_read(const DeltaIn& x, int T, size_t es, Operands* o, DeltaArgs* a)

@@ -293,3 +293,15 @@ def test_binding_refuses_what_it_cannot_hand_on():
         binding.chela_layer_norm_fwd(x)
     with pytest.raises(ValueError):
         binding.chela_layer_norm_bwd(x, x)
+
+
+@pytest.mark.parametrize("form,sfx", FORMS)
+def test_the_walk_of_the_states_stays_below_2_to_the_32_threads(L, form, sfx):
+    # eight workgroups at a time, of 4 dk threads, one for sixteen columns of a state: 2^21 - 1 states of 128 x 64 would be 2^32 threads
+    n, dtype = (1 << 21) - 1, int(sfx == "_f32")
+    for m, ok in ((n - 1, True), (n, False)):
+        got = [L.chela_gated_delta_workspace_bytes(64, m, 1, 1, 128, 64, dtype, b, 0) for b in (0, 1)] + [L.chela_gated_delta_saved_bytes(64, m, 1, 1, 128, 64, dtype)]
+        assert all((x > 0) == ok for x in got)
+    x = (at(0), 128, at(1), 128, at(2), 64, None, 0, at(3), 1, 1.0, at(4), n, 64, 1, 1, 128, 64)
+    assert getattr(L, "chela_gated_delta_fwd" + form + sfx)(*x, None, None, None, n, at(5), None, None) == SHAPE
+    assert getattr(L, "chela_gated_delta_bwd" + form + sfx)(*x, None, at(5), 64, None, None, at(6), at(7), at(8), None, at(9), None, None) == SHAPE
