@@ -75,12 +75,6 @@ __device__ __forceinline__ Op<E, P> operand(f32x4 lo, f32x4 hi)
     }
     return o;
 }
-template <typename E>
-__device__ __forceinline__ Op<E, 1> first_part(const Op<E, 2>& x)
-{
-    if constexpr (sizeof(E) == 4) return Op<E, 1>{x.v};
-    else return Op<E, 1>{x.h};
-}
 
 template <typename E> using Vec4 = typename std::conditional<sizeof(E) == 2, bf16x4, f32x4>::type;
 template <typename E> using Vec8 = typename std::conditional<sizeof(E) == 2, bf16x8, f32x8>::type;
