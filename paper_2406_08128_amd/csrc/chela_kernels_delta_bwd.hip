@@ -137,7 +137,8 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 // ---- the same for a run of chunks, from its last to its first: one N^T and one Z' for all of them.  What a chunk makes of a state's gradient,
 //     dS <- e^gamma dS + scale (e^gamma Q)^T dO - (beta e^gamma K)^T T^T (P^T dO + K~ dS),
 // with Z' beside what is left of the identity (X = M^T - w, as forward, without the terms in dO), thirty-two columns to a wave.  65536 tokens in 4
-// sequences, 12 heads of 64: 134 us, 400 MB at 3.0 TB/s: products in a chain, two waves to a SIMD (150 registers and more).
+// sequences, 12 heads of 64: 140 us, 400 MB at 2.9 TB/s: instruction issue, vector instructions 66 % of the time, matrix 29, with three waves to a SIMD
+// (156 registers; heads of 128 up to 199, two waves).
 template <typename E, int DK, int DV>
 __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(DeltaArgs a)
 {
@@ -331,9 +332,10 @@ __device__ __forceinline__ float column_sum(float x)
 // and a head, from the last chunk to the first with the gradient of the state behind each in registers, sixteen value columns to a wave.  Sixteen value
 // columns to a wave for U and dR; then sixteen tokens, as queries and as keys, and a part of the key columns.  X and Y are worked out twice, by the wave
 // of the query's tokens and by that of the key's: as the operands of its own products they then lie in a wave's registers as they are.
-// 65536 tokens in 4 sequences, 12 heads of 64: 340 us, 900 MB at 2.6 TB/s; 32768 in 8, 12 heads of 64 and 128 with 4 key heads: 298.  Registers bound it:
-// 203 to 247 leave two waves to a SIMD, which wait for LDS and each other half the time (eight barriers to a chunk; vector instructions 45 % of the
-// time, LDS 38, matrix instructions 15).
+// 65536 tokens in 4 sequences, 12 heads of 64: 366 us, 900 MB at 2.5 TB/s; 32768 in 8, 12 heads of 64 and 128 with 4 key heads: 321.  Two waves to a SIMD
+// wait for LDS and each other half the time (six barriers to a chunk, eight with 128 key columns; vector instructions 43 % of the time, LDS 37, matrix
+// instructions 17).  Registers (183 to 256 in bf16) and LDS (76 KB with heads of 64, twice that where there are 128 value columns) each allow two; with 128 key and
+// 64 value columns 92 KB and 256 registers, more of them for accumulators, allow one.  (dg by the pairs that a token divides, of that: 25 and 16.)
 template <typename E, int DK, int DV, bool RUN>
 __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
 {
