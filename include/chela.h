@@ -449,7 +449,8 @@ size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int
  * token's key already.  H value heads, Hk key heads, Hk divides H, value head h has key head h / (H / Hk); dk, dv in {64, 128}:
  *     S' = e^(g_t) S_{t-1},   S_t = S' + beta_t k_t (v_t - S'^T k_t)^T,   o_t = scale S_t^T q_t.
  * Nothing is normalised: keys of length one and beta in [0, 1] keep the state bounded (chela_block_norm_fwd with w_pre = dk^-1/2 makes rows of
- * length one).  A log decay g of -infinity empties the state; one below -256 does the same.
+ * length one).  A log decay g of -infinity empties a state (a finite one: zero times what is not finite is not a number); one
+ *   below -256 does the same.
  *   A g above 0 lets the state grow.  The rows are worked out in pieces (below), and as much as g lets grow within one, the largest e^(sum of g) over
  *   neighbouring rows of it, do the roundings inside count for more than without growth, however long the sequence is; where that is no fp32 number
  *   any more (e^88) outputs are not finite.
