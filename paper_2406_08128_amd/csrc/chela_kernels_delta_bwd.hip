@@ -334,8 +334,8 @@ __device__ __forceinline__ float column_sum(float x)
 // of the query's tokens and by that of the key's: as the operands of its own products they then lie in a wave's registers as they are.
 // 65536 tokens in 4 sequences, 12 heads of 64: 366 us, 900 MB at 2.5 TB/s; 32768 in 8, 12 heads of 64 and 128 with 4 key heads: 321.  Two waves to a SIMD
 // wait for LDS and each other half the time (six barriers to a chunk, eight with 128 key columns; vector instructions 43 % of the time, LDS 37, matrix
-// instructions 17).  Registers (183 to 256 in bf16) and LDS (76 KB with heads of 64, twice that where there are 128 value columns) each allow two; with 128 key and
-// 64 value columns 92 KB and 256 registers, more of them for accumulators, allow one.  (dg by the pairs that a token divides, of that: 25 and 16.)
+// instructions 17).  Registers (181 to 256 in bf16) and LDS (76 KB with heads of 64, twice that where there are 128 value columns) each allow two; with 128 key and
+// 64 value columns 92 KB and 256 registers, more of them for accumulators, allow one.  (dg by the pairs that a token divides, of that, where there are decays: 25 and 16.)
 template <typename E, int DK, int DV, bool RUN>
 __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
 {
@@ -534,7 +534,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                 x[b] = y[b] = zero4();
                 read_afresh();
                 if (b <= tw) {                                         // keys b
-                    f32x4 g = zero4(), p = zero4();
+                    f32x4 g = zero4();
 #pragma unroll
                     for (int ks = 0; ks < VS; ++ks) {
                         const Op<E, 1> m = rows_op(sU, LV, 16 * b, 32 * ks, lane);
@@ -543,11 +543,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                     }
                     if (gi == 0)
 #pragma unroll
-                        for (int ks = 0; ks < KS; ++ks) {
-                            const Op<E, 1> k = rows_op(sK, LK, 16 * b, 32 * ks, lane);
-                            g = mma(k, rows_op(sK, LK, 16 * tw, 32 * ks, lane), g);
-                            p = mma(k, rows_op(sQ, LK, 16 * tw, 32 * ks, lane), p);
-                        }
+                        for (int ks = 0; ks < KS; ++ks) g = mma(rows_op(sK, LK, 16 * b, 32 * ks, lane), rows_op(sK, LK, 16 * tw, 32 * ks, lane), g);
                     const f32x4 d = st.decays_from(t, 16 * b + 4 * q);
                     x[b] *= splat4(a.scale) * d;
                     y[b] *= d;
@@ -559,7 +555,10 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
                         }
                     dbeta -= dot4(y[b], g);
                     y[b] *= splat4(st.beta[t]);
-                    if (gi == 0) {
+                    if (gi == 0 && a.g != nullptr) {
+                        f32x4 p = zero4();
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks) p = mma(rows_op(sK, LK, 16 * b, 32 * ks, lane), rows_op(sQ, LK, 16 * tw, 32 * ks, lane), p);
                         // sum of W_us over s < t for the t of the keys' block, by a product with ones below the diagonal; then over the wave's u, u >= t
                         const f32x4 W = x[b] * p - y[b] * g;
                         f32x4 v = rest;
