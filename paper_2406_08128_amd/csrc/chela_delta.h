@@ -26,10 +26,10 @@ template <typename E> constexpr int kPad = sizeof(E) == 2 ? 16 : 4;
 // registers, summed over its rows.
 // P parts: a value that was worked out in fp32 is rounded to bf16 (P = 1, off by 2^-8 at most) or kept as a sum of two (P = 2, 2^-16).  What the caller
 // gave in bf16 has one part.  fp32 operands have all bits, and their products are fp32: eight instructions over four terms each.
-// Operands that stay in registers have two parts where the result goes into a state, or through the inverse: they cost matrix instructions, of
-// which there are enough.  Those that go through memory (N, T, the states that the outputs are made of) have one, but N, and T where it goes into N, two in
-// calls that take or return states in fp32: with one part each everywhere bf16 outputs are 4.1e-3 to 5.0e-3 off (root mean square, relative, of
-// which 1.7e-3 are their own rounding; one head of 64, 4096 tokens without decay), so 3.0e-3 to 3.7e-3, with N and T in two 2.7e-3 to 3.4e-3.
+// What goes into a state or through the inverse has two parts, and so have the inverse T and the scores P: tokens with keys alike take back most of what
+// the one in front wrote, and with T and P in one part what is left was off by 1e-2 to 8e-2 (64 tokens alike; 1e-2 with keys of positive numbers) where
+// two leave the output's own rounding, 1.7e-3.  One part have the states that outputs and gradients are made of, N in calls without states in fp32, the
+// inner values U, dR and the scores X, Y that only gradients are made of.
 template <typename E, int P> struct Op;
 template <> struct Op<bf16, 1> { bf16x8 h; };
 template <> struct Op<bf16, 2> { bf16x8 h, l; };
@@ -407,11 +407,112 @@ __device__ __forceinline__ void clear_rows(const Rows& r, int block, E* to, int 
     }
 }
 
+// T between LDS and memory.  Its diagonal is ones and nothing is above it: the C (C - 1) / 2 elements below, as words of both parts (the second in the upper
+// half), take what one part of all its elements would.  Pieces of four words, C / 4 to a pair of rows, t behind C - 1 - t, which has as many fours below the
+// diagonal's more as t has fewer; the last piece has the three words that the two rows have in the diagonal's fours.  (fp32: all elements as they are.)
+template <typename E, int C, int NT>
+struct PackedT {
+    static constexpr bool PACK = sizeof(E) == 2;
+    static constexpr int F = C / 4, W = F - 1, ALL = PACK ? C / 2 * F : C * F, M = (ALL + NT - 1) / NT;
+    u32x4 x[M];
+    struct Place { int row, four; };                               // (of the last piece: the lower row's four on the diagonal)
+    static __device__ __forceinline__ Place place(int i)
+    {
+        const int r = i / F, p = i % F, a = r / 4;
+        if constexpr (!PACK) return Place{r, p};
+        return p < W - a ? Place{C - 1 - r, p} : Place{r, p - (W - a)};
+    }
+    __device__ __forceinline__ void fetch(const E* from, int tid)
+    {
+#pragma unroll
+        for (int m = 0; m < M; ++m) x[m] = ((const u32x4*)from)[ALL % NT == 0 ? m * NT + tid : min(m * NT + tid, ALL - 1)];
+    }
+    __device__ __forceinline__ void put(const Planes<E, 2>& T, int tid) const
+    {
+        auto four = [&](int t, int j, u32x4 w) {
+            E* p = T.h + t * T.ld + place_of<E>(4 * j);
+            *(u32x2*)p = u32x2{w[0] & 0xffffu | w[1] << 16, w[2] & 0xffffu | w[3] << 16};
+            *(u32x2*)(p + T.plane) = u32x2{w[0] >> 16 | w[1] & 0xffff0000u, w[2] >> 16 | w[3] & 0xffff0000u};
+        };
+        constexpr unsigned ONE = 0x3f80u;
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const int i = m * NT + tid, r = i / F, b = r % 4;
+            if (ALL % NT != 0 && i >= ALL) break;
+            const Place at = place(i);
+            u32x4 w = x[m];
+            if constexpr (!PACK) {
+                *(u32x4*)(T.h + at.row * T.ld + 4 * at.four) = w;
+            } else {
+                if (i % F == W) {
+                    const int o = 3 - b;                           // words of the upper row
+                    four(C - 1 - r, W - r / 4, u32x4{o > 0 ? w[0] : ONE, o > 1 ? w[1] : o == 1 ? ONE : 0u, o > 2 ? w[2] : o == 2 ? ONE : 0u, o > 2 ? ONE : 0u});
+                    w = u32x4{b > 2 ? w[0] : b > 1 ? w[1] : b > 0 ? w[2] : ONE, b > 2 ? w[1] : b > 1 ? w[2] : b > 0 ? ONE : 0u, b > 2 ? w[2] : b > 1 ? ONE : 0u, b > 2 ? ONE : 0u};
+                }
+                four(at.row, at.four, w);
+            }
+        }
+        // zeros behind the diagonal's fours, where a product reads them: to the end of the 32 columns; four threads to a row
+        if constexpr (PACK)
+            if (NT == 4 * C || tid < 4 * C) {
+                const int t = tid / 4;
+#pragma unroll
+                for (int j = tid % 4 + 1; j < 8; j += 4)
+                    if (t / 4 % 8 + j < 8) four(t, t / 4 + j, u32x4{0, 0, 0, 0});
+            }
+    }
+    // read(row, four): those words
+    template <typename R>
+    static __device__ __forceinline__ void store(const R& read, E* to, int tid)
+    {
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            const int i = m * NT + tid, r = i / F, o = 3 - r % 4;
+            if (ALL % NT != 0 && i >= ALL) break;
+            const Place at = place(i);
+            u32x4 w = read(at.row, at.four);
+            if (PACK && i % F == W) {
+                const u32x4 u = read(C - 1 - r, W - r / 4);
+                w = u32x4{o > 0 ? u[0] : w[0], o > 1 ? u[1] : o > 0 ? w[0] : w[1], o > 2 ? u[2] : o > 1 ? w[0] : o > 0 ? w[1] : w[2], 0u};
+            }
+            ((u32x4*)to)[i] = w;
+        }
+    }
+};
+// ... from its two parts, a plane apart
+template <typename E>
+struct WordsOfPlanes {
+    const Planes<E, 2>& T;
+    __device__ __forceinline__ u32x4 operator()(int t, int j) const
+    {
+        const E* p = T.h + t * T.ld + place_of<E>(4 * j);
+        if constexpr (sizeof(E) == 4) return *(const u32x4*)p;
+        const u32x2 h = *(const u32x2*)p, l = *(const u32x2*)(p + T.plane);
+        return u32x4{h[0] & 0xffffu | l[0] << 16, h[0] >> 16 | l[0] & 0xffff0000u, h[1] & 0xffffu | l[1] << 16, h[1] >> 16 | l[1] & 0xffff0000u};
+    }
+};
+// ... and where it goes nowhere else, as words
+template <typename E>
+struct Words {
+    unsigned* p;
+    int ld;
+    __device__ __forceinline__ void put(int row, int col, float x) const
+    {
+        if constexpr (sizeof(E) == 4) {
+            p[row * ld + col] = __float_as_uint(x);
+        } else {
+            const bf16 h = (bf16)x, l = (bf16)(x - (float)h);
+            p[row * ld + col] = __builtin_bit_cast(unsigned short, h) | (unsigned)__builtin_bit_cast(unsigned short, l) << 16;
+        }
+    }
+    __device__ __forceinline__ u32x4 operator()(int t, int j) const { return *(const u32x4*)(p + t * ld + 4 * j); }
+};
+
 // T = (1 + A)^-1 of a chunk, A_ts = beta_t e^(gamma_t - gamma_s) k_t . k_s below the diagonal, from its keys in LDS; the first 256 threads of a workgroup
 // work, all have to call.  sA: room for C (C + 4) floats, where T may be too.  fp32 throughout: blocks of 16 on the diagonal row by row, in place,
 // those below by products with them.
-template <typename E, int DK, int P, int C>
-__device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSteps<C>& st, float* sA, const Planes<E, P>& T, int tid)
+template <typename E, int DK, int C, typename O>
+__device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSteps<C>& st, float* sA, const O& T, int tid)
 {
     constexpr int NB = C / 16, LA = C + 4;
     const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
@@ -484,12 +585,16 @@ __device__ __forceinline__ void chunk_inverse(const E* sK, int LK, const ChunkSt
     }
     __syncthreads();
 }
-// Room for either, in elements.
-template <typename E, int P> constexpr int inverse_room()
+// Elements behind a row of T where it is worked out (half as many as behind other tiles' rows, so that a fourth workgroup fits in a compute unit), and the
+// room, in elements, for either.
+template <typename E> constexpr int kPadT = sizeof(E) == 2 ? 8 : 4;
+template <typename E> constexpr int inverse_room()
 {
-    constexpr int C = DeltaChunk<E>::C, t = P * C * (C + kPad<E>), a = C * (C + 4) * 4 / sizeof(E);
+    constexpr int C = DeltaChunk<E>::C, t = (sizeof(E) == 2 ? 2 : 1) * C * (C + kPadT<E>), a = C * (C + 4) * 4 / sizeof(E);
     return t > a ? t : a;
 }
+// Elements of a tile of scores or of T, its two parts.
+template <typename E> constexpr int kScores = (sizeof(E) == 2 ? 2 : 1) * DeltaChunk<E>::C * (DeltaChunk<E>::C + kPad<E>);
 
 // RUN(element type, DK, DV) for a call's.
 #define CHELA_DELTA(RUN)                                                                                              \

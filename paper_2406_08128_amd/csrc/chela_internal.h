@@ -282,7 +282,7 @@ hipError_t launch_block_norm_bwd(const BlockNormArgs& a, int dtype, hipStream_t 
 // states are walked by; `chunks` and `places` are how many there may be, and each has room for what the kernels hand to each other, per head.
 struct DeltaPlan {
     int chunk, chunks, run, places;
-    int parts, t_parts;                   // of the operands in memory that a state goes through (1, or 2 in bf16), of T
+    int parts;                            // of the operands in memory that a state goes through (1, or 2 in bf16)
     size_t N, Z, whole, S0, dS, bytes;    // byte offsets into the scratch, and its size.  S0: per run (`own_states`), where the chunks' are not the same
     size_t T, S0c, saved_bytes;           // ... into `saved` (without one: this many bytes of the scratch from `saved_at` on)
     size_t saved_at;
@@ -296,15 +296,15 @@ struct DeltaArgs {
     float *S_out, *dS_in;
     void *O, *dQ, *dK, *dV, *dg, *dbeta;
     float scale;
-    int H, Hk, places, run, t_parts;
+    int H, Hk, places, run;
     void *N, *T, *S0, *S0c, *dS;          // between the kernels, [places][H] of each; T and S0c, the states in front of all chunks (or null), [chunks][H]
     float *Z, *whole;
 };
 constexpr int kDeltaChunkBf16 = 64, kDeltaChunkF32 = 32;
 bool delta_dims_ok(int dk, int dv);
-// is_bwd, has_saved: of the gradient, given `saved` (of the forward: wanting it).  states: of a call with states or their gradients, given or
+// is_bwd, has_saved: of the gradient, given `saved` (of the forward: wanting it).  fine: of a call with states or their gradients, given or
 // wanted.
-DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int Hk, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states);
+DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int Hk, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool fine);
 hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_walk(const DeltaArgs& a, bool reverse, int parts, int dk, int dv, int dtype, hipStream_t st);

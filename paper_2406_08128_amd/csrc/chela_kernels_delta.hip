@@ -20,8 +20,8 @@ namespace chela {
 template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__(256, DK + DV == 128 ? 4 : 2) void delta_prep_kernel(DeltaArgs a)
 {
-    constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
-    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[inverse_room<E, P>()];
+    constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPadT<E>;
+    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[inverse_room<E>()];
     __shared__ ChunkSteps<C> st;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
     const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
@@ -38,17 +38,11 @@ __global__ __launch_bounds__(256, DK + DV == 128 ? 4 : 2) void delta_prep_kernel
         v.put(sV, LV, ch.n, tid);
     }
     __syncthreads();
-    const Planes<E, P> T{sT, LT, C * LT};
+    const Planes<E, 2> T{sT, LT, C * LT};
     chunk_inverse<E, DK>(sK, LK, st, (float*)sT, T, tid);
     const size_t at = (size_t)place * a.H + h;
-    {
-        // T for the kernels behind
-        constexpr int W = 16 / sizeof(E);
-        E* to = (E*)a.T + at * (C * C);
-#pragma unroll
-        for (int i = tid; i < C * (C / W); i += 256) *(u32x4*)(to + i * W) = *(const u32x4*)(sT + i / (C / W) * LT + i % (C / W) * W);
-        if (tid == 0) a.whole[at] = no_growth(st.whole);
-    }
+    PackedT<E, C, 256>::store(WordsOfPlanes<E>{T}, (E*)a.T + at * (C * C), tid);             // for the kernels behind
+    if (tid == 0) a.whole[at] = no_growth(st.whole);
     const float grown = st.whole - no_growth(st.whole);
     // T (beta e^gamma K), T (beta V), thirty-two columns at a time, and what K~ makes of them
 #pragma unroll 1
@@ -68,7 +62,7 @@ __global__ __launch_bounds__(256, DK + DV == 128 ? 4 : 2) void delta_prep_kernel
             const Op<E, 2> x1 = scaled<E, 2>(cols_op(X, ldx, 32 * ks, col + 16, lane), f, 32 * ks, lane);
 #pragma unroll
             for (int b = 2 * ks; b < NB; ++b) {
-                const Op<E, P> m = T.rows(16 * b, 32 * ks, lane);
+                const Op<E, 2> m = T.rows(16 * b, 32 * ks, lane);
                 y[b][0] = mma(m, x0, y[b][0]);
                 y[b][1] = mma(m, x1, y[b][1]);
             }
@@ -111,11 +105,12 @@ __global__ __launch_bounds__(256, DK + DV == 128 ? 4 : 2) void delta_prep_kernel
 
 // ---- T alone, of all chunks, for runs of them (within a run's workgroup it would be one chunk's after the other: (b) 890 for both kernels in one, 820 in
 // two).  (a) 68, 200 MB, where the copy's rate would give 39: the inverse's steps wait for each other; five workgroups to a compute unit.
-template <typename E, int DK, int P>
+template <typename E, int DK>
 __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 {
-    constexpr int C = DeltaChunk<E>::C, LK = DK + kPad<E>, LT = C + kPad<E>, W = 16 / sizeof(E);
-    __shared__ __align__(16) E sK[C * LK], sT[inverse_room<E, P>()];
+    constexpr int C = DeltaChunk<E>::C, LK = DK + kPad<E>;
+    __shared__ __align__(16) E sK[C * LK];
+    __shared__ __align__(16) float sT[C * (C + 4)];
     __shared__ ChunkSteps<C> st;
     const int tid = threadIdx.x, lane = tid & 63;
     const int i = blockIdx.x / a.H, h = blockIdx.x - i * a.H, hk = h / (a.H / a.Hk);
@@ -127,10 +122,9 @@ __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
     put_steps(st, s, ch.n, tid);
     k.put(sK, LK, ch.n, tid);
     __syncthreads();
-    chunk_inverse<E, DK>(sK, LK, st, (float*)sT, Planes<E, P>{sT, LT, C * LT}, tid);
-    E* to = (E*)a.T + ((size_t)i * a.H + h) * (P * C * C);
-#pragma unroll
-    for (int j = tid; j < P * C * (C / W); j += 256) *(u32x4*)(to + j * W) = *(const u32x4*)(sT + j / (C / W) * LT + j % (C / W) * W);
+    const Words<E> T{(unsigned*)sT, C + 4};
+    chunk_inverse<E, DK>(sK, LK, st, sT, T, tid);
+    PackedT<E, C, 256>::store(T, (E*)a.T + ((size_t)i * a.H + h) * (C * C), tid);
 }
 
 // ---- the same for a run of chunks: one N and one Z for all of them, so that the walk has fewer steps and less to read.  The state behind the
@@ -141,11 +135,11 @@ __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 // instruction issue: vector instructions 57 % of the time (values split into two parts, scaled), matrix instructions 34 (340 GFLOP with all
 // parts, 0.72 PFLOP/s); 193 registers, two waves to a SIMD.
 template <typename E, int DK, int DV, int P>
-__global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs a)
+__global__ __launch_bounds__((DK + DV) * 2, DK + DV == 128 ? 3 : 1) void delta_prep_run_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
     constexpr int NT = (DK + DV) * 2;
-    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[P * C * LT];
+    __shared__ __align__(16) E sK[C * LK], sV[C * LV], sT[kScores<E>];
     __shared__ ChunkSteps<C> st;
     const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6);
     const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
@@ -157,17 +151,17 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
     const int col = 32 * (of_k ? w : w - DK / 32);
     Tile<E, C, DK, NT> tk;
     Tile<E, C, DV, NT> tv;
-    Tile<E, P * C, C, NT> tt;
+    PackedT<E, C, NT> tt;
     Steps ts;
     auto fetch = [&](int r, int tid, int lane) {
         const int row = ch.row + r * C, n = min(C, ch.n - r * C);
         ts = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, row, h, n, lane);
         tk.fetch((const E*)a.K + hk * DK, a.ldk, row, n, tid);
         tv.fetch((const E*)a.V + h * DV, a.ldv, row, n, tid);
-        tt.fetch((const E*)a.T + ((size_t)(chunk0 + r) * a.H + h) * (P * C * C), C, 0, P * C, tid);
+        tt.fetch((const E*)a.T + ((size_t)(chunk0 + r) * a.H + h) * (C * C), tid);
     };
     fetch(0, tid0, lane0);
-    const Planes<E, P> T{sT, LT, C * LT};
+    const Planes<E, 2> T{sT, LT, C * LT};
     f32x4 X[DK / 16][2];
 #pragma unroll
     for (int d = 0; d < DK / 16; ++d) X[d][0] = X[d][1] = zero4();
@@ -182,7 +176,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
         put_steps(st, ts, n, tid);
         tk.put(sK, LK, n, tid);
         tv.put(sV, LV, n, tid);
-        tt.template put<true>(sT, LT, P * C, tid);
+        tt.put(T, tid);
         if (!last) fetch(r + 1, tid, lane);
         __syncthreads();
         // beta V - beta e^gamma K Z, or of the transition the same without V
@@ -229,7 +223,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_prep_run_kernel(DeltaArgs
             y[b][0] = y[b][1] = zero4();
 #pragma unroll
             for (int ks = 0; ks <= b / 2; ++ks) {
-                const Op<E, P> m = T.rows(16 * b, 32 * ks, lane);
+                const Op<E, 2> m = T.rows(16 * b, 32 * ks, lane);
                 y[b][0] = mma(m, yo[ks][0], y[b][0]);
                 y[b][1] = mma(m, yo[ks][1], y[b][1]);
             }
@@ -373,7 +367,7 @@ template <typename E, int DK, int DV>
 __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 ? 3 : 2) : 2) void delta_out_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>, NT = DV * 4;
-    __shared__ __align__(16) E sK[C * LK], sQ[C * LK], sV[C * LV], sT[C * LT], sP[C * LT];
+    __shared__ __align__(16) E sK[C * LK], sQ[C * LK], sV[C * LV], sT[kScores<E>];          // (T, then P)
     __shared__ ChunkSteps<C> st;
     const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6);
     const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
@@ -387,7 +381,7 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
     const int chunk0 = chunk_place(a.rows, C, ch, a.run, 0);
     Tile<E, C, DK, NT> tk, tq;
     Tile<E, C, DV, NT> tv;
-    Tile<E, C, C, NT> tt;
+    PackedT<E, C, NT> tt;
     Steps ts;
     auto fetch = [&](int r, int tid, int lane) {
         const int row = ch.row + r * C, n = min(C, ch.n - r * C);
@@ -395,8 +389,9 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
         tk.fetch((const E*)a.K + hk * DK, a.ldk, row, n, tid);
         tq.fetch((const E*)a.Q + hk * DK, a.ldq, row, n, tid);
         tv.fetch((const E*)a.V + h * DV, a.ldv, row, n, tid);
-        tt.fetch((const E*)a.T + ((size_t)(chunk0 + r) * a.H + h) * (a.t_parts * C * C), C, 0, C, tid);
+        tt.fetch((const E*)a.T + ((size_t)(chunk0 + r) * a.H + h) * (C * C), tid);
     };
+    const Planes<E, 2> T{sT, LT, C * LT};
     Op<E, 1> so[KS];
     f32x4 S[DK / 16];
 #pragma unroll
@@ -415,29 +410,13 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
         tk.put(sK, LK, n, tid);
         tq.put(sQ, LK, n, tid);
         tv.put(sV, LV, n, tid);
-        tt.template put<true>(sT, LT, C, tid);
+        tt.put(T, tid);
         if (AHEAD && !last) fetch(r + 1, tid, lane);
         __syncthreads();
         if (a.S0c != nullptr)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
                 store_op<E, 1>((E*)a.S0c + ((size_t)(chunk0 + r) * a.H + h) * (DK * DV) + (w * KS + ks) * 512, so[ks], lane);
-        if (w < NB) {
-            const Planes<E, 1> Pm{sP, LT, 0};
-            const int t = 16 * w + c;
-            for (int sb = 0; sb <= (w | 1); ++sb) {
-                f32x4 x = zero4();
-                if (sb <= w) {
-#pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) x = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sQ, LK, 16 * w, 32 * ks, lane), x);
-                    x *= splat4(a.scale) * st.decays_from(t, 16 * sb + 4 * q);
-                    if (sb == w)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) x[i] = 4 * q + i <= c ? x[i] : 0.f;
-                }
-                Pm.put4(t, 16 * sb, q, x);
-            }
-        }
         Op<E, 2> ro[KC], uo[KC];
         f32x4 x[NB];
 #pragma unroll
@@ -454,10 +433,27 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
         for (int b = 0; b < NB; ++b) {
             x[b] = zero4();
 #pragma unroll
-            for (int ks = 0; ks <= b / 2; ++ks) x[b] = mma(rows_op(sT, LT, 16 * b, 32 * ks, lane), ro[ks], x[b]);
+            for (int ks = 0; ks <= b / 2; ++ks) x[b] = mma(T.rows(16 * b, 32 * ks, lane), ro[ks], x[b]);
         }
 #pragma unroll
         for (int ks = 0; ks < KC; ++ks) uo[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
+        __syncthreads();
+        // the scores, where T was
+        if (w < NB) {
+            const int t = 16 * w + c;
+            for (int sb = 0; sb <= (w | 1); ++sb) {
+                f32x4 p = zero4();
+                if (sb <= w) {
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) p = mma(rows_op(sK, LK, 16 * sb, 32 * ks, lane), rows_op(sQ, LK, 16 * w, 32 * ks, lane), p);
+                    p *= splat4(a.scale) * st.decays_from(t, 16 * sb + 4 * q);
+                    if (sb == w)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) p[i] = 4 * q + i <= c ? p[i] : 0.f;
+                }
+                T.put4(t, 16 * sb, q, p);
+            }
+        }
         __syncthreads();
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -468,7 +464,7 @@ __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 
             for (int ks = 0; ks < KS; ++ks) o = mma(so[ks], rows_op(sQ, LK, 16 * b, 32 * ks, lane), o);
             o *= splat4(a.scale * st.up[t]);
 #pragma unroll
-            for (int ks = 0; ks <= b / 2; ++ks) o = mma(uo[ks], rows_op(sP, LT, 16 * b, 32 * ks, lane), o);
+            for (int ks = 0; ks <= b / 2; ++ks) o = mma(uo[ks], T.rows(16 * b, 32 * ks, lane), o);
             if (t < n)
                 *(Vec4<E>*)((E*)a.O + (size_t)(ch.row + r * C + t) * (a.H * DV) + h * DV + 16 * w + 4 * q) = __builtin_convertvector(o, Vec4<E>);
         }
@@ -581,24 +577,22 @@ static int chunks_to_a_run(long n, int dk, int dv, int dtype)
     return r;
 }
 
-DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int Hk, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool states)
+DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int Hk, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool fine)
 {
     DeltaPlan p{};
     const size_t es = dtype != 0 ? 4 : 2;
-    p.parts = dtype == 0 && states ? 2 : 1;
+    p.parts = dtype == 0 && fine ? 2 : 1;
     p.chunk = dtype != 0 ? kDeltaChunkF32 : kDeltaChunkBf16;
     const int len = n_seq > 0 ? T / n_seq : 0;
     auto places = [&](int tokens) { return T <= 0 || n_seq <= 0 ? 0 : packed ? T / tokens + n_seq : n_seq * ((len + tokens - 1) / tokens); };
     p.run = chunks_to_a_run(((long)len + p.chunk - 1) / p.chunk, dk, dv, dtype);
-    // (T is kept in one part; a gradient walks the runs with a state for one value head)
-    if (((is_bwd || has_saved) && p.parts == 2) || (is_bwd && H != Hk)) p.run = 1;
+    if (is_bwd && H != Hk) p.run = 1;                          // (a gradient walks the runs with a state for one value head)
     p.chunks = places(p.chunk);
     p.places = places(p.chunk * p.run);
     const size_t all = (size_t)p.chunks * H, n = is_bwd && !has_saved ? all : (size_t)p.places * H;      // (the states are then walked chunk by chunk)
     auto room = [](size_t& at, size_t bytes) { const size_t was = at; at += (bytes + 255) & ~(size_t)255; return was; };
-    p.t_parts = is_bwd || has_saved || p.run == 1 ? 1 : p.parts;
     p.own_states = !is_bwd && p.run > 1;
-    p.T = room(p.saved_bytes, all * p.t_parts * p.chunk * p.chunk * es);
+    p.T = room(p.saved_bytes, all * p.chunk * p.chunk * es);
     p.S0c = p.saved_bytes;
     if (is_bwd || has_saved || !p.own_states) room(p.saved_bytes, all * dk * dv * es);
     p.N = room(p.bytes, n * p.parts * dk * dk * es);
@@ -634,8 +628,7 @@ hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, int dk, int dv,
     do {                                                                                                              \
         constexpr int P2 = sizeof(E) == 2 ? 2 : 1;                                                                    \
         if (a.run > 1) {                                                                                              \
-            if (p.parts == 2) hipLaunchKernelGGL((delta_inverse_kernel<E, DK, P2>), chunks, dim3(256), 0, st, a);     \
-            else hipLaunchKernelGGL((delta_inverse_kernel<E, DK, 1>), chunks, dim3(256), 0, st, a);                   \
+            hipLaunchKernelGGL((delta_inverse_kernel<E, DK>), chunks, dim3(256), 0, st, a);                           \
             if (p.parts == 2) hipLaunchKernelGGL((delta_prep_run_kernel<E, DK, DV, P2>), grid, dim3((DK + DV) * 2), 0, st, a); \
             else hipLaunchKernelGGL((delta_prep_run_kernel<E, DK, DV, 1>), grid, dim3((DK + DV) * 2), 0, st, a);       \
         } else {                                                                                                      \
@@ -658,7 +651,6 @@ hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* sav
     if (!kept) saved = ws + p.saved_at;
     a.places = p.places;
     a.run = p.run;
-    a.t_parts = p.t_parts;
     a.N = ws + p.N;
     a.Z = (float*)(ws + p.Z);
     a.whole = (float*)(ws + p.whole);

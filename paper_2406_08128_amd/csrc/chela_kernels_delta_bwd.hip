@@ -20,7 +20,7 @@ template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
-    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sO[C * LV], sT[P == 2 ? inverse_room<E, P>() : C * LT], sP[P * C * LT];
+    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sO[C * LV], sT[kScores<E>];         // (P's transpose, then T)
     __shared__ ChunkSteps<C> st;
     __shared__ __align__(16) float s_qu[C];                        // scale e^gamma
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
@@ -28,26 +28,24 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
     const Chunk ch = chunk_at(a.rows, C, place, lane);
     if (ch.n <= 0) return;
     const size_t at = (size_t)place * a.H + h;
+    PackedT<E, C, 256> m;
     {
         Tile<E, C, DK> y, k;
         Tile<E, C, DV> o;
-        Tile<E, C, C> m;
         const Steps s = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, ch.row, h, ch.n, lane);
         y.fetch((const E*)a.Q + hk * DK, a.ldq, ch.row, ch.n, tid);
         k.fetch((const E*)a.K + hk * DK, a.ldk, ch.row, ch.n, tid);
         o.fetch((const E*)a.dO + h * DV, a.lddo, ch.row, ch.n, tid);
-        if (P == 1) m.fetch((const E*)a.T + at * (C * C), C, 0, C, tid);
+        m.fetch((const E*)a.T + at * (C * C), tid);
         put_steps(st, s, ch.n, tid);
         y.put(sQ, LK, ch.n, tid);
         k.put(sK, LK, ch.n, tid);
         o.put(sO, LV, ch.n, tid);
-        if (P == 1) m.template put<true>(sT, LT, C, tid);
     }
     __syncthreads();
     if (tid == 0) a.whole[at] = no_growth(st.whole);
     const float grown = st.whole - no_growth(st.whole);
-    const Planes<E, P> T{sT, LT, C * LT}, Pt{sP, LT, C * LT};
-    if (P == 2) chunk_inverse<E, DK>(sK, LK, st, (float*)sT, T, tid);       // (what was kept of it has one part)
+    const Planes<E, 2> T{sT, LT, C * LT};
     if (w < NB) {                                                  // P's transpose, sixteen of its rows to a wave
         const int s = 16 * w + c;
         for (int tb = w & ~1; tb < NB; ++tb) {
@@ -60,29 +58,40 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) x[i] = c <= 4 * q + i ? x[i] : 0.f;
             }
-            Pt.put4(s, 16 * tb, q, x);
+            T.put4(s, 16 * tb, q, x);
         }
     }
     if (tid < C) s_qu[tid] = a.scale * st.up[tid];
     __syncthreads();
-#pragma unroll 1
-    for (int p = w; p < (DK + DV) / 16; p += 4) {
+    f32x4 po[DV / 64][NB];                                         // P^T dO of the wave's value columns, sixteen of every 64
+#pragma unroll
+    for (int i = 0; i < DV / 64; ++i) {
+        read_afresh();
+#pragma unroll
+        for (int b = 0; b < NB; ++b) po[i][b] = zero4();
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) {
+            const Op<E, 1> o = cols_op(sO, LV, 32 * ks, 64 * i + 16 * w, lane);
+#pragma unroll
+            for (int b = 0; b <= 2 * ks + 1; ++b) po[i][b] = mma(T.rows(16 * b, 32 * ks, lane), o, po[i][b]);
+        }
+    }
+    __syncthreads();
+    m.put(T, tid);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < (DK + DV) / 64; ++i) {
+        const int p = 4 * i + w;
         read_afresh();
         f32x4 x[NB];
         Op<E, 2> xo[KC];
-        if (p < DV / 16) {
+        if (i < DV / 64) {
             Op<E, 2> qo[KC];
 #pragma unroll
-            for (int b = 0; b < NB; ++b) x[b] = zero4();
-#pragma unroll
             for (int ks = 0; ks < KC; ++ks) {
-                const Op<E, 1> o = cols_op(sO, LV, 32 * ks, 16 * p, lane);
-                qo[ks] = scaled<E, 2>(o, s_qu, 32 * ks, lane);
-#pragma unroll
-                for (int b = 0; b <= 2 * ks + 1; ++b) x[b] = mma(Pt.rows(16 * b, 32 * ks, lane), o, x[b]);
+                qo[ks] = scaled<E, 2>(cols_op(sO, LV, 32 * ks, 16 * p, lane), s_qu, 32 * ks, lane);
+                xo[ks] = operand<E, 2>(po[i < DV / 64 ? i : 0][2 * ks], po[i < DV / 64 ? i : 0][2 * ks + 1]);
             }
-#pragma unroll
-            for (int ks = 0; ks < KC; ++ks) xo[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 x[b] = zero4();
@@ -139,12 +148,12 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 // with Z' beside what is left of the identity (X = M^T - w, as forward, without the terms in dO), thirty-two columns to a wave.  65536 tokens in 4
 // sequences, 12 heads of 64: 140 us, 400 MB at 2.9 TB/s: instruction issue, vector instructions 66 % of the time, matrix 29, with three waves to a SIMD
 // (156 registers; heads of 128 up to 199, two waves).
-template <typename E, int DK, int DV>
+template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(DeltaArgs a)
 {
     constexpr int C = DeltaChunk<E>::C, NB = C / 16, KC = C / 32, KS = DK / 32, LK = DK + kPad<E>, LV = DV + kPad<E>, LT = C + kPad<E>;
     constexpr int NT = (DK + DV) * 2, NW = NT / 64;
-    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sO[C * LV], sT[C * LT], sP[C * LT];
+    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sO[C * LV], sT[kScores<E>];         // (P's transpose, then T)
     __shared__ ChunkSteps<C> st;
     const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6);
     const int place = blockIdx.x / a.H, h = blockIdx.x - place * a.H, hk = h / (a.H / a.Hk);
@@ -156,7 +165,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
     const int col = 32 * (of_k ? w : w - DK / 32);
     Tile<E, C, DK, NT> tq, tk;
     Tile<E, C, DV, NT> to;
-    Tile<E, C, C, NT> tt;
+    PackedT<E, C, NT> tt;
     Steps ts;
     auto fetch = [&](int r, int tid, int lane) {
         const int row = ch.row + r * C, n = min(C, ch.n - r * C);
@@ -164,10 +173,9 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
         tq.fetch((const E*)a.Q + hk * DK, a.ldq, row, n, tid);
         tk.fetch((const E*)a.K + hk * DK, a.ldk, row, n, tid);
         to.fetch((const E*)a.dO + h * DV, a.lddo, row, n, tid);
-        tt.fetch((const E*)a.T + ((size_t)(chunk0 + r) * a.H + h) * (C * C), C, 0, C, tid);
     };
     fetch(n_chunks - 1, tid0, lane0);
-    const Planes<E, 1> T{sT, LT, 0}, Pt{sP, LT, 0};
+    const Planes<E, 2> T{sT, LT, C * LT};
     f32x4 X[DK / 16][2];
 #pragma unroll
     for (int d = 0; d < DK / 16; ++d) X[d][0] = X[d][1] = zero4();
@@ -183,8 +191,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
         tq.put(sQ, LK, n, tid);
         tk.put(sK, LK, n, tid);
         to.put(sO, LV, n, tid);
-        tt.template put<true>(sT, LT, C, tid);
-        if (r > 0) fetch(r - 1, tid, lane);
+        tt.fetch((const E*)a.T + ((size_t)(chunk0 + r) * a.H + h) * (C * C), tid);
         __syncthreads();
         {
             constexpr int GI = NW / NB > 0 ? NW / NB : 1;
@@ -200,7 +207,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
 #pragma unroll
                             for (int i = 0; i < 4; ++i) x[i] = c <= 4 * q + i ? x[i] : 0.f;
                     }
-                    Pt.put4(s, 16 * tb, q, x);
+                    T.put4(s, 16 * tb, q, x);
                 }
         }
         f32x4 y[NB][2];
@@ -236,11 +243,15 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
                 const Op<E, 1> o0 = cols_op(sO, LV, 32 * ks, col, lane), o1 = cols_op(sO, LV, 32 * ks, col + 16, lane);
 #pragma unroll
                 for (int b = 0; b <= 2 * ks + 1; ++b) {
-                    const Op<E, 1> m = Pt.rows(16 * b, 32 * ks, lane);
+                    const Op<E, 2> m = T.rows(16 * b, 32 * ks, lane);
                     y[b][0] = mma(m, o0, y[b][0]);
                     y[b][1] = mma(m, o1, y[b][1]);
                 }
             }
+        __syncthreads();
+        tt.put(T, tid);
+        if (r > 0) fetch(r - 1, tid, lane);
+        __syncthreads();
         Op<E, 2> yo[KC][2];
 #pragma unroll
         for (int ks = 0; ks < KC; ++ks)
@@ -251,7 +262,7 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
             y[b][0] = y[b][1] = zero4();
 #pragma unroll
             for (int ks = b / 2; ks < KC; ++ks) {
-                const Op<E, 1> m = T.cols(32 * ks, 16 * b, lane);
+                const Op<E, 2> m = T.cols(32 * ks, 16 * b, lane);
                 y[b][0] = mma(m, yo[ks][0], y[b][0]);
                 y[b][1] = mma(m, yo[ks][1], y[b][1]);
             }
@@ -308,7 +319,8 @@ __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(Delta
 #pragma unroll
                 for (int j = 0; j < 4; ++j) lo[j] = 4 * q + j == c ? 1.f : 0.f;
                 const Op<E, 1> one = i == 0 ? operand<E, 1>(lo, hi) : operand<E, 1>(hi, lo);
-                store_op<E, 1>((E*)a.N + (at * (DK / 16 * KS) + (n + i) * KS + w) * 512, operand<E, 1>(mma(x0, one, zero4()), mma(x1, one, zero4())), lane0);
+                store_op<E, P>((E*)a.N + (at * (DK / 16 * KS) + (n + i) * KS + w) * kOpElems<E, P>,
+                               operand<E, P>(mma(x0, one, zero4()), mma(x1, one, zero4())), lane0);
             }
         }
     } else {
@@ -344,11 +356,11 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
     // unit's LDS: 3000 tokens, 6 heads of 64, 74 us, with 32 69.  Rows without padding where 160 KB are too few otherwise.)
     constexpr int NW = DV / 16, NT = DV * 4, GI = NW / NB, CW = sizeof(E) == 4 && DV == 64 ? 32 : 64, DT = CW / 16 / GI;
     constexpr int LT = C + kPad<E>, LS = CW + (sizeof(E) == 4 && DK + DV == 256 ? 0 : kPad<E>);
-    constexpr bool SHARED = DV * LS <= C * LT;                  // (the states' operands fit where P and T were)
-    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sV[C * LV], sO[C * LV], sU[C * LV], sT[C * LT], sP[C * LT], sS[SHARED ? 8 : 2 * DV * LS];
+    constexpr bool SHARED = 2 * DV * LS <= kScores<E>;          // (the states' operands fit where P's transpose and then T were)
+    __shared__ __align__(16) E sQ[C * LK], sK[C * LK], sV[C * LV], sO[C * LV], sU[C * LV], sT[kScores<E>], sS[SHARED ? 8 : 2 * DV * LS];
     __shared__ ChunkSteps<C> st;
     __shared__ float s_db[NW][C], s_db2[GI][C], s_near[GI][C], s_far[GI][C], s_pairs[NB][C], s_ss[NW];
-    E *const sS0 = SHARED ? sP : sS, *const sdS = SHARED ? sT : sS + DV * LS;
+    E *const sS0 = SHARED ? sT : sS, *const sdS = sS0 + DV * LS;
     const int tid0 = threadIdx.x, lane0 = tid0 & 63, w = __builtin_amdgcn_readfirstlane(tid0 >> 6), tw = w % NB, gi = w / NB;
     const int place = blockIdx.x / a.Hk, hk = blockIdx.x - place * a.Hk, share = RUN ? 1 : a.H / a.Hk;
     if (place >= a.places) {
@@ -368,7 +380,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
     // 2048 tokens, the gradient 332 us without, 324 with; 16 heads of 64 and 128, 8 of 2048, 415 and 422; of 128 and 128, 1083 and 1105.
     constexpr bool AHEAD = DV == 128, NEXT = RUN && DK + DV == 128 && DK == CW;
     Tile<E, C, DV, NT> tv, to;
-    Tile<E, C, C, NT> tt;
+    PackedT<E, C, NT> tt;
     Steps ts;
     Op<E, 1> so[KS], bo[KS];                                    // the states' operands, of the wave's value columns
     auto fetch = [&](int h, int chunk, int row, int n, int tid, int lane) {
@@ -376,7 +388,6 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         ts = fetch_steps((const E*)a.g, a.ldg, (const E*)a.beta, a.ldb, row, h, n, lane);
         tv.fetch((const E*)a.V + h * DV, a.ldv, row, n, tid);
         to.fetch((const E*)a.dO + h * DV, a.lddo, row, n, tid);
-        tt.fetch((const E*)a.T + at * (C * C), C, 0, C, tid);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             so[ks] = load_op<E, 1>((const E*)a.S0c + at * (DK * DV) + (w * KS + ks) * 512, lane);
@@ -409,7 +420,8 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         ty.put(sQ, LK, ch.n, tid0);
         tk.put(sK, LK, ch.n, tid0);
     }
-    const Planes<E, 1> Pm{sP, LT, 0}, Tm{sT, LT, 0}, Um{sU, LV, 0}, Rm{sV, LV, 0};
+    const Planes<E, 2> Tm{sT, LT, C * LT};
+    const Planes<E, 1> Um{sU, LV, 0}, Rm{sV, LV, 0};
     f32x4 sumQ[DK / CW * DT], sumK[DK / CW * DT];
 #pragma unroll
     for (int d = 0; d < DK / CW * DT; ++d) sumQ[d] = sumK[d] = zero4();
@@ -423,7 +435,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         put_steps(st, ts, ch.n, tid);
         tv.put(sV, LV, ch.n, tid);
         to.put(sO, LV, ch.n, tid);
-        tt.template put<true>(sT, LT, C, tid);
+        tt.fetch((const E*)a.T + ((size_t)(chunk0 + rc) * a.H + h) * (C * C), tid);
         __syncthreads();
         // P's transpose, sixteen of its rows to a wave
         for (int tb = (tw & ~1) + gi; tb < NB; tb += GI) {
@@ -436,7 +448,7 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) x[i] = c <= 4 * q + i ? x[i] : 0.f;
             }
-            Pm.put4(t, 16 * tb, q, x);
+            Tm.put4(t, 16 * tb, q, x);
         }
         // U and dR, sixteen value columns to a wave
         float ss = 0.f;
@@ -464,15 +476,6 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
             y[b] *= *(const f32x4*)(st.down + 16 * b + 4 * q);
         }
 #pragma unroll
-        for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            f32x4 u = zero4();
-#pragma unroll
-            for (int ks = 0; ks <= b / 2; ++ks) u = mma(ro[ks], Tm.rows(16 * b, 32 * ks, lane), u);
-            Um.put4(16 * b + c, 16 * w, q, u);
-        }
-#pragma unroll
         for (int d = 1; d < 64; d *= 2) ss += __shfl_xor(ss, d);
         if (lane == 0) s_ss[w] = ss;
         __syncthreads();                                               // (P is there)
@@ -480,7 +483,19 @@ __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
         for (int ks = 0; ks < KC; ++ks) {
             const Op<E, 1> o = cols_op(sO, LV, 32 * ks, 16 * w, lane);
 #pragma unroll
-            for (int b = 0; b <= 2 * ks + 1; ++b) y[b] = mma(Pm.rows(16 * b, 32 * ks, lane), o, y[b]);
+            for (int b = 0; b <= 2 * ks + 1; ++b) y[b] = mma(Tm.rows(16 * b, 32 * ks, lane), o, y[b]);
+        }
+        __syncthreads();
+        tt.put(Tm, tid);
+        __syncthreads();
+#pragma unroll
+        for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(x[2 * ks], x[2 * ks + 1]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            f32x4 u = zero4();
+#pragma unroll
+            for (int ks = 0; ks <= b / 2; ++ks) u = mma(ro[ks], Tm.rows(16 * b, 32 * ks, lane), u);
+            Um.put4(16 * b + c, 16 * w, q, u);
         }
 #pragma unroll
         for (int ks = 0; ks < KC; ++ks) ro[ks] = operand<E, 2>(y[2 * ks], y[2 * ks + 1]);
@@ -734,7 +749,6 @@ hipError_t launch_delta_bwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* sav
     ProfScope prof(KID_DELTA_BWD, st);
     hipError_t e = hipSuccess;
     if (!has_saved) saved = ws + p.saved_at;
-    a.t_parts = p.t_parts;
     a.N = ws + p.N;
     a.Z = (float*)(ws + p.Z);
     a.whole = (float*)(ws + p.whole);
@@ -752,9 +766,12 @@ hipError_t launch_delta_bwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* sav
         const dim3 grid((unsigned)((size_t)p.places * a.H));
 #define CHELA_RUN(E, DK, DV)                                                                                          \
     do {                                                                                                              \
-        if (p.run > 1) hipLaunchKernelGGL((delta_bwd_prep_run_kernel<E, DK, DV>), grid, dim3((DK + DV) * 2), 0, st, a); \
-        else if (sizeof(E) == 2 && p.parts == 2) hipLaunchKernelGGL((delta_bwd_prep_kernel<E, DK, DV, 3 - sizeof(E) / 2>), grid, dim3(256), 0, st, a); \
-        else hipLaunchKernelGGL((delta_bwd_prep_kernel<E, DK, DV, 1>), grid, dim3(256), 0, st, a);                    \
+        constexpr int P2 = sizeof(E) == 2 ? 2 : 1;                                                                    \
+        const dim3 threads(p.run > 1 ? (DK + DV) * 2 : 256);                                                          \
+        if (p.run > 1 && p.parts == 2) hipLaunchKernelGGL((delta_bwd_prep_run_kernel<E, DK, DV, P2>), grid, threads, 0, st, a); \
+        else if (p.run > 1) hipLaunchKernelGGL((delta_bwd_prep_run_kernel<E, DK, DV, 1>), grid, threads, 0, st, a);    \
+        else if (p.parts == 2) hipLaunchKernelGGL((delta_bwd_prep_kernel<E, DK, DV, P2>), grid, threads, 0, st, a);    \
+        else hipLaunchKernelGGL((delta_bwd_prep_kernel<E, DK, DV, 1>), grid, threads, 0, st, a);                      \
     } while (0)
         CHELA_DELTA(CHELA_RUN)
 #undef CHELA_RUN

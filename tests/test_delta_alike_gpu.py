@@ -1,0 +1,69 @@
+"""The gated delta rule in bf16 where keys are alike: tokens that repeat, keys near one direction, keys of positive numbers as an activation leaves them.
+Each token then takes back most of what the one in front wrote, and what is rounded in a chunk's inverse or its scores does not cancel as the terms do.
+
+Tolerances, before any run.  sigma = 2^-8 / sqrt(3) is the root of the mean of squares of a rounding to bf16 at most.  Outputs and the values' gradients: themselves, the
+states in front of their chunk (handed on in bf16), twice for a gradient, whose state is rounded beside it; inverses and scores have two parts, 2^-16, of which the 64 of a
+row's terms leave 64 2^-16 = 2^-10 even if all are off the same way.  So rows together 2^-8 sqrt(3 / 3) + 2^-10, of their norm.  Where a token's key is the one that all
+others have, an output is one number times the value: errors of its 64 terms are the same in all elements, and one row may be off by three times as much as rows together.
+In calls with decays and without states what a chunk makes of a state (N) has one part.  Of a key k that repeats it is k k^T, elements off by 2^-8 / sqrt(3) k_i k_j, so a state
+k v^T comes out with k_i 2^-8 / sqrt(3) sqrt(sum_j k_j^4) v more or less: 2^-8 / sqrt(dk) of itself (normal keys of length one: sum k^4 = 3 / dk).  It is the same in every chunk,
+and what is not along the keys stays but for the decay: chunk i back counts e^(64 g i)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import delta as R
+from paper_2406_08128_amd import binding
+from test_delta_gpu import BF, f64, gen, unit
+
+pytestmark = pytest.mark.gpu
+
+
+def rows(L, dk, g):
+    return 2.0 ** -8 + 2.0 ** -10 + 2.0 ** -8 / dk ** 0.5 * sum(np.exp(64 * g * i) for i in range(L // 64))
+
+
+def alike(kind, r, L, dk, dv):
+    one, i = unit(r(2, 1, dk)), torch.arange(L, device="cuda") % 2
+    if kind == "token":                                  # the same token over and over
+        k, v = one[:1].expand(L, 1, dk), r(1, 1, dv).expand(L, 1, dv)
+        return k, k, v
+    if kind == "key":
+        k = one[:1].expand(L, 1, dk)
+        return k, k, r(L, 1, dv)
+    if kind == "near":
+        return unit(r(L, 1, dk)), unit(one[:1] + 0.02 * r(L, 1, dk)), r(1, 1, dv) + 0.05 * r(L, 1, dv)
+    if kind == "two":                                    # two tokens in turn
+        return unit(r(L, 1, dk)), one[i], r(2, 1, dv)[i]
+    return unit(r(L, 1, dk).abs()), unit(r(L, 1, dk).abs()), r(L, 1, dv)
+
+
+KINDS = ["token", "key", "near", "two", "positive"]
+SIZES = [(64, 64, 200), (64, 128, 130), (128, 64, 90), (128, 128, 200), (64, 64, 1100), (128, 128, 700)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("beta,g", [(1.0, -0.01), (0.9, 0.0), (0.5, -0.05)])
+@pytest.mark.parametrize("dk,dv,L", SIZES)
+def test_keys_that_are_alike(dk, dv, L, beta, g, kind):
+    r = gen(L + dk)
+    q, k, v = (t.contiguous().to(BF) for t in alike(kind, r, L, dk, dv))
+    x = (q, k, v, torch.full((L, 1), g, device="cuda").to(BF), torch.full((L, 1), beta, device="cuda").to(BF), r(L, 1, dv).to(BF))
+    a = [f64(t)[:, 0] for t in x]
+    O, S = R.delta_fwd(*a[:5])
+    ref = R.delta_bwd(*a[:5], a[5])
+    S_out = torch.empty(1, 1, dk, dv, device="cuda")
+    tol = rows(L, dk, g)
+    for out, kept in ((None, False), (S_out, False), (None, True)):
+        got, saved = binding.chela_gated_delta_fwd(*x[:5], S_out=out, want_saved=kept)
+        off = np.linalg.norm(f64(got)[:, 0] - O, axis=1)
+        size = np.linalg.norm(O, axis=1)
+        assert np.linalg.norm(off) <= tol * np.linalg.norm(size), ("O", out is None, kept, np.linalg.norm(off) / np.linalg.norm(size))
+        worst = (off / np.maximum(size, np.sqrt((size ** 2).mean()))).max()
+        assert worst <= 3 * tol, ("row of O", out is None, kept, worst)
+    for s in (saved, None):
+        dV = f64(binding.chela_gated_delta_bwd(*x, saved=s)[2])[:, 0]
+        off, size = np.linalg.norm(dV - ref["dV"]), np.linalg.norm(ref["dV"])
+        assert off <= tol * size, ("dV", s is None, off / size)
+    off, size = np.linalg.norm(f64(S_out)[0, 0] - S), np.linalg.norm(S)
+    assert off <= 64 * 2.0 ** -16 * size, ("S_out", off / size)
