@@ -457,9 +457,9 @@ size_t chela_selscan_workspace_bytes(int T, int D, int N, int G, int is_bwd, int
  *   Q, K [T, Hk, dk], V, O [T, H, dv], g (NULL: no decay), beta [T, H] in the I/O type, with row strides; states [n_slots, H, dk, dv] fp32; scale
  *   is a finite constant.  Rows are taken 64 (bf16) or 32 (fp32) of a sequence at a time: what is not finite in one reaches the rows in front of
  *   it in the same 64 or 32 too, and never another sequence.  bf16: states that a call takes or returns, their gradients and everything that goes into them
- *   are held to 16 bits or more, and so are the inverses and the scores that outputs are made of (keys that are alike would leave few digits otherwise).
- *   The other matrix operands (states in front of 64 rows, inner values, a gradient's scores, in calls without states what a chunk makes of one) are
- *   rounded to bf16, their sums are fp32.
+ *   are held to 16 bits or more, and so are the inverses and the scores that outputs are made of (keys that are alike would leave few digits otherwise) and,
+ *   without g, what a chunk makes of a state.  The other matrix operands (states in front of 64 rows, inner values, a gradient's scores, with g and
+ *   without states what a chunk makes of a state) are rounded to bf16, their sums are fp32.
  *   fwd  : O.  saved: NULL, or a caller-owned buffer of chela_gated_delta_saved_bytes() bytes (16-byte aligned, opaque) that carries what the
  *          backward call needs of the chunks (states and inverses).
  *   bwd  : dQ, dK [T, Hk, dk] (sums over a key head's value heads), dV [T, H, dv], dg (NULL without g), dbeta [T, H] in the I/O type, dS_in

@@ -1637,7 +1637,7 @@ static int delta_fwd_common(const DeltaIn& x, const int* cu, int n_seq, int T, c
     if (rc != CHELA_OK) return rc;
     if (x.H == 0 || (T == 0 && n_seq == 0)) return CHELA_OK;
     const size_t es = esize(dtype), st = (size_t)n_slots * x.H * x.dk * x.dv * 4;
-    const DeltaPlan p = make_delta_plan(T, n_seq, cu != nullptr, x.H, x.Hk, x.dk, x.dv, kind(dtype), false, saved != nullptr, S_in || S_out);
+    const DeltaPlan p = make_delta_plan(T, n_seq, cu != nullptr, x.H, x.Hk, x.dk, x.dv, kind(dtype), false, saved != nullptr, S_in || S_out || !x.g);
     Operands o;
     delta_read(x, T, es, &o, &a);
     if (S_in) o.read_under(S_in, st);
@@ -1661,7 +1661,7 @@ static int delta_bwd_common(const DeltaIn& x, const int* cu, int n_seq, int T, c
     if (x.H == 0 || (T == 0 && n_seq == 0)) return CHELA_OK;
     const size_t es = esize(dtype), st = (size_t)n_seq * x.H * x.dk * x.dv * 4;
     const size_t qk = (size_t)T * x.Hk * x.dk * es, v = (size_t)T * x.H * x.dv * es, one = (size_t)T * x.H * es;
-    const DeltaPlan p = make_delta_plan(T, n_seq, cu != nullptr, x.H, x.Hk, x.dk, x.dv, kind(dtype), true, saved != nullptr, S_in || dS_out || dS_in);
+    const DeltaPlan p = make_delta_plan(T, n_seq, cu != nullptr, x.H, x.Hk, x.dk, x.dv, kind(dtype), true, saved != nullptr, S_in || dS_out || dS_in || !x.g);
     Operands o;
     delta_read(x, T, es, &o, &a);
     o.read_if(S_in, st);
@@ -1715,7 +1715,7 @@ size_t chela_gated_delta_saved_bytes(int T, int n_seq, int packed, int H, int dk
 size_t chela_gated_delta_workspace_bytes(int T, int n_seq, int packed, int H, int dk, int dv, int dtype, int is_bwd, int has_saved)
 {
     if (!delta_sizes_ok(T, n_seq, packed, H, dk, dv)) return 0;
-    size_t most = 0;                                          // (of calls with states and without, of key heads shared and not)
+    size_t most = 0;                                          // (of calls with states or without decays and others, of key heads shared and not)
     for (int k = 0; k < 4; ++k) {
         const size_t n = make_delta_plan(T, n_seq, packed != 0, H, k & 1 ? H : 0, dk, dv, kind(dtype), is_bwd != 0, has_saved != 0, (k & 2) != 0).bytes;
         if (n > most) most = n;

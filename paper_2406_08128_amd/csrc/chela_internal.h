@@ -302,8 +302,8 @@ struct DeltaArgs {
 };
 constexpr int kDeltaChunkBf16 = 64, kDeltaChunkF32 = 32;
 bool delta_dims_ok(int dk, int dv);
-// is_bwd, has_saved: of the gradient, given `saved` (of the forward: wanting it).  fine: of a call with states or their gradients, given or
-// wanted.
+// is_bwd, has_saved: of the gradient, given `saved` (of the forward: wanting it).  fine: of a call with states or their gradients, given or wanted, or
+// without decays (where nothing that is rounded fades).
 DeltaPlan make_delta_plan(int T, int n_seq, bool packed, int H, int Hk, int dk, int dv, int dtype, bool is_bwd, bool has_saved, bool fine);
 hipError_t launch_delta_fwd(DeltaArgs a, const DeltaPlan& p, char* ws, char* saved, int dk, int dv, int dtype, hipStream_t st);
 hipError_t launch_delta_states(DeltaArgs& a, const DeltaPlan& p, int dk, int dv, int dtype, hipStream_t st);

@@ -67,3 +67,39 @@ def test_keys_that_are_alike(dk, dv, L, beta, g, kind):
         assert off <= tol * size, ("dV", s is None, off / size)
     off, size = np.linalg.norm(f64(S_out)[0, 0] - S), np.linalg.norm(S)
     assert off <= 64 * 2.0 ** -16 * size, ("S_out", off / size)
+
+
+def _size_of_state_gradients(q, k, beta, dO):
+    """The norm of all of them, those behind every token."""
+    G, sizes = np.zeros((q.shape[1], dO.shape[1])), 0.0
+    for t in range(len(k) - 1, -1, -1):
+        sizes += (G ** 2).sum()
+        G = G + np.outer(q[t], dO[t])
+        G = G - np.outer(k[t], beta[t] * (k[t] @ G))
+    return sizes ** 0.5
+
+
+@pytest.mark.parametrize("kind", ["token", "two", "positive"])
+@pytest.mark.parametrize("share", [1, 2])
+@pytest.mark.parametrize("d,L", [(64, 8200), (128, 4100)])
+def test_without_decays_nothing_that_is_rounded_adds_up(d, L, share, kind):
+    # g None: what a chunk makes of a state has two parts, though no states are given or wanted; of 2^-16 the chunks' errors add up to a few 2^-10.  The
+    # gradient G of a state, which products read rounded to bf16, keeps all that queries put into it beside the keys there are: read at a key that is 2^-8 / sqrt(3) |G| / sqrt(dk)
+    # off (independent errors, k_j^2 about 1 / dk), however little of G lies along the key; beta of that is what the value's gradient is off by.
+    r = gen(L)
+    q, k, v = (t.contiguous().to(BF) for t in alike(kind, r, L, d, d))
+    v = v.expand(L, share, d).contiguous()
+    x = (q, k, v, None, torch.full((L, share), 0.9, device="cuda").to(BF))
+    dO = r(L, 1, d).expand(L, share, d).contiguous().to(BF)
+    a = [f64(t)[:, 0] if t is not None else None for t in x]
+    O, ref = R.delta_fwd(*a)[0], R.delta_bwd(*a, f64(dO)[:, 0])
+    tol = 2.0 ** -8 + 2.0 ** -10 + 2.0 ** -16 / d ** 0.5 * (L // 64)
+    for kept in (False, True):
+        got, saved = binding.chela_gated_delta_fwd(*x, want_saved=kept)
+        off = np.linalg.norm(f64(got)[:, 0] - O) / np.linalg.norm(O)
+        assert off <= tol, ("O", kept, off)
+    tol += 0.9 * 2.0 ** -8 / (3 * d) ** 0.5 * _size_of_state_gradients(*a[:2], a[4], f64(dO)[:, 0]) / np.linalg.norm(ref["dV"])
+    for s in (saved, None):
+        dV = f64(binding.chela_gated_delta_bwd(*x, dO, saved=s)[2])
+        off = np.linalg.norm(dV[:, -1] - ref["dV"]) / np.linalg.norm(ref["dV"])
+        assert off <= tol, ("dV", s is None, off)
