@@ -104,7 +104,8 @@ __global__ __launch_bounds__(256, DK + DV == 128 ? 4 : 2) void delta_prep_kernel
 }
 
 // ---- T alone, of all chunks, for runs of them (within a run's workgroup it would be one chunk's after the other: (b) 890 for both kernels in one, 820 in
-// two).  (a) 68, 200 MB, where the copy's rate would give 39: the inverse's steps wait for each other; five workgroups to a compute unit.
+// two).  (a) 71, 200 MB, where the copy's rate would give 39: the inverse's steps wait for each other; five workgroups to a compute unit.  (T goes through LDS as
+// words of both parts: as two planes, which only products need, 75.)
 template <typename E, int DK>
 __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 {
@@ -131,9 +132,10 @@ __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 // run's first chunks is taken through the next as the walk does it, Z beside what is left of the identity (X = M - w, M the transition so far,
 // w = e^(sum of all log decays so far), held to 1), thirty-two columns to a wave:
 //     U = T (beta V - beta e^gamma K Z),   or of X's columns  -T beta e^gamma K (X + w);   X <- e^gamma X + K~^T U + e^gamma w - w_next.
-// (K is what the caller gave and has one part, T K of the chunk alone would have two: 119 and 574 so.)  (a) 97, 400 MB at 4.1 TB/s; (b) 465,
-// instruction issue: vector instructions 57 % of the time (values split into two parts, scaled), matrix instructions 34 (340 GFLOP with all
-// parts, 0.72 PFLOP/s); 193 registers, two waves to a SIMD.
+// (K is what the caller gave and has one part, T K of the chunk alone would have two: 119 and 574 so.)  (a) 107, 400 MB at 3.7 TB/s; (b) 426,
+// instruction issue: vector instructions 56 % of the time (values split into two parts, scaled), matrix instructions 34 (340 GFLOP with all
+// parts, 0.8 PFLOP/s); 187 registers, two waves to a SIMD.  Heads of 64 and 64 are held to three waves (77 and 31 % of the time): 114 us, with two 117; where there are
+// 128 value columns that spills.
 template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__((DK + DV) * 2, DK + DV == 128 ? 3 : 1) void delta_prep_run_kernel(DeltaArgs a)
 {
@@ -361,8 +363,9 @@ __global__ __launch_bounds__(DK * 4) void delta_walk_kernel(DeltaArgs a, int DV)
 }
 
 // ---- the outputs
-// Sixteen value columns to a wave; a run's chunks one after the other, the state from chunk to chunk in the wave's registers.  (a) 130, 600 MB at
-// 4.6 TB/s, the states for the gradient among them; (b) 318, 1.0 GB at 3.1: vector instructions 55 % of the time, matrix instructions 31.
+// Sixteen value columns to a wave; a run's chunks one after the other, the state from chunk to chunk in the wave's registers.  (a) 136, 600 MB at
+// 4.4 TB/s, the states for the gradient among them; (b) 316, 1.2 GB at 3.9: vector instructions 57 % of the time, matrix instructions 32, LDS 50.  The scores
+// are worked out behind the inner values, where T was: with room of their own for both parts two workgroups would fit in a compute unit, not three.
 template <typename E, int DK, int DV>
 __global__ __launch_bounds__(DV * 4, sizeof(E) == 2 ? (DV == 128 ? 4 : DK == 64 ? 3 : 2) : 2) void delta_out_kernel(DeltaArgs a)
 {

@@ -15,7 +15,8 @@
 
 namespace chela {
 
-// ---- a chunk's N^T and Z'.  32768 tokens in 8 sequences, 12 heads of 64 and 128 (4 key heads): 111 us, 440 MB at 4.0 TB/s.
+// ---- a chunk's N^T and Z'.  32768 tokens in 8 sequences, 12 heads of 64 and 128 (4 key heads): 120 us, 440 MB at 3.7 TB/s.
+// P's transpose and T are in the same place one after the other, P^T dO in registers meanwhile.
 template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 {
@@ -146,8 +147,8 @@ __global__ __launch_bounds__(256, 2) void delta_bwd_prep_kernel(DeltaArgs a)
 // ---- the same for a run of chunks, from its last to its first: one N^T and one Z' for all of them.  What a chunk makes of a state's gradient,
 //     dS <- e^gamma dS + scale (e^gamma Q)^T dO - (beta e^gamma K)^T T^T (P^T dO + K~ dS),
 // with Z' beside what is left of the identity (X = M^T - w, as forward, without the terms in dO), thirty-two columns to a wave.  65536 tokens in 4
-// sequences, 12 heads of 64: 140 us, 400 MB at 2.9 TB/s: instruction issue, vector instructions 66 % of the time, matrix 29, with three waves to a SIMD
-// (156 registers; heads of 128 up to 199, two waves).
+// sequences, 12 heads of 64: 149 us, 400 MB at 2.7 TB/s: instruction issue, vector instructions 70 % of the time, matrix 30, with three waves to a SIMD
+// (154 registers; heads of 128 up to 197, two waves).
 template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__((DK + DV) * 2) void delta_bwd_prep_run_kernel(DeltaArgs a)
 {
@@ -344,10 +345,11 @@ __device__ __forceinline__ float column_sum(float x)
 // and a head, from the last chunk to the first with the gradient of the state behind each in registers, sixteen value columns to a wave.  Sixteen value
 // columns to a wave for U and dR; then sixteen tokens, as queries and as keys, and a part of the key columns.  X and Y are worked out twice, by the wave
 // of the query's tokens and by that of the key's: as the operands of its own products they then lie in a wave's registers as they are.
-// 65536 tokens in 4 sequences, 12 heads of 64: 366 us, 900 MB at 2.5 TB/s; 32768 in 8, 12 heads of 64 and 128 with 4 key heads: 321.  Two waves to a SIMD
-// wait for LDS and each other half the time (six barriers to a chunk, eight with 128 key columns; vector instructions 43 % of the time, LDS 37, matrix
-// instructions 17).  Registers (181 to 256 in bf16) and LDS (76 KB with heads of 64, twice that where there are 128 value columns) each allow two; with 128 key and
-// 64 value columns 92 KB and 256 registers, more of them for accumulators, allow one.  (dg by the pairs that a token divides, of that, where there are decays: 25 and 16.)
+// 65536 tokens in 4 sequences, 12 heads of 64: 377 us, 900 MB at 2.4 TB/s; 32768 in 8, 12 heads of 64 and 128 with 4 key heads: 316.  Two waves to a SIMD
+// wait for LDS and each other half the time (eight barriers to a chunk, ten with 128 key columns; vector instructions 45 % of the time, LDS 40, matrix
+// instructions 18).  Registers (199 to 256 in bf16) and LDS (76 KB with heads of 64, twice that where there are 128 value columns) each allow two; with 128 key and
+// 64 value columns 92 KB and 256 registers, more of them for accumulators, allow one.  (dg by the pairs that a token divides, of that, where there are decays: 25 and 16;
+// both parts of P and T 20 and 10.)
 template <typename E, int DK, int DV, bool RUN>
 __global__ __launch_bounds__(DV * 4, 2) void delta_grad_kernel(DeltaArgs a)
 {
