@@ -134,8 +134,8 @@ __global__ __launch_bounds__(256, 4) void delta_inverse_kernel(DeltaArgs a)
 //     U = T (beta V - beta e^gamma K Z),   or of X's columns  -T beta e^gamma K (X + w);   X <- e^gamma X + K~^T U + e^gamma w - w_next.
 // (K is what the caller gave and has one part, T K of the chunk alone would have two: 119 and 574 so.)  (a) 107, 400 MB at 3.7 TB/s; (b) 426,
 // instruction issue: vector instructions 56 % of the time (values split into two parts, scaled), matrix instructions 34 (340 GFLOP with all
-// parts, 0.8 PFLOP/s); 187 registers, two waves to a SIMD.  Heads of 64 and 64 are held to three waves (77 and 31 % of the time): 114 us, with two 117; where there are
-// 128 value columns that spills.
+// parts, 0.8 PFLOP/s); 187 registers, two waves to a SIMD.  For heads of 64 and 64 three waves are asked for (vector 77 %, matrix 31): the compiler finds three without
+// that too, and 5 % more time; where there are 128 value columns it spills for them.
 template <typename E, int DK, int DV, int P>
 __global__ __launch_bounds__((DK + DV) * 2, DK + DV == 128 ? 3 : 1) void delta_prep_run_kernel(DeltaArgs a)
 {
